@@ -59,6 +59,7 @@ extern "C" {
 #define PG_EINDEX     (-8)  /* reported by pg_rollout_status(): a gather index was out of range */
 #define PG_ECAPACITY  (-7)  /* request larger than a fixed built-in buffer (pg_score_static) */
 #define PG_EDEVICE    (-9)  /* the handle was created on another device than the current one  */
+#define PG_ENOPAGES  (-10)  /* reported by pg_kv_status(): no free page, or a row's table is full */
 
 #define PG_VEL_F32  0
 #define PG_VEL_BF16 1
@@ -447,6 +448,159 @@ int pg_survivor_logp(pg_rollout *h, const int32_t *rows, const float *logp_packe
                      void *stream);
 int pg_gather_rows(pg_rollout *h, const int32_t *rows, int32_t n_out, int32_t n_in, const void *src,
                    void *dst, size_t row_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Token rollouts: Expand-and-Prune over a paged key-value cache.
+ *
+ * The same method on an autoregressive policy (no counterpart in the paper, whose trajectories are
+ * latents): a trajectory is a row of tokens, its state is the keys and values of those tokens.  The
+ * cache is a pool of pages of page_size tokens; a row is a list of page numbers and a length.  The
+ * expansion of a prompt to N trajectories shares the prompt's full pages (pg_kv_fork), a prune keeps
+ * the survivors' rows and frees the pages of the others (pg_kv_fork with pg_prune_ovf's src_rows),
+ * rows grow by pg_kv_extend / pg_kv_append, pg_kv_attend reads the cache for one new token per row,
+ * pg_logits_process applies the sampling rules to the logits.
+ *
+ * All calls are stateless: the caller owns the pool, the table, the lengths, the reference counts
+ * and the workspace, and passes them by a descriptor (HOST memory, read during the call only).
+ * Indices that come from device memory (page numbers, row numbers, lengths, token ids) are checked
+ * in the kernels: a bad one is never dereferenced, bit 2 of *status is set and pg_kv_status returns
+ * PG_EINDEX.  Running out of pages or of table entries sets bit 3 (PG_ENOPAGES).  `status` (nullable)
+ * is a device int32 that the caller zeroes once and that calls only OR into.  Results do not depend on
+ * the order in which the GPU runs its blocks.
+ * ------------------------------------------------------------------------------------------ */
+#define PG_F32  0   /* element types of the token calls; the first two have PG_VEL_*'s values */
+#define PG_BF16 1
+#define PG_F16  2
+
+/*
+ * A paged key-value cache.  Token t of row r lies in page table[r * max_pages + t / page_size], slot
+ * t % page_size; its key for head h of layer l starts at element
+ *     l * layer_stride + page * page_stride + (h * page_size + slot) * head_dim      of k, same for v.
+ */
+typedef struct {
+  void *k, *v;             /* pools, 16-byte aligned                                          */
+  int32_t dtype;           /* PG_F32, PG_BF16 or PG_F16: of the pools, queries, new tokens and outputs */
+  int32_t n_layers, n_pages, n_kv_heads, page_size;
+  int32_t head_dim;        /* a multiple of 8, 8..256                                          */
+  int64_t page_stride;     /* elements, >= n_kv_heads * page_size * head_dim, a multiple of 8    */
+  int64_t layer_stride;    /* elements, a multiple of 8 (>= n_pages * page_stride, or any where the
+                              pages of the layers are interleaved without overlapping)             */
+  int32_t *table;          /* [n_rows, max_pages] int32; entries past a row's last page are not read */
+  const int32_t *len;      /* [n_rows] int32: tokens of each row, 0..max_pages * page_size          */
+  int32_t n_rows, max_pages;
+} pg_kv;
+
+/*
+ * Attention of one new token per row: for query head j of row r (its key-value head is
+ * j / (n_q_heads / n_kv_heads)), over the len[r] tokens of the row,
+ *     out[r][j] = sum_t softmax_t(scale * q[r][j] . k_t) v_t,   lse[r][j] = ln sum_t exp(scale * q[r][j] . k_t).
+ * A row of length 0 gives zeros and lse = -inf.  Sums and softmax statistics in fp32, out rounded
+ * once to the cache's type.
+ *   q, out [n_rows, n_q_heads, head_dim], rows q_stride / out_stride elements apart (0: contiguous)
+ *   k_new, v_new (both or neither) [n_rows, n_kv_heads, head_dim], rows new_stride apart, 16-byte
+ *     aligned: token len[r]-1 of every row is taken from them and stored into its page (the append of
+ *     a decoding step, without a call of its own)
+ *   lse (nullable) [n_rows, n_q_heads] fp32
+ *   group, shared: rows come in groups of `group` (group-major, as everywhere in this library), and the
+ *     first shared[g] tokens (device int32 [n_rows / group]; NULL: none) of all rows of group g lie in
+ *     the same pages - the state after an expansion.  Those pages are read through the table row of
+ *     the group's first row, once for the whole group.
+ *   workspace: at least pg_kv_attend_workspace_bytes(kv, n_q_heads, group) bytes of device memory,
+ *     16-byte aligned, zeroed once before its first use; every call leaves its counters zero again.
+ *     Two calls that can overlap on the GPU need a workspace each.
+ */
+size_t pg_kv_attend_workspace_bytes(const pg_kv *kv, int32_t n_q_heads, int32_t group);
+int pg_kv_attend(const pg_kv *kv, int32_t layer, int32_t n_q_heads, const void *q, int64_t q_stride,
+                 const void *k_new, const void *v_new, int64_t new_stride, float scale, int32_t group,
+                 const int32_t *shared, void *out, int64_t out_stride, float *lse, void *workspace,
+                 size_t workspace_bytes, int32_t *status, void *stream);
+
+/*
+ * Room for new tokens: len_out[r] = len[r] + n_new[r] (n_new device [n_rows] int32, or NULL: n_uniform
+ * for every row), and for every page that a row starts to use the lowest free page (refs == 0), in row
+ * order, is entered in the table and gets refs_out = 1.  A row whose table is too short, and every row
+ * from the one on that finds no free page, keeps its length (status bit 3).  refs, refs_out [n_pages]
+ * int32 and len, len_out may be the same arrays.  The kv's table is written.
+ */
+int pg_kv_extend(const pg_kv *kv, const int32_t *n_new, int32_t n_uniform, int32_t *len_out,
+                 const int32_t *refs, int32_t *refs_out, int32_t *status, void *stream);
+
+/*
+ * Writes the keys and values of new tokens of one layer into the pages.  Row r's tokens are
+ * k_new[start[r] .. start[r+1]) (start device [n_rows + 1] int32, ascending; NULL: one token per row,
+ * n_tokens = n_rows) and become its last ones, i.e. the call follows pg_kv_extend with the kv's len
+ * pointing at len_out.  k_new, v_new [n_tokens, n_kv_heads, head_dim], tokens new_stride elements
+ * apart (0: contiguous), 16-byte aligned.  A row that was not extended for lack of pages must be given
+ * no tokens.
+ */
+int pg_kv_append(const pg_kv *kv, int32_t layer, int32_t n_tokens, const void *k_new, const void *v_new,
+                 int64_t new_stride, const int32_t *start, int32_t *status, void *stream);
+
+/*
+ * Forks, drops and reorders rows (expansion, prune, release): new row i is a fork of old row
+ * src_rows[i] (device [n_out] int32, any order, -1 = an empty row); old rows that no entry names are
+ * dropped, their pages freed when nobody else refers to them.  Full pages are shared (reference counts);
+ * a partly filled last page stays with the first of its row's forks, every other fork gets the lowest
+ * free pages, in row order, with the page copied in all layers.  src_rows as pg_prune_ovf writes it
+ * compacts a cache to the survivors without moving a page; n_out = 0 releases all rows.
+ *   table_out [n_out, max_pages] (entries past a row's last page become -1), len_out [n_out]: not
+ *   overlapping the kv's; refs, refs_out [n_pages]: may be the same array.  A fork that finds no free
+ *   page is shortened to its full pages (status bit 3).
+ *   workspace: pg_kv_fork_workspace_bytes(kv, n_out) bytes, 16-byte aligned, zeroed once before its
+ *   first use.
+ */
+size_t pg_kv_fork_workspace_bytes(const pg_kv *kv, int32_t n_out);
+int pg_kv_fork(const pg_kv *kv, int32_t n_out, const int32_t *src_rows, int32_t *table_out,
+               int32_t *len_out, const int32_t *refs, int32_t *refs_out, void *workspace,
+               size_t workspace_bytes, int32_t *status, void *stream);
+
+/*
+ * Packs the pool: with n_live pages in use (refs > 0), every page in use at n_live or above moves, in
+ * order, into the free pages below n_live (all layers), and the table and counts follow; afterwards
+ * pages [0, n_live) are in use and the rest is free.  No page is both read and written.  table_out
+ * [n_rows, max_pages] may be the kv's table (entries past a row's last page become -1), refs_out may be
+ * refs.  Other holders of page numbers (forks kept outside this table) must be remapped by the caller: page_map
+ * (nullable, [n_pages] int32) receives the new number of every page in use, -1 for free ones.
+ * workspace as above, pg_kv_pack_workspace_bytes(kv).
+ */
+size_t pg_kv_pack_workspace_bytes(const pg_kv *kv);
+int pg_kv_pack(const pg_kv *kv, const int32_t *refs, int32_t *refs_out, int32_t *table_out,
+               int32_t *page_map, void *workspace, size_t workspace_bytes, int32_t *status, void *stream);
+
+/* Synchronises `stream` and reports a status word of the calls above: PG_EINDEX (bit 2) or PG_ENOPAGES
+ * (bit 3), in that order of precedence, else PG_OK. */
+int pg_kv_status(const int32_t *status, void *stream);
+
+/*
+ * Sampling rules on logits.  For token v of row r, with c = its count among the generated tokens
+ * tokens[r][n_prompt[r] .. n_tokens[r]) and `seen` = it occurs in tokens[r][0 .. n_tokens[r]):
+ *     x = logits[r][v];   seen: x = x > 0 ? x / repetition[r] : x * repetition[r]
+ *     x = x - (frequency[r] * c + presence[r] * (c > 0));   x = x + bias(r, v);   x = x / temperature[r]
+ *     out[r][v] = mask bit v of row r set ? x : -inf
+ * in fp32, rounded once to out_dtype.  Every array is optional (NULL: the rule is not applied).
+ */
+typedef struct {
+  const int32_t *tokens;      /* [n_rows] histories, token_stride int32 apart; ids outside [0, vocab) are
+                                 skipped (padding)                                                      */
+  int64_t token_stride;
+  int32_t max_tokens;         /* most tokens of any row, <= PG_LOGITS_MAX_TOKENS; larger n_tokens count as it */
+  const int32_t *n_tokens;    /* [n_rows]; NULL: max_tokens for every row                               */
+  const int32_t *n_prompt;    /* [n_rows]; NULL: 0 (all tokens were generated)                          */
+  const float *repetition, *presence, *frequency, *temperature;   /* [n_rows] fp32; repetition, temperature > 0 */
+  const int32_t *bias_ids;    /* [n_rows, n_bias] token ids; outside [0, vocab): unused.  Of entries with
+                                 the same id the last one counts                                         */
+  const float *bias_values;   /* [n_rows, n_bias]                                                       */
+  int32_t n_bias;             /* <= PG_LOGITS_MAX_BIAS                                                   */
+  const uint32_t *mask;       /* [n_rows] bit rows, mask_stride words apart: bit v % 32 of word v / 32   */
+  int64_t mask_stride;        /* >= ceil(vocab / 32), or 0: one row of bits for all rows                 */
+} pg_logits_rules;
+#define PG_LOGITS_MAX_TOKENS 1048575
+#define PG_LOGITS_MAX_BIAS   2046
+
+/* logits, out: [n_rows, vocab] of the given types, rows logits_stride / out_stride elements apart (0: contiguous),
+ * aligned to their element; out may be logits when type and stride agree (no other overlap). */
+int pg_logits_process(int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t logits_stride,
+                      int32_t out_dtype, void *out, int64_t out_stride, const pg_logits_rules *rules, void *stream);
 
 /*
  * Diagnostic (the paper has no counterpart): exercises the library's bounded device-side wait.

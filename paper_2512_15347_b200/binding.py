@@ -16,7 +16,10 @@ LIB_PATH = os.path.join(_HERE, "libprogrpo.so")
 
 OK, EINVAL, ESTATE, ECUDA, ENONFINITE, ETIMEOUT, ENOMEM, ECAPACITY, EINDEX, EDEVICE = 0, -1, -2, -3, -4, -5, -6, -7, -8, -9
 STATIC_MAX_ROWS, STATIC_MAX_PARTIALS = 8192, 65536
+ENOPAGES = -10
 VEL_F32, VEL_BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2              # element types of the token calls
+LOGITS_MAX_TOKENS, LOGITS_MAX_BIAS = 1048575, 2046
 MAX_GROUP = 1024
 
 
@@ -51,6 +54,24 @@ class RolloutOutputs(ctypes.Structure):
 
 class PreviewCoef(ctypes.Structure):
     _fields_ = [("p_x", ctypes.c_double), ("p_v", ctypes.c_double)]
+
+
+class Kv(ctypes.Structure):
+    """Descriptor of a paged key-value cache (``make_kv``)."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_stride", ctypes.c_int64),
+                ("layer_stride", ctypes.c_int64), ("table", ctypes.c_void_p), ("len", ctypes.c_void_p),
+                ("n_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
+class LogitsRules(ctypes.Structure):
+    """Sampling rules (``make_logits_rules``)."""
+    _fields_ = [("tokens", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("max_tokens", ctypes.c_int32),
+                ("n_tokens", ctypes.c_void_p), ("n_prompt", ctypes.c_void_p), ("repetition", ctypes.c_void_p),
+                ("presence", ctypes.c_void_p), ("frequency", ctypes.c_void_p), ("temperature", ctypes.c_void_p),
+                ("bias_ids", ctypes.c_void_p), ("bias_values", ctypes.c_void_p), ("n_bias", ctypes.c_int32),
+                ("mask", ctypes.c_void_p), ("mask_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -106,6 +127,24 @@ def lib() -> ctypes.CDLL:
     L.pg_gather_rows.argtypes = [vp, vp, i32, i32, vp, vp, sz, vp]
     L.pg_philox_raw.argtypes = [i64, vp, vp, vp, vp]
     L.pg_normal_rows.argtypes = [u64, i32, i32, i32, i32, vp, vp, vp]
+    pkv = ctypes.POINTER(Kv)
+    L.pg_kv_attend_workspace_bytes.argtypes = [pkv, i32, i32]
+    L.pg_kv_attend_workspace_bytes.restype = sz
+    L.pg_kv_attend.argtypes = [pkv, i32, i32, vp, i64, vp, vp, i64, ctypes.c_float, i32, vp, vp, i64, vp, vp, sz,
+                               vp, vp]
+    L.pg_kv_extend.argtypes = [pkv, vp, i32, vp, vp, vp, vp, vp]
+    L.pg_kv_append.argtypes = [pkv, i32, i32, vp, vp, i64, vp, vp, vp]
+    L.pg_kv_fork_workspace_bytes.argtypes = [pkv, i32]
+    L.pg_kv_fork_workspace_bytes.restype = sz
+    L.pg_kv_fork.argtypes = [pkv, i32, vp, vp, vp, vp, vp, vp, sz, vp, vp]
+    L.pg_kv_pack_workspace_bytes.argtypes = [pkv]
+    L.pg_kv_pack_workspace_bytes.restype = sz
+    L.pg_kv_pack.argtypes = [pkv, vp, vp, vp, vp, vp, sz, vp, vp]
+    L.pg_kv_status.argtypes = [vp, vp]
+    L.pg_logits_process.argtypes = [i32, i32, i32, vp, i64, i32, vp, i64, ctypes.POINTER(LogitsRules), vp]
+    for name in ("pg_kv_attend", "pg_kv_extend", "pg_kv_append", "pg_kv_fork", "pg_kv_pack", "pg_kv_status",
+                 "pg_logits_process"):
+        getattr(L, name).restype = ctypes.c_int
     L.pg_strerror.argtypes = [ctypes.c_int]
     L.pg_strerror.restype = ctypes.c_char_p
     L.pg_last_cuda_error.restype = ctypes.c_int
@@ -387,6 +426,182 @@ def rollout_run(h: int, args: "RunArgs", x0, final_rewards, workspace, stream=No
                                 _p(workspace), workspace.numel() * workspace.element_size(),
                                 ctypes.byref(args.out), _stream(stream)), "pg_rollout_run")
     return args.out
+
+
+# ---------------------------------------------------------------- token rollouts
+
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _want(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _i32(t, what: str, n: Optional[int] = None) -> Optional[int]:
+    """Address of a contiguous int32 tensor (of n elements)."""
+    if t is None:
+        return None
+    _want(t.dtype == torch.int32 and t.is_contiguous(), f"{what}: a contiguous int32 tensor")
+    _want(n is None or t.numel() == n, f"{what}: {n} elements")
+    return t.data_ptr()
+
+
+def make_kv(k, v, table, length) -> Kv:
+    """Descriptor of a paged cache over caller-owned tensors: k, v [layers, pages, kv heads, page size,
+    head dim] (or without the layers), each page contiguous, the page and layer strides free; table
+    [rows, max pages] and length [rows] int32.  Keeps references to all four."""
+    if k.dim() == 4:
+        k, v = k[None], v[None]
+    _want(k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and
+          k.dtype in _DTYPES, "k and v: alike, [layers, pages, kv heads, page size, head dim], fp32, bf16 or fp16")
+    n_layers, n_pages, heads, page, dim = k.shape
+    _want(k.stride()[2:] == (page * dim, dim, 1) or k[0, 0].is_contiguous(), "the elements of a page must be contiguous")
+    _want(table.dim() == 2 and length.numel() == table.shape[0], "table [rows, max pages], length [rows]")
+    c = Kv(k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], n_layers, n_pages, heads, page, dim,
+           k.stride(1) if n_pages > 1 else heads * page * dim, k.stride(0) if n_layers > 1 else 0,
+           _i32(table, "table"), _i32(length, "length"), table.shape[0], table.shape[1])
+    c._keepalive = (k, v, table, length)
+    c._ref = ctypes.byref(c)
+    return c
+
+
+def _rows_of(t, kv: Kv, heads: int, what: str, rows: int) -> int:
+    """Row stride of [rows, heads, head dim] whose rows are contiguous inside."""
+    _want(t.shape == (rows, heads, kv.head_dim) and _DTYPES.get(t.dtype) == kv.dtype, f"{what}: [rows, heads, head dim] of the cache's type")
+    s = t.stride()
+    _want(s[2] == 1 and (s[1] == kv.head_dim or heads == 1) and (s[0] >= heads * kv.head_dim or rows <= 1),
+          f"{what}: contiguous inside a row, rows apart")
+    return s[0] if rows > 1 else 0
+
+
+def kv_attend_workspace_bytes(kv: Kv, n_q_heads: int, group: int = 1) -> int:
+    return int(lib().pg_kv_attend_workspace_bytes(kv._ref, n_q_heads, group))
+
+
+def kv_attend(kv: Kv, layer: int, q, out, workspace, *, k_new=None, v_new=None, lse=None,
+              scale: Optional[float] = None, group: int = 1, shared=None, status=None, stream=None) -> None:
+    """Attention of one new token per row over the cache (see pg_kv_attend).  q, out [rows, query heads,
+    head dim]; with k_new / v_new the rows' last token is stored on the way; scale defaults to
+    head_dim ** -0.5."""
+    rows, heads = kv.n_rows, q.shape[1]
+    q_stride, out_stride, new_stride = _rows_of(q, kv, heads, "q", rows), _rows_of(out, kv, heads, "out", rows), 0
+    if k_new is not None:
+        new_stride = _rows_of(k_new, kv, kv.n_kv_heads, "k_new", rows)
+        _want(v_new is not None and new_stride == _rows_of(v_new, kv, kv.n_kv_heads, "v_new", rows), "k_new and v_new alike")
+    if lse is not None:
+        _want(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == rows * heads, "lse: [rows, query heads] fp32")
+    _check(lib().pg_kv_attend(kv._ref, layer, heads, q.data_ptr(), q_stride, None if k_new is None else k_new.data_ptr(),
+                              None if v_new is None else v_new.data_ptr(), new_stride,
+                              kv.head_dim ** -0.5 if scale is None else scale, group,
+                              _i32(shared, "shared", rows // max(group, 1)), out.data_ptr(), out_stride,
+                              None if lse is None else lse.data_ptr(), _p(workspace),
+                              workspace.numel() * workspace.element_size(), _i32(status, "status"), _stream(stream)),
+           "pg_kv_attend")
+
+
+def kv_extend(kv: Kv, n_new, len_out, refs, refs_out, status=None, stream=None) -> None:
+    """Room for n_new more tokens (an int for all rows, or int32 [rows]): lengths, pages, counts."""
+    one = isinstance(n_new, int)
+    _check(lib().pg_kv_extend(kv._ref, None if one else _i32(n_new, "n_new", kv.n_rows), n_new if one else 0,
+                              _i32(len_out, "len_out", kv.n_rows), _i32(refs, "refs", kv.n_pages),
+                              _i32(refs_out, "refs_out", kv.n_pages), _i32(status, "status"), _stream(stream)), "pg_kv_extend")
+
+
+def kv_append(kv: Kv, layer: int, k_new, v_new, start=None, status=None, stream=None) -> None:
+    """Keys and values [tokens, kv heads, head dim] of the rows' last tokens into one layer's pages;
+    start [rows + 1] int32 says whose they are (None: one token per row)."""
+    n = k_new.shape[0]
+    stride = _rows_of(k_new, kv, kv.n_kv_heads, "k_new", n)
+    _want(stride == _rows_of(v_new, kv, kv.n_kv_heads, "v_new", n), "k_new and v_new alike")
+    _check(lib().pg_kv_append(kv._ref, layer, n, k_new.data_ptr(), v_new.data_ptr(), stride,
+                              _i32(start, "start", kv.n_rows + 1), _i32(status, "status"), _stream(stream)), "pg_kv_append")
+
+
+def kv_fork_workspace_bytes(kv: Kv, n_out: int) -> int:
+    return int(lib().pg_kv_fork_workspace_bytes(kv._ref, n_out))
+
+
+def kv_fork(kv: Kv, src_rows, table_out, len_out, refs, refs_out, workspace, status=None, stream=None) -> None:
+    """New row i becomes a fork of old row src_rows[i]; rows without a fork give up their pages."""
+    n = 0 if src_rows is None else src_rows.numel()
+    _check(lib().pg_kv_fork(kv._ref, n, _i32(src_rows, "src_rows"), _i32(table_out, "table_out", n * kv.max_pages),
+                            _i32(len_out, "len_out", n), _i32(refs, "refs", kv.n_pages), _i32(refs_out, "refs_out", kv.n_pages),
+                            _p(workspace), workspace.numel() * workspace.element_size(), _i32(status, "status"),
+                            _stream(stream)), "pg_kv_fork")
+
+
+def kv_pack_workspace_bytes(kv: Kv) -> int:
+    return int(lib().pg_kv_pack_workspace_bytes(kv._ref))
+
+
+def kv_pack(kv: Kv, refs, refs_out, table_out, workspace, page_map=None, status=None, stream=None) -> None:
+    """Moves the pages in use to the front of the pool; the table and the counts follow."""
+    _check(lib().pg_kv_pack(kv._ref, _i32(refs, "refs", kv.n_pages), _i32(refs_out, "refs_out", kv.n_pages),
+                            _i32(table_out, "table_out", kv.n_rows * kv.max_pages), _i32(page_map, "page_map", kv.n_pages),
+                            _p(workspace), workspace.numel() * workspace.element_size(), _i32(status, "status"),
+                            _stream(stream)), "pg_kv_pack")
+
+
+def kv_status(status, stream=None) -> None:
+    """Raises PgError (EINDEX, ENOPAGES) if a call has flagged the status word; synchronises the stream."""
+    _check(lib().pg_kv_status(_i32(status, "status"), _stream(stream)), "pg_kv_status")
+
+
+def make_logits_rules(*, tokens=None, n_tokens=None, n_prompt=None, repetition=None, presence=None, frequency=None,
+                      temperature=None, bias_ids=None, bias_values=None, mask=None) -> LogitsRules:
+    """Rules for ``logits_process`` over caller-owned tensors (see pg_logits_rules): tokens [rows, most
+    tokens] int32 (the rows may be strided), n_tokens / n_prompt [rows] int32, the penalties and the
+    temperature [rows] fp32, bias_ids / bias_values [rows, n], mask [rows or 1, >= vocab / 32] int32."""
+    r = LogitsRules()
+    rows = None
+
+    def see(t, what):
+        nonlocal rows
+        _want(rows is None or rows == t.shape[0], f"{what}: one entry per row")
+        rows = t.shape[0]
+
+    if tokens is not None:
+        _want(tokens.dim() == 2 and tokens.dtype == torch.int32 and (tokens.stride(1) == 1 or tokens.shape[1] <= 1),
+              "tokens: [rows, most tokens] int32")
+        see(tokens, "tokens")
+        r.tokens, r.token_stride, r.max_tokens = tokens.data_ptr(), tokens.stride(0), tokens.shape[1]
+    for name, t in (("n_tokens", n_tokens), ("n_prompt", n_prompt)):
+        if t is not None:
+            see(t, name)
+            setattr(r, name, _i32(t, name))
+    for name, t in (("repetition", repetition), ("presence", presence), ("frequency", frequency), ("temperature", temperature)):
+        if t is not None:
+            _want(t.dtype == torch.float32 and t.dim() == 1 and t.is_contiguous(), f"{name}: [rows] fp32")
+            see(t, name)
+            setattr(r, name, t.data_ptr())
+    if bias_ids is not None and bias_ids.shape[1] > 0:
+        _want(bias_values is not None and bias_values.shape == bias_ids.shape and bias_values.dtype == torch.float32 and
+              bias_values.is_contiguous(), "bias_values: fp32, shaped like bias_ids")
+        see(bias_ids, "bias_ids")
+        r.bias_ids, r.bias_values, r.n_bias = _i32(bias_ids, "bias_ids"), bias_values.data_ptr(), bias_ids.shape[1]
+    if mask is not None:
+        _want(mask.dim() == 2 and mask.dtype == torch.int32 and (mask.stride(1) == 1 or mask.shape[1] == 1), "mask: [rows or 1, words] int32")
+        if mask.shape[0] > 1:
+            see(mask, "mask")
+        r.mask, r.mask_stride = mask.data_ptr(), mask.stride(0) if mask.shape[0] > 1 else 0
+    r._rows, r._mask_words = rows, None if mask is None else mask.shape[1]
+    r._keepalive = (tokens, n_tokens, n_prompt, repetition, presence, frequency, temperature, bias_ids, bias_values, mask)
+    r._ref = ctypes.byref(r)
+    return r
+
+
+def logits_process(logits, out, rules: LogitsRules, stream=None) -> None:
+    """Applies the rules to logits [rows, vocab] (rows may be strided) into out (may be logits)."""
+    rows, vocab = logits.shape
+    _want(logits.dtype in _DTYPES and out.dtype in _DTYPES and out.shape == logits.shape, "logits and out: [rows, vocab], fp32, bf16 or fp16")
+    _want((logits.stride(1) == 1 and out.stride(1) == 1) or vocab == 1, "logits and out: contiguous rows")
+    _want(rows <= 1 or (logits.stride(0) >= vocab and out.stride(0) >= vocab), "logits and out: rows apart")
+    _want(rules._rows in (None, rows), "the rules are for another number of rows")
+    _want(rules._mask_words is None or rules._mask_words * 32 >= vocab, "mask: too few words for the vocabulary")
+    _check(lib().pg_logits_process(rows, vocab, _DTYPES[logits.dtype], logits.data_ptr(), logits.stride(0) if rows > 1 else 0,
+                                   _DTYPES[out.dtype], out.data_ptr(), out.stride(0) if rows > 1 else 0, rules._ref,
+                                   _stream(stream)), "pg_logits_process")
 
 
 def strerror(code: int) -> str:

@@ -1,0 +1,89 @@
+// Shared pieces of the token-rollout calls: the cache descriptor as the kernels see it, its
+// argument checks, element conversions.
+#pragma once
+
+#include "pg_common.cuh"
+
+#include <cuda_fp16.h>
+
+namespace pg {
+
+constexpr int kStatusIndex = 4;     // status bit 2: an index from device memory was out of range
+constexpr int kStatusPages = 8;     // status bit 3: no free page, or a row's table is full
+
+// One layer of the cache, by value in the kernel parameters.  Strides in elements.
+struct KvView {
+  void *k, *v;
+  int64_t page_stride, layer_stride;
+  int32_t* table;
+  const int32_t* len;
+  int32_t* status;
+  int n_layers, n_pages, n_kv_heads, page_size, head_dim, n_rows, max_pages;
+};
+
+// Checks that need no device access.  The product of all sizes must stay addressable in 63 bits.
+inline int kv_check(const pg_kv* c) {
+  if (!c) return PG_EINVAL;
+  if (c->dtype != PG_F32 && c->dtype != PG_BF16 && c->dtype != PG_F16) return PG_EINVAL;
+  if (c->n_layers < 1 || c->n_pages < 1 || c->n_kv_heads < 1 || c->page_size < 1) return PG_EINVAL;
+  if (c->head_dim < 8 || c->head_dim > 256 || (c->head_dim & 7)) return PG_EINVAL;
+  if (c->n_rows < 0 || c->max_pages < 1) return PG_EINVAL;
+  if ((int64_t)c->max_pages * c->page_size > 0x7FFFFFFFLL - 4096) return PG_EINVAL;
+  const int64_t head = (int64_t)c->page_size * c->head_dim;
+  if (head > ((int64_t)1 << 40) / c->n_kv_heads) return PG_EINVAL;
+  if (c->page_stride < head * c->n_kv_heads || (c->page_stride & 7)) return PG_EINVAL;
+  if (c->page_stride > ((int64_t)1 << 60) / c->n_pages) return PG_EINVAL;
+  if (c->layer_stride < 0 || (c->layer_stride & 7)) return PG_EINVAL;
+  if (c->n_layers > 1 && (c->layer_stride < head * c->n_kv_heads ||
+                          c->layer_stride > ((int64_t)1 << 60) / c->n_layers)) return PG_EINVAL;
+  if (!c->k || !c->v || (((uintptr_t)c->k | (uintptr_t)c->v) & 15)) return PG_EINVAL;
+  if (c->n_rows > 0 && (!c->table || !c->len)) return PG_EINVAL;
+  return PG_OK;
+}
+
+inline KvView kv_view(const pg_kv* c, int32_t* status) {
+  KvView v;
+  v.k = c->k;
+  v.v = c->v;
+  v.page_stride = c->page_stride;
+  v.layer_stride = c->n_layers > 1 ? c->layer_stride : 0;
+  v.table = c->table;
+  v.len = c->len;
+  v.status = status;
+  v.n_layers = c->n_layers;
+  v.n_pages = c->n_pages;
+  v.n_kv_heads = c->n_kv_heads;
+  v.page_size = c->page_size;
+  v.head_dim = c->head_dim;
+  v.n_rows = c->n_rows;
+  v.max_pages = c->max_pages;
+  return v;
+}
+
+inline size_t dtype_bytes(int dtype) { return dtype == PG_F32 ? 4 : 2; }
+
+#ifdef __CUDACC__
+__device__ __forceinline__ void flag(int32_t* status, int bit) {
+  if (status) atomicOr(status, bit);
+}
+
+// Tokens of a row, kept inside what its table can hold.
+__device__ __forceinline__ int row_len(const KvView& kv, int row) {
+  const int n = kv.len[row], most = kv.max_pages * kv.page_size;
+  if ((unsigned int)n > (unsigned int)most) {
+    flag(kv.status, kStatusIndex);
+    return n < 0 ? 0 : most;
+  }
+  return n;
+}
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+#endif
+
+}  // namespace pg

@@ -1,0 +1,548 @@
+// Pages of the key-value cache: forking, dropping and reordering rows (pg_kv_fork), packing the pool
+// (pg_kv_pack), room for new tokens (pg_kv_extend) and writing them (pg_kv_append).
+//
+// A page's count is the number of rows that refer to it.  Counts move by integer atomics, whose result
+// does not depend on their order, and free pages are always taken lowest first through a scan of the
+// counts, so that tables, counts and pools come out the same on every run.
+#include "pg_kv.cuh"
+
+#include <algorithm>
+
+namespace pg {
+
+// ---------------------------------------------------------------- scans in one CTA
+constexpr int kScanThreads = 1024;
+
+// Exclusive prefix sum over the CTA; *total gets the sum.  All threads call.
+__device__ __forceinline__ int block_scan(int v, int* total) {
+  __shared__ int warp_sums[kScanThreads / 32 + 1];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();                       // the previous call's readers are done
+  if (lane == 31) warp_sums[warp] = x;
+  __syncthreads();
+  if (warp == 0) {
+    int s = lane < (int)(blockDim.x >> 5) ? warp_sums[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xFFFFFFFFu, s, o);
+      if (lane >= o) s += y;
+    }
+    warp_sums[lane] = s;
+  }
+  __syncthreads();
+  *total = warp_sums[(blockDim.x >> 5) - 1];
+  return x - v + (warp ? warp_sums[warp - 1] : 0);
+}
+
+// Hands the free pages (refs == 0), lowest first, to take(k, page) for k < wanted; returns how many
+// there were (at most wanted).  One CTA.
+template <typename Take>
+__device__ __forceinline__ int take_free(const int32_t* refs, int n_pages, int wanted, Take take) {
+  int found = 0;
+  for (int base = 0; base < n_pages && found < wanted; base += kScanThreads * 4) {
+    const int p = base + threadIdx.x * 4;
+    bool free[4];
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      free[i] = p + i < n_pages && __ldcg(&refs[p + i]) == 0;
+      mine += free[i];
+    }
+    int total;
+    int k = found + block_scan(mine, &total);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (free[i]) {
+        if (k < wanted) take(k, p + i);
+        ++k;
+      }
+    found += total;
+  }
+  __syncthreads();
+  return min(found, wanted);
+}
+
+// ---------------------------------------------------------------- copies of whole pages
+// Pairs (from, to) in device memory, their number too.  A page of one layer and one of k / v is
+// contiguous but for its stride: kv heads * page_size * head_dim elements.
+struct CopyParams {
+  KvView kv;
+  const int2* pairs;
+  const int32_t* n_pairs;
+  int64_t page_words, stride_words, layer_words;   // 16-byte words
+  int pieces;                                       // CTA-sized pieces of a page
+};
+constexpr int kCopyThreads = 256;
+constexpr int kCopyWords = kCopyThreads * 8;        // 32 KB a piece
+
+__global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_constant__ CopyParams p) {
+  const int64_t per_pair = (int64_t)p.pieces * p.kv.n_layers * 2;
+  const int64_t items = *p.n_pairs * per_pair;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int64_t pair = item / per_pair;
+    int rest = (int)(item - pair * per_pair);
+    const int piece = rest % p.pieces;
+    rest /= p.pieces;
+    const int2 move = p.pairs[pair];
+    uint4* pool = (uint4*)((rest & 1) ? p.kv.v : p.kv.k) + (rest >> 1) * p.layer_words + (int64_t)piece * kCopyWords;
+    const uint4* from = pool + move.x * p.stride_words;
+    uint4* to = pool + move.y * p.stride_words;
+    const int n = (int)min((int64_t)kCopyWords, p.page_words - (int64_t)piece * kCopyWords);
+    uint4 w[kCopyWords / kCopyThreads];
+#pragma unroll
+    for (int i = 0; i < kCopyWords / kCopyThreads; ++i) {
+      const int at = threadIdx.x + i * kCopyThreads;
+      if (at < n) w[i] = __ldcs(from + at);
+    }
+#pragma unroll
+    for (int i = 0; i < kCopyWords / kCopyThreads; ++i) {
+      const int at = threadIdx.x + i * kCopyThreads;
+      if (at < n) __stcs(to + at, w[i]);
+    }
+  }
+}
+
+static int launch_copy(const pg_kv* kv, const KvView& view, const int2* pairs, const int32_t* n_pairs, int64_t most,
+                       cudaStream_t st) {
+  const int64_t b = (int64_t)dtype_bytes(kv->dtype);
+  CopyParams p;
+  p.kv = view;
+  p.pairs = pairs;
+  p.n_pairs = n_pairs;
+  p.page_words = (int64_t)kv->n_kv_heads * kv->page_size * kv->head_dim * b / 16;
+  p.stride_words = kv->page_stride * b / 16;
+  p.layer_words = view.layer_stride * b / 16;
+  const int64_t pieces = (p.page_words + kCopyWords - 1) / kCopyWords;
+  if (pieces * kv->n_layers * 2 > 0x7FFFFFFFLL) return PG_EINVAL;
+  p.pieces = (int)pieces;
+  const int64_t items = most * pieces * kv->n_layers * 2;
+  copy_pages_kernel<<<(unsigned)std::min<int64_t>(std::max<int64_t>(items, 1), 148 * 8), kCopyThreads, 0, st>>>(p);
+  PG_LAUNCH_CHECK();
+  return PG_OK;
+}
+
+// ---------------------------------------------------------------- fork
+
+struct ForkWork {            // in the caller's workspace
+  int32_t* n_pairs;          // copies to make
+  int32_t* need;             // [n_out] 1 where new row i needs a page for its partly filled last page
+  int2* pairs;               // [n_out]
+};
+static size_t fork_work(char* base, int64_t n_out, ForkWork* w) {
+  auto up = [](size_t b) { return (b + 15) & ~(size_t)15; };
+  const size_t need = up(n_out * 4), pairs = up(n_out * 8);
+  if (w) {
+    w->n_pairs = (int32_t*)base;
+    w->need = (int32_t*)(base + 16);
+    w->pairs = (int2*)(base + 16 + need);
+  }
+  return 16 + need + pairs;
+}
+
+struct ForkParams {
+  KvView kv;
+  const int32_t* src;
+  int32_t *table_out, *len_out, *refs;
+  ForkWork w;
+  int n_out;
+};
+
+// Sum over the CTA of a per-thread count.
+__device__ __forceinline__ int block_sum(int v) {
+  __shared__ int parts[32];
+  v = __reduce_add_sync(0xFFFFFFFFu, v);
+  if ((threadIdx.x & 31) == 0) parts[threadIdx.x >> 5] = v;
+  __syncthreads();
+  int s = 0;
+  for (int w = 0; w < (int)(blockDim.x >> 5); ++w) s += parts[w];
+  __syncthreads();
+  return s;
+}
+
+// CTAs [0, n_rows): the pages of old row s change by (children - 1); its partly filled last page stays
+// with one child, or goes.  CTAs [n_rows, n_rows + n_out): the table row of a new row.
+__global__ void __launch_bounds__(128) fork_rows_kernel(const __grid_constant__ ForkParams p) {
+  const KvView& kv = p.kv;
+  const int n_old = kv.n_rows;
+  if ((int)blockIdx.x < n_old) {
+    const int s = blockIdx.x;
+    int mine = 0;
+    for (int i = threadIdx.x; i < p.n_out; i += blockDim.x) mine += p.src[i] == s;
+    const int children = block_sum(mine);
+    const int n = row_len(kv, s), pages = (n + kv.page_size - 1) / kv.page_size;
+    const bool part = n % kv.page_size != 0;
+    for (int j = threadIdx.x; j < pages; j += blockDim.x) {
+      const int page = kv.table[(int64_t)s * kv.max_pages + j];
+      if ((unsigned int)page >= (unsigned int)kv.n_pages) { flag(kv.status, kStatusIndex); continue; }
+      const int delta = (part && j == pages - 1 ? min(children, 1) : children) - 1;
+      if (delta) atomicAdd(&p.refs[page], delta);
+    }
+    return;
+  }
+  const int i = blockIdx.x - n_old;
+  const int s = p.src[i];
+  const bool ok = (unsigned int)s < (unsigned int)n_old;
+  if (!ok && s != -1 && threadIdx.x == 0) flag(kv.status, kStatusIndex);
+  int mine = 0;
+  for (int j = threadIdx.x; j < i; j += blockDim.x) mine += p.src[j] == s;
+  const bool first = block_sum(mine) == 0;
+  const int n = ok ? row_len(kv, s) : 0, pages = (n + kv.page_size - 1) / kv.page_size;
+  for (int j = threadIdx.x; j < kv.max_pages; j += blockDim.x)
+    p.table_out[(int64_t)i * kv.max_pages + j] = j < pages ? kv.table[(int64_t)s * kv.max_pages + j] : -1;
+  if (threadIdx.x == 0) {
+    p.len_out[i] = n;
+    p.w.need[i] = n % kv.page_size != 0 && !first;
+  }
+}
+
+// Pages for the rows that need one, and the list of copies.
+__global__ void __launch_bounds__(kScanThreads) fork_assign_kernel(const __grid_constant__ ForkParams p) {
+  const KvView& kv = p.kv;
+  int wanted = 0;
+  for (int base = 0; base < p.n_out; base += kScanThreads) {     // pairs[k].x = the k-th row in need, for now
+    const int i = base + threadIdx.x;
+    const int need = i < p.n_out ? p.w.need[i] : 0;
+    int total;
+    const int k = wanted + block_scan(need, &total);
+    if (need) p.w.pairs[k].x = i;
+    wanted += total;
+  }
+  __syncthreads();
+  const int found = take_free(p.refs, kv.n_pages, wanted, [&](int k, int page) {
+    const int i = p.w.pairs[k].x;
+    const int64_t last = (int64_t)i * kv.max_pages + p.len_out[i] / kv.page_size;
+    const int from = p.table_out[last];
+    p.table_out[last] = page;
+    p.refs[page] = 1;
+    p.w.pairs[k] = (unsigned int)from < (unsigned int)kv.n_pages ? make_int2(from, page) : make_int2(page, page);
+  });
+  for (int k = found + threadIdx.x; k < wanted; k += kScanThreads) {   // no page: the full pages remain
+    const int i = p.w.pairs[k].x;
+    const int full = p.len_out[i] / kv.page_size;
+    p.table_out[(int64_t)i * kv.max_pages + full] = -1;
+    p.len_out[i] = full * kv.page_size;
+    flag(kv.status, kStatusPages);
+  }
+  if (threadIdx.x == 0) *p.w.n_pairs = found;
+}
+
+// ---------------------------------------------------------------- pack
+
+struct PackWork {
+  int32_t* n_pairs;
+  int32_t* to;         // [n_pages] new number of a page in use, -1 of a free one
+  int2* pairs;         // [n_pages / 2 + 1] moves
+};
+static size_t pack_work(char* base, int64_t n_pages, PackWork* w) {
+  auto up = [](size_t b) { return (b + 15) & ~(size_t)15; };
+  const size_t to = up(n_pages * 4), pairs = up((n_pages / 2 + 1) * 8);
+  if (w) {
+    w->n_pairs = (int32_t*)base;
+    w->to = (int32_t*)(base + 16);
+    w->pairs = (int2*)(base + 16 + to);
+  }
+  return 16 + to + pairs;
+}
+
+struct PackParams {
+  KvView kv;
+  const int32_t* refs;
+  int32_t *refs_out, *table_out, *page_map;
+  PackWork w;
+};
+
+// The k-th page in use at n_live or above moves into the k-th free page below n_live.
+__global__ void __launch_bounds__(kScanThreads) pack_plan_kernel(const __grid_constant__ PackParams p) {
+  const int n = p.kv.n_pages;
+  int mine = 0, n_live, moves = 0;
+  for (int i = threadIdx.x; i < n; i += kScanThreads) mine += p.refs[i] > 0;
+  block_scan(mine, &n_live);
+  int holes = 0;
+  for (int base = 0; base < n; base += kScanThreads) {
+    const int i = base + threadIdx.x;
+    const bool live = i < n && p.refs[i] > 0;
+    const int hole = i < n_live && !live, mover = i >= n_live && live;
+    int total, total2;
+    const int kh = holes + block_scan(hole, &total), km = moves + block_scan(mover, &total2);
+    if (hole) p.w.pairs[kh].y = i;
+    if (mover) p.w.pairs[km].x = i;
+    if (i < n) p.w.to[i] = live ? i : -1;
+    holes += total;
+    moves += total2;
+  }
+  __syncthreads();
+  for (int k = threadIdx.x; k < moves; k += kScanThreads) p.w.to[p.w.pairs[k].x] = p.w.pairs[k].y;
+  if (threadIdx.x == 0) *p.w.n_pairs = moves;
+  __syncthreads();
+  for (int k = threadIdx.x; k < moves; k += kScanThreads) {
+    const int2 m = p.w.pairs[k];
+    const int c = p.refs[m.x];
+    p.refs_out[m.y] = c;
+    p.refs_out[m.x] = 0;
+  }
+  if (p.page_map)
+    for (int i = threadIdx.x; i < n; i += kScanThreads) p.page_map[i] = p.w.to[i];
+}
+
+__global__ void __launch_bounds__(256) pack_table_kernel(const __grid_constant__ PackParams p) {
+  const KvView& kv = p.kv;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (int64_t)kv.n_rows * kv.max_pages) return;
+  const int row = (int)(i / kv.max_pages), j = (int)(i - (int64_t)row * kv.max_pages);
+  const int n = row_len(kv, row), pages = (n + kv.page_size - 1) / kv.page_size;
+  int to = -1;
+  if (j < pages) {
+    const int page = kv.table[i];
+    if ((unsigned int)page < (unsigned int)kv.n_pages) to = p.w.to[page];
+    if (to < 0) flag(kv.status, kStatusIndex);
+  }
+  p.table_out[i] = to;
+}
+
+// ---------------------------------------------------------------- extend
+
+struct ExtendParams {
+  KvView kv;
+  const int32_t* n_new;
+  int32_t *len_out, *refs;
+  int n_uniform;
+};
+
+// One CTA.  Rows in chunks of 1024: pages wanted, their prefix, then the free pages in order.
+__global__ void __launch_bounds__(kScanThreads) extend_kernel(const __grid_constant__ ExtendParams p) {
+  __shared__ int first[kScanThreads + 1];       // pages handed to the chunk's rows before this one
+  __shared__ int have[kScanThreads];
+  const KvView& kv = p.kv;
+  const int most = kv.max_pages * kv.page_size;
+  bool dry = false;
+  for (int base = 0; base < kv.n_rows; base += kScanThreads) {
+    const int r = base + threadIdx.x;
+    int n = 0, add = 0, old_pages = 0, want = 0;
+    if (r < kv.n_rows) {
+      n = row_len(kv, r);
+      add = p.n_new ? p.n_new[r] : p.n_uniform;
+      if (add < 0) { flag(kv.status, kStatusIndex); add = 0; }
+      if (add > most - n) { flag(kv.status, kStatusPages); add = 0; }
+      old_pages = (n + kv.page_size - 1) / kv.page_size;
+      want = (n + add + kv.page_size - 1) / kv.page_size - old_pages;
+    }
+    int total;
+    const int before = block_scan(want, &total);
+    first[threadIdx.x] = before;
+    have[threadIdx.x] = old_pages;
+    if (threadIdx.x == 0) first[kScanThreads] = total;
+    __syncthreads();
+    int found = 0;
+    if (total && !dry)
+      found = take_free(p.refs, kv.n_pages, total, [&](int k, int page) {
+        int lo = 0, hi = kScanThreads - 1;                 // last row with first[row] <= k
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) >> 1;
+          if (first[mid] <= k) lo = mid; else hi = mid - 1;
+        }
+        kv.table[(int64_t)(base + lo) * kv.max_pages + have[lo] + k - first[lo]] = page;
+      });
+    __syncthreads();
+    const bool fits = before + want <= found || want == 0;
+    const bool late = dry || (found < total && before + want > found);
+    if (r < kv.n_rows) {
+      const bool grown = fits && !late;
+      if (grown)
+        for (int j = 0; j < want; ++j) p.refs[kv.table[(int64_t)r * kv.max_pages + old_pages + j]] = 1;
+      if (!grown && add) flag(kv.status, kStatusPages);
+      p.len_out[r] = grown ? n + add : n;
+    }
+    dry = dry || found < total;
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------- append
+
+struct AppendParams {
+  KvView kv;
+  const uint4 *k_new, *v_new;
+  const int32_t* start;
+  int64_t new_words;        // 16-byte words between tokens
+  int n_tokens, row_words;  // words of a token and head
+  int elem_words;           // elements in a word
+};
+
+constexpr int kAppendTokens = 8;
+
+// A CTA writes eight tokens: the page of each is looked up once, then its words are moved.
+__global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ AppendParams p) {
+  __shared__ int64_t slot[kAppendTokens];       // element offset of the token's head 0, -1: none
+  const KvView& kv = p.kv;
+  const int t0 = blockIdx.x * kAppendTokens;
+  if (threadIdx.x < kAppendTokens) {
+    const int t = t0 + threadIdx.x;
+    int64_t at = -1;
+    if (t < p.n_tokens) {
+      int row = t, pos = -1;
+      if (p.start) {
+        int lo = 0, hi = kv.n_rows;             // first row whose end is past t
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (p.start[mid + 1] <= t) lo = mid + 1; else hi = mid;
+        }
+        row = lo;
+        if (row < kv.n_rows && t >= p.start[row]) pos = row_len(kv, row) - (p.start[row + 1] - t);
+      } else if (row < kv.n_rows) {
+        pos = row_len(kv, row) - 1;
+      }
+      if (pos >= 0) {
+        const int page = kv.table[(int64_t)row * kv.max_pages + pos / kv.page_size];
+        if ((unsigned int)page < (unsigned int)kv.n_pages)
+          at = page * kv.page_stride + (int64_t)(pos % kv.page_size) * kv.head_dim;
+      }
+      if (at < 0) flag(kv.status, kStatusIndex);
+    }
+    slot[threadIdx.x] = at;
+  }
+  __syncthreads();
+  const int per_token = kv.n_kv_heads * p.row_words;
+  for (int i = threadIdx.x; i < kAppendTokens * per_token; i += 256) {
+    const int tok = i / per_token, w = i - tok * per_token, h = w / p.row_words, c = w - h * p.row_words;
+    const int64_t at = slot[tok];
+    if (at < 0) continue;
+    const int64_t to = (at + (int64_t)h * kv.page_size * kv.head_dim) / p.elem_words + c;
+    const int64_t from = (t0 + tok) * p.new_words + w;
+    ((uint4*)kv.k)[to] = p.k_new[from];
+    ((uint4*)kv.v)[to] = p.v_new[from];
+  }
+}
+
+static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + nb && y < x + na;
+}
+
+}  // namespace pg
+
+extern "C" {
+
+size_t pg_kv_fork_workspace_bytes(const pg_kv* kv, int32_t n_out) {
+  if (pg::kv_check(kv) != PG_OK || n_out < 0) return 0;
+  return pg::fork_work(nullptr, n_out, nullptr);
+}
+
+int pg_kv_fork(const pg_kv* kv, int32_t n_out, const int32_t* src_rows, int32_t* table_out, int32_t* len_out,
+               const int32_t* refs, int32_t* refs_out, void* workspace, size_t workspace_bytes, int32_t* status,
+               void* stream) {
+  const int rc = pg::kv_check(kv);
+  if (rc != PG_OK) return rc;
+  if (n_out < 0 || !refs || !refs_out) return PG_EINVAL;
+  if (n_out > 0 && (!src_rows || !table_out || !len_out)) return PG_EINVAL;
+  if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < pg_kv_fork_workspace_bytes(kv, n_out)) return PG_EINVAL;
+  if ((int64_t)kv->n_rows + n_out > 0x7FFFFFFFLL) return PG_EINVAL;
+  const size_t in_t = (size_t)kv->n_rows * kv->max_pages * 4, out_t = (size_t)n_out * kv->max_pages * 4;
+  if (n_out > 0 && kv->n_rows > 0 &&
+      (pg::overlap(table_out, out_t, kv->table, in_t) || pg::overlap(len_out, (size_t)n_out * 4, kv->len, (size_t)kv->n_rows * 4)))
+    return PG_EINVAL;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (refs != refs_out) PG_CUDA(cudaMemcpyAsync(refs_out, refs, (size_t)kv->n_pages * 4, cudaMemcpyDeviceToDevice, st));
+  if (kv->n_rows + n_out == 0) return PG_OK;
+  pg::ForkParams p;
+  p.kv = pg::kv_view(kv, status);
+  p.src = src_rows; p.table_out = table_out; p.len_out = len_out; p.refs = refs_out; p.n_out = n_out;
+  pg::fork_work((char*)workspace, n_out, &p.w);
+  pg::fork_rows_kernel<<<(unsigned)(kv->n_rows + n_out), 128, 0, st>>>(p);
+  PG_LAUNCH_CHECK();
+  if (n_out == 0) return PG_OK;
+  pg::fork_assign_kernel<<<1, pg::kScanThreads, 0, st>>>(p);
+  PG_LAUNCH_CHECK();
+  return pg::launch_copy(kv, p.kv, p.w.pairs, p.w.n_pairs, n_out, st);
+}
+
+size_t pg_kv_pack_workspace_bytes(const pg_kv* kv) {
+  if (pg::kv_check(kv) != PG_OK) return 0;
+  return pg::pack_work(nullptr, kv->n_pages, nullptr);
+}
+
+int pg_kv_pack(const pg_kv* kv, const int32_t* refs, int32_t* refs_out, int32_t* table_out, int32_t* page_map,
+               void* workspace, size_t workspace_bytes, int32_t* status, void* stream) {
+  const int rc = pg::kv_check(kv);
+  if (rc != PG_OK) return rc;
+  if (!refs || !refs_out || (kv->n_rows > 0 && !table_out)) return PG_EINVAL;
+  if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < pg_kv_pack_workspace_bytes(kv)) return PG_EINVAL;
+  const size_t t = (size_t)kv->n_rows * kv->max_pages * 4;
+  if (kv->n_rows > 0 && table_out != kv->table && pg::overlap(table_out, t, kv->table, t)) return PG_EINVAL;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (refs != refs_out) PG_CUDA(cudaMemcpyAsync(refs_out, refs, (size_t)kv->n_pages * 4, cudaMemcpyDeviceToDevice, st));
+  pg::PackParams p;
+  p.kv = pg::kv_view(kv, status);
+  p.refs = refs; p.refs_out = refs_out; p.table_out = table_out; p.page_map = page_map;
+  pg::pack_work((char*)workspace, kv->n_pages, &p.w);
+  pg::pack_plan_kernel<<<1, pg::kScanThreads, 0, st>>>(p);
+  PG_LAUNCH_CHECK();
+  const int64_t entries = (int64_t)kv->n_rows * kv->max_pages;
+  if ((entries + 255) / 256 > 0x7FFFFFFFLL) return PG_EINVAL;
+  if (entries > 0) {
+    pg::pack_table_kernel<<<(unsigned)((entries + 255) / 256), 256, 0, st>>>(p);
+    PG_LAUNCH_CHECK();
+  }
+  return pg::launch_copy(kv, p.kv, p.w.pairs, p.w.n_pairs, kv->n_pages / 2, st);
+}
+
+int pg_kv_extend(const pg_kv* kv, const int32_t* n_new, int32_t n_uniform, int32_t* len_out, const int32_t* refs,
+                 int32_t* refs_out, int32_t* status, void* stream) {
+  const int rc = pg::kv_check(kv);
+  if (rc != PG_OK) return rc;
+  if ((!n_new && n_uniform < 0) || !refs || !refs_out || (kv->n_rows > 0 && !len_out)) return PG_EINVAL;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (refs != refs_out) PG_CUDA(cudaMemcpyAsync(refs_out, refs, (size_t)kv->n_pages * 4, cudaMemcpyDeviceToDevice, st));
+  if (kv->n_rows == 0) return PG_OK;
+  pg::ExtendParams p;
+  p.kv = pg::kv_view(kv, status);
+  p.n_new = n_new; p.n_uniform = n_uniform; p.len_out = len_out; p.refs = refs_out;
+  pg::extend_kernel<<<1, pg::kScanThreads, 0, st>>>(p);
+  PG_LAUNCH_CHECK();
+  return PG_OK;
+}
+
+int pg_kv_append(const pg_kv* kv, int32_t layer, int32_t n_tokens, const void* k_new, const void* v_new,
+                 int64_t new_stride, const int32_t* start, int32_t* status, void* stream) {
+  const int rc = pg::kv_check(kv);
+  if (rc != PG_OK) return rc;
+  if (layer < 0 || layer >= kv->n_layers || n_tokens < 0) return PG_EINVAL;
+  if (!start && n_tokens != kv->n_rows) return PG_EINVAL;
+  if (n_tokens == 0) return PG_OK;
+  const size_t b = pg::dtype_bytes(kv->dtype);
+  const int64_t dense = (int64_t)kv->n_kv_heads * kv->head_dim;
+  if (new_stride == 0) new_stride = dense;
+  if (!k_new || !v_new || (((uintptr_t)k_new | (uintptr_t)v_new) & 15) || new_stride < dense || (new_stride * b & 15))
+    return PG_EINVAL;
+  pg::AppendParams p;
+  p.kv = pg::kv_view(kv, status);
+  p.kv.k = (char*)kv->k + (size_t)layer * p.kv.layer_stride * b;
+  p.kv.v = (char*)kv->v + (size_t)layer * p.kv.layer_stride * b;
+  p.k_new = (const uint4*)k_new; p.v_new = (const uint4*)v_new;
+  p.start = start;
+  p.new_words = new_stride * (int64_t)b / 16;
+  p.n_tokens = n_tokens;
+  p.row_words = (int)(kv->head_dim * b / 16);
+  p.elem_words = (int)(16 / b);
+  if ((int64_t)kv->n_kv_heads * p.row_words > (1 << 24)) return PG_EINVAL;
+  pg::append_kernel<<<(unsigned)((n_tokens + (int64_t)pg::kAppendTokens - 1) / pg::kAppendTokens), 256, 0, (cudaStream_t)stream>>>(p);
+  PG_LAUNCH_CHECK();
+  return PG_OK;
+}
+
+int pg_kv_status(const int32_t* status, void* stream) {
+  if (!status) return PG_EINVAL;
+  int32_t word = 0;
+  PG_CUDA(cudaMemcpyAsync(&word, status, sizeof(word), cudaMemcpyDeviceToHost, (cudaStream_t)stream));
+  PG_CUDA(cudaStreamSynchronize((cudaStream_t)stream));
+  if (word & pg::kStatusIndex) return PG_EINDEX;
+  if (word & pg::kStatusPages) return PG_ENOPAGES;
+  return PG_OK;
+}
+
+}  // extern "C"

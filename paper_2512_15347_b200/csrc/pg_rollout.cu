@@ -509,6 +509,7 @@ const char* pg_strerror(int code) {
     case PG_EINDEX: return "a gather index (src_rows / keep_idx) was out of range; the rows were not read";
     case PG_ECAPACITY: return "request exceeds the capacity of a fixed built-in buffer";
     case PG_EDEVICE: return "the handle belongs to another device than the current one";
+    case PG_ENOPAGES: return "no free page was left in the pool, or a row's page table was full";
     default: return "unknown error code";
   }
 }
