@@ -1,8 +1,51 @@
 // Attention of one new token per row over the paged cache (pg_kv_attend).
-//   out = sum_t p_t v_t,  p = softmax(scale q.k_t) over the row's tokens, lse = ln sum exp.
+//
+// For each query head:  out = sum_t p_t v_t,  p = softmax(scale q.k_t),  lse = ln sum_t exp(scale q.k_t),
+// in one pass over the tokens with a running maximum m, sum l and accumulator o per warp:
+//     m' = max(m, max_t x_t),  l' = l 2^(m-m') + sum 2^(x_t-m'),  o' = o 2^(m-m') + sum 2^(x_t-m') v_t
+// with x = scale log2(e) q.k; two such triples over disjoint tokens join by the same rule, which is how
+// warps, and the CTAs that share a row, are put together.
+//
+// Bound: HBM.  A token's K and V of one kv head are 4 D bytes (16-bit) for 4 D flops per query head that
+// shares them, i.e. per_kv flop per byte; every byte is read once, by one warp, for all query heads of
+// its kv head.
+//
+// Work split.  The unit is a chunk: the K and V of kChunk consecutive tokens of one (row, kv head).
+// All chunks of the call, ordered (row, kv head, chunk), form one line that the resident CTAs cut into
+// equal parts, so ragged lengths, one long row and many short ones all balance; the cut points follow
+// from the lengths in device memory (every CTA sums them itself), nothing is planned on the host.
+// Inside a CTA chunks go round the warps; each warp copies its own chunks through a ring of kStages
+// buffers with 16-byte asynchronous copies and never waits for another warp except at the end of a
+// (row, head) piece, where the warps' triples are joined in shared memory.  A piece that a cut has
+// split is joined by the CTA that arrives last (wait-free ticket; parts are added in CTA order, so the
+// bits do not depend on who that is).
 #include "pg_kv.cuh"
 
+#include <type_traits>
+
 namespace pg {
+
+constexpr int kSms = 148;
+constexpr int kWarps = 4;
+constexpr int kThreads = kWarps * 32;
+constexpr int kMaxCtas = kSms * 2;
+constexpr int kMaxHeads = 16;                 // query heads of a (row, kv head) piece
+constexpr size_t kTicketBytes = 4096;         // >= 4 * kMaxCtas
+
+// n / d for 0 <= n < 2^31 by a multiplication (d >= 1): m = ceil(2^(32+s) / d), s = ceil(log2 d) - 1.
+struct FastDiv {
+  uint32_t d, m, s;
+};
+inline FastDiv fast_div(uint32_t d) {
+  FastDiv f{d, 0, 0};
+  if (d > 1) {
+    uint32_t s = 0;
+    while ((1ull << (s + 1)) < d) ++s;
+    f.s = s;
+    f.m = (uint32_t)((((unsigned __int128)1 << (32 + s)) + d - 1) / d);
+  }
+  return f;
+}
 
 struct AttendParams {
   KvView kv;
@@ -13,79 +56,670 @@ struct AttendParams {
   const int32_t* shared;
   int64_t q_stride, new_stride, out_stride;   // elements
   int n_q_heads, per_kv, group;
-  float scale;
+  int n_split, piece_heads;                   // pieces per kv head, query heads of a piece
+  float scale_log2;                           // scale * log2(e)
+  FastDiv page;
+  unsigned int* tickets;                      // [kMaxCtas], zero between calls
+  float* parts;                               // [2 * CTAs][REGS * 32 + 2 * kMaxHeads]
 };
 
-constexpr int kAttendWarps = 4;
+#ifdef __CUDACC__
+__device__ __forceinline__ uint32_t div_by(uint32_t n, const FastDiv& f) {
+  return f.d == 1 ? n : __umulhi(n, f.m) >> f.s;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t shared_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool some) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(some ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// One CTA per (row, query head): each warp takes every fourth token with a running maximum m and sum
-// l of its own, lanes hold the elements lane, lane + 32, ...; the warps are joined at the end.
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
 template <typename T>
-__global__ void __launch_bounds__(kAttendWarps * 32)
-attend_kernel(const __grid_constant__ AttendParams p) {
-  constexpr int kPer = 256 / 32;
-  __shared__ float part[kAttendWarps][256];
-  __shared__ float stat[kAttendWarps][2];
-  const KvView& kv = p.kv;
-  const int row = blockIdx.x / p.n_q_heads, head = blockIdx.x - row * p.n_q_heads;
-  const int h = head / p.per_kv, D = kv.head_dim;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int n = row_len(kv, row);
-  const T* q = (const T*)p.q + row * p.q_stride + (int64_t)head * D;
-  float qr[kPer], acc[kPer];
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, __half) {
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// ---------------------------------------------------------------- bodies: one warp, one chunk at a time
+// A body holds a warp's triple for up to NT * 8 query heads over head dimensions padded to DP (copies
+// fill what is past head_dim with zeros).  o[REGS] is its part of the accumulator; head_of / dim_of say
+// which element lane `lane` holds in register i.
+
+// 16-bit: tensor cores, with keys as the rows of the product (S^T = K Q^T, O^T = V^T P^T), so that a kv
+// head with few query heads fills the n = 8 side instead of padding m = 16.  P^T comes from S^T's
+// accumulators by an 8x8 register transposition; P is rounded to the cache's type for the product (the
+// sum l is taken before the rounding), which adds less to the result than its own last rounding.
+template <typename T, int DP, int NT>
+struct MmaBody {
+  static constexpr int kChunk = DP > 128 ? 16 : 32;
+  static constexpr int kTiles = kChunk / 16;
+  static constexpr int kRegs = DP / 16 * NT * 4;
+  static constexpr int kRowBytes = DP * 2;
+  static constexpr size_t kQBytes = 0;              // shared memory per warp for the queries
+  float o[kRegs];
+  float m[NT][2], l[NT][2];
+  uint32_t q[DP / 16][NT][2];
+
+  static __device__ __forceinline__ int head_of(int i, int lane) { return (i >> 2) % NT * 8 + (lane & 3) * 2 + (i & 1); }
+  static __device__ __forceinline__ int dim_of(int i, int lane) { return (i >> 2) / NT * 16 + (lane >> 2) + ((i >> 1) & 1) * 8; }
+  // 16-byte piece c of token row t: pieces are swizzled so that eight rows' equal pieces hit all banks
+  static __device__ __forceinline__ uint32_t piece_at(int t, int c) { return t * kRowBytes + ((c ^ (t & 7)) << 4); }
+
+  __device__ __forceinline__ void begin(const AttendParams& p, int row, int head0, int heads, int lane, char*) {
+    const T* base = (const T*)p.q + row * p.q_stride;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    qr[i] = lane + 32 * i < D ? to_float(q[lane + 32 * i]) * p.scale : 0.f;
-    acc[i] = 0.f;
+    for (int nt = 0; nt < NT; ++nt) {
+      const int g = nt * 8 + (lane >> 2);
+      const T* qh = base + (int64_t)(head0 + g) * p.kv.head_dim;
+#pragma unroll
+      for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int d = s * 16 + j * 8 + (lane & 3) * 2;
+          uint32_t w = 0;
+          if (g < heads && d < p.kv.head_dim) {
+            uint16_t lo, hi;
+            lo = *(const uint16_t*)(qh + d);
+            hi = *(const uint16_t*)(qh + d + 1);
+            w = lo | (uint32_t)hi << 16;
+          }
+          q[s][nt][j] = w;
+        }
+      m[nt][0] = m[nt][1] = -INFINITY;
+      l[nt][0] = l[nt][1] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kRegs; ++i) o[i] = 0.f;
   }
-  float m = -INFINITY, l = 0.f;
-  for (int t = warp; t < n; t += kAttendWarps) {
-    const int page = kv.table[(int64_t)row * kv.max_pages + t / kv.page_size];
-    const bool ok = (unsigned int)page < (unsigned int)kv.n_pages;
-    if (!ok) flag(kv.status, kStatusIndex);
-    const int64_t at = (ok ? page : 0) * kv.page_stride + ((int64_t)h * kv.page_size + t % kv.page_size) * D;
-    T* kp = (T*)kv.k + at;
-    T* vp = (T*)kv.v + at;
-    const bool fresh = p.k_new && t == n - 1;
-    const T* ks = fresh ? (const T*)p.k_new + row * p.new_stride + (int64_t)h * D : kp;
-    const T* vs = fresh ? (const T*)p.v_new + row * p.new_stride + (int64_t)h * D : vp;
-    float s = 0.f, vr[kPer];
+
+  // keys [t0, t0 + kChunk) in kbuf / vbuf (shared addresses), of which [lo, hi) count
+  __device__ __forceinline__ void step(const AttendParams& p, uint32_t kbuf, uint32_t vbuf, const char*, int t0, int lo, int hi,
+                                       int lane) {
+    float s[kTiles][NT][4];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int d = lane + 32 * i;
-      vr[i] = 0.f;
-      if (d < D && (ok || fresh)) {
-        const T a = ks[d], b = vs[d];
-        s = fmaf(qr[i], to_float(a), s);
-        vr[i] = to_float(b);
-        if (fresh && ok && head % p.per_kv == 0) { kp[d] = a; vp[d] = b; }
+    for (int mt = 0; mt < kTiles; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[mt][nt][j] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < DP / 16; ++ks)
+#pragma unroll
+      for (int mt = 0; mt < kTiles; ++mt) {
+        uint32_t a[4];
+        ldmatrix4(a, kbuf + piece_at(mt * 16 + (lane & 15), ks * 2 + (lane >> 4)));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) mma16816<T>(s[mt][nt], a, q[ks][nt][0], q[ks][nt][1]);
+      }
+    const bool whole = t0 >= lo && t0 + kChunk <= hi;
+    float top[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      top[nt][0] = top[nt][1] = -INFINITY;
+#pragma unroll
+      for (int mt = 0; mt < kTiles; ++mt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float x = s[mt][nt][j] * p.scale_log2;
+          if (!whole) {
+            const int t = t0 + mt * 16 + (lane >> 2) + (j >> 1) * 8;
+            if (t < lo || t >= hi) x = -INFINITY;
+          }
+          s[mt][nt][j] = x;
+          top[nt][j & 1] = fmaxf(top[nt][j & 1], x);
+        }
+    }
+#pragma unroll
+    for (int d = 4; d < 32; d <<= 1)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) top[nt][j] = fmaxf(top[nt][j], __shfl_xor_sync(0xFFFFFFFFu, top[nt][j], d));
+    bool rose = false;
+    float f[NT][2], off[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float m2 = fmaxf(m[nt][j], top[nt][j]);
+        off[nt][j] = m2 == -INFINITY ? 0.f : m2;       // nothing counted yet: every weight below is 0
+        f[nt][j] = exp2_fast(m[nt][j] - off[nt][j]);
+        rose |= m2 != m[nt][j];
+        m[nt][j] = m2;
+      }
+    if (__any_sync(0xFFFFFFFFu, rose)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        l[nt][0] *= f[nt][0];
+        l[nt][1] *= f[nt][1];
+      }
+#pragma unroll
+      for (int i = 0; i < kRegs; ++i) o[i] *= f[(i >> 2) % NT][i & 1];
+    }
+    uint32_t b[kTiles][NT][2];
+#pragma unroll
+    for (int mt = 0; mt < kTiles; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          w[j] = exp2_fast(s[mt][nt][j] - off[nt][j & 1]);
+          l[nt][j & 1] += w[j];
+        }
+        b[mt][nt][0] = transpose8x8(pack2(w[0], w[1], T()));
+        b[mt][nt][1] = transpose8x8(pack2(w[2], w[3], T()));
+      }
+#pragma unroll
+    for (int dt = 0; dt < DP / 16; ++dt)
+#pragma unroll
+      for (int mt = 0; mt < kTiles; ++mt) {
+        uint32_t a[4];
+        ldmatrix4_trans(a, vbuf + piece_at(mt * 16 + (lane & 7) + (lane >> 4) * 8, dt * 2 + ((lane >> 3) & 1)));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float(&c)[4] = *reinterpret_cast<float(*)[4]>(&o[(dt * NT + nt) * 4]);
+          mma16816<T>(c, a, b[mt][nt][0], b[mt][nt][1]);
+        }
+      }
+  }
+
+  // stats[head] = (m, l), by the lanes that hold them
+  __device__ __forceinline__ void stats(float2* out, int lane) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float s = l[nt][j];
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+        if (lane < 4) out[nt * 8 + lane * 2 + j] = make_float2(m[nt][j], s);
+      }
+  }
+};
+
+// fp32: fused multiply-adds (the tensor cores would round the inputs).  Eight lanes share a key for the
+// scores, every lane owns DP / 32 dimensions for the products with V; queries and weights pass through
+// shared memory.
+template <int DP, int NT>
+struct F32Body {
+  static constexpr int kChunk = DP <= 128 ? 16 : NT == 1 ? 8 : 4;
+  static constexpr int kHeads = NT * 8;
+  static constexpr int kPer = DP / 32;              // elements of o and v per lane and head
+  static constexpr int kRegs = kHeads * kPer;
+  static constexpr int kRowBytes = DP * 4;
+  static constexpr int kKeys = kChunk / 4;          // keys of a lane
+  static constexpr int kVec = DP / 32;              // 16-byte pieces of a key per lane
+  static constexpr size_t kQBytes = kHeads * DP * 4 + kChunk * kHeads * 4;
+  float o[kRegs];
+  float m[kHeads], l[kHeads];
+
+  static __device__ __forceinline__ int head_of(int i, int) { return i / kPer; }
+  static __device__ __forceinline__ int dim_of(int i, int lane) {
+    const int j = i % kPer;
+    return kPer == 2 ? lane * 2 + j : (j >> 2) * 128 + lane * 4 + (j & 3);
+  }
+  static __device__ __forceinline__ uint32_t piece_at(int t, int c) { return t * kRowBytes + (c << 4); }
+
+  __device__ __forceinline__ void begin(const AttendParams& p, int row, int head0, int heads, int lane, char* scratch) {
+    float* q = (float*)scratch;
+    const float* base = (const float*)p.q + row * p.q_stride + (int64_t)head0 * p.kv.head_dim;
+    __syncwarp();
+    for (int i = lane; i < kHeads * DP; i += 32) {
+      const int g = i / DP, d = i - g * DP;
+      q[i] = g < heads && d < p.kv.head_dim ? base[(int64_t)g * p.kv.head_dim + d] : 0.f;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kRegs; ++i) o[i] = 0.f;
+#pragma unroll
+    for (int g = 0; g < kHeads; ++g) { m[g] = -INFINITY; l[g] = 0.f; }
+  }
+
+  __device__ __forceinline__ void step(const AttendParams& p, uint32_t kbuf, uint32_t vbuf, char* scratch, int t0, int lo, int hi,
+                                       int lane) {
+    const char* kb = (const char*)__cvta_shared_to_generic(kbuf);
+    const char* vb = (const char*)__cvta_shared_to_generic(vbuf);
+    const float4* q = (const float4*)scratch;
+    float* w = (float*)(scratch + kHeads * DP * 4);
+    const int part = lane & 7, sub = lane >> 3;
+    float4 k[kKeys][kVec];
+#pragma unroll
+    for (int a = 0; a < kKeys; ++a)
+#pragma unroll
+      for (int c = 0; c < kVec; ++c) k[a][c] = *(const float4*)(kb + piece_at(a * 4 + sub, c * 8 + part));
+#pragma unroll
+    for (int g = 0; g < kHeads; ++g) {
+      if (g >= p.piece_heads) continue;
+      float s[kKeys];
+#pragma unroll
+      for (int a = 0; a < kKeys; ++a) s[a] = 0.f;
+#pragma unroll
+      for (int c = 0; c < kVec; ++c) {
+        const float4 x = q[g * (DP / 4) + c * 8 + part];
+#pragma unroll
+        for (int a = 0; a < kKeys; ++a)
+          s[a] = fmaf(x.x, k[a][c].x, fmaf(x.y, k[a][c].y, fmaf(x.z, k[a][c].z, fmaf(x.w, k[a][c].w, s[a]))));
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int a = 0; a < kKeys; ++a) {
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) s[a] += __shfl_xor_sync(0xFFFFFFFFu, s[a], d);
+        const int t = t0 + a * 4 + sub;
+        s[a] = t < lo || t >= hi ? -INFINITY : s[a] * p.scale_log2;
+        top = fmaxf(top, s[a]);
+      }
+      top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 8));
+      top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 16));
+      const float m2 = fmaxf(m[g], top), off = m2 == -INFINITY ? 0.f : m2;
+      if (m2 != m[g]) {                              // the same for all lanes
+        const float f = exp2_fast(m[g] - off);
+        l[g] *= f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) o[g * kPer + i] *= f;
+        m[g] = m2;
+      }
+#pragma unroll
+      for (int a = 0; a < kKeys; ++a) {
+        const float e = exp2_fast(s[a] - off);
+        l[g] += e;                                   // eight lanes count the same key
+        if (part == 0) w[(a * 4 + sub) * kHeads + g] = e;
       }
     }
-    s = warp_sum(s);
-    const float m2 = fmaxf(m, s), safe = fmaxf(m2, -3e38f);
-    const float keep = expf(m - safe), w = expf(s - safe);
-    l = l * keep + w;
+    __syncwarp();
+#pragma unroll 4
+    for (int t = 0; t < kChunk; ++t) {
+      float v[kPer];
+      if constexpr (kPer == 2) {
+        const float2 x = *(const float2*)(vb + t * kRowBytes + lane * 8);
+        v[0] = x.x; v[1] = x.y;
+      } else {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) acc[i] = acc[i] * keep + w * vr[i];
-    m = m2;
-  }
-  if (lane == 0) { stat[warp][0] = m; stat[warp][1] = l; }
+        for (int c = 0; c < kPer / 4; ++c) {
+          const float4 x = *(const float4*)(vb + t * kRowBytes + c * 512 + lane * 16);
+          v[c * 4] = x.x; v[c * 4 + 1] = x.y; v[c * 4 + 2] = x.z; v[c * 4 + 3] = x.w;
+        }
+      }
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) part[warp][lane + 32 * i] = acc[i];
-  __syncthreads();
-  float top = -3e38f, total = 0.f, f[kAttendWarps];
-  for (int w = 0; w < kAttendWarps; ++w) top = fmaxf(top, stat[w][0]);
-  for (int w = 0; w < kAttendWarps; ++w) {
-    f[w] = expf(stat[w][0] - top);
-    total += f[w] * stat[w][1];
+      for (int g4 = 0; g4 < kHeads; g4 += 4) {
+        if (g4 >= p.piece_heads) continue;
+        const float4 e = *(const float4*)(w + t * kHeads + g4);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          o[(g4 + 0) * kPer + i] = fmaf(e.x, v[i], o[(g4 + 0) * kPer + i]);
+          if (g4 + 1 < p.piece_heads) o[(g4 + 1) * kPer + i] = fmaf(e.y, v[i], o[(g4 + 1) * kPer + i]);
+          if (g4 + 2 < p.piece_heads) o[(g4 + 2) * kPer + i] = fmaf(e.z, v[i], o[(g4 + 2) * kPer + i]);
+          if (g4 + 3 < p.piece_heads) o[(g4 + 3) * kPer + i] = fmaf(e.w, v[i], o[(g4 + 3) * kPer + i]);
+        }
+      }
+    }
+    __syncwarp();
   }
-  for (int d = threadIdx.x; d < D; d += blockDim.x) {
-    float o = 0.f;
-    for (int w = 0; w < kAttendWarps; ++w) o += f[w] * part[w][d];
-    ((T*)p.out)[row * p.out_stride + (int64_t)head * D + d] = from_float<T>(total == 0.f ? 0.f : o / total);
+
+  __device__ __forceinline__ void stats(float2* out, int lane) {
+#pragma unroll
+    for (int g = 0; g < kHeads; ++g) {
+      float s = l[g];
+      s += __shfl_xor_sync(0xFFFFFFFFu, s, 8);
+      s += __shfl_xor_sync(0xFFFFFFFFu, s, 16);
+      if (lane == 0) out[g] = make_float2(m[g], s);
+    }
   }
-  if (threadIdx.x == 0 && p.lse) p.lse[(int64_t)row * p.n_q_heads + head] = total == 0.f ? -INFINITY : top + logf(total);
+};
+
+// ---------------------------------------------------------------- the line of chunks
+
+// Tokens [lo, hi) of a row that the line covers, and its chunks [c0, c1).
+struct RowSpan {
+  int lo, hi, c0, c1;
+};
+template <int kChunk>
+__device__ __forceinline__ RowSpan row_span(const AttendParams& p, int row) {
+  RowSpan s;
+  s.hi = row_len(p.kv, row);
+  s.lo = 0;
+  s.c0 = s.lo / kChunk;
+  s.c1 = s.hi > s.lo ? (s.hi + kChunk - 1) / kChunk : s.c0;
+  return s;
 }
+
+// A place on the line: chunk `chunk` of (row, piece), pieces numbered (kv head, split) within the row.
+template <int kChunk>
+struct Place {
+  int row, piece, chunk;
+  RowSpan span;
+  __device__ __forceinline__ void advance(const AttendParams& p, int by, int pieces) {
+    chunk += by;
+    while (chunk >= span.c1) {
+      chunk -= span.c1 - span.c0;
+      if (++piece == pieces) {
+        piece = 0;
+        const int over = chunk - span.c0;
+        do {
+          if (++row >= p.kv.n_rows) return;
+          span = row_span<kChunk>(p, row);
+        } while (span.c1 == span.c0);
+        chunk = span.c0 + over;
+      }
+    }
+  }
+};
+
+template <typename T, typename Body, int kStages>
+struct AttendShared {
+  static constexpr int kStageBytes = 2 * Body::kChunk * Body::kRowBytes;
+  static constexpr size_t kRing = (size_t)kWarps * kStages * kStageBytes;
+  static constexpr size_t kJoin = (size_t)kWarps * Body::kRegs * 32 * 4;
+  static constexpr size_t kBytes = kRing + kJoin + kWarps * Body::kQBytes;
+};
+
+template <typename T, typename Body, int kStages, int kCtasPerSm>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __grid_constant__ AttendParams p) {
+  using S = AttendShared<T, Body, kStages>;
+  constexpr int kChunk = Body::kChunk, kRegs = Body::kRegs;
+  constexpr int kPart = kRegs * 32 + 2 * kMaxHeads;
+  extern __shared__ __align__(1024) char smem[];
+  __shared__ long long warp_sum_[kWarps];
+  __shared__ Place<kChunk> first;
+  __shared__ float2 stat[kWarps][kMaxHeads];
+  __shared__ int is_last;
+  constexpr int kMaxEmpty = 64;
+  __shared__ int n_empty, empty[kMaxEmpty];
+  const KvView& kv = p.kv;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int pieces = kv.n_kv_heads * p.n_split;
+
+  // Where this CTA's part of the line begins: sum of the rows' chunks, then the row that holds the cut.
+  const int per = (kv.n_rows + kThreads - 1) / kThreads;
+  const int r0 = min((int)threadIdx.x * per, kv.n_rows), r1 = min(r0 + per, kv.n_rows);
+  if (threadIdx.x == 0) n_empty = 0;
+  __syncthreads();
+  // rows without tokens, dealt round the CTAs, are cleared at the end of the planning
+  auto clear_row = [&](int r, int from, int step) {
+    T* out = (T*)p.out + r * p.out_stride;
+    for (int i = from; i < p.n_q_heads * kv.head_dim; i += step) out[i] = from_float<T>(0.f);
+    if (p.lse)
+      for (int i = from; i < p.n_q_heads; i += step) p.lse[(int64_t)r * p.n_q_heads + i] = -INFINITY;
+  };
+  long long mine = 0;
+  for (int r = r0; r < r1; ++r) {
+    const RowSpan s = row_span<kChunk>(p, r);
+    mine += s.c1 - s.c0;
+    if (s.c1 == s.c0 && r % gridDim.x == blockIdx.x) {
+      const int at = atomicAdd(&n_empty, 1);
+      if (at < kMaxEmpty) empty[at] = r;
+      else clear_row(r, 0, 1);
+    }
+  }
+  long long upto = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const long long y = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+    if (lane >= d) upto += y;
+  }
+  if (lane == 31) warp_sum_[warp] = upto;
+  __syncthreads();
+  long long all = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) upto += warp_sum_[w];
+    all += warp_sum_[w];
+  }
+  const long long total = all * pieces;
+  // equal parts; but a part is not shorter than an average (row, head) if that is at most one chunk a warp
+  long long quota = (total + gridDim.x - 1) / gridDim.x;
+  const long long avg = (all + kv.n_rows - 1) / kv.n_rows;
+  quota = max(quota, min(avg, (long long)kWarps));
+  const long long begin = blockIdx.x * quota;
+  const int count = (int)max(0ll, min(quota, total - begin));
+  if (count > 0) {
+    const long long before = (upto - mine) * pieces;
+    if (begin >= before && begin < before + mine * pieces) {
+      Place<kChunk> at;
+      long long rest = begin - before;
+      for (int r = r0; r < r1; ++r) {
+        at.span = row_span<kChunk>(p, r);
+        const int n = at.span.c1 - at.span.c0;
+        if (rest < (long long)n * pieces) {
+          at.row = r;
+          at.piece = (int)(rest / n);
+          at.chunk = at.span.c0 + (int)(rest - (long long)at.piece * n);
+          break;
+        }
+        rest -= (long long)n * pieces;
+      }
+      first = at;
+    }
+  }
+  for (int i = 0; i < min(n_empty, kMaxEmpty); ++i) clear_row(empty[i], threadIdx.x, kThreads);
+  if (count == 0) return;
+  __syncthreads();
+
+  // Loads.  A lane looks up the page of one token of the chunk (one chunk ahead of its copies); the
+  // copies then go two or more tokens at a time, 16 bytes a lane.
+  const uint32_t ring = shared_addr(smem) + warp * kStages * S::kStageBytes;
+  char* scratch = smem + S::kRing + S::kJoin + warp * Body::kQBytes;
+  constexpr int kLanesPerRow = Body::kRowBytes / 16 < 32 ? Body::kRowBytes / 16 : 32;
+  constexpr int kRowsPerCopy = 32 / kLanesPerRow;
+  constexpr int kPiecesPerLane = Body::kRowBytes / 16 / kLanesPerRow;
+  const int row_pieces = kv.head_dim * (int)sizeof(T) / 16;
+  Place<kChunk> ahead = first;
+  int issued = warp;                                  // this warp's next chunk, counted from the CTA's first
+  if (issued < count) ahead.advance(p, warp, pieces);
+  int entry = 0;
+  auto look_up = [&]() {
+    if (issued >= count) return;
+    const int t = ahead.chunk * kChunk + lane;
+    if (lane < kChunk && t < ahead.span.hi && t >= ahead.span.lo)
+      entry = kv.table[(int64_t)ahead.row * kv.max_pages + div_by(t, p.page)];
+  };
+  look_up();
+  auto issue = [&](int stage) {
+    if (issued < count) {
+      const int t = ahead.chunk * kChunk + lane, h = ahead.piece / p.n_split;
+      const bool in = lane < kChunk && t < ahead.span.hi && t >= ahead.span.lo;
+      const T *ks = nullptr, *vs = nullptr;           // null: zeros
+      if (in) {
+        if (p.k_new && t == ahead.span.hi - 1) {
+          const int64_t at = ahead.row * p.new_stride + (int64_t)h * kv.head_dim;
+          ks = (const T*)p.k_new + at;
+          vs = (const T*)p.v_new + at;
+        } else if ((unsigned int)entry < (unsigned int)kv.n_pages) {
+          const int slot = t - (int)div_by(t, p.page) * kv.page_size;
+          const int64_t at = entry * kv.page_stride + ((int64_t)h * kv.page_size + slot) * kv.head_dim;
+          ks = (const T*)kv.k + at;
+          vs = (const T*)kv.v + at;
+        } else {
+          flag(kv.status, kStatusIndex);
+        }
+      }
+      const uint32_t kb = ring + stage * S::kStageBytes, vb = kb + kChunk * Body::kRowBytes;
+#pragma unroll
+      for (int i = 0; i < kChunk; i += kRowsPerCopy) {
+        const int tok = i + lane / kLanesPerRow;
+        const char* kp = (const char*)__shfl_sync(0xFFFFFFFFu, (unsigned long long)ks, tok);
+        const char* vp = (const char*)__shfl_sync(0xFFFFFFFFu, (unsigned long long)vs, tok);
+#pragma unroll
+        for (int j = 0; j < kPiecesPerLane; ++j) {
+          const int c = lane % kLanesPerRow + j * kLanesPerRow;
+          const bool some = kp != nullptr && c < row_pieces;
+          copy_async(kb + Body::piece_at(tok, c), some ? kp + c * 16 : (const char*)kv.k, some);
+          copy_async(vb + Body::piece_at(tok, c), some ? vp + c * 16 : (const char*)kv.v, some);
+        }
+      }
+      issued += kWarps;
+      if (issued < count) ahead.advance(p, kWarps, pieces);
+      look_up();
+    }
+    copy_commit();
+  };
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) issue(s);
+
+  Body body;
+  Place<kChunk> here = first;
+  int done = 0, stage = 0, next = warp;               // chunks of the CTA's part before `here`; this warp's next
+  float* join = (float*)(smem + S::kRing);
+  while (done < count) {
+    const RowSpan span = here.span;
+    const int n = min(span.c1 - here.chunk, count - done);       // chunks of this piece in this part
+    const int h = here.piece / p.n_split, split = here.piece - h * p.n_split;
+    const int head0 = h * p.per_kv + split * p.piece_heads;
+    const int heads = min(p.piece_heads, p.per_kv - split * p.piece_heads);
+    body.begin(p, here.row, head0, heads, lane, scratch);
+    for (; next < done + n; next += kWarps) {
+      copy_wait<kStages - 2>();
+      __syncwarp();
+      issue(stage == 0 ? kStages - 1 : stage - 1);
+      const uint32_t kb = ring + stage * S::kStageBytes;
+      body.step(p, kb, kb + kChunk * Body::kRowBytes, scratch, (here.chunk + next - done) * kChunk, span.lo, span.hi, lane);
+      stage = stage + 1 == kStages ? 0 : stage + 1;
+    }
+    // the new token's keys and values go to their page, once per kv head
+    if (p.k_new && split == 0 && here.chunk + n == span.c1 && warp == 0) {
+      const int t = span.hi - 1, pg = (int)div_by(t, p.page);
+      const int page = kv.table[(int64_t)here.row * kv.max_pages + pg];
+      if ((unsigned int)page < (unsigned int)kv.n_pages) {
+        const int64_t to = page * kv.page_stride + ((int64_t)h * kv.page_size + t - pg * kv.page_size) * kv.head_dim;
+        const int64_t from = here.row * p.new_stride + (int64_t)h * kv.head_dim;
+        for (int c = lane; c < row_pieces; c += 32) {
+          ((uint4*)((T*)kv.k + to))[c] = ((const uint4*)((const T*)p.k_new + from))[c];
+          ((uint4*)((T*)kv.v + to))[c] = ((const uint4*)((const T*)p.v_new + from))[c];
+        }
+      } else if (lane == 0) {
+        flag(kv.status, kStatusIndex);
+      }
+    }
+    // join the warps
+    body.stats(stat[warp], lane);
+#pragma unroll
+    for (int i = 0; i < kRegs; ++i) join[(warp * kRegs + i) * 32 + lane] = body.o[i];
+    __syncthreads();
+    const bool whole = here.chunk == span.c0 && n == span.c1 - span.c0;
+    const long long at = begin + done - (here.chunk - span.c0);          // the piece's first chunk on the line
+    const long long end = at + (span.c1 - span.c0);
+    const int cta0 = (int)(at / quota), cta1 = (int)((end - 1) / quota);
+    float* part = p.parts + (size_t)(2 * blockIdx.x + (cta0 == (int)blockIdx.x ? 1 : 0)) * kPart;
+    auto write_out = [&](int i, float x, float l) {
+      const int head = Body::head_of(i, lane), d = Body::dim_of(i, lane);
+      if (head < heads && d < kv.head_dim)
+        ((T*)p.out)[here.row * p.out_stride + (int64_t)(head0 + head) * kv.head_dim + d] = from_float<T>(l == 0.f ? 0.f : x / l);
+    };
+    auto write_lse = [&](int head, float m, float l) {
+      if (p.lse && head < heads)
+        p.lse[(int64_t)here.row * p.n_q_heads + head0 + head] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) * 0.6931471805599453f + logf(l);
+    };
+    constexpr int kShare = kRegs / kWarps;
+#pragma unroll 4
+    for (int u = 0; u < kShare; ++u) {
+      const int i = warp * kShare + u, head = Body::head_of(i, lane);
+      float m = -INFINITY, x = 0.f, l = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) m = fmaxf(m, stat[w][head].x);
+      const float off = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = exp2_fast(stat[w][head].x - off);
+        x = fmaf(f, join[(w * kRegs + i) * 32 + lane], x);
+        l = fmaf(f, stat[w][head].y, l);
+      }
+      if (whole) write_out(i, x, l);
+      else __stcg(&part[i * 32 + lane], x);
+    }
+    if (threadIdx.x < kMaxHeads) {
+      const int head = threadIdx.x;
+      if (head < heads) {
+        float m = -INFINITY, l = 0.f;
+        for (int w = 0; w < kWarps; ++w) m = fmaxf(m, stat[w][head].x);
+        const float off = m == -INFINITY ? 0.f : m;
+        for (int w = 0; w < kWarps; ++w) l = fmaf(exp2_fast(stat[w][head].x - off), stat[w][head].y, l);
+        if (whole) write_lse(head, m, l);
+        else __stcg((float2*)&part[kRegs * 32 + 2 * head], make_float2(m, l));
+      }
+    }
+    __syncthreads();
+    if (!whole) {
+      // the last of the CTAs that hold a part of this piece adds them, in CTA order
+      if (threadIdx.x == 0) {
+        __threadfence();
+        is_last = atomicAdd(&p.tickets[cta0], 1u) == (unsigned int)(cta1 - cta0);
+        if (is_last) p.tickets[cta0] = 0;
+      }
+      __syncthreads();
+      if (is_last) {
+        __threadfence();
+        float2* sums = (float2*)join;                                    // [head]: (m, l) of all parts
+        if (threadIdx.x < (unsigned)heads) {
+          float m = -INFINITY, l = 0.f;
+          for (int c = cta0; c <= cta1; ++c) {
+            const float2 s = __ldcg((const float2*)(p.parts + (size_t)(2 * c + (c == cta0 ? 1 : 0)) * kPart + kRegs * 32) + threadIdx.x);
+            const float m2 = fmaxf(m, s.x), off = m2 == -INFINITY ? 0.f : m2;
+            l = l * exp2_fast(m - off) + s.y * exp2_fast(s.x - off);
+            m = m2;
+          }
+          sums[threadIdx.x] = make_float2(m, l);
+          write_lse(threadIdx.x, m, l);
+        }
+        __syncthreads();
+#pragma unroll 2
+        for (int u = 0; u < kShare; ++u) {
+          const int i = warp * kShare + u, head = Body::head_of(i, lane);
+          if (head >= heads) continue;
+          const float2 s = sums[head];
+          const float off = s.x == -INFINITY ? 0.f : s.x;
+          float x = 0.f;
+#pragma unroll 4
+          for (int c = cta0; c <= cta1; ++c) {
+            const float* q = p.parts + (size_t)(2 * c + (c == cta0 ? 1 : 0)) * kPart;
+            const float f = exp2_fast(__ldcg(q + kRegs * 32 + 2 * head) - off);
+            x = fmaf(f, __ldcg(q + i * 32 + lane), x);
+          }
+          write_out(i, x, s.y);
+        }
+        __syncthreads();
+      }
+    }
+    done += n;
+    if (done < count) here.advance(p, n, pieces);
+  }
+  copy_wait<0>();
+}
+#endif
+
+// ---------------------------------------------------------------- launch
 
 static int attend_check(const pg_kv* kv, int n_q_heads, int group) {
   const int rc = kv_check(kv);
@@ -95,13 +729,58 @@ static int attend_check(const pg_kv* kv, int n_q_heads, int group) {
   return PG_OK;
 }
 
+// Query heads of a kv head beyond kMaxHeads are dealt to several pieces, evenly.
+static void split_heads(int per_kv, int* n_split, int* piece_heads) {
+  *n_split = (per_kv + kMaxHeads - 1) / kMaxHeads;
+  *piece_heads = (per_kv + *n_split - 1) / *n_split;
+}
+
+template <typename T, typename Body, int kStages, int kCtasPerSm>
+static int launch_attend(const AttendParams& p, cudaStream_t st) {
+  using S = AttendShared<T, Body, kStages>;
+  static_assert(S::kBytes <= 227 * 1024 / kCtasPerSm - 1024, "shared memory");
+  auto kernel = attend_kernel<T, Body, kStages, kCtasPerSm>;
+  PG_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes));
+  const long long most = (long long)p.kv.n_rows * p.kv.n_kv_heads * p.n_split *
+                         (((long long)p.kv.max_pages * p.kv.page_size + Body::kChunk - 1) / Body::kChunk);
+  const unsigned grid = (unsigned)(most < kSms * kCtasPerSm ? most : kSms * kCtasPerSm);
+  kernel<<<grid, kThreads, S::kBytes, st>>>(p);
+  PG_LAUNCH_CHECK();
+  return PG_OK;
+}
+
+template <typename T, template <int, int> class Body, int DP, int NT>
+static int launch_body(const AttendParams& p, cudaStream_t st) {
+  // 64: two CTAs of 96 KB rings to an SM; 128, 256: one of 128-192 KB
+  if constexpr (DP <= 64) return launch_attend<T, Body<DP, NT>, 3, sizeof(T) == 2 ? 2 : 1>(p, st);
+  else return launch_attend<T, Body<DP, NT>, sizeof(T) == 4 || (DP == 256 && NT == 2) ? 2 : 3, 1>(p, st);
+}
+
+template <typename T, template <int, int> class Body>
+static int launch_type(const AttendParams& p, cudaStream_t st) {
+  const int d = p.kv.head_dim;
+  if (p.piece_heads <= 8) {
+    if (d <= 64) return launch_body<T, Body, 64, 1>(p, st);
+    if (d <= 128) return launch_body<T, Body, 128, 1>(p, st);
+    return launch_body<T, Body, 256, 1>(p, st);
+  }
+  if (d <= 64) return launch_body<T, Body, 64, 2>(p, st);
+  if (d <= 128) return launch_body<T, Body, 128, 2>(p, st);
+  return launch_body<T, Body, 256, 2>(p, st);
+}
+
+template <int DP, int NT> using Bf16Body = MmaBody<__nv_bfloat16, DP, NT>;
+template <int DP, int NT> using F16Body = MmaBody<__half, DP, NT>;
+
 }  // namespace pg
 
 extern "C" {
 
 size_t pg_kv_attend_workspace_bytes(const pg_kv* kv, int32_t n_q_heads, int32_t group) {
   if (pg::attend_check(kv, n_q_heads, group) != PG_OK) return 0;
-  return 16;
+  // tickets first, so that their place depends on nothing
+  const size_t dp = kv->head_dim <= 64 ? 64 : kv->head_dim <= 128 ? 128 : 256;
+  return pg::kTicketBytes + (size_t)2 * pg::kMaxCtas * (dp * pg::kMaxHeads + 2 * pg::kMaxHeads) * sizeof(float);
 }
 
 int pg_kv_attend(const pg_kv* kv, int32_t layer, int32_t n_q_heads, const void* q, int64_t q_stride,
@@ -132,14 +811,15 @@ int pg_kv_attend(const pg_kv* kv, int32_t layer, int32_t n_q_heads, const void* 
   p.shared = group > 1 ? shared : nullptr;
   p.q_stride = q_stride; p.new_stride = new_stride; p.out_stride = out_stride;
   p.n_q_heads = n_q_heads; p.per_kv = n_q_heads / kv->n_kv_heads; p.group = group;
-  p.scale = scale;
-  const unsigned grid = (unsigned)(kv->n_rows * n_q_heads);
+  pg::split_heads(p.per_kv, &p.n_split, &p.piece_heads);
+  p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  p.page = pg::fast_div((uint32_t)kv->page_size);
+  p.tickets = (unsigned int*)workspace;
+  p.parts = (float*)((char*)workspace + pg::kTicketBytes);
   cudaStream_t st = (cudaStream_t)stream;
-  if (kv->dtype == PG_F32) pg::attend_kernel<float><<<grid, pg::kAttendWarps * 32, 0, st>>>(p);
-  else if (kv->dtype == PG_BF16) pg::attend_kernel<__nv_bfloat16><<<grid, pg::kAttendWarps * 32, 0, st>>>(p);
-  else pg::attend_kernel<__half><<<grid, pg::kAttendWarps * 32, 0, st>>>(p);
-  PG_LAUNCH_CHECK();
-  return PG_OK;
+  if (kv->dtype == PG_F32) return pg::launch_type<float, pg::F32Body>(p, st);
+  if (kv->dtype == PG_BF16) return pg::launch_type<__nv_bfloat16, pg::Bf16Body>(p, st);
+  return pg::launch_type<__half, pg::F16Body>(p, st);
 }
 
 }  // extern "C"
