@@ -402,9 +402,15 @@ struct F32Body {
 
 // ---------------------------------------------------------------- the line of chunks
 
-// Tokens [lo, hi) of a row that the line covers, and its chunks [c0, c1).
+// A piece costs its warp more than its chunks: queries are fetched, statistics joined, results
+// written.  On the line every piece is therefore kPieceCost units longer than it has chunks.
+constexpr int kPieceCost = 2;
+
+// Tokens [lo, hi) of a row that the line covers, in chunks [c0, c1).
 struct RowSpan {
   int lo, hi, c0, c1;
+  __device__ __forceinline__ int chunks() const { return c1 - c0; }
+  __device__ __forceinline__ int units() const { return c1 > c0 ? c1 - c0 + kPieceCost : 0; }
 };
 template <int kChunk>
 __device__ __forceinline__ RowSpan row_span(const AttendParams& p, int row) {
@@ -416,25 +422,20 @@ __device__ __forceinline__ RowSpan row_span(const AttendParams& p, int row) {
   return s;
 }
 
-// A place on the line: chunk `chunk` of (row, piece), pieces numbered (kv head, split) within the row.
+// A place on the line: unit `unit` of (row, piece), pieces numbered (kv head, split) within the row;
+// the first kPieceCost units of a piece stand for no chunk.
 template <int kChunk>
 struct Place {
-  int row, piece, chunk;
+  int row, piece, unit;
   RowSpan span;
-  __device__ __forceinline__ void advance(const AttendParams& p, int by, int pieces) {
-    chunk += by;
-    while (chunk >= span.c1) {
-      chunk -= span.c1 - span.c0;
-      if (++piece == pieces) {
-        piece = 0;
-        const int over = chunk - span.c0;
-        do {
-          if (++row >= p.kv.n_rows) return;
-          span = row_span<kChunk>(p, row);
-        } while (span.c1 == span.c0);
-        chunk = span.c0 + over;
-      }
-    }
+  __device__ __forceinline__ void next_piece(const AttendParams& p, int pieces) {
+    unit = 0;
+    if (++piece < pieces) return;
+    piece = 0;
+    do {
+      if (++row >= p.kv.n_rows) return;
+      span = row_span<kChunk>(p, row);
+    } while (span.c1 == span.c0);
   }
 };
 
@@ -444,6 +445,15 @@ struct AttendShared {
   static constexpr size_t kRing = (size_t)kWarps * kStages * kStageBytes;
   static constexpr size_t kJoin = (size_t)kWarps * Body::kRegs * 32 * 4;
   static constexpr size_t kBytes = kRing + kJoin + kWarps * Body::kQBytes;
+  static_assert(Body::kRegs * 128 <= kStages * kStageBytes, "a warp's ring takes a dump of its accumulator");
+};
+
+// What a warp leaves behind of a piece that it has not seen whole.
+struct Left {
+  int row, piece, chunk0;      // the piece, and the first of its chunks in this part
+  long long line;              // line unit of the piece's chunk 0
+  int chunks;                  // chunks of the whole piece
+  int any, goes_on;            // filled; continues in the next warp
 };
 
 template <typename T, typename Body, int kStages, int kCtasPerSm>
@@ -453,8 +463,11 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
   constexpr int kPart = kRegs * 32 + 2 * kMaxHeads;
   extern __shared__ __align__(1024) char smem[];
   __shared__ long long warp_sum_[kWarps];
-  __shared__ Place<kChunk> first;
-  __shared__ float2 stat[kWarps][kMaxHeads];
+  __shared__ int warp_max_[kWarps];
+  __shared__ Place<kChunk> first[kWarps];
+  __shared__ Left left[kWarps][2];                    // [0]: began before the warp's part, [1]: began in it
+  __shared__ float2 stat[kWarps][2][kMaxHeads];
+  __shared__ float2 sums[kMaxHeads];
   __shared__ int is_last;
   constexpr int kMaxEmpty = 64;
   __shared__ int n_empty, empty[kMaxEmpty];
@@ -462,10 +475,11 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int pieces = kv.n_kv_heads * p.n_split;
 
-  // Where this CTA's part of the line begins: sum of the rows' chunks, then the row that holds the cut.
+  // Planning: the rows' units are summed, then the rows that hold this CTA's cuts are found.
   const int per = (kv.n_rows + kThreads - 1) / kThreads;
   const int r0 = min((int)threadIdx.x * per, kv.n_rows), r1 = min(r0 + per, kv.n_rows);
   if (threadIdx.x == 0) n_empty = 0;
+  if (lane < 2) left[warp][lane].any = 0;
   __syncthreads();
   // rows without tokens, dealt round the CTAs, are cleared at the end of the planning
   auto clear_row = [&](int r, int from, int step) {
@@ -475,9 +489,11 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
       for (int i = from; i < p.n_q_heads; i += step) p.lse[(int64_t)r * p.n_q_heads + i] = -INFINITY;
   };
   long long mine = 0;
+  int longest = 0;
   for (int r = r0; r < r1; ++r) {
     const RowSpan s = row_span<kChunk>(p, r);
-    mine += s.c1 - s.c0;
+    mine += s.units();
+    longest = max(longest, s.chunks());
     if (s.c1 == s.c0 && r % gridDim.x == blockIdx.x) {
       const int at = atomicAdd(&n_empty, 1);
       if (at < kMaxEmpty) empty[at] = r;
@@ -490,43 +506,68 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
     const long long y = __shfl_up_sync(0xFFFFFFFFu, upto, d);
     if (lane >= d) upto += y;
   }
-  if (lane == 31) warp_sum_[warp] = upto;
+  longest = __reduce_max_sync(0xFFFFFFFFu, longest);
+  if (lane == 31) {
+    warp_sum_[warp] = upto;
+    warp_max_[warp] = longest;
+  }
   __syncthreads();
   long long all = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
     if (w < warp) upto += warp_sum_[w];
     all += warp_sum_[w];
+    longest = max(longest, warp_max_[w]);
   }
   const long long total = all * pieces;
-  // equal parts; but a part is not shorter than an average (row, head) if that is at most one chunk a warp
-  long long quota = (total + gridDim.x - 1) / gridDim.x;
-  const long long avg = (all + kv.n_rows - 1) / kv.n_rows;
-  quota = max(quota, min(avg, (long long)kWarps));
-  const long long begin = blockIdx.x * quota;
-  const int count = (int)max(0ll, min(quota, total - begin));
-  if (count > 0) {
-    const long long before = (upto - mine) * pieces;
-    if (begin >= before && begin < before + mine * pieces) {
-      Place<kChunk> at;
-      long long rest = begin - before;
+  // Few and short rows: a CTA for every (row, piece), so that nothing is joined across CTAs.
+  const bool by_piece = (long long)kv.n_rows * pieces <= gridDim.x && longest <= kWarps * 4;
+  long long quota = 0, begin = 0;                     // units of a CTA's part, and its first
+  long long wbegin, wend;                             // this warp's units
+  if (by_piece) {
+    const int r = blockIdx.x / pieces;
+    if (r < kv.n_rows) {
+      const RowSpan s = row_span<kChunk>(p, r);
+      const int share = (s.chunks() + kWarps - 1) / kWarps, from = min(warp * share, s.chunks());
+      wbegin = kPieceCost + from;                     // counted from the piece's own start
+      wend = kPieceCost + min(from + share, s.chunks());
+      if (lane == 0) {
+        first[warp].row = r;
+        first[warp].piece = blockIdx.x - r * pieces;
+        first[warp].unit = (int)wbegin;
+        first[warp].span = s;
+      }
+    } else {
+      wbegin = wend = 0;
+    }
+  } else {
+    const long long share = (total + (long long)gridDim.x * kWarps - 1) / ((long long)gridDim.x * kWarps);
+    quota = share * kWarps;
+    begin = blockIdx.x * quota;
+    wbegin = min(begin + warp * share, total);
+    wend = min(wbegin + share, total);
+    const long long before = (upto - mine) * pieces, end = before + mine * pieces;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const long long cut = begin + w * share;
+      if (cut < before || cut >= end) continue;
+      long long rest = cut - before;
       for (int r = r0; r < r1; ++r) {
-        at.span = row_span<kChunk>(p, r);
-        const int n = at.span.c1 - at.span.c0;
-        if (rest < (long long)n * pieces) {
-          at.row = r;
-          at.piece = (int)(rest / n);
-          at.chunk = at.span.c0 + (int)(rest - (long long)at.piece * n);
+        const RowSpan s = row_span<kChunk>(p, r);
+        const long long n = (long long)s.units() * pieces;
+        if (rest < n) {
+          first[w].row = r;
+          first[w].piece = (int)(rest / s.units());
+          first[w].unit = (int)(rest - (long long)first[w].piece * s.units());
+          first[w].span = s;
           break;
         }
-        rest -= (long long)n * pieces;
+        rest -= n;
       }
-      first = at;
     }
   }
-  for (int i = 0; i < min(n_empty, kMaxEmpty); ++i) clear_row(empty[i], threadIdx.x, kThreads);
-  if (count == 0) return;
   __syncthreads();
+  for (int i = 0; i < min(n_empty, kMaxEmpty); ++i) clear_row(empty[i], threadIdx.x, kThreads);
 
   // Loads.  A lane looks up the page of one token of the chunk (one chunk ahead of its copies); the
   // copies then go two or more tokens at a time, 16 bytes a lane.
@@ -536,20 +577,23 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
   constexpr int kRowsPerCopy = 32 / kLanesPerRow;
   constexpr int kPiecesPerLane = Body::kRowBytes / 16 / kLanesPerRow;
   const int row_pieces = kv.head_dim * (int)sizeof(T) / 16;
-  Place<kChunk> ahead = first;
-  int issued = warp;                                  // this warp's next chunk, counted from the CTA's first
-  if (issued < count) ahead.advance(p, warp, pieces);
+  Place<kChunk> ahead = first[warp];
+  long long ahead_at = wbegin;                        // line unit of `ahead`, at a chunk or past the end
+  if (ahead_at < wend && ahead.unit < kPieceCost) {
+    ahead_at += kPieceCost - ahead.unit;
+    ahead.unit = kPieceCost;
+  }
   int entry = 0;
   auto look_up = [&]() {
-    if (issued >= count) return;
-    const int t = ahead.chunk * kChunk + lane;
+    if (ahead_at >= wend) return;
+    const int t = (ahead.span.c0 + ahead.unit - kPieceCost) * kChunk + lane;
     if (lane < kChunk && t < ahead.span.hi && t >= ahead.span.lo)
       entry = kv.table[(int64_t)ahead.row * kv.max_pages + div_by(t, p.page)];
   };
   look_up();
   auto issue = [&](int stage) {
-    if (issued < count) {
-      const int t = ahead.chunk * kChunk + lane, h = ahead.piece / p.n_split;
+    if (ahead_at < wend) {
+      const int t = (ahead.span.c0 + ahead.unit - kPieceCost) * kChunk + lane, h = ahead.piece / p.n_split;
       const bool in = lane < kChunk && t < ahead.span.hi && t >= ahead.span.lo;
       const T *ks = nullptr, *vs = nullptr;           // null: zeros
       if (in) {
@@ -580,8 +624,12 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
           copy_async(vb + Body::piece_at(tok, c), some ? vp + c * 16 : (const char*)kv.v, some);
         }
       }
-      issued += kWarps;
-      if (issued < count) ahead.advance(p, kWarps, pieces);
+      ++ahead_at;
+      if (++ahead.unit == ahead.span.units()) {
+        if (ahead_at < wend) ahead.next_piece(p, pieces);
+        ahead_at += kPieceCost;
+        ahead.unit = kPieceCost;
+      }
       look_up();
     }
     copy_commit();
@@ -590,89 +638,139 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
   for (int s = 0; s < kStages - 1; ++s) issue(s);
 
   Body body;
-  Place<kChunk> here = first;
-  int done = 0, stage = 0, next = warp;               // chunks of the CTA's part before `here`; this warp's next
-  float* join = (float*)(smem + S::kRing);
-  while (done < count) {
+  Place<kChunk> here = first[warp];
+  long long pos = wbegin;
+  int stage = 0;
+  float* join = (float*)(smem + S::kRing) + warp * kRegs * 32;
+  auto out_at = [&](int row, int head) { return (T*)p.out + row * p.out_stride + (int64_t)head * kv.head_dim; };
+  auto lse_of = [&](float m, float l) {
+    return l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) * 0.6931471805599453f + logf(l);
+  };
+  while (pos < wend) {
     const RowSpan span = here.span;
-    const int n = min(span.c1 - here.chunk, count - done);       // chunks of this piece in this part
-    const int h = here.piece / p.n_split, split = here.piece - h * p.n_split;
-    const int head0 = h * p.per_kv + split * p.piece_heads;
-    const int heads = min(p.piece_heads, p.per_kv - split * p.piece_heads);
-    body.begin(p, here.row, head0, heads, lane, scratch);
-    for (; next < done + n; next += kWarps) {
-      copy_wait<kStages - 2>();
-      __syncwarp();
-      issue(stage == 0 ? kStages - 1 : stage - 1);
-      const uint32_t kb = ring + stage * S::kStageBytes;
-      body.step(p, kb, kb + kChunk * Body::kRowBytes, scratch, (here.chunk + next - done) * kChunk, span.lo, span.hi, lane);
-      stage = stage + 1 == kStages ? 0 : stage + 1;
-    }
-    // the new token's keys and values go to their page, once per kv head
-    if (p.k_new && split == 0 && here.chunk + n == span.c1 && warp == 0) {
-      const int t = span.hi - 1, pg = (int)div_by(t, p.page);
-      const int page = kv.table[(int64_t)here.row * kv.max_pages + pg];
-      if ((unsigned int)page < (unsigned int)kv.n_pages) {
-        const int64_t to = page * kv.page_stride + ((int64_t)h * kv.page_size + t - pg * kv.page_size) * kv.head_dim;
-        const int64_t from = here.row * p.new_stride + (int64_t)h * kv.head_dim;
-        for (int c = lane; c < row_pieces; c += 32) {
-          ((uint4*)((T*)kv.k + to))[c] = ((const uint4*)((const T*)p.k_new + from))[c];
-          ((uint4*)((T*)kv.v + to))[c] = ((const uint4*)((const T*)p.v_new + from))[c];
+    const int n_units = (int)min((long long)(span.units() - here.unit), wend - pos);
+    const int j0 = max(here.unit - kPieceCost, 0), j1 = here.unit + n_units - kPieceCost;
+    if (j1 > j0) {
+      const int h = here.piece / p.n_split, split = here.piece - h * p.n_split;
+      const int head0 = h * p.per_kv + split * p.piece_heads;
+      const int heads = min(p.piece_heads, p.per_kv - split * p.piece_heads);
+      body.begin(p, here.row, head0, heads, lane, scratch);
+      for (int j = j0; j < j1; ++j) {
+        copy_wait<kStages - 2>();
+        __syncwarp();
+        issue(stage == 0 ? kStages - 1 : stage - 1);
+        const uint32_t kb = ring + stage * S::kStageBytes;
+        body.step(p, kb, kb + kChunk * Body::kRowBytes, scratch, (span.c0 + j) * kChunk, span.lo, span.hi, lane);
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+      }
+      // the new token's keys and values go to their page, once per kv head
+      if (p.k_new && split == 0 && j1 == span.chunks()) {
+        const int t = span.hi - 1, pg = (int)div_by(t, p.page);
+        const int page = kv.table[(int64_t)here.row * kv.max_pages + pg];
+        if ((unsigned int)page < (unsigned int)kv.n_pages) {
+          const int64_t to = page * kv.page_stride + ((int64_t)h * kv.page_size + t - pg * kv.page_size) * kv.head_dim;
+          const int64_t from = here.row * p.new_stride + (int64_t)h * kv.head_dim;
+          for (int c = lane; c < row_pieces; c += 32) {
+            ((uint4*)((T*)kv.k + to))[c] = ((const uint4*)((const T*)p.k_new + from))[c];
+            ((uint4*)((T*)kv.v + to))[c] = ((const uint4*)((const T*)p.v_new + from))[c];
+          }
+        } else if (lane == 0) {
+          flag(kv.status, kStatusIndex);
         }
-      } else if (lane == 0) {
-        flag(kv.status, kStatusIndex);
+      }
+      const int slot = j0 == 0 ? 1 : 0;
+      body.stats(stat[warp][slot], lane);
+      if (j0 == 0 && j1 == span.chunks()) {            // seen whole: nothing to join
+        __syncwarp();
+        const float2* st = stat[warp][1];
+#pragma unroll
+        for (int i = 0; i < kRegs; ++i) {
+          const int head = Body::head_of(i, lane), d = Body::dim_of(i, lane);
+          const float l = st[head].y;
+          if (head < heads && d < kv.head_dim) out_at(here.row, head0 + head)[d] = from_float<T>(l == 0.f ? 0.f : body.o[i] / l);
+        }
+        if (p.lse && lane < heads) p.lse[(int64_t)here.row * p.n_q_heads + head0 + lane] = lse_of(st[lane].x, st[lane].y);
+        __syncwarp();
+      } else {
+        // a piece that goes on past this warp is its last: its loads are done, and the ring is free
+        if (j0 == 0) copy_wait<0>();
+        __syncwarp();
+        float* dump = j0 == 0 ? (float*)(smem + (size_t)warp * kStages * S::kStageBytes) : join;
+#pragma unroll
+        for (int i = 0; i < kRegs; ++i) dump[i * 32 + lane] = body.o[i];
+        if (lane == 0) {
+          Left& x = left[warp][slot];
+          x.row = here.row;
+          x.piece = here.piece;
+          x.chunk0 = j0;
+          x.line = pos - here.unit + kPieceCost;
+          x.chunks = span.chunks();
+          x.goes_on = j1 < span.chunks();
+          x.any = 1;
+        }
       }
     }
-    // join the warps
-    body.stats(stat[warp], lane);
-#pragma unroll
-    for (int i = 0; i < kRegs; ++i) join[(warp * kRegs + i) * 32 + lane] = body.o[i];
-    __syncthreads();
-    const bool whole = here.chunk == span.c0 && n == span.c1 - span.c0;
-    const long long at = begin + done - (here.chunk - span.c0);          // the piece's first chunk on the line
-    const long long end = at + (span.c1 - span.c0);
-    const int cta0 = (int)(at / quota), cta1 = (int)((end - 1) / quota);
-    float* part = p.parts + (size_t)(2 * blockIdx.x + (cta0 == (int)blockIdx.x ? 1 : 0)) * kPart;
-    auto write_out = [&](int i, float x, float l) {
-      const int head = Body::head_of(i, lane), d = Body::dim_of(i, lane);
-      if (head < heads && d < kv.head_dim)
-        ((T*)p.out)[here.row * p.out_stride + (int64_t)(head0 + head) * kv.head_dim + d] = from_float<T>(l == 0.f ? 0.f : x / l);
-    };
-    auto write_lse = [&](int head, float m, float l) {
-      if (p.lse && head < heads)
-        p.lse[(int64_t)here.row * p.n_q_heads + head0 + head] = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) * 0.6931471805599453f + logf(l);
-    };
+    pos += n_units;
+    if (pos < wend) here.next_piece(p, pieces);
+    else break;
+  }
+  copy_wait<0>();
+  __syncthreads();
+
+  // Pieces that the warps of this CTA, or several CTAs, have shared: a run of dumps is slot s0 of warp w0
+  // and then slot 0 of the warps after it, up to w1.
+  auto dump_of = [&](int w, int s) {
+    return s ? (const float*)(smem + (size_t)w * kStages * S::kStageBytes) : (const float*)(smem + S::kRing) + w * kRegs * 32;
+  };
+  for (int k = 0; k < 2 * kWarps;) {
+    const int w0 = k >> 1, s0 = k & 1;
+    if (!left[w0][s0].any) {
+      ++k;
+      continue;
+    }
+    const Left x = left[w0][s0];
+    int w1 = w0;
+    bool goes_on = x.goes_on;
+    while (goes_on && w1 + 1 < kWarps) goes_on = left[++w1][0].goes_on;
+    k = (w1 > w0 ? 2 * w1 : k) + 1;
+    const bool whole = x.chunk0 == 0 && !goes_on;
+    const int h = x.piece / p.n_split, split = x.piece - h * p.n_split;
+    const int head0 = h * p.per_kv + split * p.piece_heads;
+    const int heads = min(p.piece_heads, p.per_kv - split * p.piece_heads);
+    const int cta0 = whole ? 0 : (int)(x.line / quota), cta1 = whole ? 0 : (int)((x.line + x.chunks - 1) / quota);
+    auto part_of = [&](int c) { return p.parts + (size_t)(2 * c + (c == cta0 ? 1 : 0)) * kPart; };
+    float* part = whole ? nullptr : part_of(blockIdx.x);
     constexpr int kShare = kRegs / kWarps;
 #pragma unroll 4
     for (int u = 0; u < kShare; ++u) {
-      const int i = warp * kShare + u, head = Body::head_of(i, lane);
-      float m = -INFINITY, x = 0.f, l = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) m = fmaxf(m, stat[w][head].x);
+      const int i = warp * kShare + u, head = Body::head_of(i, lane), d = Body::dim_of(i, lane);
+      float m = -INFINITY, v = 0.f, l = 0.f;
+      for (int w = w0; w <= w1; ++w) m = fmaxf(m, stat[w][w == w0 ? s0 : 0][head].x);
       const float off = m == -INFINITY ? 0.f : m;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float f = exp2_fast(stat[w][head].x - off);
-        x = fmaf(f, join[(w * kRegs + i) * 32 + lane], x);
-        l = fmaf(f, stat[w][head].y, l);
+      for (int w = w0; w <= w1; ++w) {
+        const int s = w == w0 ? s0 : 0;
+        const float f = exp2_fast(stat[w][s][head].x - off);
+        v = fmaf(f, dump_of(w, s)[i * 32 + lane], v);
+        l = fmaf(f, stat[w][s][head].y, l);
       }
-      if (whole) write_out(i, x, l);
-      else __stcg(&part[i * 32 + lane], x);
+      if (!whole) __stcg(&part[i * 32 + lane], v);
+      else if (head < heads && d < kv.head_dim) out_at(x.row, head0 + head)[d] = from_float<T>(l == 0.f ? 0.f : v / l);
     }
-    if (threadIdx.x < kMaxHeads) {
+    if ((int)threadIdx.x < heads) {
       const int head = threadIdx.x;
-      if (head < heads) {
-        float m = -INFINITY, l = 0.f;
-        for (int w = 0; w < kWarps; ++w) m = fmaxf(m, stat[w][head].x);
-        const float off = m == -INFINITY ? 0.f : m;
-        for (int w = 0; w < kWarps; ++w) l = fmaf(exp2_fast(stat[w][head].x - off), stat[w][head].y, l);
-        if (whole) write_lse(head, m, l);
-        else __stcg((float2*)&part[kRegs * 32 + 2 * head], make_float2(m, l));
+      float m = -INFINITY, l = 0.f;
+      for (int w = w0; w <= w1; ++w) m = fmaxf(m, stat[w][w == w0 ? s0 : 0][head].x);
+      const float off = m == -INFINITY ? 0.f : m;
+      for (int w = w0; w <= w1; ++w) {
+        const float2 s = stat[w][w == w0 ? s0 : 0][head];
+        l = fmaf(exp2_fast(s.x - off), s.y, l);
       }
+      if (!whole) __stcg((float2*)&part[kRegs * 32 + 2 * head], make_float2(m, l));
+      else if (p.lse) p.lse[(int64_t)x.row * p.n_q_heads + head0 + head] = lse_of(m, l);
     }
-    __syncthreads();
     if (!whole) {
       // the last of the CTAs that hold a part of this piece adds them, in CTA order
+      __syncthreads();
       if (threadIdx.x == 0) {
         __threadfence();
         is_last = atomicAdd(&p.tickets[cta0], 1u) == (unsigned int)(cta1 - cta0);
@@ -681,41 +779,36 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
       __syncthreads();
       if (is_last) {
         __threadfence();
-        float2* sums = (float2*)join;                                    // [head]: (m, l) of all parts
-        if (threadIdx.x < (unsigned)heads) {
+        if ((int)threadIdx.x < heads) {
           float m = -INFINITY, l = 0.f;
           for (int c = cta0; c <= cta1; ++c) {
-            const float2 s = __ldcg((const float2*)(p.parts + (size_t)(2 * c + (c == cta0 ? 1 : 0)) * kPart + kRegs * 32) + threadIdx.x);
+            const float2 s = __ldcg((const float2*)(part_of(c) + kRegs * 32) + threadIdx.x);
             const float m2 = fmaxf(m, s.x), off = m2 == -INFINITY ? 0.f : m2;
             l = l * exp2_fast(m - off) + s.y * exp2_fast(s.x - off);
             m = m2;
           }
           sums[threadIdx.x] = make_float2(m, l);
-          write_lse(threadIdx.x, m, l);
+          if (p.lse) p.lse[(int64_t)x.row * p.n_q_heads + head0 + threadIdx.x] = lse_of(m, l);
         }
         __syncthreads();
 #pragma unroll 2
         for (int u = 0; u < kShare; ++u) {
-          const int i = warp * kShare + u, head = Body::head_of(i, lane);
+          const int i = warp * kShare + u, head = Body::head_of(i, lane), d = Body::dim_of(i, lane);
           if (head >= heads) continue;
           const float2 s = sums[head];
           const float off = s.x == -INFINITY ? 0.f : s.x;
-          float x = 0.f;
+          float v = 0.f;
 #pragma unroll 4
           for (int c = cta0; c <= cta1; ++c) {
-            const float* q = p.parts + (size_t)(2 * c + (c == cta0 ? 1 : 0)) * kPart;
-            const float f = exp2_fast(__ldcg(q + kRegs * 32 + 2 * head) - off);
-            x = fmaf(f, __ldcg(q + i * 32 + lane), x);
+            const float* q = part_of(c);
+            v = fmaf(exp2_fast(__ldcg(q + kRegs * 32 + 2 * head) - off), __ldcg(q + i * 32 + lane), v);
           }
-          write_out(i, x, s.y);
+          if (d < kv.head_dim) out_at(x.row, head0 + head)[d] = from_float<T>(s.y == 0.f ? 0.f : v / s.y);
         }
         __syncthreads();
       }
     }
-    done += n;
-    if (done < count) here.advance(p, n, pieces);
   }
-  copy_wait<0>();
 }
 #endif
 
