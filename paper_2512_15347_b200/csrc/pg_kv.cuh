@@ -67,15 +67,16 @@ __device__ __forceinline__ void flag(int32_t* status, int bit) {
   if (status) atomicOr(status, bit);
 }
 
-// Tokens of a row, kept inside what its table can hold.
-__device__ __forceinline__ int row_len(const KvView& kv, int row) {
-  const int n = kv.len[row], most = kv.max_pages * kv.page_size;
+// A row's length, kept inside what its table can hold.
+__device__ __forceinline__ int checked_len(const KvView& kv, int n) {
+  const int most = kv.max_pages * kv.page_size;
   if ((unsigned int)n > (unsigned int)most) {
     flag(kv.status, kStatusIndex);
     return n < 0 ? 0 : most;
   }
   return n;
 }
+__device__ __forceinline__ int row_len(const KvView& kv, int row) { return checked_len(kv, kv.len[row]); }
 
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }

@@ -26,11 +26,9 @@
 namespace pg {
 
 constexpr int kSms = 148;
-constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32;
-constexpr int kMaxCtas = kSms * 2;
+constexpr int kMaxWarps = 8;
 constexpr int kMaxHeads = 16;                 // query heads of a (row, kv head) piece
-constexpr size_t kTicketBytes = 4096;         // >= 4 * kMaxCtas
+constexpr size_t kTicketBytes = 4096;         // >= 4 * kSms
 
 // n / d for 0 <= n < 2^31 by a multiplication (d >= 1): m = ceil(2^(32+s) / d), s = ceil(log2 d) - 1.
 struct FastDiv {
@@ -59,8 +57,9 @@ struct AttendParams {
   int n_split, piece_heads;                   // pieces per kv head, query heads of a piece
   float scale_log2;                           // scale * log2(e)
   FastDiv page;
-  unsigned int* tickets;                      // [kMaxCtas], zero between calls
+  unsigned int* tickets;                      // [CTAs], zero between calls
   float* parts;                               // [2 * CTAs][REGS * 32 + 2 * kMaxHeads]
+  float* dumps;                               // [CTAs][kWarps][REGS * 32]
 };
 
 #ifdef __CUDACC__
@@ -123,7 +122,7 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, __half) {
 // sum l is taken before the rounding), which adds less to the result than its own last rounding.
 template <typename T, int DP, int NT>
 struct MmaBody {
-  static constexpr int kChunk = DP > 128 ? 16 : 32;
+  static constexpr int kChunk = DP > 64 ? 16 : 32;
   static constexpr int kTiles = kChunk / 16;
   static constexpr int kRegs = DP / 16 * NT * 4;
   static constexpr int kRowBytes = DP * 2;
@@ -134,6 +133,9 @@ struct MmaBody {
 
   static __device__ __forceinline__ int head_of(int i, int lane) { return (i >> 2) % NT * 8 + (lane & 3) * 2 + (i & 1); }
   static __device__ __forceinline__ int dim_of(int i, int lane) { return (i >> 2) / NT * 16 + (lane >> 2) + ((i >> 1) & 1) * 8; }
+  // of four registers 4 u .. 4 u + 3, the heads are those of the first and of the kSecond-th; which one each has
+  static constexpr int kSecond = 1;
+  static __device__ __forceinline__ int pair_of(int j) { return j & 1; }
   // 16-byte piece c of token row t: pieces are swizzled so that eight rows' equal pieces hit all banks
   static __device__ __forceinline__ uint32_t piece_at(int t, int c) { return t * kRowBytes + ((c ^ (t & 7)) << 4); }
 
@@ -291,6 +293,8 @@ struct F32Body {
     const int j = i % kPer;
     return kPer == 2 ? lane * 2 + j : (j >> 2) * 128 + lane * 4 + (j & 3);
   }
+  static constexpr int kSecond = 2;
+  static __device__ __forceinline__ int pair_of(int j) { return kPer == 2 ? j >> 1 : 0; }
   static __device__ __forceinline__ uint32_t piece_at(int t, int c) { return t * kRowBytes + (c << 4); }
 
   __device__ __forceinline__ void begin(const AttendParams& p, int row, int head0, int heads, int lane, char* scratch) {
@@ -404,7 +408,7 @@ struct F32Body {
 
 // A piece costs its warp more than its chunks: queries are fetched, statistics joined, results
 // written.  On the line every piece is therefore kPieceCost units longer than it has chunks.
-constexpr int kPieceCost = 2;
+constexpr int kPieceCost = 8;
 
 // Tokens [lo, hi) of a row that the line covers, in chunks [c0, c1).
 struct RowSpan {
@@ -413,9 +417,9 @@ struct RowSpan {
   __device__ __forceinline__ int units() const { return c1 > c0 ? c1 - c0 + kPieceCost : 0; }
 };
 template <int kChunk>
-__device__ __forceinline__ RowSpan row_span(const AttendParams& p, int row) {
+__device__ __forceinline__ RowSpan row_span(const AttendParams& p, int row, int len) {
   RowSpan s;
-  s.hi = row_len(p.kv, row);
+  s.hi = checked_len(p.kv, len);
   s.lo = 0;
   s.c0 = s.lo / kChunk;
   s.c1 = s.hi > s.lo ? (s.hi + kChunk - 1) / kChunk : s.c0;
@@ -427,24 +431,28 @@ __device__ __forceinline__ RowSpan row_span(const AttendParams& p, int row) {
 template <int kChunk>
 struct Place {
   int row, piece, unit;
+  int next_len;                // of the next row, fetched long before it is needed
   RowSpan span;
+  __device__ __forceinline__ void fetch(const AttendParams& p) {
+    if (row + 1 < p.kv.n_rows) next_len = p.kv.len[row + 1];
+  }
   __device__ __forceinline__ void next_piece(const AttendParams& p, int pieces) {
     unit = 0;
     if (++piece < pieces) return;
     piece = 0;
     do {
       if (++row >= p.kv.n_rows) return;
-      span = row_span<kChunk>(p, row);
+      span = row_span<kChunk>(p, row, next_len);
+      fetch(p);
     } while (span.c1 == span.c0);
   }
 };
 
-template <typename T, typename Body, int kStages>
+template <typename T, typename Body, int kWarps, int kStages>
 struct AttendShared {
   static constexpr int kStageBytes = 2 * Body::kChunk * Body::kRowBytes;
   static constexpr size_t kRing = (size_t)kWarps * kStages * kStageBytes;
-  static constexpr size_t kJoin = (size_t)kWarps * Body::kRegs * 32 * 4;
-  static constexpr size_t kBytes = kRing + kJoin + kWarps * Body::kQBytes;
+  static constexpr size_t kBytes = kRing + kWarps * Body::kQBytes;
   static_assert(Body::kRegs * 128 <= kStages * kStageBytes, "a warp's ring takes a dump of its accumulator");
 };
 
@@ -456,9 +464,10 @@ struct Left {
   int any, goes_on;            // filled; continues in the next warp
 };
 
-template <typename T, typename Body, int kStages, int kCtasPerSm>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __grid_constant__ AttendParams p) {
-  using S = AttendShared<T, Body, kStages>;
+template <typename T, typename Body, int kWarps, int kStages>
+__global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_constant__ AttendParams p) {
+  using S = AttendShared<T, Body, kWarps, kStages>;
+  constexpr int kThreads = kWarps * 32;
   constexpr int kChunk = Body::kChunk, kRegs = Body::kRegs;
   constexpr int kPart = kRegs * 32 + 2 * kMaxHeads;
   extern __shared__ __align__(1024) char smem[];
@@ -468,6 +477,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
   __shared__ Left left[kWarps][2];                    // [0]: began before the warp's part, [1]: began in it
   __shared__ float2 stat[kWarps][2][kMaxHeads];
   __shared__ float2 sums[kMaxHeads];
+  __shared__ float factor[kWarps][kMaxHeads];
   __shared__ int is_last;
   constexpr int kMaxEmpty = 64;
   __shared__ int n_empty, empty[kMaxEmpty];
@@ -491,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
   long long mine = 0;
   int longest = 0;
   for (int r = r0; r < r1; ++r) {
-    const RowSpan s = row_span<kChunk>(p, r);
+    const RowSpan s = row_span<kChunk>(p, r, kv.len[r]);
     mine += s.units();
     longest = max(longest, s.chunks());
     if (s.c1 == s.c0 && r % gridDim.x == blockIdx.x) {
@@ -527,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
   if (by_piece) {
     const int r = blockIdx.x / pieces;
     if (r < kv.n_rows) {
-      const RowSpan s = row_span<kChunk>(p, r);
+      const RowSpan s = row_span<kChunk>(p, r, kv.len[r]);
       const int share = (s.chunks() + kWarps - 1) / kWarps, from = min(warp * share, s.chunks());
       wbegin = kPieceCost + from;                     // counted from the piece's own start
       wend = kPieceCost + min(from + share, s.chunks());
@@ -553,7 +563,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
       if (cut < before || cut >= end) continue;
       long long rest = cut - before;
       for (int r = r0; r < r1; ++r) {
-        const RowSpan s = row_span<kChunk>(p, r);
+        const RowSpan s = row_span<kChunk>(p, r, kv.len[r]);
         const long long n = (long long)s.units() * pieces;
         if (rest < n) {
           first[w].row = r;
@@ -572,12 +582,13 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
   // Loads.  A lane looks up the page of one token of the chunk (one chunk ahead of its copies); the
   // copies then go two or more tokens at a time, 16 bytes a lane.
   const uint32_t ring = shared_addr(smem) + warp * kStages * S::kStageBytes;
-  char* scratch = smem + S::kRing + S::kJoin + warp * Body::kQBytes;
+  char* scratch = smem + S::kRing + warp * Body::kQBytes;
   constexpr int kLanesPerRow = Body::kRowBytes / 16 < 32 ? Body::kRowBytes / 16 : 32;
   constexpr int kRowsPerCopy = 32 / kLanesPerRow;
   constexpr int kPiecesPerLane = Body::kRowBytes / 16 / kLanesPerRow;
   const int row_pieces = kv.head_dim * (int)sizeof(T) / 16;
   Place<kChunk> ahead = first[warp];
+  if (wbegin < wend) ahead.fetch(p);
   long long ahead_at = wbegin;                        // line unit of `ahead`, at a chunk or past the end
   if (ahead_at < wend && ahead.unit < kPieceCost) {
     ahead_at += kPieceCost - ahead.unit;
@@ -637,11 +648,34 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) issue(s);
 
+  // While the first chunks are on their way: the new tokens' keys and values go to their pages, a warp
+  // for each row and kv head.
+  if (p.k_new) {
+    for (int64_t i = (int64_t)blockIdx.x * kWarps + warp; i < (int64_t)kv.n_rows * kv.n_kv_heads; i += (int64_t)gridDim.x * kWarps) {
+      const int r = (int)(i / kv.n_kv_heads), h = (int)(i - (int64_t)r * kv.n_kv_heads);
+      const int t = checked_len(kv, kv.len[r]) - 1;
+      if (t < 0) continue;
+      const int pg = (int)div_by(t, p.page), page = kv.table[(int64_t)r * kv.max_pages + pg];
+      if ((unsigned int)page >= (unsigned int)kv.n_pages) {
+        if (lane == 0) flag(kv.status, kStatusIndex);
+        continue;
+      }
+      const int64_t to = page * kv.page_stride + ((int64_t)h * kv.page_size + t - pg * kv.page_size) * kv.head_dim;
+      const int64_t from = r * p.new_stride + (int64_t)h * kv.head_dim;
+      for (int c = lane; c < row_pieces; c += 32) {
+        const uint4 a = ((const uint4*)((const T*)p.k_new + from))[c], b = ((const uint4*)((const T*)p.v_new + from))[c];
+        ((uint4*)((T*)kv.k + to))[c] = a;
+        ((uint4*)((T*)kv.v + to))[c] = b;
+      }
+    }
+  }
+
   Body body;
   Place<kChunk> here = first[warp];
+  if (wbegin < wend) here.fetch(p);
   long long pos = wbegin;
   int stage = 0;
-  float* join = (float*)(smem + S::kRing) + warp * kRegs * 32;
+  float* dumps = p.dumps + (size_t)blockIdx.x * kWarps * kRegs * 32;
   auto out_at = [&](int row, int head) { return (T*)p.out + row * p.out_stride + (int64_t)head * kv.head_dim; };
   auto lse_of = [&](float m, float l) {
     return l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) * 0.6931471805599453f + logf(l);
@@ -663,21 +697,6 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
         body.step(p, kb, kb + kChunk * Body::kRowBytes, scratch, (span.c0 + j) * kChunk, span.lo, span.hi, lane);
         stage = stage + 1 == kStages ? 0 : stage + 1;
       }
-      // the new token's keys and values go to their page, once per kv head
-      if (p.k_new && split == 0 && j1 == span.chunks()) {
-        const int t = span.hi - 1, pg = (int)div_by(t, p.page);
-        const int page = kv.table[(int64_t)here.row * kv.max_pages + pg];
-        if ((unsigned int)page < (unsigned int)kv.n_pages) {
-          const int64_t to = page * kv.page_stride + ((int64_t)h * kv.page_size + t - pg * kv.page_size) * kv.head_dim;
-          const int64_t from = here.row * p.new_stride + (int64_t)h * kv.head_dim;
-          for (int c = lane; c < row_pieces; c += 32) {
-            ((uint4*)((T*)kv.k + to))[c] = ((const uint4*)((const T*)p.k_new + from))[c];
-            ((uint4*)((T*)kv.v + to))[c] = ((const uint4*)((const T*)p.v_new + from))[c];
-          }
-        } else if (lane == 0) {
-          flag(kv.status, kStatusIndex);
-        }
-      }
       const int slot = j0 == 0 ? 1 : 0;
       body.stats(stat[warp][slot], lane);
       if (j0 == 0 && j1 == span.chunks()) {            // seen whole: nothing to join
@@ -695,9 +714,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
         // a piece that goes on past this warp is its last: its loads are done, and the ring is free
         if (j0 == 0) copy_wait<0>();
         __syncwarp();
-        float* dump = j0 == 0 ? (float*)(smem + (size_t)warp * kStages * S::kStageBytes) : join;
+        float* dump = j0 == 0 ? (float*)(smem + (size_t)warp * kStages * S::kStageBytes) : dumps + warp * kRegs * 32;
 #pragma unroll
-        for (int i = 0; i < kRegs; ++i) dump[i * 32 + lane] = body.o[i];
+        for (int i = 0; i < kRegs; i += 4)
+          ((float4*)dump)[i * 8 + lane] = make_float4(body.o[i], body.o[i + 1], body.o[i + 2], body.o[i + 3]);
         if (lane == 0) {
           Left& x = left[warp][slot];
           x.row = here.row;
@@ -720,7 +740,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
   // Pieces that the warps of this CTA, or several CTAs, have shared: a run of dumps is slot s0 of warp w0
   // and then slot 0 of the warps after it, up to w1.
   auto dump_of = [&](int w, int s) {
-    return s ? (const float*)(smem + (size_t)w * kStages * S::kStageBytes) : (const float*)(smem + S::kRing) + w * kRegs * 32;
+    return s ? (const float*)(smem + (size_t)w * kStages * S::kStageBytes) : (const float*)dumps + w * kRegs * 32;
   };
   for (int k = 0; k < 2 * kWarps;) {
     const int w0 = k >> 1, s0 = k & 1;
@@ -740,37 +760,52 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
     const int cta0 = whole ? 0 : (int)(x.line / quota), cta1 = whole ? 0 : (int)((x.line + x.chunks - 1) / quota);
     auto part_of = [&](int c) { return p.parts + (size_t)(2 * c + (c == cta0 ? 1 : 0)) * kPart; };
     float* part = whole ? nullptr : part_of(blockIdx.x);
-    constexpr int kShare = kRegs / kWarps;
-#pragma unroll 4
-    for (int u = 0; u < kShare; ++u) {
-      const int i = warp * kShare + u, head = Body::head_of(i, lane), d = Body::dim_of(i, lane);
-      float m = -INFINITY, v = 0.f, l = 0.f;
-      for (int w = w0; w <= w1; ++w) m = fmaxf(m, stat[w][w == w0 ? s0 : 0][head].x);
-      const float off = m == -INFINITY ? 0.f : m;
-      for (int w = w0; w <= w1; ++w) {
-        const int s = w == w0 ? s0 : 0;
-        const float f = exp2_fast(stat[w][s][head].x - off);
-        v = fmaf(f, dump_of(w, s)[i * 32 + lane], v);
-        l = fmaf(f, stat[w][s][head].y, l);
+    // Thread (warp, lane) adds the float4s (registers 4 u .. 4 u + 3 of lane `lane`) of u = warp, warp + kWarps, ...
+    auto store_out = [&](int u, const float4& v, float l0, float l1, float l2, float l3) {
+      const float vs[4] = {v.x, v.y, v.z, v.w}, ls[4] = {l0, l1, l2, l3};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int head = Body::head_of(4 * u + j, lane), d = Body::dim_of(4 * u + j, lane);
+        if (head < heads && d < kv.head_dim) out_at(x.row, head0 + head)[d] = from_float<T>(ls[j] == 0.f ? 0.f : vs[j] / ls[j]);
       }
-      if (!whole) __stcg(&part[i * 32 + lane], v);
-      else if (head < heads && d < kv.head_dim) out_at(x.row, head0 + head)[d] = from_float<T>(l == 0.f ? 0.f : v / l);
-    }
-    if ((int)threadIdx.x < heads) {
+    };
+    // statistics of the run, and its dumps' factors
+    if (threadIdx.x < kMaxHeads) {
       const int head = threadIdx.x;
       float m = -INFINITY, l = 0.f;
       for (int w = w0; w <= w1; ++w) m = fmaxf(m, stat[w][w == w0 ? s0 : 0][head].x);
       const float off = m == -INFINITY ? 0.f : m;
       for (int w = w0; w <= w1; ++w) {
         const float2 s = stat[w][w == w0 ? s0 : 0][head];
-        l = fmaf(exp2_fast(s.x - off), s.y, l);
+        factor[w][head] = exp2_fast(s.x - off);
+        l = fmaf(factor[w][head], s.y, l);
       }
-      if (!whole) __stcg((float2*)&part[kRegs * 32 + 2 * head], make_float2(m, l));
-      else if (p.lse) p.lse[(int64_t)x.row * p.n_q_heads + head0 + head] = lse_of(m, l);
+      sums[head] = make_float2(m, l);
+      if (head < heads) {
+        if (!whole) __stcg((float2*)&part[kRegs * 32 + 2 * head], make_float2(m, l));
+        else if (p.lse) p.lse[(int64_t)x.row * p.n_q_heads + head0 + head] = lse_of(m, l);
+      }
     }
+    __syncthreads();
+#pragma unroll
+    for (int u = warp; u < kRegs / 4; u += kWarps) {
+      int hd[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) hd[j] = Body::head_of(4 * u + j, lane);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int w = w0; w <= w1; ++w) {
+        const float4 y = ((const float4*)dump_of(w, w == w0 ? s0 : 0))[u * 32 + lane];
+        v.x = fmaf(factor[w][hd[0]], y.x, v.x);
+        v.y = fmaf(factor[w][hd[1]], y.y, v.y);
+        v.z = fmaf(factor[w][hd[2]], y.z, v.z);
+        v.w = fmaf(factor[w][hd[3]], y.w, v.w);
+      }
+      if (!whole) __stcg((float4*)part + u * 32 + lane, v);
+      else store_out(u, v, sums[hd[0]].y, sums[hd[1]].y, sums[hd[2]].y, sums[hd[3]].y);
+    }
+    __syncthreads();
     if (!whole) {
       // the last of the CTAs that hold a part of this piece adds them, in CTA order
-      __syncthreads();
       if (threadIdx.x == 0) {
         __threadfence();
         is_last = atomicAdd(&p.tickets[cta0], 1u) == (unsigned int)(cta1 - cta0);
@@ -779,31 +814,35 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_kernel(const __gr
       __syncthreads();
       if (is_last) {
         __threadfence();
-        if ((int)threadIdx.x < heads) {
-          float m = -INFINITY, l = 0.f;
-          for (int c = cta0; c <= cta1; ++c) {
-            const float2 s = __ldcg((const float2*)(part_of(c) + kRegs * 32) + threadIdx.x);
-            const float m2 = fmaxf(m, s.x), off = m2 == -INFINITY ? 0.f : m2;
-            l = l * exp2_fast(m - off) + s.y * exp2_fast(s.x - off);
-            m = m2;
+        const int n = cta1 - cta0 + 1;
+#pragma unroll 1
+        for (int u = warp; u < kRegs / 4; u += kWarps) {
+          int hd[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) hd[j] = Body::head_of(4 * u + j, lane);
+          float v[4] = {0.f, 0.f, 0.f, 0.f}, m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll 8
+          for (int c = 0; c < n; ++c) {
+            const float* q = part_of(cta0 + c);
+            const float4 y = __ldcg((const float4*)q + u * 32 + lane);
+            float f[2], g[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float2 s = __ldcg((const float2*)(q + kRegs * 32) + hd[e * Body::kSecond]);
+              const float m2 = fmaxf(m[e], s.x), off = m2 == -INFINITY ? 0.f : m2;
+              f[e] = exp2_fast(m[e] - off);
+              g[e] = exp2_fast(s.x - off);
+              l[e] = l[e] * f[e] + s.y * g[e];
+              m[e] = m2;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = v[j] * f[Body::pair_of(j)] + (&y.x)[j] * g[Body::pair_of(j)];
           }
-          sums[threadIdx.x] = make_float2(m, l);
-          if (p.lse) p.lse[(int64_t)x.row * p.n_q_heads + head0 + threadIdx.x] = lse_of(m, l);
-        }
-        __syncthreads();
-#pragma unroll 2
-        for (int u = 0; u < kShare; ++u) {
-          const int i = warp * kShare + u, head = Body::head_of(i, lane), d = Body::dim_of(i, lane);
-          if (head >= heads) continue;
-          const float2 s = sums[head];
-          const float off = s.x == -INFINITY ? 0.f : s.x;
-          float v = 0.f;
-#pragma unroll 4
-          for (int c = cta0; c <= cta1; ++c) {
-            const float* q = part_of(c);
-            v = fmaf(exp2_fast(__ldcg(q + kRegs * 32 + 2 * head) - off), __ldcg(q + i * 32 + lane), v);
-          }
-          if (d < kv.head_dim) out_at(x.row, head0 + head)[d] = from_float<T>(s.y == 0.f ? 0.f : v / s.y);
+          store_out(u, make_float4(v[0], v[1], v[2], v[3]), l[Body::pair_of(0)], l[Body::pair_of(1)], l[Body::pair_of(2)], l[Body::pair_of(3)]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (p.lse && hd[j] < heads && Body::dim_of(4 * u + j, lane) == 0)
+              p.lse[(int64_t)x.row * p.n_q_heads + head0 + hd[j]] = lse_of(m[Body::pair_of(j)], l[Body::pair_of(j)]);
         }
         __syncthreads();
       }
@@ -828,25 +867,27 @@ static void split_heads(int per_kv, int* n_split, int* piece_heads) {
   *piece_heads = (per_kv + *n_split - 1) / *n_split;
 }
 
-template <typename T, typename Body, int kStages, int kCtasPerSm>
+template <typename T, typename Body, int kWarps, int kStages>
 static int launch_attend(const AttendParams& p, cudaStream_t st) {
-  using S = AttendShared<T, Body, kStages>;
-  static_assert(S::kBytes <= 227 * 1024 / kCtasPerSm - 1024, "shared memory");
-  auto kernel = attend_kernel<T, Body, kStages, kCtasPerSm>;
+  using S = AttendShared<T, Body, kWarps, kStages>;
+  static_assert(S::kBytes <= 222 * 1024, "shared memory");
+  static_assert(kWarps <= kMaxWarps, "workspace");
+  auto kernel = attend_kernel<T, Body, kWarps, kStages>;
   PG_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes));
   const long long most = (long long)p.kv.n_rows * p.kv.n_kv_heads * p.n_split *
                          (((long long)p.kv.max_pages * p.kv.page_size + Body::kChunk - 1) / Body::kChunk);
-  const unsigned grid = (unsigned)(most < kSms * kCtasPerSm ? most : kSms * kCtasPerSm);
-  kernel<<<grid, kThreads, S::kBytes, st>>>(p);
+  kernel<<<(unsigned)(most < kSms ? most : kSms), kWarps * 32, S::kBytes, st>>>(p);
   PG_LAUNCH_CHECK();
   return PG_OK;
 }
 
+// One CTA per SM; its warps' rings take most of the shared memory (three stages of 8 KB for eight warps,
+// or of 16 KB for four).
 template <typename T, template <int, int> class Body, int DP, int NT>
 static int launch_body(const AttendParams& p, cudaStream_t st) {
-  // 64: two CTAs of 96 KB rings to an SM; 128, 256: one of 128-192 KB
-  if constexpr (DP <= 64) return launch_attend<T, Body<DP, NT>, 3, sizeof(T) == 2 ? 2 : 1>(p, st);
-  else return launch_attend<T, Body<DP, NT>, sizeof(T) == 4 || (DP == 256 && NT == 2) ? 2 : 3, 1>(p, st);
+  constexpr int kStage = 2 * Body<DP, NT>::kChunk * Body<DP, NT>::kRowBytes;
+  if constexpr (sizeof(T) == 2 && DP <= 128) return launch_attend<T, Body<DP, NT>, 8, 3>(p, st);
+  else return launch_attend<T, Body<DP, NT>, 4, 4 * (3 * kStage + (int)Body<DP, NT>::kQBytes) <= 222 * 1024 ? 3 : 2>(p, st);
 }
 
 template <typename T, template <int, int> class Body>
@@ -873,7 +914,8 @@ size_t pg_kv_attend_workspace_bytes(const pg_kv* kv, int32_t n_q_heads, int32_t 
   if (pg::attend_check(kv, n_q_heads, group) != PG_OK) return 0;
   // tickets first, so that their place depends on nothing
   const size_t dp = kv->head_dim <= 64 ? 64 : kv->head_dim <= 128 ? 128 : 256;
-  return pg::kTicketBytes + (size_t)2 * pg::kMaxCtas * (dp * pg::kMaxHeads + 2 * pg::kMaxHeads) * sizeof(float);
+  const size_t acc = dp * pg::kMaxHeads;
+  return pg::kTicketBytes + pg::kSms * (2 * (acc + 2 * pg::kMaxHeads) + pg::kMaxWarps * acc) * sizeof(float);
 }
 
 int pg_kv_attend(const pg_kv* kv, int32_t layer, int32_t n_q_heads, const void* q, int64_t q_stride,
@@ -909,6 +951,8 @@ int pg_kv_attend(const pg_kv* kv, int32_t layer, int32_t n_q_heads, const void* 
   p.page = pg::fast_div((uint32_t)kv->page_size);
   p.tickets = (unsigned int*)workspace;
   p.parts = (float*)((char*)workspace + pg::kTicketBytes);
+  const size_t dp = kv->head_dim <= 64 ? 64 : kv->head_dim <= 128 ? 128 : 256;
+  p.dumps = p.parts + 2 * pg::kSms * (dp + 2) * pg::kMaxHeads;
   cudaStream_t st = (cudaStream_t)stream;
   if (kv->dtype == PG_F32) return pg::launch_type<float, pg::F32Body>(p, st);
   if (kv->dtype == PG_BF16) return pg::launch_type<__nv_bfloat16, pg::Bf16Body>(p, st);
