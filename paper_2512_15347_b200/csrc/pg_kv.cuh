@@ -8,6 +8,7 @@
 
 namespace pg {
 
+constexpr int kStatusTimeout = 2;   // status bit 1: a bounded wait ran out
 constexpr int kStatusIndex = 4;     // status bit 2: an index from device memory was out of range
 constexpr int kStatusPages = 8;     // status bit 3: no free page, or a row's table is full
 

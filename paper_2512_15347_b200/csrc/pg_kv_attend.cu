@@ -19,69 +19,13 @@
 // (row, head) piece, where the warps' triples are joined in shared memory.  A piece that a cut has
 // split is joined by the CTA that arrives last (wait-free ticket; parts are added in CTA order, so the
 // bits do not depend on who that is).
-#include "pg_kv.cuh"
+#include "pg_kv_attend.cuh"
 
 #include <type_traits>
 
 namespace pg {
 
-constexpr int kSms = 148;
-constexpr int kMaxWarps = 8;
-constexpr int kMaxHeads = 16;                 // query heads of a (row, kv head) piece
-constexpr size_t kTicketBytes = 4096;         // >= 4 * kSms
-
-// n / d for 0 <= n < 2^31 by a multiplication (d >= 1): m = ceil(2^(32+s) / d), s = ceil(log2 d) - 1.
-struct FastDiv {
-  uint32_t d, m, s;
-};
-inline FastDiv fast_div(uint32_t d) {
-  FastDiv f{d, 0, 0};
-  if (d > 1) {
-    uint32_t s = 0;
-    while ((1ull << (s + 1)) < d) ++s;
-    f.s = s;
-    f.m = (uint32_t)((((unsigned __int128)1 << (32 + s)) + d - 1) / d);
-  }
-  return f;
-}
-
-struct AttendParams {
-  KvView kv;
-  const void* q;
-  const void *k_new, *v_new;
-  void* out;
-  float* lse;
-  const int32_t* shared;
-  int64_t q_stride, new_stride, out_stride;   // elements
-  int n_q_heads, per_kv, group;
-  int n_split, piece_heads;                   // pieces per kv head, query heads of a piece
-  float scale_log2;                           // scale * log2(e)
-  FastDiv page;
-  // shared pages of groups (shared != null): see prefix_kernel
-  int q_blocks, block_rows, block_queries;    // query blocks of a (group, kv head); rows and places of queries of a block
-  long long* line;                            // [groups + 1]: the groups' first tiles on the line of shared tiles, and the quota
-  float* shared_out;                          // [CTAs + units][block_queries][2 + head_dim]: (m, l, o)
-  unsigned int* tickets;                      // [CTAs], zero between calls
-  float* parts;                               // [2 * CTAs][REGS * 32 + 2 * kMaxHeads]
-  float* dumps;                               // [CTAs][kWarps][REGS * 32]
-};
-
 #ifdef __CUDACC__
-__device__ __forceinline__ uint32_t div_by(uint32_t n, const FastDiv& f) {
-  return f.d == 1 ? n : __umulhi(n, f.m) >> f.s;
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint32_t shared_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool some) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(some ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -113,42 +57,6 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16) {
 __device__ __forceinline__ uint32_t pack2(float a, float b, __half) {
   const __half2 v = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&v);
-}
-
-// ---------------------------------------------------------------- pages shared by a group
-constexpr int kTile = 64;            // tokens of a tile of the shared part
-constexpr int kMinShared = 64;       // fewer shared tokens are read row by row
-
-// Tokens of group g that are computed once for its rows: whole tiles, and at least the last token of
-// the first row (through whose table they are read) stays outside.
-__device__ __forceinline__ int group_tokens(const AttendParams& p, int g) {
-  if (!p.shared) return 0;
-  const int n = min(p.shared[g], checked_len(p.kv, p.kv.len[g * p.group]) - 1);
-  return n < kMinShared ? 0 : n / kTile * kTile;
-}
-
-// Where the shared part of a (row, piece) lies: its unit's line of tiles was cut at multiples of `quota`
-// tiles, CTA c left the part of unit u in block c + u (the pairs (c, u) that occur form a monotone path).
-struct SharedParts {
-  int cta0, cta1, unit, column;      // cta1 < cta0: none
-};
-__device__ __forceinline__ SharedParts shared_parts(const AttendParams& p, int row, int head0) {
-  const int g = row / p.group, tiles = group_tokens(p, g) / kTile;
-  const int h = head0 / p.per_kv, n = row - g * p.group, block = n / p.block_rows;
-  const int local = h * p.q_blocks + block;
-  SharedParts s;
-  s.cta0 = 0;
-  s.cta1 = -1;
-  if (tiles == 0) return s;
-  const long long first = p.line[g] + (long long)local * tiles, quota = p.line[p.kv.n_rows / p.group];
-  s.cta0 = (int)(first / quota);
-  s.cta1 = (int)((first + tiles - 1) / quota);
-  s.unit = g * p.kv.n_kv_heads * p.q_blocks + local;
-  s.column = (n - block * p.block_rows) * p.per_kv + head0 - h * p.per_kv;
-  return s;
-}
-__device__ __forceinline__ float* shared_part(const AttendParams& p, const SharedParts& s, int cta) {
-  return p.shared_out + (size_t)(cta + s.unit) * p.block_queries * (p.kv.head_dim + 2);
 }
 
 // ---------------------------------------------------------------- bodies: one warp, one chunk at a time
@@ -227,8 +135,8 @@ struct MmaBody {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int head = min(nt * 8 + (lane & 3) * 2 + j, heads - 1);
-          col[nt][j] = part + (size_t)(sp.column + head) * (p.kv.head_dim + 2);
-          const float2 s = __ldcg((const float2*)col[nt][j]);
+          col[nt][j] = part + 2 * p.block_queries + (size_t)(sp.column + head) * p.kv.head_dim;
+          const float2 s = __ldcg((const float2*)part + sp.column + head);
           const float m2 = fmaxf(m[nt][j], s.x), off = m2 == -INFINITY ? 0.f : m2;
           f[nt][j] = exp2_fast(m[nt][j] - off);
           g[nt][j] = exp2_fast(s.x - off);
@@ -238,7 +146,7 @@ struct MmaBody {
 #pragma unroll
       for (int i = 0; i < kRegs; ++i) {
         const int nt = (i >> 2) % NT, j = i & 1, d = dim_of(i, lane);
-        const float y = d < p.kv.head_dim ? __ldcg(col[nt][j] + 2 + d) : 0.f;
+        const float y = d < p.kv.head_dim ? __ldcg(col[nt][j] + d) : 0.f;
         o[i] = o[i] * f[nt][j] + y * g[nt][j];
       }
     }
@@ -506,7 +414,8 @@ template <int kChunk>
 __device__ __forceinline__ RowSpan row_span(const AttendParams& p, int row, int len) {
   RowSpan s;
   s.hi = checked_len(p.kv, len);
-  s.lo = p.shared ? max(0, min(group_tokens(p, row / p.group), s.hi - 1)) : 0;
+  s.lo = p.shared ? group_tokens(p, row / p.group) : 0;
+  if (s.lo >= s.hi) s.lo = 0;                         // a row that ends inside the shared tokens reads them by itself
   s.c0 = s.lo / kChunk;
   s.c1 = s.hi > s.lo ? (s.hi + kChunk - 1) / kChunk : s.c0;
   return s;
@@ -936,194 +845,6 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
     }
   }
 }
-// ---------------------------------------------------------------- the shared part
-// The first group_tokens(g) tokens of group g against the queries of all its rows: a unit is (group, kv
-// head, block of up to 8 warps x NT * 8 queries), its keys come in tiles of 64 tokens that the eight
-// warps share in shared memory, each with its own queries.  The tiles of all units form one line that
-// is cut into equal parts over the CTAs, as above; every (CTA, unit) leaves its queries' (m, l, o) in
-// global memory, and the rows' own pieces start from them.
-// Bound: the tensor pipe (group * per_kv flop per byte).
-constexpr int kPrefixWarps = 8;
-
-template <typename T, int DP, int NT>
-__global__ void __launch_bounds__(kPrefixWarps * 32, 1) prefix_kernel(const __grid_constant__ AttendParams p) {
-  using Body = MmaBody<T, DP, NT, 16>;
-  constexpr int kThreads = kPrefixWarps * 32, kStages = DP > 128 ? 3 : 4;
-  constexpr int kTileBytes = kTile * Body::kRowBytes, kStageBytes = 2 * kTileBytes;
-  extern __shared__ __align__(1024) char smem[];
-  __shared__ long long warp_sum_[kPrefixWarps];
-  __shared__ int first_group;
-  __shared__ long long first_tile;
-  const KvView& kv = p.kv;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int groups = kv.n_rows / p.group, units = kv.n_kv_heads * p.q_blocks;    // of a group
-
-  // planning, as for the rows' own chunks; CTA 0 keeps the groups' places for the second kernel
-  const int per = (groups + kThreads - 1) / kThreads;
-  const int g0 = min((int)threadIdx.x * per, groups), g1 = min(g0 + per, groups);
-  long long mine = 0;
-  for (int g = g0; g < g1; ++g) mine += (long long)(group_tokens(p, g) / kTile) * units;
-  long long upto = mine;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const long long y = __shfl_up_sync(0xFFFFFFFFu, upto, d);
-    if (lane >= d) upto += y;
-  }
-  if (lane == 31) warp_sum_[warp] = upto;
-  __syncthreads();
-  long long total = 0;
-#pragma unroll
-  for (int w = 0; w < kPrefixWarps; ++w) {
-    if (w < warp) upto += warp_sum_[w];
-    total += warp_sum_[w];
-  }
-  // parts of at least four tiles: a part leaves more bytes behind than a tile has
-  const long long quota = max((total + gridDim.x - 1) / gridDim.x, 4ll);
-  const long long begin = blockIdx.x * quota;
-  const int count = (int)max(0ll, min(quota, total - begin));
-  if (blockIdx.x == 0) {
-    long long at = upto - mine;
-    for (int g = g0; g < g1; ++g) {
-      p.line[g] = at;
-      at += (long long)(group_tokens(p, g) / kTile) * units;
-    }
-    if (threadIdx.x == 0) p.line[groups] = quota;
-  }
-  if (count == 0) return;
-  if (begin >= upto - mine && begin < upto) {
-    long long rest = begin - (upto - mine);
-    for (int g = g0; g < g1; ++g) {
-      const long long n = (long long)(group_tokens(p, g) / kTile) * units;
-      if (rest < n) {
-        first_group = g;
-        first_tile = rest;
-        break;
-      }
-      rest -= n;
-    }
-  }
-  __syncthreads();
-
-  struct At {
-    int group, tiles, local, tile;       // tiles of a unit; unit within the group; tile within the unit
-    __device__ __forceinline__ void next(const AttendParams& p, int units) {
-      if (++tile < tiles) return;
-      tile = 0;
-      if (++local < units) return;
-      local = 0;
-      do {
-        if (++group >= p.kv.n_rows / p.group) return;
-        tiles = group_tokens(p, group) / kTile;
-      } while (tiles == 0);
-    }
-  };
-  At ahead;
-  ahead.group = first_group;
-  ahead.tiles = group_tokens(p, first_group) / kTile;
-  ahead.local = (int)(first_tile / ahead.tiles);
-  ahead.tile = (int)(first_tile - (long long)ahead.local * ahead.tiles);
-  At here = ahead;
-
-  // Loads: a thread moves 16-byte pieces of the same column of several tokens; their pages are looked up
-  // one tile ahead.
-  constexpr int kPieces = Body::kRowBytes / 16;                  // pieces of a token, 8, 16 or 32
-  constexpr int kToks = kThreads / kPieces, kLoads = kTile / kToks;
-  const int piece = threadIdx.x % kPieces, tok0 = threadIdx.x / kPieces;
-  const bool inside = piece < kv.head_dim / 8;
-  const uint32_t ring = shared_addr(smem);
-  int issued = 0, entry[kLoads];
-  auto look_up = [&]() {
-    if (issued >= count) return;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i)
-      entry[i] = kv.table[(int64_t)ahead.group * p.group * kv.max_pages + div_by(ahead.tile * kTile + tok0 + i * kToks, p.page)];
-  };
-  look_up();
-  auto issue = [&](int stage) {
-    if (issued < count) {
-      const int h = ahead.local / p.q_blocks;
-      const uint32_t kb = ring + stage * kStageBytes, vb = kb + kTileBytes;
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int tok = tok0 + i * kToks, t = ahead.tile * kTile + tok;
-        const bool ok = (unsigned int)entry[i] < (unsigned int)kv.n_pages;
-        if (!ok) flag(kv.status, kStatusIndex);
-        const int slot = t - (int)div_by(t, p.page) * kv.page_size;
-        const int64_t at = (ok ? entry[i] : 0) * kv.page_stride + ((int64_t)h * kv.page_size + slot) * kv.head_dim + (inside ? piece * 8 : 0);
-        copy_async(kb + Body::piece_at(tok, piece), (const T*)kv.k + at, ok && inside);
-        copy_async(vb + Body::piece_at(tok, piece), (const T*)kv.v + at, ok && inside);
-      }
-      ++issued;
-      if (issued < count) ahead.next(p, units);
-      look_up();
-    }
-    copy_commit();
-  };
-#pragma unroll
-  for (int s = 0; s < kStages - 1; ++s) issue(s);
-
-  Body body;
-  int done = 0, stage = 0;
-  while (done < count) {
-    const int n = min(here.tiles - here.tile, count - done);
-    const int h = here.local / p.q_blocks, block = here.local - h * p.q_blocks;
-    const int block0 = block * p.block_rows * p.per_kv, q0 = block0 + warp * NT * 8;      // the warp's first query
-    const int q_end = min(p.group, (block + 1) * p.block_rows) * p.per_kv;
-    body.load_queries(kv.head_dim, lane, [&](int c) {
-      const int q = q0 + c;
-      if (q >= q_end) return (const T*)nullptr;
-      const int i = q / p.per_kv;
-      return (const T*)p.q + ((int64_t)here.group * p.group + i) * p.q_stride + (int64_t)(h * p.per_kv + q - i * p.per_kv) * kv.head_dim;
-    });
-    body.clear();
-    // tokens that a column's row takes from the shared part
-    const int tokens = here.tiles * kTile;
-    int limit[NT][2], least = tokens;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int q = q0 + nt * 8 + (lane & 3) * 2 + j;
-        limit[nt][j] = q < q_end ? max(0, min(tokens, checked_len(kv, kv.len[here.group * p.group + q / p.per_kv]) - 1)) : tokens;
-        least = min(least, limit[nt][j]);
-      }
-    least = __reduce_min_sync(0xFFFFFFFFu, least);
-    for (int i = 0; i < n; ++i) {
-      copy_wait<kStages - 2>();
-      __syncthreads();
-      issue(stage == 0 ? kStages - 1 : stage - 1);
-      const uint32_t kb = ring + stage * kStageBytes;
-      const int t0 = (here.tile + i) * kTile;
-      if (q0 < q_end) {
-#pragma unroll 1
-        for (int u = 0; u < kTile; u += 16)
-          body.step_masked(p, kb + u * Body::kRowBytes, kb + kTileBytes + u * Body::kRowBytes, t0 + u, lane, t0 + u + 16 <= least,
-                           [&](int t, int nt, int j) { return t < limit[nt][j]; });
-      }
-      stage = stage + 1 == kStages ? 0 : stage + 1;
-    }
-    float* out = p.shared_out + (size_t)(blockIdx.x + here.group * units + here.local) * p.block_queries * (kv.head_dim + 2);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float s = body.l[nt][j];
-#pragma unroll
-        for (int d = 4; d < 32; d <<= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
-        const int c = warp * NT * 8 + nt * 8 + (lane & 3) * 2 + j;
-        if (lane < 4 && q0 + c - warp * NT * 8 < q_end) __stcg((float2*)(out + (size_t)c * (kv.head_dim + 2)), make_float2(body.m[nt][j], s));
-      }
-#pragma unroll
-    for (int i = 0; i < Body::kRegs; ++i) {
-      const int c = warp * NT * 8 + Body::head_of(i, lane), d = Body::dim_of(i, lane);
-      if (block0 + c < q_end && d < kv.head_dim) __stcg(out + (size_t)c * (kv.head_dim + 2) + 2 + d, body.o[i]);
-    }
-    done += n;
-    here.tile += n - 1;
-    if (done < count) here.next(p, units);
-  }
-  copy_wait<0>();
-}
 #endif
 
 // ---------------------------------------------------------------- launch
@@ -1181,43 +902,13 @@ static int launch_type(const AttendParams& p, cudaStream_t st) {
 template <int DP, int NT> using Bf16Body = MmaBody<__nv_bfloat16, DP, NT, DP <= 64 ? 32 : 16>;
 template <int DP, int NT> using F16Body = MmaBody<__half, DP, NT, DP <= 64 ? 32 : 16>;
 
-// Blocks of the shared part's queries: whole rows, evenly, as many as eight warps hold in up to four columns
-// of eight each (three from head dim 65, two from 129: what fits the registers).  columns 0: a row has more query
-// heads per kv head than a block holds, its group is read row by row.
-static void query_blocks(int group, int per_kv, int head_dim, int* blocks, int* rows, int* columns) {
-  const int most = kPrefixWarps * 8 * (head_dim > 128 ? 2 : head_dim > 64 ? 3 : 4);
-  *blocks = *rows = *columns = 0;
-  if (per_kv > most) return;
-  *blocks = (group + most / per_kv - 1) / (most / per_kv);
-  *rows = (group + *blocks - 1) / *blocks;
-  *columns = (*rows * per_kv + kPrefixWarps * 8 - 1) / (kPrefixWarps * 8);
-}
 static size_t line_bytes(const pg_kv* kv, int group) { return ((size_t)(kv->n_rows / group + 1) * 8 + 15) & ~(size_t)15; }
 static size_t shared_bytes(const pg_kv* kv, int n_q_heads, int group) {
-  if (group < 2 || kv->dtype == PG_F32) return 0;
-  int blocks, rows, columns;
-  query_blocks(group, n_q_heads / kv->n_kv_heads, kv->head_dim, &blocks, &rows, &columns);
+  int blocks, rows, queries;
+  if (group < 2 || kv->dtype == PG_F32 || !shared_blocks(group, n_q_heads / kv->n_kv_heads, kv->head_dim, &blocks, &rows, &queries))
+    return 0;
   const size_t units = (size_t)(kv->n_rows / group) * kv->n_kv_heads * blocks;
-  return line_bytes(kv, group) + (kSms + units) * columns * kPrefixWarps * 8 * (kv->head_dim + 2) * sizeof(float);
-}
-
-template <typename T, int DP, int NT>
-static int launch_prefix(const AttendParams& p, cudaStream_t st) {
-  constexpr int kBytes = (DP > 128 ? 3 : 4) * 2 * kTile * DP * 2;
-  auto kernel = prefix_kernel<T, DP, NT>;
-  PG_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes));
-  kernel<<<kSms, kPrefixWarps * 32, kBytes, st>>>(p);
-  PG_LAUNCH_CHECK();
-  return PG_OK;
-}
-template <typename T>
-static int launch_prefix_type(const AttendParams& p, int columns, cudaStream_t st) {
-  const int d = p.kv.head_dim;
-  if (d <= 64) return columns == 1 ? launch_prefix<T, 64, 1>(p, st) : columns == 2 ? launch_prefix<T, 64, 2>(p, st)
-                    : columns == 3 ? launch_prefix<T, 64, 3>(p, st) : launch_prefix<T, 64, 4>(p, st);
-  if (d <= 128) return columns == 1 ? launch_prefix<T, 128, 1>(p, st) : columns == 2 ? launch_prefix<T, 128, 2>(p, st)
-                     : launch_prefix<T, 128, 3>(p, st);
-  return columns == 1 ? launch_prefix<T, 256, 1>(p, st) : launch_prefix<T, 256, 2>(p, st);
+  return line_bytes(kv, group) + (kSms + units) * queries * (kv->head_dim + 2) * sizeof(float);
 }
 
 }  // namespace pg
@@ -1269,15 +960,12 @@ int pg_kv_attend(const pg_kv* kv, int32_t layer, int32_t n_q_heads, const void* 
   const size_t dp = kv->head_dim <= 64 ? 64 : kv->head_dim <= 128 ? 128 : 256;
   p.dumps = p.parts + 2 * pg::kSms * (dp + 2) * pg::kMaxHeads;
   cudaStream_t st = (cudaStream_t)stream;
-  int columns = 0;
-  if (kv->dtype != PG_F32 && p.shared) pg::query_blocks(group, p.per_kv, kv->head_dim, &p.q_blocks, &p.block_rows, &columns);
-  if (columns == 0) p.shared = nullptr;
+  if (kv->dtype == PG_F32 || (p.shared && !pg::shared_blocks(group, p.per_kv, kv->head_dim, &p.q_blocks, &p.block_rows, &p.block_queries)))
+    p.shared = nullptr;
   if (p.shared) {
-    p.block_queries = columns * pg::kPrefixWarps * 8;
     p.line = (long long*)(p.dumps + pg::kSms * pg::kMaxWarps * dp * pg::kMaxHeads);
     p.shared_out = (float*)((char*)p.line + pg::line_bytes(kv, group));
-    const int e = kv->dtype == PG_BF16 ? pg::launch_prefix_type<__nv_bfloat16>(p, columns, st)
-                                       : pg::launch_prefix_type<__half>(p, columns, st);
+    const int e = pg::launch_shared(p, kv->dtype, st);
     if (e != PG_OK) return e;
   }
   if (kv->dtype == PG_F32) return pg::launch_type<float, pg::F32Body>(p, st);

@@ -541,6 +541,7 @@ int pg_kv_status(const int32_t* status, void* stream) {
   PG_CUDA(cudaMemcpyAsync(&word, status, sizeof(word), cudaMemcpyDeviceToHost, (cudaStream_t)stream));
   PG_CUDA(cudaStreamSynchronize((cudaStream_t)stream));
   if (word & pg::kStatusIndex) return PG_EINDEX;
+  if (word & pg::kStatusTimeout) return PG_ETIMEOUT;
   if (word & pg::kStatusPages) return PG_ENOPAGES;
   return PG_OK;
 }
