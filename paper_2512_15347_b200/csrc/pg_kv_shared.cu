@@ -6,7 +6,7 @@
 // work becomes a dense product of group * per_kv flop per byte.  The fifth-generation tensor cores do it:
 //   loader warps    gather 64-token tiles of K and V from the pages with 16-byte asynchronous copies,
 //                   laid out in the 128-byte swizzle that the tensor cores read (K along its head
-//                   dimension, V along it too, i.e. transposed as an operand), three tiles ahead
+//                   dimension, V along it too, i.e. transposed as an operand), up to three tiles ahead
 //   one MMA thread  issues S_t = Q_t K^T and O_t += P_t V into tensor memory
 //   softmax warps   a warpgroup for each of the (up to two) 128-query tiles t: a thread owns a query row,
 //                   reads its S, keeps its maximum and sum, writes P (rounded to the cache's type) to
@@ -25,7 +25,6 @@
 namespace pg {
 
 constexpr int kRows = 128;           // queries of a product
-constexpr int kLoaders = 128;        // threads
 constexpr float kSlack = 8.f;
 constexpr int kWaitLimit = 1 << 14;
 
@@ -55,6 +54,11 @@ template <typename T>
 __device__ __forceinline__ constexpr uint32_t instr_desc(int n, bool b_mn) {
   const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
   return 1u << 4 | type << 7 | type << 10 | (b_mn ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(kRows >> 4) << 24;
+}
+__device__ __forceinline__ bool elected() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
 }
 __device__ __forceinline__ void mma_async(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool accumulate) {
   asm volatile(
@@ -105,6 +109,24 @@ __device__ __forceinline__ uint32_t pack_pair(float a, float b, __half) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pair_of_floats(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void floats_of_pair(uint64_t p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // A tile of the line: tile `tile` of unit `local` of group `group`, whose units have `tiles` tiles.
 struct TilePlace {
   int group, tiles, local, tile;
@@ -126,8 +148,9 @@ struct SharedLayout {
   static constexpr int kKBytes = kBlocks * kTile * 128, kStageBytes = 2 * kKBytes;
   static constexpr int kQBytes = kBlocks * kRows * 128, kPBytes = kRows * 128;
   static constexpr int kBytes = kStages * kStageBytes + kSlots * (kQBytes + kPBytes) + 1024;
-  static constexpr int kThreads = kSlots * kRows + kLoaders + 32;
-  static constexpr int kColumns = kSlots * (kTile + DP) > 256 ? 512 : 256;     // tensor memory: S and O of every slot
+  static constexpr int kThreads = kSlots * kRows + kStages * 32 + 32;
+  static constexpr int kColumns = 512;                             // tensor memory: two S and an O for every slot
+  static_assert(kSlots * (2 * kTile + DP) <= kColumns, "tensor memory");
 };
 
 template <typename T, int DP, int kSlots>
@@ -139,9 +162,10 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
   __shared__ int first_group, gave_up;
   __shared__ long long first_tile;
   __shared__ uint32_t tmem_base;
-  __shared__ __align__(8) uint64_t bars[2 * kStages + 4 * kSlots + 1];
+  __shared__ __align__(8) uint64_t bars[2 * kStages + 5 * kSlots + 1];
   const KvView& kv = p.kv;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // (broadcasts tell the compiler what is the same for the warp: the products' operands are uniform registers)
+  const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int groups = kv.n_rows / p.group, units = kv.n_kv_heads * p.q_blocks;    // of a group
   char* smem = smem_raw + (-(int)shared_addr(smem_raw) & 1023);
 
@@ -168,7 +192,7 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
   // parts of at least four tiles: a part leaves more bytes behind than a tile has
   const long long quota = max((total + gridDim.x - 1) / gridDim.x, 4ll);
   const long long begin = blockIdx.x * quota;
-  const int count = (int)max(0ll, min(quota, total - begin));
+  const int count = __shfl_sync(0xFFFFFFFFu, (int)max(0ll, min(quota, total - begin)), 0);
   if (blockIdx.x == 0) {
     long long at = upto - mine;
     for (int g = g0; g < g1; ++g) {
@@ -196,19 +220,20 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
   auto full = [&](int s) { return bar0 + 8 * s; };
   auto empty = [&](int s) { return bar0 + 8 * (kStages + s); };
   auto q_full = [&](int t) { return bar0 + 8 * (2 * kStages + t); };
-  auto s_full = [&](int t) { return bar0 + 8 * (2 * kStages + kSlots + t); };
-  auto p_full = [&](int t) { return bar0 + 8 * (2 * kStages + 2 * kSlots + t); };
-  auto o_done = [&](int t) { return bar0 + 8 * (2 * kStages + 3 * kSlots + t); };
-  const uint32_t drained = bar0 + 8 * (2 * kStages + 4 * kSlots);
+  auto p_full = [&](int t) { return bar0 + 8 * (2 * kStages + kSlots + t); };
+  auto o_done = [&](int t) { return bar0 + 8 * (2 * kStages + 2 * kSlots + t); };
+  auto s_full = [&](int t, int tile) { return bar0 + 8 * (2 * kStages + 3 * kSlots + 2 * t + (tile & 1)); };   // S is double buffered
+  const uint32_t drained = bar0 + 8 * (2 * kStages + 5 * kSlots);
   if (threadIdx.x == 0) {
     auto init = [](uint32_t b, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(b), "r"(n) : "memory"); };
     for (int s = 0; s < kStages; ++s) {
-      init(full(s), kLoaders);
+      init(full(s), 32);
       init(empty(s), 1);
     }
     for (int t = 0; t < kSlots; ++t) {
       init(q_full(t), kRows);
-      init(s_full(t), 1);
+      init(s_full(t, 0), 1);
+      init(s_full(t, 1), 1);
       init(p_full(t), kRows);
       init(o_done(t), 1);
     }
@@ -248,7 +273,9 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
     // ------------------------------------------------------------ softmax: a thread per query
     const int t = warp >> 2, row = threadIdx.x & (kRows - 1);
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;               // tensor-memory lanes 32 (warp % 4) ..
-    const uint32_t s_addr = tmem + lanes + t * kTile, o_addr = tmem + lanes + kSlots * kTile + t * DP;
+    const uint32_t s_addr = tmem + lanes + t * 2 * kTile, o_addr = tmem + lanes + kSlots * 2 * kTile + t * DP;
+    const float scale = fabsf(p.scale_log2);                         // a negative one goes into the queries' signs
+    const uint32_t sign = p.scale_log2 < 0.f ? 0x80008000u : 0u;
     const bool aligned = (((uintptr_t)p.q | (p.q_stride * sizeof(T))) & 15) == 0;
     int tiles_done = 0;                                              // of this slot
     bool ok = true;
@@ -277,25 +304,24 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
               w = make_uint4(u[0], u[1], u[2], u[3]);
             }
           }
-          *(uint4*)(dst + (c8 >> 3) * kRows * 128 + swizzled(row, c8 & 7)) = w;
+          *(uint4*)(dst + (c8 >> 3) * kRows * 128 + swizzled(row, c8 & 7)) = make_uint4(w.x ^ sign, w.y ^ sign, w.z ^ sign, w.w ^ sign);
         }
         to_async_proxy();
         tmem_before();
         arrive(q_full(t));
         float m = -INFINITY, l = 0.f;
         for (int k = 0; k < n; ++k) {
-          if (lost() || !wait(s_full(t), tiles_done)) { ok = false; break; }
+          if (lost() || !wait(s_full(t, tiles_done), tiles_done >> 1)) { ok = false; break; }
           __syncwarp();
           tmem_after();
           float s[kTile];
-          tmem_load32(*reinterpret_cast<float(*)[32]>(s), s_addr);
-          tmem_load32(*reinterpret_cast<float(*)[32]>(s + 32), s_addr + 32);
-#pragma unroll
-          for (int j = 0; j < kTile; ++j) s[j] *= p.scale_log2;
+          const uint32_t s_here = s_addr + (tiles_done & 1) * kTile;
+          tmem_load32(*reinterpret_cast<float(*)[32]>(s), s_here);
+          tmem_load32(*reinterpret_cast<float(*)[32]>(s + 32), s_here + 32);
           float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int j = 0; j < kTile; ++j) tops[j & 3] = fmaxf(tops[j & 3], s[j]);
-          const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+          for (int j = 0; j < kTile; j += 2) tops[(j >> 1) & 3] = fmaxf(fmaxf(tops[(j >> 1) & 3], s[j]), s[j + 1]);
+          const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * scale;
           // the previous product has read P and updated O
           if (k > 0 && !wait(o_done(t), tiles_done - 1)) { ok = false; break; }
           const bool raise = top > m + kSlack || m == -INFINITY;
@@ -319,19 +345,25 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
           l *= f;
           const float off = m == -INFINITY ? 0.f : m;
           char* pd = smem + kStages * L::kStageBytes + kSlots * L::kQBytes + t * L::kPBytes;
-          float ls[2] = {0.f, 0.f};
+          uint64_t sums[2] = {0, 0};
+          const uint64_t scale2 = pair_of_floats(scale, scale), off2 = pair_of_floats(-off, -off);
 #pragma unroll
           for (int c8 = 0; c8 < kTile / 8; ++c8) {
-            float w[8];
+            uint32_t packed[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              w[j] = exp2_fast(s[c8 * 8 + j] - off);
-              ls[j & 1] += w[j];
+            for (int j = 0; j < 4; ++j) {
+              float x, y;
+              floats_of_pair(fma_pair(pair_of_floats(s[c8 * 8 + 2 * j], s[c8 * 8 + 2 * j + 1]), scale2, off2), x, y);
+              x = exp2_fast(x);
+              y = exp2_fast(y);
+              sums[j & 1] = add_pair(sums[j & 1], pair_of_floats(x, y));
+              packed[j] = pack_pair(x, y, T());
             }
-            *(uint4*)(pd + swizzled(row, c8)) = make_uint4(pack_pair(w[0], w[1], T()), pack_pair(w[2], w[3], T()),
-                                                           pack_pair(w[4], w[5], T()), pack_pair(w[6], w[7], T()));
+            *(uint4*)(pd + swizzled(row, c8)) = make_uint4(packed[0], packed[1], packed[2], packed[3]);
           }
-          l += ls[0] + ls[1];
+          float l0, l1;
+          floats_of_pair(add_pair(sums[0], sums[1]), l0, l1);
+          l += l0 + l1;
           to_async_proxy();
           tmem_before();
           arrive(p_full(t));
@@ -358,96 +390,106 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
       if (done < count) here.next_unit(p, units);
     }
   } else if (warp < kWarps - 1) {
-    // ------------------------------------------------------------ loaders
-    constexpr int kPieces = DP / 8, kToks = kLoaders / kPieces, kLoads = kTile / kToks;   // 16-byte pieces of a token
-    const int id = threadIdx.x - kSlots * kRows, piece = id % kPieces, tok0 = id / kPieces;
+    // ------------------------------------------------------------ loaders: a warp for each stage
+    constexpr int kPieces = DP / 8, kToks = 32 / kPieces > 0 ? 32 / kPieces : 1;     // 16-byte pieces of a token, tokens at a time
+    static_assert(kPieces <= 32, "a token at a time at most");
+    const int stage = warp - kSlots * 4, piece = lane % kPieces;
     const bool inside = piece < kv.head_dim / 8;
-    const uint32_t place = (piece >> 3) * kTile * 128;
-    bool ok = true;
-    int left = min(here.tiles - here.tile, count);                   // tiles of this unit in this part
-    for (int k = 0; k < count; ++k) {
-      const int stage = k % kStages;
-      int entry[kLoads];
+    const uint32_t kb = ring + stage * L::kStageBytes + (piece >> 3) * kTile * 128, vb = kb + L::kKBytes;
+    int at = 0;                                                      // tile of the part that `here` is at
+    for (int k = stage; k < count; k += kStages) {
+      for (; at < k; ++at)
+        if (++here.tile == here.tiles) here.next_unit(p, units);
+      // a lane looks up two tokens' pages
+      int64_t from[kTile / 32];
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i)
-        entry[i] = kv.table[(int64_t)here.group * p.group * kv.max_pages + div_by(here.tile * kTile + tok0 + i * kToks, p.page)];
-      if (lost() || (k >= kStages && !wait(empty(stage), k / kStages - 1))) { ok = false; break; }
-      const int h = here.local / p.q_blocks;
-      const uint32_t kb = ring + stage * L::kStageBytes + place, vb = kb + L::kKBytes;
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int tok = tok0 + i * kToks, tt = here.tile * kTile + tok;
-        const bool good = (unsigned int)entry[i] < (unsigned int)kv.n_pages;
+      for (int i = 0; i < kTile / 32; ++i) {
+        const int tok = here.tile * kTile + i * 32 + lane, page = (int)div_by(tok, p.page);
+        const int entry = kv.table[(int64_t)here.group * p.group * kv.max_pages + page];
+        const bool good = (unsigned int)entry < (unsigned int)kv.n_pages;
         if (!good) flag(kv.status, kStatusIndex);
-        const int slot = tt - (int)div_by(tt, p.page) * kv.page_size;
-        const int64_t at = (good ? entry[i] : 0) * kv.page_stride + ((int64_t)h * kv.page_size + slot) * kv.head_dim + (inside ? piece * 8 : 0);
-        copy_async(kb + swizzled(tok, piece & 7), (const T*)kv.k + at, good && inside);
-        copy_async(vb + swizzled(tok, piece & 7), (const T*)kv.v + at, good && inside);
+        from[i] = good ? entry * kv.page_stride + ((int64_t)(here.local / p.q_blocks) * kv.page_size + tok - page * kv.page_size) * kv.head_dim : -1;
+      }
+      if (lost() || (k >= kStages && !wait(empty(stage), k / kStages - 1))) break;
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < kTile; i += kToks) {
+        const int tok = i + lane / kPieces;
+        const int64_t src = __shfl_sync(0xFFFFFFFFu, from[i / 32], tok & 31);
+        const bool some = src >= 0 && inside;
+        const int64_t e = some ? src + piece * 8 : 0;
+        copy_async(kb + swizzled(tok, piece & 7), (const T*)kv.k + e, some);
+        copy_async(vb + swizzled(tok, piece & 7), (const T*)kv.v + e, some);
       }
       copy_commit();
-      if (k > 0) {
-        copy_wait<1>();
-        to_async_proxy();
-        arrive(full((k - 1) % kStages));
-      }
-      ++here.tile;
-      if (--left == 0 && k + 1 < count) {
-        here.next_unit(p, units);
-        left = min(here.tiles, count - k - 1);
-      }
+      copy_wait<0>();
+      to_async_proxy();
+      arrive(full(stage));
     }
     copy_wait<0>();
-    if (ok) {
-      to_async_proxy();
-      arrive(full((count - 1) % kStages));
-    }
-  } else if (lane == 0) {
-    // ------------------------------------------------------------ one thread issues the products
+  } else {
+    // ------------------------------------------------------------ one warp issues the products, by one of its threads
+    const uint32_t tmem_u = __shfl_sync(0xFFFFFFFFu, tmem, 0);
     const uint32_t qk = instr_desc<T>(kTile, false), pv = instr_desc<T>(DP, true);
     int tiles_done[kSlots] = {}, units_done[kSlots] = {};
     bool ok = true;
-    auto scores = [&](int t, int stage) {
-      const uint32_t a = q_at + t * L::kQBytes, b = ring + stage * L::kStageBytes;
+    const bool issuer = elected();
+    auto wait_all = [&](uint32_t bar, int parity) { return __all_sync(0xFFFFFFFFu, !lost() && wait(bar, parity)) != 0; };
+    auto scores = [&](int t, int stage, int tile) {                  // tile: counted over the slot, picks the S buffer
+      const uint32_t a = q_at + t * L::kQBytes, b = ring + stage * L::kStageBytes, d = tmem_u + (2 * t + (tile & 1)) * kTile;
+      if (issuer) {
 #pragma unroll
-      for (int s = 0; s < DP / 16; ++s)
-        mma_async(tmem + t * kTile, matrix_desc(a + (s >> 2) * kRows * 128 + (s & 3) * 32, 16, 1024),
-                  matrix_desc(b + (s >> 2) * kTile * 128 + (s & 3) * 32, 16, 1024), qk, s > 0);
-      commit_to(s_full(t));
+        for (int s = 0; s < DP / 16; ++s)
+          mma_async(d, matrix_desc(a + (s >> 2) * kRows * 128 + (s & 3) * 32, 16, 1024),
+                    matrix_desc(b + (s >> 2) * kTile * 128 + (s & 3) * 32, 16, 1024), qk, s > 0);
+        commit_to(s_full(t, tile));
+      }
+      __syncwarp();
     };
     int k = 0;                                                       // tile of the part
     for (int done = 0; ok && done < count;) {
-      const int n = min(here.tiles - here.tile, count - done);
-      const int slots = (block_queries(here.local) + kRows - 1) / kRows;
-      if (lost() || !wait(full(k % kStages), k / kStages)) break;
-      for (int t = 0; ok && t < slots; ++t) {
-        ok = wait(q_full(t), units_done[t]++);
-        tmem_after();
-        if (ok) scores(t, k % kStages);
-      }
+      const int n = __shfl_sync(0xFFFFFFFFu, min(here.tiles - here.tile, count - done), 0);
+      const int slots = __shfl_sync(0xFFFFFFFFu, (block_queries(here.local) + kRows - 1) / kRows, 0);
+      ok = wait_all(full(k % kStages), k / kStages);
+#pragma unroll
+      for (int t = 0; t < kSlots; ++t)
+        if (ok && t < slots) {
+          ok = wait_all(q_full(t), units_done[t]++);
+          tmem_after();
+          if (ok) scores(t, k % kStages, tiles_done[t]);
+        }
       for (int i = 0; ok && i < n; ++i, ++k) {
         const int stage = k % kStages, next = (k + 1) % kStages;
         const uint32_t v = ring + stage * L::kStageBytes + L::kKBytes;
-        for (int t = 0; ok && t < slots; ++t) {
-          ok = !lost() && wait(p_full(t), tiles_done[t]++);
-          if (!ok) break;
+        if (i + 1 < n) {                                             // the next scores run under this tile's softmax
+          ok = wait_all(full(next), (k + 1) / kStages);
           tmem_after();
-          const uint32_t a = p_at + t * L::kPBytes;
 #pragma unroll
-          for (int s = 0; s < kTile / 16; ++s)
-            mma_async(tmem + kSlots * kTile + t * DP, matrix_desc(a + s * 32, 16, 1024),
-                      matrix_desc(v + s * 2048, kTile * 128, 1024), pv, i > 0 || s > 0);
-          commit_to(o_done(t));
-          if (t == slots - 1) commit_to(empty(stage));
-          if (i + 1 < n) {
-            if (t == 0) ok = wait(full(next), (k + 1) / kStages);
-            if (ok) scores(t, next);
+          for (int t = 0; t < kSlots; ++t)
+            if (ok && t < slots) scores(t, next, tiles_done[t] + 1);
+        }
+#pragma unroll
+        for (int t = 0; t < kSlots; ++t) {
+          if (!ok || t >= slots) continue;
+          ok = wait_all(p_full(t), tiles_done[t]++);
+          if (!ok) continue;
+          tmem_after();
+          const uint32_t a = p_at + t * L::kPBytes, d = tmem_u + kSlots * 2 * kTile + t * DP;
+          if (issuer) {
+#pragma unroll
+            for (int s = 0; s < kTile / 16; ++s)
+              mma_async(d, matrix_desc(a + s * 32, 16, 1024), matrix_desc(v + s * 2048, kTile * 128, 1024), pv, i > 0 || s > 0);
+            commit_to(o_done(t));
+            if (t == slots - 1) commit_to(empty(stage));
           }
+          __syncwarp();
         }
       }
       done += n;
       if (done < count) here.next_unit(p, units);
     }
-    commit_to(drained);                                              // no product is in flight when the CTA leaves
+    if (issuer) commit_to(drained);                                  // no product is in flight when the CTA leaves
+    __syncwarp();
     wait(drained, 0);
   }
   __syncwarp();
