@@ -87,9 +87,9 @@ struct MmaBody {
   // 16-byte piece c of token row t: pieces are swizzled so that eight rows' equal pieces hit all banks
   static __device__ __forceinline__ uint32_t piece_at(int t, int c) { return t * kRowBytes + ((c ^ (t & 7)) << 4); }
 
-  // query(g): the vector of column g of the warp, or null
+  // query(g): the vector of column g of the warp, or null; words: on 4-byte boundaries
   template <typename Query>
-  __device__ __forceinline__ void load_queries(int dim, int lane, Query query) {
+  __device__ __forceinline__ void load_queries(int dim, bool words, int lane, Query query) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const T* qh = query(nt * 8 + (lane >> 2));
@@ -99,7 +99,10 @@ struct MmaBody {
         for (int j = 0; j < 2; ++j) {
           const int d = s * 16 + j * 8 + (lane & 3) * 2;
           uint32_t w = 0;
-          if (qh && d < dim) w = *(const uint16_t*)(qh + d) | (uint32_t)*(const uint16_t*)(qh + d + 1) << 16;
+          if (qh && d < dim) {
+            if (words) w = *(const uint32_t*)(qh + d);
+            else w = *(const uint16_t*)(qh + d) | (uint32_t)*(const uint16_t*)(qh + d + 1) << 16;
+          }
           q[s][nt][j] = w;
         }
     }
@@ -117,17 +120,17 @@ struct MmaBody {
 
   __device__ __forceinline__ void begin(const AttendParams& p, int row, int head0, int heads, int lane, char*) {
     const T* base = (const T*)p.q + row * p.q_stride + (int64_t)head0 * p.kv.head_dim;
-    load_queries(p.kv.head_dim, lane, [&](int g) { return g < heads ? base + (int64_t)g * p.kv.head_dim : (const T*)nullptr; });
+    load_queries(p.kv.head_dim, p.q_words, lane, [&](int g) { return g < heads ? base + (int64_t)g * p.kv.head_dim : (const T*)nullptr; });
     clear();
   }
 
   // The triple of the group's shared tokens goes in front of a row's own (sums are per lane: one of the
   // eight lanes of a head starts with the whole l).
-  __device__ __forceinline__ void join_shared(const AttendParams& p, int row, int head0, int heads, int lane) {
-    const SharedParts sp = shared_parts(p, row, head0);
+  __device__ __forceinline__ void join_shared(const AttendParams& p, int unit, int column, int heads, int lane) {
+    const int2 span = __ldcg(&p.spans[unit]);
 #pragma unroll 1
-    for (int c = sp.cta0; c <= sp.cta1; ++c) {
-      const float* part = shared_part(p, sp, c);
+    for (int c = span.x; c <= span.y; ++c) {
+      const float* part = shared_block(p, c, unit);
       float f[NT][2], g[NT][2];
       const float* col[NT][2];
 #pragma unroll
@@ -135,8 +138,8 @@ struct MmaBody {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int head = min(nt * 8 + (lane & 3) * 2 + j, heads - 1);
-          col[nt][j] = part + 2 * p.block_queries + (size_t)(sp.column + head) * p.kv.head_dim;
-          const float2 s = __ldcg((const float2*)part + sp.column + head);
+          col[nt][j] = part + 2 * p.block_queries + (size_t)(column + head) * p.kv.head_dim;
+          const float2 s = __ldcg((const float2*)part + column + head);
           const float m2 = fmaxf(m[nt][j], s.x), off = m2 == -INFINITY ? 0.f : m2;
           f[nt][j] = exp2_fast(m[nt][j] - off);
           g[nt][j] = exp2_fast(s.x - off);
@@ -248,6 +251,35 @@ struct MmaBody {
           mma16816<T>(c, a, b[mt][nt][0], b[mt][nt][1]);
         }
       }
+  }
+
+  // o / l of a piece seen whole, sums[head] = (m, l).  An 8x8 transposition of the rounded values leaves
+  // a lane with two neighbouring elements of one head.
+  __device__ __forceinline__ void store(const AttendParams& p, const float2* sums, int row, int head0, int heads, int lane) {
+    T* out = (T*)p.out + row * p.out_stride + (int64_t)head0 * p.kv.head_dim;
+    float r[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float l = sums[nt * 8 + (lane & 3) * 2 + j].y;
+        r[nt][j] = l == 0.f ? 0.f : 1.f / l;
+      }
+#pragma unroll
+    for (int i = 0; i < kRegs; i += 2) {
+      const int nt = (i >> 2) % NT;
+      const uint32_t w = transpose8x8(pack2(o[i] * r[nt][0], o[i + 1] * r[nt][1], T()));
+      const int head = nt * 8 + (lane >> 2), d = (i >> 2) / NT * 16 + ((i >> 1) & 1) * 8 + (lane & 3) * 2;
+      if (head < heads && d < p.kv.head_dim) {
+        T* at = out + (int64_t)head * p.kv.head_dim + d;
+        if (p.out_words) {
+          *(uint32_t*)at = w;
+        } else {
+          ((uint16_t*)at)[0] = (uint16_t)w;
+          ((uint16_t*)at)[1] = (uint16_t)(w >> 16);
+        }
+      }
+    }
   }
 
   // stats[head] = (m, l), by the lanes that hold them
@@ -387,6 +419,20 @@ struct F32Body {
     __syncwarp();
   }
 
+  __device__ __forceinline__ void store(const AttendParams& p, const float2* sums, int row, int head0, int heads, int lane) {
+    float* out = (float*)p.out + row * p.out_stride + (int64_t)head0 * p.kv.head_dim;
+#pragma unroll
+    for (int g = 0; g < kHeads; ++g) {
+      if (g >= heads) continue;
+      const float l = sums[g].y, r = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int d = dim_of(i, lane);
+        if (d < p.kv.head_dim) out[(int64_t)g * p.kv.head_dim + d] = o[g * kPer + i] * r;
+      }
+    }
+  }
+
   __device__ __forceinline__ void stats(float2* out, int lane) {
 #pragma unroll
     for (int g = 0; g < kHeads; ++g) {
@@ -411,35 +457,56 @@ struct RowSpan {
   __device__ __forceinline__ int units() const { return c1 > c0 ? c1 - c0 + kPieceCost : 0; }
 };
 template <int kChunk>
-__device__ __forceinline__ RowSpan row_span(const AttendParams& p, int row, int len) {
+__device__ __forceinline__ RowSpan row_span(const AttendParams& p, int shared_tokens, int len) {
   RowSpan s;
   s.hi = checked_len(p.kv, len);
-  s.lo = p.shared ? group_tokens(p, row / p.group) : 0;
-  if (s.lo >= s.hi) s.lo = 0;                         // a row that ends inside the shared tokens reads them by itself
+  s.lo = shared_tokens < s.hi ? shared_tokens : 0;    // a row that ends inside the shared tokens reads them by itself
   s.c0 = s.lo / kChunk;
   s.c1 = s.hi > s.lo ? (s.hi + kChunk - 1) / kChunk : s.c0;
   return s;
 }
+template <int kChunk>
+__device__ __forceinline__ RowSpan row_span(const AttendParams& p, int row) {
+  return row_span<kChunk>(p, p.shared ? group_tokens(p, (int)div_by(row, p.group_div)) : 0, p.kv.len[row]);
+}
 
-// A place on the line: unit `unit` of (row, piece), pieces numbered (kv head, split) within the row;
-// the first kPieceCost units of a piece stand for no chunk.
+// A place on the line: unit `unit` of piece (row, kv head h, split), in that order; the first kPieceCost units of a
+// piece stand for no chunk.  Divisions are kept out of the walk.
 template <int kChunk>
 struct Place {
-  int row, piece, unit;
+  int row, h, split, unit;
+  int group, n, tokens;        // row = group * p.group + n; the group's shared tokens
   int next_len;                // of the next row, fetched long before it is needed
   RowSpan span;
   __device__ __forceinline__ void fetch(const AttendParams& p) {
     if (row + 1 < p.kv.n_rows) next_len = p.kv.len[row + 1];
   }
-  __device__ __forceinline__ void next_piece(const AttendParams& p, int pieces) {
+  __device__ __forceinline__ void next_piece(const AttendParams& p) {
     unit = 0;
-    if (++piece < pieces) return;
-    piece = 0;
+    if (++split < p.n_split) return;
+    split = 0;
+    if (++h < p.kv.n_kv_heads) return;
+    h = 0;
     do {
       if (++row >= p.kv.n_rows) return;
-      span = row_span<kChunk>(p, row, next_len);
+      if (++n == p.group) {
+        n = 0;
+        ++group;
+        tokens = p.shared ? group_tokens(p, group) : 0;
+      }
+      span = row_span<kChunk>(p, tokens, next_len);
       fetch(p);
     } while (span.c1 == span.c0);
+  }
+  __device__ __forceinline__ void set(const AttendParams& p, int row_, int piece, int unit_, const RowSpan& span_) {
+    row = row_;
+    h = piece / p.n_split;
+    split = piece - h * p.n_split;
+    unit = unit_;
+    group = (int)div_by(row_, p.group_div);
+    n = row_ - group * p.group;
+    tokens = p.shared ? group_tokens(p, group) : 0;
+    span = span_;
   }
 };
 
@@ -453,7 +520,7 @@ struct AttendShared {
 
 // What a warp leaves behind of a piece that it has not seen whole.
 struct Left {
-  int row, piece, chunk0;      // the piece, and the first of its chunks in this part
+  int row, h, split, chunk0;   // the piece, and the first of its chunks in this part
   long long line;              // line unit of the piece's chunk 0
   int chunks;                  // chunks of the whole piece
   int any, goes_on;            // filled; continues in the next warp
@@ -496,7 +563,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
   long long mine = 0;
   int longest = 0;
   for (int r = r0; r < r1; ++r) {
-    const RowSpan s = row_span<kChunk>(p, r, kv.len[r]);
+    const RowSpan s = row_span<kChunk>(p, r);
     mine += s.units();
     longest = max(longest, s.chunks());
     if (s.c1 == s.c0 && r % gridDim.x == blockIdx.x) {
@@ -532,16 +599,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
   if (by_piece) {
     const int r = blockIdx.x / pieces;
     if (r < kv.n_rows) {
-      const RowSpan s = row_span<kChunk>(p, r, kv.len[r]);
+      const RowSpan s = row_span<kChunk>(p, r);
       const int share = (s.chunks() + kWarps - 1) / kWarps, from = min(warp * share, s.chunks());
       wbegin = kPieceCost + from;                     // counted from the piece's own start
       wend = kPieceCost + min(from + share, s.chunks());
-      if (lane == 0) {
-        first[warp].row = r;
-        first[warp].piece = blockIdx.x - r * pieces;
-        first[warp].unit = (int)wbegin;
-        first[warp].span = s;
-      }
+      if (lane == 0) first[warp].set(p, r, blockIdx.x - r * pieces, (int)wbegin, s);
     } else {
       wbegin = wend = 0;
     }
@@ -558,13 +620,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
       if (cut < before || cut >= end) continue;
       long long rest = cut - before;
       for (int r = r0; r < r1; ++r) {
-        const RowSpan s = row_span<kChunk>(p, r, kv.len[r]);
+        const RowSpan s = row_span<kChunk>(p, r);
         const long long n = (long long)s.units() * pieces;
         if (rest < n) {
-          first[w].row = r;
-          first[w].piece = (int)(rest / s.units());
-          first[w].unit = (int)(rest - (long long)first[w].piece * s.units());
-          first[w].span = s;
+          const int piece = (int)(rest / s.units());
+          first[w].set(p, r, piece, (int)(rest - (long long)piece * s.units()), s);
           break;
         }
         rest -= n;
@@ -599,19 +659,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
   look_up();
   auto issue = [&](int stage) {
     if (ahead_at < wend) {
-      const int t = (ahead.span.c0 + ahead.unit - kPieceCost) * kChunk + lane, h = ahead.piece / p.n_split;
+      const int t = (ahead.span.c0 + ahead.unit - kPieceCost) * kChunk + lane, h = ahead.h;
       const bool in = lane < kChunk && t < ahead.span.hi && t >= ahead.span.lo;
-      const T *ks = nullptr, *vs = nullptr;           // null: zeros
+      // where the token is: an element offset in the pools, -1 for zeros, -2 - e for element e of the new tokens
+      int64_t from = -1;
       if (in) {
         if (p.k_new && t == ahead.span.hi - 1) {
-          const int64_t at = ahead.row * p.new_stride + (int64_t)h * kv.head_dim;
-          ks = (const T*)p.k_new + at;
-          vs = (const T*)p.v_new + at;
+          from = -2 - (ahead.row * p.new_stride + (int64_t)h * kv.head_dim);
         } else if ((unsigned int)entry < (unsigned int)kv.n_pages) {
           const int slot = t - (int)div_by(t, p.page) * kv.page_size;
-          const int64_t at = entry * kv.page_stride + ((int64_t)h * kv.page_size + slot) * kv.head_dim;
-          ks = (const T*)kv.k + at;
-          vs = (const T*)kv.v + at;
+          from = entry * kv.page_stride + ((int64_t)h * kv.page_size + slot) * kv.head_dim;
         } else {
           flag(kv.status, kStatusIndex);
         }
@@ -620,19 +677,20 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
 #pragma unroll
       for (int i = 0; i < kChunk; i += kRowsPerCopy) {
         const int tok = i + lane / kLanesPerRow;
-        const char* kp = (const char*)__shfl_sync(0xFFFFFFFFu, (unsigned long long)ks, tok);
-        const char* vp = (const char*)__shfl_sync(0xFFFFFFFFu, (unsigned long long)vs, tok);
+        const int64_t e = __shfl_sync(0xFFFFFFFFu, from, tok);
+        const T* kp = e >= 0 ? (const T*)kv.k + e : (const T*)p.k_new + (-2 - e);
+        const T* vp = e >= 0 ? (const T*)kv.v + e : (const T*)p.v_new + (-2 - e);
 #pragma unroll
         for (int j = 0; j < kPiecesPerLane; ++j) {
           const int c = lane % kLanesPerRow + j * kLanesPerRow;
-          const bool some = kp != nullptr && c < row_pieces;
-          copy_async(kb + Body::piece_at(tok, c), some ? kp + c * 16 : (const char*)kv.k, some);
-          copy_async(vb + Body::piece_at(tok, c), some ? vp + c * 16 : (const char*)kv.v, some);
+          const bool some = e != -1 && c < row_pieces;
+          copy_async(kb + Body::piece_at(tok, c), some ? (const char*)kp + c * 16 : (const char*)kv.k, some);
+          copy_async(vb + Body::piece_at(tok, c), some ? (const char*)vp + c * 16 : (const char*)kv.v, some);
         }
       }
       ++ahead_at;
       if (++ahead.unit == ahead.span.units()) {
-        if (ahead_at < wend) ahead.next_piece(p, pieces);
+        if (ahead_at < wend) ahead.next_piece(p);
         ahead_at += kPieceCost;
         ahead.unit = kPieceCost;
       }
@@ -680,11 +738,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
     const int n_units = (int)min((long long)(span.units() - here.unit), wend - pos);
     const int j0 = max(here.unit - kPieceCost, 0), j1 = here.unit + n_units - kPieceCost;
     if (j1 > j0) {
-      const int h = here.piece / p.n_split, split = here.piece - h * p.n_split;
-      const int head0 = h * p.per_kv + split * p.piece_heads;
-      const int heads = min(p.piece_heads, p.per_kv - split * p.piece_heads);
+      const int head0 = here.h * p.per_kv + here.split * p.piece_heads;
+      const int heads = min(p.piece_heads, p.per_kv - here.split * p.piece_heads);
       body.begin(p, here.row, head0, heads, lane, scratch);
-      if (span.lo > 0 && j0 == 0) body.join_shared(p, here.row, head0, heads, lane);
+      if (span.lo > 0 && j0 == 0) {
+        int column;
+        const int unit = shared_unit(p, here.group, here.n, here.h, &column);
+        body.join_shared(p, unit, column + here.split * p.piece_heads, heads, lane);
+      }
       for (int j = j0; j < j1; ++j) {
         copy_wait<kStages - 2>();
         __syncwarp();
@@ -698,12 +759,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
       if (j0 == 0 && j1 == span.chunks()) {            // seen whole: nothing to join
         __syncwarp();
         const float2* st = stat[warp][1];
-#pragma unroll
-        for (int i = 0; i < kRegs; ++i) {
-          const int head = Body::head_of(i, lane), d = Body::dim_of(i, lane);
-          const float l = st[head].y;
-          if (head < heads && d < kv.head_dim) out_at(here.row, head0 + head)[d] = from_float<T>(l == 0.f ? 0.f : body.o[i] / l);
-        }
+        body.store(p, st, here.row, head0, heads, lane);
         if (p.lse && lane < heads) p.lse[(int64_t)here.row * p.n_q_heads + head0 + lane] = lse_of(st[lane].x, st[lane].y);
         __syncwarp();
       } else {
@@ -717,7 +773,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
         if (lane == 0) {
           Left& x = left[warp][slot];
           x.row = here.row;
-          x.piece = here.piece;
+          x.h = here.h;
+          x.split = here.split;
           x.chunk0 = j0;
           x.line = pos - here.unit + kPieceCost;
           x.chunks = span.chunks();
@@ -727,7 +784,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
       }
     }
     pos += n_units;
-    if (pos < wend) here.next_piece(p, pieces);
+    if (pos < wend) here.next_piece(p);
     else break;
   }
   copy_wait<0>();
@@ -750,9 +807,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
     while (goes_on && w1 + 1 < kWarps) goes_on = left[++w1][0].goes_on;
     k = (w1 > w0 ? 2 * w1 : k) + 1;
     const bool whole = x.chunk0 == 0 && !goes_on;
-    const int h = x.piece / p.n_split, split = x.piece - h * p.n_split;
-    const int head0 = h * p.per_kv + split * p.piece_heads;
-    const int heads = min(p.piece_heads, p.per_kv - split * p.piece_heads);
+    const int head0 = x.h * p.per_kv + x.split * p.piece_heads;
+    const int heads = min(p.piece_heads, p.per_kv - x.split * p.piece_heads);
     const int cta0 = whole ? 0 : (int)(x.line / quota), cta1 = whole ? 0 : (int)((x.line + x.chunks - 1) / quota);
     auto part_of = [&](int c) { return p.parts + (size_t)(2 * c + (c == cta0 ? 1 : 0)) * kPart; };
     float* part = whole ? nullptr : part_of(blockIdx.x);
@@ -902,13 +958,15 @@ static int launch_type(const AttendParams& p, cudaStream_t st) {
 template <int DP, int NT> using Bf16Body = MmaBody<__nv_bfloat16, DP, NT, DP <= 64 ? 32 : 16>;
 template <int DP, int NT> using F16Body = MmaBody<__half, DP, NT, DP <= 64 ? 32 : 16>;
 
-static size_t line_bytes(const pg_kv* kv, int group) { return ((size_t)(kv->n_rows / group + 1) * 8 + 15) & ~(size_t)15; }
+static size_t spans_bytes(const pg_kv* kv, int group, int blocks) {
+  return ((size_t)(kv->n_rows / group) * kv->n_kv_heads * blocks * sizeof(int2) + 15) & ~(size_t)15;
+}
 static size_t shared_bytes(const pg_kv* kv, int n_q_heads, int group) {
   int blocks, rows, queries;
   if (group < 2 || kv->dtype == PG_F32 || !shared_blocks(group, n_q_heads / kv->n_kv_heads, kv->head_dim, &blocks, &rows, &queries))
     return 0;
   const size_t units = (size_t)(kv->n_rows / group) * kv->n_kv_heads * blocks;
-  return line_bytes(kv, group) + (kSms + units) * queries * (kv->head_dim + 2) * sizeof(float);
+  return spans_bytes(kv, group, blocks) + (kSms + units) * queries * (kv->head_dim + 2) * sizeof(float);
 }
 
 }  // namespace pg
@@ -953,8 +1011,11 @@ int pg_kv_attend(const pg_kv* kv, int32_t layer, int32_t n_q_heads, const void* 
   p.q_stride = q_stride; p.new_stride = new_stride; p.out_stride = out_stride;
   p.n_q_heads = n_q_heads; p.per_kv = n_q_heads / kv->n_kv_heads; p.group = group;
   pg::split_heads(p.per_kv, &p.n_split, &p.piece_heads);
+  p.q_words = ((((uintptr_t)q) | (uintptr_t)(q_stride * b)) & 3) == 0;
+  p.out_words = ((((uintptr_t)out) | (uintptr_t)(out_stride * b)) & 3) == 0;
   p.scale_log2 = (float)((double)scale * 1.4426950408889634);
   p.page = pg::fast_div((uint32_t)kv->page_size);
+  p.group_div = pg::fast_div((uint32_t)group);
   p.tickets = (unsigned int*)workspace;
   p.parts = (float*)((char*)workspace + pg::kTicketBytes);
   const size_t dp = kv->head_dim <= 64 ? 64 : kv->head_dim <= 128 ? 128 : 256;
@@ -963,8 +1024,8 @@ int pg_kv_attend(const pg_kv* kv, int32_t layer, int32_t n_q_heads, const void* 
   if (kv->dtype == PG_F32 || (p.shared && !pg::shared_blocks(group, p.per_kv, kv->head_dim, &p.q_blocks, &p.block_rows, &p.block_queries)))
     p.shared = nullptr;
   if (p.shared) {
-    p.line = (long long*)(p.dumps + pg::kSms * pg::kMaxWarps * dp * pg::kMaxHeads);
-    p.shared_out = (float*)((char*)p.line + pg::line_bytes(kv, group));
+    p.spans = (int2*)(p.dumps + pg::kSms * pg::kMaxWarps * dp * pg::kMaxHeads);
+    p.shared_out = (float*)((char*)p.spans + pg::spans_bytes(kv, group, p.q_blocks));
     const int e = pg::launch_shared(p, kv->dtype, st);
     if (e != PG_OK) return e;
   }

@@ -35,11 +35,12 @@ struct AttendParams {
   int64_t q_stride, new_stride, out_stride;   // elements
   int n_q_heads, per_kv, group;
   int n_split, piece_heads;                   // pieces per kv head, query heads of a piece
+  int q_words, out_words;                     // rows of q / out on 4-byte boundaries
   float scale_log2;                           // scale * log2(e)
-  FastDiv page;
+  FastDiv page, group_div;
   // shared pages of groups (shared != null), pg_kv_shared.cu
   int q_blocks, block_rows, block_queries;    // query blocks of a (group, kv head); rows and places of queries of a block
-  long long* line;                            // [groups + 1]: the groups' first tiles on the line of shared tiles, and the quota
+  int2* spans;                                // [units]: first and last CTA with a part of the unit
   float* shared_out;                          // [CTAs + units]: (m, l) [block_queries][2], then o [block_queries][head_dim]
   unsigned int* tickets;                      // [CTAs], zero between calls
   float* parts;                               // [2 * CTAs][REGS * 32 + 2 * kMaxHeads]
@@ -74,28 +75,16 @@ __device__ __forceinline__ int group_tokens(const AttendParams& p, int g) {
   return n < kMinShared ? 0 : n / kTile * kTile;
 }
 
-// Where the shared part of a (row, piece) lies: its unit's line of tiles was cut at multiples of `quota`
-// tiles, CTA c left the part of unit u in block c + u (the pairs (c, u) that occur form a monotone path).
-struct SharedParts {
-  int cta0, cta1, unit, column;      // cta1 < cta0: none
-};
-__device__ __forceinline__ SharedParts shared_parts(const AttendParams& p, int row, int head0) {
-  const int g = row / p.group, tiles = group_tokens(p, g) / kTile;
-  const int h = head0 / p.per_kv, n = row - g * p.group, block = n / p.block_rows;
-  const int local = h * p.q_blocks + block;
-  SharedParts s;
-  s.cta0 = 0;
-  s.cta1 = -1;
-  if (tiles == 0) return s;
-  const long long first = p.line[g] + (long long)local * tiles, quota = p.line[p.kv.n_rows / p.group];
-  s.cta0 = (int)(first / quota);
-  s.cta1 = (int)((first + tiles - 1) / quota);
-  s.unit = g * p.kv.n_kv_heads * p.q_blocks + local;
-  s.column = (n - block * p.block_rows) * p.per_kv + head0 - h * p.per_kv;
-  return s;
+// The unit of (group, kv head) that holds the queries of the group's row n, and their first column in it.
+// The line of all units' tiles was cut into parts; CTA c left its part of unit u in block c + u (the pairs (c, u)
+// that occur form a monotone path), and spans[u] holds the first and the last c.
+__device__ __forceinline__ int shared_unit(const AttendParams& p, int group, int n, int h, int* column) {
+  const int block = p.q_blocks == 1 ? 0 : n / p.block_rows;
+  *column = (n - block * p.block_rows) * p.per_kv;
+  return (group * p.kv.n_kv_heads + h) * p.q_blocks + block;
 }
-__device__ __forceinline__ float* shared_part(const AttendParams& p, const SharedParts& s, int cta) {
-  return p.shared_out + (size_t)(cta + s.unit) * p.block_queries * (p.kv.head_dim + 2);
+__device__ __forceinline__ float* shared_block(const AttendParams& p, int cta, int unit) {
+  return p.shared_out + (size_t)(cta + unit) * p.block_queries * (p.kv.head_dim + 2);
 }
 #endif
 

@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
   extern __shared__ char smem_raw[];
   __shared__ long long warp_sum_[kWarps];
   __shared__ int first_group, gave_up;
-  __shared__ long long first_tile;
+  __shared__ long long first_tile;                    // within the group
   __shared__ uint32_t tmem_base;
   __shared__ __align__(8) uint64_t bars[2 * kStages + 5 * kSlots + 1];
   const KvView& kv = p.kv;
@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
   const int groups = kv.n_rows / p.group, units = kv.n_kv_heads * p.q_blocks;    // of a group
   char* smem = smem_raw + (-(int)shared_addr(smem_raw) & 1023);
 
-  // planning, as for the rows' own chunks; CTA 0 keeps the groups' places for the second kernel
+  // planning, as for the rows' own chunks
   const int per = (groups + kThreads - 1) / kThreads;
   const int g0 = min((int)threadIdx.x * per, groups), g1 = min(g0 + per, groups);
   long long mine = 0;
@@ -193,14 +193,6 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
   const long long quota = max((total + gridDim.x - 1) / gridDim.x, 4ll);
   const long long begin = blockIdx.x * quota;
   const int count = __shfl_sync(0xFFFFFFFFu, (int)max(0ll, min(quota, total - begin)), 0);
-  if (blockIdx.x == 0) {
-    long long at = upto - mine;
-    for (int g = g0; g < g1; ++g) {
-      p.line[g] = at;
-      at += (long long)(group_tokens(p, g) / kTile) * units;
-    }
-    if (threadIdx.x == 0) p.line[groups] = quota;
-  }
   if (count == 0) return;
   if (begin >= upto - mine && begin < upto) {
     long long rest = begin - (upto - mine);
@@ -372,7 +364,7 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
         if (!ok || !wait(o_done(t), tiles_done - 1)) { ok = false; break; }
         __syncwarp();
         tmem_after();
-        float* out = p.shared_out + (size_t)(blockIdx.x + here.group * units + here.local) * p.block_queries * (kv.head_dim + 2);
+        float* out = shared_block(p, blockIdx.x, here.group * units + here.local);
         if (mine) __stcg((float2*)out + c, make_float2(m, l));
         float* o_out = out + 2 * p.block_queries + (size_t)c * kv.head_dim;
 #pragma unroll 1
@@ -447,9 +439,13 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
       __syncwarp();
     };
     int k = 0;                                                       // tile of the part
+    long long unit_line = begin - here.tile;                         // the unit's first tile on the line
     for (int done = 0; ok && done < count;) {
       const int n = __shfl_sync(0xFFFFFFFFu, min(here.tiles - here.tile, count - done), 0);
       const int slots = __shfl_sync(0xFFFFFFFFu, (block_queries(here.local) + kRows - 1) / kRows, 0);
+      if (issuer && (here.tile == 0 || done == 0))                   // CTAs that share a unit write the same
+        p.spans[here.group * units + here.local] = make_int2((int)(unit_line / quota), (int)((unit_line + here.tiles - 1) / quota));
+      unit_line += here.tiles;
       ok = wait_all(full(k % kStages), k / kStages);
 #pragma unroll
       for (int t = 0; t < kSlots; ++t)
