@@ -21,6 +21,8 @@
 // bits do not depend on who that is).
 #include "pg_kv_attend.cuh"
 
+#include <cuda.h>
+
 #include <type_traits>
 
 namespace pg {
@@ -38,6 +40,20 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
+}
+__device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_tensor(uint32_t dst, const CUtensorMap* map, int row, int page, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2, %4}], [%5];" ::"r"(dst),
+      "l"(map), "r"(0), "r"(row), "r"(page), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void copy_bulk(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
+               "r"(bar)
+               : "memory");
 }
 template <typename T>
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -84,8 +100,11 @@ struct MmaBody {
   // of four registers 4 u .. 4 u + 3, the heads are those of the first and of the kSecond-th; which one each has
   static constexpr int kSecond = 1;
   static __device__ __forceinline__ int pair_of(int j) { return j & 1; }
-  // 16-byte piece c of token row t: pieces are swizzled so that eight rows' equal pieces hit all banks
-  static __device__ __forceinline__ uint32_t piece_at(int t, int c) { return t * kRowBytes + ((c ^ (t & 7)) << 4); }
+  // 16-byte piece c of token t: blocks of 64 elements, tokens 128 bytes apart, pieces swizzled so that eight
+  // tokens' equal pieces hit all banks (the tensor copies' 128-byte swizzle)
+  static __device__ __forceinline__ uint32_t piece_at(int t, int c) {
+    return (c >> 3) * kChunk * 128 + t * 128 + (((c & 7) ^ (t & 7)) << 4);
+  }
 
   // query(g): the vector of column g of the warp, or null; words: on 4-byte boundaries
   template <typename Query>
@@ -514,7 +533,7 @@ template <typename T, typename Body, int kWarps, int kStages>
 struct AttendShared {
   static constexpr int kStageBytes = 2 * Body::kChunk * Body::kRowBytes;
   static constexpr size_t kRing = (size_t)kWarps * kStages * kStageBytes;
-  static constexpr size_t kBytes = kRing + kWarps * Body::kQBytes;
+  static constexpr size_t kBytes = 1024 + kRing + kWarps * Body::kQBytes;          // the ring starts on 1024 bytes
   static_assert(Body::kRegs * 128 <= kStages * kStageBytes, "a warp's ring takes a dump of its accumulator");
 };
 
@@ -526,13 +545,24 @@ struct Left {
   int any, goes_on;            // filled; continues in the next warp
 };
 
-template <typename T, typename Body, int kWarps, int kStages>
-__global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_constant__ AttendParams p) {
+// The pools as the tensor copies see them: [page][64-element block of the head dimension][kv head, slot][64].
+struct PoolMaps {
+  CUtensorMap k, v;
+};
+constexpr int kBoxTokens = 16;       // tokens of a tensor copy
+
+// kBulk: whole chunks (16 tokens of a page at a time) come by bulk copies that one lane issues - tensor
+// copies with the 128-byte swizzle in 16 bits, plain ones in fp32 - instead of 16 bytes a lane.  Against the latter the
+// walk takes about a third fewer instructions, which is what bounds a warp with short pieces.
+template <typename T, typename Body, int kWarps, int kStages, bool kBulk>
+__global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ PoolMaps maps) {
   using S = AttendShared<T, Body, kWarps, kStages>;
   constexpr int kThreads = kWarps * 32;
   constexpr int kChunk = Body::kChunk, kRegs = Body::kRegs;
   constexpr int kPart = kRegs * 32 + 2 * kMaxHeads;
-  extern __shared__ __align__(1024) char smem[];
+  extern __shared__ char smem_raw[];
+  char* smem = smem_raw + (-(int)shared_addr(smem_raw) & 1023);
+  __shared__ __align__(8) uint64_t bars[kBulk ? kWarps * kStages : 1];
   __shared__ long long warp_sum_[kWarps];
   __shared__ int warp_max_[kWarps];
   __shared__ Place<kChunk> first[kWarps];
@@ -550,6 +580,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
   // Planning: the rows' units are summed, then the rows that hold this CTA's cuts are found.
   const int per = (kv.n_rows + kThreads - 1) / kThreads;
   const int r0 = min((int)threadIdx.x * per, kv.n_rows), r1 = min(r0 + per, kv.n_rows);
+  const uint32_t bar = shared_addr(bars) + (kBulk ? warp * kStages * 8 : 0);
+  if (kBulk && lane == 0) {
+    for (int i = 0; i < kStages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + 8 * i) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
   if (threadIdx.x == 0) n_empty = 0;
   if (lane < 2) left[warp][lane].any = 0;
   __syncthreads();
@@ -649,43 +684,80 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
     ahead_at += kPieceCost - ahead.unit;
     ahead.unit = kPieceCost;
   }
-  int entry = 0;
+  constexpr int kBoxes = kBulk && kChunk > kBoxTokens ? kChunk / kBoxTokens : 1;
+  int entry[kBoxes];
+  bool gave_up = false;
   auto look_up = [&]() {
     if (ahead_at >= wend) return;
-    const int t = (ahead.span.c0 + ahead.unit - kPieceCost) * kChunk + lane;
-    if (lane < kChunk && t < ahead.span.hi && t >= ahead.span.lo)
-      entry = kv.table[(int64_t)ahead.row * kv.max_pages + div_by(t, p.page)];
+    const int t0 = (ahead.span.c0 + ahead.unit - kPieceCost) * kChunk;
+    const int32_t* row = kv.table + (int64_t)ahead.row * kv.max_pages;
+    if constexpr (kBulk) {
+#pragma unroll
+      for (int i = 0; i < kBoxes; ++i)
+        if (t0 + i * kBoxTokens < ahead.span.hi) entry[i] = row[div_by(t0 + i * kBoxTokens, p.page)];
+    } else {
+      const int t = t0 + lane;
+      if (lane < kChunk && t < ahead.span.hi && t >= ahead.span.lo) entry[0] = row[div_by(t, p.page)];
+    }
   };
   look_up();
   auto issue = [&](int stage) {
-    if (ahead_at < wend) {
-      const int t = (ahead.span.c0 + ahead.unit - kPieceCost) * kChunk + lane, h = ahead.h;
-      const bool in = lane < kChunk && t < ahead.span.hi && t >= ahead.span.lo;
-      // where the token is: an element offset in the pools, -1 for zeros, -2 - e for element e of the new tokens
-      int64_t from = -1;
-      if (in) {
-        if (p.k_new && t == ahead.span.hi - 1) {
-          from = -2 - (ahead.row * p.new_stride + (int64_t)h * kv.head_dim);
-        } else if ((unsigned int)entry < (unsigned int)kv.n_pages) {
-          const int slot = t - (int)div_by(t, p.page) * kv.page_size;
-          from = entry * kv.page_stride + ((int64_t)h * kv.page_size + slot) * kv.head_dim;
-        } else {
-          flag(kv.status, kStatusIndex);
-        }
-      }
+    if (ahead_at < wend && !gave_up) {
+      const int t0 = (ahead.span.c0 + ahead.unit - kPieceCost) * kChunk;
       const uint32_t kb = ring + stage * S::kStageBytes, vb = kb + kChunk * Body::kRowBytes;
+      if constexpr (kBulk) {
+        // slots past the row's end come along and are cleared when the chunk is used; a bad entry reads page 0
+        const int boxes = min(kBoxes, (ahead.span.hi - t0 + kBoxTokens - 1) / kBoxTokens);
+        constexpr int kBox = kChunk / kBoxes * Body::kRowBytes;
+        if (lane == 0) expect_bytes(bar + 8 * stage, 2 * boxes * kBox);
 #pragma unroll
-      for (int i = 0; i < kChunk; i += kRowsPerCopy) {
-        const int tok = i + lane / kLanesPerRow;
-        const int64_t e = __shfl_sync(0xFFFFFFFFu, from, tok);
-        const T* kp = e >= 0 ? (const T*)kv.k + e : (const T*)p.k_new + (-2 - e);
-        const T* vp = e >= 0 ? (const T*)kv.v + e : (const T*)p.v_new + (-2 - e);
+        for (int i = 0; i < kBoxes; ++i) {
+          if (i >= boxes) continue;
+          const int t = t0 + i * kBoxTokens;
+          int page = entry[i];
+          if ((unsigned int)page >= (unsigned int)kv.n_pages) {
+            flag(kv.status, kStatusIndex);
+            page = 0;
+          }
+          const int at = ahead.h * kv.page_size + t - (int)div_by(t, p.page) * kv.page_size;
+          if (lane == 0) {
+            if constexpr (sizeof(T) == 2) {
+              copy_tensor(kb + i * kBoxTokens * 128, &maps.k, at, page, bar + 8 * stage);
+              copy_tensor(vb + i * kBoxTokens * 128, &maps.v, at, page, bar + 8 * stage);
+            } else {
+              const int64_t e = page * kv.page_stride + (int64_t)at * kv.head_dim;
+              copy_bulk(kb, (const T*)kv.k + e, kBox, bar + 8 * stage);
+              copy_bulk(vb, (const T*)kv.v + e, kBox, bar + 8 * stage);
+            }
+          }
+        }
+      } else {
+        const int t = t0 + lane;
+        // where the token is: an element offset in the pools, -1 for zeros, -2 - e for element e of the new tokens
+        int64_t from = -1;
+        if (lane < kChunk && t < ahead.span.hi && t >= ahead.span.lo) {
+          if (p.k_new && t == ahead.span.hi - 1) {
+            from = -2 - (ahead.row * p.new_stride + (int64_t)ahead.h * kv.head_dim);
+          } else if ((unsigned int)entry[0] < (unsigned int)kv.n_pages) {
+            const int slot = t - (int)div_by(t, p.page) * kv.page_size;
+            from = entry[0] * kv.page_stride + ((int64_t)ahead.h * kv.page_size + slot) * kv.head_dim;
+          } else {
+            flag(kv.status, kStatusIndex);
+          }
+        }
 #pragma unroll
-        for (int j = 0; j < kPiecesPerLane; ++j) {
-          const int c = lane % kLanesPerRow + j * kLanesPerRow;
-          const bool some = e != -1 && c < row_pieces;
-          copy_async(kb + Body::piece_at(tok, c), some ? (const char*)kp + c * 16 : (const char*)kv.k, some);
-          copy_async(vb + Body::piece_at(tok, c), some ? (const char*)vp + c * 16 : (const char*)kv.v, some);
+        for (int i = 0; i < kChunk; i += kRowsPerCopy) {
+          const int tok = i + lane / kLanesPerRow;
+          const int64_t e = __shfl_sync(0xFFFFFFFFu, from, tok);
+          const T* kp = e >= 0 ? (const T*)kv.k + e : (const T*)p.k_new + (-2 - e);
+          const T* vp = e >= 0 ? (const T*)kv.v + e : (const T*)p.v_new + (-2 - e);
+#pragma unroll
+          for (int j = 0; j < kPiecesPerLane; ++j) {
+            const int c = lane % kLanesPerRow + j * kLanesPerRow;
+            const bool some = e != -1 && c < row_pieces;
+            copy_async(kb + Body::piece_at(tok, c), some ? (const char*)kp + c * 16 : (const char*)kv.k, some);
+            copy_async(vb + Body::piece_at(tok, c), some ? (const char*)vp + c * 16 : (const char*)kv.v, some);
+          }
         }
       }
       ++ahead_at;
@@ -696,7 +768,43 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
       }
       look_up();
     }
-    copy_commit();
+    if constexpr (!kBulk) copy_commit();
+  };
+  // the stage's chunk is in place (bulk: phase parity; a wait that runs out is reported and ends the loads)
+  uint32_t parity = 0;
+  auto arrived = [&](int stage) {
+    if constexpr (kBulk) {
+      if (!gave_up && !mbarrier_wait_bounded(bar + 8 * stage, parity >> stage & 1u, kBulkWaitLimit)) {
+        gave_up = true;
+        flag(kv.status, kStatusTimeout);
+      }
+      gave_up = __any_sync(0xFFFFFFFFu, gave_up);
+      parity ^= 1u << stage;
+    } else {
+      copy_wait<kStages - 2>();
+    }
+    __syncwarp();
+  };
+  // What a bulk copy cannot do for a row's last chunk: the new token's row, and zeros past the end (V only: the
+  // scores there are masked, but 0 times what a free slot holds need not be 0).
+  auto complete = [&](const Place<kChunk>& at, int t0, char* kb, char* vb) {
+    if constexpr (kBulk) {
+      if (t0 + kChunk < at.span.hi) return;
+      for (int i = lane; i < kChunk * row_pieces; i += 32) {
+        const int tok = i / row_pieces, c = i - tok * row_pieces;
+        if (t0 + tok >= at.span.hi) *(uint4*)(vb + Body::piece_at(tok, c)) = make_uint4(0, 0, 0, 0);
+      }
+      if (p.k_new) {
+        const int64_t e = at.row * p.new_stride + (int64_t)at.h * kv.head_dim;
+        for (int c = lane; c < row_pieces; c += 32) {
+          const uint32_t to = Body::piece_at(at.span.hi - 1 - t0, c);
+          *(uint4*)(kb + to) = ((const uint4*)((const T*)p.k_new + e))[c];
+          *(uint4*)(vb + to) = ((const uint4*)((const T*)p.v_new + e))[c];
+        }
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");        // before the stage's next bulk copy
+      __syncwarp();
+    }
   };
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) issue(s);
@@ -747,10 +855,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
         body.join_shared(p, unit, column + here.split * p.piece_heads, heads, lane);
       }
       for (int j = j0; j < j1; ++j) {
-        copy_wait<kStages - 2>();
-        __syncwarp();
+        arrived(stage);
         issue(stage == 0 ? kStages - 1 : stage - 1);
         const uint32_t kb = ring + stage * S::kStageBytes;
+        char* kp = smem + (size_t)(warp * kStages + stage) * S::kStageBytes;
+        complete(here, (span.c0 + j) * kChunk, kp, kp + kChunk * Body::kRowBytes);
         body.step(p, kb, kb + kChunk * Body::kRowBytes, scratch, (span.c0 + j) * kChunk, span.lo, span.hi, lane);
         stage = stage + 1 == kStages ? 0 : stage + 1;
       }
@@ -764,7 +873,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
         __syncwarp();
       } else {
         // a piece that goes on past this warp is its last: its loads are done, and the ring is free
-        if (j0 == 0) copy_wait<0>();
+        if (!kBulk && j0 == 0) copy_wait<0>();
         __syncwarp();
         float* dump = j0 == 0 ? (float*)(smem + (size_t)warp * kStages * S::kStageBytes) : dumps + warp * kRegs * 32;
 #pragma unroll
@@ -787,7 +896,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
     if (pos < wend) here.next_piece(p);
     else break;
   }
-  copy_wait<0>();
+  if constexpr (kBulk) {
+    if (gave_up)                                       // what may still be on its way gets a second, last wait
+      for (int i = 0; i < kStages; ++i) mbarrier_wait_bounded(bar + 8 * i, parity >> i & 1u, kBulkWaitLimit);
+  } else {
+    copy_wait<0>();
+  }
   __syncthreads();
 
   // Pieces that the warps of this CTA, or several CTAs, have shared: a run of dumps is slot s0 of warp w0
@@ -919,18 +1033,53 @@ static void split_heads(int per_kv, int* n_split, int* piece_heads) {
   *piece_heads = (per_kv + *n_split - 1) / *n_split;
 }
 
-template <typename T, typename Body, int kWarps, int kStages>
-static int launch_attend(const AttendParams& p, cudaStream_t st) {
+// [n_pages][head_dim / 64][kv heads * page_size][64] 16-bit elements, boxes of 16 tokens and `blocks` blocks.
+static bool make_map(CUtensorMap* map, const AttendParams& p, const void* pool, int dtype_bf16, int blocks) {
+  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static Encode encode = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
+      f = nullptr;
+    return (Encode)f;
+  }();
+  if (!encode) return false;
+  const KvView& kv = p.kv;
+  const cuuint64_t size[4] = {64, (cuuint64_t)kv.n_kv_heads * kv.page_size, (cuuint64_t)kv.head_dim / 64, (cuuint64_t)kv.n_pages};
+  const cuuint64_t stride[3] = {(cuuint64_t)kv.head_dim * 2, 128, (cuuint64_t)kv.page_stride * 2};
+  const cuuint32_t box[4] = {64, (cuuint32_t)kBoxTokens, (cuuint32_t)blocks, 1}, step[4] = {1, 1, 1, 1};
+  return encode(map, dtype_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, (void*)pool, size, stride, box, step,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, typename Body, int kWarps, int kStages, bool kBulk>
+static int launch_attend(const AttendParams& p, const PoolMaps& maps, cudaStream_t st) {
   using S = AttendShared<T, Body, kWarps, kStages>;
-  static_assert(S::kBytes <= 222 * 1024, "shared memory");
+  static_assert(S::kBytes <= 223 * 1024, "shared memory");
   static_assert(kWarps <= kMaxWarps, "workspace");
-  auto kernel = attend_kernel<T, Body, kWarps, kStages>;
+  auto kernel = attend_kernel<T, Body, kWarps, kStages, kBulk>;
   PG_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes));
   const long long most = (long long)p.kv.n_rows * p.kv.n_kv_heads * p.n_split *
                          (((long long)p.kv.max_pages * p.kv.page_size + Body::kChunk - 1) / Body::kChunk);
-  kernel<<<(unsigned)(most < kSms ? most : kSms), kWarps * 32, S::kBytes, st>>>(p);
+  kernel<<<(unsigned)(most < kSms ? most : kSms), kWarps * 32, S::kBytes, st>>>(p, maps);
   PG_LAUNCH_CHECK();
   return PG_OK;
+}
+
+// Bulk copies where 16 tokens in a row always lie in one page, and no padding has to be filled in between: head
+// dim a multiple of 64 (tensor copies, 16 bits; what is past it up to the body's size is outside the map and reads
+// as zeros) or the body's own size (fp32).
+template <typename T, typename Body, int DP, int kWarps, int kStages>
+static int launch_copies(const AttendParams& p, cudaStream_t st) {
+  PoolMaps maps;
+  bool bulk = p.kv.page_size % kBoxTokens == 0 && p.kv.head_dim % 64 == 0 && (sizeof(T) == 2 || p.kv.head_dim == DP);
+  if (bulk && sizeof(T) == 2) {
+    const bool bf = std::is_same<T, __nv_bfloat16>::value;
+    bulk = make_map(&maps.k, p, p.kv.k, bf, DP / 64) && make_map(&maps.v, p, p.kv.v, bf, DP / 64);
+  }
+  return bulk ? launch_attend<T, Body, kWarps, kStages, true>(p, maps, st) : launch_attend<T, Body, kWarps, kStages, false>(p, maps, st);
 }
 
 // One CTA per SM; its warps' rings take most of the shared memory (three stages of 8 KB for eight warps,
@@ -938,8 +1087,8 @@ static int launch_attend(const AttendParams& p, cudaStream_t st) {
 template <typename T, template <int, int> class Body, int DP, int NT>
 static int launch_body(const AttendParams& p, cudaStream_t st) {
   constexpr int kStage = 2 * Body<DP, NT>::kChunk * Body<DP, NT>::kRowBytes;
-  if constexpr (sizeof(T) == 2 && DP <= 128) return launch_attend<T, Body<DP, NT>, 8, 3>(p, st);
-  else return launch_attend<T, Body<DP, NT>, 4, 4 * (3 * kStage + (int)Body<DP, NT>::kQBytes) <= 222 * 1024 ? 3 : 2>(p, st);
+  if constexpr (sizeof(T) == 2 && DP <= 128) return launch_copies<T, Body<DP, NT>, DP, 8, 3>(p, st);
+  else return launch_copies<T, Body<DP, NT>, DP, 4, 4 * (3 * kStage + (int)Body<DP, NT>::kQBytes) <= 221 * 1024 ? 3 : 2>(p, st);
 }
 
 template <typename T, template <int, int> class Body>
