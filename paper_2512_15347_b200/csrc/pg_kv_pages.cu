@@ -11,7 +11,7 @@
 namespace pg {
 
 // ---------------------------------------------------------------- scans in one CTA
-constexpr int kScanThreads = 1024;
+constexpr int kScanThreads = 1024;          // of the kernels that are one CTA
 
 // Exclusive prefix sum over the CTA; *total gets the sum.  All threads call.
 __device__ __forceinline__ int block_scan(int v, int* total) {
@@ -44,24 +44,17 @@ __device__ __forceinline__ int block_scan(int v, int* total) {
 // there were (at most wanted).  One CTA.
 template <typename Take>
 __device__ __forceinline__ int take_free(const int32_t* refs, int n_pages, int wanted, Take take) {
+  constexpr int kPer = 8;
   int found = 0;
-  for (int base = 0; base < n_pages && found < wanted; base += kScanThreads * 4) {
-    const int p = base + threadIdx.x * 4;
-    bool free[4];
-    int mine = 0;
+  for (int base = 0; base < n_pages && found < wanted; base += blockDim.x * kPer) {
+    const int p = base + threadIdx.x * kPer;
+    uint32_t free = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      free[i] = p + i < n_pages && __ldcg(&refs[p + i]) == 0;
-      mine += free[i];
-    }
+    for (int i = 0; i < kPer; ++i) free |= (uint32_t)(p + i < n_pages && __ldcg(&refs[p + i]) == 0) << i;
     int total;
-    int k = found + block_scan(mine, &total);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (free[i]) {
-        if (k < wanted) take(k, p + i);
-        ++k;
-      }
+    int k = found + block_scan(__popc(free), &total);
+    for (; free; free &= free - 1, ++k)
+      if (k < wanted) take(k, p + __ffs(free) - 1);
     found += total;
   }
   __syncthreads();
@@ -70,46 +63,75 @@ __device__ __forceinline__ int take_free(const int32_t* refs, int n_pages, int w
 
 // ---------------------------------------------------------------- copies of whole pages
 // Pairs (from, to) in device memory, their number too.  A page of one layer and one of k / v is
-// contiguous but for its stride: kv heads * page_size * head_dim elements.
+// contiguous but for its stride: kv heads * page_size * head_dim elements.  An item is one 32 KB piece of
+// `run` consecutive pairs: forks of one row follow each other and have the same source, which is then read once a run.
+// Bound: HBM.  The first table_ctas CTAs remap the table instead (pack).
 struct CopyParams {
   KvView kv;
   const int2* pairs;
   const int32_t* n_pairs;
   int64_t page_words, stride_words, layer_words;   // 16-byte words
-  int pieces;                                       // CTA-sized pieces of a page
+  int pieces, run;                                  // CTA-sized pieces of a page
+  const int32_t* to;
+  int32_t* table_out;
+  unsigned table_ctas;
 };
 constexpr int kCopyThreads = 256;
-constexpr int kCopyWords = kCopyThreads * 8;        // 32 KB a piece
+constexpr int kCopyPer = 8;
+constexpr int kCopyWords = kCopyThreads * kCopyPer; // 32 KB a piece
+
+__device__ __forceinline__ void remap_table(const CopyParams& p) {
+  const KvView& kv = p.kv;
+  const int64_t entries = (int64_t)kv.n_rows * kv.max_pages;
+  for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < entries; i += (int64_t)p.table_ctas * kCopyThreads) {
+    const int row = (int)(i / kv.max_pages), j = (int)(i - (int64_t)row * kv.max_pages);
+    const int n = row_len(kv, row), pages = (n + kv.page_size - 1) / kv.page_size;
+    int to = -1;
+    if (j < pages) {
+      const int page = kv.table[i];
+      if ((unsigned int)page < (unsigned int)kv.n_pages) to = p.to[page];
+      if (to < 0) flag(kv.status, kStatusIndex);
+    }
+    p.table_out[i] = to;
+  }
+}
 
 __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_constant__ CopyParams p) {
-  const int64_t per_pair = (int64_t)p.pieces * p.kv.n_layers * 2;
-  const int64_t items = *p.n_pairs * per_pair;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int64_t pair = item / per_pair;
-    int rest = (int)(item - pair * per_pair);
+  if (blockIdx.x < p.table_ctas) return remap_table(p);
+  const int n_pairs = *p.n_pairs, per_run = p.pieces * p.kv.n_layers * 2;
+  const int64_t items = (int64_t)((n_pairs + p.run - 1) / p.run) * per_run;
+  for (int64_t item = blockIdx.x - p.table_ctas; item < items; item += gridDim.x - p.table_ctas) {
+    const int first = (int)(item / per_run) * p.run;
+    int rest = (int)(item % per_run);
     const int piece = rest % p.pieces;
     rest /= p.pieces;
-    const int2 move = p.pairs[pair];
     uint4* pool = (uint4*)((rest & 1) ? p.kv.v : p.kv.k) + (rest >> 1) * p.layer_words + (int64_t)piece * kCopyWords;
-    const uint4* from = pool + move.x * p.stride_words;
-    uint4* to = pool + move.y * p.stride_words;
     const int n = (int)min((int64_t)kCopyWords, p.page_words - (int64_t)piece * kCopyWords);
-    uint4 w[kCopyWords / kCopyThreads];
+    uint4 w[kCopyPer];
+    int held = -1;
+    for (int k = first; k < min(first + p.run, n_pairs); ++k) {
+      const int2 move = p.pairs[k];
+      if (move.x != held) {
+        const uint4* from = pool + move.x * p.stride_words;
 #pragma unroll
-    for (int i = 0; i < kCopyWords / kCopyThreads; ++i) {
-      const int at = threadIdx.x + i * kCopyThreads;
-      if (at < n) w[i] = __ldcs(from + at);
-    }
+        for (int i = 0; i < kCopyPer; ++i) {
+          const int at = threadIdx.x + i * kCopyThreads;
+          if (at < n) w[i] = __ldcs(from + at);
+        }
+        held = move.x;
+      }
+      uint4* to = pool + move.y * p.stride_words;
 #pragma unroll
-    for (int i = 0; i < kCopyWords / kCopyThreads; ++i) {
-      const int at = threadIdx.x + i * kCopyThreads;
-      if (at < n) __stcs(to + at, w[i]);
+      for (int i = 0; i < kCopyPer; ++i) {
+        const int at = threadIdx.x + i * kCopyThreads;
+        if (at < n) __stcs(to + at, w[i]);
+      }
     }
   }
 }
 
-static int launch_copy(const pg_kv* kv, const KvView& view, const int2* pairs, const int32_t* n_pairs, int64_t most,
-                       cudaStream_t st) {
+static int launch_copy(const pg_kv* kv, const KvView& view, const int2* pairs, const int32_t* n_pairs, int64_t most, int run,
+                       const int32_t* to, int32_t* table_out, cudaStream_t st) {
   const int64_t b = (int64_t)dtype_bytes(kv->dtype);
   CopyParams p;
   p.kv = view;
@@ -121,8 +143,13 @@ static int launch_copy(const pg_kv* kv, const KvView& view, const int2* pairs, c
   const int64_t pieces = (p.page_words + kCopyWords - 1) / kCopyWords;
   if (pieces * kv->n_layers * 2 > 0x7FFFFFFFLL) return PG_EINVAL;
   p.pieces = (int)pieces;
-  const int64_t items = most * pieces * kv->n_layers * 2;
-  copy_pages_kernel<<<(unsigned)std::min<int64_t>(std::max<int64_t>(items, 1), 148 * 8), kCopyThreads, 0, st>>>(p);
+  p.run = run;
+  p.to = to;
+  p.table_out = table_out;
+  const int64_t entries = table_out ? (int64_t)kv->n_rows * kv->max_pages : 0;
+  p.table_ctas = (unsigned)std::min<int64_t>((entries + kCopyThreads * 4 - 1) / (kCopyThreads * 4), 148);
+  const int64_t items = (most + run - 1) / run * pieces * kv->n_layers * 2;
+  copy_pages_kernel<<<p.table_ctas + (unsigned)std::min<int64_t>(std::max<int64_t>(items, 1), 148 * 8), kCopyThreads, 0, st>>>(p);
   PG_LAUNCH_CHECK();
   return PG_OK;
 }
@@ -130,6 +157,7 @@ static int launch_copy(const pg_kv* kv, const KvView& view, const int2* pairs, c
 // ---------------------------------------------------------------- fork
 
 struct ForkWork {            // in the caller's workspace
+  unsigned int* ticket;      // zero between calls
   int32_t* n_pairs;          // copies to make
   int32_t* need;             // [n_out] 1 where new row i needs a page for its partly filled last page
   int2* pairs;               // [n_out]
@@ -138,98 +166,134 @@ static size_t fork_work(char* base, int64_t n_out, ForkWork* w) {
   auto up = [](size_t b) { return (b + 15) & ~(size_t)15; };
   const size_t need = up(n_out * 4), pairs = up(n_out * 8);
   if (w) {
-    w->n_pairs = (int32_t*)base;
+    w->ticket = (unsigned int*)base;
+    w->n_pairs = (int32_t*)(base + 4);
     w->need = (int32_t*)(base + 16);
     w->pairs = (int2*)(base + 16 + need);
   }
   return 16 + need + pairs;
 }
 
+constexpr int kForkThreads = 256, kForkRows = 32;   // most old rows of a CTA
+
 struct ForkParams {
   KvView kv;
   const int32_t* src;
   int32_t *table_out, *len_out, *refs;
   ForkWork w;
-  int n_out;
+  int n_out, rows;           // rows: old rows of a CTA
 };
 
-// Sum over the CTA of a per-thread count.
-__device__ __forceinline__ int block_sum(int v) {
-  __shared__ int parts[32];
-  v = __reduce_add_sync(0xFFFFFFFFu, v);
-  if ((threadIdx.x & 31) == 0) parts[threadIdx.x >> 5] = v;
-  __syncthreads();
-  int s = 0;
-  for (int w = 0; w < (int)(blockDim.x >> 5); ++w) s += parts[w];
-  __syncthreads();
-  return s;
-}
-
-// CTAs [0, n_rows): the pages of old row s change by (children - 1); its partly filled last page stays
-// with one child, or goes.  CTAs [n_rows, n_rows + n_out): the table row of a new row.
-__global__ void __launch_bounds__(128) fork_rows_kernel(const __grid_constant__ ForkParams p) {
-  const KvView& kv = p.kv;
-  const int n_old = kv.n_rows;
-  if ((int)blockIdx.x < n_old) {
-    const int s = blockIdx.x;
-    int mine = 0;
-    for (int i = threadIdx.x; i < p.n_out; i += blockDim.x) mine += p.src[i] == s;
-    const int children = block_sum(mine);
-    const int n = row_len(kv, s), pages = (n + kv.page_size - 1) / kv.page_size;
-    const bool part = n % kv.page_size != 0;
-    for (int j = threadIdx.x; j < pages; j += blockDim.x) {
-      const int page = kv.table[(int64_t)s * kv.max_pages + j];
-      if ((unsigned int)page >= (unsigned int)kv.n_pages) { flag(kv.status, kStatusIndex); continue; }
-      const int delta = (part && j == pages - 1 ? min(children, 1) : children) - 1;
-      if (delta) atomicAdd(&p.refs[page], delta);
-    }
-    return;
-  }
-  const int i = blockIdx.x - n_old;
-  const int s = p.src[i];
-  const bool ok = (unsigned int)s < (unsigned int)n_old;
-  if (!ok && s != -1 && threadIdx.x == 0) flag(kv.status, kStatusIndex);
-  int mine = 0;
-  for (int j = threadIdx.x; j < i; j += blockDim.x) mine += p.src[j] == s;
-  const bool first = block_sum(mine) == 0;
-  const int n = ok ? row_len(kv, s) : 0, pages = (n + kv.page_size - 1) / kv.page_size;
-  for (int j = threadIdx.x; j < kv.max_pages; j += blockDim.x)
-    p.table_out[(int64_t)i * kv.max_pages + j] = j < pages ? kv.table[(int64_t)s * kv.max_pages + j] : -1;
-  if (threadIdx.x == 0) {
-    p.len_out[i] = n;
-    p.w.need[i] = n % kv.page_size != 0 && !first;
-  }
-}
-
-// Pages for the rows that need one, and the list of copies.
-__global__ void __launch_bounds__(kScanThreads) fork_assign_kernel(const __grid_constant__ ForkParams p) {
+// Pages for the rows that need one, and the list of copies.  One CTA, after all others.
+__device__ __forceinline__ void fork_assign(const ForkParams& p) {
   const KvView& kv = p.kv;
   int wanted = 0;
-  for (int base = 0; base < p.n_out; base += kScanThreads) {     // pairs[k].x = the k-th row in need, for now
-    const int i = base + threadIdx.x;
-    const int need = i < p.n_out ? p.w.need[i] : 0;
+  for (int base = 0; base < p.n_out; base += blockDim.x * 4) {     // pairs[k].x = the k-th row in need, for now
+    const int i0 = base + threadIdx.x * 4;
+    int need[4], mine = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      need[e] = i0 + e < p.n_out ? __ldcg(&p.w.need[i0 + e]) : 0;
+      mine += need[e];
+    }
     int total;
-    const int k = wanted + block_scan(need, &total);
-    if (need) p.w.pairs[k].x = i;
+    int k = wanted + block_scan(mine, &total);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (need[e]) p.w.pairs[k++].x = i0 + e;
     wanted += total;
   }
   __syncthreads();
   const int found = take_free(p.refs, kv.n_pages, wanted, [&](int k, int page) {
     const int i = p.w.pairs[k].x;
-    const int64_t last = (int64_t)i * kv.max_pages + p.len_out[i] / kv.page_size;
-    const int from = p.table_out[last];
+    const int64_t last = (int64_t)i * kv.max_pages + __ldcg(&p.len_out[i]) / kv.page_size;
+    const int from = __ldcg(&p.table_out[last]);
     p.table_out[last] = page;
     p.refs[page] = 1;
     p.w.pairs[k] = (unsigned int)from < (unsigned int)kv.n_pages ? make_int2(from, page) : make_int2(page, page);
   });
-  for (int k = found + threadIdx.x; k < wanted; k += kScanThreads) {   // no page: the full pages remain
+  for (int k = found + threadIdx.x; k < wanted; k += blockDim.x) {   // no page: the full pages remain
     const int i = p.w.pairs[k].x;
-    const int full = p.len_out[i] / kv.page_size;
+    const int full = __ldcg(&p.len_out[i]) / kv.page_size;
     p.table_out[(int64_t)i * kv.max_pages + full] = -1;
     p.len_out[i] = full * kv.page_size;
     flag(kv.status, kStatusPages);
   }
   if (threadIdx.x == 0) *p.w.n_pairs = found;
+}
+
+// A CTA takes `rows` old rows: it goes through src_rows once, 1024 entries at a time, and writes the table rows
+// of their forks (CTA 0: also of entries that name no row); then the rows' pages change by (forks - 1), a
+// partly filled last page by (min(forks, 1) - 1).  The last CTA to finish hands out the pages.
+__global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constant__ ForkParams p) {
+  __shared__ int forks[kForkRows], length[kForkRows], n_found, is_last;
+  __shared__ int2 found[kForkThreads * 4];            // (new row, old row within the CTA or -1)
+  const KvView& kv = p.kv;
+  const int s0 = blockIdx.x * p.rows, n_rows = max(0, min(p.rows, kv.n_rows - s0));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if ((int)threadIdx.x < n_rows) {
+    forks[threadIdx.x] = 0;
+    length[threadIdx.x] = row_len(kv, s0 + threadIdx.x);
+  }
+  for (int base = 0; base < p.n_out; base += kForkThreads * 4) {
+    __syncthreads();
+    if (threadIdx.x == 0) n_found = 0;
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int i = base + e * kForkThreads + threadIdx.x;
+      if (i >= p.n_out) continue;
+      const int s = p.src[i];
+      const bool none = (unsigned int)s >= (unsigned int)kv.n_rows;
+      if ((unsigned int)(s - s0) < (unsigned int)n_rows) found[atomicAdd(&n_found, 1)] = make_int2(i, s - s0);
+      else if (none && blockIdx.x == 0) found[atomicAdd(&n_found, 1)] = make_int2(i, s == -1 ? -1 : -2);
+    }
+    __syncthreads();
+    // the first fork of a row in need of a page keeps the row's own: the smallest new row of the earliest batch
+    for (int f = warp; f < n_found; f += kForkThreads / 32) {
+      const int2 x = found[f];
+      const int n = x.y >= 0 ? length[x.y] : 0, pages = (n + kv.page_size - 1) / kv.page_size;
+      const int32_t* from = kv.table + (int64_t)(s0 + max(x.y, 0)) * kv.max_pages;
+      int32_t* to = p.table_out + (int64_t)x.x * kv.max_pages;
+      for (int j = lane; j < kv.max_pages; j += 32) to[j] = j < pages ? from[j] : -1;
+      bool need = false;
+      if (x.y >= 0 && n % kv.page_size != 0) {
+        need = forks[x.y] > 0;                        // of earlier batches
+        for (int g = lane; g < n_found && !need; g += 32) need = found[g].y == x.y && found[g].x < x.x;
+        need = __any_sync(0xFFFFFFFFu, need);
+      }
+      if (lane == 0) {
+        if (x.y == -2) flag(kv.status, kStatusIndex);
+        p.len_out[x.x] = n;
+        p.w.need[x.x] = need;
+      }
+    }
+    __syncthreads();
+    for (int f = threadIdx.x; f < n_found; f += kForkThreads)
+      if (found[f].y >= 0) atomicAdd(&forks[found[f].y], 1);
+  }
+  __syncthreads();
+  for (int r = warp; r < n_rows; r += kForkThreads / 32) {
+    const int n = length[r], pages = (n + kv.page_size - 1) / kv.page_size, full = n / kv.page_size;
+    const int all = forks[r] - 1, part = min(forks[r], 1) - 1;
+    if (all == 0) continue;
+    for (int j = lane; j < pages; j += 32) {
+      const int page = kv.table[(int64_t)(s0 + r) * kv.max_pages + j];
+      if ((unsigned int)page >= (unsigned int)kv.n_pages) flag(kv.status, kStatusIndex);
+      else if (const int d = j < full ? all : part) atomicAdd(&p.refs[page], d);
+    }
+  }
+  if (p.n_out == 0) return;
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    is_last = atomicAdd(p.w.ticket, 1u) == gridDim.x - 1;
+    if (is_last) *p.w.ticket = 0;
+  }
+  __syncthreads();
+  if (!is_last) return;
+  __threadfence();
+  fork_assign(p);
 }
 
 // ---------------------------------------------------------------- pack
@@ -257,52 +321,48 @@ struct PackParams {
   PackWork w;
 };
 
-// The k-th page in use at n_live or above moves into the k-th free page below n_live.
+// The k-th page in use at n_live or above moves into the k-th free page below n_live.  One CTA; a thread
+// has eight pages at a time.
 __global__ void __launch_bounds__(kScanThreads) pack_plan_kernel(const __grid_constant__ PackParams p) {
+  constexpr int kPer = 8;
   const int n = p.kv.n_pages;
   int mine = 0, n_live, moves = 0;
   for (int i = threadIdx.x; i < n; i += kScanThreads) mine += p.refs[i] > 0;
   block_scan(mine, &n_live);
   int holes = 0;
-  for (int base = 0; base < n; base += kScanThreads) {
-    const int i = base + threadIdx.x;
-    const bool live = i < n && p.refs[i] > 0;
-    const int hole = i < n_live && !live, mover = i >= n_live && live;
-    int total, total2;
-    const int kh = holes + block_scan(hole, &total), km = moves + block_scan(mover, &total2);
-    if (hole) p.w.pairs[kh].y = i;
-    if (mover) p.w.pairs[km].x = i;
-    if (i < n) p.w.to[i] = live ? i : -1;
-    holes += total;
-    moves += total2;
+  for (int base = 0; base < n; base += kScanThreads * kPer) {
+    const int i0 = base + threadIdx.x * kPer;
+    uint32_t hole = 0, mover = 0;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const int i = i0 + e;
+      if (i >= n) continue;
+      const bool live = p.refs[i] > 0;
+      hole |= (uint32_t)(i < n_live && !live) << e;
+      mover |= (uint32_t)(i >= n_live && live) << e;
+      p.w.to[i] = live ? i : -1;
+    }
+    int total;                                        // both counts in one scan: at most 8192 a batch
+    const int before = block_scan(__popc(hole) | __popc(mover) << 16, &total);
+    int kh = holes + (before & 0xFFFF), km = moves + (before >> 16);
+    for (; hole; hole &= hole - 1) p.w.pairs[kh++].y = i0 + __ffs(hole) - 1;
+    for (; mover; mover &= mover - 1) p.w.pairs[km++].x = i0 + __ffs(mover) - 1;
+    holes += total & 0xFFFF;
+    moves += total >> 16;
   }
-  __syncthreads();
-  for (int k = threadIdx.x; k < moves; k += kScanThreads) p.w.to[p.w.pairs[k].x] = p.w.pairs[k].y;
-  if (threadIdx.x == 0) *p.w.n_pairs = moves;
   __syncthreads();
   for (int k = threadIdx.x; k < moves; k += kScanThreads) {
     const int2 m = p.w.pairs[k];
+    p.w.to[m.x] = m.y;
     const int c = p.refs[m.x];
     p.refs_out[m.y] = c;
     p.refs_out[m.x] = 0;
   }
-  if (p.page_map)
+  if (threadIdx.x == 0) *p.w.n_pairs = moves;
+  if (p.page_map) {
+    __syncthreads();
     for (int i = threadIdx.x; i < n; i += kScanThreads) p.page_map[i] = p.w.to[i];
-}
-
-__global__ void __launch_bounds__(256) pack_table_kernel(const __grid_constant__ PackParams p) {
-  const KvView& kv = p.kv;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (int64_t)kv.n_rows * kv.max_pages) return;
-  const int row = (int)(i / kv.max_pages), j = (int)(i - (int64_t)row * kv.max_pages);
-  const int n = row_len(kv, row), pages = (n + kv.page_size - 1) / kv.page_size;
-  int to = -1;
-  if (j < pages) {
-    const int page = kv.table[i];
-    if ((unsigned int)page < (unsigned int)kv.n_pages) to = p.w.to[page];
-    if (to < 0) flag(kv.status, kStatusIndex);
   }
-  p.table_out[i] = to;
 }
 
 // ---------------------------------------------------------------- extend
@@ -453,12 +513,13 @@ int pg_kv_fork(const pg_kv* kv, int32_t n_out, const int32_t* src_rows, int32_t*
   p.kv = pg::kv_view(kv, status);
   p.src = src_rows; p.table_out = table_out; p.len_out = len_out; p.refs = refs_out; p.n_out = n_out;
   pg::fork_work((char*)workspace, n_out, &p.w);
-  pg::fork_rows_kernel<<<(unsigned)(kv->n_rows + n_out), 128, 0, st>>>(p);
+  // few old rows: one a CTA; many: as many as leave two CTAs per SM
+  p.rows = (int)std::min<int64_t>(std::max<int64_t>(kv->n_rows / (148 * 2), 1), pg::kForkRows);
+  const unsigned ctas = (unsigned)std::max<int64_t>(((int64_t)kv->n_rows + p.rows - 1) / p.rows, 1);
+  pg::fork_kernel<<<ctas, pg::kForkThreads, 0, st>>>(p);
   PG_LAUNCH_CHECK();
   if (n_out == 0) return PG_OK;
-  pg::fork_assign_kernel<<<1, pg::kScanThreads, 0, st>>>(p);
-  PG_LAUNCH_CHECK();
-  return pg::launch_copy(kv, p.kv, p.w.pairs, p.w.n_pairs, n_out, st);
+  return pg::launch_copy(kv, p.kv, p.w.pairs, p.w.n_pairs, n_out, 8, nullptr, nullptr, st);
 }
 
 size_t pg_kv_pack_workspace_bytes(const pg_kv* kv) {
@@ -482,13 +543,7 @@ int pg_kv_pack(const pg_kv* kv, const int32_t* refs, int32_t* refs_out, int32_t*
   pg::pack_work((char*)workspace, kv->n_pages, &p.w);
   pg::pack_plan_kernel<<<1, pg::kScanThreads, 0, st>>>(p);
   PG_LAUNCH_CHECK();
-  const int64_t entries = (int64_t)kv->n_rows * kv->max_pages;
-  if ((entries + 255) / 256 > 0x7FFFFFFFLL) return PG_EINVAL;
-  if (entries > 0) {
-    pg::pack_table_kernel<<<(unsigned)((entries + 255) / 256), 256, 0, st>>>(p);
-    PG_LAUNCH_CHECK();
-  }
-  return pg::launch_copy(kv, p.kv, p.w.pairs, p.w.n_pairs, kv->n_pages / 2, st);
+  return pg::launch_copy(kv, p.kv, p.w.pairs, p.w.n_pairs, kv->n_pages / 2, 1, p.w.to, kv->n_rows > 0 ? table_out : nullptr, st);
 }
 
 int pg_kv_extend(const pg_kv* kv, const int32_t* n_new, int32_t n_uniform, int32_t* len_out, const int32_t* refs,
