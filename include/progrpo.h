@@ -575,7 +575,7 @@ int pg_kv_status(const int32_t *status, void *stream);
  * Sampling rules on logits.  For token v of row r, with c = its count among the generated tokens
  * tokens[r][n_prompt[r] .. n_tokens[r]) and `seen` = it occurs in tokens[r][0 .. n_tokens[r]):
  *     x = logits[r][v];   seen: x = x > 0 ? x / repetition[r] : x * repetition[r]
- *     x = x - (frequency[r] * c + presence[r] * (c > 0));   x = x + bias(r, v);   x = x / temperature[r]
+ *     x = x - (frequency[r] * c + presence[r] * (c > 0));   x = x + bias(r, v);   x = x * (1 / temperature[r])
  *     out[r][v] = mask bit v of row r set ? x : -inf
  * in fp32, rounded once to out_dtype.  Every array is optional (NULL: the rule is not applied).
  */
@@ -583,7 +583,8 @@ typedef struct {
   const int32_t *tokens;      /* [n_rows] histories, token_stride int32 apart; ids outside [0, vocab) are
                                  skipped (padding)                                                      */
   int64_t token_stride;
-  int32_t max_tokens;         /* most tokens of any row, <= PG_LOGITS_MAX_TOKENS; larger n_tokens count as it */
+  int32_t max_tokens;         /* most tokens of any row, <= PG_LOGITS_MAX_TOKENS; larger n_tokens count as it;
+                                 so many entries of every row must be readable                           */
   const int32_t *n_tokens;    /* [n_rows]; NULL: max_tokens for every row                               */
   const int32_t *n_prompt;    /* [n_rows]; NULL: 0 (all tokens were generated)                          */
   const float *repetition, *presence, *frequency, *temperature;   /* [n_rows] fp32; repetition, temperature > 0 */

@@ -1,13 +1,17 @@
 // Sampling rules on logits (pg_logits_process): penalties for repeated tokens, biases, temperature and
 // grammar masks in one pass over the logits.
 //
-// Bound: HBM, each logit read and written once.  A row is cut into slices of 2048 * kUnits tokens, one CTA
-// each: it starts its loads, counts the row's history into one word per token of its slice in shared
-// memory (every slice scans the whole history - 4 bytes a token from L2, against 4 to 8 bytes a token of
-// the vocabulary from HBM - which needs neither a count array in global memory nor a second launch),
-// then applies the rules from registers.  A bit per token says whether its word has to be read at all.
-// Slices are 8192 tokens where that fills the GPU several times over, else shorter ones (latency).
+// Bound: HBM, each logit read and written once.  A CTA takes a part of a row and works in three steps:
+//   1. the tokens of the row's history and the biases that fall into the part go into a table in shared memory
+//      (a hash table, or one place per token where that is no larger); their results are computed there;
+//   2. the part streams through registers with the temperature and the mask alone;
+//   3. the table's results are written over the streamed ones.
+// So the penalties cost what the few tokens cost that have one: testing every logit for a penalty on the way
+// (a word or a bit per token of the part) took twice the time of the stream in instructions and barriers.
+// Every part scans the row's whole history, so parts are as long as the number of rows allows.
 #include "pg_kv.cuh"
+
+#include <algorithm>
 
 namespace pg {
 
@@ -16,12 +20,14 @@ struct LogitsParams {
   const void* in;
   void* out;
   int64_t in_stride, out_stride;
-  int vocab, slices;
+  int vocab, parts, part;      // parts of a row, tokens of a part
+  int slots, direct;           // of the table; direct: one for each token of the part
 };
 
-constexpr int kLogitsThreads = 256;
+constexpr int kLogitsThreads = 512;
 constexpr int kUnit = 8;                      // tokens that a thread handles at a time
-// Per token of the slice one word: bit 31 seen, bits 20..30 bias entry + 1, bits 0..19 count.
+constexpr int kGrain = kLogitsThreads * kUnit;
+// A table entry counts in one word: bit 31 seen, bits 20..30 bias entry + 1, bits 0..19 count.
 constexpr uint32_t kSeen = 0x80000000u, kCountMask = 0xFFFFFu;
 constexpr int kBiasShift = 20;
 
@@ -81,132 +87,161 @@ __device__ __forceinline__ void store8(T* at, const float (&x)[8]) {
   }
 }
 
-template <typename In, typename Out, int kUnits>
-__global__ void __launch_bounds__(kLogitsThreads, 4)
+template <typename In, typename Out>
+__global__ void __launch_bounds__(kLogitsThreads, 3)
 logits_kernel(const __grid_constant__ LogitsParams p) {
-  constexpr int kSlice = kLogitsThreads * kUnits * kUnit;
-  __shared__ __align__(16) uint32_t word[kSlice];
-  __shared__ uint32_t touched[kSlice / 32];
+  constexpr int kBatch = 4;                                       // units of a thread in flight
+  extern __shared__ int32_t table[];                              // [slots] tokens (-1: none), [slots] words, later results
   const pg_logits_rules& r = p.r;
-  const int row = blockIdx.x / p.slices, slice = blockIdx.x - row * p.slices;
+  const int row = blockIdx.x / p.parts;
   const In* in = (const In*)p.in + row * p.in_stride;
   Out* out = (Out*)p.out + row * p.out_stride;
   // Units of eight tokens lie on 16-byte boundaries of the row's memory: the first begins `lead` tokens before it.
   const int lead = (int)(((uintptr_t)in & 15) / sizeof(In));
-  const int first = slice * kSlice - lead;                        // token of the slice's word 0, may be negative
+  const int begin = (blockIdx.x - row * p.parts) * p.part - lead;      // the part's first unit, may be negative
+  const int lo = max(begin, 0), hi = min(begin + p.part, p.vocab);
+  if (lo >= hi) return;
   const bool out_aligned = (((uintptr_t)(out - lead)) & 15) == 0;
-
-  Raw8<In> raw[kUnits];
-#pragma unroll
-  for (int u = 0; u < kUnits; ++u) {
-    const int t = first + (u * kLogitsThreads + (int)threadIdx.x) * kUnit;
-    if (t >= 0 && t + kUnit <= p.vocab) load8(in + t, raw[u]);
-  }
-  const float rho = r.repetition ? r.repetition[row] : 1.f, pi = r.presence ? r.presence[row] : 0.f;
-  const float phi = r.frequency ? r.frequency[row] : 0.f, tau = r.temperature ? r.temperature[row] : 1.f;
   const uint32_t* mask = r.mask ? r.mask + row * r.mask_stride : nullptr;
   const int words = (p.vocab + 31) >> 5;
+  const float inv = r.temperature ? 1.f / r.temperature[row] : 1.f;
 
-  const bool any = r.tokens || r.bias_ids;
-  if (any) {
-    for (int i = threadIdx.x; i < kSlice / 4; i += kLogitsThreads) ((uint4*)word)[i] = make_uint4(0, 0, 0, 0);
-    for (int i = threadIdx.x; i < kSlice / 32; i += kLogitsThreads) touched[i] = 0;
+  // step 1
+  int32_t* key = table;
+  uint32_t* word = (uint32_t*)table + p.slots;
+  if (p.slots) {
+    const int32_t* tokens = r.tokens ? r.tokens + row * r.token_stride : nullptr;
+    const int n = tokens ? min(max(r.n_tokens ? r.n_tokens[row] : r.max_tokens, 0), r.max_tokens) : 0;
+    const int n0 = r.n_prompt ? r.n_prompt[row] : 0;
+    const float rho = r.repetition ? r.repetition[row] : 1.f, pi = r.presence ? r.presence[row] : 0.f;
+    const float phi = r.frequency ? r.frequency[row] : 0.f;
+    for (int i = threadIdx.x; i < p.slots; i += kLogitsThreads) {
+      key[i] = -1;
+      word[i] = 0;
+    }
     __syncthreads();
+    // place of a token of the part; there are more slots than tokens and biases, so the search ends
+    auto place = [&](int id) {
+      if (p.direct) {
+        key[id - begin] = id;
+        return id - begin;
+      }
+      int at = (int)__umulhi((uint32_t)id * 2654435761u, (uint32_t)p.slots);
+      for (;;) {
+        const int held = atomicCAS(&key[at], -1, id);
+        if (held == -1 || held == id) return at;
+        at = at + 1 == p.slots ? 0 : at + 1;
+      }
+    };
     if (r.bias_ids) {
       for (int j = threadIdx.x; j < r.n_bias; j += kLogitsThreads) {
         const int id = r.bias_ids[(int64_t)row * r.n_bias + j];
-        const unsigned int at = (unsigned int)(id - first);
-        if ((unsigned int)id < (unsigned int)p.vocab && at < (unsigned int)kSlice) {
-          atomicMax(&word[at], (uint32_t)(j + 1) << kBiasShift);
-          atomicOr(&touched[at >> 5], 1u << (at & 31));
-        }
+        if (id >= lo && id < hi) atomicMax(&word[place(id)], (uint32_t)(j + 1) << kBiasShift);
       }
       __syncthreads();                                            // entries first: the maximum must see no counts
     }
-    if (r.tokens) {
-      const int n = min(max(r.n_tokens ? r.n_tokens[row] : r.max_tokens, 0), r.max_tokens);
-      const int n0 = r.n_prompt ? r.n_prompt[row] : 0;
-      const int32_t* tokens = r.tokens + row * r.token_stride;
 #pragma unroll 4
-      for (int j = threadIdx.x; j < n; j += kLogitsThreads) {
-        const int id = tokens[j];
-        const unsigned int at = (unsigned int)(id - first);
-        if ((unsigned int)id < (unsigned int)p.vocab && at < (unsigned int)kSlice) {
-          atomicOr(&word[at], kSeen);
-          atomicOr(&touched[at >> 5], 1u << (at & 31));
-          if (j >= n0) atomicAdd(&word[at], 1u);
+    for (int j = threadIdx.x; j < n; j += kLogitsThreads) {
+      const int id = tokens[j];
+      if (id < lo || id >= hi) continue;
+      uint32_t* w = &word[place(id)];
+      if (j < n0) atomicOr(w, kSeen);                             // prompt tokens set `seen`, generated ones count
+      else atomicAdd(w, 1u);
+    }
+    __syncthreads();
+#pragma unroll 2
+    for (int i = threadIdx.x; i < p.slots; i += kLogitsThreads) {
+      const int id = key[i];
+      if (id < 0) continue;
+      const uint32_t w = word[i], c = w & kCountMask;
+      const int b = (int)((w & ~kSeen) >> kBiasShift);
+      float x = to_float(in[id]);
+      if ((w & kSeen) || c) x = x > 0.f ? x / rho : x * rho;
+      if (c) x -= phi * (float)c + pi;
+      if (b) x += r.bias_values[(int64_t)row * r.n_bias + b - 1];
+      x *= inv;
+      if (mask && !(mask[id >> 5] >> (id & 31) & 1)) x = -INFINITY;
+      word[i] = __float_as_uint(x);
+    }
+    __syncthreads();                                              // in may be out: all reads of the part's own logits are
+  }                                                               // done, or are the stream's, which writes what it read
+
+  // step 2
+  for (int t0 = begin + (int)threadIdx.x * kUnit; t0 < hi; t0 += kBatch * kGrain) {
+    Raw8<In> raw[kBatch];
+    uint32_t allowed[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int t = t0 + u * kGrain;
+      if (t >= lo && t + kUnit <= hi) load8(in + t, raw[u]);
+      allowed[u] = 0xFFu;
+      if (mask && t < hi) {
+        const int w0 = t >> 5;                                    // rounds down for negative t too
+        const uint32_t a = w0 >= 0 ? mask[w0] : 0, b = (t & 31) > 32 - kUnit && w0 + 1 < words ? mask[w0 + 1] : 0;
+        allowed[u] = __funnelshift_r(a, b, t & 31);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int t = t0 + u * kGrain;
+      const uint32_t free = allowed[u];
+      if (t >= lo && t + kUnit <= hi) {
+        float x[8];
+        floats8(raw[u], x);
+#pragma unroll
+        for (int k = 0; k < kUnit; ++k) x[k] *= inv;
+        if ((free & 0xFFu) != 0xFFu) {
+#pragma unroll
+          for (int k = 0; k < kUnit; ++k)
+            if (!(free >> k & 1)) x[k] = -INFINITY;
+        }
+        if (out_aligned) {
+          store8(out + t, x);
+        } else {
+#pragma unroll
+          for (int k = 0; k < kUnit; ++k) out[t + k] = from_float<Out>(x[k]);
+        }
+      } else if (t < hi) {                                        // the row begins or ends inside the unit
+        for (int k = max(0, lo - t); k < min(kUnit, hi - t); ++k) {
+          const float x = to_float(in[t + k]) * inv;
+          out[t + k] = from_float<Out>(free >> k & 1 ? x : -INFINITY);
         }
       }
     }
-    __syncthreads();
   }
-  // x / tau as a product with 1 / tau (one rounding more); a tau whose inverse is no number divides
-  const float inv = 1.f / tau;
-  const bool divide = !(fabsf(inv) < INFINITY);
-  auto rules = [&](float x, uint32_t w) {
-    if (w & kSeen) x = x > 0.f ? x / rho : x * rho;
-    const uint32_t c = w & kCountMask;
-    if (c) x -= phi * (float)c + pi;
-    const int b = (int)((w & ~kSeen) >> kBiasShift);
-    if (b) x += r.bias_values[(int64_t)row * r.n_bias + b - 1];
-    return x;
-  };
-#pragma unroll
-  for (int u = 0; u < kUnits; ++u) {
-    const int i = u * kLogitsThreads + (int)threadIdx.x, t = first + i * kUnit;
-    if (t >= p.vocab || t + kUnit <= 0) continue;
-    uint32_t hit = any ? touched[i >> 2] >> (i & 3) * 8 & 0xFFu : 0;
-    uint32_t allowed = 0xFFu;
-    if (mask) {
-      const int w0 = t >> 5;                                      // rounds down for negative t too
-      const uint32_t lo = w0 >= 0 ? mask[w0] : 0, hi = (t & 31) > 32 - kUnit && w0 + 1 < words ? mask[w0 + 1] : 0;
-      allowed = __funnelshift_r(lo, hi, t & 31) & 0xFFu;
-    }
-    if (t >= 0 && t + kUnit <= p.vocab) {
-      float x[8];
-      floats8(raw[u], x);
-      if (hit) {
-#pragma unroll
-        for (int k = 0; k < kUnit; ++k)
-          if (hit >> k & 1) x[k] = rules(x[k], word[i * kUnit + k]);
-      }
-#pragma unroll
-      for (int k = 0; k < kUnit; ++k) {
-        x[k] = divide ? x[k] / tau : x[k] * inv;
-        if (!(allowed >> k & 1)) x[k] = -INFINITY;
-      }
-      if (out_aligned) {
-        store8(out + t, x);
-      } else {
-#pragma unroll
-        for (int k = 0; k < kUnit; ++k) out[t + k] = from_float<Out>(x[k]);
-      }
-    } else {                                                      // the row begins or ends inside the unit
-      for (int k = max(0, -t); k < min(kUnit, p.vocab - t); ++k) {
-        float x = to_float(in[t + k]);
-        if (hit >> k & 1) x = rules(x, word[i * kUnit + k]);
-        x = divide ? x / tau : x * inv;
-        out[t + k] = from_float<Out>(allowed >> k & 1 ? x : -INFINITY);
-      }
-    }
-  }
+
+  // step 3
+  if (p.slots == 0) return;
+  __syncthreads();
+  for (int i = threadIdx.x; i < p.slots; i += kLogitsThreads)
+    if (const int id = key[i]; id >= 0) out[id] = from_float<Out>(__uint_as_float(word[i]));
 }
 
 template <typename In, typename Out>
 static int launch_logits(LogitsParams p, int n_rows, cudaStream_t st) {
-  // the last unit may begin up to seven tokens later than the row's length says (lead)
-  auto slices = [&](int units) {
-    const int64_t slice = (int64_t)kLogitsThreads * units * kUnit;
-    return ((int64_t)p.vocab + kUnit - 1 + slice - 1) / slice;
-  };
-  const int64_t wanted = 148 * 12;                                // CTAs that fill the GPU twice
-  const int units = n_rows * slices(4) >= wanted ? 4 : n_rows * slices(2) >= wanted ? 2 : 1;
-  const int64_t grid = n_rows * slices(units);
-  if (grid > 0x7FFFFFFFLL) return PG_EINVAL;
-  p.slices = (int)slices(units);
-  if (units == 4) logits_kernel<In, Out, 4><<<(unsigned)grid, kLogitsThreads, 0, st>>>(p);
-  else if (units == 2) logits_kernel<In, Out, 2><<<(unsigned)grid, kLogitsThreads, 0, st>>>(p);
-  else logits_kernel<In, Out, 1><<<(unsigned)grid, kLogitsThreads, 0, st>>>(p);
+  // rows that do not all start on 16 bytes may need a unit more (lead)
+  const bool aligned = (((uintptr_t)p.in | (uintptr_t)(p.in_stride * sizeof(In))) & 15) == 0;
+  const int64_t tokens = (int64_t)p.vocab + (aligned ? 0 : kUnit - 1);
+  const int64_t entries = (p.r.tokens ? p.r.max_tokens : 0) + (p.r.bias_ids ? p.r.n_bias : 0);
+  const int64_t hashed = entries ? entries + entries / 4 + 32 : 0;
+  // Parts for about eight CTAs per SM - four if the table leaves room for less - of whole grains; a part whose
+  // tokens would need more than 128 KB of table either way is shortened to 16384 tokens.
+  const int64_t ctas = 148 * (hashed * 8 > 48 * 1024 ? 4 : 8);
+  int64_t part = (tokens * n_rows + ctas - 1) / ctas;
+  part = std::max<int64_t>((part + kGrain - 1) / kGrain * kGrain, kGrain);
+  const int64_t whole = (tokens + kGrain - 1) / kGrain * kGrain;
+  part = std::min(part, whole);
+  if (std::min(hashed, part) > 16384) part = 16384;
+  const int64_t parts = (tokens + part - 1) / part;
+  if (n_rows * parts > 0x7FFFFFFFLL) return PG_EINVAL;
+  p.parts = (int)parts;
+  p.part = (int)part;
+  p.slots = (int)std::min(hashed, part);
+  p.direct = hashed >= part;
+  const size_t bytes = (size_t)p.slots * 8;
+  auto kernel = logits_kernel<In, Out>;
+  if (bytes > 48 * 1024) PG_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 16384 * 8));
+  kernel<<<(unsigned)(n_rows * parts), kLogitsThreads, bytes, st>>>(p);
   PG_LAUNCH_CHECK();
   return PG_OK;
 }
