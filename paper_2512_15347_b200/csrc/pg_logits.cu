@@ -6,6 +6,8 @@
 //      (a hash table, or one place per token where that is no larger); their results are computed there;
 //   2. the part streams through registers with the temperature and the mask alone;
 //   3. the table's results are written over the streamed ones.
+// All warps do the first step together (four or eight of sixteen, with the others streaming meanwhile, took 200 and
+// 156 us where all take 139: 1024 x 131072, bf16, 1024 tokens of history).
 // So the penalties cost what the few tokens cost that have one: testing every logit for a penalty on the way
 // (a word or a bit per token of the part) took twice the time of the stream in instructions and barriers.
 // Every part scans the row's whole history, so parts are as long as the number of rows allows.
@@ -103,7 +105,6 @@ logits_kernel(const __grid_constant__ LogitsParams p) {
   if (lo >= hi) return;
   const bool out_aligned = (((uintptr_t)(out - lead)) & 15) == 0;
   const uint32_t* mask = r.mask ? r.mask + row * r.mask_stride : nullptr;
-  const int words = (p.vocab + 31) >> 5;
   const float inv = r.temperature ? 1.f / r.temperature[row] : 1.f;
 
   // step 1
@@ -115,6 +116,13 @@ logits_kernel(const __grid_constant__ LogitsParams p) {
     const int n0 = r.n_prompt ? r.n_prompt[row] : 0;
     const float rho = r.repetition ? r.repetition[row] : 1.f, pi = r.presence ? r.presence[row] : 0.f;
     const float phi = r.frequency ? r.frequency[row] : 0.f;
+    constexpr int kAhead = 4;                                     // tokens of the history on their way meanwhile
+    int ahead[kAhead];
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+      const int j = e * kLogitsThreads + (int)threadIdx.x;
+      ahead[e] = tokens && j < r.max_tokens ? tokens[j] : -1;
+    }
     for (int i = threadIdx.x; i < p.slots; i += kLogitsThreads) {
       key[i] = -1;
       word[i] = 0;
@@ -140,73 +148,113 @@ logits_kernel(const __grid_constant__ LogitsParams p) {
       }
       __syncthreads();                                            // entries first: the maximum must see no counts
     }
-#pragma unroll 4
-    for (int j = threadIdx.x; j < n; j += kLogitsThreads) {
-      const int id = tokens[j];
-      if (id < lo || id >= hi) continue;
+    auto count = [&](int id, int j) {                             // prompt tokens set `seen`, generated ones count
+      if (id < lo || id >= hi) return;
       uint32_t* w = &word[place(id)];
-      if (j < n0) atomicOr(w, kSeen);                             // prompt tokens set `seen`, generated ones count
+      if (j < n0) atomicOr(w, kSeen);
       else atomicAdd(w, 1u);
+    };
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+      const int j = e * kLogitsThreads + (int)threadIdx.x;
+      if (j < n) count(ahead[e], j);
     }
+#pragma unroll 4
+    for (int j = kAhead * kLogitsThreads + (int)threadIdx.x; j < n; j += kLogitsThreads) count(tokens[j], j);
     __syncthreads();
-#pragma unroll 2
-    for (int i = threadIdx.x; i < p.slots; i += kLogitsThreads) {
-      const int id = key[i];
-      if (id < 0) continue;
-      const uint32_t w = word[i], c = w & kCountMask;
-      const int b = (int)((w & ~kSeen) >> kBiasShift);
-      float x = to_float(in[id]);
-      if ((w & kSeen) || c) x = x > 0.f ? x / rho : x * rho;
-      if (c) x -= phi * (float)c + pi;
-      if (b) x += r.bias_values[(int64_t)row * r.n_bias + b - 1];
-      x *= inv;
-      if (mask && !(mask[id >> 5] >> (id & 31) & 1)) x = -INFINITY;
-      word[i] = __float_as_uint(x);
+    // four entries at a time: what they need from global memory is asked for together
+    constexpr int kEntries = 4;
+    for (int i0 = threadIdx.x; i0 < p.slots; i0 += kLogitsThreads * kEntries) {
+      int id[kEntries];
+      uint32_t w[kEntries], bits[kEntries];
+      float x[kEntries], bias[kEntries];
+#pragma unroll
+      for (int e = 0; e < kEntries; ++e) {
+        const int i = i0 + e * kLogitsThreads;
+        id[e] = i < p.slots ? key[i] : -1;
+        w[e] = i < p.slots ? word[i] : 0;
+        const int b = (int)((w[e] & ~kSeen) >> kBiasShift);
+        x[e] = id[e] >= 0 ? to_float(in[id[e]]) : 0.f;
+        bits[e] = mask && id[e] >= 0 ? mask[id[e] >> 5] : 0xFFFFFFFFu;
+        bias[e] = b ? r.bias_values[(int64_t)row * r.n_bias + b - 1] : 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < kEntries; ++e) {
+        if (id[e] < 0) continue;
+        const uint32_t c = w[e] & kCountMask;
+        if ((w[e] & kSeen) || c) x[e] = x[e] > 0.f ? x[e] / rho : x[e] * rho;
+        if (c) x[e] -= phi * (float)c + pi;
+        if ((w[e] & ~kSeen) >> kBiasShift) x[e] += bias[e];
+        x[e] *= inv;
+        word[i0 + e * kLogitsThreads] = __float_as_uint(bits[e] >> (id[e] & 31) & 1 ? x[e] : -INFINITY);
+      }
     }
-    __syncthreads();                                              // in may be out: all reads of the part's own logits are
-  }                                                               // done, or are the stream's, which writes what it read
+    __syncthreads();                                                       // out = in: all that is read here has been read
+  }
 
   // step 2
-  for (int t0 = begin + (int)threadIdx.x * kUnit; t0 < hi; t0 += kBatch * kGrain) {
+  auto finish = [&](int t, float (&x)[8], uint32_t free) {
+#pragma unroll
+    for (int k = 0; k < kUnit; ++k) x[k] *= inv;
+    if ((free & 0xFFu) != 0xFFu) {
+#pragma unroll
+      for (int k = 0; k < kUnit; ++k)
+        if (!(free >> k & 1)) x[k] = -INFINITY;
+    }
+    if (out_aligned) {
+      store8(out + t, x);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kUnit; ++k) out[t + k] = from_float<Out>(x[k]);
+    }
+  };
+  const bool bytes = (begin & 7) == 0;                            // a unit's mask bits are one byte of the row of bits
+  auto one_unit = [&](int t) {                                    // whole, or cut by the row's ends
+    if (t >= lo && t + kUnit <= hi) {
+      Raw8<In> raw;
+      load8(in + t, raw);
+      float x[8];
+      floats8(raw, x);
+      finish(t, x, !mask ? 0xFFu : bytes ? ((const uint8_t*)mask)[t >> 3] : __funnelshift_r(mask[t >> 5], mask[(t + kUnit - 1) >> 5], t & 31));
+    } else {
+#pragma unroll 1
+      for (int k = max(0, lo - t); k < min(kUnit, hi - t); ++k) {
+        const float x = to_float(in[t + k]) * inv;
+        out[t + k] = from_float<Out>(!mask || (mask[(t + k) >> 5] >> ((t + k) & 31) & 1) ? x : -INFINITY);
+      }
+    }
+  };
+  // Blocks of kBatch units a lane, a warp each.
+  constexpr int kBlock = 32 * kUnit * kBatch;
+  const int lane = threadIdx.x & 31;
+  for (int first = begin + (int)(threadIdx.x >> 5) * kBlock; first < hi; first += kLogitsThreads / 32 * kBlock) {
+    const int t0 = first + lane * kUnit;
+    if (first < lo || first + kBlock > hi) {
+#pragma unroll 1
+      for (int u = 0; u < kBatch; ++u) one_unit(t0 + u * 32 * kUnit);
+      continue;
+    }
     Raw8<In> raw[kBatch];
     uint32_t allowed[kBatch];
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      const int t = t0 + u * kGrain;
-      if (t >= lo && t + kUnit <= hi) load8(in + t, raw[u]);
-      allowed[u] = 0xFFu;
-      if (mask && t < hi) {
-        const int w0 = t >> 5;                                    // rounds down for negative t too
-        const uint32_t a = w0 >= 0 ? mask[w0] : 0, b = (t & 31) > 32 - kUnit && w0 + 1 < words ? mask[w0 + 1] : 0;
-        allowed[u] = __funnelshift_r(a, b, t & 31);
-      }
+    for (int u = 0; u < kBatch; ++u) load8(in + t0 + u * 32 * kUnit, raw[u]);
+    if (!mask) {
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) allowed[u] = 0xFFu;
+    } else if (bytes) {
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) allowed[u] = ((const uint8_t*)mask)[(t0 >> 3) + u * 32];
+    } else {
+      // the bits may reach into the next word, which exists: all eight tokens do
+      const int w = t0 >> 5, w1 = (t0 + kUnit - 1) >> 5;
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) allowed[u] = __funnelshift_r(mask[w + u * kUnit], mask[w1 + u * kUnit], t0 & 31);
     }
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      const int t = t0 + u * kGrain;
-      const uint32_t free = allowed[u];
-      if (t >= lo && t + kUnit <= hi) {
-        float x[8];
-        floats8(raw[u], x);
-#pragma unroll
-        for (int k = 0; k < kUnit; ++k) x[k] *= inv;
-        if ((free & 0xFFu) != 0xFFu) {
-#pragma unroll
-          for (int k = 0; k < kUnit; ++k)
-            if (!(free >> k & 1)) x[k] = -INFINITY;
-        }
-        if (out_aligned) {
-          store8(out + t, x);
-        } else {
-#pragma unroll
-          for (int k = 0; k < kUnit; ++k) out[t + k] = from_float<Out>(x[k]);
-        }
-      } else if (t < hi) {                                        // the row begins or ends inside the unit
-        for (int k = max(0, lo - t); k < min(kUnit, hi - t); ++k) {
-          const float x = to_float(in[t + k]) * inv;
-          out[t + k] = from_float<Out>(free >> k & 1 ? x : -INFINITY);
-        }
-      }
+      float x[8];
+      floats8(raw[u], x);
+      finish(t0 + u * 32 * kUnit, x, allowed[u]);
     }
   }
 
@@ -224,9 +272,9 @@ static int launch_logits(LogitsParams p, int n_rows, cudaStream_t st) {
   const int64_t tokens = (int64_t)p.vocab + (aligned ? 0 : kUnit - 1);
   const int64_t entries = (p.r.tokens ? p.r.max_tokens : 0) + (p.r.bias_ids ? p.r.n_bias : 0);
   const int64_t hashed = entries ? entries + entries / 4 + 32 : 0;
-  // Parts for about eight CTAs per SM - four if the table leaves room for less - of whole grains; a part whose
+  // Parts for about twelve CTAs per SM - four rounds of three, two of two if the table is large - of whole grains; a part whose
   // tokens would need more than 128 KB of table either way is shortened to 16384 tokens.
-  const int64_t ctas = 148 * (hashed * 8 > 48 * 1024 ? 4 : 8);
+  const int64_t ctas = 148 * (hashed * 8 > 48 * 1024 ? 4 : 12);
   int64_t part = (tokens * n_rows + ctas - 1) / ctas;
   part = std::max<int64_t>((part + kGrain - 1) / kGrain * kGrain, kGrain);
   const int64_t whole = (tokens + kGrain - 1) / kGrain * kGrain;
