@@ -170,8 +170,15 @@ def _p(t) -> Optional[int]:
     return t.data_ptr()
 
 
+# The current stream's handle without building a Stream object (1.5 us a call), where torch offers it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
+        if _raw_stream is not None and _device is not None:
+            return _raw_stream(_device()) or None
         return torch.cuda.current_stream().cuda_stream or None
     if isinstance(stream, int):
         return stream or None
@@ -442,8 +449,10 @@ def _i32(t, what: str, n: Optional[int] = None) -> Optional[int]:
     """Address of a contiguous int32 tensor (of n elements)."""
     if t is None:
         return None
-    _want(t.dtype == torch.int32 and t.is_contiguous(), f"{what}: a contiguous int32 tensor")
-    _want(n is None or t.numel() == n, f"{what}: {n} elements")
+    if t.dtype is not torch.int32 or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous int32 tensor")
+    if n is not None and t.numel() != n:
+        raise ValueError(f"{what}: {n} elements")
     return t.data_ptr()
 
 
@@ -463,16 +472,18 @@ def make_kv(k, v, table, length) -> Kv:
            _i32(table, "table"), _i32(length, "length"), table.shape[0], table.shape[1])
     c._keepalive = (k, v, table, length)
     c._ref = ctypes.byref(c)
+    c._plain = (k.dtype, table.shape[0], heads, dim, n_pages, table.shape[1])   # plain values, cheaper to read than the fields
     return c
 
 
-def _rows_of(t, kv: Kv, heads: int, what: str, rows: int) -> int:
+def _rows_of(t, dtype, heads: int, dim: int, what: str, rows: int) -> int:
     """Row stride of [rows, heads, head dim] whose rows are contiguous inside."""
-    _want(t.shape == (rows, heads, kv.head_dim) and _DTYPES.get(t.dtype) == kv.dtype, f"{what}: [rows, heads, head dim] of the cache's type")
-    s = t.stride()
-    _want(s[2] == 1 and (s[1] == kv.head_dim or heads == 1) and (s[0] >= heads * kv.head_dim or rows <= 1),
-          f"{what}: contiguous inside a row, rows apart")
-    return s[0] if rows > 1 else 0
+    if t.dtype is not dtype or t.shape != (rows, heads, dim):
+        raise ValueError(f"{what}: [rows, heads, head dim] of the cache's type")
+    a, b, c = t.stride()
+    if c != 1 or (b != dim and heads != 1) or (a < heads * dim and rows > 1):
+        raise ValueError(f"{what}: contiguous inside a row, rows apart")
+    return a if rows > 1 else 0
 
 
 def kv_attend_workspace_bytes(kv: Kv, n_q_heads: int, group: int = 1) -> int:
@@ -484,38 +495,45 @@ def kv_attend(kv: Kv, layer: int, q, out, workspace, *, k_new=None, v_new=None, 
     """Attention of one new token per row over the cache (see pg_kv_attend).  q, out [rows, query heads,
     head dim]; with k_new / v_new the rows' last token is stored on the way; scale defaults to
     head_dim ** -0.5."""
-    rows, heads = kv.n_rows, q.shape[1]
-    q_stride, out_stride, new_stride = _rows_of(q, kv, heads, "q", rows), _rows_of(out, kv, heads, "out", rows), 0
+    dtype, rows, kv_heads, dim, _, _ = kv._plain
+    heads, k_at, v_at, new_stride = q.shape[1], None, None, 0
+    q_stride = _rows_of(q, dtype, heads, dim, "q", rows)
+    out_stride = _rows_of(out, dtype, heads, dim, "out", rows)
     if k_new is not None:
-        new_stride = _rows_of(k_new, kv, kv.n_kv_heads, "k_new", rows)
-        _want(v_new is not None and new_stride == _rows_of(v_new, kv, kv.n_kv_heads, "v_new", rows), "k_new and v_new alike")
+        new_stride = _rows_of(k_new, dtype, kv_heads, dim, "k_new", rows)
+        if v_new is None or new_stride != _rows_of(v_new, dtype, kv_heads, dim, "v_new", rows):
+            raise ValueError("k_new and v_new alike")
+        k_at, v_at = k_new.data_ptr(), v_new.data_ptr()
     if lse is not None:
-        _want(lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == rows * heads, "lse: [rows, query heads] fp32")
-    _check(lib().pg_kv_attend(kv._ref, layer, heads, q.data_ptr(), q_stride, None if k_new is None else k_new.data_ptr(),
-                              None if v_new is None else v_new.data_ptr(), new_stride,
-                              kv.head_dim ** -0.5 if scale is None else scale, group,
-                              _i32(shared, "shared", rows // max(group, 1)), out.data_ptr(), out_stride,
-                              None if lse is None else lse.data_ptr(), _p(workspace),
-                              workspace.numel() * workspace.element_size(), _i32(status, "status"), _stream(stream)),
-           "pg_kv_attend")
+        if lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.numel() != rows * heads:
+            raise ValueError("lse: [rows, query heads] fp32")
+        lse = lse.data_ptr()
+    _check(lib().pg_kv_attend(kv._ref, layer, heads, q.data_ptr(), q_stride, k_at, v_at, new_stride,
+                              dim ** -0.5 if scale is None else scale, group,
+                              None if shared is None else _i32(shared, "shared", rows // max(group, 1)), out.data_ptr(), out_stride,
+                              lse, _p(workspace), workspace.nbytes, None if status is None else _i32(status, "status"),
+                              _stream(stream)), "pg_kv_attend")
 
 
 def kv_extend(kv: Kv, n_new, len_out, refs, refs_out, status=None, stream=None) -> None:
     """Room for n_new more tokens (an int for all rows, or int32 [rows]): lengths, pages, counts."""
+    _, rows, _, _, pages, _ = kv._plain
     one = isinstance(n_new, int)
-    _check(lib().pg_kv_extend(kv._ref, None if one else _i32(n_new, "n_new", kv.n_rows), n_new if one else 0,
-                              _i32(len_out, "len_out", kv.n_rows), _i32(refs, "refs", kv.n_pages),
-                              _i32(refs_out, "refs_out", kv.n_pages), _i32(status, "status"), _stream(stream)), "pg_kv_extend")
+    _check(lib().pg_kv_extend(kv._ref, None if one else _i32(n_new, "n_new", rows), n_new if one else 0,
+                              _i32(len_out, "len_out", rows), _i32(refs, "refs", pages), _i32(refs_out, "refs_out", pages),
+                              _i32(status, "status"), _stream(stream)), "pg_kv_extend")
 
 
 def kv_append(kv: Kv, layer: int, k_new, v_new, start=None, status=None, stream=None) -> None:
     """Keys and values [tokens, kv heads, head dim] of the rows' last tokens into one layer's pages;
     start [rows + 1] int32 says whose they are (None: one token per row)."""
+    dtype, rows, kv_heads, dim, _, _ = kv._plain
     n = k_new.shape[0]
-    stride = _rows_of(k_new, kv, kv.n_kv_heads, "k_new", n)
-    _want(stride == _rows_of(v_new, kv, kv.n_kv_heads, "v_new", n), "k_new and v_new alike")
+    stride = _rows_of(k_new, dtype, kv_heads, dim, "k_new", n)
+    if stride != _rows_of(v_new, dtype, kv_heads, dim, "v_new", n):
+        raise ValueError("k_new and v_new alike")
     _check(lib().pg_kv_append(kv._ref, layer, n, k_new.data_ptr(), v_new.data_ptr(), stride,
-                              _i32(start, "start", kv.n_rows + 1), _i32(status, "status"), _stream(stream)), "pg_kv_append")
+                              _i32(start, "start", rows + 1), _i32(status, "status"), _stream(stream)), "pg_kv_append")
 
 
 def kv_fork_workspace_bytes(kv: Kv, n_out: int) -> int:
@@ -524,11 +542,11 @@ def kv_fork_workspace_bytes(kv: Kv, n_out: int) -> int:
 
 def kv_fork(kv: Kv, src_rows, table_out, len_out, refs, refs_out, workspace, status=None, stream=None) -> None:
     """New row i becomes a fork of old row src_rows[i]; rows without a fork give up their pages."""
+    pages, width = kv._plain[4:]
     n = 0 if src_rows is None else src_rows.numel()
-    _check(lib().pg_kv_fork(kv._ref, n, _i32(src_rows, "src_rows"), _i32(table_out, "table_out", n * kv.max_pages),
-                            _i32(len_out, "len_out", n), _i32(refs, "refs", kv.n_pages), _i32(refs_out, "refs_out", kv.n_pages),
-                            _p(workspace), workspace.numel() * workspace.element_size(), _i32(status, "status"),
-                            _stream(stream)), "pg_kv_fork")
+    _check(lib().pg_kv_fork(kv._ref, n, _i32(src_rows, "src_rows"), _i32(table_out, "table_out", n * width),
+                            _i32(len_out, "len_out", n), _i32(refs, "refs", pages), _i32(refs_out, "refs_out", pages),
+                            _p(workspace), workspace.nbytes, _i32(status, "status"), _stream(stream)), "pg_kv_fork")
 
 
 def kv_pack_workspace_bytes(kv: Kv) -> int:
@@ -537,10 +555,10 @@ def kv_pack_workspace_bytes(kv: Kv) -> int:
 
 def kv_pack(kv: Kv, refs, refs_out, table_out, workspace, page_map=None, status=None, stream=None) -> None:
     """Moves the pages in use to the front of the pool; the table and the counts follow."""
-    _check(lib().pg_kv_pack(kv._ref, _i32(refs, "refs", kv.n_pages), _i32(refs_out, "refs_out", kv.n_pages),
-                            _i32(table_out, "table_out", kv.n_rows * kv.max_pages), _i32(page_map, "page_map", kv.n_pages),
-                            _p(workspace), workspace.numel() * workspace.element_size(), _i32(status, "status"),
-                            _stream(stream)), "pg_kv_pack")
+    _, rows, _, _, pages, width = kv._plain
+    _check(lib().pg_kv_pack(kv._ref, _i32(refs, "refs", pages), _i32(refs_out, "refs_out", pages),
+                            _i32(table_out, "table_out", rows * width), _i32(page_map, "page_map", pages),
+                            _p(workspace), workspace.nbytes, _i32(status, "status"), _stream(stream)), "pg_kv_pack")
 
 
 def kv_status(status, stream=None) -> None:
@@ -594,13 +612,21 @@ def make_logits_rules(*, tokens=None, n_tokens=None, n_prompt=None, repetition=N
 def logits_process(logits, out, rules: LogitsRules, stream=None) -> None:
     """Applies the rules to logits [rows, vocab] (rows may be strided) into out (may be logits)."""
     rows, vocab = logits.shape
-    _want(logits.dtype in _DTYPES and out.dtype in _DTYPES and out.shape == logits.shape, "logits and out: [rows, vocab], fp32, bf16 or fp16")
-    _want((logits.stride(1) == 1 and out.stride(1) == 1) or vocab == 1, "logits and out: contiguous rows")
-    _want(rows <= 1 or (logits.stride(0) >= vocab and out.stride(0) >= vocab), "logits and out: rows apart")
-    _want(rules._rows in (None, rows), "the rules are for another number of rows")
-    _want(rules._mask_words is None or rules._mask_words * 32 >= vocab, "mask: too few words for the vocabulary")
-    _check(lib().pg_logits_process(rows, vocab, _DTYPES[logits.dtype], logits.data_ptr(), logits.stride(0) if rows > 1 else 0,
-                                   _DTYPES[out.dtype], out.data_ptr(), out.stride(0) if rows > 1 else 0, rules._ref,
+    from_type, to_type = _DTYPES.get(logits.dtype), _DTYPES.get(out.dtype)
+    if from_type is None or to_type is None or out.shape != logits.shape:
+        raise ValueError("logits and out: [rows, vocab], fp32, bf16 or fp16")
+    (a, one), (b, one_out) = logits.stride(), out.stride()
+    if (one != 1 or one_out != 1) and vocab > 1:
+        raise ValueError("logits and out: contiguous rows")
+    if rows <= 1:
+        a = b = 0
+    elif a < vocab or b < vocab:
+        raise ValueError("logits and out: rows apart")
+    if rules._rows is not None and rules._rows != rows:
+        raise ValueError("the rules are for another number of rows")
+    if rules._mask_words is not None and rules._mask_words * 32 < vocab:
+        raise ValueError("mask: too few words for the vocabulary")
+    _check(lib().pg_logits_process(rows, vocab, from_type, logits.data_ptr(), a, to_type, out.data_ptr(), b, rules._ref,
                                    _stream(stream)), "pg_logits_process")
 
 

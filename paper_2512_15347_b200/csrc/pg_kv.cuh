@@ -6,6 +6,8 @@
 
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 namespace pg {
 
 constexpr int kStatusTimeout = 2;   // status bit 1: a bounded wait ran out
@@ -61,9 +63,38 @@ inline KvView kv_view(const pg_kv* c, int32_t* status) {
   return v;
 }
 
+// Lets a kernel use `bytes` of dynamic shared memory; asked of the runtime once per kernel and device.
+template <typename Kernel>
+inline int allow_shared(Kernel* kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  PG_CUDA(cudaGetDevice(&dev));
+  if (dev < 64 && (done.load(std::memory_order_acquire) >> dev & 1)) return PG_OK;
+  PG_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  if (dev < 64) done.fetch_or(1ull << dev, std::memory_order_release);
+  return PG_OK;
+}
+
 inline size_t dtype_bytes(int dtype) { return dtype == PG_F32 ? 4 : 2; }
 
+// n / d for 0 <= n < 2^31 by a multiplication (d >= 1): m = ceil(2^(32+s) / d), s = ceil(log2 d) - 1.
+struct FastDiv {
+  uint32_t d, m, s;
+};
+inline FastDiv fast_div(uint32_t d) {
+  FastDiv f{d, 0, 0};
+  if (d > 1) {
+    uint32_t s = 0;
+    while ((1ull << (s + 1)) < d) ++s;
+    f.s = s;
+    f.m = (uint32_t)((((unsigned __int128)1 << (32 + s)) + d - 1) / d);
+  }
+  return f;
+}
+
 #ifdef __CUDACC__
+__device__ __forceinline__ uint32_t div_by(uint32_t n, const FastDiv& f) {
+  return f.d == 1 ? n : __umulhi(n, f.m) >> f.s;
+}
 __device__ __forceinline__ void flag(int32_t* status, int bit) {
   if (status) atomicOr(status, bit);
 }

@@ -1060,7 +1060,8 @@ static int launch_attend(const AttendParams& p, const PoolMaps& maps, cudaStream
   static_assert(S::kBytes <= 223 * 1024, "shared memory");
   static_assert(kWarps <= kMaxWarps, "workspace");
   auto kernel = attend_kernel<T, Body, kWarps, kStages, kBulk>;
-  PG_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes));
+  static std::atomic<uint64_t> done{0};
+  if (const int rc = allow_shared(kernel, (int)S::kBytes, done)) return rc;
   const long long most = (long long)p.kv.n_rows * p.kv.n_kv_heads * p.n_split *
                          (((long long)p.kv.max_pages * p.kv.page_size + Body::kChunk - 1) / Body::kChunk);
   kernel<<<(unsigned)(most < kSms ? most : kSms), kWarps * 32, S::kBytes, st>>>(p, maps);

@@ -10,21 +10,6 @@ constexpr int kMaxWarps = 8;
 constexpr int kMaxHeads = 16;                 // query heads of a (row, kv head) piece
 constexpr size_t kTicketBytes = 4096;         // >= 4 * kSms
 
-// n / d for 0 <= n < 2^31 by a multiplication (d >= 1): m = ceil(2^(32+s) / d), s = ceil(log2 d) - 1.
-struct FastDiv {
-  uint32_t d, m, s;
-};
-inline FastDiv fast_div(uint32_t d) {
-  FastDiv f{d, 0, 0};
-  if (d > 1) {
-    uint32_t s = 0;
-    while ((1ull << (s + 1)) < d) ++s;
-    f.s = s;
-    f.m = (uint32_t)((((unsigned __int128)1 << (32 + s)) + d - 1) / d);
-  }
-  return f;
-}
-
 struct AttendParams {
   KvView kv;
   const void* q;
@@ -48,9 +33,6 @@ struct AttendParams {
 };
 
 #ifdef __CUDACC__
-__device__ __forceinline__ uint32_t div_by(uint32_t n, const FastDiv& f) {
-  return f.d == 1 ? n : __umulhi(n, f.m) >> f.s;
-}
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -44,13 +44,20 @@ __device__ __forceinline__ int block_scan(int v, int* total) {
 // there were (at most wanted).  One CTA.
 template <typename Take>
 __device__ __forceinline__ int take_free(const int32_t* refs, int n_pages, int wanted, Take take) {
-  constexpr int kPer = 8;
+  // A warp looks at 1024 counts a round, 32 coalesced loads of 32; the ballot over load i is what lane i keeps.
+  const int lane = threadIdx.x & 31;
   int found = 0;
-  for (int base = 0; base < n_pages && found < wanted; base += blockDim.x * kPer) {
-    const int p = base + threadIdx.x * kPer;
+  for (int base = 0; base < n_pages && found < wanted; base += blockDim.x * 32) {
+    const int w0 = base + (threadIdx.x - lane) * 32, p = w0 + lane * 32;
     uint32_t free = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) free |= (uint32_t)(p + i < n_pages && __ldcg(&refs[p + i]) == 0) << i;
+    if (w0 < n_pages) {
+#pragma unroll 16
+      for (int i = 0; i < 32; ++i) {
+        const int at = w0 + i * 32 + lane;
+        const uint32_t b = __ballot_sync(0xFFFFFFFFu, at < n_pages && __ldcg(&refs[at]) == 0);
+        if (lane == i) free = b;
+      }
+    }
     int total;
     int k = found + block_scan(__popc(free), &total);
     for (; free; free &= free - 1, ++k)
@@ -59,6 +66,20 @@ __device__ __forceinline__ int take_free(const int32_t* refs, int n_pages, int w
   }
   __syncthreads();
   return min(found, wanted);
+}
+
+// Counts to their output, by one CTA (few pages: a launch less than a copy of its own).
+constexpr int kCopyCounts = 1 << 17;         // pages up to which the one-CTA kernels do it
+__device__ __forceinline__ void copy_counts(const int32_t* from, int32_t* to, int n) {
+  if ((((uintptr_t)from | (uintptr_t)to) & 15) == 0) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n / 4; i += blockDim.x) ((int4*)to)[i] = ((const int4*)from)[i];
+    for (int i = n / 4 * 4 + threadIdx.x; i < n; i += blockDim.x) to[i] = from[i];
+  } else {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += blockDim.x) to[i] = from[i];
+  }
+  __syncthreads();
 }
 
 // ---------------------------------------------------------------- copies of whole pages
@@ -149,7 +170,7 @@ static int launch_copy(const pg_kv* kv, const KvView& view, const int2* pairs, c
   const int64_t entries = table_out ? (int64_t)kv->n_rows * kv->max_pages : 0;
   p.table_ctas = (unsigned)std::min<int64_t>((entries + kCopyThreads * 4 - 1) / (kCopyThreads * 4), 148);
   const int64_t items = (most + run - 1) / run * pieces * kv->n_layers * 2;
-  copy_pages_kernel<<<p.table_ctas + (unsigned)std::min<int64_t>(std::max<int64_t>(items, 1), 148 * 8), kCopyThreads, 0, st>>>(p);
+  copy_pages_kernel<<<p.table_ctas + (unsigned)std::min<int64_t>(std::max<int64_t>(items, 1), 148 * 64), kCopyThreads, 0, st>>>(p);
   PG_LAUNCH_CHECK();
   return PG_OK;
 }
@@ -204,14 +225,30 @@ __device__ __forceinline__ void fork_assign(const ForkParams& p) {
     wanted += total;
   }
   __syncthreads();
-  const int found = take_free(p.refs, kv.n_pages, wanted, [&](int k, int page) {
-    const int i = p.w.pairs[k].x;
-    const int64_t last = (int64_t)i * kv.max_pages + __ldcg(&p.len_out[i]) / kv.page_size;
-    const int from = __ldcg(&p.table_out[last]);
-    p.table_out[last] = page;
-    p.refs[page] = 1;
-    p.w.pairs[k] = (unsigned int)from < (unsigned int)kv.n_pages ? make_int2(from, page) : make_int2(page, page);
-  });
+  const int found = take_free(p.refs, kv.n_pages, wanted, [&](int k, int page) { p.w.pairs[k].y = page; });
+  constexpr int kAhead = 4;                           // rows of a thread whose look-ups are under way together
+  for (int k0 = threadIdx.x; k0 < found; k0 += blockDim.x * kAhead) {
+    int2 x[kAhead];
+    int64_t last[kAhead];
+    int from[kAhead];
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+      const int k = k0 + e * blockDim.x;
+      x[e] = k < found ? p.w.pairs[k] : make_int2(-1, -1);
+    }
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e)
+      last[e] = x[e].x >= 0 ? (int64_t)x[e].x * kv.max_pages + __ldcg(&p.len_out[x[e].x]) / kv.page_size : 0;
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) from[e] = x[e].x >= 0 ? __ldcg(&p.table_out[last[e]]) : 0;
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+      if (x[e].x < 0) continue;
+      p.table_out[last[e]] = x[e].y;
+      p.refs[x[e].y] = 1;
+      p.w.pairs[k0 + e * blockDim.x].x = (unsigned int)from[e] < (unsigned int)kv.n_pages ? from[e] : x[e].y;
+    }
+  }
   for (int k = found + threadIdx.x; k < wanted; k += blockDim.x) {   // no page: the full pages remain
     const int i = p.w.pairs[k].x;
     const int full = __ldcg(&p.len_out[i]) / kv.page_size;
@@ -319,6 +356,7 @@ struct PackParams {
   const int32_t* refs;
   int32_t *refs_out, *table_out, *page_map;
   PackWork w;
+  int copy_refs;
 };
 
 // The k-th page in use at n_live or above moves into the k-th free page below n_live.  One CTA; a thread
@@ -327,6 +365,8 @@ __global__ void __launch_bounds__(kScanThreads) pack_plan_kernel(const __grid_co
   constexpr int kPer = 8;
   const int n = p.kv.n_pages;
   int mine = 0, n_live, moves = 0;
+  if (p.copy_refs) copy_counts(p.refs, p.refs_out, n);
+#pragma unroll 4
   for (int i = threadIdx.x; i < n; i += kScanThreads) mine += p.refs[i] > 0;
   block_scan(mine, &n_live);
   int holes = 0;
@@ -431,7 +471,8 @@ struct AppendParams {
   const int32_t* start;
   int64_t new_words;        // 16-byte words between tokens
   int n_tokens, row_words;  // words of a token and head
-  int elem_words;           // elements in a word
+  int elem_shift;           // log2 of the elements in a word
+  FastDiv per_token, per_head;
 };
 
 constexpr int kAppendTokens = 8;
@@ -467,15 +508,32 @@ __global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ App
     slot[threadIdx.x] = at;
   }
   __syncthreads();
-  const int per_token = kv.n_kv_heads * p.row_words;
-  for (int i = threadIdx.x; i < kAppendTokens * per_token; i += 256) {
-    const int tok = i / per_token, w = i - tok * per_token, h = w / p.row_words, c = w - h * p.row_words;
-    const int64_t at = slot[tok];
-    if (at < 0) continue;
-    const int64_t to = (at + (int64_t)h * kv.page_size * kv.head_dim) / p.elem_words + c;
-    const int64_t from = (t0 + tok) * p.new_words + w;
-    ((uint4*)kv.k)[to] = p.k_new[from];
-    ((uint4*)kv.v)[to] = p.v_new[from];
+  // four words of K and of V a thread under way at a time
+  constexpr int kAhead = 4;
+  const int total = kAppendTokens * (int)p.per_token.d;
+  for (int i0 = threadIdx.x; i0 < total; i0 += 256 * kAhead) {
+    uint4 k[kAhead], v[kAhead];
+    int64_t to[kAhead];
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+      const int i = i0 + e * 256;
+      to[e] = -1;
+      if (i >= total) continue;
+      const int tok = (int)div_by(i, p.per_token), w = i - tok * (int)p.per_token.d;
+      const int h = (int)div_by(w, p.per_head), c = w - h * p.row_words;
+      const int64_t at = slot[tok];
+      if (at < 0) continue;
+      to[e] = ((at + (int64_t)h * kv.page_size * kv.head_dim) >> p.elem_shift) + c;
+      const int64_t from = (t0 + tok) * p.new_words + w;
+      k[e] = __ldcs(p.k_new + from);
+      v[e] = __ldcs(p.v_new + from);
+    }
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e)
+      if (to[e] >= 0) {
+        ((uint4*)kv.k)[to[e]] = k[e];
+        ((uint4*)kv.v)[to[e]] = v[e];
+      }
   }
 }
 
@@ -536,8 +594,10 @@ int pg_kv_pack(const pg_kv* kv, const int32_t* refs, int32_t* refs_out, int32_t*
   const size_t t = (size_t)kv->n_rows * kv->max_pages * 4;
   if (kv->n_rows > 0 && table_out != kv->table && pg::overlap(table_out, t, kv->table, t)) return PG_EINVAL;
   cudaStream_t st = (cudaStream_t)stream;
-  if (refs != refs_out) PG_CUDA(cudaMemcpyAsync(refs_out, refs, (size_t)kv->n_pages * 4, cudaMemcpyDeviceToDevice, st));
   pg::PackParams p;
+  p.copy_refs = refs != refs_out && kv->n_pages <= pg::kCopyCounts;
+  if (refs != refs_out && !p.copy_refs)
+    PG_CUDA(cudaMemcpyAsync(refs_out, refs, (size_t)kv->n_pages * 4, cudaMemcpyDeviceToDevice, st));
   p.kv = pg::kv_view(kv, status);
   p.refs = refs; p.refs_out = refs_out; p.table_out = table_out; p.page_map = page_map;
   pg::pack_work((char*)workspace, kv->n_pages, &p.w);
@@ -583,8 +643,10 @@ int pg_kv_append(const pg_kv* kv, int32_t layer, int32_t n_tokens, const void* k
   p.new_words = new_stride * (int64_t)b / 16;
   p.n_tokens = n_tokens;
   p.row_words = (int)(kv->head_dim * b / 16);
-  p.elem_words = (int)(16 / b);
+  p.elem_shift = b == 4 ? 2 : 3;
   if ((int64_t)kv->n_kv_heads * p.row_words > (1 << 24)) return PG_EINVAL;
+  p.per_token = pg::fast_div((uint32_t)(kv->n_kv_heads * p.row_words));
+  p.per_head = pg::fast_div((uint32_t)p.row_words);
   pg::append_kernel<<<(unsigned)((n_tokens + (int64_t)pg::kAppendTokens - 1) / pg::kAppendTokens), 256, 0, (cudaStream_t)stream>>>(p);
   PG_LAUNCH_CHECK();
   return PG_OK;

@@ -502,7 +502,8 @@ static int launch_shared_as(const AttendParams& p, cudaStream_t st) {
   using L = SharedLayout<DP, kSlots>;
   static_assert(L::kBytes <= 224 * 1024, "shared memory");
   auto kernel = shared_kernel<T, DP, kSlots>;
-  PG_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
+  static std::atomic<uint64_t> done{0};
+  if (const int rc = allow_shared(kernel, L::kBytes, done)) return rc;
   kernel<<<kSms, L::kThreads, L::kBytes, st>>>(p);
   PG_LAUNCH_CHECK();
   return PG_OK;

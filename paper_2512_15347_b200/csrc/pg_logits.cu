@@ -288,7 +288,9 @@ static int launch_logits(LogitsParams p, int n_rows, cudaStream_t st) {
   p.direct = hashed >= part;
   const size_t bytes = (size_t)p.slots * 8;
   auto kernel = logits_kernel<In, Out>;
-  if (bytes > 48 * 1024) PG_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 16384 * 8));
+  static std::atomic<uint64_t> done{0};
+  if (bytes > 48 * 1024)
+    if (const int rc = allow_shared(kernel, 16384 * 8, done)) return rc;
   kernel<<<(unsigned)(n_rows * parts), kLogitsThreads, bytes, st>>>(p);
   PG_LAUNCH_CHECK();
   return PG_OK;
