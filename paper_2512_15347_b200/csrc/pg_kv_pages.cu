@@ -180,6 +180,7 @@ static int launch_copy(const pg_kv* kv, const KvView& view, const int2* pairs, c
 struct ForkWork {            // in the caller's workspace
   unsigned int* ticket;      // zero between calls
   int32_t* n_pairs;          // copies to make
+  int32_t* n_need;           // rows in need, zero between calls
   int32_t* need;             // [n_out] 1 where new row i needs a page for its partly filled last page
   int2* pairs;               // [n_out]
 };
@@ -189,6 +190,7 @@ static size_t fork_work(char* base, int64_t n_out, ForkWork* w) {
   if (w) {
     w->ticket = (unsigned int*)base;
     w->n_pairs = (int32_t*)(base + 4);
+    w->n_need = (int32_t*)(base + 8);
     w->need = (int32_t*)(base + 16);
     w->pairs = (int2*)(base + 16 + need);
   }
@@ -196,6 +198,7 @@ static size_t fork_work(char* base, int64_t n_out, ForkWork* w) {
 }
 
 constexpr int kForkThreads = 256, kForkRows = 32;   // most old rows of a CTA
+constexpr int kForkBatch = 12;                      // entries of src_rows a thread looks at a time
 
 struct ForkParams {
   KvView kv;
@@ -259,12 +262,12 @@ __device__ __forceinline__ void fork_assign(const ForkParams& p) {
   if (threadIdx.x == 0) *p.w.n_pairs = found;
 }
 
-// A CTA takes `rows` old rows: it goes through src_rows once, 1024 entries at a time, and writes the table rows
+// A CTA takes `rows` old rows: it goes through src_rows once, 3072 entries at a time, and writes the table rows
 // of their forks (CTA 0: also of entries that name no row); then the rows' pages change by (forks - 1), a
 // partly filled last page by (min(forks, 1) - 1).  The last CTA to finish hands out the pages.
 __global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constant__ ForkParams p) {
   __shared__ int forks[kForkRows], length[kForkRows], n_found, is_last;
-  __shared__ int2 found[kForkThreads * 4];            // (new row, old row within the CTA or -1)
+  __shared__ int2 found[kForkThreads * kForkBatch];   // (new row, old row within the CTA or -1)
   const KvView& kv = p.kv;
   const int s0 = blockIdx.x * p.rows, n_rows = max(0, min(p.rows, kv.n_rows - s0));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -272,15 +275,21 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constan
     forks[threadIdx.x] = 0;
     length[threadIdx.x] = row_len(kv, s0 + threadIdx.x);
   }
-  for (int base = 0; base < p.n_out; base += kForkThreads * 4) {
+  for (int base = 0; base < p.n_out; base += kForkThreads * kForkBatch) {
+    int src[kForkBatch];
+#pragma unroll
+    for (int e = 0; e < kForkBatch; ++e) {
+      const int i = base + e * kForkThreads + threadIdx.x;
+      src[e] = i < p.n_out ? p.src[i] : 0;
+    }
     __syncthreads();
     if (threadIdx.x == 0) n_found = 0;
     __syncthreads();
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < kForkBatch; ++e) {
       const int i = base + e * kForkThreads + threadIdx.x;
       if (i >= p.n_out) continue;
-      const int s = p.src[i];
+      const int s = src[e];
       const bool none = (unsigned int)s >= (unsigned int)kv.n_rows;
       if ((unsigned int)(s - s0) < (unsigned int)n_rows) found[atomicAdd(&n_found, 1)] = make_int2(i, s - s0);
       else if (none && blockIdx.x == 0) found[atomicAdd(&n_found, 1)] = make_int2(i, s == -1 ? -1 : -2);
@@ -303,6 +312,7 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constan
         if (x.y == -2) flag(kv.status, kStatusIndex);
         p.len_out[x.x] = n;
         p.w.need[x.x] = need;
+        if (need) atomicAdd(p.w.n_need, 1);
       }
     }
     __syncthreads();
@@ -330,7 +340,12 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constan
   __syncthreads();
   if (!is_last) return;
   __threadfence();
+  if (__ldcg(p.w.n_need) == 0) {
+    if (threadIdx.x == 0) *p.w.n_pairs = 0;
+    return;
+  }
   fork_assign(p);
+  if (threadIdx.x == 0) *p.w.n_need = 0;
 }
 
 // ---------------------------------------------------------------- pack

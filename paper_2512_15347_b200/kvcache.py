@@ -1,0 +1,121 @@
+"""Driver of token rollouts: owns the pool, the page tables and the workspaces of a paged key-value
+cache for groups of trajectories and issues the library calls in the order of a rollout (prompts in,
+expansion, decoding steps, prunes, release).  Allocation and streams are torch's; every number is
+computed by the library's kernels.
+"""
+from __future__ import annotations
+
+from typing import Optional
+
+import torch
+
+from . import binding as B
+
+
+class PagedCache:
+    """A paged cache of up to ``max_rows`` rows of up to ``max_tokens`` tokens on the current device.
+
+    Rows are group-major, as everywhere in the library; after ``fork`` with a fan-out the cache knows
+    how many tokens a group's rows have in common, and attention reads those once per group."""
+
+    def __init__(self, n_pages: int, page_size: int, n_layers: int, n_kv_heads: int, head_dim: int, max_rows: int,
+                 max_tokens: int, dtype: torch.dtype = torch.bfloat16):
+        if not torch.cuda.is_available():
+            raise RuntimeError("the rollout library needs a CUDA device; there is no CPU path")
+        dev = torch.device("cuda", torch.cuda.current_device())
+        self.dev, self.page_size, self.max_rows = dev, page_size, max_rows
+        self.k, self.v = (torch.zeros(n_layers, n_pages, n_kv_heads, page_size, head_dim, device=dev, dtype=dtype) for _ in range(2))
+        width = -(-max_tokens // page_size)
+        self._tables = [torch.full((max_rows, width), -1, device=dev, dtype=torch.int32) for _ in range(2)]
+        self._lens = [torch.zeros(max_rows, device=dev, dtype=torch.int32) for _ in range(2)]
+        self._cur = 0
+        self.refs = torch.zeros(n_pages, device=dev, dtype=torch.int32)
+        self.status = torch.zeros(1, device=dev, dtype=torch.int32)
+        self.group, self.shared = 1, None
+        self._spaces = {}
+        self.n_rows = 0
+
+    def _describe(self):
+        self.kv = B.make_kv(self.k, self.v, self.table, self.len)
+
+    @property
+    def n_rows(self) -> int:
+        return self._n_rows
+
+    @n_rows.setter
+    def n_rows(self, n: int):
+        if not 0 <= n <= self.max_rows:
+            raise ValueError(f"{n} rows in a cache of {self.max_rows}")
+        self._n_rows = n
+        self._describe()
+
+    @property
+    def table(self) -> torch.Tensor:
+        return self._tables[self._cur][: self._n_rows]
+
+    @property
+    def len(self) -> torch.Tensor:
+        return self._lens[self._cur][: self._n_rows]
+
+    def _space(self, name: str, nbytes: int) -> torch.Tensor:
+        """A zeroed workspace of its own for every call, grown when a call asks for more."""
+        if name not in self._spaces or self._spaces[name].nbytes < nbytes:
+            self._spaces[name] = torch.zeros(nbytes, device=self.dev, dtype=torch.uint8)
+        return self._spaces[name]
+
+    def admit(self, n_rows: int) -> None:
+        """Starts over with n_rows empty rows; whatever the cache held is released."""
+        B.kv_fork(self.kv, None, None, None, self.refs, self.refs, self._space("fork", B.kv_fork_workspace_bytes(self.kv, 0)),
+                  status=self.status)
+        self._lens[self._cur].zero_()
+        self.group, self.shared = 1, None
+        self.n_rows = n_rows
+
+    def extend(self, n_new) -> None:
+        """Room for n_new more tokens in every row (an int, or int32 [rows])."""
+        B.kv_extend(self.kv, n_new, self.len, self.refs, self.refs, status=self.status)
+
+    def append(self, layer: int, k_new, v_new, start=None) -> None:
+        """Keys and values of the rows' last tokens (after ``extend``)."""
+        B.kv_append(self.kv, layer, k_new, v_new, start, status=self.status)
+
+    def attend(self, layer: int, q, k_new=None, v_new=None, out=None, lse=None, scale: Optional[float] = None):
+        """Attention of the rows' newest token over the cache; with k_new / v_new that token is stored on
+        the way (after ``extend(1)``)."""
+        out = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
+        ws = self._space("attend", B.kv_attend_workspace_bytes(self.kv, q.shape[1], self.group))
+        B.kv_attend(self.kv, layer, q, out, ws, k_new=k_new, v_new=v_new, lse=lse, scale=scale, group=self.group, shared=self.shared,
+                    status=self.status)
+        return out
+
+    def _fork(self, src_rows) -> None:
+        n = src_rows.numel()
+        if n > self.max_rows:
+            raise ValueError(f"{n} rows in a cache of {self.max_rows}")
+        other = self._cur ^ 1
+        B.kv_fork(self.kv, src_rows, self._tables[other][:n], self._lens[other][:n], self.refs, self.refs,
+                  self._space("fork", B.kv_fork_workspace_bytes(self.kv, n)), status=self.status)
+        self._cur = other
+        self.n_rows = n
+
+    def expand(self, fan: int) -> None:
+        """Every row becomes a group of ``fan`` rows that share its full pages."""
+        shared = torch.div(self.len, self.page_size, rounding_mode="floor") * self.page_size
+        self._fork(torch.arange(self.n_rows, device=self.dev, dtype=torch.int32).repeat_interleave(fan))
+        self.group, self.shared = fan, shared.to(torch.int32)
+
+    def prune(self, src_rows, keep: int) -> None:
+        """Keeps the rows that a prune has kept (pg_prune_ovf's src_rows: ``keep`` per group, group-major)
+        and frees the pages of the others."""
+        if src_rows.numel() * self.group != self.n_rows * keep:
+            raise ValueError("src_rows: `keep` rows of every group")
+        self._fork(src_rows)
+        self.group = keep
+
+    def pack(self) -> None:
+        """Moves the pages in use to the front of the pool."""
+        B.kv_pack(self.kv, self.refs, self.refs, self.table, self._space("pack", B.kv_pack_workspace_bytes(self.kv)), status=self.status)
+
+    def check(self) -> None:
+        """Raises PgError if a call has flagged a bad index, a full table or an exhausted pool; synchronises."""
+        B.kv_status(self.status)
