@@ -464,7 +464,8 @@ int pg_gather_rows(pg_rollout *h, const int32_t *rows, int32_t n_out, int32_t n_
  * and the workspace, and passes them by a descriptor (HOST memory, read during the call only).
  * Indices that come from device memory (page numbers, row numbers, lengths, token ids) are checked
  * in the kernels: a bad one is never dereferenced, bit 2 of *status is set and pg_kv_status returns
- * PG_EINDEX.  Running out of pages or of table entries sets bit 3 (PG_ENOPAGES).  `status` (nullable)
+ * PG_EINDEX.  Running out of pages or of table entries sets bit 3 (PG_ENOPAGES); a bounded device-side
+ * wait that expires sets bit 1 (PG_ETIMEOUT, the call's results are then not valid).  `status` (nullable)
  * is a device int32 that the caller zeroes once and that calls only OR into.  Results do not depend on
  * the order in which the GPU runs its blocks.
  * ------------------------------------------------------------------------------------------ */
@@ -504,7 +505,8 @@ typedef struct {
  *   group, shared: rows come in groups of `group` (group-major, as everywhere in this library), and the
  *     first shared[g] tokens (device int32 [n_rows / group]; NULL: none) of all rows of group g lie in
  *     the same pages - the state after an expansion.  Those pages are read through the table row of
- *     the group's first row, once for the whole group.
+ *     the group's first row, once for the whole group (16-bit caches, from 64 tokens on, whole 64s of
+ *     them; the rest, and rows that end inside the shared tokens, are read row by row).
  *   workspace: at least pg_kv_attend_workspace_bytes(kv, n_q_heads, group) bytes of device memory,
  *     16-byte aligned, zeroed once before its first use; every call leaves its counters zero again.
  *     Two calls that can overlap on the GPU need a workspace each.
@@ -567,8 +569,8 @@ size_t pg_kv_pack_workspace_bytes(const pg_kv *kv);
 int pg_kv_pack(const pg_kv *kv, const int32_t *refs, int32_t *refs_out, int32_t *table_out,
                int32_t *page_map, void *workspace, size_t workspace_bytes, int32_t *status, void *stream);
 
-/* Synchronises `stream` and reports a status word of the calls above: PG_EINDEX (bit 2) or PG_ENOPAGES
- * (bit 3), in that order of precedence, else PG_OK. */
+/* Synchronises `stream` and reports a status word of the calls above: PG_EINDEX (bit 2), PG_ETIMEOUT (bit 1)
+ * or PG_ENOPAGES (bit 3), in that order of precedence, else PG_OK. */
 int pg_kv_status(const int32_t *status, void *stream);
 
 /*
