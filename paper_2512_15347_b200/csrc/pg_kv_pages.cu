@@ -462,14 +462,15 @@ __global__ void __launch_bounds__(kScanThreads) extend_kernel(const __grid_const
           if (first[mid] <= k) lo = mid; else hi = mid - 1;
         }
         kv.table[(int64_t)(base + lo) * kv.max_pages + have[lo] + k - first[lo]] = page;
+        p.refs[page] = 1;
       });
     __syncthreads();
     const bool fits = before + want <= found || want == 0;
     const bool late = dry || (found < total && before + want > found);
     if (r < kv.n_rows) {
       const bool grown = fits && !late;
-      if (grown)
-        for (int j = 0; j < want; ++j) p.refs[kv.table[(int64_t)r * kv.max_pages + old_pages + j]] = 1;
+      if (!grown)                                      // the one row that got some of its pages gives them back
+        for (int j = 0; j < min(want, found - before); ++j) p.refs[kv.table[(int64_t)r * kv.max_pages + old_pages + j]] = 0;
       if (!grown && add) flag(kv.status, kStatusPages);
       p.len_out[r] = grown ? n + add : n;
     }
