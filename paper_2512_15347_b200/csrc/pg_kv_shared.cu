@@ -16,7 +16,7 @@
 // stay exact, and O is rescaled a few times per unit instead of every tile.
 // The tiles of all units form one line cut into equal parts over the CTAs; every (CTA, unit) leaves its
 // queries' (m, l, O), and the rows' own pieces start from them.
-// Measured: 768 rows in groups of 48 (192 queries a kv head) over 2048 shared tokens, bf16, 8 kv heads x 128: about 60 us
+// Measured: 768 rows in groups of 48 (192 queries a kv head) over 2048 shared tokens, bf16, 8 kv heads x 128: about 65 us
 // for 25.8 GFLOP and 134 MB; the legacy mma path took 140 us.  Bound now: the softmax warps (about 1800 cycles a
 // 64-token tile) and the restart of the pipeline at every unit, not the tensor pipe.
 // Every wait is bounded: when one runs out, status bit 1 is set and the CTA leaves (its results are then
