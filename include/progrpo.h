@@ -616,6 +616,15 @@ int pg_logits_process(int32_t n_rows, int32_t vocab, int32_t dtype, const void *
  */
 int pg_selftest_bounded_wait(pg_rollout *h, void *stream);
 
+/*
+ * Diagnostic: makes waits of pg_kv_attend run out.  Its kernels wait for tiles of keys and values (bit 0), for free
+ * stages to load them into (bit 1), for queries (bit 2), scores (bit 3), weights (bit 4) and products (bit 5) of the shared
+ * part; each wait is bounded.  Calls of the process that follow give up those whose bit is set at once, as if they had run
+ * out, until the word is set to 0 again: the call ends, its results are not valid, pg_kv_status returns PG_ETIMEOUT, and
+ * the workspace serves the next call.  PG_EINVAL for any other bit.
+ */
+int pg_selftest_token_waits(uint32_t kinds);
+
 /* Raw Philox4x32-10 blocks for n (counter, key) pairs: ctr [n,4], key [n,2],
  * out [n,4] uint32 device arrays.  Exposes the library's generator so that it
  * can be compared bit for bit with another implementation. */

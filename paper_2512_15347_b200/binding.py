@@ -142,8 +142,9 @@ def lib() -> ctypes.CDLL:
     L.pg_kv_pack.argtypes = [pkv, vp, vp, vp, vp, vp, sz, vp, vp]
     L.pg_kv_status.argtypes = [vp, vp]
     L.pg_logits_process.argtypes = [i32, i32, i32, vp, i64, i32, vp, i64, ctypes.POINTER(LogitsRules), vp]
+    L.pg_selftest_token_waits.argtypes = [ctypes.c_uint32]
     for name in ("pg_kv_attend", "pg_kv_extend", "pg_kv_append", "pg_kv_fork", "pg_kv_pack", "pg_kv_status",
-                 "pg_logits_process"):
+                 "pg_logits_process", "pg_selftest_token_waits"):
         getattr(L, name).restype = ctypes.c_int
     L.pg_strerror.argtypes = [ctypes.c_int]
     L.pg_strerror.restype = ctypes.c_char_p
@@ -564,6 +565,14 @@ def kv_pack(kv: Kv, refs, refs_out, table_out, workspace, page_map=None, status=
 def kv_status(status, stream=None) -> None:
     """Raises PgError (EINDEX, ENOPAGES) if a call has flagged the status word; synchronises the stream."""
     _check(lib().pg_kv_status(_i32(status, "status"), _stream(stream)), "pg_kv_status")
+
+
+TOKEN_WAITS = ("tiles", "stages", "queries", "scores", "weights", "products")
+
+
+def selftest_token_waits(*kinds: str) -> None:
+    """Makes the named waits of the attention (``TOKEN_WAITS``) run out at once in the calls that follow; none: all wait again."""
+    _check(lib().pg_selftest_token_waits(sum(1 << TOKEN_WAITS.index(k) for k in set(kinds))), "pg_selftest_token_waits")
 
 
 def make_logits_rules(*, tokens=None, n_tokens=None, n_prompt=None, repetition=None, presence=None, frequency=None,

@@ -1024,6 +1024,8 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
 
 // ---------------------------------------------------------------- launch
 
+static std::atomic<uint32_t> lost_waits{0};          // pg_selftest_token_waits
+
 static int attend_check(const pg_kv* kv, int n_q_heads, int group) {
   const int rc = kv_check(kv);
   if (rc != PG_OK) return rc;
@@ -1169,6 +1171,7 @@ int pg_kv_attend(const pg_kv* kv, int32_t layer, int32_t n_q_heads, const void* 
   p.q_words = ((((uintptr_t)q) | (uintptr_t)(q_stride * b)) & 3) == 0;
   p.out_words = ((((uintptr_t)out) | (uintptr_t)(out_stride * b)) & 3) == 0;
   p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+  p.lost_waits = pg::lost_waits.load(std::memory_order_relaxed);
   p.page = pg::fast_div((uint32_t)kv->page_size);
   p.group_div = pg::fast_div((uint32_t)group);
   p.tickets = (unsigned int*)workspace;
@@ -1187,6 +1190,12 @@ int pg_kv_attend(const pg_kv* kv, int32_t layer, int32_t n_q_heads, const void* 
   if (kv->dtype == PG_F32) return pg::launch_type<float, pg::F32Body>(p, st);
   if (kv->dtype == PG_BF16) return pg::launch_type<__nv_bfloat16, pg::Bf16Body>(p, st);
   return pg::launch_type<__half, pg::F16Body>(p, st);
+}
+
+int pg_selftest_token_waits(uint32_t kinds) {
+  if (kinds >> (int)pg::TokenWait::kKinds) return PG_EINVAL;
+  pg::lost_waits.store(kinds, std::memory_order_relaxed);
+  return PG_OK;
 }
 
 }  // extern "C"

@@ -10,6 +10,9 @@ constexpr int kMaxWarps = 8;
 constexpr int kMaxHeads = 16;                 // query heads of a (row, kv head) piece
 constexpr size_t kTicketBytes = 4096;         // >= 4 * kSms
 
+// The bounded waits of the attention; bit k of AttendParams::lost_waits makes those of kind k run out at once.
+enum class TokenWait : int { kTiles, kStages, kQueries, kScores, kWeights, kProducts, kKinds };
+
 struct AttendParams {
   KvView kv;
   const void* q;
@@ -22,6 +25,7 @@ struct AttendParams {
   int n_split, piece_heads;                   // pieces per kv head, query heads of a piece
   int q_words, out_words;                     // rows of q / out on 4-byte boundaries
   float scale_log2;                           // scale * log2(e)
+  uint32_t lost_waits;                        // pg_selftest_token_waits
   FastDiv page, group_div;
   // shared pages of groups (shared != null), pg_kv_shared.cu
   int q_blocks, block_rows, block_queries;    // query blocks of a (group, kv head); rows and places of queries of a block
@@ -33,6 +37,9 @@ struct AttendParams {
 };
 
 #ifdef __CUDACC__
+__device__ __forceinline__ int wait_limit(const AttendParams& p, TokenWait kind, int limit) {
+  return p.lost_waits >> (int)kind & 1u ? 0 : limit;
+}
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

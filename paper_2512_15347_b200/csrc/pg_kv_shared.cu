@@ -243,14 +243,21 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
   __syncthreads();
   tmem_after();
   const uint32_t tmem = tmem_base;
-  // a bounded wait; after one has run out nobody waits any more
-  auto wait = [&](uint32_t bar, int parity) -> bool {
-    if (mbarrier_wait_bounded(bar, (unsigned)parity & 1u, kWaitLimit)) return true;
-    *(volatile int*)&gave_up = 1;
-    flag(kv.status, kStatusTimeout);
-    return false;
-  };
+  // A bounded wait of a whole warp; after one has run out nobody waits any more.  The warp votes, so that it goes on
+  // or leaves as one: what follows the waits (tensor memory, votes, shuffles) needs all its lanes, and `gave_up` may be
+  // set by another warp between two lanes' looks at it.
   auto lost = [&]() { return *(volatile int*)&gave_up != 0; };
+  auto wait = [&](uint32_t bar, int parity, TokenWait kind) -> bool {
+    bool there = false;
+    if (!lost()) {
+      there = mbarrier_wait_bounded(bar, (unsigned)parity & 1u, wait_limit(p, kind, kWaitLimit));
+      if (!there) {
+        *(volatile int*)&gave_up = 1;
+        flag(kv.status, kStatusTimeout);
+      }
+    }
+    return __all_sync(0xFFFFFFFFu, there) != 0;
+  };
 
   TilePlace here;
   here.group = first_group;
@@ -306,8 +313,7 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
         arrive(q_full(t));
         float m = -INFINITY, l = 0.f;
         for (int k = 0; k < n; ++k) {
-          if (lost() || !wait(s_full(t, tiles_done), tiles_done >> 1)) { ok = false; break; }
-          __syncwarp();
+          if (!wait(s_full(t, tiles_done), tiles_done >> 1, TokenWait::kScores)) { ok = false; break; }
           tmem_after();
           float s[kTile];
           const uint32_t s_here = s_addr + (tiles_done & 1) * kTile;
@@ -318,7 +324,7 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
           for (int j = 0; j < kTile; j += 2) tops[(j >> 1) & 3] = fmaxf(fmaxf(tops[(j >> 1) & 3], s[j]), s[j + 1]);
           const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * scale;
           // the previous product has read P and updated O
-          if (k > 0 && !wait(o_done(t), tiles_done - 1)) { ok = false; break; }
+          if (k > 0 && !wait(o_done(t), tiles_done - 1, TokenWait::kProducts)) { ok = false; break; }
           const bool raise = top > m + kSlack || m == -INFINITY;
           float f = 1.f;
           if (raise && top > m) {
@@ -364,8 +370,7 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
           arrive(p_full(t));
           ++tiles_done;
         }
-        if (!ok || !wait(o_done(t), tiles_done - 1)) { ok = false; break; }
-        __syncwarp();
+        if (!ok || !wait(o_done(t), tiles_done - 1, TokenWait::kProducts)) { ok = false; break; }
         tmem_after();
         float* out = shared_block(p, blockIdx.x, here.group * units + here.local);
         if (mine) __stcg((float2*)out + c, make_float2(m, l));
@@ -405,8 +410,7 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
         if (!good) flag(kv.status, kStatusIndex);
         from[i] = good ? entry * kv.page_stride + ((int64_t)(here.local / p.q_blocks) * kv.page_size + tok - page * kv.page_size) * kv.head_dim : -1;
       }
-      if (lost() || (k >= kStages && !wait(empty(stage), k / kStages - 1))) break;
-      __syncwarp();
+      if (k >= kStages && !wait(empty(stage), k / kStages - 1, TokenWait::kStages)) break;
 #pragma unroll
       for (int i = 0; i < kTile; i += kToks) {
         const int tok = i + lane / kPieces;
@@ -429,7 +433,6 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
     int tiles_done[kSlots] = {}, units_done[kSlots] = {};
     bool ok = true;
     const bool issuer = elected();
-    auto wait_all = [&](uint32_t bar, int parity) { return __all_sync(0xFFFFFFFFu, !lost() && wait(bar, parity)) != 0; };
     auto scores = [&](int t, int stage, int tile) {                  // tile: counted over the slot, picks the S buffer
       const uint32_t a = q_at + t * L::kQBytes, b = ring + stage * L::kStageBytes, d = tmem_u + (2 * t + (tile & 1)) * kTile;
       if (issuer) {
@@ -449,11 +452,11 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
       if (issuer && (here.tile == 0 || done == 0))                   // CTAs that share a unit write the same
         p.spans[here.group * units + here.local] = make_int2((int)(unit_line / quota), (int)((unit_line + here.tiles - 1) / quota));
       unit_line += here.tiles;
-      ok = wait_all(full(k % kStages), k / kStages);
+      ok = wait(full(k % kStages), k / kStages, TokenWait::kTiles);
 #pragma unroll
       for (int t = 0; t < kSlots; ++t)
         if (ok && t < slots) {
-          ok = wait_all(q_full(t), units_done[t]++);
+          ok = wait(q_full(t), units_done[t]++, TokenWait::kQueries);
           tmem_after();
           if (ok) scores(t, k % kStages, tiles_done[t]);
         }
@@ -461,7 +464,7 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
         const int stage = k % kStages, next = (k + 1) % kStages;
         const uint32_t v = ring + stage * L::kStageBytes + L::kKBytes;
         if (i + 1 < n) {                                             // the next scores run under this tile's softmax
-          ok = wait_all(full(next), (k + 1) / kStages);
+          ok = wait(full(next), (k + 1) / kStages, TokenWait::kTiles);
           tmem_after();
 #pragma unroll
           for (int t = 0; t < kSlots; ++t)
@@ -470,7 +473,7 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
 #pragma unroll
         for (int t = 0; t < kSlots; ++t) {
           if (!ok || t >= slots) continue;
-          ok = wait_all(p_full(t), tiles_done[t]++);
+          ok = wait(p_full(t), tiles_done[t]++, TokenWait::kWeights);
           if (!ok) continue;
           tmem_after();
           const uint32_t a = p_at + t * L::kPBytes, d = tmem_u + kSlots * 2 * kTile + t * DP;
@@ -487,9 +490,9 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
       done += n;
       if (done < count) here.next_unit(p, units);
     }
-    if (issuer) commit_to(drained);                                  // no product is in flight when the CTA leaves
+    if (issuer) commit_to(drained);                                  // no product is in flight when the CTA leaves, whoever gave up
     __syncwarp();
-    wait(drained, 0);
+    if (!mbarrier_wait_bounded(drained, 0, kWaitLimit)) flag(kv.status, kStatusTimeout);
   }
   __syncwarp();
   tmem_before();
