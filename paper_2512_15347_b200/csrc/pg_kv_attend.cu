@@ -150,6 +150,10 @@ struct MmaBody {
   // eight lanes of a head starts with the whole l).
   __device__ __forceinline__ void join_shared(const AttendParams& p, int unit, int column, int heads, int lane) {
     const int2 span = __ldcg(&p.spans[unit]);
+    if ((unsigned int)span.x >= (unsigned int)kSms || (unsigned int)span.y >= (unsigned int)kSms) {   // of no CTA: nothing to join
+      flag(p.kv.status, kStatusTimeout);
+      return;
+    }
 #pragma unroll 1
     for (int c = span.x; c <= span.y; ++c) {
       const float* part = shared_block(p, c, unit);

@@ -444,14 +444,22 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
       }
       __syncwarp();
     };
+    // The spans of the part's units, before any wait: the rows' own kernel follows them whatever happens here.
+    if (issuer) {
+      TilePlace unit = here;
+      long long line = begin - here.tile;                            // the unit's first tile on the line
+      for (int done = 0; done < count;) {                            // CTAs that share a unit write the same
+        p.spans[unit.group * units + unit.local] = make_int2((int)(line / quota), (int)((line + unit.tiles - 1) / quota));
+        line += unit.tiles;
+        done += min(unit.tiles - unit.tile, count - done);
+        if (done < count) unit.next_unit(p, units);
+      }
+    }
+    __syncwarp();
     int k = 0;                                                       // tile of the part
-    long long unit_line = begin - here.tile;                         // the unit's first tile on the line
     for (int done = 0; ok && done < count;) {
       const int n = __shfl_sync(0xFFFFFFFFu, min(here.tiles - here.tile, count - done), 0);
       const int slots = __shfl_sync(0xFFFFFFFFu, (block_queries(here.local) + kRows - 1) / kRows, 0);
-      if (issuer && (here.tile == 0 || done == 0))                   // CTAs that share a unit write the same
-        p.spans[here.group * units + here.local] = make_int2((int)(unit_line / quota), (int)((unit_line + here.tiles - 1) / quota));
-      unit_line += here.tiles;
       ok = wait(full(k % kStages), k / kStages, TokenWait::kTiles);
 #pragma unroll
       for (int t = 0; t < kSlots; ++t)

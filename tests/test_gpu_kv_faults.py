@@ -56,6 +56,37 @@ def test_a_wait_of_the_shared_part_that_runs_out_is_reported(kind, dim, dtype):
     T.check_attention(c, q, out, lse, dim ** -0.5, dtype)
 
 
+@pytest.mark.parametrize("dim,dtype", [(64, "f16"), (128, "bf16"), (256, "bf16")])
+@pytest.mark.parametrize("fill", [0x7F, 0x3F, 0xBF, 0xFF])
+def test_shared_part_that_gave_up_over_a_used_workspace(dim, dtype, fill):
+    """Behind its counters a workspace holds anything (another shape's partial results): the units that the shared part has
+    not come to are followed through none of it.  Many units a CTA, so that most are not come to."""
+    c = T.shared_cache(40, 3, 64, [1 + i % 20 for i in range(120)], 8, dim, 16, dtype)
+    q = T.queries(120, 8, dim, dtype)
+    kw = dict(group=3, shared=torch.full((40,), 64, device="cuda", dtype=torch.int32))
+    ws = torch.zeros(B.kv_attend_workspace_bytes(c.kv, 8, 3), device="cuda", dtype=torch.uint8)
+    for kind in ("tiles", "weights"):
+        ws[4096:] = fill
+        with lost(kind):
+            assert attend_status(c, q, ws, **kw) == B.ETIMEOUT
+    out, lse = T.run_attention(c, q, dtype, ws=ws, **kw)
+    T.check_attention(c, q, out, lse, dim ** -0.5, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_one_attention_workspace_over_group_sizes(dtype):
+    """The counters' place depends on nothing; what lies behind them moves with the group size and is written before it is read."""
+    cases = [(2, 48, 1024), (12, 2, 64), (1, 200, 128), (2, 16, 320)]
+    made = []
+    for groups, n, shared in cases:
+        c = T.shared_cache(groups, n, shared, [1 + 5 * i % 61 for i in range(groups * n)], 2, 64, 16, dtype, seed=n)
+        made.append((c, T.queries(groups * n, 8, 64, dtype), n, torch.full((groups,), shared, device="cuda", dtype=torch.int32)))
+    ws = torch.zeros(max(B.kv_attend_workspace_bytes(c.kv, 8, n) for c, _, n, _ in made), device="cuda", dtype=torch.uint8)
+    for c, q, n, sh in made + made[::-1]:
+        out, lse = T.run_attention(c, q, dtype, group=n, shared=sh, ws=ws)
+        T.check_attention(c, q, out, lse, 0.125, dtype)
+
+
 def test_waits_are_named_or_refused():
     assert B.lib().pg_selftest_token_waits(1 << 31) == B.EINVAL
     with pytest.raises(ValueError):
