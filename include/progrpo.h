@@ -619,7 +619,7 @@ int pg_selftest_bounded_wait(pg_rollout *h, void *stream);
 /*
  * Diagnostic: makes waits of pg_kv_attend run out.  Its kernels wait for tiles of keys and values (bit 0), for free
  * stages to load them into (bit 1), for queries (bit 2), scores (bit 3), weights (bit 4) and products (bit 5) of the shared
- * part; each wait is bounded.  Calls of the process that follow give up those whose bit is set at once, as if they had run
+ * part, and for the chunks of a row's own tokens (bit 6); each wait is bounded.  Calls of the process that follow give up those whose bit is set at once, as if they had run
  * out, until the word is set to 0 again: the call ends, its results are not valid, pg_kv_status returns PG_ETIMEOUT, and
  * the workspace serves the next call.  PG_EINVAL for any other bit.
  */

@@ -567,7 +567,7 @@ def kv_status(status, stream=None) -> None:
     _check(lib().pg_kv_status(_i32(status, "status"), _stream(stream)), "pg_kv_status")
 
 
-TOKEN_WAITS = ("tiles", "stages", "queries", "scores", "weights", "products")
+TOKEN_WAITS = ("tiles", "stages", "queries", "scores", "weights", "products", "chunks")
 
 
 def selftest_token_waits(*kinds: str) -> None:

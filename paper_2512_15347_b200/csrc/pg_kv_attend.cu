@@ -696,6 +696,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
   constexpr int kBoxes = kBulk && kChunk > kBoxTokens ? kChunk / kBoxTokens : 1;
   int entry[kBoxes];
   bool gave_up = false;
+  uint32_t parity = 0;                                // bulk copies: the phase that every stage's next chunk completes
   auto look_up = [&]() {
     if (ahead_at >= wend) return;
     const int t0 = (ahead.span.c0 + ahead.unit - kPieceCost) * kChunk;
@@ -779,16 +780,22 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
     }
     if constexpr (!kBulk) copy_commit();
   };
-  // the stage's chunk is in place (bulk: phase parity; a wait that runs out is reported and ends the loads)
-  uint32_t parity = 0;
+  // The stage's chunk is in place.  Bulk: a wait that runs out is reported and ends the loads; what is still on its way
+  // (this stage's and those after it; one with nothing on its way waits in vain) gets a second, last wait, so that no copy
+  // lands in memory that has been given to something else.
   auto arrived = [&](int stage) {
     if constexpr (kBulk) {
-      if (!gave_up && !mbarrier_wait_bounded(bar + 8 * stage, parity >> stage & 1u, kBulkWaitLimit)) {
-        gave_up = true;
-        flag(kv.status, kStatusTimeout);
+      if (!gave_up) {
+        const bool there = mbarrier_wait_bounded(bar + 8 * stage, parity >> stage & 1u, wait_limit(p, TokenWait::kChunks, kBulkWaitLimit));
+        if (__all_sync(0xFFFFFFFFu, there)) {
+          parity ^= 1u << stage;
+        } else {
+          gave_up = true;
+          flag(kv.status, kStatusTimeout);
+          for (int i = 0, s = stage; i < kStages - 1; ++i, s = s + 1 == kStages ? 0 : s + 1)
+            mbarrier_wait_bounded(bar + 8 * s, parity >> s & 1u, kBulkWaitLimit);
+        }
       }
-      gave_up = __any_sync(0xFFFFFFFFu, gave_up);
-      parity ^= 1u << stage;
     } else {
       copy_wait<kStages - 2>();
     }
@@ -905,12 +912,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
     if (pos < wend) here.next_piece(p);
     else break;
   }
-  if constexpr (kBulk) {
-    if (gave_up)                                       // what may still be on its way gets a second, last wait
-      for (int i = 0; i < kStages; ++i) mbarrier_wait_bounded(bar + 8 * i, parity >> i & 1u, kBulkWaitLimit);
-  } else {
-    copy_wait<0>();
-  }
+  if constexpr (!kBulk) copy_wait<0>();
   __syncthreads();
 
   // Pieces that the warps of this CTA, or several CTAs, have shared: a run of dumps is slot s0 of warp w0

@@ -11,7 +11,7 @@ constexpr int kMaxHeads = 16;                 // query heads of a (row, kv head)
 constexpr size_t kTicketBytes = 4096;         // >= 4 * kSms
 
 // The bounded waits of the attention; bit k of AttendParams::lost_waits makes those of kind k run out at once.
-enum class TokenWait : int { kTiles, kStages, kQueries, kScores, kWeights, kProducts, kKinds };
+enum class TokenWait : int { kTiles, kStages, kQueries, kScores, kWeights, kProducts, kChunks, kKinds };
 
 struct AttendParams {
   KvView kv;

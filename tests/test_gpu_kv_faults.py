@@ -56,6 +56,21 @@ def test_a_wait_of_the_shared_part_that_runs_out_is_reported(kind, dim, dtype):
     T.check_attention(c, q, out, lse, dim ** -0.5, dtype)
 
 
+@pytest.mark.parametrize("dim,dtype", [(64, "f16"), (64, "f32"), (128, "bf16"), (256, "bf16"), (256, "f32")])
+@pytest.mark.parametrize("lens", [[5000, 300, 0, 77], [17], [40] * 200])
+def test_a_wait_for_a_rows_own_chunks_that_runs_out_is_reported(dim, dtype, lens):
+    """Bulk copies that are under way when their warp gives up: in long pieces that are dumped into the ring and joined, and in
+    short ones; the calls after it find their counters at zero."""
+    c = T.Cache(lens, 2, dim, 16, dtype, seed=3)
+    q = T.queries(len(lens), 8, dim, dtype)
+    ws = torch.zeros(B.kv_attend_workspace_bytes(c.kv, 8, 1), device="cuda", dtype=torch.uint8)
+    with lost("chunks"):
+        for _ in range(3):
+            assert attend_status(c, q, ws) == B.ETIMEOUT
+    out, lse = T.run_attention(c, q, dtype, ws=ws)
+    T.check_attention(c, q, out, lse, dim ** -0.5, dtype)
+
+
 @pytest.mark.parametrize("dim,dtype", [(64, "f16"), (128, "bf16"), (256, "bf16")])
 @pytest.mark.parametrize("fill", [0x7F, 0x3F, 0xBF, 0xFF])
 def test_shared_part_that_gave_up_over_a_used_workspace(dim, dtype, fill):
