@@ -446,14 +446,40 @@ def _want(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _i32(t, what: str, n: Optional[int] = None) -> Optional[int]:
-    """Address of a contiguous int32 tensor (of n elements)."""
+# Every tensor of a call lies on one CUDA device, the current one (a cache's calls: the cache's).  What the kernels are given are bare
+# addresses: one of host memory, or of another GPU's, would fault there.
+_INT32 = torch.int32
+
+
+def _current(dev: int) -> None:
+    """Refuses a call for tensors of `dev` while another device is current."""
+    now = _device() if _device is not None else torch.cuda.current_device()
+    if now != dev:
+        raise ValueError(f"tensors of cuda:{dev}, while cuda:{now} is the current device")
+
+
+def _elsewhere(what: str, dev: int) -> ValueError:
+    return ValueError(f"{what}: a tensor on cuda:{dev}")
+
+
+def _i32(t, what: str, n: Optional[int] = None, dev: Optional[int] = None) -> Optional[int]:
+    """Address of a contiguous int32 tensor (of n elements) on device dev (None: on any CUDA device)."""
     if t is None:
         return None
-    if t.dtype is not torch.int32 or not t.is_contiguous():
+    if t.dtype is not _INT32 or not t.is_contiguous():
         raise ValueError(f"{what}: a contiguous int32 tensor")
+    on = t.get_device()
+    if on != dev and (dev is not None or on < 0):
+        raise _elsewhere(what, max(dev or 0, 0))
     if n is not None and t.numel() != n:
         raise ValueError(f"{what}: {n} elements")
+    return t.data_ptr()
+
+
+def _space(t, dev: int) -> int:
+    """Address of a workspace."""
+    if not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"workspace: a contiguous tensor on cuda:{dev}")
     return t.data_ptr()
 
 
@@ -465,22 +491,26 @@ def make_kv(k, v, table, length) -> Kv:
         k, v = k[None], v[None]
     _want(k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and
           k.dtype in _DTYPES, "k and v: alike, [layers, pages, kv heads, page size, head dim], fp32, bf16 or fp16")
+    dev = k.get_device()
+    _want(dev >= 0 and v.get_device() == dev, "k and v: on one CUDA device")
     n_layers, n_pages, heads, page, dim = k.shape
     _want(k.stride()[2:] == (page * dim, dim, 1) or k[0, 0].is_contiguous(), "the elements of a page must be contiguous")
     _want(table.dim() == 2 and length.numel() == table.shape[0], "table [rows, max pages], length [rows]")
     c = Kv(k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], n_layers, n_pages, heads, page, dim,
            k.stride(1) if n_pages > 1 else heads * page * dim, k.stride(0) if n_layers > 1 else 0,
-           _i32(table, "table"), _i32(length, "length"), table.shape[0], table.shape[1])
+           _i32(table, "table", dev=dev), _i32(length, "length", dev=dev), table.shape[0], table.shape[1])
     c._keepalive = (k, v, table, length)
     c._ref = ctypes.byref(c)
-    c._plain = (k.dtype, table.shape[0], heads, dim, n_pages, table.shape[1])   # plain values, cheaper to read than the fields
+    c._plain = (k.dtype, table.shape[0], heads, dim, n_pages, table.shape[1], dev)   # plain values, cheaper to read than the fields
     return c
 
 
-def _rows_of(t, dtype, heads: int, dim: int, what: str, rows: int) -> int:
+def _rows_of(t, dtype, heads: int, dim: int, what: str, rows: int, dev: int) -> int:
     """Row stride of [rows, heads, head dim] whose rows are contiguous inside."""
     if t.dtype is not dtype or t.shape != (rows, heads, dim):
         raise ValueError(f"{what}: [rows, heads, head dim] of the cache's type")
+    if t.get_device() != dev:
+        raise _elsewhere(what, dev)
     a, b, c = t.stride()
     if c != 1 or (b != dim and heads != 1) or (a < heads * dim and rows > 1):
         raise ValueError(f"{what}: contiguous inside a row, rows apart")
@@ -496,45 +526,50 @@ def kv_attend(kv: Kv, layer: int, q, out, workspace, *, k_new=None, v_new=None, 
     """Attention of one new token per row over the cache (see pg_kv_attend).  q, out [rows, query heads,
     head dim]; with k_new / v_new the rows' last token is stored on the way; scale defaults to
     head_dim ** -0.5."""
-    dtype, rows, kv_heads, dim, _, _ = kv._plain
+    dtype, rows, kv_heads, dim, _, _, dev = kv._plain
+    _current(dev)
     heads, k_at, v_at, new_stride = q.shape[1], None, None, 0
-    q_stride = _rows_of(q, dtype, heads, dim, "q", rows)
-    out_stride = _rows_of(out, dtype, heads, dim, "out", rows)
+    q_stride = _rows_of(q, dtype, heads, dim, "q", rows, dev)
+    out_stride = _rows_of(out, dtype, heads, dim, "out", rows, dev)
     if k_new is not None:
-        new_stride = _rows_of(k_new, dtype, kv_heads, dim, "k_new", rows)
-        if v_new is None or new_stride != _rows_of(v_new, dtype, kv_heads, dim, "v_new", rows):
+        new_stride = _rows_of(k_new, dtype, kv_heads, dim, "k_new", rows, dev)
+        if v_new is None or new_stride != _rows_of(v_new, dtype, kv_heads, dim, "v_new", rows, dev):
             raise ValueError("k_new and v_new alike")
         k_at, v_at = k_new.data_ptr(), v_new.data_ptr()
     if lse is not None:
         if lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.numel() != rows * heads:
             raise ValueError("lse: [rows, query heads] fp32")
+        if lse.get_device() != dev:
+            raise _elsewhere("lse", dev)
         lse = lse.data_ptr()
     _check(lib().pg_kv_attend(kv._ref, layer, heads, q.data_ptr(), q_stride, k_at, v_at, new_stride,
                               dim ** -0.5 if scale is None else scale, group,
-                              None if shared is None else _i32(shared, "shared", rows // max(group, 1)), out.data_ptr(), out_stride,
-                              lse, _p(workspace), workspace.nbytes, None if status is None else _i32(status, "status"),
+                              None if shared is None else _i32(shared, "shared", rows // max(group, 1), dev), out.data_ptr(), out_stride,
+                              lse, _space(workspace, dev), workspace.nbytes, None if status is None else _i32(status, "status", None, dev),
                               _stream(stream)), "pg_kv_attend")
 
 
 def kv_extend(kv: Kv, n_new, len_out, refs, refs_out, status=None, stream=None) -> None:
     """Room for n_new more tokens (an int for all rows, or int32 [rows]): lengths, pages, counts."""
-    _, rows, _, _, pages, _ = kv._plain
+    _, rows, _, _, pages, _, dev = kv._plain
+    _current(dev)
     one = isinstance(n_new, int)
-    _check(lib().pg_kv_extend(kv._ref, None if one else _i32(n_new, "n_new", rows), n_new if one else 0,
-                              _i32(len_out, "len_out", rows), _i32(refs, "refs", pages), _i32(refs_out, "refs_out", pages),
-                              _i32(status, "status"), _stream(stream)), "pg_kv_extend")
+    _check(lib().pg_kv_extend(kv._ref, None if one else _i32(n_new, "n_new", rows, dev), n_new if one else 0,
+                              _i32(len_out, "len_out", rows, dev), _i32(refs, "refs", pages, dev), _i32(refs_out, "refs_out", pages, dev),
+                              _i32(status, "status", None, dev), _stream(stream)), "pg_kv_extend")
 
 
 def kv_append(kv: Kv, layer: int, k_new, v_new, start=None, status=None, stream=None) -> None:
     """Keys and values [tokens, kv heads, head dim] of the rows' last tokens into one layer's pages;
     start [rows + 1] int32 says whose they are (None: one token per row)."""
-    dtype, rows, kv_heads, dim, _, _ = kv._plain
+    dtype, rows, kv_heads, dim, _, _, dev = kv._plain
+    _current(dev)
     n = k_new.shape[0]
-    stride = _rows_of(k_new, dtype, kv_heads, dim, "k_new", n)
-    if stride != _rows_of(v_new, dtype, kv_heads, dim, "v_new", n):
+    stride = _rows_of(k_new, dtype, kv_heads, dim, "k_new", n, dev)
+    if stride != _rows_of(v_new, dtype, kv_heads, dim, "v_new", n, dev):
         raise ValueError("k_new and v_new alike")
     _check(lib().pg_kv_append(kv._ref, layer, n, k_new.data_ptr(), v_new.data_ptr(), stride,
-                              _i32(start, "start", rows + 1), _i32(status, "status"), _stream(stream)), "pg_kv_append")
+                              _i32(start, "start", rows + 1, dev), _i32(status, "status", None, dev), _stream(stream)), "pg_kv_append")
 
 
 def kv_fork_workspace_bytes(kv: Kv, n_out: int) -> int:
@@ -543,11 +578,12 @@ def kv_fork_workspace_bytes(kv: Kv, n_out: int) -> int:
 
 def kv_fork(kv: Kv, src_rows, table_out, len_out, refs, refs_out, workspace, status=None, stream=None) -> None:
     """New row i becomes a fork of old row src_rows[i]; rows without a fork give up their pages."""
-    pages, width = kv._plain[4:]
+    pages, width, dev = kv._plain[4:]
+    _current(dev)
     n = 0 if src_rows is None else src_rows.numel()
-    _check(lib().pg_kv_fork(kv._ref, n, _i32(src_rows, "src_rows"), _i32(table_out, "table_out", n * width),
-                            _i32(len_out, "len_out", n), _i32(refs, "refs", pages), _i32(refs_out, "refs_out", pages),
-                            _p(workspace), workspace.nbytes, _i32(status, "status"), _stream(stream)), "pg_kv_fork")
+    _check(lib().pg_kv_fork(kv._ref, n, _i32(src_rows, "src_rows", None, dev), _i32(table_out, "table_out", n * width, dev),
+                            _i32(len_out, "len_out", n, dev), _i32(refs, "refs", pages, dev), _i32(refs_out, "refs_out", pages, dev),
+                            _space(workspace, dev), workspace.nbytes, _i32(status, "status", None, dev), _stream(stream)), "pg_kv_fork")
 
 
 def kv_pack_workspace_bytes(kv: Kv) -> int:
@@ -556,10 +592,11 @@ def kv_pack_workspace_bytes(kv: Kv) -> int:
 
 def kv_pack(kv: Kv, refs, refs_out, table_out, workspace, page_map=None, status=None, stream=None) -> None:
     """Moves the pages in use to the front of the pool; the table and the counts follow."""
-    _, rows, _, _, pages, width = kv._plain
-    _check(lib().pg_kv_pack(kv._ref, _i32(refs, "refs", pages), _i32(refs_out, "refs_out", pages),
-                            _i32(table_out, "table_out", rows * width), _i32(page_map, "page_map", pages),
-                            _p(workspace), workspace.nbytes, _i32(status, "status"), _stream(stream)), "pg_kv_pack")
+    _, rows, _, _, pages, width, dev = kv._plain
+    _current(dev)
+    _check(lib().pg_kv_pack(kv._ref, _i32(refs, "refs", pages, dev), _i32(refs_out, "refs_out", pages, dev),
+                            _i32(table_out, "table_out", rows * width, dev), _i32(page_map, "page_map", pages, dev),
+                            _space(workspace, dev), workspace.nbytes, _i32(status, "status", None, dev), _stream(stream)), "pg_kv_pack")
 
 
 def kv_status(status, stream=None) -> None:
@@ -581,10 +618,16 @@ def make_logits_rules(*, tokens=None, n_tokens=None, n_prompt=None, repetition=N
     tokens] int32 (the rows may be strided), n_tokens / n_prompt [rows] int32, the penalties and the
     temperature [rows] fp32, bias_ids / bias_values [rows, n], mask [rows or 1, >= vocab / 32] int32."""
     r = LogitsRules()
-    rows = None
+    rows = dev = None
+
+    def on(t, what):
+        nonlocal dev
+        dev = t.get_device() if dev is None else dev
+        _want(dev >= 0 and t.get_device() == dev, f"{what}: all tensors of the rules on one CUDA device")
 
     def see(t, what):
         nonlocal rows
+        on(t, what)
         _want(rows is None or rows == t.shape[0], f"{what}: one entry per row")
         rows = t.shape[0]
 
@@ -606,13 +649,15 @@ def make_logits_rules(*, tokens=None, n_tokens=None, n_prompt=None, repetition=N
         _want(bias_values is not None and bias_values.shape == bias_ids.shape and bias_values.dtype == torch.float32 and
               bias_values.is_contiguous(), "bias_values: fp32, shaped like bias_ids")
         see(bias_ids, "bias_ids")
+        on(bias_values, "bias_values")
         r.bias_ids, r.bias_values, r.n_bias = _i32(bias_ids, "bias_ids"), bias_values.data_ptr(), bias_ids.shape[1]
     if mask is not None:
         _want(mask.dim() == 2 and mask.dtype == torch.int32 and (mask.stride(1) == 1 or mask.shape[1] == 1), "mask: [rows or 1, words] int32")
+        on(mask, "mask")
         if mask.shape[0] > 1:
             see(mask, "mask")
         r.mask, r.mask_stride = mask.data_ptr(), mask.stride(0) if mask.shape[0] > 1 else 0
-    r._rows, r._mask_words = rows, None if mask is None else mask.shape[1]
+    r._rows, r._mask_words, r._dev = rows, None if mask is None else mask.shape[1], dev
     r._keepalive = (tokens, n_tokens, n_prompt, repetition, presence, frequency, temperature, bias_ids, bias_values, mask)
     r._ref = ctypes.byref(r)
     return r
@@ -631,6 +676,10 @@ def logits_process(logits, out, rules: LogitsRules, stream=None) -> None:
         a = b = 0
     elif a < vocab or b < vocab:
         raise ValueError("logits and out: rows apart")
+    dev = logits.get_device()
+    if dev < 0 or out.get_device() != dev or (rules._dev is not None and rules._dev != dev):
+        raise ValueError("logits, out and the rules: on one CUDA device")
+    _current(dev)
     if rules._rows is not None and rules._rows != rows:
         raise ValueError("the rules are for another number of rows")
     if rules._mask_words is not None and rules._mask_words * 32 < vocab:

@@ -107,3 +107,58 @@ def test_waits_are_named_or_refused():
     with pytest.raises(ValueError):
         B.selftest_token_waits("nothing")
     B.selftest_token_waits()
+
+
+# ------------------------------------------------------------------------------ tensors that are not the device's
+
+def test_host_tensors_are_refused_before_any_launch(monkeypatch):
+    """A host address in a kernel is a fault: every tensor of every call is looked at."""
+    c = T.Cache([20, 20], 1, 64, 16, "bf16", seed=1)
+    q = T.queries(2, 2, 64, "bf16")
+    kn = torch.zeros((2, 1, 64), device="cuda", dtype=torch.bfloat16)
+    i32 = dict(device="cuda", dtype=torch.int32)
+    ws = torch.zeros(1 << 24, device="cuda", dtype=torch.uint8)
+    attend = dict(q=q, out=torch.empty_like(q), workspace=ws, k_new=kn, v_new=kn, lse=torch.zeros((2, 2), device="cuda"),
+                  shared=torch.zeros(1, **i32), status=T.status_word())
+    extend = dict(n_new=torch.ones(2, **i32), len_out=c.len, refs=c.refs, refs_out=c.refs, status=T.status_word())
+    append = dict(k_new=kn, v_new=kn, start=torch.zeros(3, **i32), status=T.status_word())
+    fork = dict(src_rows=torch.zeros(2, **i32), table_out=torch.zeros_like(c.table), len_out=torch.zeros(2, **i32), refs=c.refs, refs_out=c.refs,
+                workspace=ws, status=T.status_word())
+    pack = dict(refs=c.refs, refs_out=c.refs, table_out=c.table, workspace=ws, page_map=torch.zeros_like(c.refs), status=T.status_word())
+    x = torch.zeros((2, 64), device="cuda")
+    logits = dict(logits=x, out=torch.zeros_like(x))
+    rules = dict(tokens=torch.zeros((2, 4), **i32), n_tokens=torch.zeros(2, **i32), n_prompt=torch.zeros(2, **i32), repetition=torch.ones(2, device="cuda"),
+                 presence=torch.ones(2, device="cuda"), frequency=torch.ones(2, device="cuda"), temperature=torch.ones(2, device="cuda"),
+                 bias_ids=torch.zeros((2, 1), **i32), bias_values=torch.zeros((2, 1), device="cuda"), mask=torch.zeros((2, 2), **i32))
+    calls = [(lambda **a: B.kv_attend(c.kv, 0, group=2, **a), attend), (lambda **a: B.kv_extend(c.kv, **a), extend),
+             (lambda **a: B.kv_append(c.kv, 0, **a), append), (lambda **a: B.kv_fork(c.kv, **a), fork),
+             (lambda **a: B.kv_pack(c.kv, **a), pack), (lambda **a: B.logits_process(rules=B.make_logits_rules(), **a), logits),
+             (B.make_logits_rules, rules), (lambda **a: B.make_kv(a["k"], a["v"], a["table"], a["length"]),
+                                            dict(k=c.k, v=c.v, table=c.table, length=c.len))]
+    before = B.launch_count()
+    for call, args in calls:
+        for name in args:
+            with pytest.raises(ValueError):
+                call(**{**args, name: args[name].cpu()})
+        with pytest.raises(ValueError):
+            call(**{name: t.cpu() for name, t in args.items()})
+    with pytest.raises(ValueError):
+        B.kv_status(torch.zeros(1, dtype=torch.int32))
+    monkeypatch.setattr(B, "_device", lambda: 1)                # another device is current
+    for call, args in calls[:6]:
+        with pytest.raises(ValueError):
+            call(**args)
+    assert B.launch_count() == before
+
+
+def test_driver_refuses_host_tensors():
+    from paper_2512_15347_b200.kvcache import PagedCache
+    c = PagedCache(32, 16, 1, 1, 64, 8, 64)
+    c.admit(2)
+    with pytest.raises(ValueError):
+        c.extend(torch.tensor([3, 4], dtype=torch.int32))
+    c.extend(torch.tensor([3, 4], device="cuda", dtype=torch.int32))
+    with pytest.raises(ValueError):
+        c.prune(torch.zeros(2, dtype=torch.int32), 1)
+    assert c.n_rows == 2 and c.len.tolist() == [3, 4]
+    c.check()
