@@ -536,6 +536,8 @@ def kv_attend(kv: Kv, layer: int, q, out, workspace, *, k_new=None, v_new=None, 
         if v_new is None or new_stride != _rows_of(v_new, dtype, kv_heads, dim, "v_new", rows, dev):
             raise ValueError("k_new and v_new alike")
         k_at, v_at = k_new.data_ptr(), v_new.data_ptr()
+    elif v_new is not None:
+        raise ValueError("v_new without k_new")
     if lse is not None:
         if lse.dtype is not torch.float32 or not lse.is_contiguous() or lse.numel() != rows * heads:
             raise ValueError("lse: [rows, query heads] fp32")

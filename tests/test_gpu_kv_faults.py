@@ -162,3 +162,13 @@ def test_driver_refuses_host_tensors():
         c.prune(torch.zeros(2, dtype=torch.int32), 1)
     assert c.n_rows == 2 and c.len.tolist() == [3, 4]
     c.check()
+
+
+def test_new_values_without_keys_are_refused():
+    c = T.Cache([20, 20], 1, 64, 16, "bf16", seed=1)
+    q = T.queries(2, 2, 64, "bf16")
+    new = torch.zeros((2, 1, 64), device="cuda", dtype=torch.bfloat16)
+    ws = torch.zeros(B.kv_attend_workspace_bytes(c.kv, 2), device="cuda", dtype=torch.uint8)
+    for kw in (dict(v_new=new), dict(k_new=new)):
+        with pytest.raises(ValueError):
+            B.kv_attend(c.kv, 0, q, torch.empty_like(q), ws, **kw)
