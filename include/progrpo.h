@@ -489,6 +489,10 @@ typedef struct {
   int32_t *table;          /* [n_rows, max_pages] int32; entries past a row's last page are not read */
   const int32_t *len;      /* [n_rows] int32: tokens of each row, 0..max_pages * page_size          */
   int32_t n_rows, max_pages;
+  int32_t *grown;          /* [n_rows] int32 or NULL: how many tokens pg_kv_extend has last found room for in each row
+                              (0 where it found none).  pg_kv_extend writes it; pg_kv_attend and pg_kv_append leave
+                              out new tokens that have no room by it.  NULL: every new token is taken to have room -
+                              one that has none would overwrite the row's last token, which other rows may share. */
 } pg_kv;
 
 /*
@@ -500,7 +504,8 @@ typedef struct {
  *   q, out [n_rows, n_q_heads, head_dim], rows q_stride / out_stride elements apart (0: contiguous)
  *   k_new, v_new (both or neither) [n_rows, n_kv_heads, head_dim], rows new_stride apart, 16-byte
  *     aligned: token len[r]-1 of every row is taken from them and stored into its page (the append of
- *     a decoding step, without a call of its own)
+ *     a decoding step after pg_kv_extend, without a call of its own).  A row with grown[r] = 0 (see pg_kv) is
+ *     attended over the tokens that it has; its entries of k_new and v_new are not read and nothing is stored.
  *   lse (nullable) [n_rows, n_q_heads] fp32
  *   group, shared: rows come in groups of `group` (group-major, as everywhere in this library), and the
  *     first shared[g] tokens (device int32 [n_rows / group]; NULL: none) of all rows of group g lie in
@@ -522,7 +527,8 @@ int pg_kv_attend(const pg_kv *kv, int32_t layer, int32_t n_q_heads, const void *
  * for every row), and for every page that a row starts to use the lowest free page (refs == 0), in row
  * order, is entered in the table and gets refs_out = 1.  A row whose table is too short, and every row
  * from the one on that finds no free page, keeps its length (status bit 3).  refs, refs_out [n_pages]
- * int32 and len, len_out may be the same arrays.  The kv's table is written.
+ * int32 and len, len_out may be the same arrays.  The kv's table is written, and its `grown` array if it has one: n_new[r],
+ * or 0 for a row that kept its length.
  */
 int pg_kv_extend(const pg_kv *kv, const int32_t *n_new, int32_t n_uniform, int32_t *len_out,
                  const int32_t *refs, int32_t *refs_out, int32_t *status, void *stream);
@@ -532,8 +538,8 @@ int pg_kv_extend(const pg_kv *kv, const int32_t *n_new, int32_t n_uniform, int32
  * k_new[start[r] .. start[r+1]) (start device [n_rows + 1] int32, ascending; NULL: one token per row,
  * n_tokens = n_rows) and become its last ones, i.e. the call follows pg_kv_extend with the kv's len
  * pointing at len_out.  k_new, v_new [n_tokens, n_kv_heads, head_dim], tokens new_stride elements
- * apart (0: contiguous), 16-byte aligned.  A row that was not extended for lack of pages must be given
- * no tokens.
+ * apart (0: contiguous), 16-byte aligned.  With the kv's `grown` array, tokens of a row beyond its last grown[r] are
+ * left out (a row that was not extended for lack of pages); without it such a row must be given no tokens.
  */
 int pg_kv_append(const pg_kv *kv, int32_t layer, int32_t n_tokens, const void *k_new, const void *v_new,
                  int64_t new_stride, const int32_t *start, int32_t *status, void *stream);

@@ -62,7 +62,7 @@ class Kv(ctypes.Structure):
                 ("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_stride", ctypes.c_int64),
                 ("layer_stride", ctypes.c_int64), ("table", ctypes.c_void_p), ("len", ctypes.c_void_p),
-                ("n_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+                ("n_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("grown", ctypes.c_void_p)]
 
 
 class LogitsRules(ctypes.Structure):
@@ -483,10 +483,11 @@ def _space(t, dev: int) -> int:
     return t.data_ptr()
 
 
-def make_kv(k, v, table, length) -> Kv:
+def make_kv(k, v, table, length, grown=None) -> Kv:
     """Descriptor of a paged cache over caller-owned tensors: k, v [layers, pages, kv heads, page size,
     head dim] (or without the layers), each page contiguous, the page and layer strides free; table
-    [rows, max pages] and length [rows] int32.  Keeps references to all four."""
+    [rows, max pages] and length [rows] int32; grown [rows] int32 (nullable) keeps which rows ``kv_extend`` found
+    room in, so that new tokens of the others are left out.  Keeps references to all of them."""
     if k.dim() == 4:
         k, v = k[None], v[None]
     _want(k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and
@@ -498,8 +499,9 @@ def make_kv(k, v, table, length) -> Kv:
     _want(table.dim() == 2 and length.numel() == table.shape[0], "table [rows, max pages], length [rows]")
     c = Kv(k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], n_layers, n_pages, heads, page, dim,
            k.stride(1) if n_pages > 1 else heads * page * dim, k.stride(0) if n_layers > 1 else 0,
-           _i32(table, "table", dev=dev), _i32(length, "length", dev=dev), table.shape[0], table.shape[1])
-    c._keepalive = (k, v, table, length)
+           _i32(table, "table", dev=dev), _i32(length, "length", dev=dev), table.shape[0], table.shape[1],
+           _i32(grown, "grown", table.shape[0], dev))
+    c._keepalive = (k, v, table, length, grown)
     c._ref = ctypes.byref(c)
     c._plain = (k.dtype, table.shape[0], heads, dim, n_pages, table.shape[1], dev)   # plain values, cheaper to read than the fields
     return c
@@ -524,8 +526,8 @@ def kv_attend_workspace_bytes(kv: Kv, n_q_heads: int, group: int = 1) -> int:
 def kv_attend(kv: Kv, layer: int, q, out, workspace, *, k_new=None, v_new=None, lse=None,
               scale: Optional[float] = None, group: int = 1, shared=None, status=None, stream=None) -> None:
     """Attention of one new token per row over the cache (see pg_kv_attend).  q, out [rows, query heads,
-    head dim]; with k_new / v_new the rows' last token is stored on the way; scale defaults to
-    head_dim ** -0.5."""
+    head dim]; with k_new / v_new the rows' last token is stored on the way (not in a row that ``kv.grown`` says has no room for
+    it); scale defaults to head_dim ** -0.5."""
     dtype, rows, kv_heads, dim, _, _, dev = kv._plain
     _current(dev)
     heads, k_at, v_at, new_stride = q.shape[1], None, None, 0

@@ -20,6 +20,7 @@ struct KvView {
   int64_t page_stride, layer_stride;
   int32_t* table;
   const int32_t* len;
+  int32_t* grown;
   int32_t* status;
   int n_layers, n_pages, n_kv_heads, page_size, head_dim, n_rows, max_pages;
 };
@@ -52,6 +53,7 @@ inline KvView kv_view(const pg_kv* c, int32_t* status) {
   v.layer_stride = c->n_layers > 1 ? c->layer_stride : 0;
   v.table = c->table;
   v.len = c->len;
+  v.grown = c->grown;
   v.status = status;
   v.n_layers = c->n_layers;
   v.n_pages = c->n_pages;
@@ -109,6 +111,9 @@ __device__ __forceinline__ int checked_len(const KvView& kv, int n) {
   return n;
 }
 __device__ __forceinline__ int row_len(const KvView& kv, int row) { return checked_len(kv, kv.len[row]); }
+
+// Whether pg_kv_extend has last found room for n new tokens of a row, as far as the cache keeps that.
+__device__ __forceinline__ bool has_room(const KvView& kv, int row, int n) { return !kv.grown || n <= kv.grown[row]; }
 
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }

@@ -504,9 +504,13 @@ struct Place {
   int row, h, split, unit;
   int group, n, tokens;        // row = group * p.group + n; the group's shared tokens
   int next_len;                // of the next row, fetched long before it is needed
+  bool takes, next_takes;      // the row's last token is its new one; the next row's
   RowSpan span;
+  static __device__ __forceinline__ bool takes_new(const AttendParams& p, int row) { return p.k_new && has_room(p.kv, row, 1); }
   __device__ __forceinline__ void fetch(const AttendParams& p) {
-    if (row + 1 < p.kv.n_rows) next_len = p.kv.len[row + 1];
+    if (row + 1 >= p.kv.n_rows) return;
+    next_len = p.kv.len[row + 1];
+    next_takes = takes_new(p, row + 1);
   }
   __device__ __forceinline__ void next_piece(const AttendParams& p) {
     unit = 0;
@@ -522,6 +526,7 @@ struct Place {
         tokens = p.shared ? group_tokens(p, group) : 0;
       }
       span = row_span<kChunk>(p, tokens, next_len);
+      takes = next_takes;
       fetch(p);
     } while (span.c1 == span.c0);
   }
@@ -532,6 +537,7 @@ struct Place {
     unit = unit_;
     group = (int)div_by(row_, p.group_div);
     n = row_ - group * p.group;
+    takes = takes_new(p, row_);
     tokens = p.shared ? group_tokens(p, group) : 0;
     span = span_;
   }
@@ -746,7 +752,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
         // where the token is: an element offset in the pools, -1 for zeros, -2 - e for element e of the new tokens
         int64_t from = -1;
         if (lane < kChunk && t < ahead.span.hi && t >= ahead.span.lo) {
-          if (p.k_new && t == ahead.span.hi - 1) {
+          if (ahead.takes && t == ahead.span.hi - 1) {
             from = -2 - (ahead.row * p.new_stride + (int64_t)ahead.h * kv.head_dim);
           } else if ((unsigned int)entry[0] < (unsigned int)kv.n_pages) {
             const int slot = t - (int)div_by(t, p.page) * kv.page_size;
@@ -810,7 +816,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
         const int tok = i / row_pieces, c = i - tok * row_pieces;
         if (t0 + tok >= at.span.hi) *(uint4*)(vb + Body::piece_at(tok, c)) = make_uint4(0, 0, 0, 0);
       }
-      if (p.k_new) {
+      if (at.takes) {
         const int64_t e = at.row * p.new_stride + (int64_t)at.h * kv.head_dim;
         for (int c = lane; c < row_pieces; c += 32) {
           const uint32_t to = Body::piece_at(at.span.hi - 1 - t0, c);
@@ -831,7 +837,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
     for (int64_t i = (int64_t)blockIdx.x * kWarps + warp; i < (int64_t)kv.n_rows * kv.n_kv_heads; i += (int64_t)gridDim.x * kWarps) {
       const int r = (int)(i / kv.n_kv_heads), h = (int)(i - (int64_t)r * kv.n_kv_heads);
       const int t = checked_len(kv, kv.len[r]) - 1;
-      if (t < 0) continue;
+      if (t < 0 || !has_room(kv, r, 1)) continue;
       const int pg = (int)div_by(t, p.page), page = kv.table[(int64_t)r * kv.max_pages + pg];
       if ((unsigned int)page >= (unsigned int)kv.n_pages) {
         if (lane == 0) flag(kv.status, kStatusIndex);

@@ -473,6 +473,7 @@ __global__ void __launch_bounds__(kScanThreads) extend_kernel(const __grid_const
         for (int j = 0; j < min(want, found - before); ++j) p.refs[kv.table[(int64_t)r * kv.max_pages + old_pages + j]] = 0;
       if (!grown && add) flag(kv.status, kStatusPages);
       p.len_out[r] = grown ? n + add : n;
+      if (kv.grown) kv.grown[r] = grown ? add : 0;
     }
     dry = dry || found < total;
     __syncthreads();
@@ -503,6 +504,7 @@ __global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ App
     int64_t at = -1;
     if (t < p.n_tokens) {
       int row = t, pos = -1;
+      int last = 1;                             // place of the token from the row's end
       if (p.start) {
         int lo = 0, hi = kv.n_rows;             // first row whose end is past t
         while (lo < hi) {
@@ -510,16 +512,20 @@ __global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ App
           if (p.start[mid + 1] <= t) lo = mid + 1; else hi = mid;
         }
         row = lo;
-        if (row < kv.n_rows && t >= p.start[row]) pos = row_len(kv, row) - (p.start[row + 1] - t);
+        if (row < kv.n_rows && t >= p.start[row]) {
+          last = p.start[row + 1] - t;
+          pos = row_len(kv, row) - last;
+        }
       } else if (row < kv.n_rows) {
         pos = row_len(kv, row) - 1;
       }
-      if (pos >= 0) {
+      const bool left_out = row < kv.n_rows && !has_room(kv, row, last);
+      if (pos >= 0 && !left_out) {
         const int page = kv.table[(int64_t)row * kv.max_pages + pos / kv.page_size];
         if ((unsigned int)page < (unsigned int)kv.n_pages)
           at = page * kv.page_stride + (int64_t)(pos % kv.page_size) * kv.head_dim;
       }
-      if (at < 0) flag(kv.status, kStatusIndex);
+      if (at < 0 && !left_out) flag(kv.status, kStatusIndex);
     }
     slot[threadIdx.x] = at;
   }

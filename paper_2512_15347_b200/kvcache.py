@@ -28,6 +28,8 @@ class PagedCache:
         width = -(-max_tokens // page_size)
         self._tables = [torch.full((max_rows, width), -1, device=dev, dtype=torch.int32) for _ in range(2)]
         self._lens = [torch.zeros(max_rows, device=dev, dtype=torch.int32) for _ in range(2)]
+        self._grown = torch.zeros(max_rows, device=dev, dtype=torch.int32)
+        self._extended = False               # whether _grown is about the present rows
         self._cur = 0
         self.refs = torch.zeros(n_pages, device=dev, dtype=torch.int32)
         self.status = torch.zeros(1, device=dev, dtype=torch.int32)
@@ -36,7 +38,7 @@ class PagedCache:
         self.n_rows = 0
 
     def _describe(self):
-        self.kv = B.make_kv(self.k, self.v, self.table, self.len)
+        self.kv = B.make_kv(self.k, self.v, self.table, self.len, self._grown[: self._n_rows])
 
     @property
     def n_rows(self) -> int:
@@ -68,20 +70,30 @@ class PagedCache:
         B.kv_fork(self.kv, None, None, None, self.refs, self.refs, self._space("fork", B.kv_fork_workspace_bytes(self.kv, 0)),
                   status=self.status)
         self._lens[self._cur].zero_()
+        self._extended = False
         self.group, self.shared = 1, None
         self.n_rows = n_rows
 
     def extend(self, n_new) -> None:
-        """Room for n_new more tokens in every row (an int, or int32 [rows])."""
+        """Room for n_new more tokens in every row (an int, or int32 [rows]).  A row without room (``check`` reports it)
+        keeps its tokens: the new ones that ``append`` and ``attend`` are given for it are left out."""
         B.kv_extend(self.kv, n_new, self.len, self.refs, self.refs, status=self.status)
+        self._extended = True
+
+    def _want_room(self) -> None:
+        if not self._extended:
+            raise ValueError("new tokens without room for them: extend first")
 
     def append(self, layer: int, k_new, v_new, start=None) -> None:
         """Keys and values of the rows' last tokens (after ``extend``)."""
+        self._want_room()
         B.kv_append(self.kv, layer, k_new, v_new, start, status=self.status)
 
     def attend(self, layer: int, q, k_new=None, v_new=None, out=None, lse=None, scale: Optional[float] = None):
         """Attention of the rows' newest token over the cache; with k_new / v_new that token is stored on
         the way (after ``extend(1)``)."""
+        if k_new is not None:
+            self._want_room()
         out = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
         ws = self._space("attend", B.kv_attend_workspace_bytes(self.kv, q.shape[1], self.group))
         B.kv_attend(self.kv, layer, q, out, ws, k_new=k_new, v_new=v_new, lse=lse, scale=scale, group=self.group, shared=self.shared,
@@ -96,6 +108,7 @@ class PagedCache:
         B.kv_fork(self.kv, src_rows, self._tables[other][:n], self._lens[other][:n], self.refs, self.refs,
                   self._space("fork", B.kv_fork_workspace_bytes(self.kv, n)), status=self.status)
         self._cur = other
+        self._extended = False
         self.n_rows = n
 
     def expand(self, fan: int) -> None:

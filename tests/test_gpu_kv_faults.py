@@ -172,3 +172,93 @@ def test_new_values_without_keys_are_refused():
     for kw in (dict(v_new=new), dict(k_new=new)):
         with pytest.raises(ValueError):
             B.kv_attend(c.kv, 0, q, torch.empty_like(q), ws, **kw)
+
+
+# ------------------------------------------------------------------------------ rows that found no page
+
+def look(cache):
+    """What check_attention needs of a driver's cache, as it is now."""
+    from types import SimpleNamespace
+    return SimpleNamespace(k=cache.k, v=cache.v, table=cache.table.clone(), len=cache.len.clone())
+
+
+@pytest.mark.parametrize("dtype,dim,page,prompt", [("bf16", 64, 16, 64), ("f16", 128, 16, 128), ("f32", 64, 16, 32), ("bf16", 72, 8, 64), ("f32", 40, 3, 9)])
+def test_rows_without_a_page_take_no_new_token(dtype, dim, page, prompt):
+    """A prompt of whole pages is expanded, the pool has pages for some of the rows only: the others' new tokens must not
+    land in the prompt's last page, which all of them share.  Once by the decoding step, once by the appending call."""
+    from paper_2512_15347_b200.kvcache import PagedCache
+    G, N, heads, layers = 2, 6, 2, 2
+    c = PagedCache(G * prompt // page + 5, page, layers, heads, dim, G * N, prompt + 4 * page, T.DT[dtype])
+    c.admit(G)
+    c.extend(prompt)
+    new = lambda n, seed: torch.randn((n, heads, dim), generator=T.gen(seed), device="cuda").to(T.DT[dtype])
+    start = torch.tensor([0, prompt, 2 * prompt], device="cuda", dtype=torch.int32)
+    for layer in range(layers):
+        c.append(layer, new(2 * prompt, layer), new(2 * prompt, 10 + layer), start)
+    c.expand(N)
+    c.check()
+    c.extend(1)                                                 # pages for the first five rows
+    with pytest.raises(B.PgError) as e:
+        c.check()
+    assert e.value.code == B.ENOPAGES
+    assert c.len.tolist() == [prompt + 1] * 5 + [prompt] * 7
+    q, kn, vn = T.queries(G * N, 4, dim, dtype), new(G * N, 20), new(G * N, 21)
+    want_k, want_v = c.k.clone(), c.v.clone()
+    for r in range(5):
+        at = int(c.table[r, prompt // page])
+        want_k[0, at, :, 0], want_v[0, at, :, 0] = kn[r], vn[r]
+        want_k[1, at, :, 0], want_v[1, at, :, 0] = kn[r], vn[r]
+    lse = torch.empty((G * N, 4), device="cuda")
+    out = c.attend(0, q, kn, vn, lse=lse)
+    T.check_attention(look(c), q, out, lse, dim ** -0.5, dtype)
+    c.append(1, kn, vn)                                         # one token a row
+    assert T.same_bits(c.k, want_k) and T.same_bits(c.v, want_v)
+    c.status.zero_()
+    c.append(1, kn, vn, torch.arange(G * N + 1, device="cuda", dtype=torch.int32))
+    assert T.same_bits(c.k, want_k) and T.same_bits(c.v, want_v)
+    c.check()
+    # pruned to the rows that grew and one that did not, there are pages again
+    c.prune(torch.tensor([0, 4, 6, 7], device="cuda", dtype=torch.int32), 2)
+    c.extend(torch.tensor([1, 0, 1, 1], device="cuda", dtype=torch.int32))
+    c.check()
+    q, kn, vn = T.queries(4, 4, dim, dtype, seed=5), new(4, 22), new(4, 23)
+    want_k, want_v = c.k.clone(), c.v.clone()
+    for r in (0, 2, 3):
+        n = int(c.len[r]) - 1
+        want_k[1, c.table[r, n // page], :, n % page], want_v[1, c.table[r, n // page], :, n % page] = kn[r], vn[r]
+    lse = torch.empty((4, 4), device="cuda")
+    out = c.attend(1, q, kn, vn, lse=lse)
+    assert T.same_bits(c.k, want_k) and T.same_bits(c.v, want_v)
+    T.check_attention(look(c), q, out, lse, dim ** -0.5, dtype, layer=1)
+
+
+def test_appended_tokens_beyond_what_a_row_has_grown_by_are_left_out():
+    c = T.Cache([10, 20, 30], 1, 8, 8, "f32", seed=4)
+    grown = torch.tensor([3, 2, 0], device="cuda", dtype=torch.int32)
+    kv = B.make_kv(c.k, c.v, c.table, c.len, grown)
+    new = torch.randn((9, 1, 8), generator=T.gen(5), device="cuda")
+    want = c.k.clone()
+    for r, t, pos in ((0, 0, 7), (0, 1, 8), (0, 2, 9), (1, 4, 18), (1, 5, 19)):
+        want[0, c.rows[r][pos // 8], :, pos % 8] = new[t]
+    st = T.status_word()
+    B.kv_append(kv, 0, new, new, torch.tensor([0, 3, 6, 9], device="cuda", dtype=torch.int32), status=st)
+    B.kv_status(st)
+    assert T.same_bits(c.k, want)
+
+
+def test_driver_wants_room_before_new_tokens():
+    from paper_2512_15347_b200.kvcache import PagedCache
+    c = PagedCache(32, 16, 1, 1, 64, 8, 64)
+    q, new = (torch.zeros((2, 1, 64), device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    c.admit(1)
+    with pytest.raises(ValueError):
+        c.append(0, new[:1], new[:1])
+    c.extend(16)
+    c.append(0, new[:1], new[:1])
+    c.expand(2)
+    with pytest.raises(ValueError):
+        c.attend(0, q, new, new)                                # would overwrite the prompt's last token
+    c.attend(0, q)
+    c.extend(1)
+    c.attend(0, q, new, new)
+    c.check()
