@@ -462,6 +462,9 @@ int pg_gather_rows(pg_rollout *h, const int32_t *rows, int32_t n_out, int32_t n_
  *
  * All calls are stateless: the caller owns the pool, the table, the lengths, the reference counts
  * and the workspace, and passes them by a descriptor (HOST memory, read during the call only).
+ * Workspaces are device memory, 16-byte aligned, zeroed once before their first use; every call leaves
+ * its counters in them zero again.  One buffer may serve calls of any kind and shape one after the
+ * other; calls that can overlap on the GPU need one each.
  * Indices that come from device memory (page numbers, row numbers, lengths, token ids) are checked
  * in the kernels: a bad one is never dereferenced, bit 2 of *status is set and pg_kv_status returns
  * PG_EINDEX.  Running out of pages or of table entries sets bit 3 (PG_ENOPAGES); a bounded device-side
@@ -512,9 +515,7 @@ typedef struct {
  *     the same pages - the state after an expansion.  Those pages are read through the table row of
  *     the group's first row, once for the whole group (16-bit caches, from 64 tokens on, whole 64s of
  *     them; the rest, and rows that end inside the shared tokens, are read row by row).
- *   workspace: at least pg_kv_attend_workspace_bytes(kv, n_q_heads, group) bytes of device memory,
- *     16-byte aligned, zeroed once before its first use; every call leaves its counters zero again.
- *     Two calls that can overlap on the GPU need a workspace each.
+ *   workspace: at least pg_kv_attend_workspace_bytes(kv, n_q_heads, group) bytes.
  */
 size_t pg_kv_attend_workspace_bytes(const pg_kv *kv, int32_t n_q_heads, int32_t group);
 int pg_kv_attend(const pg_kv *kv, int32_t layer, int32_t n_q_heads, const void *q, int64_t q_stride,
@@ -554,8 +555,7 @@ int pg_kv_append(const pg_kv *kv, int32_t layer, int32_t n_tokens, const void *k
  *   table_out [n_out, max_pages] (entries past a row's last page become -1), len_out [n_out]: not
  *   overlapping the kv's; refs, refs_out [n_pages]: may be the same array.  A fork that finds no free
  *   page is shortened to its full pages (status bit 3).
- *   workspace: pg_kv_fork_workspace_bytes(kv, n_out) bytes, 16-byte aligned, zeroed once before its
- *   first use.
+ *   workspace: at least pg_kv_fork_workspace_bytes(kv, n_out) bytes.
  */
 size_t pg_kv_fork_workspace_bytes(const pg_kv *kv, int32_t n_out);
 int pg_kv_fork(const pg_kv *kv, int32_t n_out, const int32_t *src_rows, int32_t *table_out,
@@ -569,7 +569,7 @@ int pg_kv_fork(const pg_kv *kv, int32_t n_out, const int32_t *src_rows, int32_t 
  * [n_rows, max_pages] may be the kv's table (entries past a row's last page become -1), refs_out may be
  * refs.  Other holders of page numbers (forks kept outside this table) must be remapped by the caller: page_map
  * (nullable, [n_pages] int32) receives the new number of every page in use, -1 for free ones.
- * workspace as above, pg_kv_pack_workspace_bytes(kv).
+ * workspace: at least pg_kv_pack_workspace_bytes(kv) bytes.
  */
 size_t pg_kv_pack_workspace_bytes(const pg_kv *kv);
 int pg_kv_pack(const pg_kv *kv, const int32_t *refs, int32_t *refs_out, int32_t *table_out,

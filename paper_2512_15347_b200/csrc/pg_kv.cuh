@@ -14,6 +14,10 @@ constexpr int kStatusTimeout = 2;   // status bit 1: a bounded wait ran out
 constexpr int kStatusIndex = 4;     // status bit 2: an index from device memory was out of range
 constexpr int kStatusPages = 8;     // status bit 3: no free page, or a row's table is full
 
+// Every call's workspace begins with this many bytes of counters that are zero between calls; what lies behind them is written
+// before it is read.  So one buffer may serve all calls of a stream.
+constexpr size_t kCounterBytes = 4096;
+
 // One layer of the cache, by value in the kernel parameters.  Strides in elements.
 struct KvView {
   void *k, *v;

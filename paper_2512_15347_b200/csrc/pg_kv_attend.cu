@@ -1147,7 +1147,7 @@ size_t pg_kv_attend_workspace_bytes(const pg_kv* kv, int32_t n_q_heads, int32_t 
   // tickets first, so that their place depends on nothing
   const size_t dp = kv->head_dim <= 64 ? 64 : kv->head_dim <= 128 ? 128 : 256;
   const size_t acc = dp * pg::kMaxHeads;
-  return pg::kTicketBytes + pg::kSms * (2 * (acc + 2 * pg::kMaxHeads) + pg::kMaxWarps * acc) * sizeof(float) +
+  return pg::kCounterBytes + pg::kSms * (2 * (acc + 2 * pg::kMaxHeads) + pg::kMaxWarps * acc) * sizeof(float) +
          pg::shared_bytes(kv, n_q_heads, group);
 }
 
@@ -1187,7 +1187,7 @@ int pg_kv_attend(const pg_kv* kv, int32_t layer, int32_t n_q_heads, const void* 
   p.page = pg::fast_div((uint32_t)kv->page_size);
   p.group_div = pg::fast_div((uint32_t)group);
   p.tickets = (unsigned int*)workspace;
-  p.parts = (float*)((char*)workspace + pg::kTicketBytes);
+  p.parts = (float*)((char*)workspace + pg::kCounterBytes);
   const size_t dp = kv->head_dim <= 64 ? 64 : kv->head_dim <= 128 ? 128 : 256;
   p.dumps = p.parts + 2 * pg::kSms * (dp + 2) * pg::kMaxHeads;
   cudaStream_t st = (cudaStream_t)stream;

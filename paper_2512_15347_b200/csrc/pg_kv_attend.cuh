@@ -8,7 +8,7 @@ namespace pg {
 constexpr int kSms = 148;
 constexpr int kMaxWarps = 8;
 constexpr int kMaxHeads = 16;                 // query heads of a (row, kv head) piece
-constexpr size_t kTicketBytes = 4096;         // >= 4 * kSms
+static_assert(kSms * sizeof(unsigned int) <= kCounterBytes, "a ticket for every CTA");
 
 // The bounded waits of the attention; bit k of AttendParams::lost_waits makes those of kind k run out at once.
 enum class TokenWait : int { kTiles, kStages, kQueries, kScores, kWeights, kProducts, kChunks, kKinds };

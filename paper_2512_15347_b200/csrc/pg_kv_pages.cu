@@ -178,9 +178,9 @@ static int launch_copy(const pg_kv* kv, const KvView& view, const int2* pairs, c
 // ---------------------------------------------------------------- fork
 
 struct ForkWork {            // in the caller's workspace
-  unsigned int* ticket;      // zero between calls
+  unsigned int* ticket;      // counters
+  int32_t* n_need;           // rows in need
   int32_t* n_pairs;          // copies to make
-  int32_t* n_need;           // rows in need, zero between calls
   int32_t* need;             // [n_out] 1 where new row i needs a page for its partly filled last page
   int2* pairs;               // [n_out]
 };
@@ -189,12 +189,13 @@ static size_t fork_work(char* base, int64_t n_out, ForkWork* w) {
   const size_t need = up(n_out * 4), pairs = up(n_out * 8);
   if (w) {
     w->ticket = (unsigned int*)base;
-    w->n_pairs = (int32_t*)(base + 4);
-    w->n_need = (int32_t*)(base + 8);
+    w->n_need = (int32_t*)(base + 4);
+    base += kCounterBytes;
+    w->n_pairs = (int32_t*)base;
     w->need = (int32_t*)(base + 16);
     w->pairs = (int2*)(base + 16 + need);
   }
-  return 16 + need + pairs;
+  return kCounterBytes + 16 + need + pairs;
 }
 
 constexpr int kForkThreads = 256, kForkRows = 32;   // most old rows of a CTA
@@ -350,7 +351,7 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constan
 
 // ---------------------------------------------------------------- pack
 
-struct PackWork {
+struct PackWork {          // in the caller's workspace, behind the counters
   int32_t* n_pairs;
   int32_t* to;         // [n_pages] new number of a page in use, -1 of a free one
   int2* pairs;         // [n_pages / 2 + 1] moves
@@ -359,11 +360,12 @@ static size_t pack_work(char* base, int64_t n_pages, PackWork* w) {
   auto up = [](size_t b) { return (b + 15) & ~(size_t)15; };
   const size_t to = up(n_pages * 4), pairs = up((n_pages / 2 + 1) * 8);
   if (w) {
+    base += kCounterBytes;
     w->n_pairs = (int32_t*)base;
     w->to = (int32_t*)(base + 16);
     w->pairs = (int2*)(base + 16 + to);
   }
-  return 16 + to + pairs;
+  return kCounterBytes + 16 + to + pairs;
 }
 
 struct PackParams {

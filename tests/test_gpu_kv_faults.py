@@ -109,6 +109,41 @@ def test_waits_are_named_or_refused():
     B.selftest_token_waits()
 
 
+# ------------------------------------------------------------------------------ one buffer for all calls
+
+def test_one_workspace_for_calls_of_every_kind():
+    """Packing, forking and attention in turn over one buffer: none finds its counters at what another has left."""
+    def cache(seed):
+        return T.Cache([77, 5, 130, 64], 2, 64, 16, "bf16", spare=90, seed=seed)
+    need = lambda c: max(B.kv_pack_workspace_bytes(c.kv), B.kv_fork_workspace_bytes(c.kv, 12), B.kv_attend_workspace_bytes(c.kv, 8, 1))
+    ws = torch.zeros(need(cache(1)), device="cuda", dtype=torch.uint8)
+    long = T.Cache([9000, 41], 2, 64, 16, "bf16", seed=9)                 # pieces that several CTAs share
+    ql = T.queries(2, 8, 64, "bf16")
+    for seed in range(1, 4):
+        c = cache(seed)
+        table, refs, moves, _ = ref.pack(T.clean_rows(c), c.lens, c.refs.tolist(), c.page)
+        assert moves
+        want_k, want_v = T.pools_after(c, moves)
+        st = T.status_word()
+        B.kv_pack(c.kv, c.refs, c.refs, c.table, ws, status=st)
+        B.kv_status(st)
+        assert c.table.tolist() == table and c.refs.tolist() == refs and T.same_bits(c.k, want_k) and T.same_bits(c.v, want_v)
+        out, lse = T.run_attention(long, ql, "bf16", ws=ws)
+        T.check_attention(long, ql, out, lse, 0.125, "bf16")
+        c.rows = table
+        src = [0, 0, 0, 1, 1, 2, 2, 3, 2]
+        want_t, want_l, want_r, copies, _ = ref.fork(c.rows, c.lens, refs, src, c.page, c.n_pages)
+        want_k, want_v = T.pools_after(c, copies)
+        t, n = torch.empty((9, c.width), device="cuda", dtype=torch.int32), torch.empty(9, device="cuda", dtype=torch.int32)
+        B.kv_fork(c.kv, torch.tensor(src, device="cuda", dtype=torch.int32), t, n, c.refs, c.refs, ws, status=st)
+        B.kv_status(st)
+        assert t.tolist() == want_t and n.tolist() == want_l and c.refs.tolist() == want_r
+        assert T.same_bits(c.k, want_k) and T.same_bits(c.v, want_v)
+        assert int(ws[:4096].sum()) == 0
+        out, lse = T.run_attention(long, ql, "bf16", ws=ws)
+        T.check_attention(long, ql, out, lse, 0.125, "bf16")
+
+
 # ------------------------------------------------------------------------------ tensors that are not the device's
 
 def test_host_tensors_are_refused_before_any_launch(monkeypatch):
