@@ -29,6 +29,7 @@ namespace pg {
 
 constexpr int kRows = 128;           // queries of a product
 constexpr float kSlack = 8.f;
+constexpr float kFarScore = 4194304.f;         // 2^22: half a unit in the last place is 2^-2
 constexpr int kWaitLimit = 1 << 14;
 
 // Two tiles of 128 queries share the tensor memory with their scores up to head dim 128, one above.
@@ -325,7 +326,15 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
           const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * scale;
           // the previous product has read P and updated O
           if (k > 0 && !wait(o_done(t), tiles_done - 1, TokenWait::kProducts)) { ok = false; break; }
-          const bool raise = top > m + kSlack || m == -INFINITY;
+          // Far from zero a rounded product and the fused one below differ by more than a weight can hold: there the
+          // scores are scaled first, as the maximum has been.
+          float by = scale;
+          if (__any_sync(0xFFFFFFFFu, fabsf(top) >= kFarScore)) {
+#pragma unroll
+            for (int j = 0; j < kTile; ++j) s[j] *= scale;
+            by = 1.f;
+          }
+          const bool raise = top > __fadd_rd(m, kSlack) || m == -INFINITY;
           float f = 1.f;
           if (raise && top > m) {
             f = exp2_fast(m - top);
@@ -347,7 +356,7 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
           const float off = m == -INFINITY ? 0.f : m;
           char* pd = smem + kStages * L::kStageBytes + kSlots * L::kQBytes + t * L::kPBytes;
           uint64_t sums[2] = {0, 0};
-          const uint64_t scale2 = pair_of_floats(scale, scale), off2 = pair_of_floats(-off, -off);
+          const uint64_t scale2 = pair_of_floats(by, by), off2 = pair_of_floats(-off, -off);
 #pragma unroll
           for (int c8 = 0; c8 < kTile / 8; ++c8) {
             uint32_t packed[4];

@@ -297,3 +297,38 @@ def test_driver_wants_room_before_new_tokens():
     c.extend(1)
     c.attend(0, q, new, new)
     c.check()
+
+
+# ------------------------------------------------------------------------------ scores far from zero
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("size", [2.0 ** 6, 2.0 ** 9, 2.0 ** 11, 2.0 ** 13, 2.0 ** 15])
+@pytest.mark.parametrize("scale", [0.125, 0.1, -0.1])
+def test_scores_far_from_zero_take_the_largest(dtype, size, scale):
+    """Queries and keys up to half the range of the smallest type: the largest score is apart from the rest by more than any weight
+    spans, and the result is its token's value - in the tokens that a group shares and in the rows' own."""
+    n, dim, tokens = 16, 64, 320
+    c = T.shared_cache(2, n, 256, [64] * 2 * n, 1, dim, 16, dtype, seed=2)
+    q = torch.full((2 * n, 4, dim), size, device="cuda", dtype=T.DT[dtype])
+    q *= torch.linspace(0.5, 1, 2 * n, device="cuda").to(T.DT[dtype])[:, None, None]
+    sign = 1 if scale > 0 else -1
+    for g, best in ((0, 200), (1, 100)):
+        for t in range(256):                                       # shared tokens: levels below the best one, rising and falling
+            level = size if t == best else size * (0.25 + 0.125 * (t % 5))
+            c.k[0, c.rows[g * n][t // 16], 0, t % 16] = sign * level
+    own = {}
+    for r in range(2 * n):
+        for t in range(256, tokens):
+            c.k[0, c.rows[r][t // 16], 0, t % 16] = sign * size * 0.5
+        if r % 2:                                                  # every other row has its largest score in a token of its own
+            own[r] = 256 + r
+            c.k[0, c.rows[r][own[r] // 16], 0, own[r] % 16] = sign * size * 1.5
+    sh = torch.full((2,), 256, device="cuda", dtype=torch.int32)
+    for kw in (dict(group=n, shared=sh), dict()):
+        out, lse = T.run_attention(c, q, dtype, scale=scale, **kw)
+        assert torch.isfinite(lse).all()
+        for r in range(2 * n):
+            t = own.get(r, (200, 100)[r // n])
+            v = c.v[0, c.rows[r][t // 16], 0, t % 16].double()
+            # the one weight is rounded to the type, and the result: u each, and fp32's roundings beside them
+            assert ((out[r].double() - v).abs() <= 2.1 * T.UNIT[dtype] * v.abs() + 2.0 ** -22 * v.abs() + 2.0 ** -24).all(), (r, t)
