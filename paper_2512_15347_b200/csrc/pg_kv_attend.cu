@@ -86,7 +86,10 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, __half) {
 // 16-bit: tensor cores, with keys as the rows of the product (S^T = K Q^T, O^T = V^T P^T), so that a kv
 // head with few query heads fills the n = 8 side instead of padding m = 16.  P^T comes from S^T's
 // accumulators by an 8x8 register transposition; P is rounded to the cache's type for the product (the
-// sum l is taken before the rounding), which adds less to the result than its own last rounding.
+// sum l is taken before the rounding): one more error of the size of the result's own rounding, and independent from token to
+// token (bf16, 96 ragged rows: 1.6e-3 of the result against 1.5e-3 for the plain form in fp32).  fp16 has weights of full
+// precision down to 2^-14 only, and none below 2^-25, which many small ones beside a large one would be missed by: its m is
+// kept kLift powers of two below the largest score, so that P, l and o are 2^kLift times as large.
 template <typename T, int DP, int NT, int kKeys>
 struct MmaBody {
   static constexpr int kChunk = kKeys;
@@ -94,6 +97,7 @@ struct MmaBody {
   static constexpr int kRegs = DP / 16 * NT * 4;
   static constexpr int kRowBytes = DP * 2;
   static constexpr size_t kQBytes = 0;              // shared memory per warp for the queries
+  static constexpr float kLift = std::is_same<T, __half>::value ? 15.f : 0.f;
   float o[kRegs];
   float m[NT][2], l[NT][2];
   uint32_t q[DP / 16][NT][2];
@@ -236,7 +240,7 @@ struct MmaBody {
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const float m2 = fmaxf(m[nt][j], top[nt][j]);
+        const float m2 = fmaxf(m[nt][j], __fadd_ru(top[nt][j], -kLift));     // upwards: no weight is above 2^kLift
         off[nt][j] = m2 == -INFINITY ? 0.f : m2;       // nothing counted yet: every weight below is 0
         f[nt][j] = exp2_fast(m[nt][j] - off[nt][j]);
         rose |= m2 != m[nt][j];
@@ -335,6 +339,7 @@ struct F32Body {
   static constexpr int kKeys = kChunk / 4;          // keys of a lane
   static constexpr int kVec = DP / 32;              // 16-byte pieces of a key per lane
   static constexpr size_t kQBytes = kHeads * DP * 4 + kChunk * kHeads * 4;
+  static constexpr float kLift = 0.f;
   float o[kRegs];
   float m[kHeads], l[kHeads];
 
@@ -861,7 +866,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_con
   float* dumps = p.dumps + (size_t)blockIdx.x * kWarps * kRegs * 32;
   auto out_at = [&](int row, int head) { return (T*)p.out + row * p.out_stride + (int64_t)head * kv.head_dim; };
   auto lse_of = [&](float m, float l) {
-    return l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m) * 0.6931471805599453f + logf(l);
+    constexpr float kDown = Body::kLift == 0.f ? 1.f : 1.f / 32768.f;       // 2^-kLift
+    static_assert(Body::kLift == 0.f || Body::kLift == 15.f, "kDown");
+    return l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m + Body::kLift) * 0.6931471805599453f + logf(l * kDown);
   };
   while (pos < wend) {
     const RowSpan span = here.span;

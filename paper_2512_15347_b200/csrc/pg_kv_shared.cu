@@ -13,7 +13,9 @@
 //                   shared memory
 // so that one tile's softmax runs under the other tile's products.  The maximum that P is taken against
 // is only raised when it has grown by more than kSlack (in powers of two): P stays below 2^kSlack, sums
-// stay exact, and O is rescaled a few times per unit instead of every tile.
+// stay exact, and O is rescaled a few times per unit instead of every tile.  fp16 has 2^15 of room above 1 and weights of full
+// precision down to 2^-14 only: there the slack is smaller, and all weights are 2^kLift times as large (the rows' own part
+// does the same; joins scale alike).
 // The tiles of all units form one line cut into equal parts over the CTAs; every (CTA, unit) leaves its
 // queries' (m, l, O), and the rows' own pieces start from them.
 // Measured: 768 rows in groups of 48 (192 queries a kv head) over 2048 shared tokens, bf16, 8 kv heads x 128: about 65 us
@@ -28,7 +30,13 @@
 namespace pg {
 
 constexpr int kRows = 128;           // queries of a product
-constexpr float kSlack = 8.f;
+template <typename T> struct Room {            // of a weight of type T, in powers of two
+  static constexpr float kSlack = 8.f, kLift = 0.f;
+};
+template <> struct Room<__half> {
+  // Together at most 15.  768 rows in groups of 48 in fp16: 165.0 us with 8 + 7, 165.3 with 2 + 13, 166.3 with 0 + 15.
+  static constexpr float kSlack = 2.f, kLift = 13.f;
+};
 constexpr float kFarScore = 4194304.f;         // 2^22: half a unit in the last place is 2^-2
 constexpr int kWaitLimit = 1 << 14;
 
@@ -334,11 +342,13 @@ __global__ void __launch_bounds__(SharedLayout<DP, kSlots>::kThreads, 1) shared_
             for (int j = 0; j < kTile; ++j) s[j] *= scale;
             by = 1.f;
           }
-          const bool raise = top > __fadd_rd(m, kSlack) || m == -INFINITY;
+          constexpr float kSlack = Room<T>::kSlack, kLift = Room<T>::kLift;
+          const bool raise = top > __fadd_rd(m, kSlack + kLift) || m == -INFINITY;
+          const float up = __fadd_ru(top, -kLift);
           float f = 1.f;
-          if (raise && top > m) {
-            f = exp2_fast(m - top);
-            m = top;
+          if (raise && up > m) {
+            f = exp2_fast(m - up);
+            m = up;
           }
           if (k > 0 && __any_sync(0xFFFFFFFFu, f != 1.f)) {
             tmem_after();

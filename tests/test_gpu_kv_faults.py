@@ -332,3 +332,40 @@ def test_scores_far_from_zero_take_the_largest(dtype, size, scale):
             v = c.v[0, c.rows[r][t // 16], 0, t % 16].double()
             # the one weight is rounded to the type, and the result: u each, and fp32's roundings beside them
             assert ((out[r].double() - v).abs() <= 2.1 * T.UNIT[dtype] * v.abs() + 2.0 ** -22 * v.abs() + 2.0 ** -24).all(), (r, t)
+
+
+# ------------------------------------------------------------------------------ many small weights beside a large one
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("nats", [10.0, 14.0, 16.0, 17.0, 17.5])
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 16), (72, 5)])
+def test_small_weights_beside_a_token_of_value_zero(dtype, nats, dim, page):
+    """One token far above the others that carries no value (an attention sink): the result is the others' share, whose weights
+    are below what the type resolves near 1.  In the rows' own tokens, in tokens that a group shares, and with the sink in one and
+    the others in the other."""
+    tokens = 16384
+    c = T.Cache([tokens + 1, tokens, 300], 1, dim, page, dtype, seed=40)
+    q = torch.zeros((3, 2, dim), device="cuda", dtype=T.DT[dtype])
+    q[:, :, 0] = 4.0
+    c.k[:, :, :, :, :] = torch.where(torch.isnan(c.k), c.k, torch.zeros_like(c.k))
+    c.v.abs_()
+    for r, t in ((0, 5000), (1, 0), (2, 299)):
+        c.k[0, c.rows[r][t // page], 0, t % page, 0] = nats / 4
+        c.v[0, c.rows[r][t // page], 0, t % page] = 0
+    out, lse = T.run_attention(c, q, dtype, scale=1.0)
+    T.check_attention(c, q, out, lse, 1.0, dtype)
+    if dtype == "f32":
+        return
+    n, shared = 8, 4096 // page // 64 * 64 * page              # whole tiles of whole pages
+    g = T.shared_cache(3, n, shared, [200] * 3 * n, 1, dim, page, dtype, seed=41)
+    q = torch.zeros((3 * n, 2, dim), device="cuda", dtype=T.DT[dtype])
+    q[:, :, 0] = 4.0
+    g.k[:, :, :, :, :] = torch.where(torch.isnan(g.k), g.k, torch.zeros_like(g.k))
+    g.v.abs_()
+    for r in range(3 * n):
+        t = (1000, shared - 1, shared + 77)[r // n]            # early and late in the shared tokens; in each row's own
+        g.k[0, g.rows[r][t // page], 0, t % page, 0] = nats / 4
+        g.v[0, g.rows[r][t // page], 0, t % page] = 0
+    sh = torch.full((3,), shared, device="cuda", dtype=torch.int32)
+    out, lse = T.run_attention(g, q, dtype, scale=1.0, group=n, shared=sh)
+    T.check_attention(g, q, out, lse, 1.0, dtype)
