@@ -14,23 +14,24 @@ namespace pg {
 constexpr int kScanThreads = 1024;          // of the kernels that are one CTA
 
 // Exclusive prefix sum over the CTA; *total gets the sum.  All threads call.
-__device__ __forceinline__ int block_scan(int v, int* total) {
-  __shared__ int warp_sums[kScanThreads / 32 + 1];
+template <typename Int>
+__device__ __forceinline__ Int block_scan(Int v, Int* total) {
+  __shared__ Int warp_sums[kScanThreads / 32 + 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int x = v;
+  Int x = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+    const Int y = __shfl_up_sync(0xFFFFFFFFu, x, o);
     if (lane >= o) x += y;
   }
   __syncthreads();                       // the previous call's readers are done
   if (lane == 31) warp_sums[warp] = x;
   __syncthreads();
   if (warp == 0) {
-    int s = lane < (int)(blockDim.x >> 5) ? warp_sums[lane] : 0;
+    Int s = lane < (int)(blockDim.x >> 5) ? warp_sums[lane] : 0;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xFFFFFFFFu, s, o);
+      const Int y = __shfl_up_sync(0xFFFFFFFFu, s, o);
       if (lane >= o) s += y;
     }
     warp_sums[lane] = s;
@@ -431,9 +432,10 @@ struct ExtendParams {
   int n_uniform;
 };
 
-// One CTA.  Rows in chunks of 1024: pages wanted, their prefix, then the free pages in order.
+// One CTA.  Rows in chunks of 1024: pages wanted, their prefix, then the free pages in order.  1024 rows may want more
+// than 2^31 pages together, so the prefix has 64 bits; past what the pool has it only says "none".
 __global__ void __launch_bounds__(kScanThreads) extend_kernel(const __grid_constant__ ExtendParams p) {
-  __shared__ int first[kScanThreads + 1];       // pages handed to the chunk's rows before this one
+  __shared__ int first[kScanThreads];           // pages handed to the chunk's rows before this one
   __shared__ int have[kScanThreads];
   const KvView& kv = p.kv;
   const int most = kv.max_pages * kv.page_size;
@@ -449,15 +451,14 @@ __global__ void __launch_bounds__(kScanThreads) extend_kernel(const __grid_const
       old_pages = (n + kv.page_size - 1) / kv.page_size;
       want = (n + add + kv.page_size - 1) / kv.page_size - old_pages;
     }
-    int total;
-    const int before = block_scan(want, &total);
-    first[threadIdx.x] = before;
+    long long total;
+    const long long before = block_scan((long long)want, &total);
+    first[threadIdx.x] = (int)min(before, 0x7FFFFFFFll);
     have[threadIdx.x] = old_pages;
-    if (threadIdx.x == 0) first[kScanThreads] = total;
     __syncthreads();
     int found = 0;
     if (total && !dry)
-      found = take_free(p.refs, kv.n_pages, total, [&](int k, int page) {
+      found = take_free(p.refs, kv.n_pages, (int)min(total, (long long)kv.n_pages), [&](int k, int page) {
         int lo = 0, hi = kScanThreads - 1;                 // last row with first[row] <= k
         while (lo < hi) {
           const int mid = (lo + hi + 1) >> 1;
@@ -472,7 +473,7 @@ __global__ void __launch_bounds__(kScanThreads) extend_kernel(const __grid_const
     if (r < kv.n_rows) {
       const bool grown = fits && !late;
       if (!grown)                                      // the one row that got some of its pages gives them back
-        for (int j = 0; j < min(want, found - before); ++j) p.refs[kv.table[(int64_t)r * kv.max_pages + old_pages + j]] = 0;
+        for (int j = 0; j < min((long long)want, found - before); ++j) p.refs[kv.table[(int64_t)r * kv.max_pages + old_pages + j]] = 0;
       if (!grown && add) flag(kv.status, kStatusPages);
       p.len_out[r] = grown ? n + add : n;
       if (kv.grown) kv.grown[r] = grown ? add : 0;

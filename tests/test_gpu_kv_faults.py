@@ -299,6 +299,26 @@ def test_driver_wants_room_before_new_tokens():
     c.check()
 
 
+# ------------------------------------------------------------------------------ sizes near the ends of their types
+
+@pytest.mark.parametrize("first", [0, 5])
+def test_extend_by_more_pages_than_32_bits_count(first):
+    """1024 rows that want 2^21 pages each, all at once, from a pool of a few: a row that fits, the rest refused, nothing handed out twice."""
+    rows, width, pages = 1024, 1 << 21, 64
+    k = torch.zeros((1, pages, 1, 1, 8), device="cuda", dtype=torch.bfloat16)
+    table = torch.full((rows, width), -1, device="cuda", dtype=torch.int32)          # 8 GB
+    length, refs, st = torch.zeros(rows, device="cuda", dtype=torch.int32), torch.zeros(pages, device="cuda", dtype=torch.int32), T.status_word()
+    n_new = torch.full((rows,), width, device="cuda", dtype=torch.int32)
+    n_new[0] = first
+    grown = torch.full((rows,), 77, device="cuda", dtype=torch.int32)
+    kv = B.make_kv(k, k.clone(), table, length, grown)
+    B.kv_extend(kv, n_new, length, refs, refs, status=st)
+    assert int(st) == 8
+    assert length.tolist() == [first] + [0] * (rows - 1) and grown.tolist() == length.tolist()
+    assert refs.tolist() == [1] * first + [0] * (pages - first)
+    assert table[0, :first].tolist() == list(range(first))
+
+
 # ------------------------------------------------------------------------------ scores far from zero
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
