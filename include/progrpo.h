@@ -491,6 +491,7 @@ typedef struct {
                               pages of the layers are interleaved without overlapping)             */
   int32_t *table;          /* [n_rows, max_pages] int32; entries past a row's last page are not read */
   const int32_t *len;      /* [n_rows] int32: tokens of each row, 0..max_pages * page_size          */
+  /* n_rows and n_pages up to 2^31 - 2^20, (max_pages + 1) * page_size up to 2^31 - 4096 */
   int32_t n_rows, max_pages;
   int32_t *grown;          /* [n_rows] int32 or NULL: how many tokens pg_kv_extend has last found room for in each row
                               (0 where it found none).  pg_kv_extend writes it; pg_kv_attend and pg_kv_append leave

@@ -29,6 +29,9 @@ struct KvView {
   int n_layers, n_pages, n_kv_heads, page_size, head_dim, n_rows, max_pages;
 };
 
+// Rows and pages of a cache, rows of a fork: a loop over as many in steps of a CTA still ends inside 32 bits.
+constexpr int32_t kMostItems = 0x7FF00000;
+
 // Checks that need no device access.  The product of all sizes must stay addressable in 63 bits.
 inline int kv_check(const pg_kv* c) {
   if (!c) return PG_EINVAL;
@@ -36,7 +39,8 @@ inline int kv_check(const pg_kv* c) {
   if (c->n_layers < 1 || c->n_pages < 1 || c->n_kv_heads < 1 || c->page_size < 1) return PG_EINVAL;
   if (c->head_dim < 8 || c->head_dim > 256 || (c->head_dim & 7)) return PG_EINVAL;
   if (c->n_rows < 0 || c->max_pages < 1) return PG_EINVAL;
-  if ((int64_t)c->max_pages * c->page_size > 0x7FFFFFFFLL - 4096) return PG_EINVAL;
+  if (c->n_rows > kMostItems || c->n_pages > kMostItems) return PG_EINVAL;
+  if (((int64_t)c->max_pages + 1) * c->page_size > 0x80000000LL - 4096) return PG_EINVAL;   // a length rounded up to a page fits
   const int64_t head = (int64_t)c->page_size * c->head_dim;
   if (head > ((int64_t)1 << 40) / c->n_kv_heads) return PG_EINVAL;
   if (c->page_stride < head * c->n_kv_heads || (c->page_stride & 7)) return PG_EINVAL;

@@ -152,6 +152,13 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_c
   }
 }
 
+// CTA-sized pieces of a page of one layer; 0 if a copy in all layers would have more of them than 32 bits count.
+static int copy_pieces(const pg_kv* kv) {
+  const int64_t words = (int64_t)kv->n_kv_heads * kv->page_size * kv->head_dim * (int64_t)dtype_bytes(kv->dtype) / 16;
+  const int64_t pieces = (words + kCopyWords - 1) / kCopyWords;
+  return pieces > 0x7FFFFFFFLL / 2 / kv->n_layers ? 0 : (int)pieces;
+}
+
 static int launch_copy(const pg_kv* kv, const KvView& view, const int2* pairs, const int32_t* n_pairs, int64_t most, int run,
                        const int32_t* to, int32_t* table_out, cudaStream_t st) {
   const int64_t b = (int64_t)dtype_bytes(kv->dtype);
@@ -162,8 +169,7 @@ static int launch_copy(const pg_kv* kv, const KvView& view, const int2* pairs, c
   p.page_words = (int64_t)kv->n_kv_heads * kv->page_size * kv->head_dim * b / 16;
   p.stride_words = kv->page_stride * b / 16;
   p.layer_words = view.layer_stride * b / 16;
-  const int64_t pieces = (p.page_words + kCopyWords - 1) / kCopyWords;
-  if (pieces * kv->n_layers * 2 > 0x7FFFFFFFLL) return PG_EINVAL;
+  const int64_t pieces = copy_pieces(kv);
   p.pieces = (int)pieces;
   p.run = run;
   p.to = to;
@@ -572,7 +578,7 @@ static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 extern "C" {
 
 size_t pg_kv_fork_workspace_bytes(const pg_kv* kv, int32_t n_out) {
-  if (pg::kv_check(kv) != PG_OK || n_out < 0) return 0;
+  if (pg::kv_check(kv) != PG_OK || n_out < 0 || n_out > pg::kMostItems || pg::copy_pieces(kv) == 0) return 0;
   return pg::fork_work(nullptr, n_out, nullptr);
 }
 
@@ -581,7 +587,7 @@ int pg_kv_fork(const pg_kv* kv, int32_t n_out, const int32_t* src_rows, int32_t*
                void* stream) {
   const int rc = pg::kv_check(kv);
   if (rc != PG_OK) return rc;
-  if (n_out < 0 || !refs || !refs_out) return PG_EINVAL;
+  if (n_out < 0 || n_out > pg::kMostItems || pg::copy_pieces(kv) == 0 || !refs || !refs_out) return PG_EINVAL;
   if (n_out > 0 && (!src_rows || !table_out || !len_out)) return PG_EINVAL;
   if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < pg_kv_fork_workspace_bytes(kv, n_out)) return PG_EINVAL;
   if ((int64_t)kv->n_rows + n_out > 0x7FFFFFFFLL) return PG_EINVAL;
@@ -606,7 +612,7 @@ int pg_kv_fork(const pg_kv* kv, int32_t n_out, const int32_t* src_rows, int32_t*
 }
 
 size_t pg_kv_pack_workspace_bytes(const pg_kv* kv) {
-  if (pg::kv_check(kv) != PG_OK) return 0;
+  if (pg::kv_check(kv) != PG_OK || pg::copy_pieces(kv) == 0) return 0;
   return pg::pack_work(nullptr, kv->n_pages, nullptr);
 }
 
@@ -614,7 +620,7 @@ int pg_kv_pack(const pg_kv* kv, const int32_t* refs, int32_t* refs_out, int32_t*
                void* workspace, size_t workspace_bytes, int32_t* status, void* stream) {
   const int rc = pg::kv_check(kv);
   if (rc != PG_OK) return rc;
-  if (!refs || !refs_out || (kv->n_rows > 0 && !table_out)) return PG_EINVAL;
+  if (pg::copy_pieces(kv) == 0 || !refs || !refs_out || (kv->n_rows > 0 && !table_out)) return PG_EINVAL;
   if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < pg_kv_pack_workspace_bytes(kv)) return PG_EINVAL;
   const size_t t = (size_t)kv->n_rows * kv->max_pages * 4;
   if (kv->n_rows > 0 && table_out != kv->table && pg::overlap(table_out, t, kv->table, t)) return PG_EINVAL;
