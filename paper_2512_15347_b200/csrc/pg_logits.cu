@@ -101,7 +101,7 @@ logits_kernel(const __grid_constant__ LogitsParams p) {
   // Units of eight tokens lie on 16-byte boundaries of the row's memory: the first begins `lead` tokens before it.
   const int lead = (int)(((uintptr_t)in & 15) / sizeof(In));
   const int begin = (blockIdx.x - row * p.parts) * p.part - lead;      // the part's first unit, may be negative
-  const int lo = max(begin, 0), hi = min(begin + p.part, p.vocab);
+  const int lo = max(begin, 0), hi = (int)min((int64_t)begin + p.part, (int64_t)p.vocab);
   if (lo >= hi) return;
   const bool out_aligned = (((uintptr_t)(out - lead)) & 15) == 0;
   const uint32_t* mask = r.mask ? r.mask + row * r.mask_stride : nullptr;

@@ -319,6 +319,14 @@ def test_extend_by_more_pages_than_32_bits_count(first):
     assert table[0, :first].tolist() == list(range(first))
 
 
+def test_logits_of_the_longest_row():
+    """The end of the last part passes 2^31."""
+    x = torch.ones((1, 0x7FFF0000), device="cuda", dtype=torch.bfloat16)
+    x[0, -1] = 3.0
+    B.logits_process(x, x, B.make_logits_rules(temperature=torch.full((1,), 0.5, device="cuda")))
+    assert x[0, -1] == 6.0 and bool((x[0, :-1] == 2.0).all())
+
+
 # ------------------------------------------------------------------------------ scores far from zero
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
