@@ -309,7 +309,11 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const __grid_constan
       const int n = x.y >= 0 ? length[x.y] : 0, pages = (n + kv.page_size - 1) / kv.page_size;
       const int32_t* from = kv.table + (int64_t)(s0 + max(x.y, 0)) * kv.max_pages;
       int32_t* to = p.table_out + (int64_t)x.x * kv.max_pages;
-      for (int j = lane; j < kv.max_pages; j += 32) to[j] = j < pages ? from[j] : -1;
+      for (int j = lane; j < kv.max_pages; j += 32) {
+        const int page = j < pages ? from[j] : -1;
+        if (j < pages && (unsigned int)page >= (unsigned int)kv.n_pages) flag(kv.status, kStatusIndex);
+        to[j] = page;
+      }
       bool need = false;
       if (x.y >= 0 && n % kv.page_size != 0) {
         need = forks[x.y] > 0;                        // of earlier batches

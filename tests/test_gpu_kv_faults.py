@@ -109,6 +109,22 @@ def test_waits_are_named_or_refused():
     B.selftest_token_waits()
 
 
+@pytest.mark.parametrize("src", [[0, 1, 2], [2, 1], [1, 1, 0], [0, 2], []])
+@pytest.mark.parametrize("bad", [-1, 10 ** 6, 2 ** 31 - 1])
+def test_fork_reports_a_bad_page_whatever_becomes_of_its_row(src, bad):
+    """Kept by one fork (its counts do not change), by several, or dropped; also in the partly filled last page."""
+    for at in (0, 2):
+        c = T.Cache([40, 40, 16], 1, 8, 16, "f32", spare=9, seed=45)
+        c.table[1, at] = bad
+        st, n = T.status_word(), len(src)
+        ws = torch.zeros(B.kv_fork_workspace_bytes(c.kv, n), device="cuda", dtype=torch.uint8)
+        t, l = torch.empty((n, c.width), device="cuda", dtype=torch.int32), torch.empty(n, device="cuda", dtype=torch.int32)
+        B.kv_fork(c.kv, torch.tensor(src, device="cuda", dtype=torch.int32), t, l, c.refs, c.refs, ws, status=st)
+        with pytest.raises(B.PgError) as e:
+            B.kv_status(st)
+        assert e.value.code == B.EINDEX
+
+
 # ------------------------------------------------------------------------------ one buffer for all calls
 
 def test_one_workspace_for_calls_of_every_kind():
