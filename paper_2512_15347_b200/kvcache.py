@@ -16,7 +16,10 @@ class PagedCache:
     """A paged cache of up to ``max_rows`` rows of up to ``max_tokens`` tokens on the current device.
 
     Rows are group-major, as everywhere in the library; after ``fork`` with a fan-out the cache knows
-    how many tokens a group's rows have in common, and attention reads those once per group."""
+    how many tokens a group's rows have in common, and attention reads those once per group.
+
+    Calls run on the current stream.  The workspaces are the stream's own, so calls on several streams may overlap;
+    the pool, the tables and the lengths are one, and who changes them while another stream reads them orders the two."""
 
     def __init__(self, n_pages: int, page_size: int, n_layers: int, n_kv_heads: int, head_dim: int, max_rows: int,
                  max_tokens: int, dtype: torch.dtype = torch.bfloat16):
@@ -34,7 +37,7 @@ class PagedCache:
         self.refs = torch.zeros(n_pages, device=dev, dtype=torch.int32)
         self.status = torch.zeros(1, device=dev, dtype=torch.int32)
         self.group, self.shared = 1, None
-        self._spaces = {}
+        self._spaces, self._in_graphs = {}, {}
         self.n_rows = 0
 
     def _describe(self):
@@ -59,15 +62,23 @@ class PagedCache:
     def len(self) -> torch.Tensor:
         return self._lens[self._cur][: self._n_rows]
 
-    def _space(self, name: str, nbytes: int) -> torch.Tensor:
-        """A zeroed workspace of its own for every call, grown when a call asks for more."""
-        if name not in self._spaces or self._spaces[name].nbytes < nbytes:
-            self._spaces[name] = torch.zeros(nbytes, device=self.dev, dtype=torch.uint8)
-        return self._spaces[name]
+    def _space(self, nbytes: int) -> torch.Tensor:
+        """The current stream's workspace, zeroed when it is made and grown when a call asks for more.  Calls on two streams may
+        overlap, so each stream has its own.  A graph under capture whose stream has none yet gets one that only the graph knows,
+        since what zeroes it runs at the replay; one that a graph has been given is kept when the stream's grows."""
+        stream, capturing = B._stream(None), torch.cuda.is_current_stream_capturing()
+        space = self._spaces.get(stream)
+        if space is None or space.nbytes < nbytes:
+            space = torch.zeros(nbytes, device=self.dev, dtype=torch.uint8)
+            if not capturing:
+                self._spaces[stream] = space
+        elif capturing:
+            self._in_graphs[space.data_ptr()] = space
+        return space
 
     def admit(self, n_rows: int) -> None:
         """Starts over with n_rows empty rows; whatever the cache held is released."""
-        B.kv_fork(self.kv, None, None, None, self.refs, self.refs, self._space("fork", B.kv_fork_workspace_bytes(self.kv, 0)),
+        B.kv_fork(self.kv, None, None, None, self.refs, self.refs, self._space(B.kv_fork_workspace_bytes(self.kv, 0)),
                   status=self.status)
         self._lens[self._cur].zero_()
         self._extended = False
@@ -95,7 +106,7 @@ class PagedCache:
         if k_new is not None:
             self._want_room()
         out = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
-        ws = self._space("attend", B.kv_attend_workspace_bytes(self.kv, q.shape[1], self.group))
+        ws = self._space(B.kv_attend_workspace_bytes(self.kv, q.shape[1], self.group))
         B.kv_attend(self.kv, layer, q, out, ws, k_new=k_new, v_new=v_new, lse=lse, scale=scale, group=self.group, shared=self.shared,
                     status=self.status)
         return out
@@ -106,7 +117,7 @@ class PagedCache:
             raise ValueError(f"{n} rows in a cache of {self.max_rows}")
         other = self._cur ^ 1
         B.kv_fork(self.kv, src_rows, self._tables[other][:n], self._lens[other][:n], self.refs, self.refs,
-                  self._space("fork", B.kv_fork_workspace_bytes(self.kv, n)), status=self.status)
+                  self._space(B.kv_fork_workspace_bytes(self.kv, n)), status=self.status)
         self._cur = other
         self._extended = False
         self.n_rows = n
@@ -127,7 +138,7 @@ class PagedCache:
 
     def pack(self) -> None:
         """Moves the pages in use to the front of the pool."""
-        B.kv_pack(self.kv, self.refs, self.refs, self.table, self._space("pack", B.kv_pack_workspace_bytes(self.kv)), status=self.status)
+        B.kv_pack(self.kv, self.refs, self.refs, self.table, self._space(B.kv_pack_workspace_bytes(self.kv)), status=self.status)
 
     def check(self) -> None:
         """Raises PgError if a call has flagged a bad index, a full table or an exhausted pool; synchronises."""

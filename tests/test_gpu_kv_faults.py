@@ -413,3 +413,85 @@ def test_small_weights_beside_a_token_of_value_zero(dtype, nats, dim, page):
     sh = torch.full((3,), shared, device="cuda", dtype=torch.int32)
     out, lse = T.run_attention(g, q, dtype, scale=1.0, group=n, shared=sh)
     T.check_attention(g, q, out, lse, 1.0, dtype)
+
+
+# ------------------------------------------------------------------------------ the driver's streams
+
+def driver(tokens, rows=3):
+    from paper_2512_15347_b200.kvcache import PagedCache
+    c = PagedCache(rows * -(-tokens // 16) + 4, 16, 1, 2, 64, rows, tokens + 40)
+    c.admit(rows)
+    c.extend(tokens)
+    kn = torch.randn((rows * tokens, 2, 64), generator=T.gen(8), device="cuda").bfloat16()
+    c.append(0, kn, kn.flip(0).contiguous(), torch.arange(rows + 1, device="cuda", dtype=torch.int32) * tokens)
+    return c
+
+
+def test_driver_calls_on_two_streams_share_no_workspace():
+    c = driver(5000)
+    qs = [T.queries(3, 8, 64, "bf16", seed=s) for s in range(6)]
+    good = [c.attend(0, q) for q in qs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    here = c._space(1)
+    with torch.cuda.stream(side):
+        c.attend(0, qs[0])
+        there = c._space(1)
+    assert here.data_ptr() != there.data_ptr()
+    torch.cuda.synchronize()
+    outs = [torch.empty_like(q) for q in qs]
+    for _ in range(5):
+        for i, q in enumerate(qs):                             # calls that overlap
+            with torch.cuda.stream(side if i % 2 else torch.cuda.current_stream()):
+                c.attend(0, q, out=outs[i])
+        torch.cuda.synchronize()
+        for a, b in zip(outs, good):
+            assert torch.equal(a, b)
+
+
+def test_driver_workspace_made_under_capture_stays_with_the_graph():
+    """What zeroes it runs at the replay, not when it is made: a call outside the graph must not find it."""
+    c = driver(5000)
+    q = T.queries(3, 8, 64, "bf16")
+    good = c.attend(0, q)
+    c._spaces.clear()                                          # as before any call
+    side, out = torch.cuda.Stream(), torch.empty_like(q)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        c.attend(0, q, out=out)
+    assert not c._spaces
+    with torch.cuda.stream(side):
+        again = c.attend(0, q)
+    torch.cuda.synchronize()
+    assert torch.equal(again, good)
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, good)
+
+
+def test_driver_workspace_that_a_graph_uses_outlives_growth():
+    c = driver(5000)
+    q = T.queries(3, 8, 64, "bf16")
+    side, out = torch.cuda.Stream(), torch.empty_like(q)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        good = c.attend(0, q)
+        used = c._space(1).data_ptr()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        c.attend(0, q, out=out)
+    with torch.cuda.stream(side):
+        grown = c._space(1 << 30)
+        assert grown.data_ptr() != used and c._space(1) is grown
+        taken = [torch.full((1 << 20,), 255, device="cuda", dtype=torch.uint8) for _ in range(64)]
+        assert all(not t.data_ptr() <= used < t.data_ptr() + t.nbytes for t in taken)
+    torch.cuda.synchronize()
+    for _ in range(2):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, good)
