@@ -78,6 +78,8 @@ class PagedCache:
 
     def admit(self, n_rows: int) -> None:
         """Starts over with n_rows empty rows; whatever the cache held is released."""
+        if not 0 <= n_rows <= self.max_rows:
+            raise ValueError(f"{n_rows} rows in a cache of {self.max_rows}")
         B.kv_fork(self.kv, None, None, None, self.refs, self.refs, self._space(B.kv_fork_workspace_bytes(self.kv, 0)),
                   status=self.status)
         self._lens[self._cur].zero_()
@@ -124,6 +126,8 @@ class PagedCache:
 
     def expand(self, fan: int) -> None:
         """Every row becomes a group of ``fan`` rows that share its full pages."""
+        if fan < 1:
+            raise ValueError("fan: at least one row of each")
         shared = torch.div(self.len, self.page_size, rounding_mode="floor") * self.page_size
         self._fork(torch.arange(self.n_rows, device=self.dev, dtype=torch.int32).repeat_interleave(fan))
         self.group, self.shared = fan, shared.to(torch.int32)
@@ -131,7 +135,7 @@ class PagedCache:
     def prune(self, src_rows, keep: int) -> None:
         """Keeps the rows that a prune has kept (pg_prune_ovf's src_rows: ``keep`` per group, group-major)
         and frees the pages of the others."""
-        if src_rows.numel() * self.group != self.n_rows * keep:
+        if keep < 1 or src_rows.numel() * self.group != self.n_rows * keep:
             raise ValueError("src_rows: `keep` rows of every group")
         self._fork(src_rows)
         self.group = keep

@@ -495,3 +495,16 @@ def test_driver_workspace_that_a_graph_uses_outlives_growth():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, good)
+
+
+def test_driver_refuses_before_it_changes_anything():
+    c = driver(100)
+    q = T.queries(3, 8, 64, "bf16")
+    good, refs = c.attend(0, q), c.refs.clone()
+    for refused in (lambda: c.admit(4), lambda: c.admit(-1), lambda: c.expand(0), lambda: c.expand(-2), lambda: c.expand(2),
+                    lambda: c.prune(torch.zeros(0, device="cuda", dtype=torch.int32), 0)):
+        with pytest.raises(ValueError):
+            refused()
+        assert c.n_rows == 3 and c.group == 1 and c.len.tolist() == [100] * 3 and torch.equal(c.refs, refs)
+        assert torch.equal(c.attend(0, q), good)
+    c.check()
