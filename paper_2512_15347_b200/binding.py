@@ -642,6 +642,7 @@ def make_logits_rules(*, tokens=None, n_tokens=None, n_prompt=None, repetition=N
         r.tokens, r.token_stride, r.max_tokens = tokens.data_ptr(), tokens.stride(0), tokens.shape[1]
     for name, t in (("n_tokens", n_tokens), ("n_prompt", n_prompt)):
         if t is not None:
+            _want(t.dim() >= 1 and t.numel() == t.shape[0], f"{name}: [rows] int32")
             see(t, name)
             setattr(r, name, _i32(t, name))
     for name, t in (("repetition", repetition), ("presence", presence), ("frequency", frequency), ("temperature", temperature)):
@@ -649,6 +650,7 @@ def make_logits_rules(*, tokens=None, n_tokens=None, n_prompt=None, repetition=N
             _want(t.dtype == torch.float32 and t.dim() == 1 and t.is_contiguous(), f"{name}: [rows] fp32")
             see(t, name)
             setattr(r, name, t.data_ptr())
+    _want(bias_ids is None or bias_ids.dim() == 2, "bias_ids: [rows, n] int32")
     if bias_ids is not None and bias_ids.shape[1] > 0:
         _want(bias_values is not None and bias_values.shape == bias_ids.shape and bias_values.dtype == torch.float32 and
               bias_values.is_contiguous(), "bias_values: fp32, shaped like bias_ids")

@@ -508,3 +508,13 @@ def test_driver_refuses_before_it_changes_anything():
         assert c.n_rows == 3 and c.group == 1 and c.len.tolist() == [100] * 3 and torch.equal(c.refs, refs)
         assert torch.equal(c.attend(0, q), good)
     c.check()
+
+
+def test_rules_of_another_shape_are_refused():
+    i32 = dict(device="cuda", dtype=torch.int32)
+    for rules in (dict(n_tokens=torch.zeros((2, 3), **i32)), dict(n_prompt=torch.zeros((2, 2), **i32)), dict(n_tokens=torch.zeros((), **i32)),
+                  dict(bias_ids=torch.zeros(2, **i32), bias_values=torch.zeros(2, device="cuda")),
+                  dict(bias_ids=torch.zeros((2, 1, 1), **i32), bias_values=torch.zeros((2, 1, 1), device="cuda"))):
+        with pytest.raises(ValueError):
+            B.make_logits_rules(tokens=torch.zeros((2, 4), **i32), **rules)
+    B.make_logits_rules(tokens=torch.zeros((2, 4), **i32), n_tokens=torch.zeros((2, 1), **i32))
