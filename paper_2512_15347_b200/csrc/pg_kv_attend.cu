@@ -23,6 +23,7 @@
 // of 1..8192 tokens 81 us (4.4 TB/s).  Bound now: the former by HBM and the join of the 18 parts of a piece, the
 // latter by the instructions of a warp around its chunks (two warps a scheduler, 0.24 issued a cycle).
 #include "pg_kv_attend.cuh"
+#include "pg_trace.cuh"
 
 #include <cuda.h>
 
@@ -1162,6 +1163,7 @@ int pg_kv_attend(const pg_kv* kv, int32_t layer, int32_t n_q_heads, const void* 
                  const void* k_new, const void* v_new, int64_t new_stride, float scale, int32_t group,
                  const int32_t* shared, void* out, int64_t out_stride, float* lse, void* workspace,
                  size_t workspace_bytes, int32_t* status, void* stream) {
+  pg::TraceRange trace_range("pg_kv_attend");
   const int rc = pg::attend_check(kv, n_q_heads, group);
   if (rc != PG_OK) return rc;
   if (layer < 0 || layer >= kv->n_layers || !(scale == scale) || (!k_new != !v_new)) return PG_EINVAL;

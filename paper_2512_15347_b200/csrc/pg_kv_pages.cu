@@ -5,6 +5,7 @@
 // does not depend on their order, and free pages are always taken lowest first through a scan of the
 // counts, so that tables, counts and pools come out the same on every run.
 #include "pg_kv.cuh"
+#include "pg_trace.cuh"
 
 #include <algorithm>
 
@@ -589,6 +590,7 @@ size_t pg_kv_fork_workspace_bytes(const pg_kv* kv, int32_t n_out) {
 int pg_kv_fork(const pg_kv* kv, int32_t n_out, const int32_t* src_rows, int32_t* table_out, int32_t* len_out,
                const int32_t* refs, int32_t* refs_out, void* workspace, size_t workspace_bytes, int32_t* status,
                void* stream) {
+  pg::TraceRange trace_range("pg_kv_fork");
   const int rc = pg::kv_check(kv);
   if (rc != PG_OK) return rc;
   if (n_out < 0 || n_out > pg::kMostItems || pg::copy_pieces(kv) == 0 || !refs || !refs_out) return PG_EINVAL;
@@ -622,6 +624,7 @@ size_t pg_kv_pack_workspace_bytes(const pg_kv* kv) {
 
 int pg_kv_pack(const pg_kv* kv, const int32_t* refs, int32_t* refs_out, int32_t* table_out, int32_t* page_map,
                void* workspace, size_t workspace_bytes, int32_t* status, void* stream) {
+  pg::TraceRange trace_range("pg_kv_pack");
   const int rc = pg::kv_check(kv);
   if (rc != PG_OK) return rc;
   if (pg::copy_pieces(kv) == 0 || !refs || !refs_out || (kv->n_rows > 0 && !table_out)) return PG_EINVAL;
@@ -643,6 +646,7 @@ int pg_kv_pack(const pg_kv* kv, const int32_t* refs, int32_t* refs_out, int32_t*
 
 int pg_kv_extend(const pg_kv* kv, const int32_t* n_new, int32_t n_uniform, int32_t* len_out, const int32_t* refs,
                  int32_t* refs_out, int32_t* status, void* stream) {
+  pg::TraceRange trace_range("pg_kv_extend");
   const int rc = pg::kv_check(kv);
   if (rc != PG_OK) return rc;
   if ((!n_new && n_uniform < 0) || !refs || !refs_out || (kv->n_rows > 0 && !len_out)) return PG_EINVAL;
@@ -659,6 +663,7 @@ int pg_kv_extend(const pg_kv* kv, const int32_t* n_new, int32_t n_uniform, int32
 
 int pg_kv_append(const pg_kv* kv, int32_t layer, int32_t n_tokens, const void* k_new, const void* v_new,
                  int64_t new_stride, const int32_t* start, int32_t* status, void* stream) {
+  pg::TraceRange trace_range("pg_kv_append");
   const int rc = pg::kv_check(kv);
   if (rc != PG_OK) return rc;
   if (layer < 0 || layer >= kv->n_layers || n_tokens < 0) return PG_EINVAL;

@@ -12,6 +12,7 @@
 // (a word or a bit per token of the part) took twice the time of the stream in instructions and barriers.
 // Every part scans the row's whole history, so parts are as long as the number of rows allows.
 #include "pg_kv.cuh"
+#include "pg_trace.cuh"
 
 #include <algorithm>
 
@@ -308,6 +309,7 @@ static int launch_logits_out(int out_dtype, const LogitsParams& p, int n_rows, c
 extern "C" int pg_logits_process(int32_t n_rows, int32_t vocab, int32_t dtype, const void* logits,
                                  int64_t logits_stride, int32_t out_dtype, void* out, int64_t out_stride,
                                  const pg_logits_rules* rules, void* stream) {
+  pg::TraceRange trace_range("pg_logits_process");
   if (n_rows < 0 || vocab < 1 || vocab > 0x7FFF0000 || !rules) return PG_EINVAL;
   if (dtype != PG_F32 && dtype != PG_BF16 && dtype != PG_F16) return PG_EINVAL;
   if (out_dtype != PG_F32 && out_dtype != PG_BF16 && out_dtype != PG_F16) return PG_EINVAL;

@@ -2,8 +2,7 @@
 // end-to-end driver.  All arithmetic is in the kernels of pg_step.cu / pg_score.cu / pg_ovf.cu /
 // pg_compact.cu; this file only validates, keeps the cursor and enqueues.
 #include "pg_common.cuh"
-
-#include <nvtx3/nvToolsExt.h>
+#include "pg_trace.cuh"
 
 #include <atomic>
 #include <cmath>
@@ -49,17 +48,9 @@ struct pg_rollout {
 };
 
 using pg::cuda_fail;
+using pg::TraceRange;
 
 static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
-// Named range around a library call for timeline tools (NVTX; a no-op costing a pointer test when
-// no tool is attached).
-struct TraceRange {
-  explicit TraceRange(const char* name) { nvtxRangePushA(name); }
-  ~TraceRange() { nvtxRangePop(); }
-  TraceRange(const TraceRange&) = delete;
-  TraceRange& operator=(const TraceRange&) = delete;
-};
 
 // A handle's device memory belongs to the device that was current at pg_rollout_init: a call made
 // with another device current would hand that device pointers it cannot reach.
