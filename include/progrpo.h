@@ -467,7 +467,7 @@ int pg_gather_rows(pg_rollout *h, const int32_t *rows, int32_t n_out, int32_t n_
  * other; calls that can overlap on the GPU need one each.
  * Indices that come from device memory (page numbers, row numbers, lengths, token ids) are checked
  * in the kernels: a bad one is never dereferenced, bit 2 of *status is set and pg_kv_status returns
- * PG_EINDEX.  Running out of pages or of table entries sets bit 3 (PG_ENOPAGES); a bounded device-side
+ * PG_EINDEX.  Running out of pages or of table entries sets bit 3 (PG_ENOPAGES; see `grown` for the new tokens of such rows); a bounded device-side
  * wait that expires sets bit 1 (PG_ETIMEOUT, the call's results are then not valid).  `status` (nullable)
  * is a device int32 that the caller zeroes once and that calls only OR into.  Results do not depend on
  * the order in which the GPU runs its blocks.
@@ -503,8 +503,9 @@ typedef struct {
  * Attention of one new token per row: for query head j of row r (its key-value head is
  * j / (n_q_heads / n_kv_heads)), over the len[r] tokens of the row,
  *     out[r][j] = sum_t softmax_t(scale * q[r][j] . k_t) v_t,   lse[r][j] = ln sum_t exp(scale * q[r][j] . k_t).
- * A row of length 0 gives zeros and lse = -inf.  Sums and softmax statistics in fp32, out rounded
- * once to the cache's type.
+ * A row of length 0 gives zeros and lse = -inf.  Sums and softmax statistics are in fp32.  fp32 caches: out is that.  16-bit
+ * caches: the weights are rounded to the cache's type for their product with v (not in the sum that they are divided
+ * by), then out is rounded; the two errors are of one size.
  *   q, out [n_rows, n_q_heads, head_dim], rows q_stride / out_stride elements apart (0: contiguous)
  *   k_new, v_new (both or neither) [n_rows, n_kv_heads, head_dim], rows new_stride apart, 16-byte
  *     aligned: token len[r]-1 of every row is taken from them and stored into its page (the append of
@@ -614,8 +615,8 @@ int pg_logits_process(int32_t n_rows, int32_t vocab, int32_t dtype, const void *
 
 /*
  * Diagnostic (the paper has no counterpart): exercises the library's bounded device-side wait.
- * The only wait inside the kernels is the selection kernel's wait for its score rows to land in
- * shared memory; it gives up after a fixed number of attempts, sets status bit 1 and lets the
+ * The only wait inside the kernels of a handle is the selection kernel's wait for its score rows to land in
+ * shared memory (pg_kv_attend, which has no handle, has waits of its own: pg_selftest_token_waits); it gives up after a fixed number of attempts, sets status bit 1 and lets the
  * kernel return, so that a lost copy shows up as PG_ETIMEOUT from pg_rollout_status instead of a
  * hung GPU.  This call launches one warp that waits the same way on a barrier nothing completes:
  * the wait runs out (a fraction of a second at most), bit 1 of the handle's status word is set,

@@ -19,9 +19,11 @@
 // whole without waiting for anybody.  The two it may share are joined once at the end, first in the CTA, and
 // where a cut between CTAs has split a piece, by the CTA that arrives last (wait-free ticket; parts are
 // added in CTA order, so the bits do not depend on who that is).
-// Measured on a B200 (bf16 / fp16, 32 query and 8 kv heads x 128): one row of 131071 tokens 104 us (5.1 TB/s), 96 rows
-// of 1..8192 tokens 81 us (4.4 TB/s).  Bound now: the former by HBM and the join of the 18 parts of a piece, the
-// latter by the instructions of a warp around its chunks (two warps a scheduler, 0.24 issued a cycle).
+// Measured on a B200 (bf16 / fp16, 32 query and 8 kv heads x 128): one row of 131071 tokens 105 us (5.1 TB/s), 96 rows
+// of 1..8192 tokens 82 us (4.4 TB/s).  Bound now: the former by HBM and the join of the 18 parts of a piece, the
+// latter by latency: two warps a scheduler, each a chain of scores, maximum, exponentials and second product, issue 0.21
+// instructions a cycle (stalled by results of fixed latency, looked-up lengths and pages, and copies, about alike).  fp32:
+// 313 us and 258 us, 1.9 and 2.3 times what its bytes take.
 #include "pg_kv_attend.cuh"
 #include "pg_trace.cuh"
 
@@ -574,7 +576,7 @@ constexpr int kBoxTokens = 16;       // tokens of a tensor copy
 // kBulk: whole chunks (16 tokens of a page at a time) come by bulk copies that one lane issues - tensor
 // copies with the 128-byte swizzle in 16 bits, plain ones in fp32 - instead of 16 bytes a lane.  Against the latter the
 // walk takes a quarter fewer instructions (29.5 M to 22.3 M, 117 to 98 us for the own tokens of 768 rows of 1..512), which
-// is what bounds a warp with short pieces.
+// a warp with short pieces gains most from.
 template <typename T, typename Body, int kWarps, int kStages, bool kBulk>
 __global__ void __launch_bounds__(kWarps * 32, 1) attend_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ PoolMaps maps) {
   using S = AttendShared<T, Body, kWarps, kStages>;

@@ -18,11 +18,12 @@
 // does the same; joins scale alike).
 // The tiles of all units form one line cut into equal parts over the CTAs; every (CTA, unit) leaves its
 // queries' (m, l, O), and the rows' own pieces start from them.
-// Measured: 768 rows in groups of 48 (192 queries a kv head) over 2048 shared tokens, bf16, 8 kv heads x 128: about 65 us
-// for 25.8 GFLOP and 134 MB; the legacy mma path took 140 us.  Bound now: the softmax warps (about 1800 cycles a
-// 64-token tile) and the restart of the pipeline at every unit, not the tensor pipe.
-// Every wait is bounded: when one runs out, status bit 1 is set and the CTA leaves (its results are then
-// not valid; pg_kv_status returns PG_ETIMEOUT).
+// Measured: 768 rows in groups of 48 (192 queries a kv head) over 2048 shared tokens, bf16, 8 kv heads x 128: about 66 us
+// for 25.8 GFLOP and 134 MB; the legacy mma path took 140 us.  Bound now: latency, not a pipe - 3700 cycles for a 64-token tile
+// on average, at 27 % of the tensor pipe, 27 % issue and 2.3 TB/s, with most stalls on loads; which of the roles holds the
+// others up has not been measured.
+// Every wait is bounded: when one runs out, status bit 1 is set and its warp leaves, then those that wait for it (the
+// results are not valid; pg_kv_status returns PG_ETIMEOUT).  What the rows' own kernel follows is in place before the first wait.
 #include "pg_kv_attend.cuh"
 
 #include <type_traits>

@@ -4,7 +4,9 @@ Variance Filtering half-way, finish, and get their group-relative advantages.
 
 The policy is a small random-weight transformer stand-in (queries, keys, values and logits are plain torch
 products); what the library does is the cache, the attention, the sampling rules, the selection and the
-advantages.  `python -m paper_2512_15347_b200.examples.token_rollout`
+advantages.  The library has no attention of several new tokens of a row, and the stand-in none for its prompts: their keys
+and values of every layer are products of the embeddings alone, not of what the layers before make of them.  A policy in earnest
+runs its own prompt pass there and appends what it gives.  `python -m paper_2512_15347_b200.examples.token_rollout`
 """
 from __future__ import annotations
 
@@ -59,7 +61,7 @@ def rollout(policy, prompts, n_expand, n_keep, steps, prune_at, page_size=16, se
                        longest + steps, policy.embed.dtype)
     g = torch.Generator(device=dev).manual_seed(seed)
 
-    # prompts: their keys and values (all but each one's last token, which the first step brings)
+    # prompts: their keys and values from the embeddings (all but each one's last token, which the first step brings)
     cache.admit(G)
     cache.extend(lens - 1)
     start = torch.cat([lens.new_zeros(1), torch.cumsum(lens - 1, 0).to(torch.int32)])
