@@ -88,7 +88,7 @@ def _logits(g, R, V, dt, ids, dead):
     for j in range(ids.shape[1]):                        # one by one: a token may be given twice
         x.scatter_add_(1, ids[:, j: j + 1].clamp(min=0).long(), (9 * torch.rand((R, 1), generator=g, device=DEV)).to(dt))
     if R > 6:
-        some = torch.rand(V, generator=g, device=DEV) < 0.9
+        some = torch.rand(V, generator=g, device=DEV) < 0.6        # more stay allowed than the longest list has
         some[ids[1:3].clamp(min=0).long().view(-1)] = False
         x[1].masked_fill_(some, -math.inf)
         x[2].masked_fill_(some, torch.finfo(dt).min)
