@@ -613,6 +613,132 @@ typedef struct {
 int pg_logits_process(int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t logits_stride,
                       int32_t out_dtype, void *out, int64_t out_stride, const pg_logits_rules *rules, void *stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Policy update on token trajectories: the token counterpart of pg_policy_logprob / _objective / _backward.
+ *
+ * pg_token_forward reads rows of logits (one row per position to be scored) and gives the log-probabilities of given tokens, the
+ * entropy, the most likely alternatives and the divergence from a teacher's list of tokens - whichever are asked for, in one
+ * pass; pg_token_objective turns log-probs of ragged rows of tokens into the clipped objective and its derivatives;
+ * pg_token_backward takes those back to the logits.  pg_token_forward_backward is for weights that are known before
+ * (distillation, supervised tokens, the first update after a rollout): both passes in one, each logit read once.
+ * All are stateless; results do not depend on the order in which the GPU runs its blocks.
+ *
+ * With l the row's logits, T its temperature, x = l / T, lse = ln sum_v exp x_v, ln p_v = x_v - lse:
+ *     logp[j]    = ln p[ids[j]]                       (0 where ids[j] lies outside [0, vocab): padding)
+ *     entropy    = - sum_v p_v ln p_v
+ *     top        : the n_top largest logits, largest first, of equal ones the lowest index first: ids and ln p.  Logits of -inf
+ *                  and NaN are no alternatives; where there are too few: id -1 and ln p -inf
+ *     distill    : the divergence between the row and the teacher's list, see PG_DISTILL_*
+ * A row whose logits are all -inf allows nothing: lse and its log-probs are -inf, entropy and distill 0, its gradient zero.
+ * A row with a NaN or a logit of +inf gives NaN.  Sums and statistics are in fp32, the teacher's total mass in fp64.
+ * ------------------------------------------------------------------------------------------ */
+#define PG_TOKEN_MAX_VOCAB 1048576
+#define PG_TOKEN_MAX_TOP   128
+#define PG_TOKEN_MAX_LIST  256    /* most given tokens, and most entries of a teacher's list, of a row  */
+#define PG_TOKEN_SAVED     12     /* floats of a row that pg_token_forward keeps for pg_token_backward  */
+#define PG_TOKEN_STATS     5
+
+/* Divergences between the policy p and a teacher known by a list of its likely tokens i with log-probabilities tl_i, t_i = exp(tl_i).
+ * p is the policy's distribution over the whole vocabulary in all of them; entries with an id outside [0, vocab) or tl = -inf are
+ * unused, and of used entries with the same id the last one counts.
+ *   FORWARD       sum_i t_i (ln t_i - ln p_i) with t renormalised over the list (any logits may stand for tl); 0 for an empty list
+ *   FORWARD_REST  the tokens outside the list are one bucket, t_r = max(1 - sum_i t_i, 2^-20), p_r = sum of p outside the list:
+ *                 sum_i t_i (ln t_i - ln p_i) + t_r (ln t_r - ln p_r)
+ *   REVERSE_REST  sum_i p_i (ln p_i - ln t_i) + p_r (ln p_r - ln t_r)
+ * Where the policy gives nothing outside the list (p_r = 0) the bucket's term is left out.  A t_i of 0 and, in REVERSE_REST, a p_i of
+ * 0 add nothing. */
+#define PG_DISTILL_FORWARD      0
+#define PG_DISTILL_FORWARD_REST 1
+#define PG_DISTILL_REVERSE_REST 2
+
+/* What the rows are asked about.  Every array is optional. */
+typedef struct {
+  const float *temperature;    /* [n_rows] fp32 > 0; NULL: 1                                    */
+  const int32_t *ids;          /* [n_rows, n_ids] given tokens; the same one may be given twice  */
+  int32_t n_ids;               /* 0..PG_TOKEN_MAX_LIST                                           */
+  int32_t n_top;               /* alternatives, 0..min(vocab, PG_TOKEN_MAX_TOP)                    */
+  const int32_t *teacher_ids;  /* [n_rows, n_teacher]                                           */
+  const float *teacher_logp;   /* [n_rows, n_teacher] fp32                                      */
+  int32_t n_teacher;           /* 0..PG_TOKEN_MAX_LIST                                           */
+  int32_t kind;                /* PG_DISTILL_*                                                  */
+} pg_token_terms;
+
+/* Results, fp32 unless stated otherwise.  Every array is optional. */
+typedef struct {
+  float *logp;                 /* [n_rows, n_ids]                                               */
+  float *lse;                  /* [n_rows]                                                      */
+  float *entropy;              /* [n_rows]                                                      */
+  int32_t *top_ids;            /* [n_rows, n_top] int32                                         */
+  float *top_logp;             /* [n_rows, n_top]                                               */
+  float *distill;              /* [n_rows]                                                      */
+  float *saved;                /* [n_rows, PG_TOKEN_SAVED], 16-byte aligned: for pg_token_backward with the same terms */
+} pg_token_out;
+
+/* Derivatives of what is to be differentiated with respect to the results.  Every array is optional. */
+typedef struct {
+  const float *dlogp;          /* [n_rows, n_ids]; entries of padding are not read into the result */
+  const float *dentropy;       /* [n_rows], times entropy_scale                                  */
+  const float *ddistill;       /* [n_rows], times distill_scale                                  */
+  float entropy_scale, distill_scale;
+} pg_token_grads;
+
+/*
+ * logits [n_rows, vocab] of dtype, rows logits_stride elements apart (0: contiguous), aligned to their element.
+ */
+int pg_token_forward(int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t logits_stride,
+                     const pg_token_terms *terms, const pg_token_out *out, void *stream);
+
+/*
+ * Gradient with respect to the logits,
+ *     dlogits_v = 1/T ( sum_{j: ids[j] = v} dlogp_j - p_v sum_j dlogp_j - dentropy p_v (ln p_v + entropy) + ddistill d distill / d x_v ),
+ * of dtype, rounded once.  dlogits has the logits' shape, rows dlogits_stride elements apart; it may be logits when the
+ * strides agree (no other overlap).  terms and saved are those of pg_token_forward on the same logits (n_top plays no part).
+ * Rows whose derivatives are all zero get zeros and are not read.
+ */
+int pg_token_backward(int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t logits_stride,
+                      const pg_token_terms *terms, const float *saved, const pg_token_grads *grads, void *dlogits,
+                      int64_t dlogits_stride, void *stream);
+
+/* pg_token_forward and pg_token_backward in one pass: a row stays on chip between the two. */
+int pg_token_forward_backward(int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t logits_stride,
+                              const pg_token_terms *terms, const pg_token_out *out, const pg_token_grads *grads, void *dlogits,
+                              int64_t dlogits_stride, void *stream);
+
+/*
+ * The clipped objective of Eq. "pro_grpo_method" over ragged rows of tokens.  Row i's tokens are start[i] .. start[i+1] of the
+ * packed arrays, A_i its advantage.  With r = exp(logp_new - logp_old), d = logp_ref - logp_new, w a token's weight:
+ *     surr = min(r A, clip(r, 1 - clip_low, 1 + clip_high) A),   kl = exp(d) - d - 1
+ *     objective = sum_t w_t (surr_t - beta kl_t + entropy_coef entropy_t - distill_coef distill_t)
+ *     dlogp_t = w_t (A r [unclipped branch active] - beta (1 - exp(d))),   weight_t = w_t
+ *     w = scale / (n_rows * the row's tokens) | scale / all rows' tokens | scale     (PG_NORM_ROWS | _TOKENS | _SUM)
+ * so that dentropy = weight, entropy_scale = entropy_coef, ddistill = weight, distill_scale = -distill_coef belong to it in
+ * pg_token_backward.  Evaluated in fp64 from the fp32 inputs, sums in a fixed order.  Empty rows add nothing; tokens that
+ * belong to no row get dlogp, weight 0 and ratio 1, and their inputs are not read.
+ * stats: the weighted sums of surr, kl, entropy and distill, and the share of the rows' tokens that are clipped.
+ */
+#define PG_NORM_ROWS   0
+#define PG_NORM_TOKENS 1
+#define PG_NORM_SUM    2
+typedef struct {
+  const int32_t *start;        /* [n_rows + 1] ascending, 0 <= start[i] <= n_tokens             */
+  const float *logp_new;       /* [n_tokens] fp32                                               */
+  const float *logp_old;       /* [n_tokens]; NULL: logp_new (r = 1)                             */
+  const float *logp_ref;       /* [n_tokens]; NULL: kl = 0                                       */
+  const float *adv;            /* [n_rows]                                                      */
+  const float *entropy;        /* [n_tokens] or NULL                                            */
+  const float *distill;        /* [n_tokens] or NULL                                            */
+  float clip_low, clip_high;   /* >= 0, clip_low <= 1                                            */
+  float beta, entropy_coef, distill_coef, scale;
+  int32_t norm;                /* PG_NORM_*                                                     */
+} pg_token_batch;
+
+/* objective [1]; dlogp [n_tokens]; weight, ratio [n_tokens] and stats [PG_TOKEN_STATS] nullable; dlogp may be logp_new.
+ * workspace as for the cache calls, at least pg_token_objective_workspace_bytes(n_tokens) bytes.  A start that does not ascend inside
+ * [0, n_tokens] is not followed (status bit 2). */
+size_t pg_token_objective_workspace_bytes(int32_t n_tokens);
+int pg_token_objective(int32_t n_rows, int32_t n_tokens, const pg_token_batch *batch, float *objective, float *dlogp, float *weight,
+                       float *ratio, float *stats, void *workspace, size_t workspace_bytes, int32_t *status, void *stream);
+
 /*
  * Diagnostic (the paper has no counterpart): exercises the library's bounded device-side wait.
  * The only wait inside the kernels of a handle is the selection kernel's wait for its score rows to land in

@@ -21,6 +21,9 @@ VEL_F32, VEL_BF16 = 0, 1
 F32, BF16, F16 = 0, 1, 2              # element types of the token calls
 LOGITS_MAX_TOKENS, LOGITS_MAX_BIAS = 1048575, 2046
 MAX_GROUP = 1024
+TOKEN_MAX_VOCAB, TOKEN_MAX_TOP, TOKEN_MAX_LIST, TOKEN_SAVED, TOKEN_STATS = 1 << 20, 128, 256, 12, 5
+DISTILL_KINDS = ("forward", "forward_rest", "reverse_rest")
+TOKEN_NORMS = ("rows", "tokens", "sum")
 
 
 class PgError(RuntimeError):
@@ -72,6 +75,28 @@ class LogitsRules(ctypes.Structure):
                 ("presence", ctypes.c_void_p), ("frequency", ctypes.c_void_p), ("temperature", ctypes.c_void_p),
                 ("bias_ids", ctypes.c_void_p), ("bias_values", ctypes.c_void_p), ("n_bias", ctypes.c_int32),
                 ("mask", ctypes.c_void_p), ("mask_stride", ctypes.c_int64)]
+
+
+class TokenTerms(ctypes.Structure):
+    """What rows of logits are asked about (``make_token_terms``)."""
+    _fields_ = [("temperature", ctypes.c_void_p), ("ids", ctypes.c_void_p), ("n_ids", ctypes.c_int32), ("n_top", ctypes.c_int32),
+                ("teacher_ids", ctypes.c_void_p), ("teacher_logp", ctypes.c_void_p), ("n_teacher", ctypes.c_int32),
+                ("kind", ctypes.c_int32)]
+
+
+class TokenOut(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("logp", "lse", "entropy", "top_ids", "top_logp", "distill", "saved")]
+
+
+class TokenGrads(ctypes.Structure):
+    _fields_ = [("dlogp", ctypes.c_void_p), ("dentropy", ctypes.c_void_p), ("ddistill", ctypes.c_void_p),
+                ("entropy_scale", ctypes.c_float), ("distill_scale", ctypes.c_float)]
+
+
+class TokenBatch(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("start", "logp_new", "logp_old", "logp_ref", "adv", "entropy", "distill")] + \
+               [(name, ctypes.c_float) for name in ("clip_low", "clip_high", "beta", "entropy_coef", "distill_coef", "scale")] + \
+               [("norm", ctypes.c_int32)]
 
 
 _lib = None
@@ -142,8 +167,16 @@ def lib() -> ctypes.CDLL:
     L.pg_kv_pack.argtypes = [pkv, vp, vp, vp, vp, vp, sz, vp, vp]
     L.pg_kv_status.argtypes = [vp, vp]
     L.pg_logits_process.argtypes = [i32, i32, i32, vp, i64, i32, vp, i64, ctypes.POINTER(LogitsRules), vp]
+    L.pg_token_forward.argtypes = [i32, i32, i32, vp, i64, ctypes.POINTER(TokenTerms), ctypes.POINTER(TokenOut), vp]
+    L.pg_token_backward.argtypes = [i32, i32, i32, vp, i64, ctypes.POINTER(TokenTerms), vp, ctypes.POINTER(TokenGrads), vp, i64, vp]
+    L.pg_token_forward_backward.argtypes = [i32, i32, i32, vp, i64, ctypes.POINTER(TokenTerms), ctypes.POINTER(TokenOut),
+                                            ctypes.POINTER(TokenGrads), vp, i64, vp]
+    L.pg_token_objective_workspace_bytes.argtypes = [i32]
+    L.pg_token_objective_workspace_bytes.restype = sz
+    L.pg_token_objective.argtypes = [i32, i32, ctypes.POINTER(TokenBatch), vp, vp, vp, vp, vp, vp, sz, vp, vp]
     L.pg_selftest_token_waits.argtypes = [ctypes.c_uint32]
-    for name in ("pg_kv_attend", "pg_kv_extend", "pg_kv_append", "pg_kv_fork", "pg_kv_pack", "pg_kv_status",
+    for name in ("pg_token_forward", "pg_token_backward", "pg_token_forward_backward", "pg_token_objective",
+                 "pg_kv_attend", "pg_kv_extend", "pg_kv_append", "pg_kv_fork", "pg_kv_pack", "pg_kv_status",
                  "pg_logits_process", "pg_selftest_token_waits"):
         getattr(L, name).restype = ctypes.c_int
     L.pg_strerror.argtypes = [ctypes.c_int]
@@ -692,6 +725,165 @@ def logits_process(logits, out, rules: LogitsRules, stream=None) -> None:
         raise ValueError("mask: too few words for the vocabulary")
     _check(lib().pg_logits_process(rows, vocab, from_type, logits.data_ptr(), a, to_type, out.data_ptr(), b, rules._ref,
                                    _stream(stream)), "pg_logits_process")
+
+
+# ---------------------------------------------------------------- policy update on token trajectories
+
+def _f32(t, what: str, n: int, dev: int) -> Optional[int]:
+    """Address of a contiguous fp32 tensor of n elements on device dev."""
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or not t.is_contiguous() or t.numel() != n:
+        raise ValueError(f"{what}: {n} contiguous fp32 elements")
+    if t.get_device() != dev:
+        raise _elsewhere(what, dev)
+    return t.data_ptr()
+
+
+def make_token_terms(*, temperature=None, ids=None, n_top: int = 0, teacher_ids=None, teacher_logp=None, kind: str = "forward") -> TokenTerms:
+    """What ``token_forward`` and the others are asked about, over caller-owned tensors (see pg_token_terms): temperature [rows] fp32,
+    ids [rows] or [rows, n] int32 given tokens, n_top alternatives, a teacher's list teacher_ids [rows, n] int32 with its
+    log-probs teacher_logp [rows, n] fp32 and the kind of divergence (``DISTILL_KINDS``).  Keeps references to all of them."""
+    r = TokenTerms()
+    rows = dev = None
+
+    def see(t, what):
+        nonlocal rows, dev
+        dev = t.get_device() if dev is None else dev
+        _want(dev >= 0 and t.get_device() == dev, f"{what}: all tensors of the terms on one CUDA device")
+        _want(rows is None or rows == t.shape[0], f"{what}: one entry per row")
+        rows = t.shape[0]
+
+    if temperature is not None:
+        _want(temperature.dtype == torch.float32 and temperature.dim() == 1 and temperature.is_contiguous(), "temperature: [rows] fp32")
+        see(temperature, "temperature")
+        r.temperature = temperature.data_ptr()
+    n_ids = 0
+    if ids is not None:
+        _want(ids.dim() in (1, 2), "ids: [rows] or [rows, n] int32")
+        see(ids, "ids")
+        n_ids = 1 if ids.dim() == 1 else ids.shape[1]
+        _want(n_ids <= TOKEN_MAX_LIST, f"ids: at most {TOKEN_MAX_LIST} a row")
+        r.ids, r.n_ids = _i32(ids, "ids") if n_ids else None, n_ids
+    n_teacher = 0
+    _want((teacher_ids is None) == (teacher_logp is None), "teacher_ids and teacher_logp: both or neither")
+    if teacher_ids is not None:
+        _want(teacher_ids.dim() == 2 and teacher_logp.shape == teacher_ids.shape and teacher_logp.dtype == torch.float32 and
+              teacher_logp.is_contiguous(), "teacher_ids [rows, n] int32, teacher_logp fp32 of its shape")
+        see(teacher_ids, "teacher_ids")
+        see(teacher_logp, "teacher_logp")
+        n_teacher = teacher_ids.shape[1]
+        _want(n_teacher <= TOKEN_MAX_LIST, f"teacher_ids: at most {TOKEN_MAX_LIST} a row")
+        if n_teacher:
+            r.teacher_ids, r.teacher_logp, r.n_teacher = _i32(teacher_ids, "teacher_ids"), teacher_logp.data_ptr(), n_teacher
+    _want(0 <= n_top <= TOKEN_MAX_TOP, f"n_top: 0..{TOKEN_MAX_TOP}")
+    _want(kind in DISTILL_KINDS, f"kind: one of {DISTILL_KINDS}")
+    r.n_top, r.kind = n_top, DISTILL_KINDS.index(kind)
+    r._plain = (rows, dev, n_ids, n_top, n_teacher)
+    r._keepalive = (temperature, ids, teacher_ids, teacher_logp)
+    r._ref = ctypes.byref(r)
+    return r
+
+
+def _token_rows(t, terms: TokenTerms, what: str):
+    """(rows, vocab, type, row stride, device) of logits or their gradient."""
+    if t.dim() != 2 or t.dtype not in _DTYPES:
+        raise ValueError(f"{what}: [rows, vocab], fp32, bf16 or fp16")
+    rows, vocab = t.shape
+    a, one = t.stride()
+    if (one != 1 and vocab > 1) or (rows > 1 and a < vocab):
+        raise ValueError(f"{what}: contiguous rows, apart")
+    dev = t.get_device()
+    at, on = terms._plain[:2]
+    if dev < 0 or (on is not None and on != dev):
+        raise ValueError(f"{what} and the terms: on one CUDA device")
+    if at is not None and at != rows:
+        raise ValueError("the terms are for another number of rows")
+    return rows, vocab, _DTYPES[t.dtype], a if rows > 1 else 0, dev
+
+
+def _token_out(terms, rows, dev, logp, lse, entropy, top_ids, top_logp, distill, saved) -> TokenOut:
+    n_ids, n_top, n_teacher = terms._plain[2:]
+    if (logp is not None and not n_ids) or (distill is not None and not n_teacher) or (top_ids is not None and not n_top):
+        raise ValueError("an output that the terms do not ask for")
+    if top_logp is not None and top_ids is None:
+        raise ValueError("top_logp without top_ids")
+    return TokenOut(_f32(logp, "logp", rows * n_ids, dev), _f32(lse, "lse", rows, dev), _f32(entropy, "entropy", rows, dev),
+                    None if top_ids is None else _i32(top_ids, "top_ids", rows * n_top, dev), _f32(top_logp, "top_logp", rows * n_top, dev),
+                    _f32(distill, "distill", rows, dev), _f32(saved, "saved", rows * TOKEN_SAVED, dev))
+
+
+def _token_grads(terms, rows, dev, dlogp, dentropy, ddistill, entropy_scale, distill_scale) -> TokenGrads:
+    n_ids, _, n_teacher = terms._plain[2:]
+    if (dlogp is not None and not n_ids) or (ddistill is not None and not n_teacher):
+        raise ValueError("a derivative of what the terms do not ask for")
+    return TokenGrads(_f32(dlogp, "dlogp", rows * n_ids, dev), _f32(dentropy, "dentropy", rows, dev), _f32(ddistill, "ddistill", rows, dev),
+                      entropy_scale, distill_scale)
+
+
+def _token_dlogits(logits, dlogits, terms):
+    if dlogits.dtype is not logits.dtype or dlogits.shape != logits.shape or dlogits.get_device() != logits.get_device():
+        raise ValueError("dlogits: like the logits")
+    return _token_rows(dlogits, terms, "dlogits")[3]
+
+
+def token_forward(logits, terms: TokenTerms, *, logp=None, lse=None, entropy=None, top_ids=None, top_logp=None, distill=None, saved=None,
+                  stream=None) -> None:
+    """One pass over logits [rows, vocab] (rows may be strided) for whatever outputs are given (see pg_token_forward): logp [rows, given
+    tokens], lse, entropy, distill [rows], top_ids (int32) / top_logp [rows, n_top], saved [rows, TOKEN_SAVED] for ``token_backward``."""
+    rows, vocab, dtype, stride, dev = _token_rows(logits, terms, "logits")
+    _current(dev)
+    out = _token_out(terms, rows, dev, logp, lse, entropy, top_ids, top_logp, distill, saved)
+    _check(lib().pg_token_forward(rows, vocab, dtype, logits.data_ptr(), stride, terms._ref, out, _stream(stream)), "pg_token_forward")
+
+
+def token_backward(logits, terms: TokenTerms, saved, dlogits, *, dlogp=None, dentropy=None, ddistill=None, entropy_scale: float = 1.0,
+                   distill_scale: float = 1.0, stream=None) -> None:
+    """Gradient to the logits of what ``token_forward`` computed with the same terms (see pg_token_backward); dlogits may be logits."""
+    rows, vocab, dtype, stride, dev = _token_rows(logits, terms, "logits")
+    _current(dev)
+    grads = _token_grads(terms, rows, dev, dlogp, dentropy, ddistill, entropy_scale, distill_scale)
+    _check(lib().pg_token_backward(rows, vocab, dtype, logits.data_ptr(), stride, terms._ref, _f32(saved, "saved", rows * TOKEN_SAVED, dev),
+                                   grads, dlogits.data_ptr(), _token_dlogits(logits, dlogits, terms), _stream(stream)), "pg_token_backward")
+
+
+def token_forward_backward(logits, terms: TokenTerms, dlogits, *, logp=None, lse=None, entropy=None, top_ids=None, top_logp=None,
+                           distill=None, saved=None, dlogp=None, dentropy=None, ddistill=None, entropy_scale: float = 1.0,
+                           distill_scale: float = 1.0, stream=None) -> None:
+    """``token_forward`` and ``token_backward`` in one pass, for derivatives that are known before (see pg_token_forward_backward)."""
+    rows, vocab, dtype, stride, dev = _token_rows(logits, terms, "logits")
+    _current(dev)
+    out = _token_out(terms, rows, dev, logp, lse, entropy, top_ids, top_logp, distill, saved)
+    grads = _token_grads(terms, rows, dev, dlogp, dentropy, ddistill, entropy_scale, distill_scale)
+    _check(lib().pg_token_forward_backward(rows, vocab, dtype, logits.data_ptr(), stride, terms._ref, out, grads, dlogits.data_ptr(),
+                                           _token_dlogits(logits, dlogits, terms), _stream(stream)), "pg_token_forward_backward")
+
+
+def token_objective_workspace_bytes(n_tokens: int) -> int:
+    return int(lib().pg_token_objective_workspace_bytes(n_tokens))
+
+
+def token_objective(start, logp_new, adv, objective, dlogp, workspace, *, logp_old=None, logp_ref=None, entropy=None, distill=None,
+                    clip_low: float = 0.2, clip_high: float = 0.2, beta: float = 0.0, entropy_coef: float = 0.0, distill_coef: float = 0.0,
+                    scale: float = 1.0, norm: str = "rows", weight=None, ratio=None, stats=None, status=None, stream=None) -> None:
+    """Clipped objective over ragged rows of tokens and its derivative (see pg_token_objective): start [rows + 1] int32, adv [rows], the
+    other arrays [tokens], objective [1], stats [TOKEN_STATS], norm one of ``TOKEN_NORMS``."""
+    dev = logp_new.get_device()
+    if dev < 0:
+        raise ValueError("logp_new: a CUDA tensor")
+    _current(dev)
+    rows, n = start.numel() - 1, logp_new.numel()
+    if rows < 0:
+        raise ValueError("start: [rows + 1] int32")
+    if norm not in TOKEN_NORMS:
+        raise ValueError(f"norm: one of {TOKEN_NORMS}")
+    b = TokenBatch(_i32(start, "start", rows + 1, dev), _f32(logp_new, "logp_new", n, dev), _f32(logp_old, "logp_old", n, dev),
+                   _f32(logp_ref, "logp_ref", n, dev), _f32(adv, "adv", rows, dev), _f32(entropy, "entropy", n, dev),
+                   _f32(distill, "distill", n, dev), clip_low, clip_high, beta, entropy_coef, distill_coef, scale, TOKEN_NORMS.index(norm))
+    _check(lib().pg_token_objective(rows, n, b, _f32(objective, "objective", 1, dev), _f32(dlogp, "dlogp", n, dev),
+                                    _f32(weight, "weight", n, dev), _f32(ratio, "ratio", n, dev), _f32(stats, "stats", TOKEN_STATS, dev),
+                                    _space(workspace, dev), workspace.nbytes, _i32(status, "status", None, dev), _stream(stream)),
+           "pg_token_objective")
 
 
 def strerror(code: int) -> str:
