@@ -3,15 +3,15 @@
 
 namespace pg {
 
-extern template int token_launch<float, kForward>(const TokenParams&, int, cudaStream_t);
-extern template int token_launch<float, kBackward>(const TokenParams&, int, cudaStream_t);
-extern template int token_launch<float, kBoth>(const TokenParams&, int, cudaStream_t);
-extern template int token_launch<__nv_bfloat16, kForward>(const TokenParams&, int, cudaStream_t);
-extern template int token_launch<__nv_bfloat16, kBackward>(const TokenParams&, int, cudaStream_t);
-extern template int token_launch<__nv_bfloat16, kBoth>(const TokenParams&, int, cudaStream_t);
-extern template int token_launch<__half, kForward>(const TokenParams&, int, cudaStream_t);
-extern template int token_launch<__half, kBackward>(const TokenParams&, int, cudaStream_t);
-extern template int token_launch<__half, kBoth>(const TokenParams&, int, cudaStream_t);
+extern template int token_launch<float, kForward>(const TokenParams&, cudaStream_t);
+extern template int token_launch<float, kBackward>(const TokenParams&, cudaStream_t);
+extern template int token_launch<float, kBoth>(const TokenParams&, cudaStream_t);
+extern template int token_launch<__nv_bfloat16, kForward>(const TokenParams&, cudaStream_t);
+extern template int token_launch<__nv_bfloat16, kBackward>(const TokenParams&, cudaStream_t);
+extern template int token_launch<__nv_bfloat16, kBoth>(const TokenParams&, cudaStream_t);
+extern template int token_launch<__half, kForward>(const TokenParams&, cudaStream_t);
+extern template int token_launch<__half, kBackward>(const TokenParams&, cudaStream_t);
+extern template int token_launch<__half, kBoth>(const TokenParams&, cudaStream_t);
 
 template <int kMode>
 static int token_call(int32_t n_rows, int32_t vocab, int32_t dtype, const void* logits, int64_t logits_stride, const pg_token_terms* terms,
@@ -42,13 +42,17 @@ static int token_call(int32_t n_rows, int32_t vocab, int32_t dtype, const void* 
   }
   p.in = logits;
   p.dl = dlogits;
+  p.n_rows = n_rows;
   p.vocab = vocab;
+  if (!p.t.ids) p.t.n_ids = 0;
+  if (!p.t.teacher_ids) p.t.n_teacher = 0;
+  if (!p.o.top_ids) p.t.n_top = 0;
   p.in_stride = logits_stride;
   p.dl_stride = dlogits_stride;
   cudaStream_t st = (cudaStream_t)stream;
-  if (dtype == PG_F32) return token_launch<float, kMode>(p, n_rows, st);
-  if (dtype == PG_BF16) return token_launch<__nv_bfloat16, kMode>(p, n_rows, st);
-  return token_launch<__half, kMode>(p, n_rows, st);
+  if (dtype == PG_F32) return token_launch<float, kMode>(p, st);
+  if (dtype == PG_BF16) return token_launch<__nv_bfloat16, kMode>(p, st);
+  return token_launch<__half, kMode>(p, st);
 }
 
 }  // namespace pg

@@ -25,12 +25,22 @@
 namespace pg {
 
 
-constexpr int kTokThreads = 512;
+#ifndef NB
+#define NB 4
+#endif
+constexpr int kTokThreads = 256;
+constexpr int kTokCtas = NB;                    // of an SM
+#ifndef PB
+#define PB 131072
+#endif
+constexpr int kPartBytes = PB;
 constexpr int kTokWarps = kTokThreads / 32;
 constexpr int kMostParts = 8;                   // CTAs of a cluster
 constexpr int kCandidates = 1024;
+constexpr int kMergeBytes = kMostParts * PG_TOKEN_MAX_TOP * 8;
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr float kFloorY = -1e4f;                // 2^y = 0 long before; keeps 0 * y from being NaN
+constexpr float kHuge = 1e30f;                  // logits from here on (the type's lowest value as a mask) have no l c in 32 bits
 
 enum TokenMode { kForward, kBackward, kBoth };
 
@@ -41,7 +51,20 @@ struct TokenParams {
   const void* in;
   void* dl;
   int64_t in_stride, dl_stride;
-  int vocab, parts, units, tiles;               // CTAs of a row; units of a part; tiles of a part
+  int n_rows, vocab;
+  int parts, units, tiles;                      // CTAs of a row; units of a part; tiles of a part
+};
+
+// What is known of a row when its logits have been read.
+struct TokenRow {
+  float m, l2, h;                // p_v = 2^((l_v - m) c - l2); entropy
+  float mr, l2r, lr;             // the same of the distribution outside the list; ln p_r (-inf: nothing there)
+  float loss, lt, w;             // divergence; ln t_r, or ln of the list's mass (FORWARD); sum t (+ t_r)
+  float some;                    // 0: a row that allows nothing
+};
+// The gradient away from given and listed tokens: e (a + b ln e), e = 2^((l - ref) c - l2).
+struct TokenSlope {
+  float a, b, ref, l2;
 };
 
 // Sums over a warp's share of a teacher's list.  Reference of e: the largest logit m among them; of t: `tm` (FORWARD), else 0.
@@ -52,26 +75,25 @@ struct ListSums {
 };
 
 struct TokenShared {
-  float wm[kTokWarps], ws0[kTokWarps], ws1[kTokWarps];
-  float part[kMostParts][4];                    // triples of the cluster's CTAs, written by each
+  float4 part[kMostParts * kTokWarps];          // triples of the cluster's warps, written by each
+  TokenRow row;
+  TokenSlope slope;
+  float lp_part;
   ListSums list[PG_TOKEN_MAX_LIST / 32];
   float dsum[PG_TOKEN_MAX_LIST / 32];
   int gid[PG_TOKEN_MAX_LIST];                   // given tokens, -1: padding
   float gdl[PG_TOKEN_MAX_LIST];
-  int tid[PG_TOKEN_MAX_LIST];                   // listed tokens, -1: unused
+  alignas(16) int tid[PG_TOKEN_MAX_LIST];       // listed tokens, -1: unused
+  uint32_t edges;                               // bits of the listed ones among the edge tokens
 };
-// Behind it, for alternatives; keys order by (logit, lowest index first).
-struct TopShared {
-  unsigned long long cand[kCandidates];
-  unsigned long long merge[kMostParts][PG_TOKEN_MAX_TOP];   // the parts' lists, in part 0's
-  unsigned long long best[PG_TOKEN_MAX_TOP];
-  float tmax[kTokThreads];
-  unsigned int hist[256];
-  unsigned long long prefix;
-  float bound;
-  int count, left, shift;
-};
-
+#ifdef SCALAR
+typedef float2 f2;
+__device__ __forceinline__ f2 make2(float a, float b) { return make_float2(a, b); }
+__device__ __forceinline__ void split2(f2 v, float& a, float& b) { a = v.x; b = v.y; }
+__device__ __forceinline__ f2 add2(f2 a, f2 b) { return make_float2(a.x + b.x, a.y + b.y); }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) { return make_float2(a.x * b.x, a.y * b.y); }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { return make_float2(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)); }
+#else
 typedef unsigned long long f2;                  // two floats for the packed fp32 instructions
 __device__ __forceinline__ f2 make2(float a, float b) {
   f2 r;
@@ -94,6 +116,7 @@ __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
+#endif
 __device__ __forceinline__ float ex2(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -108,8 +131,8 @@ __device__ __forceinline__ uint32_t peer(const void* p, int r) {
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(r));
   return at;
 }
-__device__ __forceinline__ void peer_store(uint32_t at, float v) {
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory");
+__device__ __forceinline__ void peer_store(uint32_t at, float a, float b, float c) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(a), "f"(b), "f"(c), "f"(0.f) : "memory");
 }
 __device__ __forceinline__ void peer_store(uint32_t at, unsigned long long v) {
   asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at), "l"(v) : "memory");
@@ -190,13 +213,6 @@ __device__ __forceinline__ unsigned long long top_key(float x, int id) {
   return (unsigned long long)(b ^ (b >> 31 ? 0xFFFFFFFFu : 0x80000000u)) << 32 | (0xFFFFFFFFu - (uint32_t)id);
 }
 
-// What is known of a row when its logits have been read.
-struct TokenRow {
-  float m, l2, h;                // p_v = 2^((l_v - m) c - l2); entropy
-  float mr, l2r, lr;             // the same of the distribution outside the list; ln p_r (-inf: nothing there)
-  float loss, lt, w;             // divergence; ln t_r, or ln of the list's mass (FORWARD); sum t (+ t_r)
-  float some;                    // 0: a row that allows nothing
-};
 __device__ __forceinline__ void save_row(float4* at, const TokenRow& r) {
   at[0] = make_float4(r.m, r.l2, r.h, r.mr);
   at[1] = make_float4(r.l2r, r.lr, r.loss, r.lt);
@@ -207,33 +223,52 @@ __device__ __forceinline__ TokenRow load_row(const float4* at) {
   return {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, d.x, d.y};
 }
 
-// From the sums over the row outside the list (`rest`) or over all of it, and the list's.
-__device__ __forceinline__ TokenRow finish_row(const TokenShared& s, int parts, int lists, bool rest, int kind, float inv) {
+// Joins triples of the lanes of a warp; all lanes get the result.
+__device__ __forceinline__ void join_warp(float& m, float& s0, float& s1, float c) {
+  const float to = warp_most(m);
+  refer(m, to, c, s0, s1);
+  m = to;
+  s0 = warp_total(s0);
+  s1 = warp_total(s1);
+}
+
+// By one warp: from the sums over the row outside the list (`rest`) or over all of it, and the list's.
+__device__ __forceinline__ TokenRow finish_row(const TokenShared& s, const float4* triples, int parts, int lists, bool rest, int kind, float inv) {
   const float c = inv * kLog2e;
+  const int lane = threadIdx.x & 31;
   TokenRow r;
   float m = -INFINITY, s0 = 0.f, s1 = 0.f;
-  for (int i = 0; i < parts; ++i) m = fmaxf(m, s.part[i][0]);
-  for (int i = 0; i < parts; ++i) {
-    float a = s.part[i][1], b = s.part[i][2];
-    refer(s.part[i][0], m, c, a, b);
-    s0 += a;
-    s1 += b;
+  for (int i = lane; i < parts * kTokWarps; i += 32) {
+    float4 v = triples[i];
+    const float to = fmaxf(m, v.x);
+    refer(m, to, c, s0, s1);
+    refer(v.x, to, c, v.y, v.z);
+    m = to;
+    s0 += v.y;
+    s1 += v.z;
   }
+  join_warp(m, s0, s1, c);
   r.mr = m;
   const bool outside = !(s0 == 0.f);
   r.l2r = outside ? log2f(s0) : 0.f;
-  if (rest) {
-    const float sr = s0, sr1 = s1;
-    for (int i = 0; i < lists; ++i) m = fmaxf(m, s.list[i].m);
-    s0 = sr;
-    s1 = sr1;
-    refer(r.mr, m, c, s0, s1);
-    for (int i = 0; i < lists; ++i) {
-      float a = s.list[i].s0, b = s.list[i].s1;
-      refer(s.list[i].m, m, c, a, b);
-      s0 += a;
-      s1 += b;
+  ListSums l;
+  l.m = l.tm = -INFINITY;
+  l.s0 = l.s1 = l.etl = l.ts = l.ttl = l.ty = 0.f;
+  l.mass = 0.;
+  if (lane < lists) l = s.list[lane];
+  if (rest && lists > 0) {
+    float a = l.s0, b = l.s1;
+    if (lane == 31) {                                                  // the lists end before: at most eight
+      l.m = m;
+      a = s0;
+      b = s1;
     }
+    float to = l.m;
+    join_warp(to, a, b, c);
+    if (lane == 31) l.m = -INFINITY;
+    m = to;
+    s0 = a;
+    s1 = b;
   }
   r.some = s0 == 0.f ? 0.f : 1.f;
   r.m = finite_ref(m);
@@ -246,16 +281,17 @@ __device__ __forceinline__ TokenRow finish_row(const TokenShared& s, int parts, 
   r.loss = r.lt = r.w = 0.f;
   if (lists == 0 || r.some == 0.f) return r;
   if (kind == PG_DISTILL_FORWARD) {
-    float tm = -INFINITY, z = 0.f, ttl = 0.f, tlp = 0.f;
-    for (int i = 0; i < lists; ++i) tm = fmaxf(tm, s.list[i].tm);
-    for (int i = 0; i < lists; ++i) {
-      const ListSums& l = s.list[i];
-      if (l.tm == -INFINITY) { z += l.ts; continue; }                 // nothing used (or NaN)
+    const float tm = warp_most(l.tm);
+    float z = l.ts, ttl = 0.f, tlp = 0.f;                              // ts without tm: NaN
+    if (l.tm != -INFINITY) {
       const float f = expf(l.tm - tm);
-      z += f * l.ts;
-      ttl += f * (l.ttl + l.ts * (l.tm - tm));
-      tlp += f * (l.ty + l.ts * ((finite_ref(l.m) - r.m) * inv - kLn2 * r.l2));
+      z = f * l.ts;
+      ttl = f * (l.ttl + l.ts * (l.tm - tm));
+      tlp = f * (l.ty + l.ts * ((finite_ref(l.m) - r.m) * inv - kLn2 * r.l2));
     }
+    z = warp_total(z);
+    ttl = warp_total(ttl);
+    tlp = warp_total(tlp);
     if (z == 0.f) {                                                    // no list
       r.loss = 0.f * r.l2;                                             // NaN in a row with one
       return r;
@@ -265,87 +301,382 @@ __device__ __forceinline__ TokenRow finish_row(const TokenShared& s, int parts, 
     r.loss = ttl / z - logf(z) - tlp / z;
     return r;
   }
-  double mass = 0.;
-  for (int i = 0; i < lists; ++i) mass += s.list[i].mass;
+  const double mass = warp_total(l.mass);
   const double tr = fmax(1. - mass, 1. / (1 << 20));
   r.lt = (float)log(tr);
   r.w = (float)(outside ? mass + tr : mass);
   if (mass != mass) r.lt = r.w = NAN;
   if (kind == PG_DISTILL_FORWARD_REST) {
-    float ttl = 0.f, tlp = 0.f;
-    for (int i = 0; i < lists; ++i) {
-      const ListSums& l = s.list[i];
-      ttl += l.ttl;
-      if (l.ts != 0.f) tlp += l.ty + l.ts * ((finite_ref(l.m) - r.m) * inv - kLn2 * r.l2);
-    }
-    r.loss = ttl - tlp + (outside ? (float)(tr * (r.lt - lr)) : 0.f);
+    const float tlp = warp_total(l.ts != 0.f ? l.ty + l.ts * ((finite_ref(l.m) - r.m) * inv - kLn2 * r.l2) : 0.f);
+    r.loss = warp_total(l.ttl) - tlp + (outside ? (float)(tr * (r.lt - lr)) : 0.f);
   } else {
     float plp = 0.f, ptl = 0.f;
-    for (int i = 0; i < lists; ++i) {
-      const ListSums& l = s.list[i];
-      if (l.s0 == 0.f) continue;
+    if (l.s0 != 0.f) {
       const float d = (l.m - r.m) * c, f = ex2(fmaxf(d, kFloorY));
-      if (f == 0.f) continue;
-      plp += f * (l.s1 + l.s0 * (d - r.l2));
-      ptl += f * l.etl;
+      if (f != 0.f) {
+        plp = f * (l.s1 + l.s0 * (d - r.l2));
+        ptl = f * l.etl;
+      }
     }
+    plp = warp_total(plp);
+    ptl = warp_total(ptl);
     const float pr = outside ? expf(r.lr) : 0.f;
     r.loss = (kLn2 * plp - ptl) / s0 + (outside ? pr * (r.lr - r.lt) : 0.f);
   }
   return r;
 }
 
-template <typename T, int kMode, bool kEnt, bool kRest>
-__global__ void __launch_bounds__(kTokThreads, 2)
-token_kernel(const __grid_constant__ TokenParams p) {
-  constexpr int kUnits = sizeof(T) == 4 ? 4 : 8;                    // of a thread and tile
-  constexpr int kTile = kUnits * kTokThreads;
-  __shared__ TokenShared s;
-  extern __shared__ __align__(16) unsigned char more[];             // TopShared if there are alternatives, then bits of listed tokens (kRest)
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int row = blockIdx.x / p.parts, part = blockIdx.x - row * p.parts;
-  const bool many = kMode != kBackward && p.parts > 1;
-  if (many) cluster_arrive();                                       // all CTAs run before one writes into another's memory
-  const int n_ids = p.t.ids ? p.t.n_ids : 0, n_list = p.t.teacher_ids ? p.t.n_teacher : 0;
-  const int lists = (n_list + 31) / 32, n_top = kMode != kBackward && p.o.top_ids ? p.t.n_top : 0;
-  TopShared& top = *reinterpret_cast<TopShared*>(more);
-  uint32_t* bits = reinterpret_cast<uint32_t*>(more + (n_top ? sizeof(TopShared) : 0));
+__device__ __forceinline__ float key_value(unsigned long long key) {
+  const uint32_t b = (uint32_t)(key >> 32);
+  return __uint_as_float(b >> 31 ? b ^ 0x80000000u : ~b);
+}
 
-  const T* in = (const T*)p.in + row * p.in_stride;
-  // Units of eight tokens lie on 16-byte boundaries of the row's memory: the first begins `lead` tokens before it.
-  const int lead = (int)(((uintptr_t)in & 15) / sizeof(T));
-  const int first = part * p.units;                                 // the part's first unit
-  const int last = min(first + p.units, (p.vocab + lead + kUnit - 1) / kUnit);
-  const int lo = max(first * kUnit - lead, 0), hi = min((first + p.units) * kUnit - lead, p.vocab);   // its tokens
+// A part of a row.  Units of eight tokens lie on 16-byte boundaries of the row's memory.  The up to 14 tokens before the first and
+// behind the last one, the row's edges, are part 0's, one a thread.
+template <typename T>
+struct RowPart {
+  const T* in;
+  int head, units, first, last, edges, part;
+  __device__ __forceinline__ RowPart(const TokenParams& p, int row, int part_) : part(part_) {
+    in = (const T*)p.in + row * p.in_stride;
+    head = min((int)((16 - ((uintptr_t)in & 15)) & 15) / (int)sizeof(T), p.vocab);
+    units = (p.vocab - head) / kUnit;
+    first = part * p.units;
+    last = min(first + p.units, units);
+    edges = part == 0 ? p.vocab - units * kUnit : 0;
+  }
+  __device__ __forceinline__ bool owns(int t) const {
+    const int u = (t - head) >> 3;
+    return u < 0 || u >= units ? part == 0 : u >= first && u < last;
+  }
+  __device__ __forceinline__ int edge(int i) const { return i < head ? i : i + units * kUnit; }
+};
 
-  Raw8<T> raw[kUnits];
-  auto load_tile = [&](int tile) {
+// Behind the tile, for alternatives.  Keys order by (logit, lowest index first); 0 is none.
+struct TopShared {
+  unsigned long long cand[kCandidates], few[kCandidates], best[PG_TOKEN_MAX_TOP];
+  float bounds[2][kTokWarps];
+  unsigned int hist[256];
+  unsigned long long prefix;
+  int count, kept, left, shift;
+
+  __device__ __forceinline__ void push(float x, int id) {
+    if (!(x > -INFINITY)) return;
+    const int at = atomicAdd(&count, 1);
+    if (at < kCandidates) cand[at] = top_key(x, id);
+  }
+  // The n largest keys of the part into `best`, in order; by all threads.
+  template <typename T>
+  __device__ void select(const RowPart<T>& at, int vocab, int n, float bound);
+};
+
+template <typename T>
+__device__ __noinline__ void TopShared::select(const RowPart<T>& at, int vocab, int n, float bound) {
+  const int tid = threadIdx.x;
+  if (tid == 0) kept = 0;
+  __syncthreads();
+  int total = count;
+  if (total > kCandidates) {
+    // Many equal logits: the n-th largest key of the part, from memory, eight bits at a time, until few enough reach it.
+    auto each = [&](auto f) {
+      for (int t = at.head + at.first * kUnit + tid; t < at.head + at.last * kUnit; t += kTokThreads) {
+        const float x = to_float(at.in[t]);
+        if (x > -INFINITY) f(top_key(x, t));
+      }
+      if (tid < at.edges) {
+        const float x = to_float(at.in[at.edge(tid)]);
+        if (x > -INFINITY) f(top_key(x, at.edge(tid)));
+      }
+    };
+    if (tid == 0) {
+      prefix = 0;
+      left = n;
+    }
+    __syncthreads();
+    for (int by = 56; by >= 0; by -= 8) {
+      hist[tid] = 0;
+      __syncthreads();
+      const unsigned long long before = prefix;
+      each([&](unsigned long long key) {
+        if (by == 56 || key >> (by + 8) == before) atomicAdd(&hist[key >> by & 255], 1u);
+      });
+      __syncthreads();
+      if (tid == 0) {
+        int want = left, b = 255;
+        while (b > 0 && (int)hist[b] < want) want -= hist[b--];
+        prefix = before << 8 | (unsigned)b;
+        shift = by;
+        count = n - want + (int)hist[b] <= kCandidates ? 0 : -1;
+        left = want;
+      }
+      __syncthreads();
+      if (count == 0) break;
+    }
+    const unsigned long long from = prefix << shift;
+    __syncthreads();
+    each([&](unsigned long long key) {
+      if (key >= from) cand[atomicAdd(&count, 1) & (kCandidates - 1)] = key;
+    });
+    __syncthreads();
+    total = count;
+    bound = -INFINITY;
+  }
+  // What earlier tiles let through may lie below the last bound.
+  const unsigned long long from = bound == -INFINITY ? 0 : top_key(bound, 0x7FFFFFFF);
+  for (int i = tid; i < total; i += kTokThreads)
+    if (cand[i] >= from) few[atomicAdd(&kept, 1)] = cand[i];
+  for (int i = tid; i < n; i += kTokThreads) best[i] = 0;
+  __syncthreads();
+  const int k = kept;
+  if (tid == 0) few[min(k, kCandidates - 1)] = k < kCandidates ? 0 : few[kCandidates - 1];
+  __syncthreads();
+  for (int i = tid; i < k; i += kTokThreads) {
+    const unsigned long long key = few[i];
+    int rank = 0;
+    for (int j = 0; j < k; j += 2) {
+      const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&few[j]);
+      rank += (o.x > key) + (o.y > key);
+    }
+    if (rank < n) best[rank] = key;
+  }
+  __syncthreads();
+}
+
+// What a thread knows of its given token and of its entry of the teacher's list (-1: none, padding, unused).
+struct Entry {
+  int id, tid;
+  float x, tx, tl, dl;
+};
+
+// The slope for the stream: y = l c - r in one rounding, with r = ref c + l2 rounded; what the roundings of r leave, up to 1e-6 of
+// every p_v, is a factor of a and b.
+struct Slope2 {
+  f2 c, nr, a, b;
+  __device__ __forceinline__ Slope2(const TokenSlope& k, float c_) {
+    const float mc = k.ref * c_, r = mc + k.l2;
+    const float back = r - mc, off = fmaf(k.ref, c_, -mc) + ((mc - (r - back)) + (k.l2 - back));   // ref c + l2 - r
+    const float f = ex2(-off), bl = k.b * kLn2;
+    c = make2(c_, c_);
+    nr = make2(-r, -r);
+    const float af = f * fmaf(-off, bl, k.a), bf = f * bl;
+    a = make2(af, af);
+    b = make2(bf, bf);
+  }
+};
+template <typename T, bool kEnt>
+__device__ __forceinline__ void slope8(const Raw8<T>& r, const Slope2& k, float (&g)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float y0, y1;
+    split2(fma2(pair_of(r, i), k.c, k.nr), y0, y1);
+    const f2 e = make2(ex2(y0), ex2(y1));
+    f2 f = k.a;
+    if (kEnt) f = fma2(make2(fmaxf(y0, kFloorY), fmaxf(y1, kFloorY)), k.b, k.a);
+    split2(mul2(e, f), g[2 * i], g[2 * i + 1]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void put8(T* to, const float (&g)[8], bool aligned) {
+  if (aligned) {
+    store8(to, g);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) to[i] = from_float<T>(g[i]);
+  }
+}
+// A part whose reference is that far down, from memory: differences first.
+template <typename T>
+__device__ __noinline__ void slope_huge(const RowPart<T>& at, T* dl, const TokenSlope& k, float c) {
+  for (int t = at.head + at.first * kUnit + threadIdx.x; t < at.head + at.last * kUnit; t += kTokThreads) {
+    const float y = (to_float(at.in[t]) - k.ref) * c - k.l2;
+    dl[t] = from_float<T>(ex2(y) * fmaf(fmaxf(y, kFloorY), k.b * kLn2, k.a));
+  }
+}
+template <typename T>
+__device__ __forceinline__ void put_edge(T* to, float x, const TokenSlope& k, float c) {
+  const float y = (x - k.ref) * c - k.l2;
+  *to = from_float<T>(ex2(y) * fmaf(fmaxf(y, kFloorY), k.b * kLn2, k.a));
+}
+
+// By one warp: the gradient's slope from what is known of the row.
+__device__ __forceinline__ TokenSlope slope_of(const TokenRow& r, bool rest, int kind, float lp_part, float dh, float dd, float inv) {
+  TokenSlope k;
+  if (rest) {
+    const bool outside = r.lr > -INFINITY;
+    const float pr = outside ? expf(r.lr) : 0.f, lr = outside ? r.lr : 0.f;
+    const float dist = kind == PG_DISTILL_FORWARD_REST ? pr * r.w - expf(r.lt) : pr * (lr - r.lt - r.loss);
+    k.a = outside || r.lr != r.lr ? inv * (pr * (lp_part - dh * lr) + dd * dist) : 0.f;
+    k.b = -inv * dh * pr;
+    k.ref = r.mr;
+    k.l2 = r.l2r;
+  } else {
+    k.a = inv * (lp_part + dd * r.w);
+    k.b = -inv * dh;
+    k.ref = r.m;
+    k.l2 = r.l2;
+  }
+  if (r.some == 0.f) k.a = k.b = 0.f;
+  return k;
+}
+
+// Given and listed tokens, over what the stream has written.
+template <typename T>
+__device__ __forceinline__ void fix_tokens(const TokenShared& s, const RowPart<T>& at, const Entry& e, const TokenRow& r, T* dl, int n_ids,
+                                           int n_list, bool fix_list, bool rest, bool distill, int kind, float lp_part, float dh, float dd,
+                                           float inv) {
+  const int tid = threadIdx.x;
+  const float c = inv * kLog2e;
+  auto base = [&](float pv, float lp) { return pv == 0.f ? 0.f : pv * (lp_part - dh * lp); };
+  if (fix_list && e.tid >= 0 && at.owns(e.tid)) {
+    const float y = (e.tx - r.m) * c - r.l2, pv = ex2(y), lp = kLn2 * y;
+    float dist;
+    if (kind == PG_DISTILL_FORWARD) dist = r.w * pv - expf(e.tl - r.lt);
+    else if (kind == PG_DISTILL_FORWARD_REST) dist = r.w * pv - expf(e.tl);
+    else dist = pv == 0.f ? 0.f : pv * (lp - e.tl - r.loss);
+    float sum = base(pv, lp) + dd * dist;
+    for (int j = 0; j < n_ids; ++j)
+      if (s.gid[j] == e.tid) sum += s.gdl[j];
+    dl[e.tid] = from_float<T>(r.some != 0.f ? inv * sum : 0.f);
+  }
+  if (e.id >= 0 && at.owns(e.id)) {
+    bool mine = true;                                               // the last of its token, and not on the list
+    for (int j = tid + 1; j < n_ids; ++j) mine &= s.gid[j] != e.id;
+    if (fix_list)
+      for (int j = 0; j < n_list; ++j) mine &= s.tid[j] != e.id;
+    if (mine) {
+      const float y = (e.x - r.m) * c - r.l2, pv = ex2(y);
+      float sum = base(pv, kLn2 * y);
+      if (!rest) sum += dd * r.w * pv;
+      else if (distill) {                                           // outside the list
+        const float rv = ex2((e.x - r.mr) * c - r.l2r), pr = expf(r.lr);
+        sum += dd * rv * (kind == PG_DISTILL_FORWARD_REST ? pr * r.w - expf(r.lt) : pr * (r.lr - r.lt - r.loss));
+      }
+      for (int j = 0; j <= tid; ++j)
+        if (s.gid[j] == e.id) sum += s.gdl[j];
+      dl[e.id] = from_float<T>(r.some != 0.f ? inv * sum : 0.f);
+    }
+  }
+}
+
+// Whether a later entry of the list has the same id: of those the last one counts.
+__device__ __forceinline__ bool again_later(const TokenShared& s, int id, int n_list) {
+  const int tid = threadIdx.x;
+  bool later = false;
+  for (int j = tid & ~3; j < n_list; j += 4) {
+    const int4 o = *reinterpret_cast<const int4*>(&s.tid[j]);
+    later |= (o.x == id && j > tid) || (o.y == id && j + 1 > tid) || (o.z == id && j + 2 > tid) || (o.w == id && j + 3 > tid);
+  }
+  return later;
+}
+
+// The n-th largest of the warp's values, 1 <= n <= 32.
+__device__ __forceinline__ float nth_largest(float v, int n) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+    for (int j = k >> 1; j; j >>= 1) {
+      const float o = __shfl_xor_sync(~0u, v, j);
+      v = ((lane & j) == 0) == ((lane & k) == 0) ? fmaxf(v, o) : fminf(v, o);
+    }
+  return __shfl_sync(~0u, v, n - 1);
+}
+
+template <typename T> constexpr int kTokUnits = sizeof(T) == 4 ? 4 : 8;          // units of a thread and tile
+template <typename T> constexpr int kTileUnits = kTokUnits<T> * kTokThreads;
+
+// The thread's units of a tile; -inf where the part has none.  Streamed: read for the last time.
+template <typename T, bool kStreamed>
+__device__ __forceinline__ void load_tile(const RowPart<T>& at, int tile, Raw8<T> (&raw)[kTokUnits<T>]) {
+  constexpr int kUnits = kTokUnits<T>;
+  const int u0 = at.first + tile * kTileUnits<T> + (int)threadIdx.x;
+  const uint4* from = (const uint4*)(at.in + at.head + (int64_t)u0 * kUnit);
+  constexpr int kStep = kTokThreads * (int)sizeof(Raw8<T>) / 16;
+  if (at.first + (tile + 1) * kTileUnits<T> <= at.last) {           // all of them
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j)
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j].v[i] = kStreamed ? __ldcs(from + j * kStep + i) : from[j * kStep + i];
+  } else {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
-      const int u = first + tile * kTile + j * kTokThreads + tid;
-      const int t0 = u * kUnit - lead;
-      if (u < last && t0 >= 0 && t0 + kUnit <= p.vocab) {
-        load8(in + t0, raw[j]);
-      } else {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(Raw8<T>) / 4; ++i) word_of(raw[j], i) = Empty8<T>::word;
-        if (u < last) {                                             // cut by the row's ends
+      for (int i = 0; i < (int)sizeof(Raw8<T>) / 4; ++i) word_of(raw[j], i) = Empty8<T>::word;
+      if (u0 + j * kTokThreads < at.last)
 #pragma unroll
-          for (int k = 0; k < kUnit; ++k) {
-            if (t0 + k < 0 || t0 + k >= p.vocab) continue;
-            const T x = in[t0 + k];
-            if constexpr (sizeof(T) == 4) word_of(raw[j], k) = __float_as_uint(x);
-            else {
-              const uint32_t b = *reinterpret_cast<const uint16_t*>(&x);
-              uint32_t& w = word_of(raw[j], k >> 1);
-              w = k & 1 ? (w & 0xFFFFu) | b << 16 : (w & 0xFFFF0000u) | b;
-            }
-          }
-        }
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j].v[i] = kStreamed ? __ldcs(from + j * kStep + i) : from[j * kStep + i];
+    }
+  }
+}
+
+// Forward, with the gradient on top (kGrad).
+template <typename T, bool kGrad, bool kEnt, bool kRest>
+__global__ void __launch_bounds__(kTokThreads, kTokCtas)
+token_kernel(const __grid_constant__ TokenParams p) {
+  constexpr int kUnits = kTokUnits<T>, kTile = kTileUnits<T>;
+  __shared__ TokenShared s;
+  extern __shared__ __align__(16) unsigned char more[];             // TopShared and the parts' lists if there are alternatives; bits (kRest)
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int row = blockIdx.x / p.parts;
+  const RowPart<T> at(p, row, blockIdx.x - row * p.parts);
+  const bool many = p.parts > 1;
+  if (many) cluster_arrive();                                       // all CTAs run before one writes into another's memory
+  const int n_ids = p.t.n_ids, n_list = p.t.n_teacher, n_top = p.t.n_top;
+  const int lists = (n_list + 31) / 32;
+  TopShared& top = *reinterpret_cast<TopShared*>(more);
+  unsigned long long* const merge = reinterpret_cast<unsigned long long*>(more + sizeof(TopShared));
+  uint32_t* const bits = reinterpret_cast<uint32_t*>(more + (n_top ? (int)sizeof(TopShared) + (many ? kMergeBytes : 0) : 0));
+
+  Raw8<T> raw[kUnits];
+  load_tile<T, !kGrad>(at, 0, raw);
+  const float inv = p.t.temperature ? 1.f / p.t.temperature[row] : 1.f, c = inv * kLog2e;
+  const float dh = kGrad && p.g.dentropy ? p.g.dentropy[row] * p.g.entropy_scale : 0.f;
+  const float dd = kGrad && p.g.ddistill ? p.g.ddistill[row] * p.g.distill_scale : 0.f;
+  const float edge_x = tid < at.edges ? to_float(at.in[at.edge(tid)]) : -INFINITY;
+  Entry my = {-1, -1, 0.f, -INFINITY, 0.f, 0.f};
+  if (tid < n_ids) {
+    const int id = p.t.ids[(int64_t)row * n_ids + tid];
+    if ((unsigned int)id < (unsigned int)p.vocab) {
+      my.id = id;
+      my.x = to_float(at.in[id]);
+      if (kGrad && p.g.dlogp) my.dl = p.g.dlogp[(int64_t)row * n_ids + tid];
+    }
+    s.gid[tid] = my.id;
+    s.gdl[tid] = my.dl;
+  }
+  if (tid < n_list) {
+    const int id = p.t.teacher_ids[(int64_t)row * n_list + tid];
+    my.tl = p.t.teacher_logp[(int64_t)row * n_list + tid];
+    if ((unsigned int)id < (unsigned int)p.vocab && !(my.tl == -INFINITY)) {
+      my.tid = id;
+      my.tx = to_float(at.in[id]);
+    }
+  }
+  if (tid < (n_list + 3 & ~3)) s.tid[tid] = my.tid;
+  if (kGrad && warp < (n_ids + 31) / 32) {
+    const float d = warp_total(my.dl);
+    if (lane == 0) s.dsum[warp] = d;
+  }
+  if constexpr (kRest)
+    for (int i = tid; i < (p.units + 3) / 4; i += kTokThreads) bits[i] = 0;
+  if (tid == 0) {
+    if (kRest) s.edges = 0;
+    if (n_top) top.count = 0;                                       // synchronised by the first tile's bound
+  }
+  if (n_list > 0) {
+    __syncthreads();
+    if (my.tid >= 0) {
+      if (again_later(s, my.tid, n_list)) my.tid = -1;
+      else if (kRest && at.owns(my.tid)) {
+        const int t = my.tid - at.head, u = t >> 3;
+        if (u < 0 || u >= at.units) atomicOr(&s.edges, 1u << (u < 0 ? my.tid : my.tid - at.units * kUnit));
+        else atomicOr(&bits[(t - at.first * kUnit) >> 5], 1u << ((t - at.first * kUnit) & 31));
       }
     }
-  };
-  auto mask_tile = [&](int tile) {                                  // takes the listed tokens out
+    if (kRest) __syncthreads();
+  }
+  // Takes the listed tokens out of the registers.
+  auto mask_tile = [&](int tile) {
     if constexpr (kRest) {
 #pragma unroll
       for (int j = 0; j < kUnits; ++j) {
@@ -359,74 +690,22 @@ token_kernel(const __grid_constant__ TokenParams p) {
       }
     }
   };
-
-  const float inv = p.t.temperature ? 1.f / p.t.temperature[row] : 1.f, c = inv * kLog2e;
-  if constexpr (kMode != kBackward) load_tile(0);
-
-  // given and listed tokens, one a thread
-  int my_id = -1, my_tid = -1;
-  float my_x = 0.f, my_tx = -INFINITY, my_tl = 0.f, my_dl = 0.f;
-  if (tid < n_ids) {
-    const int id = p.t.ids[(int64_t)row * n_ids + tid];
-    if ((unsigned int)id < (unsigned int)p.vocab) {
-      my_id = id;
-      if (kMode != kBackward || (id >= lo && id < hi)) my_x = to_float(in[id]);
-      if (kMode != kForward && p.g.dlogp) my_dl = p.g.dlogp[(int64_t)row * n_ids + tid];
+  // The thread's units of a tile whose logits are all that far down, from memory: differences first.
+  auto sum_huge = [&](const RowPart<T>& at, const uint32_t* bits, float m, float c, int tile, float& s0, float& s1) {
+    for (int u = tile * kTile + tid; u < (tile + 1) * kTile && at.first + u < at.last; u += kTokThreads) {
+      for (int k = 0; k < kUnit; ++k) {
+        if (kRest && reinterpret_cast<const uint8_t*>(bits)[u] >> k & 1) continue;
+        const float y = (to_float(at.in[at.head + (at.first + u) * kUnit + k]) - m) * c, e = ex2(y);
+        s0 += e;
+        s1 += e * fmaxf(y, kFloorY);
+      }
     }
-    s.gid[tid] = my_id;
-    s.gdl[tid] = my_dl;
-  }
-  if (tid < n_list) {
-    const int id = p.t.teacher_ids[(int64_t)row * n_list + tid];
-    my_tl = p.t.teacher_logp[(int64_t)row * n_list + tid];
-    if ((unsigned int)id < (unsigned int)p.vocab && !(my_tl == -INFINITY)) my_tid = id;
-    s.tid[tid] = my_tid;
-    if (my_tid >= 0 && (kMode != kBackward || (my_tid >= lo && my_tid < hi))) my_tx = to_float(in[my_tid]);
-  }
-  if (kMode != kForward && warp < PG_TOKEN_MAX_LIST / 32) {
-    const float d = warp_total(my_dl);
-    if (lane == 0) s.dsum[warp] = d;
-  }
-  if constexpr (kRest)
-    for (int i = tid; i < (p.units + 3) / 4; i += kTokThreads) bits[i] = 0;
-  if (n_ids + n_list > 0 || kRest) __syncthreads();
-  if (my_tid >= 0) {
-    bool later = false;                                             // of entries with the same id the last one counts
-    for (int j = tid + 1; j < n_list; ++j) later |= s.tid[j] == my_tid;
-    if (later) my_tid = -1;
-    else if (kRest && my_tid >= lo && my_tid < hi) {
-      const int at = my_tid + lead - first * kUnit;
-      atomicOr(&bits[at >> 5], 1u << (at & 31));
-    }
-  }
-  if (kMode != kBackward && warp < lists) {
-    const bool used = my_tid >= 0;
-    const float x = used ? my_tx : -INFINITY;
-    ListSums l;
-    l.m = warp_most(x);
-    const float y = (x - finite_ref(l.m)) * c, e = used ? ex2(y) : 0.f;
-    l.s0 = warp_total(e);
-    l.s1 = warp_total(e * fmaxf(y, kFloorY));
-    l.etl = warp_total(e != 0.f ? e * my_tl : 0.f);
-    l.tm = p.t.kind == PG_DISTILL_FORWARD ? warp_most(used ? my_tl : -INFINITY) : 0.f;
-    const float t = used ? expf(my_tl - finite_ref(l.tm)) : 0.f;
-    l.ts = warp_total(t);
-    l.ttl = warp_total(t != 0.f ? t * (my_tl - finite_ref(l.tm)) : 0.f);
-    l.ty = warp_total(t != 0.f ? t * (x - finite_ref(l.m)) * inv : 0.f);
-    l.mass = kRest ? warp_total(used ? exp((double)my_tl) : 0.) : 0.;
-    if (lane == 0) s.list[warp] = l;
-  }
-  // the threads' own columns of the list are done with; s.tid keeps the ids that count
-  if (n_list > 0) {
-    __syncthreads();
-    if (tid < n_list) s.tid[tid] = my_tid;
-  }
+  };
 
-  TokenRow r;
-  if constexpr (kMode != kBackward) {
-    mask_tile(0);
-    float m = -INFINITY, s0 = 0.f, s1 = 0.f;
-    for (int tile = 0;;) {
+    float m = -INFINITY, s0 = 0.f, s1 = 0.f, bound = -INFINITY;
+    for (int tile = 0; tile < p.tiles; ++tile) {
+      if (tile > 0) load_tile<T, !kGrad>(at, tile, raw);
+      mask_tile(tile);
       uint32_t w = Empty8<T>::word;
 #pragma unroll
       for (int j = 0; j < kUnits; ++j) {
@@ -434,187 +713,139 @@ token_kernel(const __grid_constant__ TokenParams p) {
         for (int i = 0; i < (int)sizeof(Raw8<T>) / 4; ++i) w = max2(w, word_of(raw[j], i), T());
       }
       const float tm = max_of<T>(w);
-      refer(m, tm, c, s0, s1);
+      refer(m, fmaxf(m, tm), c, s0, s1);
       m = fmaxf(m, tm);
-      const float ref = finite_ref(m);
-      const f2 nref = make2(-ref, -ref), c2 = make2(c, c);
-      f2 a0 = make2(s0, 0.f), a1 = make2(s1, 0.f), b0 = make2(0.f, 0.f), b1 = b0;
+      if (m < -kHuge && m > -INFINITY) {
+        sum_huge(at, bits, m, c, tile, s0, s1);
+      } else {
+        // y = l c - r in one rounding; what r = m c rounded is off by is taken back from the sums
+        const float ref = finite_ref(m), r = ref * c, off = fmaf(ref, c, -r);
+        const f2 nr = make2(-r, -r), c2 = make2(c, c);
+        f2 a0 = make2(0.f, 0.f), a1 = a0, b0 = a0, b1 = a0;
 #pragma unroll
-      for (int j = 0; j < kUnits; ++j) {
-        if (tile * kTile + j * kTokThreads >= p.units) break;
+        for (int j = 0; j < kUnits; ++j) {
+          if (tile * kTile + j * kTokThreads >= p.units) break;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float y0, y1;
-          split2(mul2(add2(pair_of(raw[j], i), nref), c2), y0, y1);
-          const f2 e = make2(ex2(y0), ex2(y1));
-          if (i & 1) b0 = add2(b0, e);
-          else a0 = add2(a0, e);
-          if (kEnt) {
-            const f2 y = make2(fmaxf(y0, kFloorY), fmaxf(y1, kFloorY));
-            if (i & 1) b1 = fma2(e, y, b1);
-            else a1 = fma2(e, y, a1);
+          for (int i = 0; i < 4; ++i) {
+            float y0, y1;
+            split2(fma2(pair_of(raw[j], i), c2, nr), y0, y1);
+            const f2 e = make2(ex2(y0), ex2(y1));
+            if (i & 1) b0 = add2(b0, e);
+            else a0 = add2(a0, e);
+            if (kEnt) {
+              const f2 y = make2(fmaxf(y0, kFloorY), fmaxf(y1, kFloorY));
+              if (i & 1) b1 = fma2(e, y, b1);
+              else a1 = fma2(e, y, a1);
+            }
           }
         }
+        float u, v, t0, t1;
+        split2(add2(a0, b0), u, v);
+        t0 = u + v;
+        split2(add2(a1, b1), u, v);
+        t1 = u + v;
+        const float f = ex2(-off);
+        s0 += f * t0;
+        if (kEnt) s1 += f * fmaf(-off, t0, t1);
       }
-      float u, v;
-      split2(add2(a0, b0), u, v);
-      s0 = u + v;
-      split2(add2(a1, b1), u, v);
-      s1 = u + v;
-      if (++tile == p.tiles) break;
-      load_tile(tile);
-      mask_tile(tile);
-    }
-    const float own = m;                                             // the thread's largest
-    m = warp_most(m);
-    refer(own, m, c, s0, s1);
-    s0 = warp_total(s0);
-    if (kEnt) s1 = warp_total(s1);
-    if (lane == 0) {
-      s.wm[warp] = m;
-      s.ws0[warp] = s0;
-      s.ws1[warp] = s1;
-    }
-    if (n_top) {
-      top.tmax[tid] = own;
-      if (tid == 0) {
-        top.count = 0;
-        top.bound = -INFINITY;
-      }
-    }
-    __syncthreads();
-    if (warp == 0) {
-      float wm = lane < kTokWarps ? s.wm[lane] : -INFINITY, a = lane < kTokWarps ? s.ws0[lane] : 0.f, b = lane < kTokWarps ? s.ws1[lane] : 0.f;
-      const float cm = warp_most(wm);
-      refer(wm, cm, c, a, b);
-      a = warp_total(a);
-      b = warp_total(b);
-      if (!many) {
-        if (lane == 0) {
-          s.part[0][0] = cm;
-          s.part[0][1] = a;
-          s.part[0][2] = b;
-        }
-      }
-      m = cm;
-      s0 = a;
-      s1 = b;
-    }
-    if (n_top) {
-      // the n_top-th largest of the threads' maxima
-      const float mine = top.tmax[tid];
-      int above = 0;
-      for (int j = 0; j < kTokThreads; j += 4) {
-        const float4 o = *reinterpret_cast<const float4*>(&top.tmax[j]);
-        above += (o.x > mine || (o.x == mine && j < tid)) + (o.y > mine || (o.y == mine && j + 1 < tid)) +
-                 (o.z > mine || (o.z == mine && j + 2 < tid)) + (o.w > mine || (o.w == mine && j + 3 < tid));
-      }
-      if (above == n_top - 1) top.bound = mine;
-      __syncthreads();
-      const float bound = top.bound;
-      // f(logit, token) for every logit of the part that is an alternative
-      auto each = [&](auto f) {
-        for (int tile = p.tiles - 1; tile >= 0; --tile) {
-          if (p.tiles > 1) {
-            load_tile(tile);
-            mask_tile(tile);
-          }
+      if (n_top) {
+        // every warp has as many threads with a logit at or above its own bound that all of them make n_top
+        const float wb = nth_largest(m, (n_top + kTokWarps - 1) / kTokWarps);
+        if (lane == 0) top.bounds[tile & 1][warp] = wb;
+        __syncthreads();
+        bound = INFINITY;
+#pragma unroll
+        for (int i = 0; i < kTokWarps; ++i) bound = fminf(bound, top.bounds[tile & 1][i]);
+        if (tm >= bound) {
 #pragma unroll
           for (int j = 0; j < kUnits; ++j) {
-            const int t0 = (first + tile * kTile + j * kTokThreads + tid) * kUnit - lead;
+            uint32_t v = word_of(raw[j], 0);
+#pragma unroll
+            for (int i = 1; i < (int)sizeof(Raw8<T>) / 4; ++i) v = max2(v, word_of(raw[j], i), T());
+            if (!(max_of<T>(v) >= bound)) continue;
+            const int t0 = at.head + (at.first + tile * kTile + j * kTokThreads + tid) * kUnit;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               float x0, x1;
               split2(pair_of(raw[j], i), x0, x1);
-              if (x0 > -INFINITY) f(x0, t0 + 2 * i);
-              if (x1 > -INFINITY) f(x1, t0 + 2 * i + 1);
+              if (x0 >= bound) top.push(x0, t0 + 2 * i);
+              if (x1 >= bound) top.push(x1, t0 + 2 * i + 1);
             }
           }
         }
-        if (kRest && my_tid >= lo && my_tid < hi && my_tx > -INFINITY) f(my_tx, my_tid);
-      };
-      auto each_again = [&](auto f) {                               // from memory, for the rare path below
-        for (int t = lo + tid; t < hi; t += kTokThreads) {
-          const float x = to_float(in[t]);
-          if (x > -INFINITY) f(x, t);
-        }
-      };
-      auto push = [&](unsigned long long key) {
-        const int at = atomicAdd(&top.count, 1);
-        if (at < kCandidates) top.cand[at] = key;
-      };
-      if (own >= bound || (kRest && my_tx >= bound))
-        each([&](float x, int id) { if (x >= bound) push(top_key(x, id)); });
-      __syncthreads();
-      if (top.count > kCandidates) {
-        // Many equal logits: the n_top-th largest key, eight bits at a time, until few enough reach it.
-        __syncthreads();
-        if (tid == 0) {
-          top.prefix = 0;
-          top.left = n_top;
-          top.shift = 64;
-        }
-        __syncthreads();
-        for (int shift = 56; shift >= 0; shift -= 8) {
-          if (tid < 256) top.hist[tid] = 0;
-          __syncthreads();
-          const unsigned long long prefix = top.prefix;
-          each_again([&](float x, int id) {
-            const unsigned long long key = top_key(x, id);
-            if (shift == 56 || key >> (shift + 8) == prefix) atomicAdd(&top.hist[key >> shift & 255], 1u);
-          });
-          __syncthreads();
-          if (tid == 0) {
-            int left = top.left, b = 255;
-            while (b > 0 && (int)top.hist[b] < left) left -= top.hist[b--];
-            top.prefix = prefix << 8 | (unsigned)b;
-            top.shift = shift;
-            const bool few = n_top - left + (int)top.hist[b] <= kCandidates;
-            top.left = left;
-            top.count = few ? 0 : -1;
-          }
-          __syncthreads();
-          if (top.count == 0) break;
-        }
-        const unsigned long long from = top.prefix << top.shift;
-        __syncthreads();
-        each_again([&](float x, int id) {
-          const unsigned long long key = top_key(x, id);
-          if (key >= from) push(key);
-        });
-        __syncthreads();
       }
-      const int n = min(top.count, kCandidates);
-      for (int i = tid; i < n_top; i += kTokThreads)
-        if (i >= n) top.best[i] = 0;
-      for (int i = tid; i < n; i += kTokThreads) {
-        const unsigned long long key = top.cand[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += top.cand[j] > key;
-        if (rank < n_top) top.best[rank] = key;
-      }
-      __syncthreads();
     }
+    if (at.edges > 0) {
+      const float x = kRest && tid < at.edges && s.edges >> tid & 1 ? -INFINITY : edge_x;
+      const float to = fmaxf(m, x), y = (x - finite_ref(to)) * c, e = ex2(y);
+      refer(m, to, c, s0, s1);
+      m = to;
+      s0 += e;
+      s1 += e * fmaxf(y, kFloorY);
+      if (n_top && x >= bound) top.push(x, at.edge(tid));
+    }
+    if (kRest && n_top && my.tid >= 0 && my.tx >= bound && at.owns(my.tid)) top.push(my.tx, my.tid);
+    if (warp < lists) {
+      const bool used = my.tid >= 0;
+      const float x = used ? my.tx : -INFINITY;
+      ListSums l;
+      l.m = warp_most(x);
+      const float y = (x - finite_ref(l.m)) * c, e = used ? ex2(y) : 0.f;
+      l.s0 = warp_total(e);
+      l.s1 = warp_total(e * fmaxf(y, kFloorY));
+      l.etl = warp_total(e != 0.f ? e * my.tl : 0.f);
+      l.tm = p.t.kind == PG_DISTILL_FORWARD ? warp_most(used ? my.tl : -INFINITY) : 0.f;
+      const float t = used ? expf(my.tl - finite_ref(l.tm)) : 0.f;
+      l.ts = warp_total(t);
+      l.ttl = warp_total(t != 0.f ? t * (my.tl - finite_ref(l.tm)) : 0.f);
+      l.ty = warp_total(t != 0.f ? t * (x - finite_ref(l.m)) * inv : 0.f);
+      l.mass = kRest ? warp_total(used ? exp((double)my.tl) : 0.) : 0.;
+      if (lane == 0) s.list[warp] = l;
+    }
+    {
+      const float own = m;
+      m = warp_most(m);
+      refer(own, m, c, s0, s1);
+      s0 = warp_total(s0);
+      if (kEnt) s1 = warp_total(s1);
+    }
+    if (n_top) top.select(at, p.vocab, n_top, bound);
+    // the triples of the parts' warps, to all parts
+    float4* const triples = s.part;
     if (many) {
       cluster_wait();
-      if (warp == 0 && lane < p.parts) {
-        const uint32_t at = peer(&s.part[part][0], lane);
-        peer_store(at, m);
-        peer_store(at + 4, s0);
-        peer_store(at + 8, s1);
-      }
-      for (int i = tid; i < n_top; i += kTokThreads) peer_store(peer(&top.merge[part][i], 0), top.best[i]);
+      if (lane < p.parts) peer_store(peer(&triples[at.part * kTokWarps + warp], lane), m, s0, s1);
+      for (int i = tid; i < n_top; i += kTokThreads) peer_store(peer(merge + at.part * PG_TOKEN_MAX_TOP + i, 0), top.best[i]);
       __syncwarp();
       cluster_arrive();
       cluster_wait();
     } else {
+      if (lane == 0) triples[warp] = make_float4(m, s0, s1, 0.f);
       __syncthreads();
     }
-    r = finish_row(s, p.parts, lists, kRest, p.t.kind, inv);
-    if (part == 0) {
+    TokenRow r;
+    if (warp == 0) {
+      r = finish_row(s, triples, p.parts, lists, kRest, p.t.kind, inv);
+      float lp_part = 0.f;
+      TokenSlope k = {};
+      if (kGrad) {
+        float d = 0.f;
+        for (int i = 0; i < (n_ids + 31) / 32; ++i) d += s.dsum[i];
+        lp_part = -fmaf(dh, r.h, d);                                // of p_v (.. - dh ln p_v)
+        k = slope_of(r, kRest, p.t.kind, lp_part, dh, dd, inv);
+      }
+      if (lane == 0) {
+        s.row = r;
+        s.slope = k;
+        s.lp_part = lp_part;
+      }
+    }
+    __syncthreads();
+    r = s.row;
+    if (at.part == 0) {
       if (tid < n_ids && p.o.logp) {
-        const float lp = r.some != 0.f ? (my_x - r.m) * inv - kLn2 * r.l2 : -INFINITY;
-        p.o.logp[(int64_t)row * n_ids + tid] = my_id >= 0 ? lp : 0.f;
+        const float lp = r.some != 0.f ? (my.x - r.m) * inv - kLn2 * r.l2 : -INFINITY;
+        p.o.logp[(int64_t)row * n_ids + tid] = my.id >= 0 ? lp : 0.f;
       }
       if (tid == 0) {
         if (p.o.lse) p.o.lse[row] = r.some != 0.f ? r.m * inv + kLn2 * r.l2 : -INFINITY;
@@ -624,8 +855,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
       }
       if (n_top) {
         auto write = [&](int at, unsigned long long key) {
-          const uint32_t b = (uint32_t)(key >> 32);
-          const float x = __uint_as_float(b >> 31 ? b ^ 0x80000000u : ~b);
+          const float x = key_value(key);
           p.o.top_ids[(int64_t)row * n_top + at] = key ? (int)(0xFFFFFFFFu - (uint32_t)key) : -1;
           if (p.o.top_logp) p.o.top_logp[(int64_t)row * n_top + at] = key ? (x - r.m) * inv - kLn2 * r.l2 : -INFINITY;
         };
@@ -633,179 +863,156 @@ token_kernel(const __grid_constant__ TokenParams p) {
           for (int i = tid; i < n_top; i += kTokThreads) write(i, top.best[i]);
         } else {
           // the parts' lists are sorted: a key's rank is its own place and how many of each other list are above it
+          const unsigned long long* from = merge;
+          auto above = [&](int o, unsigned long long key) {
+            int a = 0, b = n_top;
+            while (a < b) {
+              const int mid = (a + b) >> 1;
+              if (from[o * PG_TOKEN_MAX_TOP + mid] > key) a = mid + 1;
+              else b = mid;
+            }
+            return a;
+          };
           for (int i = tid; i < n_top * p.parts; i += kTokThreads) {
             const int q = i / n_top, at = i - q * n_top;
-            const unsigned long long key = top.merge[q][at];
+            const unsigned long long key = from[q * PG_TOKEN_MAX_TOP + at];
+            if (!key) continue;
             int rank = at;
-            if (key) {
-              for (int o = 0; o < p.parts; ++o) {
-                if (o == q) continue;
-                int a = 0, b = n_top;
-                while (a < b) {
-                  const int mid = (a + b) >> 1;
-                  if (top.merge[o][mid] > key) a = mid + 1;
-                  else b = mid;
-                }
-                rank += a;
-              }
-              if (rank < n_top) write(rank, key);
-            }
+            for (int o = 0; o < p.parts; ++o)
+              if (o != q) rank += above(o, key);
+            if (rank < n_top) write(rank, key);
           }
           if (tid < n_top) {                                        // places that are left over
             int some = 0;
-            for (int o = 0; o < p.parts; ++o) {
-              int a = 0, b = n_top;
-              while (a < b) {
-                const int mid = (a + b) >> 1;
-                if (top.merge[o][mid] > 0) a = mid + 1;
-                else b = mid;
-              }
-              some += a;
-            }
+            for (int o = 0; o < p.parts; ++o) some += above(o, 0);
             if (tid >= some) write(tid, 0);
           }
         }
       }
     }
-  } else {
-    r = load_row((const float4*)p.o.saved + (int64_t)row * (PG_TOKEN_SAVED / 4));
-  }
-
-  if constexpr (kMode != kForward) {
-    const float dh = p.g.dentropy ? p.g.dentropy[row] * p.g.entropy_scale : 0.f;
-    const float dd = p.g.ddistill ? p.g.ddistill[row] * p.g.distill_scale : 0.f;
-    const bool rest = kMode == kBackward ? p.g.ddistill && n_list > 0 && p.t.kind != PG_DISTILL_FORWARD : kRest;
-    const bool fix_list = n_list > 0 && (rest || p.g.ddistill);
-    float d = 0.f;
-    if (n_ids > 0)
-      for (int i = 0; i < (n_ids + 31) / 32; ++i) d += s.dsum[i];
-    const float lp_part = -fmaf(dh, r.h, d);                        // of p_v (.. - dh ln p_v)
-    float a, b, ref, l2;
-    if (rest) {
-      const bool outside = r.lr > -INFINITY;
-      const float pr = outside ? expf(r.lr) : 0.f, lr = outside ? r.lr : 0.f;
-      const float dist = p.t.kind == PG_DISTILL_FORWARD_REST ? pr * r.w - expf(r.lt) : pr * (lr - r.lt - r.loss);
-      a = outside || r.lr != r.lr ? inv * (pr * (lp_part - dh * lr) + dd * dist) : 0.f;
-      b = -inv * dh * pr;
-      ref = r.mr;
-      l2 = r.l2r;
-    } else {
-      a = inv * (lp_part + dd * r.w);
-      b = -inv * dh;
-      ref = r.m;
-      l2 = r.l2;
-    }
-    if (r.some == 0.f) a = b = 0.f;
-    bool quiet = false;
-    if constexpr (kMode == kBackward) quiet = !__syncthreads_or(my_dl != 0.f || dh != 0.f || dd != 0.f);
-    if (quiet) a = b = 0.f;
-    T* dl = (T*)p.dl + row * p.dl_stride;
-    const bool aligned = ((uintptr_t)(dl - lead) & 15) == 0;
-    const f2 nref = make2(-ref, -ref), c2 = make2(c, c), nl2 = make2(-l2, -l2), a2 = make2(a, a), b2 = make2(b * kLn2, b * kLn2);
-    const bool kept = p.tiles == 1 || n_top == 0;                   // the last tile, in registers
-    for (int tile = p.tiles - 1; tile >= 0; --tile) {
-      if (kMode == kBackward ? !quiet : tile != p.tiles - 1 || !kept) load_tile(tile);
-      if (kMode == kBackward && quiet) {
+    if constexpr (kGrad) {
+      const TokenSlope slope = s.slope;
+      const Slope2 k(slope, c);
+      T* dl = (T*)p.dl + row * p.dl_stride;
+      const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0;
+      const bool huge = slope.ref < -kHuge;                         // rows masked throughout, by the type's lowest value
+      if (huge) slope_huge(at, dl, slope, c);
+      for (int tile = p.tiles - 1;;) {
+        const int u0 = at.first + tile * kTile + tid;
 #pragma unroll
-        for (int j = 0; j < kUnits; ++j)
-#pragma unroll
-          for (int i = 0; i < (int)sizeof(Raw8<T>) / 4; ++i) word_of(raw[j], i) = Empty8<T>::word;
+        for (int j = 0; j < kUnits; ++j) {
+          if (tile * kTile + j * kTokThreads >= p.units) break;
+          float g[8];
+          slope8<T, kEnt>(raw[j], k, g);
+          if (u0 + j * kTokThreads < at.last && !huge) put8(dl + at.head + (int64_t)(u0 + j * kTokThreads) * kUnit, g, aligned);
+        }
+        if (--tile < 0) break;
+        load_tile<T, true>(at, tile, raw);                          // from the L2 cache
       }
-#pragma unroll
-      for (int j = 0; j < kUnits; ++j) {
-        if (tile * kTile + j * kTokThreads >= p.units) break;
-        const int u = first + tile * kTile + j * kTokThreads + tid;
-        const int t0 = u * kUnit - lead;
-        float g[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          f2 y = fma2(add2(pair_of(raw[j], i), nref), c2, nl2);
-          float y0, y1;
-          split2(y, y0, y1);
-          const f2 e = make2(ex2(y0), ex2(y1));
-          f2 k = a2;
-          if (kEnt) k = fma2(make2(fmaxf(y0, kFloorY), fmaxf(y1, kFloorY)), b2, a2);
-          split2(mul2(e, k), g[2 * i], g[2 * i + 1]);
-        }
-        if (u >= last) continue;
-        if (aligned && t0 >= 0 && t0 + kUnit <= p.vocab) {
-          store8(dl + t0, g);
-        } else {
-#pragma unroll
-          for (int k = 0; k < kUnit; ++k)
-            if (t0 + k >= 0 && t0 + k < p.vocab) dl[t0 + k] = from_float<T>(g[k]);
-        }
+      if (tid < at.edges) put_edge(dl + at.edge(tid), edge_x, slope, c);
+      const bool fix_list = n_list > 0 && (kRest || p.g.ddistill);
+      if (n_ids > 0 || fix_list) {
+        __syncthreads();
+        fix_tokens(s, at, my, r, dl, n_ids, n_list, fix_list, kRest, p.g.ddistill != nullptr, p.t.kind, s.lp_part, dh, dd, inv);
       }
     }
-    // given and listed tokens
-    if (quiet || (n_ids == 0 && !fix_list)) return;
-    __syncthreads();
-    auto about = [&](float x, float& pv, float& lp) {
-      const float y = (x - r.m) * c - r.l2;
-      pv = ex2(y);
-      lp = kLn2 * y;
-    };
-    auto base = [&](float pv, float lp) { return pv == 0.f ? 0.f : pv * (lp_part - dh * lp); };
-    if (fix_list && my_tid >= lo && my_tid < hi) {
-      float pv, lp, dist;
-      about(my_tx, pv, lp);
-      if (p.t.kind == PG_DISTILL_FORWARD) dist = r.w * pv - expf(my_tl - r.lt);
-      else if (p.t.kind == PG_DISTILL_FORWARD_REST) dist = r.w * pv - expf(my_tl);
-      else dist = pv == 0.f ? 0.f : pv * (lp - my_tl - r.loss);
-      float sum = base(pv, lp) + dd * dist;
-      for (int j = 0; j < n_ids; ++j)
-        if (s.gid[j] == my_tid) sum += s.gdl[j];
-      dl[my_tid] = from_float<T>(r.some != 0.f ? inv * sum : 0.f);
-    }
-    if (my_id >= lo && my_id < hi) {
-      bool mine = true;                                             // the last of its token, and not on the list
-      for (int j = tid + 1; j < n_ids; ++j) mine &= s.gid[j] != my_id;
-      if (fix_list)
-        for (int j = 0; j < n_list; ++j) mine &= s.tid[j] != my_id;
-      if (mine) {
-        float pv, lp;
-        about(my_x, pv, lp);
-        float sum = base(pv, lp);
-        if (!rest) sum += dd * r.w * pv;
-        else if (p.g.ddistill) {                                    // outside the list
-          const float rv = ex2((my_x - r.mr) * c - r.l2r), pr = expf(r.lr);
-          sum += dd * rv * (p.t.kind == PG_DISTILL_FORWARD_REST ? pr * r.w - expf(r.lt) : pr * (r.lr - r.lt - r.loss));
-        }
-        for (int j = 0; j <= tid; ++j)
-          if (s.gid[j] == my_id) sum += s.gdl[j];
-        dl[my_id] = from_float<T>(r.some != 0.f ? inv * sum : 0.f);
-      }
-    }
-  }
 }
 
-template <typename T, int kMode, bool kEnt, bool kRest>
-int launch_token(TokenParams p, int n_rows, cudaStream_t st) {
-  constexpr int kTile = (sizeof(T) == 4 ? 4 : 8) * kTokThreads;
-  // rows that do not all start on 16 bytes may need a unit more (lead)
-  const bool aligned = (((uintptr_t)p.in | (uintptr_t)(p.in_stride * sizeof(T))) & 15) == 0;
-  const int total = (p.vocab + (aligned ? 0 : 16 / (int)sizeof(T) - 1) + kUnit - 1) / kUnit;
-  int parts = 1;
-  if (kMode == kBackward) {
-    parts = (total + kTile - 1) / kTile;
-  } else {
-    // a part for each tile, so that the rows stay in registers; more, down to a unit a thread, while that leaves SMs without work
-    while (parts < kMostParts && (kMode == kBoth ? (total + parts - 1) / parts > kTile : false)) parts *= 2;
-    while (parts < kMostParts && (int64_t)n_rows * parts < 2 * 148 && total / parts >= 2 * kTokThreads) parts *= 2;
+// The gradient alone, from what a forward pass has saved.
+template <typename T, bool kEnt>
+__global__ void __launch_bounds__(kTokThreads, kTokCtas)
+token_backward_kernel(const __grid_constant__ TokenParams p) {
+  constexpr int kUnits = kTokUnits<T>;
+  __shared__ TokenShared s;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int row = blockIdx.x / p.parts;
+  const RowPart<T> at(p, row, blockIdx.x - row * p.parts);
+  const int n_ids = p.g.dlogp ? p.t.n_ids : 0, n_list = p.t.n_teacher;
+  const bool distill = p.g.ddistill != nullptr && n_list > 0, rest = distill && p.t.kind != PG_DISTILL_FORWARD;
+  const float inv = p.t.temperature ? 1.f / p.t.temperature[row] : 1.f, c = inv * kLog2e;
+  const float dh = p.g.dentropy ? p.g.dentropy[row] * p.g.entropy_scale : 0.f;
+  const float dd = p.g.ddistill ? p.g.ddistill[row] * p.g.distill_scale : 0.f;
+  const TokenRow r = load_row((const float4*)p.o.saved + (int64_t)row * (PG_TOKEN_SAVED / 4));
+  Entry my = {-1, -1, 0.f, -INFINITY, 0.f, 0.f};
+  if (tid < n_ids) {
+    const int id = p.t.ids[(int64_t)row * n_ids + tid];
+    if ((unsigned int)id < (unsigned int)p.vocab) {
+      my.id = id;
+      my.dl = p.g.dlogp[(int64_t)row * n_ids + tid];
+    }
+    s.gid[tid] = my.id;
+    s.gdl[tid] = my.dl;
   }
+  const bool quiet = !__syncthreads_or(my.dl != 0.f || dh != 0.f || dd != 0.f);
+  Raw8<T> raw[kUnits];
+  const int u0 = at.first + tid;
+  if (!quiet) {
+    load_tile<T, true>(at, 0, raw);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j)
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(Raw8<T>) / 4; ++i) word_of(raw[j], i) = Empty8<T>::word;
+  }
+  const float edge_x = tid < at.edges && !quiet ? to_float(at.in[at.edge(tid)]) : -INFINITY;
+  if (my.id >= 0 && at.owns(my.id)) my.x = to_float(at.in[my.id]);
+  if (distill && tid < n_list) {
+    const int id = p.t.teacher_ids[(int64_t)row * n_list + tid];
+    my.tl = p.t.teacher_logp[(int64_t)row * n_list + tid];
+    if ((unsigned int)id < (unsigned int)p.vocab && !(my.tl == -INFINITY)) my.tid = id;
+    if (my.tid >= 0 && at.owns(my.tid)) my.tx = to_float(at.in[my.tid]);
+  }
+  if (distill && tid < (n_list + 3 & ~3)) s.tid[tid] = my.tid;
+  if (warp < (n_ids + 31) / 32) {
+    const float d = warp_total(my.dl);
+    if (lane == 0) s.dsum[warp] = d;
+  }
+  if (n_ids > 0 || distill) __syncthreads();
+  if (my.tid >= 0 && again_later(s, my.tid, n_list)) my.tid = -1;
+  float d = 0.f;
+  for (int i = 0; i < (n_ids + 31) / 32; ++i) d += s.dsum[i];
+  const float lp_part = -fmaf(dh, r.h, d);
+  TokenSlope slope = slope_of(r, rest, p.t.kind, lp_part, dh, dd, inv);
+  if (quiet) slope.a = slope.b = 0.f;
+  const Slope2 k(slope, c);
+  T* dl = (T*)p.dl + row * p.dl_stride;
+  const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0, huge = slope.ref < -kHuge && !quiet;
+#pragma unroll
+  for (int j = 0; j < kUnits; ++j) {
+    if (j * kTokThreads >= p.units) break;
+    float g[8];
+    slope8<T, kEnt>(raw[j], k, g);
+    if (u0 + j * kTokThreads < at.last && !huge) put8(dl + at.head + (int64_t)(u0 + j * kTokThreads) * kUnit, g, aligned);
+  }
+  if (huge) slope_huge(at, dl, slope, c);
+  if (tid < at.edges) put_edge(dl + at.edge(tid), edge_x, slope, c);
+  if (quiet || (n_ids == 0 && !distill)) return;
+  __syncthreads();
+  fix_tokens(s, at, my, r, dl, n_ids, n_list, distill, rest, distill, p.t.kind, lp_part, dh, dd, inv);
+}
+
+template <typename T, bool kGrad, bool kEnt, bool kRest>
+int launch_forward(TokenParams p, cudaStream_t st) {
+  constexpr int kTile = kTileUnits<T>;
+  const int total = std::max(p.vocab / kUnit, 1);
+  int parts = 1;
+  // Rows that are read twice: parts of 128 KB, so that what all SMs work on stays in the L2 cache.  With a bucket: bits of 16 KB at most.
+  if (kGrad) parts = std::min((total * (int)sizeof(T) * kUnit + kPartBytes - 1) / kPartBytes, kMostParts);
+  else if (kRest) parts = std::min((total + 16383) / 16384, kMostParts);
+  // more, down to a unit a thread, while that leaves SMs without work
+  while (parts * 2 <= kMostParts && (int64_t)p.n_rows * parts < 2 * 148 && total / parts >= 2 * kTokThreads) parts *= 2;
   p.parts = parts;
   p.units = (total + parts - 1) / parts;
   p.tiles = (p.units + kTile - 1) / kTile;
-  if ((int64_t)n_rows * parts > 0x7FFFFFFFLL) return PG_EINVAL;
-  const bool top = kMode != kBackward && p.o.top_ids && p.t.n_top > 0;
-  const int bytes = (top ? (int)sizeof(TopShared) : 0) + (kRest ? (p.units + 3) / 4 * 4 : 0);
-  auto kernel = token_kernel<T, kMode, kEnt, kRest>;
+  if ((int64_t)p.n_rows * parts > 0x7FFFFFFFLL) return PG_EINVAL;
+  const int bytes = (p.t.n_top ? (int)sizeof(TopShared) + (parts > 1 ? kMergeBytes : 0) : 0) + (kRest ? (p.units + 3) / 4 * 4 : 0);
+  auto kernel = token_kernel<T, kGrad, kEnt, kRest>;
   static std::atomic<uint64_t> done{0};
-  constexpr int kMostBytes = (int)sizeof(TopShared) + PG_TOKEN_MAX_VOCAB / kUnit + 16;
+  constexpr int kMostBytes = (int)sizeof(TopShared) + kMergeBytes + PG_TOKEN_MAX_VOCAB / kUnit / kMostParts + 64;
   if (bytes > 40 * 1024)
     if (const int rc = allow_shared(kernel, kMostBytes, done)) return rc;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(n_rows * parts));
+  cfg.gridDim = dim3((unsigned)(p.n_rows * parts));
   cfg.blockDim = dim3(kTokThreads);
   cfg.dynamicSmemBytes = bytes;
   cfg.stream = st;
@@ -814,21 +1021,34 @@ int launch_token(TokenParams p, int n_rows, cudaStream_t st) {
   attr.val.clusterDim.x = (unsigned)parts;
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
-  cfg.numAttrs = kMode != kBackward && parts > 1 ? 1 : 0;
+  cfg.numAttrs = parts > 1 ? 1 : 0;
   PG_CUDA(cudaLaunchKernelEx(&cfg, kernel, p));
   PG_LAUNCH_CHECK();
   return PG_OK;
 }
 
+template <typename T, bool kEnt>
+int launch_backward(TokenParams p, cudaStream_t st) {
+  const int total = std::max(p.vocab / kUnit, 1);
+  p.parts = (total + kTileUnits<T> - 1) / kTileUnits<T>;
+  p.units = (total + p.parts - 1) / p.parts;
+  if ((int64_t)p.n_rows * p.parts > 0x7FFFFFFFLL) return PG_EINVAL;
+  token_backward_kernel<T, kEnt><<<(unsigned)(p.n_rows * p.parts), kTokThreads, 0, st>>>(p);
+  PG_LAUNCH_CHECK();
+  return PG_OK;
+}
+
 template <typename T, int kMode>
-int token_launch(const TokenParams& p, int n_rows, cudaStream_t st) {
+int token_launch(const TokenParams& p, cudaStream_t st) {
   const bool ent = kMode == kBackward ? p.g.dentropy != nullptr : p.o.entropy || p.o.saved || (kMode == kBoth && p.g.dentropy);
-  const bool teacher = p.t.teacher_ids && p.t.n_teacher > 0;
-  if constexpr (kMode != kBackward) {
-    if (teacher && p.t.kind != PG_DISTILL_FORWARD)
-      return ent ? launch_token<T, kMode, true, true>(p, n_rows, st) : launch_token<T, kMode, false, true>(p, n_rows, st);
+  if constexpr (kMode == kBackward) {
+    return ent ? launch_backward<T, true>(p, st) : launch_backward<T, false>(p, st);
+  } else {
+    constexpr bool kGrad = kMode == kBoth;
+    const bool rest = p.t.n_teacher > 0 && p.t.kind != PG_DISTILL_FORWARD;
+    if (rest) return ent ? launch_forward<T, kGrad, true, true>(p, st) : launch_forward<T, kGrad, false, true>(p, st);
+    return ent ? launch_forward<T, kGrad, true, false>(p, st) : launch_forward<T, kGrad, false, false>(p, st);
   }
-  return ent ? launch_token<T, kMode, true, false>(p, n_rows, st) : launch_token<T, kMode, false, false>(p, n_rows, st);
 }
 
 }  // namespace pg

@@ -3,8 +3,8 @@
 
 namespace pg {
 
-template int token_launch<__nv_bfloat16, kForward>(const TokenParams&, int, cudaStream_t);
-template int token_launch<__nv_bfloat16, kBackward>(const TokenParams&, int, cudaStream_t);
-template int token_launch<__nv_bfloat16, kBoth>(const TokenParams&, int, cudaStream_t);
+template int token_launch<__nv_bfloat16, kForward>(const TokenParams&, cudaStream_t);
+template int token_launch<__nv_bfloat16, kBackward>(const TokenParams&, cudaStream_t);
+template int token_launch<__nv_bfloat16, kBoth>(const TokenParams&, cudaStream_t);
 
 }  // namespace pg

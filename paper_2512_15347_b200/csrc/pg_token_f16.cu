@@ -3,8 +3,8 @@
 
 namespace pg {
 
-template int token_launch<__half, kForward>(const TokenParams&, int, cudaStream_t);
-template int token_launch<__half, kBackward>(const TokenParams&, int, cudaStream_t);
-template int token_launch<__half, kBoth>(const TokenParams&, int, cudaStream_t);
+template int token_launch<__half, kForward>(const TokenParams&, cudaStream_t);
+template int token_launch<__half, kBackward>(const TokenParams&, cudaStream_t);
+template int token_launch<__half, kBoth>(const TokenParams&, cudaStream_t);
 
 }  // namespace pg

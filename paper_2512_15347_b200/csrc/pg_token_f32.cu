@@ -3,8 +3,8 @@
 
 namespace pg {
 
-template int token_launch<float, kForward>(const TokenParams&, int, cudaStream_t);
-template int token_launch<float, kBackward>(const TokenParams&, int, cudaStream_t);
-template int token_launch<float, kBoth>(const TokenParams&, int, cudaStream_t);
+template int token_launch<float, kForward>(const TokenParams&, cudaStream_t);
+template int token_launch<float, kBackward>(const TokenParams&, cudaStream_t);
+template int token_launch<float, kBoth>(const TokenParams&, cudaStream_t);
 
 }  // namespace pg
