@@ -28,7 +28,10 @@ namespace pg {
 #ifndef NB
 #define NB 4
 #endif
-constexpr int kTokThreads = 256;
+#ifndef NT
+#define NT 256
+#endif
+constexpr int kTokThreads = NT;
 constexpr int kTokCtas = NB;                    // of an SM
 #ifndef PB
 #define PB 131072
@@ -37,6 +40,7 @@ constexpr int kPartBytes = PB;
 constexpr int kTokWarps = kTokThreads / 32;
 constexpr int kMostParts = 8;                   // CTAs of a cluster
 constexpr int kCandidates = 1024;
+constexpr int kMostTiles = 16;                  // of a part with alternatives
 constexpr int kMergeBytes = kMostParts * PG_TOKEN_MAX_TOP * 8;
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr float kFloorY = -1e4f;                // 2^y = 0 long before; keeps 0 * y from being NaN
@@ -352,32 +356,92 @@ struct RowPart {
   __device__ __forceinline__ int edge(int i) const { return i < head ? i : i + units * kUnit; }
 };
 
-// Behind the tile, for alternatives.  Keys order by (logit, lowest index first); 0 is none.
+template <typename T> constexpr int kTokUnits = sizeof(T) == 4 ? 4 : 8;          // units of a thread and tile
+template <typename T> constexpr int kTileUnits = kTokUnits<T> * kTokThreads;
+
+// The n-th largest of the warp's values, 1 <= n <= 32.
+__device__ __forceinline__ float nth_largest(float v, int n) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+    for (int j = k >> 1; j; j >>= 1) {
+      const float o = __shfl_xor_sync(~0u, v, j);
+      v = ((lane & j) == 0) == ((lane & k) == 0) ? fmaxf(v, o) : fminf(v, o);
+    }
+  return __shfl_sync(~0u, v, n - 1);
+}
+
+// For alternatives.  Keys order by (logit, lowest index first); 0 is none.
 struct TopShared {
-  unsigned long long cand[kCandidates], few[kCandidates], best[PG_TOKEN_MAX_TOP];
-  float bounds[2][kTokWarps];
+  unsigned long long cand[kCandidates], best[PG_TOKEN_MAX_TOP];
+  float bounds[kTokWarps];
   unsigned int hist[256];
   unsigned long long prefix;
-  int count, kept, left, shift;
+  int count, groups, left, shift;
+  uint16_t group[kMostTiles * kTokThreads];                         // threads' tiles that may hold alternatives: tile * kTokThreads + thread
+  float most[kMostTiles * kTokThreads];                             // the largest logit of each; as many as there are tiles
 
   __device__ __forceinline__ void push(float x, int id) {
-    if (!(x > -INFINITY)) return;
     const int at = atomicAdd(&count, 1);
     if (at < kCandidates) cand[at] = top_key(x, id);
   }
-  // The n largest keys of the part into `best`, in order; by all threads.
-  template <typename T>
-  __device__ void select(const RowPart<T>& at, int vocab, int n, float bound);
 };
 
+__host__ __device__ constexpr int top_bytes(int tiles) { return (int)sizeof(TopShared) - (kMostTiles - tiles) * kTokThreads * 4; }
+
+// The n largest keys of the part into `best`, in order; by all threads.  `most` is filled, m a thread's largest logit, edge_x and list_x
+// what it has outside the tiles (-inf: nothing).
+// Every warp has as many threads with a logit at or above its own bound, the n / warps-th largest of its threads' largest, that all of
+// them make n; so the n-th largest logit is not below the least of these bounds, and few of the threads' tiles reach it.
 template <typename T>
-__device__ __noinline__ void TopShared::select(const RowPart<T>& at, int vocab, int n, float bound) {
-  const int tid = threadIdx.x;
-  if (tid == 0) kept = 0;
+__device__ __noinline__ void select_top(TopShared& s, const RowPart<T>& at, int n, int tiles, float m, float edge_x, float list_x, int list_id,
+                                        const uint32_t* bits) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const float own = nth_largest(m, (n + kTokWarps - 1) / kTokWarps);
+  if (lane == 0) s.bounds[warp] = own;
+  if (tid == 0) s.count = s.groups = 0;
   __syncthreads();
-  int total = count;
+  float bound = s.bounds[0];
+#pragma unroll
+  for (int i = 1; i < kTokWarps; ++i) bound = fminf(bound, s.bounds[i]);
+  for (int tile = 0; tile < tiles; ++tile) {
+    const bool has = s.most[tile * kTokThreads + tid] >= bound && s.most[tile * kTokThreads + tid] > -INFINITY;
+    const unsigned int those = __ballot_sync(~0u, has);
+    if (!those) continue;
+    int first = 0;
+    if (lane == 0) first = atomicAdd(&s.groups, __popc(those));
+    first = __shfl_sync(~0u, first, 0);
+    if (has) s.group[first + __popc(those & ((1u << lane) - 1))] = (uint16_t)(tile * kTokThreads + tid);
+  }
+  for (int i = tid; i < n; i += kTokThreads) s.best[i] = 0;
+  if (edge_x >= bound && edge_x > -INFINITY) s.push(edge_x, at.edge(tid));
+  if (list_x >= bound && list_x > -INFINITY) s.push(list_x, list_id);
+  __syncthreads();
+  const int work = s.groups * kTokUnits<T>;
+  for (int i = tid; i < work; i += kTokThreads) {
+    const int g = s.group[i / kTokUnits<T>], j = i % kTokUnits<T>;
+    const int u = g / kTokThreads * kTileUnits<T> + j * kTokThreads + g % kTokThreads;
+    if (at.first + u >= at.last) continue;
+    const int t0 = at.head + (at.first + u) * kUnit;
+    Raw8<T> raw;
+    const uint4* from = (const uint4*)(at.in + t0);
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(T) / 2; ++k) raw.v[k] = from[k];
+    const uint32_t listed = bits ? reinterpret_cast<const uint8_t*>(bits)[u] : 0u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float x0, x1;
+      split2(pair_of(raw, k), x0, x1);
+      if (x0 >= bound && x0 > -INFINITY && !(listed >> (2 * k) & 1)) s.push(x0, t0 + 2 * k);
+      if (x1 >= bound && x1 > -INFINITY && !(listed >> (2 * k + 1) & 1)) s.push(x1, t0 + 2 * k + 1);
+    }
+  }
+  __syncthreads();
+  int total = s.count;
+  __syncthreads();
   if (total > kCandidates) {
-    // Many equal logits: the n-th largest key of the part, from memory, eight bits at a time, until few enough reach it.
+    // Many equal logits: the n-th largest key of the part, eight bits at a time, until few enough reach it.
     auto each = [&](auto f) {
       for (int t = at.head + at.first * kUnit + tid; t < at.head + at.last * kUnit; t += kTokThreads) {
         const float x = to_float(at.in[t]);
@@ -389,55 +453,46 @@ __device__ __noinline__ void TopShared::select(const RowPart<T>& at, int vocab, 
       }
     };
     if (tid == 0) {
-      prefix = 0;
-      left = n;
+      s.prefix = 0;
+      s.left = n;
     }
     __syncthreads();
     for (int by = 56; by >= 0; by -= 8) {
-      hist[tid] = 0;
+      for (int i = tid; i < 256; i += kTokThreads) s.hist[i] = 0;
       __syncthreads();
-      const unsigned long long before = prefix;
+      const unsigned long long before = s.prefix;
       each([&](unsigned long long key) {
-        if (by == 56 || key >> (by + 8) == before) atomicAdd(&hist[key >> by & 255], 1u);
+        if (by == 56 || key >> (by + 8) == before) atomicAdd(&s.hist[key >> by & 255], 1u);
       });
       __syncthreads();
       if (tid == 0) {
-        int want = left, b = 255;
-        while (b > 0 && (int)hist[b] < want) want -= hist[b--];
-        prefix = before << 8 | (unsigned)b;
-        shift = by;
-        count = n - want + (int)hist[b] <= kCandidates ? 0 : -1;
-        left = want;
+        int want = s.left, b = 255;
+        while (b > 0 && (int)s.hist[b] < want) want -= s.hist[b--];
+        s.prefix = before << 8 | (unsigned)b;
+        s.shift = by;
+        s.count = n - want + (int)s.hist[b] <= kCandidates ? 0 : -1;
+        s.left = want;
       }
       __syncthreads();
-      if (count == 0) break;
+      if (s.count == 0) break;
     }
-    const unsigned long long from = prefix << shift;
+    const unsigned long long from = s.prefix << s.shift;
     __syncthreads();
     each([&](unsigned long long key) {
-      if (key >= from) cand[atomicAdd(&count, 1) & (kCandidates - 1)] = key;
+      if (key >= from) s.cand[atomicAdd(&s.count, 1) & (kCandidates - 1)] = key;
     });
     __syncthreads();
-    total = count;
-    bound = -INFINITY;
+    total = s.count;
   }
-  // What earlier tiles let through may lie below the last bound.
-  const unsigned long long from = bound == -INFINITY ? 0 : top_key(bound, 0x7FFFFFFF);
-  for (int i = tid; i < total; i += kTokThreads)
-    if (cand[i] >= from) few[atomicAdd(&kept, 1)] = cand[i];
-  for (int i = tid; i < n; i += kTokThreads) best[i] = 0;
-  __syncthreads();
-  const int k = kept;
-  if (tid == 0) few[min(k, kCandidates - 1)] = k < kCandidates ? 0 : few[kCandidates - 1];
-  __syncthreads();
-  for (int i = tid; i < k; i += kTokThreads) {
-    const unsigned long long key = few[i];
-    int rank = 0;
-    for (int j = 0; j < k; j += 2) {
-      const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&few[j]);
+  for (int i = tid; i < total; i += kTokThreads) {
+    const unsigned long long key = s.cand[i];
+    int rank = 0, j = 0;
+    for (; j + 1 < total; j += 2) {
+      const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&s.cand[j]);
       rank += (o.x > key) + (o.y > key);
     }
-    if (rank < n) best[rank] = key;
+    if (j < total) rank += s.cand[j] > key;
+    if (rank < n) s.best[rank] = key;
   }
   __syncthreads();
 }
@@ -569,22 +624,17 @@ __device__ __forceinline__ bool again_later(const TokenShared& s, int id, int n_
   return later;
 }
 
-// The n-th largest of the warp's values, 1 <= n <= 32.
-__device__ __forceinline__ float nth_largest(float v, int n) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int k = 2; k <= 32; k <<= 1)
-#pragma unroll
-    for (int j = k >> 1; j; j >>= 1) {
-      const float o = __shfl_xor_sync(~0u, v, j);
-      v = ((lane & j) == 0) == ((lane & k) == 0) ? fmaxf(v, o) : fminf(v, o);
-    }
-  return __shfl_sync(~0u, v, n - 1);
+#ifdef HINT
+__device__ __forceinline__ uint4 load_kept(const uint4* at) {
+  uint64_t policy;
+  uint4 v;
+  asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(policy));
+  asm volatile("ld.global.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(at), "l"(policy));
+  return v;
 }
-
-template <typename T> constexpr int kTokUnits = sizeof(T) == 4 ? 4 : 8;          // units of a thread and tile
-template <typename T> constexpr int kTileUnits = kTokUnits<T> * kTokThreads;
-
+#else
+__device__ __forceinline__ uint4 load_kept(const uint4* at) { return *at; }
+#endif
 // The thread's units of a tile; -inf where the part has none.  Streamed: read for the last time.
 template <typename T, bool kStreamed>
 __device__ __forceinline__ void load_tile(const RowPart<T>& at, int tile, Raw8<T> (&raw)[kTokUnits<T>]) {
@@ -596,7 +646,7 @@ __device__ __forceinline__ void load_tile(const RowPart<T>& at, int tile, Raw8<T
 #pragma unroll
     for (int j = 0; j < kUnits; ++j)
 #pragma unroll
-      for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j].v[i] = kStreamed ? __ldcs(from + j * kStep + i) : from[j * kStep + i];
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j].v[i] = kStreamed ? __ldcs(from + j * kStep + i) : load_kept(from + j * kStep + i);
   } else {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
@@ -604,7 +654,7 @@ __device__ __forceinline__ void load_tile(const RowPart<T>& at, int tile, Raw8<T
       for (int i = 0; i < (int)sizeof(Raw8<T>) / 4; ++i) word_of(raw[j], i) = Empty8<T>::word;
       if (u0 + j * kTokThreads < at.last)
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j].v[i] = kStreamed ? __ldcs(from + j * kStep + i) : from[j * kStep + i];
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j].v[i] = kStreamed ? __ldcs(from + j * kStep + i) : load_kept(from + j * kStep + i);
     }
   }
 }
@@ -624,8 +674,8 @@ token_kernel(const __grid_constant__ TokenParams p) {
   const int n_ids = p.t.n_ids, n_list = p.t.n_teacher, n_top = p.t.n_top;
   const int lists = (n_list + 31) / 32;
   TopShared& top = *reinterpret_cast<TopShared*>(more);
-  unsigned long long* const merge = reinterpret_cast<unsigned long long*>(more + sizeof(TopShared));
-  uint32_t* const bits = reinterpret_cast<uint32_t*>(more + (n_top ? (int)sizeof(TopShared) + (many ? kMergeBytes : 0) : 0));
+  unsigned long long* const merge = reinterpret_cast<unsigned long long*>(more + top_bytes(p.tiles));
+  uint32_t* const bits = reinterpret_cast<uint32_t*>(more + (n_top ? top_bytes(p.tiles) + (many ? kMergeBytes : 0) : 0));
 
   Raw8<T> raw[kUnits];
   load_tile<T, !kGrad>(at, 0, raw);
@@ -659,10 +709,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
   }
   if constexpr (kRest)
     for (int i = tid; i < (p.units + 3) / 4; i += kTokThreads) bits[i] = 0;
-  if (tid == 0) {
-    if (kRest) s.edges = 0;
-    if (n_top) top.count = 0;                                       // synchronised by the first tile's bound
-  }
+  if (kRest && tid == 0) s.edges = 0;
   if (n_list > 0) {
     __syncthreads();
     if (my.tid >= 0) {
@@ -702,7 +749,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
     }
   };
 
-    float m = -INFINITY, s0 = 0.f, s1 = 0.f, bound = -INFINITY;
+    float m = -INFINITY, s0 = 0.f, s1 = 0.f, edge_left = -INFINITY;
     for (int tile = 0; tile < p.tiles; ++tile) {
       if (tile > 0) load_tile<T, !kGrad>(at, tile, raw);
       mask_tile(tile);
@@ -748,32 +795,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
         s0 += f * t0;
         if (kEnt) s1 += f * fmaf(-off, t0, t1);
       }
-      if (n_top) {
-        // every warp has as many threads with a logit at or above its own bound that all of them make n_top
-        const float wb = nth_largest(m, (n_top + kTokWarps - 1) / kTokWarps);
-        if (lane == 0) top.bounds[tile & 1][warp] = wb;
-        __syncthreads();
-        bound = INFINITY;
-#pragma unroll
-        for (int i = 0; i < kTokWarps; ++i) bound = fminf(bound, top.bounds[tile & 1][i]);
-        if (tm >= bound) {
-#pragma unroll
-          for (int j = 0; j < kUnits; ++j) {
-            uint32_t v = word_of(raw[j], 0);
-#pragma unroll
-            for (int i = 1; i < (int)sizeof(Raw8<T>) / 4; ++i) v = max2(v, word_of(raw[j], i), T());
-            if (!(max_of<T>(v) >= bound)) continue;
-            const int t0 = at.head + (at.first + tile * kTile + j * kTokThreads + tid) * kUnit;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float x0, x1;
-              split2(pair_of(raw[j], i), x0, x1);
-              if (x0 >= bound) top.push(x0, t0 + 2 * i);
-              if (x1 >= bound) top.push(x1, t0 + 2 * i + 1);
-            }
-          }
-        }
-      }
+      if (n_top) top.most[tile * kTokThreads + tid] = tm;
     }
     if (at.edges > 0) {
       const float x = kRest && tid < at.edges && s.edges >> tid & 1 ? -INFINITY : edge_x;
@@ -782,9 +804,8 @@ token_kernel(const __grid_constant__ TokenParams p) {
       m = to;
       s0 += e;
       s1 += e * fmaxf(y, kFloorY);
-      if (n_top && x >= bound) top.push(x, at.edge(tid));
+      edge_left = x;
     }
-    if (kRest && n_top && my.tid >= 0 && my.tx >= bound && at.owns(my.tid)) top.push(my.tx, my.tid);
     if (warp < lists) {
       const bool used = my.tid >= 0;
       const float x = used ? my.tx : -INFINITY;
@@ -802,14 +823,14 @@ token_kernel(const __grid_constant__ TokenParams p) {
       l.mass = kRest ? warp_total(used ? exp((double)my.tl) : 0.) : 0.;
       if (lane == 0) s.list[warp] = l;
     }
-    {
-      const float own = m;
-      m = warp_most(m);
-      refer(own, m, c, s0, s1);
-      s0 = warp_total(s0);
-      if (kEnt) s1 = warp_total(s1);
-    }
-    if (n_top) top.select(at, p.vocab, n_top, bound);
+    const float own = m;
+    m = warp_most(m);
+    refer(own, m, c, s0, s1);
+    s0 = warp_total(s0);
+    if (kEnt) s1 = warp_total(s1);
+    if (n_top)
+      select_top(top, at, n_top, p.tiles, own, edge_left, kRest && my.tid >= 0 && at.owns(my.tid) ? my.tx : -INFINITY, my.tid,
+                 kRest ? bits : nullptr);
     // the triples of the parts' warps, to all parts
     float4* const triples = s.part;
     if (many) {
@@ -1001,11 +1022,12 @@ int launch_forward(TokenParams p, cudaStream_t st) {
   else if (kRest) parts = std::min((total + 16383) / 16384, kMostParts);
   // more, down to a unit a thread, while that leaves SMs without work
   while (parts * 2 <= kMostParts && (int64_t)p.n_rows * parts < 2 * 148 && total / parts >= 2 * kTokThreads) parts *= 2;
+  if (p.t.n_top) parts = std::max(parts, (total + kMostTiles * kTile - 1) / (kMostTiles * kTile));
   p.parts = parts;
   p.units = (total + parts - 1) / parts;
   p.tiles = (p.units + kTile - 1) / kTile;
   if ((int64_t)p.n_rows * parts > 0x7FFFFFFFLL) return PG_EINVAL;
-  const int bytes = (p.t.n_top ? (int)sizeof(TopShared) + (parts > 1 ? kMergeBytes : 0) : 0) + (kRest ? (p.units + 3) / 4 * 4 : 0);
+  const int bytes = (p.t.n_top ? top_bytes(p.tiles) + (parts > 1 ? kMergeBytes : 0) : 0) + (kRest ? (p.units + 3) / 4 * 4 : 0);
   auto kernel = token_kernel<T, kGrad, kEnt, kRest>;
   static std::atomic<uint64_t> done{0};
   constexpr int kMostBytes = (int)sizeof(TopShared) + kMergeBytes + PG_TOKEN_MAX_VOCAB / kUnit / kMostParts + 64;
