@@ -28,6 +28,9 @@ namespace pg {
 #ifndef NB
 #define NB 4
 #endif
+#ifndef KU
+#define KU 8
+#endif
 #ifndef NT
 #define NT 256
 #endif
@@ -356,8 +359,9 @@ struct RowPart {
   __device__ __forceinline__ int edge(int i) const { return i < head ? i : i + units * kUnit; }
 };
 
-template <typename T> constexpr int kTokUnits = sizeof(T) == 4 ? 4 : 8;          // units of a thread and tile
+template <typename T> constexpr int kTokUnits = sizeof(T) == 4 ? KU / 2 : KU;          // units of a thread and tile
 template <typename T> constexpr int kTileUnits = kTokUnits<T> * kTokThreads;
+template <typename T> constexpr int kTileBytes = kTileUnits<T> * kUnit * (int)sizeof(T);
 
 // The n-th largest of the warp's values, 1 <= n <= 32.
 __device__ __forceinline__ float nth_largest(float v, int n) {
@@ -624,17 +628,6 @@ __device__ __forceinline__ bool again_later(const TokenShared& s, int id, int n_
   return later;
 }
 
-#ifdef HINT
-__device__ __forceinline__ uint4 load_kept(const uint4* at) {
-  uint64_t policy;
-  uint4 v;
-  asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(policy));
-  asm volatile("ld.global.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(at), "l"(policy));
-  return v;
-}
-#else
-__device__ __forceinline__ uint4 load_kept(const uint4* at) { return *at; }
-#endif
 // The thread's units of a tile; -inf where the part has none.  Streamed: read for the last time.
 template <typename T, bool kStreamed>
 __device__ __forceinline__ void load_tile(const RowPart<T>& at, int tile, Raw8<T> (&raw)[kTokUnits<T>]) {
@@ -646,7 +639,7 @@ __device__ __forceinline__ void load_tile(const RowPart<T>& at, int tile, Raw8<T
 #pragma unroll
     for (int j = 0; j < kUnits; ++j)
 #pragma unroll
-      for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j].v[i] = kStreamed ? __ldcs(from + j * kStep + i) : load_kept(from + j * kStep + i);
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j].v[i] = kStreamed ? __ldcs(from + j * kStep + i) : from[j * kStep + i];
   } else {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
@@ -654,7 +647,30 @@ __device__ __forceinline__ void load_tile(const RowPart<T>& at, int tile, Raw8<T
       for (int i = 0; i < (int)sizeof(Raw8<T>) / 4; ++i) word_of(raw[j], i) = Empty8<T>::word;
       if (u0 + j * kTokThreads < at.last)
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j].v[i] = kStreamed ? __ldcs(from + j * kStep + i) : load_kept(from + j * kStep + i);
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j].v[i] = kStreamed ? __ldcs(from + j * kStep + i) : from[j * kStep + i];
+    }
+  }
+}
+
+// The gradient of a tile in registers; dl: of the row's first unit.
+template <typename T, bool kEnt>
+__device__ __forceinline__ void slope_tile(const RowPart<T>& at, int tile, const Raw8<T> (&raw)[kTokUnits<T>], const Slope2& k, T* dl, bool aligned) {
+  const int u0 = at.first + tile * kTileUnits<T> + (int)threadIdx.x;
+  T* to = dl + (int64_t)u0 * kUnit;
+  if (aligned && at.first + (tile + 1) * kTileUnits<T> <= at.last) {
+#pragma unroll
+    for (int j = 0; j < kTokUnits<T>; ++j) {
+      float g[8];
+      slope8<T, kEnt>(raw[j], k, g);
+      store8(to + j * kTokThreads * kUnit, g);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < kTokUnits<T>; ++j) {
+      if (at.first + tile * kTileUnits<T> + j * kTokThreads >= at.last) break;
+      float g[8];
+      slope8<T, kEnt>(raw[j], k, g);
+      if (u0 + j * kTokThreads < at.last) put8(to + j * kTokThreads * kUnit, g, aligned);
     }
   }
 }
@@ -665,7 +681,7 @@ __global__ void __launch_bounds__(kTokThreads, kTokCtas)
 token_kernel(const __grid_constant__ TokenParams p) {
   constexpr int kUnits = kTokUnits<T>, kTile = kTileUnits<T>;
   __shared__ TokenShared s;
-  extern __shared__ __align__(16) unsigned char more[];             // TopShared and the parts' lists if there are alternatives; bits (kRest)
+  extern __shared__ __align__(16) unsigned char more[];             // a tile; TopShared and the parts' lists if there are alternatives; bits (kRest)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int row = blockIdx.x / p.parts;
   const RowPart<T> at(p, row, blockIdx.x - row * p.parts);
@@ -673,12 +689,14 @@ token_kernel(const __grid_constant__ TokenParams p) {
   if (many) cluster_arrive();                                       // all CTAs run before one writes into another's memory
   const int n_ids = p.t.n_ids, n_list = p.t.n_teacher, n_top = p.t.n_top;
   const int lists = (n_list + 31) / 32;
-  TopShared& top = *reinterpret_cast<TopShared*>(more);
-  unsigned long long* const merge = reinterpret_cast<unsigned long long*>(more + top_bytes(p.tiles));
-  uint32_t* const bits = reinterpret_cast<uint32_t*>(more + (n_top ? top_bytes(p.tiles) + (many ? kMergeBytes : 0) : 0));
+  unsigned char* const behind = more + (kGrad && p.tiles > 1 ? kTileBytes<T> : 0);
+  TopShared& top = *reinterpret_cast<TopShared*>(behind);
+  unsigned long long* const merge = reinterpret_cast<unsigned long long*>(behind + top_bytes(p.tiles));
+  uint32_t* const bits = reinterpret_cast<uint32_t*>(behind + (n_top ? top_bytes(p.tiles) + (many ? kMergeBytes : 0) : 0));
 
+  uint4* const kept = reinterpret_cast<uint4*>(more) + tid;         // a thread's own places: its units of tile 1, those of tile 0 stay in registers
   Raw8<T> raw[kUnits];
-  load_tile<T, !kGrad>(at, 0, raw);
+  load_tile<T, !kGrad>(at, p.tiles - 1, raw);                       // the part's cut tile first: the last two, that stay here, are whole
   const float inv = p.t.temperature ? 1.f / p.t.temperature[row] : 1.f, c = inv * kLog2e;
   const float dh = kGrad && p.g.dentropy ? p.g.dentropy[row] * p.g.entropy_scale : 0.f;
   const float dd = kGrad && p.g.ddistill ? p.g.ddistill[row] * p.g.distill_scale : 0.f;
@@ -750,9 +768,15 @@ token_kernel(const __grid_constant__ TokenParams p) {
   };
 
     float m = -INFINITY, s0 = 0.f, s1 = 0.f, edge_left = -INFINITY;
-    for (int tile = 0; tile < p.tiles; ++tile) {
-      if (tile > 0) load_tile<T, !kGrad>(at, tile, raw);
+    for (int tile = p.tiles - 1; tile >= 0; --tile) {
+      if (tile < p.tiles - 1) load_tile<T, !kGrad>(at, tile, raw);
       mask_tile(tile);
+      if (kGrad && tile == 1) {
+#pragma unroll
+        for (int j = 0; j < kUnits; ++j)
+#pragma unroll
+          for (int i = 0; i < (int)sizeof(T) / 2; ++i) kept[(j * (int)sizeof(T) / 2 + i) * kTokThreads] = raw[j].v[i];
+      }
       uint32_t w = Empty8<T>::word;
 #pragma unroll
       for (int j = 0; j < kUnits; ++j) {
@@ -916,19 +940,21 @@ token_kernel(const __grid_constant__ TokenParams p) {
       const Slope2 k(slope, c);
       T* dl = (T*)p.dl + row * p.dl_stride;
       const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0;
-      const bool huge = slope.ref < -kHuge;                         // rows masked throughout, by the type's lowest value
-      if (huge) slope_huge(at, dl, slope, c);
-      for (int tile = p.tiles - 1;;) {
-        const int u0 = at.first + tile * kTile + tid;
+      if (slope.ref < -kHuge) {                                     // rows masked throughout, by the type's lowest value
+        slope_huge(at, dl, slope, c);
+      } else {
+        for (int tile = 0;;) {
+          slope_tile<T, kEnt>(at, tile, raw, k, dl + at.head, aligned);
+          if (++tile == p.tiles) break;
+          if (tile == 1) {
 #pragma unroll
-        for (int j = 0; j < kUnits; ++j) {
-          if (tile * kTile + j * kTokThreads >= p.units) break;
-          float g[8];
-          slope8<T, kEnt>(raw[j], k, g);
-          if (u0 + j * kTokThreads < at.last && !huge) put8(dl + at.head + (int64_t)(u0 + j * kTokThreads) * kUnit, g, aligned);
+            for (int j = 0; j < kUnits; ++j)
+#pragma unroll
+              for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j].v[i] = kept[(j * (int)sizeof(T) / 2 + i) * kTokThreads];
+          } else {
+            load_tile<T, true>(at, tile, raw);                      // from the L2 cache
+          }
         }
-        if (--tile < 0) break;
-        load_tile<T, true>(at, tile, raw);                          // from the L2 cache
       }
       if (tid < at.edges) put_edge(dl + at.edge(tid), edge_x, slope, c);
       const bool fix_list = n_list > 0 && (kRest || p.g.ddistill);
@@ -966,7 +992,6 @@ token_backward_kernel(const __grid_constant__ TokenParams p) {
   }
   const bool quiet = !__syncthreads_or(my.dl != 0.f || dh != 0.f || dd != 0.f);
   Raw8<T> raw[kUnits];
-  const int u0 = at.first + tid;
   if (!quiet) {
     load_tile<T, true>(at, 0, raw);
   } else {
@@ -998,14 +1023,8 @@ token_backward_kernel(const __grid_constant__ TokenParams p) {
   const Slope2 k(slope, c);
   T* dl = (T*)p.dl + row * p.dl_stride;
   const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0, huge = slope.ref < -kHuge && !quiet;
-#pragma unroll
-  for (int j = 0; j < kUnits; ++j) {
-    if (j * kTokThreads >= p.units) break;
-    float g[8];
-    slope8<T, kEnt>(raw[j], k, g);
-    if (u0 + j * kTokThreads < at.last && !huge) put8(dl + at.head + (int64_t)(u0 + j * kTokThreads) * kUnit, g, aligned);
-  }
   if (huge) slope_huge(at, dl, slope, c);
+  else slope_tile<T, kEnt>(at, 0, raw, k, dl + at.head, aligned);
   if (tid < at.edges) put_edge(dl + at.edge(tid), edge_x, slope, c);
   if (quiet || (n_ids == 0 && !distill)) return;
   __syncthreads();
@@ -1027,11 +1046,11 @@ int launch_forward(TokenParams p, cudaStream_t st) {
   p.units = (total + parts - 1) / parts;
   p.tiles = (p.units + kTile - 1) / kTile;
   if ((int64_t)p.n_rows * parts > 0x7FFFFFFFLL) return PG_EINVAL;
-  const int bytes = (p.t.n_top ? top_bytes(p.tiles) + (parts > 1 ? kMergeBytes : 0) : 0) + (kRest ? (p.units + 3) / 4 * 4 : 0);
+  const int bytes = (kGrad && p.tiles > 1 ? kTileBytes<T> : 0) + (p.t.n_top ? top_bytes(p.tiles) + (parts > 1 ? kMergeBytes : 0) : 0) + (kRest ? (p.units + 3) / 4 * 4 : 0);
   auto kernel = token_kernel<T, kGrad, kEnt, kRest>;
   static std::atomic<uint64_t> done{0};
-  constexpr int kMostBytes = (int)sizeof(TopShared) + kMergeBytes + PG_TOKEN_MAX_VOCAB / kUnit / kMostParts + 64;
-  if (bytes > 40 * 1024)
+  constexpr int kMostBytes = kTileBytes<T> + (int)sizeof(TopShared) + kMergeBytes + PG_TOKEN_MAX_VOCAB / kUnit / kMostParts + 64;
+  if (bytes > 32 * 1024)
     if (const int rc = allow_shared(kernel, kMostBytes, done)) return rc;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(p.n_rows * parts));
