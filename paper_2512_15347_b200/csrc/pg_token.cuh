@@ -40,6 +40,10 @@ constexpr int kTokCtas = NB;                    // of an SM
 #define PB 131072
 #endif
 constexpr int kPartBytes = PB;
+#ifndef OC
+#define OC 2
+#endif
+constexpr int kOnChip = OC;                     // tiles of a part that stay on chip: one in registers, one in shared memory
 constexpr int kTokWarps = kTokThreads / 32;
 constexpr int kMostParts = 8;                   // CTAs of a cluster
 constexpr int kCandidates = 1024;
@@ -281,9 +285,13 @@ __device__ __forceinline__ TokenRow finish_row(const TokenShared& s, const float
   r.m = finite_ref(m);
   r.l2 = r.some != 0.f ? log2f(s0) : 0.f;
   r.h = r.some != 0.f ? kLn2 * (r.l2 - s1 / s0) : 0.f;
-  // in 64 bits: where only tokens of the type's lowest value are left, it is finite and its share of the loss may be
-  const double lr = ((double)finite_ref(r.mr) - r.m) * inv + (double)(kLn2 * (r.l2r - r.l2));
-  r.lr = !rest ? 0.f : !outside ? -INFINITY : lr < -3e38 ? -3e38f : (float)lr;
+  double lr = 0.;
+  if (rest) {                                                          // in 64 bits: where only tokens of the type's lowest value are left,
+    lr = ((double)finite_ref(r.mr) - r.m) * inv + (double)(kLn2 * (r.l2r - r.l2));      // it is finite and its share of the loss may be
+    r.lr = !outside ? -INFINITY : lr < -3e38 ? -3e38f : (float)lr;
+  } else {
+    r.lr = 0.f;
+  }
   r.mr = finite_ref(r.mr);
   r.loss = r.lt = r.w = 0.f;
   if (lists == 0 || r.some == 0.f) return r;
@@ -534,16 +542,7 @@ __device__ __forceinline__ void slope8(const Raw8<T>& r, const Slope2& k, float 
     split2(mul2(e, f), g[2 * i], g[2 * i + 1]);
   }
 }
-template <typename T>
-__device__ __forceinline__ void put8(T* to, const float (&g)[8], bool aligned) {
-  if (aligned) {
-    store8(to, g);
-  } else {
-#pragma unroll
-    for (int i = 0; i < kUnit; ++i) to[i] = from_float<T>(g[i]);
-  }
-}
-// A part whose reference is that far down, from memory: differences first.
+// A part from memory, logit by logit, differences first: whose reference is that far down, or whose gradient lies off 16 bytes.
 template <typename T>
 __device__ __noinline__ void slope_huge(const RowPart<T>& at, T* dl, const TokenSlope& k, float c) {
   for (int t = at.head + at.first * kUnit + threadIdx.x; t < at.head + at.last * kUnit; t += kTokThreads) {
@@ -628,51 +627,89 @@ __device__ __forceinline__ bool again_later(const TokenShared& s, int id, int n_
   return later;
 }
 
-// The thread's units of a tile; -inf where the part has none.  Streamed: read for the last time.
-template <typename T, bool kStreamed>
-__device__ __forceinline__ void load_tile(const RowPart<T>& at, int tile, Raw8<T> (&raw)[kTokUnits<T>]) {
-  constexpr int kUnits = kTokUnits<T>;
-  const int u0 = at.first + tile * kTileUnits<T> + (int)threadIdx.x;
-  const uint4* from = (const uint4*)(at.in + at.head + (int64_t)u0 * kUnit);
-  constexpr int kStep = kTokThreads * (int)sizeof(Raw8<T>) / 16;
-  if (at.first + (tile + 1) * kTileUnits<T> <= at.last) {           // all of them
+// How the L2 cache is to keep what a load brings: evicted first if it is not read again, so that it does not drive out what is.
+__device__ __forceinline__ uint64_t keep_policy(bool again) {
+  uint64_t first, normal;
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(first));
+  asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(normal));
+  return again ? normal : first;
+}
+// Unit j of the thread in a tile.
+template <typename T>
+__device__ __forceinline__ void load_unit(const T* at, int j, uint64_t policy, Raw8<T>& r) {
+  const uint4* from = (const uint4*)(at + j * kTokThreads * kUnit);
 #pragma unroll
-    for (int j = 0; j < kUnits; ++j)
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+    asm volatile("ld.global.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+                 : "=r"(r.v[i].x), "=r"(r.v[i].y), "=r"(r.v[i].z), "=r"(r.v[i].w) : "l"(from + i), "l"(policy) : "memory");
+}
+template <typename T>
+__device__ __forceinline__ bool whole_tile(const RowPart<T>& at, int tile) { return at.first + (tile + 1) * kTileUnits<T> <= at.last; }
+// The thread's place in a tile.
+template <typename T>
+__device__ __forceinline__ const T* tile_at(const RowPart<T>& at, int tile) {
+  return at.in + at.head + (int64_t)(at.first + tile * kTileUnits<T> + (int)threadIdx.x) * kUnit;
+}
+// The thread's units of a tile; -inf where the part has none.
+template <typename T>
+__device__ __forceinline__ void load_tile(const RowPart<T>& at, int tile, uint64_t policy, Raw8<T> (&raw)[kTokUnits<T>]) {
+  const T* from = tile_at(at, tile);
+  if (whole_tile(at, tile)) {
 #pragma unroll
-      for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j].v[i] = kStreamed ? __ldcs(from + j * kStep + i) : from[j * kStep + i];
+    for (int j = 0; j < kTokUnits<T>; ++j) load_unit(from, j, policy, raw[j]);
   } else {
+    const int u0 = at.first + tile * kTileUnits<T> + (int)threadIdx.x;
 #pragma unroll
-    for (int j = 0; j < kUnits; ++j) {
+    for (int j = 0; j < kTokUnits<T>; ++j) {
 #pragma unroll
       for (int i = 0; i < (int)sizeof(Raw8<T>) / 4; ++i) word_of(raw[j], i) = Empty8<T>::word;
-      if (u0 + j * kTokThreads < at.last)
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j].v[i] = kStreamed ? __ldcs(from + j * kStep + i) : from[j * kStep + i];
+      if (u0 + j * kTokThreads < at.last) load_unit(from, j, policy, raw[j]);
     }
   }
 }
 
-// The gradient of a tile in registers; dl: of the row's first unit.
-template <typename T, bool kEnt>
-__device__ __forceinline__ void slope_tile(const RowPart<T>& at, int tile, const Raw8<T> (&raw)[kTokUnits<T>], const Slope2& k, T* dl, bool aligned) {
-  const int u0 = at.first + tile * kTileUnits<T> + (int)threadIdx.x;
-  T* to = dl + (int64_t)u0 * kUnit;
-  if (aligned && at.first + (tile + 1) * kTileUnits<T> <= at.last) {
+// The gradient of a tile in registers; dl: of the row's first unit, its units on 16 bytes.  kAsk: as a unit is done with, the next tile's
+// is asked for (from); that tile is whole.
+template <typename T, bool kEnt, bool kAsk>
+__device__ __forceinline__ void slope_tile(const RowPart<T>& at, int tile, Raw8<T> (&raw)[kTokUnits<T>], const Slope2& k, T* dl, const T* from,
+                                           uint64_t policy) {
+  const int left = at.last - at.first - tile * kTileUnits<T> - (int)threadIdx.x;   // units from the thread's first on
+  T* to = dl + (int64_t)(at.first + tile * kTileUnits<T> + (int)threadIdx.x) * kUnit;
 #pragma unroll
-    for (int j = 0; j < kTokUnits<T>; ++j) {
-      float g[8];
-      slope8<T, kEnt>(raw[j], k, g);
-      store8(to + j * kTokThreads * kUnit, g);
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < kTokUnits<T>; ++j) {
-      if (at.first + tile * kTileUnits<T> + j * kTokThreads >= at.last) break;
-      float g[8];
-      slope8<T, kEnt>(raw[j], k, g);
-      if (u0 + j * kTokThreads < at.last) put8(to + j * kTokThreads * kUnit, g, aligned);
-    }
+  for (int j = 0; j < kTokUnits<T>; ++j) {
+    float g[8];
+    slope8<T, kEnt>(raw[j], k, g);
+    if (kAsk) load_unit(from, j, policy, raw[j]);
+    if (j * kTokThreads < left) store8(to + j * kTokThreads * kUnit, g);
   }
+}
+// The sums of a tile in registers, against y = l c - r.
+template <typename T, bool kEnt, bool kAsk>
+__device__ __forceinline__ void sum_tile(Raw8<T> (&raw)[kTokUnits<T>], float c, float r, float& t0, float& t1, const T* from, uint64_t policy) {
+  const f2 nr = make2(-r, -r), c2 = make2(c, c);
+  f2 a0 = make2(0.f, 0.f), a1 = a0, b0 = a0, b1 = a0;
+#pragma unroll
+  for (int j = 0; j < kTokUnits<T>; ++j) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float y0, y1;
+      split2(fma2(pair_of(raw[j], i), c2, nr), y0, y1);
+      const f2 e = make2(ex2(y0), ex2(y1));
+      if (i & 1) b0 = add2(b0, e);
+      else a0 = add2(a0, e);
+      if (kEnt) {
+        const f2 y = make2(fmaxf(y0, kFloorY), fmaxf(y1, kFloorY));
+        if (i & 1) b1 = fma2(e, y, b1);
+        else a1 = fma2(e, y, a1);
+      }
+    }
+    if (kAsk) load_unit(from, j, policy, raw[j]);
+  }
+  float u, v;
+  split2(add2(a0, b0), u, v);
+  t0 = u + v;
+  split2(add2(a1, b1), u, v);
+  t1 = u + v;
 }
 
 // Forward, with the gradient on top (kGrad).
@@ -689,14 +726,15 @@ token_kernel(const __grid_constant__ TokenParams p) {
   if (many) cluster_arrive();                                       // all CTAs run before one writes into another's memory
   const int n_ids = p.t.n_ids, n_list = p.t.n_teacher, n_top = p.t.n_top;
   const int lists = (n_list + 31) / 32;
-  unsigned char* const behind = more + (kGrad && p.tiles > 1 ? kTileBytes<T> : 0);
+  unsigned char* const behind = more + (kGrad && kOnChip > 1 && p.tiles > 1 ? kTileBytes<T> : 0);
   TopShared& top = *reinterpret_cast<TopShared*>(behind);
   unsigned long long* const merge = reinterpret_cast<unsigned long long*>(behind + top_bytes(p.tiles));
   uint32_t* const bits = reinterpret_cast<uint32_t*>(behind + (n_top ? top_bytes(p.tiles) + (many ? kMergeBytes : 0) : 0));
 
   uint4* const kept = reinterpret_cast<uint4*>(more) + tid;         // a thread's own places: its units of tile 1, those of tile 0 stay in registers
   Raw8<T> raw[kUnits];
-  load_tile<T, !kGrad>(at, p.tiles - 1, raw);                       // the part's cut tile first: the last two, that stay here, are whole
+  const uint64_t last_read = keep_policy(false), read_again = keep_policy(true);
+  load_tile(at, p.tiles - 1, kGrad && p.tiles > kOnChip ? read_again : last_read, raw);                       // the part's cut tile first: the last two, that stay here, are whole
   const float inv = p.t.temperature ? 1.f / p.t.temperature[row] : 1.f, c = inv * kLog2e;
   const float dh = kGrad && p.g.dentropy ? p.g.dentropy[row] * p.g.entropy_scale : 0.f;
   const float dd = kGrad && p.g.ddistill ? p.g.ddistill[row] * p.g.distill_scale : 0.f;
@@ -769,9 +807,8 @@ token_kernel(const __grid_constant__ TokenParams p) {
 
     float m = -INFINITY, s0 = 0.f, s1 = 0.f, edge_left = -INFINITY;
     for (int tile = p.tiles - 1; tile >= 0; --tile) {
-      if (tile < p.tiles - 1) load_tile<T, !kGrad>(at, tile, raw);
       mask_tile(tile);
-      if (kGrad && tile == 1) {
+      if (kGrad && tile == kOnChip - 1 && tile > 0) {
 #pragma unroll
         for (int j = 0; j < kUnits; ++j)
 #pragma unroll
@@ -786,40 +823,25 @@ token_kernel(const __grid_constant__ TokenParams p) {
       const float tm = max_of<T>(w);
       refer(m, fmaxf(m, tm), c, s0, s1);
       m = fmaxf(m, tm);
+      bool asked = false;
       if (m < -kHuge && m > -INFINITY) {
         sum_huge(at, bits, m, c, tile, s0, s1);
       } else {
         // y = l c - r in one rounding; what r = m c rounded is off by is taken back from the sums
         const float ref = finite_ref(m), r = ref * c, off = fmaf(ref, c, -r);
-        const f2 nr = make2(-r, -r), c2 = make2(c, c);
-        f2 a0 = make2(0.f, 0.f), a1 = a0, b0 = a0, b1 = a0;
-#pragma unroll
-        for (int j = 0; j < kUnits; ++j) {
-          if (tile * kTile + j * kTokThreads >= p.units) break;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float y0, y1;
-            split2(fma2(pair_of(raw[j], i), c2, nr), y0, y1);
-            const f2 e = make2(ex2(y0), ex2(y1));
-            if (i & 1) b0 = add2(b0, e);
-            else a0 = add2(a0, e);
-            if (kEnt) {
-              const f2 y = make2(fmaxf(y0, kFloorY), fmaxf(y1, kFloorY));
-              if (i & 1) b1 = fma2(e, y, b1);
-              else a1 = fma2(e, y, a1);
-            }
-          }
-        }
-        float u, v, t0, t1;
-        split2(add2(a0, b0), u, v);
-        t0 = u + v;
-        split2(add2(a1, b1), u, v);
-        t1 = u + v;
+        // as a unit is done with, the next tile's is asked for
+        const bool ask = tile > 0 && whole_tile(at, tile - 1);
+        const uint64_t policy = kGrad && tile > kOnChip ? read_again : last_read;
+        float t0, t1;
+        if (ask) sum_tile<T, kEnt, true>(raw, c, r, t0, t1, tile_at(at, tile - 1), policy);
+        else sum_tile<T, kEnt, false>(raw, c, r, t0, t1, nullptr, 0);
+        asked = ask;
         const float f = ex2(-off);
         s0 += f * t0;
         if (kEnt) s1 += f * fmaf(-off, t0, t1);
       }
       if (n_top) top.most[tile * kTokThreads + tid] = tm;
+      if (tile > 0 && !asked) load_tile(at, tile - 1, kGrad && tile > kOnChip ? read_again : last_read, raw);
     }
     if (at.edges > 0) {
       const float x = kRest && tid < at.edges && s.edges >> tid & 1 ? -INFINITY : edge_x;
@@ -940,19 +962,21 @@ token_kernel(const __grid_constant__ TokenParams p) {
       const Slope2 k(slope, c);
       T* dl = (T*)p.dl + row * p.dl_stride;
       const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0;
-      if (slope.ref < -kHuge) {                                     // rows masked throughout, by the type's lowest value
+      if (slope.ref < -kHuge || !aligned) {                         // rows masked throughout, by the type's lowest value; or off 16 bytes
         slope_huge(at, dl, slope, c);
       } else {
-        for (int tile = 0;;) {
-          slope_tile<T, kEnt>(at, tile, raw, k, dl + at.head, aligned);
-          if (++tile == p.tiles) break;
-          if (tile == 1) {
+        for (int tile = 0; tile < p.tiles; ++tile) {
+          const int next = tile + 1;
+          const bool ask = next >= kOnChip && next < p.tiles && whole_tile(at, next);
+          if (ask) slope_tile<T, kEnt, true>(at, tile, raw, k, dl + at.head, tile_at(at, next), last_read);
+          else slope_tile<T, kEnt, false>(at, tile, raw, k, dl + at.head, nullptr, 0);
+          if (next < kOnChip && next < p.tiles) {
 #pragma unroll
             for (int j = 0; j < kUnits; ++j)
 #pragma unroll
               for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j].v[i] = kept[(j * (int)sizeof(T) / 2 + i) * kTokThreads];
-          } else {
-            load_tile<T, true>(at, tile, raw);                      // from the L2 cache
+          } else if (next < p.tiles && !ask) {
+            load_tile(at, next, last_read, raw);
           }
         }
       }
@@ -993,7 +1017,7 @@ token_backward_kernel(const __grid_constant__ TokenParams p) {
   const bool quiet = !__syncthreads_or(my.dl != 0.f || dh != 0.f || dd != 0.f);
   Raw8<T> raw[kUnits];
   if (!quiet) {
-    load_tile<T, true>(at, 0, raw);
+    load_tile(at, 0, keep_policy(false), raw);
   } else {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j)
@@ -1022,9 +1046,9 @@ token_backward_kernel(const __grid_constant__ TokenParams p) {
   if (quiet) slope.a = slope.b = 0.f;
   const Slope2 k(slope, c);
   T* dl = (T*)p.dl + row * p.dl_stride;
-  const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0, huge = slope.ref < -kHuge && !quiet;
+  const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0, huge = !aligned || (slope.ref < -kHuge && !quiet);
   if (huge) slope_huge(at, dl, slope, c);
-  else slope_tile<T, kEnt>(at, 0, raw, k, dl + at.head, aligned);
+  else slope_tile<T, kEnt, false>(at, 0, raw, k, dl + at.head, nullptr, 0);
   if (tid < at.edges) put_edge(dl + at.edge(tid), edge_x, slope, c);
   if (quiet || (n_ids == 0 && !distill)) return;
   __syncthreads();
@@ -1046,7 +1070,7 @@ int launch_forward(TokenParams p, cudaStream_t st) {
   p.units = (total + parts - 1) / parts;
   p.tiles = (p.units + kTile - 1) / kTile;
   if ((int64_t)p.n_rows * parts > 0x7FFFFFFFLL) return PG_EINVAL;
-  const int bytes = (kGrad && p.tiles > 1 ? kTileBytes<T> : 0) + (p.t.n_top ? top_bytes(p.tiles) + (parts > 1 ? kMergeBytes : 0) : 0) + (kRest ? (p.units + 3) / 4 * 4 : 0);
+  const int bytes = (kGrad && kOnChip > 1 && p.tiles > 1 ? kTileBytes<T> : 0) + (p.t.n_top ? top_bytes(p.tiles) + (parts > 1 ? kMergeBytes : 0) : 0) + (kRest ? (p.units + 3) / 4 * 4 : 0);
   auto kernel = token_kernel<T, kGrad, kEnt, kRest>;
   static std::atomic<uint64_t> done{0};
   constexpr int kMostBytes = kTileBytes<T> + (int)sizeof(TopShared) + kMergeBytes + PG_TOKEN_MAX_VOCAB / kUnit / kMostParts + 64;
