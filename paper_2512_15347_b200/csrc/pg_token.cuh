@@ -28,9 +28,6 @@ namespace pg {
 #ifndef NB
 #define NB 4
 #endif
-#ifndef KU
-#define KU 8
-#endif
 #ifndef NT
 #define NT 256
 #endif
@@ -200,23 +197,48 @@ __device__ __forceinline__ float max_of(uint32_t w) {
     return to_float(x);
   }
 }
-// Word i of a unit; token k of a unit as bits; one token replaced by -inf.
+// A unit is 16 bytes of a row: eight or four logits.
+template <typename T> constexpr int kPer = 16 / (int)sizeof(T);
 template <typename T>
-__device__ __forceinline__ uint32_t& word_of(Raw8<T>& r, int i) { return reinterpret_cast<uint32_t*>(&r)[i]; }
+__device__ __forceinline__ uint32_t max_unit(uint32_t w, const uint4& v) {
+  return max2(max2(max2(w, v.x, T()), v.y, T()), max2(v.z, v.w, T()), T());
+}
+// The logits of bits in `listed` replaced by -inf.
 template <typename T>
-__device__ __forceinline__ void set_empty(Raw8<T>& r, int k) {
-  if constexpr (sizeof(T) == 4) word_of(r, k) = Empty8<T>::word;
-  else word_of(r, k >> 1) = k & 1 ? (word_of(r, k >> 1) & 0xFFFFu) | (Empty8<T>::word & 0xFFFF0000u)
-                                  : (word_of(r, k >> 1) & 0xFFFF0000u) | (Empty8<T>::word & 0xFFFFu);
+__device__ __forceinline__ void set_empty(uint4& v, uint32_t listed) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      if (listed >> i & 1) w[i] = Empty8<T>::word;
+    } else {
+      if (listed >> (2 * i) & 1) w[i] = (w[i] & 0xFFFF0000u) | (Empty8<T>::word & 0xFFFFu);
+      if (listed >> (2 * i + 1) & 1) w[i] = (w[i] & 0xFFFFu) | (Empty8<T>::word & 0xFFFF0000u);
+    }
+  }
+  v = make_uint4(w[0], w[1], w[2], w[3]);
 }
 template <typename T>
-__device__ __forceinline__ f2 pair_of(const Raw8<T>& r, int i) {
-  const uint32_t* w = reinterpret_cast<const uint32_t*>(&r);
+__device__ __forceinline__ uint4 empty_unit() { return make_uint4(Empty8<T>::word, Empty8<T>::word, Empty8<T>::word, Empty8<T>::word); }
+// A unit's bits in the row of bits, one a token.
+template <typename T>
+__device__ __forceinline__ uint32_t unit_bits(const uint32_t* bits, int u) {
+  const uint8_t* b = reinterpret_cast<const uint8_t*>(bits);
+  return kPer<T> == 8 ? b[u] : b[u >> 1] >> ((u & 1) * 4) & 15u;
+}
+template <typename T>
+__device__ __forceinline__ f2 pair_of(const uint4& v, int i) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
   if constexpr (sizeof(T) == 4) return make2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
   else if constexpr (std::is_same<T, __half>::value) {
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
     return make2(f.x, f.y);
   } else return make2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+}
+template <typename T>
+__device__ __forceinline__ void store_unit(T* to, const float (&g)[kPer<T>]) {
+  if constexpr (sizeof(T) == 4) __stcs((float4*)to, make_float4(g[0], g[1], g[2], g[3]));
+  else __stcs((uint4*)to, make_uint4(pack2(g[0], g[1], T()), pack2(g[2], g[3], T()), pack2(g[4], g[5], T()), pack2(g[6], g[7], T())));
 }
 
 __device__ __forceinline__ unsigned long long top_key(float x, int id) {
@@ -346,8 +368,8 @@ __device__ __forceinline__ float key_value(unsigned long long key) {
   return __uint_as_float(b >> 31 ? b ^ 0x80000000u : ~b);
 }
 
-// A part of a row.  Units of eight tokens lie on 16-byte boundaries of the row's memory.  The up to 14 tokens before the first and
-// behind the last one, the row's edges, are part 0's, one a thread.
+// A part of a row.  Units lie on 16-byte boundaries of the row's memory.  The up to 14 tokens before the first and behind the last one,
+// the row's edges, are part 0's, one a thread.
 template <typename T>
 struct RowPart {
   const T* in;
@@ -355,21 +377,21 @@ struct RowPart {
   __device__ __forceinline__ RowPart(const TokenParams& p, int row, int part_) : part(part_) {
     in = (const T*)p.in + row * p.in_stride;
     head = min((int)((16 - ((uintptr_t)in & 15)) & 15) / (int)sizeof(T), p.vocab);
-    units = (p.vocab - head) / kUnit;
+    units = (p.vocab - head) / kPer<T>;
     first = part * p.units;
     last = min(first + p.units, units);
-    edges = part == 0 ? p.vocab - units * kUnit : 0;
+    edges = part == 0 ? p.vocab - units * kPer<T> : 0;
   }
   __device__ __forceinline__ bool owns(int t) const {
-    const int u = (t - head) >> 3;
+    const int u = (t - head) >> (kPer<T> == 8 ? 3 : 2);
     return u < 0 || u >= units ? part == 0 : u >= first && u < last;
   }
-  __device__ __forceinline__ int edge(int i) const { return i < head ? i : i + units * kUnit; }
+  __device__ __forceinline__ int edge(int i) const { return i < head ? i : i + units * kPer<T>; }
 };
 
-template <typename T> constexpr int kTokUnits = sizeof(T) == 4 ? KU / 2 : KU;          // units of a thread and tile
-template <typename T> constexpr int kTileUnits = kTokUnits<T> * kTokThreads;
-template <typename T> constexpr int kTileBytes = kTileUnits<T> * kUnit * (int)sizeof(T);
+constexpr int kTokUnits = 8;                    // units of a thread and tile
+constexpr int kTileUnits = kTokUnits * kTokThreads;
+constexpr int kTileBytes = kTileUnits * 16;
 
 // The n-th largest of the warp's values, 1 <= n <= 32.
 __device__ __forceinline__ float nth_largest(float v, int n) {
@@ -430,21 +452,18 @@ __device__ __noinline__ void select_top(TopShared& s, const RowPart<T>& at, int 
   if (edge_x >= bound && edge_x > -INFINITY) s.push(edge_x, at.edge(tid));
   if (list_x >= bound && list_x > -INFINITY) s.push(list_x, list_id);
   __syncthreads();
-  const int work = s.groups * kTokUnits<T>;
+  const int work = s.groups * kTokUnits;
   for (int i = tid; i < work; i += kTokThreads) {
-    const int g = s.group[i / kTokUnits<T>], j = i % kTokUnits<T>;
-    const int u = g / kTokThreads * kTileUnits<T> + j * kTokThreads + g % kTokThreads;
+    const int g = s.group[i / kTokUnits], j = i % kTokUnits;
+    const int u = g / kTokThreads * kTileUnits + j * kTokThreads + g % kTokThreads;
     if (at.first + u >= at.last) continue;
-    const int t0 = at.head + (at.first + u) * kUnit;
-    Raw8<T> raw;
-    const uint4* from = (const uint4*)(at.in + t0);
+    const int t0 = at.head + (at.first + u) * kPer<T>;
+    const uint4 unit = *(const uint4*)(at.in + t0);
+    const uint32_t listed = bits ? unit_bits<T>(bits, u) : 0u;
 #pragma unroll
-    for (int k = 0; k < (int)sizeof(T) / 2; ++k) raw.v[k] = from[k];
-    const uint32_t listed = bits ? reinterpret_cast<const uint8_t*>(bits)[u] : 0u;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < kPer<T> / 2; ++k) {
       float x0, x1;
-      split2(pair_of(raw, k), x0, x1);
+      split2(pair_of<T>(unit, k), x0, x1);
       if (x0 >= bound && x0 > -INFINITY && !(listed >> (2 * k) & 1)) s.push(x0, t0 + 2 * k);
       if (x1 >= bound && x1 > -INFINITY && !(listed >> (2 * k + 1) & 1)) s.push(x1, t0 + 2 * k + 1);
     }
@@ -455,7 +474,7 @@ __device__ __noinline__ void select_top(TopShared& s, const RowPart<T>& at, int 
   if (total > kCandidates) {
     // Many equal logits: the n-th largest key of the part, eight bits at a time, until few enough reach it.
     auto each = [&](auto f) {
-      for (int t = at.head + at.first * kUnit + tid; t < at.head + at.last * kUnit; t += kTokThreads) {
+      for (int t = at.head + at.first * kPer<T> + tid; t < at.head + at.last * kPer<T>; t += kTokThreads) {
         const float x = to_float(at.in[t]);
         if (x > -INFINITY) f(top_key(x, t));
       }
@@ -531,11 +550,11 @@ struct Slope2 {
   }
 };
 template <typename T, bool kEnt>
-__device__ __forceinline__ void slope8(const Raw8<T>& r, const Slope2& k, float (&g)[8]) {
+__device__ __forceinline__ void slope_unit(const uint4& v, const Slope2& k, float (&g)[kPer<T>]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < kPer<T> / 2; ++i) {
     float y0, y1;
-    split2(fma2(pair_of(r, i), k.c, k.nr), y0, y1);
+    split2(fma2(pair_of<T>(v, i), k.c, k.nr), y0, y1);
     const f2 e = make2(ex2(y0), ex2(y1));
     f2 f = k.a;
     if (kEnt) f = fma2(make2(fmaxf(y0, kFloorY), fmaxf(y1, kFloorY)), k.b, k.a);
@@ -545,7 +564,7 @@ __device__ __forceinline__ void slope8(const Raw8<T>& r, const Slope2& k, float 
 // A part from memory, logit by logit, differences first: whose reference is that far down, or whose gradient lies off 16 bytes.
 template <typename T>
 __device__ __noinline__ void slope_huge(const RowPart<T>& at, T* dl, const TokenSlope& k, float c) {
-  for (int t = at.head + at.first * kUnit + threadIdx.x; t < at.head + at.last * kUnit; t += kTokThreads) {
+  for (int t = at.head + at.first * kPer<T> + threadIdx.x; t < at.head + at.last * kPer<T>; t += kTokThreads) {
     const float y = (to_float(at.in[t]) - k.ref) * c - k.l2;
     dl[t] = from_float<T>(ex2(y) * fmaf(fmaxf(y, kFloorY), k.b * kLn2, k.a));
   }
@@ -636,33 +655,29 @@ __device__ __forceinline__ uint64_t keep_policy(bool again) {
 }
 // Unit j of the thread in a tile.
 template <typename T>
-__device__ __forceinline__ void load_unit(const T* at, int j, uint64_t policy, Raw8<T>& r) {
-  const uint4* from = (const uint4*)(at + j * kTokThreads * kUnit);
-#pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i)
-    asm volatile("ld.global.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
-                 : "=r"(r.v[i].x), "=r"(r.v[i].y), "=r"(r.v[i].z), "=r"(r.v[i].w) : "l"(from + i), "l"(policy) : "memory");
+__device__ __forceinline__ void load_unit(const T* at, int j, uint64_t policy, uint4& v) {
+  asm volatile("ld.global.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(at + j * kTokThreads * kPer<T>), "l"(policy) : "memory");
 }
 template <typename T>
-__device__ __forceinline__ bool whole_tile(const RowPart<T>& at, int tile) { return at.first + (tile + 1) * kTileUnits<T> <= at.last; }
+__device__ __forceinline__ bool whole_tile(const RowPart<T>& at, int tile) { return at.first + (tile + 1) * kTileUnits <= at.last; }
 // The thread's place in a tile.
 template <typename T>
 __device__ __forceinline__ const T* tile_at(const RowPart<T>& at, int tile) {
-  return at.in + at.head + (int64_t)(at.first + tile * kTileUnits<T> + (int)threadIdx.x) * kUnit;
+  return at.in + at.head + (int64_t)(at.first + tile * kTileUnits + (int)threadIdx.x) * kPer<T>;
 }
 // The thread's units of a tile; -inf where the part has none.
 template <typename T>
-__device__ __forceinline__ void load_tile(const RowPart<T>& at, int tile, uint64_t policy, Raw8<T> (&raw)[kTokUnits<T>]) {
+__device__ __forceinline__ void load_tile(const RowPart<T>& at, int tile, uint64_t policy, uint4 (&raw)[kTokUnits]) {
   const T* from = tile_at(at, tile);
   if (whole_tile(at, tile)) {
 #pragma unroll
-    for (int j = 0; j < kTokUnits<T>; ++j) load_unit(from, j, policy, raw[j]);
+    for (int j = 0; j < kTokUnits; ++j) load_unit(from, j, policy, raw[j]);
   } else {
-    const int u0 = at.first + tile * kTileUnits<T> + (int)threadIdx.x;
+    const int u0 = at.first + tile * kTileUnits + (int)threadIdx.x;
 #pragma unroll
-    for (int j = 0; j < kTokUnits<T>; ++j) {
-#pragma unroll
-      for (int i = 0; i < (int)sizeof(Raw8<T>) / 4; ++i) word_of(raw[j], i) = Empty8<T>::word;
+    for (int j = 0; j < kTokUnits; ++j) {
+      raw[j] = empty_unit<T>();
       if (u0 + j * kTokThreads < at.last) load_unit(from, j, policy, raw[j]);
     }
   }
@@ -671,29 +686,29 @@ __device__ __forceinline__ void load_tile(const RowPart<T>& at, int tile, uint64
 // The gradient of a tile in registers; dl: of the row's first unit, its units on 16 bytes.  kAsk: as a unit is done with, the next tile's
 // is asked for (from); that tile is whole.
 template <typename T, bool kEnt, bool kAsk>
-__device__ __forceinline__ void slope_tile(const RowPart<T>& at, int tile, Raw8<T> (&raw)[kTokUnits<T>], const Slope2& k, T* dl, const T* from,
+__device__ __forceinline__ void slope_tile(const RowPart<T>& at, int tile, uint4 (&raw)[kTokUnits], const Slope2& k, T* dl, const T* from,
                                            uint64_t policy) {
-  const int left = at.last - at.first - tile * kTileUnits<T> - (int)threadIdx.x;   // units from the thread's first on
-  T* to = dl + (int64_t)(at.first + tile * kTileUnits<T> + (int)threadIdx.x) * kUnit;
+  const int left = at.last - at.first - tile * kTileUnits - (int)threadIdx.x;   // units from the thread's first on
+  T* to = dl + (int64_t)(at.first + tile * kTileUnits + (int)threadIdx.x) * kPer<T>;
 #pragma unroll
-  for (int j = 0; j < kTokUnits<T>; ++j) {
-    float g[8];
-    slope8<T, kEnt>(raw[j], k, g);
+  for (int j = 0; j < kTokUnits; ++j) {
+    float g[kPer<T>];
+    slope_unit<T, kEnt>(raw[j], k, g);
     if (kAsk) load_unit(from, j, policy, raw[j]);
-    if (j * kTokThreads < left) store8(to + j * kTokThreads * kUnit, g);
+    if (j * kTokThreads < left) store_unit<T>(to + j * kTokThreads * kPer<T>, g);
   }
 }
 // The sums of a tile in registers, against y = l c - r.
 template <typename T, bool kEnt, bool kAsk>
-__device__ __forceinline__ void sum_tile(Raw8<T> (&raw)[kTokUnits<T>], float c, float r, float& t0, float& t1, const T* from, uint64_t policy) {
+__device__ __forceinline__ void sum_tile(uint4 (&raw)[kTokUnits], float c, float r, float& t0, float& t1, const T* from, uint64_t policy) {
   const f2 nr = make2(-r, -r), c2 = make2(c, c);
   f2 a0 = make2(0.f, 0.f), a1 = a0, b0 = a0, b1 = a0;
 #pragma unroll
-  for (int j = 0; j < kTokUnits<T>; ++j) {
+  for (int j = 0; j < kTokUnits; ++j) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kPer<T> / 2; ++i) {
       float y0, y1;
-      split2(fma2(pair_of(raw[j], i), c2, nr), y0, y1);
+      split2(fma2(pair_of<T>(raw[j], i), c2, nr), y0, y1);
       const f2 e = make2(ex2(y0), ex2(y1));
       if (i & 1) b0 = add2(b0, e);
       else a0 = add2(a0, e);
@@ -716,7 +731,7 @@ __device__ __forceinline__ void sum_tile(Raw8<T> (&raw)[kTokUnits<T>], float c, 
 template <typename T, bool kGrad, bool kEnt, bool kRest>
 __global__ void __launch_bounds__(kTokThreads, kTokCtas)
 token_kernel(const __grid_constant__ TokenParams p) {
-  constexpr int kUnits = kTokUnits<T>, kTile = kTileUnits<T>;
+  constexpr int kUnits = kTokUnits, kTile = kTileUnits;
   __shared__ TokenShared s;
   extern __shared__ __align__(16) unsigned char more[];             // a tile; TopShared and the parts' lists if there are alternatives; bits (kRest)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -726,13 +741,13 @@ token_kernel(const __grid_constant__ TokenParams p) {
   if (many) cluster_arrive();                                       // all CTAs run before one writes into another's memory
   const int n_ids = p.t.n_ids, n_list = p.t.n_teacher, n_top = p.t.n_top;
   const int lists = (n_list + 31) / 32;
-  unsigned char* const behind = more + (kGrad && kOnChip > 1 && p.tiles > 1 ? kTileBytes<T> : 0);
+  unsigned char* const behind = more + (kGrad && kOnChip > 1 && p.tiles > 1 ? kTileBytes : 0);
   TopShared& top = *reinterpret_cast<TopShared*>(behind);
   unsigned long long* const merge = reinterpret_cast<unsigned long long*>(behind + top_bytes(p.tiles));
   uint32_t* const bits = reinterpret_cast<uint32_t*>(behind + (n_top ? top_bytes(p.tiles) + (many ? kMergeBytes : 0) : 0));
 
   uint4* const kept = reinterpret_cast<uint4*>(more) + tid;         // a thread's own places: its units of tile 1, those of tile 0 stay in registers
-  Raw8<T> raw[kUnits];
+  uint4 raw[kUnits];
   const uint64_t last_read = keep_policy(false), read_again = keep_policy(true);
   load_tile(at, p.tiles - 1, kGrad && p.tiles > kOnChip ? read_again : last_read, raw);                       // the part's cut tile first: the last two, that stay here, are whole
   const float inv = p.t.temperature ? 1.f / p.t.temperature[row] : 1.f, c = inv * kLog2e;
@@ -764,16 +779,16 @@ token_kernel(const __grid_constant__ TokenParams p) {
     if (lane == 0) s.dsum[warp] = d;
   }
   if constexpr (kRest)
-    for (int i = tid; i < (p.units + 3) / 4; i += kTokThreads) bits[i] = 0;
+    for (int i = tid; i < (p.units * kPer<T> + 31) / 32; i += kTokThreads) bits[i] = 0;
   if (kRest && tid == 0) s.edges = 0;
   if (n_list > 0) {
     __syncthreads();
     if (my.tid >= 0) {
       if (again_later(s, my.tid, n_list)) my.tid = -1;
       else if (kRest && at.owns(my.tid)) {
-        const int t = my.tid - at.head, u = t >> 3;
-        if (u < 0 || u >= at.units) atomicOr(&s.edges, 1u << (u < 0 ? my.tid : my.tid - at.units * kUnit));
-        else atomicOr(&bits[(t - at.first * kUnit) >> 5], 1u << ((t - at.first * kUnit) & 31));
+        const int t = my.tid - at.head;
+        if (t < 0 || t >= at.units * kPer<T>) atomicOr(&s.edges, 1u << (t < 0 ? my.tid : my.tid - at.units * kPer<T>));
+        else atomicOr(&bits[(t - at.first * kPer<T>) >> 5], 1u << ((t - at.first * kPer<T>) & 31));
       }
     }
     if (kRest) __syncthreads();
@@ -784,21 +799,17 @@ token_kernel(const __grid_constant__ TokenParams p) {
 #pragma unroll
       for (int j = 0; j < kUnits; ++j) {
         const int u = tile * kTile + j * kTokThreads + tid;
-        const uint32_t b = u < p.units ? reinterpret_cast<const uint8_t*>(bits)[u] : 0u;
-        if (b) {
-#pragma unroll
-          for (int k = 0; k < kUnit; ++k)
-            if (b >> k & 1) set_empty(raw[j], k);
-        }
+        const uint32_t b = u < p.units ? unit_bits<T>(bits, u) : 0u;
+        if (b) set_empty<T>(raw[j], b);
       }
     }
   };
   // The thread's units of a tile whose logits are all that far down, from memory: differences first.
   auto sum_huge = [&](const RowPart<T>& at, const uint32_t* bits, float m, float c, int tile, float& s0, float& s1) {
     for (int u = tile * kTile + tid; u < (tile + 1) * kTile && at.first + u < at.last; u += kTokThreads) {
-      for (int k = 0; k < kUnit; ++k) {
-        if (kRest && reinterpret_cast<const uint8_t*>(bits)[u] >> k & 1) continue;
-        const float y = (to_float(at.in[at.head + (at.first + u) * kUnit + k]) - m) * c, e = ex2(y);
+      for (int k = 0; k < kPer<T>; ++k) {
+        if (kRest && unit_bits<T>(bits, u) >> k & 1) continue;
+        const float y = (to_float(at.in[at.head + (at.first + u) * kPer<T> + k]) - m) * c, e = ex2(y);
         s0 += e;
         s1 += e * fmaxf(y, kFloorY);
       }
@@ -810,16 +821,11 @@ token_kernel(const __grid_constant__ TokenParams p) {
       mask_tile(tile);
       if (kGrad && tile == kOnChip - 1 && tile > 0) {
 #pragma unroll
-        for (int j = 0; j < kUnits; ++j)
-#pragma unroll
-          for (int i = 0; i < (int)sizeof(T) / 2; ++i) kept[(j * (int)sizeof(T) / 2 + i) * kTokThreads] = raw[j].v[i];
+        for (int j = 0; j < kUnits; ++j) kept[j * kTokThreads] = raw[j];
       }
       uint32_t w = Empty8<T>::word;
 #pragma unroll
-      for (int j = 0; j < kUnits; ++j) {
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(Raw8<T>) / 4; ++i) w = max2(w, word_of(raw[j], i), T());
-      }
+      for (int j = 0; j < kUnits; ++j) w = max_unit<T>(w, raw[j]);
       const float tm = max_of<T>(w);
       refer(m, fmaxf(m, tm), c, s0, s1);
       m = fmaxf(m, tm);
@@ -972,9 +978,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
           else slope_tile<T, kEnt, false>(at, tile, raw, k, dl + at.head, nullptr, 0);
           if (next < kOnChip && next < p.tiles) {
 #pragma unroll
-            for (int j = 0; j < kUnits; ++j)
-#pragma unroll
-              for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[j].v[i] = kept[(j * (int)sizeof(T) / 2 + i) * kTokThreads];
+            for (int j = 0; j < kUnits; ++j) raw[j] = kept[j * kTokThreads];
           } else if (next < p.tiles && !ask) {
             load_tile(at, next, last_read, raw);
           }
@@ -993,7 +997,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
 template <typename T, bool kEnt>
 __global__ void __launch_bounds__(kTokThreads, kTokCtas)
 token_backward_kernel(const __grid_constant__ TokenParams p) {
-  constexpr int kUnits = kTokUnits<T>;
+  constexpr int kUnits = kTokUnits;
   __shared__ TokenShared s;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int row = blockIdx.x / p.parts;
@@ -1015,14 +1019,12 @@ token_backward_kernel(const __grid_constant__ TokenParams p) {
     s.gdl[tid] = my.dl;
   }
   const bool quiet = !__syncthreads_or(my.dl != 0.f || dh != 0.f || dd != 0.f);
-  Raw8<T> raw[kUnits];
+  uint4 raw[kUnits];
   if (!quiet) {
     load_tile(at, 0, keep_policy(false), raw);
   } else {
 #pragma unroll
-    for (int j = 0; j < kUnits; ++j)
-#pragma unroll
-      for (int i = 0; i < (int)sizeof(Raw8<T>) / 4; ++i) word_of(raw[j], i) = Empty8<T>::word;
+    for (int j = 0; j < kUnits; ++j) raw[j] = empty_unit<T>();
   }
   const float edge_x = tid < at.edges && !quiet ? to_float(at.in[at.edge(tid)]) : -INFINITY;
   if (my.id >= 0 && at.owns(my.id)) my.x = to_float(at.in[my.id]);
@@ -1057,12 +1059,12 @@ token_backward_kernel(const __grid_constant__ TokenParams p) {
 
 template <typename T, bool kGrad, bool kEnt, bool kRest>
 int launch_forward(TokenParams p, cudaStream_t st) {
-  constexpr int kTile = kTileUnits<T>;
-  const int total = std::max(p.vocab / kUnit, 1);
+  constexpr int kTile = kTileUnits;
+  const int total = std::max(p.vocab / kPer<T>, 1);
   int parts = 1;
   // Rows that are read twice: parts of 128 KB, so that what all SMs work on stays in the L2 cache.  With a bucket: bits of 16 KB at most.
-  if (kGrad) parts = std::min((total * (int)sizeof(T) * kUnit + kPartBytes - 1) / kPartBytes, kMostParts);
-  else if (kRest) parts = std::min((total + 16383) / 16384, kMostParts);
+  if (kGrad) parts = std::min((total * 16 + kPartBytes - 1) / kPartBytes, kMostParts);
+  else if (kRest) parts = (p.vocab + 131071) / 131072;
   // more, down to a unit a thread, while that leaves SMs without work
   while (parts * 2 <= kMostParts && (int64_t)p.n_rows * parts < 2 * 148 && total / parts >= 2 * kTokThreads) parts *= 2;
   if (p.t.n_top) parts = std::max(parts, (total + kMostTiles * kTile - 1) / (kMostTiles * kTile));
@@ -1070,10 +1072,10 @@ int launch_forward(TokenParams p, cudaStream_t st) {
   p.units = (total + parts - 1) / parts;
   p.tiles = (p.units + kTile - 1) / kTile;
   if ((int64_t)p.n_rows * parts > 0x7FFFFFFFLL) return PG_EINVAL;
-  const int bytes = (kGrad && kOnChip > 1 && p.tiles > 1 ? kTileBytes<T> : 0) + (p.t.n_top ? top_bytes(p.tiles) + (parts > 1 ? kMergeBytes : 0) : 0) + (kRest ? (p.units + 3) / 4 * 4 : 0);
+  const int bytes = (kGrad && kOnChip > 1 && p.tiles > 1 ? kTileBytes : 0) + (p.t.n_top ? top_bytes(p.tiles) + (parts > 1 ? kMergeBytes : 0) : 0) + (kRest ? (p.units * kPer<T> + 31) / 32 * 4 : 0);
   auto kernel = token_kernel<T, kGrad, kEnt, kRest>;
   static std::atomic<uint64_t> done{0};
-  constexpr int kMostBytes = kTileBytes<T> + (int)sizeof(TopShared) + kMergeBytes + PG_TOKEN_MAX_VOCAB / kUnit / kMostParts + 64;
+  constexpr int kMostBytes = kTileBytes + (int)sizeof(TopShared) + kMergeBytes + PG_TOKEN_MAX_VOCAB / 8 / kMostParts + 64;
   if (bytes > 32 * 1024)
     if (const int rc = allow_shared(kernel, kMostBytes, done)) return rc;
   cudaLaunchConfig_t cfg = {};
@@ -1094,8 +1096,8 @@ int launch_forward(TokenParams p, cudaStream_t st) {
 
 template <typename T, bool kEnt>
 int launch_backward(TokenParams p, cudaStream_t st) {
-  const int total = std::max(p.vocab / kUnit, 1);
-  p.parts = (total + kTileUnits<T> - 1) / kTileUnits<T>;
+  const int total = std::max(p.vocab / kPer<T>, 1);
+  p.parts = (total + kTileUnits - 1) / kTileUnits;
   p.units = (total + p.parts - 1) / p.parts;
   if ((int64_t)p.n_rows * p.parts > 0x7FFFFFFFLL) return PG_EINVAL;
   token_backward_kernel<T, kEnt><<<(unsigned)(p.n_rows * p.parts), kTokThreads, 0, st>>>(p);
