@@ -37,6 +37,9 @@ constexpr int kTokCtas = NB;                    // of an SM
 #define PB 131072
 #endif
 constexpr int kPartBytes = PB;
+#ifndef MT
+#define MT 4
+#endif
 #ifndef OC
 #define OC 2
 #endif
@@ -220,12 +223,6 @@ __device__ __forceinline__ void set_empty(uint4& v, uint32_t listed) {
 }
 template <typename T>
 __device__ __forceinline__ uint4 empty_unit() { return make_uint4(Empty8<T>::word, Empty8<T>::word, Empty8<T>::word, Empty8<T>::word); }
-// A unit's bits in the row of bits, one a token.
-template <typename T>
-__device__ __forceinline__ uint32_t unit_bits(const uint32_t* bits, int u) {
-  const uint8_t* b = reinterpret_cast<const uint8_t*>(bits);
-  return kPer<T> == 8 ? b[u] : b[u >> 1] >> ((u & 1) * 4) & 15u;
-}
 template <typename T>
 __device__ __forceinline__ f2 pair_of(const uint4& v, int i) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -340,12 +337,12 @@ __device__ __forceinline__ TokenRow finish_row(const TokenShared& s, const float
   }
   const double mass = warp_total(l.mass);
   const double tr = fmax(1. - mass, 1. / (1 << 20));
-  r.lt = (float)log(tr);
+  r.lt = logf((float)tr);
   r.w = (float)(outside ? mass + tr : mass);
   if (mass != mass) r.lt = r.w = NAN;
   if (kind == PG_DISTILL_FORWARD_REST) {
     const float tlp = warp_total(l.ts != 0.f ? l.ty + l.ts * ((finite_ref(l.m) - r.m) * inv - kLn2 * r.l2) : 0.f);
-    r.loss = warp_total(l.ttl) - tlp + (outside ? (float)(tr * (r.lt - lr)) : 0.f);
+    r.loss = warp_total(l.ttl) - tlp + (outside ? r.lr > -1e30f ? (float)tr * (r.lt - r.lr) : (float)(tr * (r.lt - lr)) : 0.f);
   } else {
     float plp = 0.f, ptl = 0.f;
     if (l.s0 != 0.f) {
@@ -392,6 +389,10 @@ struct RowPart {
 constexpr int kTokUnits = 8;                    // units of a thread and tile
 constexpr int kTileUnits = kTokUnits * kTokThreads;
 constexpr int kTileBytes = kTileUnits * 16;
+// Bits of listed tokens: a byte for each unit u of a part, a thread's of a tile side by side.
+__device__ __forceinline__ int bits_at(int u) {
+  return (u / kTileUnits * kTokThreads + u % kTokThreads) * kTokUnits + u % kTileUnits / kTokThreads;
+}
 
 // The n-th largest of the warp's values, 1 <= n <= 32.
 __device__ __forceinline__ float nth_largest(float v, int n) {
@@ -430,7 +431,7 @@ __host__ __device__ constexpr int top_bytes(int tiles) { return (int)sizeof(TopS
 // them make n; so the n-th largest logit is not below the least of these bounds, and few of the threads' tiles reach it.
 template <typename T>
 __device__ __noinline__ void select_top(TopShared& s, const RowPart<T>& at, int n, int tiles, float m, float edge_x, float list_x, int list_id,
-                                        const uint32_t* bits) {
+                                        const uint8_t* bits) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const float own = nth_largest(m, (n + kTokWarps - 1) / kTokWarps);
   if (lane == 0) s.bounds[warp] = own;
@@ -459,7 +460,7 @@ __device__ __noinline__ void select_top(TopShared& s, const RowPart<T>& at, int 
     if (at.first + u >= at.last) continue;
     const int t0 = at.head + (at.first + u) * kPer<T>;
     const uint4 unit = *(const uint4*)(at.in + t0);
-    const uint32_t listed = bits ? unit_bits<T>(bits, u) : 0u;
+    const uint32_t listed = bits ? bits[bits_at(u)] : 0u;
 #pragma unroll
     for (int k = 0; k < kPer<T> / 2; ++k) {
       float x0, x1;
@@ -563,10 +564,14 @@ __device__ __forceinline__ void slope_unit(const uint4& v, const Slope2& k, floa
 }
 // A part from memory, logit by logit, differences first: whose reference is that far down, or whose gradient lies off 16 bytes.
 template <typename T>
-__device__ __noinline__ void slope_huge(const RowPart<T>& at, T* dl, const TokenSlope& k, float c) {
+__device__ __noinline__ void slope_huge(const RowPart<T>& at, T* dl, const TokenSlope& k, float c, bool quiet = false) {
   for (int t = at.head + at.first * kPer<T> + threadIdx.x; t < at.head + at.last * kPer<T>; t += kTokThreads) {
-    const float y = (to_float(at.in[t]) - k.ref) * c - k.l2;
-    dl[t] = from_float<T>(ex2(y) * fmaf(fmaxf(y, kFloorY), k.b * kLn2, k.a));
+    float g = 0.f;
+    if (!quiet) {
+      const float y = (to_float(at.in[t]) - k.ref) * c - k.l2;
+      g = ex2(y) * fmaf(fmaxf(y, kFloorY), k.b * kLn2, k.a);
+    }
+    dl[t] = from_float<T>(g);
   }
 }
 template <typename T>
@@ -744,8 +749,12 @@ token_kernel(const __grid_constant__ TokenParams p) {
   unsigned char* const behind = more + (kGrad && kOnChip > 1 && p.tiles > 1 ? kTileBytes : 0);
   TopShared& top = *reinterpret_cast<TopShared*>(behind);
   unsigned long long* const merge = reinterpret_cast<unsigned long long*>(behind + top_bytes(p.tiles));
-  uint32_t* const bits = reinterpret_cast<uint32_t*>(behind + (n_top ? top_bytes(p.tiles) + (many ? kMergeBytes : 0) : 0));
+  uint8_t* const bits = reinterpret_cast<uint8_t*>(behind + (n_top ? top_bytes(p.tiles) + (many ? kMergeBytes : 0) : 0));
 
+  if constexpr (kRest) {
+    for (int i = tid; i < p.tiles * kTokThreads; i += kTokThreads) reinterpret_cast<uint2*>(bits)[i] = make_uint2(0u, 0u);
+    if (tid == 0) s.edges = 0;
+  }
   uint4* const kept = reinterpret_cast<uint4*>(more) + tid;         // a thread's own places: its units of tile 1, those of tile 0 stay in registers
   uint4 raw[kUnits];
   const uint64_t last_read = keep_policy(false), read_again = keep_policy(true);
@@ -778,37 +787,34 @@ token_kernel(const __grid_constant__ TokenParams p) {
     const float d = warp_total(my.dl);
     if (lane == 0) s.dsum[warp] = d;
   }
-  if constexpr (kRest)
-    for (int i = tid; i < (p.units * kPer<T> + 31) / 32; i += kTokThreads) bits[i] = 0;
-  if (kRest && tid == 0) s.edges = 0;
-  if (n_list > 0) {
-    __syncthreads();
-    if (my.tid >= 0) {
-      if (again_later(s, my.tid, n_list)) my.tid = -1;
-      else if (kRest && at.owns(my.tid)) {
-        const int t = my.tid - at.head;
-        if (t < 0 || t >= at.units * kPer<T>) atomicOr(&s.edges, 1u << (t < 0 ? my.tid : my.tid - at.units * kPer<T>));
-        else atomicOr(&bits[(t - at.first * kPer<T>) >> 5], 1u << ((t - at.first * kPer<T>) & 31));
+  if constexpr (kRest) {
+    __syncthreads();                                                // the bits are zero
+    if (my.tid >= 0 && at.owns(my.tid)) {
+      const int t = my.tid - at.head;
+      if (t < 0 || t >= at.units * kPer<T>) {
+        atomicOr(&s.edges, 1u << (t < 0 ? my.tid : my.tid - at.units * kPer<T>));
+      } else {
+        const int b = bits_at(t / kPer<T> - at.first);
+        atomicOr(reinterpret_cast<uint32_t*>(bits) + (b >> 2), 1u << ((b & 3) * 8 + t % kPer<T>));
       }
     }
-    if (kRest) __syncthreads();
+    __syncthreads();
   }
   // Takes the listed tokens out of the registers.
   auto mask_tile = [&](int tile) {
     if constexpr (kRest) {
+      const uint2 b = reinterpret_cast<const uint2*>(bits)[tile * kTokThreads + tid];
+      if (b.x | b.y) {
 #pragma unroll
-      for (int j = 0; j < kUnits; ++j) {
-        const int u = tile * kTile + j * kTokThreads + tid;
-        const uint32_t b = u < p.units ? unit_bits<T>(bits, u) : 0u;
-        if (b) set_empty<T>(raw[j], b);
+        for (int j = 0; j < kUnits; ++j) set_empty<T>(raw[j], (j < 4 ? b.x : b.y) >> (j % 4 * 8) & 255u);
       }
     }
   };
   // The thread's units of a tile whose logits are all that far down, from memory: differences first.
-  auto sum_huge = [&](const RowPart<T>& at, const uint32_t* bits, float m, float c, int tile, float& s0, float& s1) {
+  auto sum_huge = [&](const RowPart<T>& at, const uint8_t* bits, float m, float c, int tile, float& s0, float& s1) {
     for (int u = tile * kTile + tid; u < (tile + 1) * kTile && at.first + u < at.last; u += kTokThreads) {
       for (int k = 0; k < kPer<T>; ++k) {
-        if (kRest && unit_bits<T>(bits, u) >> k & 1) continue;
+        if (kRest && bits[bits_at(u)] >> k & 1) continue;
         const float y = (to_float(at.in[at.head + (at.first + u) * kPer<T> + k]) - m) * c, e = ex2(y);
         s0 += e;
         s1 += e * fmaxf(y, kFloorY);
@@ -858,7 +864,9 @@ token_kernel(const __grid_constant__ TokenParams p) {
       s1 += e * fmaxf(y, kFloorY);
       edge_left = x;
     }
+      if (n_list > 0 && !kRest) __syncthreads();                      // the list's ids are there
     if (warp < lists) {
+      if (my.tid >= 0 && again_later(s, my.tid, n_list)) my.tid = -1;
       const bool used = my.tid >= 0;
       const float x = used ? my.tx : -INFINITY;
       ListSums l;
@@ -1019,9 +1027,10 @@ token_backward_kernel(const __grid_constant__ TokenParams p) {
     s.gdl[tid] = my.dl;
   }
   const bool quiet = !__syncthreads_or(my.dl != 0.f || dh != 0.f || dd != 0.f);
+  const uint64_t last_read = keep_policy(false);
   uint4 raw[kUnits];
   if (!quiet) {
-    load_tile(at, 0, keep_policy(false), raw);
+    load_tile(at, p.tiles - 1, last_read, raw);                     // the cut tile first
   } else {
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) raw[j] = empty_unit<T>();
@@ -1049,8 +1058,16 @@ token_backward_kernel(const __grid_constant__ TokenParams p) {
   const Slope2 k(slope, c);
   T* dl = (T*)p.dl + row * p.dl_stride;
   const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0, huge = !aligned || (slope.ref < -kHuge && !quiet);
-  if (huge) slope_huge(at, dl, slope, c);
-  else slope_tile<T, kEnt, false>(at, 0, raw, k, dl + at.head, nullptr, 0);
+  if (huge) {
+    slope_huge(at, dl, slope, c, quiet);
+  } else {
+    for (int tile = p.tiles - 1; tile >= 0; --tile) {
+      const bool ask = tile > 0 && !quiet && whole_tile(at, tile - 1);
+      if (ask) slope_tile<T, kEnt, true>(at, tile, raw, k, dl + at.head, tile_at(at, tile - 1), last_read);
+      else slope_tile<T, kEnt, false>(at, tile, raw, k, dl + at.head, nullptr, 0);
+      if (tile > 0 && !ask && !quiet) load_tile(at, tile - 1, last_read, raw);
+    }
+  }
   if (tid < at.edges) put_edge(dl + at.edge(tid), edge_x, slope, c);
   if (quiet || (n_ids == 0 && !distill)) return;
   __syncthreads();
@@ -1064,7 +1081,7 @@ int launch_forward(TokenParams p, cudaStream_t st) {
   int parts = 1;
   // Rows that are read twice: parts of 128 KB, so that what all SMs work on stays in the L2 cache.  With a bucket: bits of 16 KB at most.
   if (kGrad) parts = std::min((total * 16 + kPartBytes - 1) / kPartBytes, kMostParts);
-  else if (kRest) parts = (p.vocab + 131071) / 131072;
+  else if (kRest) parts = std::min((total + 16383) / 16384, kMostParts);
   // more, down to a unit a thread, while that leaves SMs without work
   while (parts * 2 <= kMostParts && (int64_t)p.n_rows * parts < 2 * 148 && total / parts >= 2 * kTokThreads) parts *= 2;
   if (p.t.n_top) parts = std::max(parts, (total + kMostTiles * kTile - 1) / (kMostTiles * kTile));
@@ -1072,10 +1089,10 @@ int launch_forward(TokenParams p, cudaStream_t st) {
   p.units = (total + parts - 1) / parts;
   p.tiles = (p.units + kTile - 1) / kTile;
   if ((int64_t)p.n_rows * parts > 0x7FFFFFFFLL) return PG_EINVAL;
-  const int bytes = (kGrad && kOnChip > 1 && p.tiles > 1 ? kTileBytes : 0) + (p.t.n_top ? top_bytes(p.tiles) + (parts > 1 ? kMergeBytes : 0) : 0) + (kRest ? (p.units * kPer<T> + 31) / 32 * 4 : 0);
+  const int bytes = (kGrad && kOnChip > 1 && p.tiles > 1 ? kTileBytes : 0) + (p.t.n_top ? top_bytes(p.tiles) + (parts > 1 ? kMergeBytes : 0) : 0) + (kRest ? p.tiles * kTileUnits : 0);
   auto kernel = token_kernel<T, kGrad, kEnt, kRest>;
   static std::atomic<uint64_t> done{0};
-  constexpr int kMostBytes = kTileBytes + (int)sizeof(TopShared) + kMergeBytes + PG_TOKEN_MAX_VOCAB / 8 / kMostParts + 64;
+  constexpr int kMostBytes = kTileBytes + (int)sizeof(TopShared) + kMergeBytes + PG_TOKEN_MAX_VOCAB / 4 / kMostParts + kTileUnits;
   if (bytes > 32 * 1024)
     if (const int rc = allow_shared(kernel, kMostBytes, done)) return rc;
   cudaLaunchConfig_t cfg = {};
@@ -1097,8 +1114,12 @@ int launch_forward(TokenParams p, cudaStream_t st) {
 template <typename T, bool kEnt>
 int launch_backward(TokenParams p, cudaStream_t st) {
   const int total = std::max(p.vocab / kPer<T>, 1);
-  p.parts = (total + kTileUnits - 1) / kTileUnits;
+  // what a CTA learns of its row serves up to four tiles, where there are rows enough
+  const int tiles = (total + kTileUnits - 1) / kTileUnits;
+  const int most = (int)std::min<int64_t>(std::max<int64_t>((int64_t)p.n_rows * tiles / (2 * 148 * kTokCtas), 1), MT);
+  p.parts = (tiles + most - 1) / most;
   p.units = (total + p.parts - 1) / p.parts;
+  p.tiles = (p.units + kTileUnits - 1) / kTileUnits;
   if ((int64_t)p.n_rows * p.parts > 0x7FFFFFFFLL) return PG_EINVAL;
   token_backward_kernel<T, kEnt><<<(unsigned)(p.n_rows * p.parts), kTokThreads, 0, st>>>(p);
   PG_LAUNCH_CHECK();
