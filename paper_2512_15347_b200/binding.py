@@ -729,15 +729,16 @@ def logits_process(logits, out, rules: LogitsRules, stream=None) -> None:
 
 # ---------------------------------------------------------------- policy update on token trajectories
 
-def _f32(t, what: str, n: int, dev: int) -> Optional[int]:
+_FLOAT32 = torch.float32
+
+
+def _f32(t, what: str, n: int, dev: int) -> int:
     """Address of a contiguous fp32 tensor of n elements on device dev."""
-    if t is None:
-        return None
-    if t.dtype is not torch.float32 or not t.is_contiguous() or t.numel() != n:
-        raise ValueError(f"{what}: {n} contiguous fp32 elements")
+    if t.dtype is _FLOAT32 and t.numel() == n and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
     if t.get_device() != dev:
         raise _elsewhere(what, dev)
-    return t.data_ptr()
+    raise ValueError(f"{what}: {n} contiguous fp32 elements")
 
 
 def make_token_terms(*, temperature=None, ids=None, n_top: int = 0, teacher_ids=None, teacher_logp=None, kind: str = "forward") -> TokenTerms:
@@ -786,45 +787,72 @@ def make_token_terms(*, temperature=None, ids=None, n_top: int = 0, teacher_ids=
 
 
 def _token_rows(t, terms: TokenTerms, what: str):
-    """(rows, vocab, type, row stride, device) of logits or their gradient."""
-    if t.dim() != 2 or t.dtype not in _DTYPES:
+    """(rows, vocab, type, row stride, device) of logits."""
+    dtype = _DTYPES.get(t.dtype)
+    if dtype is None or t.dim() != 2:
         raise ValueError(f"{what}: [rows, vocab], fp32, bf16 or fp16")
     rows, vocab = t.shape
-    a, one = t.stride()
-    if (one != 1 and vocab > 1) or (rows > 1 and a < vocab):
-        raise ValueError(f"{what}: contiguous rows, apart")
     dev = t.get_device()
     at, on = terms._plain[:2]
     if dev < 0 or (on is not None and on != dev):
         raise ValueError(f"{what} and the terms: on one CUDA device")
     if at is not None and at != rows:
         raise ValueError("the terms are for another number of rows")
-    return rows, vocab, _DTYPES[t.dtype], a if rows > 1 else 0, dev
+    return rows, vocab, dtype, _row_stride(t, rows, vocab, what), dev
+
+
+def _row_stride(t, rows: int, vocab: int, what: str) -> int:
+    if t.is_contiguous():
+        return 0
+    a, one = t.stride()
+    if (one != 1 and vocab > 1) or (rows > 1 and a < vocab):
+        raise ValueError(f"{what}: contiguous rows, apart")
+    return a if rows > 1 else 0
 
 
 def _token_out(terms, rows, dev, logp, lse, entropy, top_ids, top_logp, distill, saved) -> TokenOut:
-    n_ids, n_top, n_teacher = terms._plain[2:]
-    if (logp is not None and not n_ids) or (distill is not None and not n_teacher) or (top_ids is not None and not n_top):
-        raise ValueError("an output that the terms do not ask for")
-    if top_logp is not None and top_ids is None:
-        raise ValueError("top_logp without top_ids")
-    return TokenOut(_f32(logp, "logp", rows * n_ids, dev), _f32(lse, "lse", rows, dev), _f32(entropy, "entropy", rows, dev),
-                    None if top_ids is None else _i32(top_ids, "top_ids", rows * n_top, dev), _f32(top_logp, "top_logp", rows * n_top, dev),
-                    _f32(distill, "distill", rows, dev), _f32(saved, "saved", rows * TOKEN_SAVED, dev))
+    _, _, n_ids, n_top, n_teacher = terms._plain
+    o = TokenOut()
+    if logp is not None:
+        _want(n_ids > 0, "logp: the terms have no ids")
+        o.logp = _f32(logp, "logp", rows * n_ids, dev)
+    if lse is not None:
+        o.lse = _f32(lse, "lse", rows, dev)
+    if entropy is not None:
+        o.entropy = _f32(entropy, "entropy", rows, dev)
+    if top_ids is not None:
+        _want(n_top > 0, "top_ids: the terms have no n_top")
+        o.top_ids = _i32(top_ids, "top_ids", rows * n_top, dev)
+    if top_logp is not None:
+        _want(top_ids is not None, "top_logp without top_ids")
+        o.top_logp = _f32(top_logp, "top_logp", rows * n_top, dev)
+    if distill is not None:
+        _want(n_teacher > 0, "distill: the terms have no teacher")
+        o.distill = _f32(distill, "distill", rows, dev)
+    if saved is not None:
+        o.saved = _f32(saved, "saved", rows * TOKEN_SAVED, dev)
+    return o
 
 
 def _token_grads(terms, rows, dev, dlogp, dentropy, ddistill, entropy_scale, distill_scale) -> TokenGrads:
-    n_ids, _, n_teacher = terms._plain[2:]
-    if (dlogp is not None and not n_ids) or (ddistill is not None and not n_teacher):
-        raise ValueError("a derivative of what the terms do not ask for")
-    return TokenGrads(_f32(dlogp, "dlogp", rows * n_ids, dev), _f32(dentropy, "dentropy", rows, dev), _f32(ddistill, "ddistill", rows, dev),
-                      entropy_scale, distill_scale)
+    _, _, n_ids, _, n_teacher = terms._plain
+    g = TokenGrads()
+    if dlogp is not None:
+        _want(n_ids > 0, "dlogp: the terms have no ids")
+        g.dlogp = _f32(dlogp, "dlogp", rows * n_ids, dev)
+    if dentropy is not None:
+        g.dentropy, g.entropy_scale = _f32(dentropy, "dentropy", rows, dev), entropy_scale
+    if ddistill is not None:
+        _want(n_teacher > 0, "ddistill: the terms have no teacher")
+        g.ddistill, g.distill_scale = _f32(ddistill, "ddistill", rows, dev), distill_scale
+    return g
 
 
-def _token_dlogits(logits, dlogits, terms):
-    if dlogits.dtype is not logits.dtype or dlogits.shape != logits.shape or dlogits.get_device() != logits.get_device():
+def _token_dlogits(logits, dlogits, rows: int, vocab: int, dev: int) -> int:
+    """Row stride of the gradient."""
+    if dlogits.dtype is not logits.dtype or dlogits.shape != logits.shape or dlogits.get_device() != dev:
         raise ValueError("dlogits: like the logits")
-    return _token_rows(dlogits, terms, "dlogits")[3]
+    return _row_stride(dlogits, rows, vocab, "dlogits")
 
 
 def token_forward(logits, terms: TokenTerms, *, logp=None, lse=None, entropy=None, top_ids=None, top_logp=None, distill=None, saved=None,
@@ -844,7 +872,8 @@ def token_backward(logits, terms: TokenTerms, saved, dlogits, *, dlogp=None, den
     _current(dev)
     grads = _token_grads(terms, rows, dev, dlogp, dentropy, ddistill, entropy_scale, distill_scale)
     _check(lib().pg_token_backward(rows, vocab, dtype, logits.data_ptr(), stride, terms._ref, _f32(saved, "saved", rows * TOKEN_SAVED, dev),
-                                   grads, dlogits.data_ptr(), _token_dlogits(logits, dlogits, terms), _stream(stream)), "pg_token_backward")
+                                   grads, dlogits.data_ptr(), _token_dlogits(logits, dlogits, rows, vocab, dev), _stream(stream)),
+           "pg_token_backward")
 
 
 def token_forward_backward(logits, terms: TokenTerms, dlogits, *, logp=None, lse=None, entropy=None, top_ids=None, top_logp=None,
@@ -856,7 +885,7 @@ def token_forward_backward(logits, terms: TokenTerms, dlogits, *, logp=None, lse
     out = _token_out(terms, rows, dev, logp, lse, entropy, top_ids, top_logp, distill, saved)
     grads = _token_grads(terms, rows, dev, dlogp, dentropy, ddistill, entropy_scale, distill_scale)
     _check(lib().pg_token_forward_backward(rows, vocab, dtype, logits.data_ptr(), stride, terms._ref, out, grads, dlogits.data_ptr(),
-                                           _token_dlogits(logits, dlogits, terms), _stream(stream)), "pg_token_forward_backward")
+                                           _token_dlogits(logits, dlogits, rows, vocab, dev), _stream(stream)), "pg_token_forward_backward")
 
 
 def token_objective_workspace_bytes(n_tokens: int) -> int:
@@ -877,13 +906,21 @@ def token_objective(start, logp_new, adv, objective, dlogp, workspace, *, logp_o
         raise ValueError("start: [rows + 1] int32")
     if norm not in TOKEN_NORMS:
         raise ValueError(f"norm: one of {TOKEN_NORMS}")
-    b = TokenBatch(_i32(start, "start", rows + 1, dev), _f32(logp_new, "logp_new", n, dev), _f32(logp_old, "logp_old", n, dev),
-                   _f32(logp_ref, "logp_ref", n, dev), _f32(adv, "adv", rows, dev), _f32(entropy, "entropy", n, dev),
-                   _f32(distill, "distill", n, dev), clip_low, clip_high, beta, entropy_coef, distill_coef, scale, TOKEN_NORMS.index(norm))
+    b = TokenBatch()
+    b.start, b.logp_new, b.adv = _i32(start, "start", rows + 1, dev), _f32(logp_new, "logp_new", n, dev), _f32(adv, "adv", rows, dev)
+    if logp_old is not None:
+        b.logp_old = _f32(logp_old, "logp_old", n, dev)
+    if logp_ref is not None:
+        b.logp_ref, b.beta = _f32(logp_ref, "logp_ref", n, dev), beta
+    if entropy is not None:
+        b.entropy, b.entropy_coef = _f32(entropy, "entropy", n, dev), entropy_coef
+    if distill is not None:
+        b.distill, b.distill_coef = _f32(distill, "distill", n, dev), distill_coef
+    b.clip_low, b.clip_high, b.scale, b.norm = clip_low, clip_high, scale, TOKEN_NORMS.index(norm)
     _check(lib().pg_token_objective(rows, n, b, _f32(objective, "objective", 1, dev), _f32(dlogp, "dlogp", n, dev),
-                                    _f32(weight, "weight", n, dev), _f32(ratio, "ratio", n, dev), _f32(stats, "stats", TOKEN_STATS, dev),
-                                    _space(workspace, dev), workspace.nbytes, _i32(status, "status", None, dev), _stream(stream)),
-           "pg_token_objective")
+                                    None if weight is None else _f32(weight, "weight", n, dev), None if ratio is None else _f32(ratio, "ratio", n, dev),
+                                    None if stats is None else _f32(stats, "stats", TOKEN_STATS, dev), _space(workspace, dev), workspace.nbytes,
+                                    None if status is None else _i32(status, "status", None, dev), _stream(stream)), "pg_token_objective")
 
 
 def strerror(code: int) -> str:

@@ -38,7 +38,13 @@ constexpr int kTokCtas = NB;                    // of an SM
 #endif
 constexpr int kPartBytes = PB;
 #ifndef MT
-#define MT 4
+#define MT 2
+#endif
+#ifndef SPT
+#define SPT 256
+#endif
+#ifndef SPN
+#define SPN 256
 #endif
 #ifndef OC
 #define OC 2
@@ -1083,7 +1089,8 @@ int launch_forward(TokenParams p, cudaStream_t st) {
   if (kGrad) parts = std::min((total * 16 + kPartBytes - 1) / kPartBytes, kMostParts);
   else if (kRest) parts = std::min((total + 16383) / 16384, kMostParts);
   // more, down to a unit a thread, while that leaves SMs without work
-  while (parts * 2 <= kMostParts && (int64_t)p.n_rows * parts < 2 * 148 && total / parts >= 2 * kTokThreads) parts *= 2;
+  const int least = p.t.n_top ? SPT : SPN;
+  while (parts * 2 <= kMostParts && (int64_t)p.n_rows * parts < 2 * 148 && total / parts >= 2 * least) parts *= 2;
   if (p.t.n_top) parts = std::max(parts, (total + kMostTiles * kTile - 1) / (kMostTiles * kTile));
   p.parts = parts;
   p.units = (total + parts - 1) / parts;

@@ -1,9 +1,10 @@
 // Clipped objective over ragged rows of tokens and its derivatives (pg_token_objective).
 //
-// Bound: latency for a few thousand tokens, HBM (three to five floats read and two or three written a token) beyond.  One launch: a CTA
-// takes a run of tokens, asks for all that a thread needs at once, brings the rows' starts into shared memory meanwhile, finds each token's row by bisection
-// and leaves its sums in a slot of the workspace; the CTA that draws the last ticket adds the slots in their order.  fp64 throughout:
-// differences of log-probs lie next to 0, where exp(d) - d - 1 has no digits left in 32 bits.
+// Bound: latency; one launch, a token a thread at a time: what the token needs is asked for first, while the warp finds the row of its first token by a search of `start` 32 ways at
+// a time, and its other lanes walk on from there.  A CTA leaves its sums in a slot of the workspace; the one that draws the last ticket
+// adds the slots in their order; up to 1024 tokens are one CTA's, which spares that.
+// fp64 throughout: differences of log-probs lie next to 0, where exp(d) - d - 1 has no digits left in 32 bits.  Results are rounded to 32
+// bits, so exponentials are Taylor polynomials good to 1e-11: exp(x) = 2^n exp(x - n ln 2), and below 0.35 exp(d) - d - 1 by its own series.
 #include "pg_kv.cuh"
 #include "pg_trace.cuh"
 
@@ -11,11 +12,9 @@
 
 namespace pg {
 
-constexpr int kObjectiveThreads = 256;
-constexpr int kObjectiveRun = 4;                            // tokens of a thread that are asked for together
-constexpr int kObjectiveChunk = kObjectiveThreads * kObjectiveRun;
-constexpr int kObjectiveMostCtas = 4096;
-constexpr int kObjectiveRows = 1024;                        // rows whose starts and advantages fit into shared memory
+constexpr int kObjectiveFew = 1024, kObjectiveThreads = 512;   // threads of a CTA, for few tokens and for many
+constexpr int kObjectiveMostCtas = 2 * 148;                 // two an SM: more in turn would wait for one another's joins (17 us, not 13)
+constexpr int kObjectiveWalk = 8;                           // rows that a lane walks before it searches
 constexpr int kSums = PG_TOKEN_STATS;                       // weighted surr, kl, entropy, distill; clipped tokens
 
 struct ObjectiveParams {
@@ -24,8 +23,39 @@ struct ObjectiveParams {
   double* slots;
   unsigned int* ticket;
   int32_t* status;
-  int n_rows, n_tokens, per_cta;                            // tokens of a CTA, a multiple of kObjectiveThreads
+  int n_rows, n_tokens, chunks;                             // runs of as many tokens as threads that a CTA takes
 };
+
+// (exp(r) - 1 - r) / r^2 for |r| <= 0.35, relative error below 1e-11.
+__device__ __forceinline__ double second_part(double r) {
+  double q = 1. / 39916800.;
+  q = fma(q, r, 1. / 3628800.);
+  q = fma(q, r, 1. / 362880.);
+  q = fma(q, r, 1. / 40320.);
+  q = fma(q, r, 1. / 5040.);
+  q = fma(q, r, 1. / 720.);
+  q = fma(q, r, 1. / 120.);
+  q = fma(q, r, 1. / 24.);
+  q = fma(q, r, 1. / 6.);
+  return fma(q, r, .5);
+}
+// exp(x), and exp(x) - x - 1 in *rest.  Outside +-87 both are 0 or infinite in 32 bits or near it, and so they are from +-700 on.
+__device__ __forceinline__ double exp_rest(double x, double* rest) {
+  const float f = (float)x;
+  const float n = rintf(fminf(fmaxf(f, -700.f), 700.f) * 1.44269504f);
+  const double r = fma((double)n, -0.693147180559945309417, x);         // off by n 2.3e-17
+  const double k = second_part(r) * r * r;
+  double y = (1. + (r + k)) * __hiloint2double((1023 + (int)n) << 20, 0);
+  if (fabsf(f) > 700.f) y = f > 0.f ? INFINITY : 0.;
+  if (rest) *rest = n == 0.f ? k : y - x - 1.;
+  return y;
+}
+// 1 / n for a whole number n >= 1.
+__device__ __forceinline__ double reciprocal(int n) {
+  double r = (double)__frcp_rn((float)n);
+  r = fma(r, fma(-(double)n, r, 1.), r);
+  return fma(r, fma(-(double)n, r, 1.), r);
+}
 
 __device__ __forceinline__ double sum_warp(double v) {
 #pragma unroll
@@ -34,97 +64,89 @@ __device__ __forceinline__ double sum_warp(double v) {
 }
 
 // Sums of every thread's `v`, the same in all threads of warp 0.
-__device__ __forceinline__ void sum_cta(double (&v)[kSums], double (&part)[kSums][kObjectiveThreads / 32]) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+__device__ __forceinline__ void sum_cta(double (&v)[kSums], double (&part)[kSums][kObjectiveFew / 32]) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
 #pragma unroll
-  for (int k = 0; k < kSums; ++k) {
-    v[k] = sum_warp(v[k]);
-    if (lane == 0) part[k][warp] = v[k];
-  }
+  for (int k = 0; k < kSums; ++k) v[k] = sum_warp(v[k]);
+  if (lane == 0)
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) part[k][warp] = v[k];
   __syncthreads();
   if (warp == 0) {
 #pragma unroll
-    for (int k = 0; k < kSums; ++k) v[k] = sum_warp(lane < kObjectiveThreads / 32 ? part[k][lane] : 0.);
+    for (int k = 0; k < kSums; ++k) v[k] = sum_warp(lane < warps ? part[k][lane] : 0.);
   }
 }
 
-__global__ void __launch_bounds__(kObjectiveThreads)
+__global__ void __launch_bounds__(kObjectiveFew)
 token_objective_kernel(const __grid_constant__ ObjectiveParams p) {
-  __shared__ double part[kSums][kObjectiveThreads / 32];
+  __shared__ double part[kSums][kObjectiveFew / 32];
   __shared__ bool is_last;
-  __shared__ int starts[kObjectiveRows + 1];
-  __shared__ float advs[kObjectiveRows];
   const pg_token_batch& b = p.b;
   const int* start = b.start;
-  const float* adv = b.adv;
-  auto bad = [&](int i) { return start[i] < 0 || start[i] > p.n_tokens || (i < p.n_rows && start[i] > start[i + 1]); };
-  for (int64_t i = (int64_t)blockIdx.x * kObjectiveThreads + threadIdx.x; i <= p.n_rows; i += (int64_t)gridDim.x * kObjectiveThreads)
-    if (bad((int)i)) flag(p.status, kStatusIndex);
+  const int lane = threadIdx.x & 31, threads = blockDim.x;
+  for (int64_t i = (int64_t)blockIdx.x * threads + threadIdx.x; i <= p.n_rows; i += (int64_t)gridDim.x * threads)
+    if (start[i] < 0 || start[i] > p.n_tokens || (i < p.n_rows && start[i] > start[i + 1])) flag(p.status, kStatusIndex);
   const int in_rows = start[p.n_rows] - start[0];
   const double lo = 1. - (double)b.clip_low, hi = 1. + (double)b.clip_high;
+  const double scale = b.norm == PG_NORM_ROWS ? (double)b.scale / p.n_rows : b.norm == PG_NORM_SUM ? (double)b.scale : in_rows > 0 ? (double)b.scale / in_rows : 0.;
   double sums[kSums] = {};
-  const int64_t first = (int64_t)blockIdx.x * p.per_cta, last = min(first + p.per_cta, (int64_t)p.n_tokens);
-  const bool shared = p.n_rows <= kObjectiveRows;
-  for (int64_t base = first + threadIdx.x; base - threadIdx.x < last; base += kObjectiveChunk) {
-    float fresh[kObjectiveRun], old[kObjectiveRun], ref[kObjectiveRun], ent[kObjectiveRun], div[kObjectiveRun];
-#pragma unroll
-    for (int e = 0; e < kObjectiveRun; ++e) {
-      const int64_t j = base + e * kObjectiveThreads;
-      const bool in = j < last;
-      fresh[e] = in ? b.logp_new[j] : 0.f;
-      old[e] = in && b.logp_old ? b.logp_old[j] : fresh[e];
-      ref[e] = in && b.logp_ref ? b.logp_ref[j] : fresh[e];
-      ent[e] = in && b.entropy ? b.entropy[j] : 0.f;
-      div[e] = in && b.distill ? b.distill[j] : 0.f;
+  for (int chunk = 0; chunk < p.chunks; ++chunk) {
+    const int64_t first = ((int64_t)blockIdx.x * p.chunks + chunk) * threads + (threadIdx.x & ~31);   // the warp's first token
+    if (first >= p.n_tokens) break;
+    const int j = (int)first + lane;
+    const bool in = first + lane < p.n_tokens;
+    const float fresh = in ? b.logp_new[j] : 0.f;
+    const float old = in && b.logp_old ? b.logp_old[j] : fresh, ref = in && b.logp_ref ? b.logp_ref[j] : fresh;
+    const float ent = in && b.entropy ? b.entropy[j] : 0.f, div = in && b.distill ? b.distill[j] : 0.f;
+    // how many rows end at the first token or before
+    int row = 0, most = p.n_rows;
+    while (row < most) {
+      const int step = (most - row + 31) / 32, at = row + (lane + 1) * step;
+      const int ended = __popc(__ballot_sync(~0u, at <= most && start[min(at, most)] <= (int)first));
+      most = min(row + (ended + 1) * step - 1, most);
+      row = min(row + ended * step, most);
     }
-    if (shared && base - threadIdx.x == first) {              // while they are on their way
-      for (int i = threadIdx.x; i <= p.n_rows; i += kObjectiveThreads) {
-        starts[i] = start[i];
-        if (i < p.n_rows) advs[i] = adv[i];
-      }
-      __syncthreads();
-      start = starts;
-      adv = advs;
-    }
-#pragma unroll
-    for (int e = 0; e < kObjectiveRun; ++e) {
-      const int64_t j64 = base + e * kObjectiveThreads;
-      if (j64 >= last) break;
-      const int j = (int)j64;
-      int l = 0, h = p.n_rows;                                // how many rows end at j or before
-      while (l < h) {
-        const int mid = l + (h - l) / 2;
-        if (start[mid + 1] <= j) l = mid + 1;
+    // a lane's token: the rows that end between them
+    for (int walked = 0; in && row < p.n_rows && start[row + 1] <= j; ++row) {
+      if (++walked < kObjectiveWalk) continue;
+      int h = p.n_rows;
+      while (row < h) {
+        const int mid = row + (h - row) / 2;
+        if (start[mid + 1] <= j) row = mid + 1;
         else h = mid;
       }
-      const int from = l < p.n_rows ? start[l] : 0, to = l < p.n_rows ? start[l + 1] : 0;
-      if (j < from || j >= to) {                              // a token of no row
-        p.dlogp[j] = 0.f;
-        if (p.weight) p.weight[j] = 0.f;
-        if (p.ratio) p.ratio[j] = 1.f;
-        continue;
-      }
-      double w = b.scale;
-      if (b.norm == PG_NORM_ROWS) w /= (double)(to - from) * p.n_rows;
-      if (b.norm == PG_NORM_TOKENS) w = in_rows > 0 ? w / in_rows : 0.;
-      const double a = adv[l];
-      const double r = b.logp_old ? exp((double)fresh[e] - (double)old[e]) : 1.;
-      const double free = r * a, held = (r < lo ? lo : r > hi ? hi : r) * a;
-      const bool clipped = held < free;
-      double g = clipped ? 0. : free;
-      sums[0] += w * (clipped ? held : free);
-      if (b.logp_ref) {
-        const double d = (double)ref[e] - (double)fresh[e], em = expm1(d);
-        sums[1] += w * (em - d);
-        g += (double)b.beta * em;
-      }
-      sums[2] += w * (double)ent[e];
-      sums[3] += w * (double)div[e];
-      sums[4] += clipped;
-      p.dlogp[j] = (float)(w * g);
-      if (p.weight) p.weight[j] = (float)w;
-      if (p.ratio) p.ratio[j] = (float)r;
+      break;
     }
+    if (!in) continue;
+    const int from = row < p.n_rows ? start[row] : 0, to = row < p.n_rows ? start[row + 1] : 0;
+    if (j < from || j >= to) {                                // a token of no row
+      p.dlogp[j] = 0.f;
+      if (p.weight) p.weight[j] = 0.f;
+      if (p.ratio) p.ratio[j] = 1.f;
+      continue;
+    }
+    const double a = b.adv[row];
+    double w = scale;
+    if (b.norm == PG_NORM_ROWS) w *= reciprocal(to - from);
+    const double r = b.logp_old ? exp_rest((double)fresh - (double)old, nullptr) : 1.;
+    const double free = r * a, held = (r < lo ? lo : r > hi ? hi : r) * a;
+    const bool clipped = held < free;
+    double g = clipped ? 0. : free;
+    sums[0] += w * (clipped ? held : free);
+    if (b.logp_ref) {
+      const double d = (double)ref - (double)fresh;
+      double kl;
+      exp_rest(d, &kl);
+      sums[1] += w * kl;
+      g += (double)b.beta * (kl + d);
+    }
+    sums[2] += w * (double)ent;
+    sums[3] += w * (double)div;
+    sums[4] += clipped;
+    p.dlogp[j] = (float)(w * g);
+    if (p.weight) p.weight[j] = (float)w;
+    if (p.ratio) p.ratio[j] = (float)r;
   }
   sum_cta(sums, part);
   if (gridDim.x > 1) {
@@ -139,7 +161,8 @@ token_objective_kernel(const __grid_constant__ ObjectiveParams p) {
     __threadfence();
 #pragma unroll
     for (int k = 0; k < kSums; ++k) sums[k] = 0.;
-    for (int i = threadIdx.x; i < (int)gridDim.x; i += kObjectiveThreads)
+#pragma unroll 2
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += threads)
 #pragma unroll
       for (int k = 0; k < kSums; ++k) sums[k] += __ldcg(p.slots + (int64_t)i * kSums + k);
     sum_cta(sums, part);
@@ -155,22 +178,22 @@ token_objective_kernel(const __grid_constant__ ObjectiveParams p) {
   }
 }
 
-// One CTA for what it takes in one go, which spares the join; else a token a thread while there are few, for latency, and
-// kObjectiveRun a thread and more from there on.
-static void objective_shape(int n_tokens, int* ctas, int* per_cta) {
-  int64_t per = n_tokens <= kObjectiveChunk ? kObjectiveChunk : kObjectiveThreads;
-  if (n_tokens > 148 * 2 * kObjectiveThreads) per = kObjectiveChunk;
-  const int64_t least = ((int64_t)n_tokens + kObjectiveMostCtas - 1) / kObjectiveMostCtas;
-  if (per < least) per = (least + kObjectiveChunk - 1) / kObjectiveChunk * kObjectiveChunk;
-  *per_cta = (int)per;
-  *ctas = (int)std::max<int64_t>(((int64_t)n_tokens + per - 1) / per, 1);
+static void objective_shape(int n_tokens, int* threads, int* chunks, int* ctas) {
+  *threads = n_tokens <= kObjectiveFew ? kObjectiveFew : kObjectiveThreads;
+  const int64_t runs = ((int64_t)n_tokens + *threads - 1) / *threads;
+  *chunks = (int)std::max<int64_t>((runs + kObjectiveMostCtas - 1) / kObjectiveMostCtas, 1);
+  *ctas = (int)std::max<int64_t>((runs + *chunks - 1) / *chunks, 1);
 }
 
 }  // namespace pg
 
 extern "C" size_t pg_token_objective_workspace_bytes(int32_t n_tokens) {
   if (n_tokens < 0) return 0;
-  return pg::kCounterBytes + (size_t)std::min<int64_t>((int64_t)n_tokens / pg::kObjectiveThreads + 1, pg::kObjectiveMostCtas) * pg::kSums * sizeof(double);
+  int threads, chunks, ctas;
+  pg::objective_shape(n_tokens, &threads, &chunks, &ctas);
+  // never less than a shorter batch needs: the slots of as many CTAs as any has
+  ctas = (int)std::min<int64_t>((int64_t)n_tokens / pg::kObjectiveThreads + 1, pg::kObjectiveMostCtas);
+  return pg::kCounterBytes + (size_t)ctas * pg::kSums * sizeof(double);
 }
 
 extern "C" int pg_token_objective(int32_t n_rows, int32_t n_tokens, const pg_token_batch* batch, float* objective, float* dlogp,
@@ -195,9 +218,9 @@ extern "C" int pg_token_objective(int32_t n_rows, int32_t n_tokens, const pg_tok
   p.status = status;
   p.n_rows = n_rows;
   p.n_tokens = n_tokens;
-  int ctas;
-  pg::objective_shape(n_tokens, &ctas, &p.per_cta);
-  pg::token_objective_kernel<<<ctas, pg::kObjectiveThreads, 0, (cudaStream_t)stream>>>(p);
+  int threads, ctas;
+  pg::objective_shape(n_tokens, &threads, &p.chunks, &ctas);
+  pg::token_objective_kernel<<<ctas, threads, 0, (cudaStream_t)stream>>>(p);
   PG_LAUNCH_CHECK();
   return PG_OK;
 }
