@@ -40,12 +40,6 @@ constexpr int kPartBytes = PB;
 #ifndef MT
 #define MT 2
 #endif
-#ifndef SPT
-#define SPT 256
-#endif
-#ifndef SPN
-#define SPN 256
-#endif
 #ifndef OC
 #define OC 2
 #endif
@@ -694,11 +688,11 @@ __device__ __forceinline__ void load_tile(const RowPart<T>& at, int tile, uint64
   }
 }
 
-// The gradient of a tile in registers; dl: of the row's first unit, its units on 16 bytes.  kAsk: as a unit is done with, the next tile's
-// is asked for (from); that tile is whole.
+// The gradient of a tile in registers; dl: of the row's first unit, its units on 16 bytes.  kAsk: as a unit is done
+// with, the next tile's is asked for (from); that tile is whole.
 template <typename T, bool kEnt, bool kAsk>
 __device__ __forceinline__ void slope_tile(const RowPart<T>& at, int tile, uint4 (&raw)[kTokUnits], const Slope2& k, T* dl, const T* from,
-                                           uint64_t policy) {
+                                            uint64_t policy) {
   const int left = at.last - at.first - tile * kTileUnits - (int)threadIdx.x;   // units from the thread's first on
   T* to = dl + (int64_t)(at.first + tile * kTileUnits + (int)threadIdx.x) * kPer<T>;
 #pragma unroll
@@ -737,7 +731,6 @@ __device__ __forceinline__ void sum_tile(uint4 (&raw)[kTokUnits], float c, float
   split2(add2(a1, b1), u, v);
   t1 = u + v;
 }
-
 // Forward, with the gradient on top (kGrad).
 template <typename T, bool kGrad, bool kEnt, bool kRest>
 __global__ void __launch_bounds__(kTokThreads, kTokCtas)
@@ -812,7 +805,8 @@ token_kernel(const __grid_constant__ TokenParams p) {
       const uint2 b = reinterpret_cast<const uint2*>(bits)[tile * kTokThreads + tid];
       if (b.x | b.y) {
 #pragma unroll
-        for (int j = 0; j < kUnits; ++j) set_empty<T>(raw[j], (j < 4 ? b.x : b.y) >> (j % 4 * 8) & 255u);
+        for (int j = 0; j < kUnits; ++j)
+          if (const uint32_t l = (j < 4 ? b.x : b.y) >> (j % 4 * 8) & 255u) set_empty<T>(raw[j], l);
       }
     }
   };
@@ -1088,9 +1082,10 @@ int launch_forward(TokenParams p, cudaStream_t st) {
   // Rows that are read twice: parts of 128 KB, so that what all SMs work on stays in the L2 cache.  With a bucket: bits of 16 KB at most.
   if (kGrad) parts = std::min((total * 16 + kPartBytes - 1) / kPartBytes, kMostParts);
   else if (kRest) parts = std::min((total + 16383) / 16384, kMostParts);
-  // more, down to a unit a thread, while that leaves SMs without work
-  const int least = p.t.n_top ? SPT : SPN;
-  while (parts * 2 <= kMostParts && (int64_t)p.n_rows * parts < 2 * 148 && total / parts >= 2 * least) parts *= 2;
+  // More while SMs are without work: down to a unit a thread, but whole tiles where lists of alternatives have to be made and joined
+  // (12 x 50001 with 100 of them 13 us in parts of a tile, 25 us in eight).
+  const int busy = p.t.n_top ? 148 : 2 * 148, least = p.t.n_top ? kTile : kTokThreads;
+  while (parts * 2 <= kMostParts && (int64_t)p.n_rows * parts * (p.t.n_top ? 2 : 1) <= busy && total / parts >= 2 * least) parts *= 2;
   if (p.t.n_top) parts = std::max(parts, (total + kMostTiles * kTile - 1) / (kMostTiles * kTile));
   p.parts = parts;
   p.units = (total + parts - 1) / parts;
