@@ -762,36 +762,42 @@ token_kernel(const __grid_constant__ TokenParams p) {
   const float dh = kGrad && p.g.dentropy ? p.g.dentropy[row] * p.g.entropy_scale : 0.f;
   const float dd = kGrad && p.g.ddistill ? p.g.ddistill[row] * p.g.distill_scale : 0.f;
   const float edge_x = tid < at.edges ? to_float(at.in[at.edge(tid)]) : -INFINITY;
+  // Given and listed tokens, one a thread.  What depends on these loads - the tokens' logits, what others see of them - comes after the first
+  // tile, so that the warps that have them do not wait for two of them in turn before the stream.
+  const int given = tid < n_ids ? p.t.ids[(int64_t)row * n_ids + tid] : -1;
+  const float given_dl = kGrad && tid < n_ids && p.g.dlogp ? p.g.dlogp[(int64_t)row * n_ids + tid] : 0.f;
+  const int listed = tid < n_list ? p.t.teacher_ids[(int64_t)row * n_list + tid] : -1;
+  const float listed_tl = tid < n_list ? p.t.teacher_logp[(int64_t)row * n_list + tid] : 0.f;
   Entry my = {-1, -1, 0.f, -INFINITY, 0.f, 0.f};
-  if (tid < n_ids) {
-    const int id = p.t.ids[(int64_t)row * n_ids + tid];
-    if ((unsigned int)id < (unsigned int)p.vocab) {
-      my.id = id;
-      my.x = to_float(at.in[id]);
-      if (kGrad && p.g.dlogp) my.dl = p.g.dlogp[(int64_t)row * n_ids + tid];
+  T given_x = from_float<T>(0.f), listed_x = given_x;
+  auto meet = [&] {
+    if ((unsigned int)given < (unsigned int)p.vocab) {
+      my.id = given;
+      my.dl = given_dl;
+      given_x = at.in[given];
     }
-    s.gid[tid] = my.id;
-    s.gdl[tid] = my.dl;
-  }
-  if (tid < n_list) {
-    const int id = p.t.teacher_ids[(int64_t)row * n_list + tid];
-    my.tl = p.t.teacher_logp[(int64_t)row * n_list + tid];
-    if ((unsigned int)id < (unsigned int)p.vocab && !(my.tl == -INFINITY)) {
-      my.tid = id;
-      my.tx = to_float(at.in[id]);
+    my.tl = listed_tl;
+    if ((unsigned int)listed < (unsigned int)p.vocab && !(listed_tl == -INFINITY)) {
+      my.tid = listed;
+      listed_x = at.in[listed];
     }
-  }
-  if (tid < (n_list + 3 & ~3)) s.tid[tid] = my.tid;
-  if (kGrad && warp < (n_ids + 31) / 32) {
-    const float d = warp_total(my.dl);
-    if (lane == 0) s.dsum[warp] = d;
-  }
+    if (tid < n_ids) {
+      s.gid[tid] = my.id;
+      s.gdl[tid] = my.dl;
+    }
+    if (tid < (n_list + 3 & ~3)) s.tid[tid] = my.tid;
+    if (kGrad && warp < (n_ids + 31) / 32) {
+      const float d = warp_total(my.dl);
+      if (lane == 0) s.dsum[warp] = d;
+    }
+  };
+  if (kGrad) meet();                                                // registers are scarce here: not through the first tile
   if constexpr (kRest) {
     __syncthreads();                                                // the bits are zero
-    if (my.tid >= 0 && at.owns(my.tid)) {
-      const int t = my.tid - at.head;
+    if ((unsigned int)listed < (unsigned int)p.vocab && !(listed_tl == -INFINITY) && at.owns(listed)) {
+      const int t = listed - at.head;
       if (t < 0 || t >= at.units * kPer<T>) {
-        atomicOr(&s.edges, 1u << (t < 0 ? my.tid : my.tid - at.units * kPer<T>));
+        atomicOr(&s.edges, 1u << (t < 0 ? listed : listed - at.units * kPer<T>));
       } else {
         const int b = bits_at(t / kPer<T> - at.first);
         atomicOr(reinterpret_cast<uint32_t*>(bits) + (b >> 2), 1u << ((b & 3) * 8 + t % kPer<T>));
@@ -836,7 +842,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
       refer(m, fmaxf(m, tm), c, s0, s1);
       m = fmaxf(m, tm);
       bool asked = false;
-      if (m < -kHuge && m > -INFINITY) {
+      if (fabsf(m) > kHuge && fabsf(m) < INFINITY) {
         sum_huge(at, bits, m, c, tile, s0, s1);
       } else {
         // y = l c - r in one rounding; what r = m c rounded is off by is taken back from the sums
@@ -853,6 +859,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
         if (kEnt) s1 += f * fmaf(-off, t0, t1);
       }
       if (n_top) top.most[tile * kTokThreads + tid] = tm;
+      if (!kGrad && tile == p.tiles - 1) meet();
       if (tile > 0 && !asked) load_tile(at, tile - 1, kGrad && tile > kOnChip ? read_again : last_read, raw);
     }
     if (at.edges > 0) {
@@ -864,8 +871,10 @@ token_kernel(const __grid_constant__ TokenParams p) {
       s1 += e * fmaxf(y, kFloorY);
       edge_left = x;
     }
-      if (n_list > 0 && !kRest) __syncthreads();                      // the list's ids are there
+    if (n_list > 0) __syncthreads();                                // the list's ids are there
+    my.x = to_float(given_x);
     if (warp < lists) {
+      if (my.tid >= 0) my.tx = to_float(listed_x);
       if (my.tid >= 0 && again_later(s, my.tid, n_list)) my.tid = -1;
       const bool used = my.tid >= 0;
       const float x = used ? my.tx : -INFINITY;
@@ -976,7 +985,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
       const Slope2 k(slope, c);
       T* dl = (T*)p.dl + row * p.dl_stride;
       const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0;
-      if (slope.ref < -kHuge || !aligned) {                         // rows masked throughout, by the type's lowest value; or off 16 bytes
+      if (fabsf(slope.ref) > kHuge || !aligned) {                       // rows masked throughout, by the type's lowest value; or off 16 bytes
         slope_huge(at, dl, slope, c);
       } else {
         for (int tile = 0; tile < p.tiles; ++tile) {
@@ -1057,7 +1066,7 @@ token_backward_kernel(const __grid_constant__ TokenParams p) {
   if (quiet) slope.a = slope.b = 0.f;
   const Slope2 k(slope, c);
   T* dl = (T*)p.dl + row * p.dl_stride;
-  const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0, huge = !aligned || (slope.ref < -kHuge && !quiet);
+  const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0, huge = !aligned || (fabsf(slope.ref) > kHuge && !quiet);
   if (huge) {
     slope_huge(at, dl, slope, c, quiet);
   } else {
