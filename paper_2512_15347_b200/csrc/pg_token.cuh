@@ -48,6 +48,7 @@ constexpr int kTokWarps = kTokThreads / 32;
 constexpr int kMostParts = 8;                   // CTAs of a cluster
 constexpr int kCandidates = 1024;
 constexpr int kMostTiles = 16;                  // of a part with alternatives
+constexpr int kMostUnits = 2048;                // of a part that are read again for them
 constexpr int kMergeBytes = kMostParts * PG_TOKEN_MAX_TOP * 8;
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr float kFloorY = -1e4f;                // 2^y = 0 long before; keeps 0 * y from being NaN
@@ -413,9 +414,9 @@ struct TopShared {
   float bounds[kTokWarps];
   unsigned int hist[256];
   unsigned long long prefix;
-  int count, groups, left, shift;
-  uint16_t group[kMostTiles * kTokThreads];                         // threads' tiles that may hold alternatives: tile * kTokThreads + thread
-  float most[kMostTiles * kTokThreads];                             // the largest logit of each; as many as there are tiles
+  int count, units, left, shift;
+  uint16_t unit[kMostUnits];                                        // of the part, that may hold alternatives
+  uint4 most[kMostTiles * kTokThreads];                             // the largest logit of each unit of a thread's tile; as many as there are tiles
 
   __device__ __forceinline__ void push(float x, int id) {
     const int at = atomicAdd(&count, 1);
@@ -423,41 +424,55 @@ struct TopShared {
   }
 };
 
-__host__ __device__ constexpr int top_bytes(int tiles) { return (int)sizeof(TopShared) - (kMostTiles - tiles) * kTokThreads * 4; }
+__host__ __device__ constexpr int top_bytes(int tiles) { return (int)sizeof(TopShared) - (kMostTiles - tiles) * kTokThreads * 16; }
 
+// The largest logit of a unit in 16 bits, not below it: as it is, or of four fp32 ones rounded up to bf16.
+template <typename T>
+__device__ __forceinline__ uint32_t unit_most(uint32_t w) {
+  if constexpr (sizeof(T) == 4) return (w >> 31 ? w : w + 0xFFFFu) >> 16;
+  else return max2(w, w >> 16 | w << 16, T()) & 0xFFFFu;
+}
+template <typename T>
+__device__ __forceinline__ float most_value(uint32_t h) {
+  if constexpr (std::is_same<T, __half>::value) return __half2float(__ushort_as_half((unsigned short)h));
+  else return __uint_as_float(h << 16);
+}
 // The n largest keys of the part into `best`, in order; by all threads.  `most` is filled, m a thread's largest logit, edge_x and list_x
-// what it has outside the tiles (-inf: nothing).
+// what it has outside the units (-inf: nothing).
 // Every warp has as many threads with a logit at or above its own bound, the n / warps-th largest of its threads' largest, that all of
-// them make n; so the n-th largest logit is not below the least of these bounds, and few of the threads' tiles reach it.
+// them make n; so the n-th largest logit is not below the least of these bounds, and few units reach it.  They are read again.
 template <typename T>
 __device__ __noinline__ void select_top(TopShared& s, const RowPart<T>& at, int n, int tiles, float m, float edge_x, float list_x, int list_id,
                                         const uint8_t* bits) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const float own = nth_largest(m, (n + kTokWarps - 1) / kTokWarps);
   if (lane == 0) s.bounds[warp] = own;
-  if (tid == 0) s.count = s.groups = 0;
+  if (tid == 0) s.count = s.units = 0;
   __syncthreads();
   float bound = s.bounds[0];
 #pragma unroll
   for (int i = 1; i < kTokWarps; ++i) bound = fminf(bound, s.bounds[i]);
-  for (int tile = 0; tile < tiles; ++tile) {
-    const bool has = s.most[tile * kTokThreads + tid] >= bound && s.most[tile * kTokThreads + tid] > -INFINITY;
-    const unsigned int those = __ballot_sync(~0u, has);
-    if (!those) continue;
-    int first = 0;
-    if (lane == 0) first = atomicAdd(&s.groups, __popc(those));
-    first = __shfl_sync(~0u, first, 0);
-    if (has) s.group[first + __popc(those & ((1u << lane) - 1))] = (uint16_t)(tile * kTokThreads + tid);
+  if (m >= bound) {
+    for (int tile = 0; tile < tiles; ++tile) {
+      const uint4 v = s.most[tile * kTokThreads + tid];
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int j = 0; j < kTokUnits; ++j) {
+        const float x = most_value<T>(w[j / 2] >> (j % 2 * 16) & 0xFFFFu);
+        if (x >= bound && x > -INFINITY) {
+          const int to = atomicAdd(&s.units, 1);
+          if (to < kMostUnits) s.unit[to] = (uint16_t)(tile * kTileUnits + j * kTokThreads + tid);
+        }
+      }
+    }
   }
   for (int i = tid; i < n; i += kTokThreads) s.best[i] = 0;
   if (edge_x >= bound && edge_x > -INFINITY) s.push(edge_x, at.edge(tid));
   if (list_x >= bound && list_x > -INFINITY) s.push(list_x, list_id);
   __syncthreads();
-  const int work = s.groups * kTokUnits;
-  for (int i = tid; i < work; i += kTokThreads) {
-    const int g = s.group[i / kTokUnits], j = i % kTokUnits;
-    const int u = g / kTokThreads * kTileUnits + j * kTokThreads + g % kTokThreads;
-    if (at.first + u >= at.last) continue;
+  const int work = s.units;
+  for (int i = tid; i < work && work <= kMostUnits; i += kTokThreads) {
+    const int u = s.unit[i];
     const int t0 = at.head + (at.first + u) * kPer<T>;
     const uint4 unit = *(const uint4*)(at.in + t0);
     const uint32_t listed = bits ? bits[bits_at(u)] : 0u;
@@ -470,7 +485,7 @@ __device__ __noinline__ void select_top(TopShared& s, const RowPart<T>& at, int 
     }
   }
   __syncthreads();
-  int total = s.count;
+  int total = work > kMostUnits ? kCandidates + 1 : s.count;
   __syncthreads();
   if (total > kCandidates) {
     // Many equal logits: the n-th largest key of the part, eight bits at a time, until few enough reach it.
@@ -519,6 +534,7 @@ __device__ __noinline__ void select_top(TopShared& s, const RowPart<T>& at, int 
   for (int i = tid; i < total; i += kTokThreads) {
     const unsigned long long key = s.cand[i];
     int rank = 0, j = 0;
+#pragma unroll 8
     for (; j + 1 < total; j += 2) {
       const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&s.cand[j]);
       rank += (o.x > key) + (o.y > key);
@@ -756,7 +772,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
   }
   uint4* const kept = reinterpret_cast<uint4*>(more) + tid;         // a thread's own places: its units of tile 1, those of tile 0 stay in registers
   uint4 raw[kUnits];
-  const uint64_t last_read = keep_policy(false), read_again = keep_policy(true);
+  const uint64_t last_read = keep_policy(!kGrad && n_top > 0), read_again = keep_policy(true);
   load_tile(at, p.tiles - 1, kGrad && p.tiles > kOnChip ? read_again : last_read, raw);                       // the part's cut tile first: the last two, that stay here, are whole
   const float inv = p.t.temperature ? 1.f / p.t.temperature[row] : 1.f, c = inv * kLog2e;
   const float dh = kGrad && p.g.dentropy ? p.g.dentropy[row] * p.g.entropy_scale : 0.f;
@@ -836,8 +852,19 @@ token_kernel(const __grid_constant__ TokenParams p) {
         for (int j = 0; j < kUnits; ++j) kept[j * kTokThreads] = raw[j];
       }
       uint32_t w = Empty8<T>::word;
+      if (n_top) {
+        uint32_t most[kUnits];
 #pragma unroll
-      for (int j = 0; j < kUnits; ++j) w = max_unit<T>(w, raw[j]);
+        for (int j = 0; j < kUnits; ++j) {
+          const uint32_t v = max_unit<T>(Empty8<T>::word, raw[j]);
+          w = max2(w, v, T());
+          most[j] = unit_most<T>(v);
+        }
+        top.most[tile * kTokThreads + tid] = make_uint4(most[0] | most[1] << 16, most[2] | most[3] << 16, most[4] | most[5] << 16, most[6] | most[7] << 16);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kUnits; ++j) w = max_unit<T>(w, raw[j]);
+      }
       const float tm = max_of<T>(w);
       refer(m, fmaxf(m, tm), c, s0, s1);
       m = fmaxf(m, tm);
@@ -858,7 +885,6 @@ token_kernel(const __grid_constant__ TokenParams p) {
         s0 += f * t0;
         if (kEnt) s1 += f * fmaf(-off, t0, t1);
       }
-      if (n_top) top.most[tile * kTokThreads + tid] = tm;
       if (!kGrad && tile == p.tiles - 1) meet();
       if (tile > 0 && !asked) load_tile(at, tile - 1, kGrad && tile > kOnChip ? read_again : last_read, raw);
     }
