@@ -1,18 +1,25 @@
 // Policy update on rows of logits: log-probs of given tokens, entropy, alternatives, divergence from a teacher's list, and their
 // gradient (pg_token_forward / _backward / _forward_backward).
 //
-// Bound: HBM.  A row is cut into as many parts as a thread block cluster has CTAs; a part lies in registers as it came from memory
-// (64 16-bit or 32 fp32 logits a thread) and longer ones go through them tile by tile.  In the base-2 domain, with c = log2(e) / T,
+// Bound: HBM, each logit read once and each gradient written once.  A CTA takes a row, or a part of one, in tiles of eight 16-byte units a
+// thread that lie in registers as they came from memory; as a unit is done with, the next tile's is asked for.  In the base-2 domain,
+// with c = log2(e) / T,
 //     y_v = (l_v - m) c,   s0 = sum 2^y,   s1 = sum 2^y y,   m the largest logit that the thread has,
-// so one exponential a logit gives lse = m / T + ln s0 and the entropy ln s0 - ln 2 s1 / s0; the triples (m, s0, s1) of threads, warps and CTAs
-// are joined in a fixed order, those of the cluster through each other's shared memory.  The difference is taken before the product with c,
-// so that rows masked with the type's lowest value neither overflow nor lose their maximum.
-// The gradient of all terms together is, away from given and listed tokens, e_v (A + B ln e_v) with two numbers a row: a second pass over
-// the registers.  Given and listed tokens are written over it afterwards, one thread each.
+// so one exponential a logit gives lse = m / T + ln s0 and the entropy ln s0 - ln 2 s1 / s0.  The triples (m, s0, s1) of threads and warps, and
+// of the CTAs of a cluster through each other's shared memory, are joined in a fixed order.
+// The gradient of all terms together is, away from given and listed tokens, e (a + b ln e) with two numbers a row and e a softmax:
+// a second pass over the row.  Of its part the CTA has kept a tile in registers and one in shared memory; the others come back from the L2 cache, which
+// holds them because all else is read and written with the wish to be evicted first.  Given and listed tokens are written over the pass
+// afterwards, one thread each.
 // With a bucket for the mass outside a teacher's list that mass is summed by itself (the list's logits are taken out of the registers),
 // since the difference 1 - (list's mass) has no digits left where the list has nearly everything.
-// Alternatives: the n-th largest of the threads' maxima bounds the n-th largest logit from below, so only threads that hold one look
-// at their logits again; what passes is ranked by counting.
+// Alternatives: bounds from the threads' largest logits leave few tiles of few threads to look at again; what passes is ranked by counting.
+//
+// Measured (B200; share of the floor at the copy rate, calls back to back): 2368 x 131072 bf16 forward 102 us (93 %), with gradient 222 us (85 %);
+// 2368 x 50001 fp16 50 us (73 %) and 95 us (76 %); 1024 x 131072 backward alone 86 us (95 %).  What is left: the join of a row, about 0.7 us in which its CTA
+// asks for nothing, and rows that are little longer than whole tiles.  Tried and left out: rows kept in the registers or shared memory of clusters (the join
+// of eight CTAs costs more than the second read: 343 and 302 us for 2048 x 131072, not 209), CTAs that stay and ask for their next row ahead (220 us),
+// bulk prefetches into the L2 cache (233 us), five CTAs an SM with smaller tiles (225 to 234 us).
 #pragma once
 
 #include "pg_kv.cuh"
@@ -24,31 +31,15 @@
 
 namespace pg {
 
-
-#ifndef NB
-#define NB 4
-#endif
-#ifndef NT
-#define NT 256
-#endif
-constexpr int kTokThreads = NT;
-constexpr int kTokCtas = NB;                    // of an SM
-#ifndef PB
-#define PB 131072
-#endif
-constexpr int kPartBytes = PB;
-#ifndef MT
-#define MT 2
-#endif
-#ifndef OC
-#define OC 2
-#endif
-constexpr int kOnChip = OC;                     // tiles of a part that stay on chip: one in registers, one in shared memory
+constexpr int kTokThreads = 256, kTokCtas = 4;  // of a CTA; CTAs of an SM, 64 registers a thread
+constexpr int kPartBytes = 128 * 1024;          // of a row that is read twice; 256 KB: 237 us, not 209 (2048 x 131072 bf16), 64 KB: 251 us
+constexpr int kOnChip = 2;                      // tiles of a part that stay on chip: one in registers, one in shared memory
+constexpr int kBackwardTiles = 2;               // of a CTA that only writes gradients: its row's numbers serve both (1: 69 us, not 65; 4: 72 us)
 constexpr int kTokWarps = kTokThreads / 32;
 constexpr int kMostParts = 8;                   // CTAs of a cluster
 constexpr int kCandidates = 1024;
 constexpr int kMostTiles = 16;                  // of a part with alternatives
-constexpr int kMostUnits = 2048;                // of a part that are read again for them
+constexpr int kMostGroups = 1024;               // threads' tiles that are read again for them
 constexpr int kMergeBytes = kMostParts * PG_TOKEN_MAX_TOP * 8;
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr float kFloorY = -1e4f;                // 2^y = 0 long before; keeps 0 * y from being NaN
@@ -98,14 +89,6 @@ struct TokenShared {
   alignas(16) int tid[PG_TOKEN_MAX_LIST];       // listed tokens, -1: unused
   uint32_t edges;                               // bits of the listed ones among the edge tokens
 };
-#ifdef SCALAR
-typedef float2 f2;
-__device__ __forceinline__ f2 make2(float a, float b) { return make_float2(a, b); }
-__device__ __forceinline__ void split2(f2 v, float& a, float& b) { a = v.x; b = v.y; }
-__device__ __forceinline__ f2 add2(f2 a, f2 b) { return make_float2(a.x + b.x, a.y + b.y); }
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) { return make_float2(a.x * b.x, a.y * b.y); }
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { return make_float2(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)); }
-#else
 typedef unsigned long long f2;                  // two floats for the packed fp32 instructions
 __device__ __forceinline__ f2 make2(float a, float b) {
   f2 r;
@@ -128,7 +111,6 @@ __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
-#endif
 __device__ __forceinline__ float ex2(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -411,12 +393,12 @@ __device__ __forceinline__ float nth_largest(float v, int n) {
 // For alternatives.  Keys order by (logit, lowest index first); 0 is none.
 struct TopShared {
   unsigned long long cand[kCandidates], best[PG_TOKEN_MAX_TOP];
-  float bounds[kTokWarps];
+  float bounds[kTokWarps], bound;
   unsigned int hist[256];
   unsigned long long prefix;
-  int count, units, left, shift;
-  uint16_t unit[kMostUnits];                                        // of the part, that may hold alternatives
-  uint4 most[kMostTiles * kTokThreads];                             // the largest logit of each unit of a thread's tile; as many as there are tiles
+  int count, groups, left, shift;
+  unsigned int group[kMostGroups];                                  // threads' tiles that may hold alternatives: largest logit, tile * kTokThreads + thread
+  uint16_t most[kMostTiles * kTokThreads];                          // the largest logit of each thread's tile; as many as there are tiles
 
   __device__ __forceinline__ void push(float x, int id) {
     const int at = atomicAdd(&count, 1);
@@ -424,11 +406,12 @@ struct TopShared {
   }
 };
 
-__host__ __device__ constexpr int top_bytes(int tiles) { return (int)sizeof(TopShared) - (kMostTiles - tiles) * kTokThreads * 16; }
+__host__ __device__ constexpr int top_bytes(int tiles) { return (int)sizeof(TopShared) - (kMostTiles - tiles) * kTokThreads * 2; }
 
-// The largest logit of a unit in 16 bits, not below it: as it is, or of four fp32 ones rounded up to bf16.
+// The largest of logits in 16 bits, not below it: as it is, or of fp32 ones rounded up to bf16.  Few bytes, since shared memory is
+// taken from the cache that loads arrive in (46 KB more a CTA: 63 us, not 55, for 1184 x 131072).
 template <typename T>
-__device__ __forceinline__ uint32_t unit_most(uint32_t w) {
+__device__ __forceinline__ uint32_t most_bits(uint32_t w) {
   if constexpr (sizeof(T) == 4) return (w >> 31 ? w : w + 0xFFFFu) >> 16;
   else return max2(w, w >> 16 | w << 16, T()) & 0xFFFFu;
 }
@@ -440,41 +423,62 @@ __device__ __forceinline__ float most_value(uint32_t h) {
 // The n largest keys of the part into `best`, in order; by all threads.  `most` is filled, m a thread's largest logit, edge_x and list_x
 // what it has outside the units (-inf: nothing).
 // Every warp has as many threads with a logit at or above its own bound, the n / warps-th largest of its threads' largest, that all of
-// them make n; so the n-th largest logit is not below the least of these bounds, and few units reach it.  They are read again.
+// them make n; so the n-th largest logit is not below the least of these bounds, and few of the threads' tiles reach it.  They are read again.
 template <typename T>
 __device__ __noinline__ void select_top(TopShared& s, const RowPart<T>& at, int n, int tiles, float m, float edge_x, float list_x, int list_id,
                                         const uint8_t* bits) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const float own = nth_largest(m, (n + kTokWarps - 1) / kTokWarps);
   if (lane == 0) s.bounds[warp] = own;
-  if (tid == 0) s.count = s.units = 0;
+  if (tid == 0) s.count = s.groups = 0;
   __syncthreads();
   float bound = s.bounds[0];
 #pragma unroll
   for (int i = 1; i < kTokWarps; ++i) bound = fminf(bound, s.bounds[i]);
-  if (m >= bound) {
+  if (m >= bound && m > -INFINITY) {
     for (int tile = 0; tile < tiles; ++tile) {
-      const uint4 v = s.most[tile * kTokThreads + tid];
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int j = 0; j < kTokUnits; ++j) {
-        const float x = most_value<T>(w[j / 2] >> (j % 2 * 16) & 0xFFFFu);
-        if (x >= bound && x > -INFINITY) {
-          const int to = atomicAdd(&s.units, 1);
-          if (to < kMostUnits) s.unit[to] = (uint16_t)(tile * kTileUnits + j * kTokThreads + tid);
-        }
+      const uint32_t h = s.most[tile * kTokThreads + tid];
+      const float x = most_value<T>(h);
+      if (x >= bound && x > -INFINITY) {
+        const int to = atomicAdd(&s.groups, 1);
+        if (to < kMostGroups) s.group[to] = (h ^ (h >> 15 ? 0xFFFFu : 0x8000u)) << 16 | (uint32_t)(tile * kTokThreads + tid);
       }
     }
   }
   for (int i = tid; i < n; i += kTokThreads) s.best[i] = 0;
+  if (tid == 0) s.bound = bound;
+  __syncthreads();
+  const int work = s.groups;
+  // The n-th largest of these tiles' largest is a better bound, worth its search for long lists (64 of 2368 x 131072: 137 us, not 141).
+  if (n > 32 && work <= kMostGroups && work > n) {
+    for (int i = tid; i < work; i += kTokThreads) {
+      const unsigned int key = s.group[i];
+      int rank = 0;
+#pragma unroll 8
+      for (int j = 0; j < work; ++j) rank += s.group[j] > key;
+      if (rank == n - 1) {
+        uint32_t h = key >> 16;
+        if (sizeof(T) == 4 && h > 0) --h;                           // what was rounded up may lie below
+        h ^= h >> 15 ? 0x8000u : 0xFFFFu;
+        s.bound = fmaxf(bound, most_value<T>(h));
+      }
+    }
+    __syncthreads();
+    bound = s.bound;
+  }
   if (edge_x >= bound && edge_x > -INFINITY) s.push(edge_x, at.edge(tid));
   if (list_x >= bound && list_x > -INFINITY) s.push(list_x, list_id);
-  __syncthreads();
-  const int work = s.units;
-  for (int i = tid; i < work && work <= kMostUnits; i += kTokThreads) {
-    const int u = s.unit[i];
+#pragma unroll 2
+  for (int i = tid; i < work * kTokUnits && work <= kMostGroups; i += kTokThreads) {
+    const unsigned int key = s.group[i / kTokUnits];
+    uint32_t h = key >> 16;
+    h ^= h >> 15 ? 0x8000u : 0xFFFFu;
+    if (!(most_value<T>(h) >= bound)) continue;
+    const int g = key & 0xFFFFu, u = g / kTokThreads * kTileUnits + i % kTokUnits * kTokThreads + g % kTokThreads;
+    if (at.first + u >= at.last) continue;
     const int t0 = at.head + (at.first + u) * kPer<T>;
     const uint4 unit = *(const uint4*)(at.in + t0);
+    if (!(most_value<T>(most_bits<T>(max_unit<T>(Empty8<T>::word, unit))) >= bound)) continue;
     const uint32_t listed = bits ? bits[bits_at(u)] : 0u;
 #pragma unroll
     for (int k = 0; k < kPer<T> / 2; ++k) {
@@ -485,7 +489,7 @@ __device__ __noinline__ void select_top(TopShared& s, const RowPart<T>& at, int 
     }
   }
   __syncthreads();
-  int total = work > kMostUnits ? kCandidates + 1 : s.count;
+  int total = work > kMostGroups ? kCandidates + 1 : s.count;
   __syncthreads();
   if (total > kCandidates) {
     // Many equal logits: the n-th largest key of the part, eight bits at a time, until few enough reach it.
@@ -761,7 +765,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
   if (many) cluster_arrive();                                       // all CTAs run before one writes into another's memory
   const int n_ids = p.t.n_ids, n_list = p.t.n_teacher, n_top = p.t.n_top;
   const int lists = (n_list + 31) / 32;
-  unsigned char* const behind = more + (kGrad && kOnChip > 1 && p.tiles > 1 ? kTileBytes : 0);
+  unsigned char* const behind = more + (kGrad && p.tiles > 1 ? kTileBytes : 0);
   TopShared& top = *reinterpret_cast<TopShared*>(behind);
   unsigned long long* const merge = reinterpret_cast<unsigned long long*>(behind + top_bytes(p.tiles));
   uint8_t* const bits = reinterpret_cast<uint8_t*>(behind + (n_top ? top_bytes(p.tiles) + (many ? kMergeBytes : 0) : 0));
@@ -772,8 +776,9 @@ token_kernel(const __grid_constant__ TokenParams p) {
   }
   uint4* const kept = reinterpret_cast<uint4*>(more) + tid;         // a thread's own places: its units of tile 1, those of tile 0 stay in registers
   uint4 raw[kUnits];
-  const uint64_t last_read = keep_policy(!kGrad && n_top > 0), read_again = keep_policy(true);
-  load_tile(at, p.tiles - 1, kGrad && p.tiles > kOnChip ? read_again : last_read, raw);                       // the part's cut tile first: the last two, that stay here, are whole
+  const uint64_t last_read = keep_policy(false), read_again = keep_policy(true);
+  // the part's cut tile first: the last two, that stay here, are whole
+  load_tile(at, p.tiles - 1, kGrad && p.tiles > kOnChip ? read_again : last_read, raw);
   const float inv = p.t.temperature ? 1.f / p.t.temperature[row] : 1.f, c = inv * kLog2e;
   const float dh = kGrad && p.g.dentropy ? p.g.dentropy[row] * p.g.entropy_scale : 0.f;
   const float dd = kGrad && p.g.ddistill ? p.g.ddistill[row] * p.g.distill_scale : 0.f;
@@ -844,196 +849,186 @@ token_kernel(const __grid_constant__ TokenParams p) {
     }
   };
 
-    float m = -INFINITY, s0 = 0.f, s1 = 0.f, edge_left = -INFINITY;
-    for (int tile = p.tiles - 1; tile >= 0; --tile) {
-      mask_tile(tile);
-      if (kGrad && tile == kOnChip - 1 && tile > 0) {
+  float m = -INFINITY, s0 = 0.f, s1 = 0.f, edge_left = -INFINITY;
+  for (int tile = p.tiles - 1; tile >= 0; --tile) {
+    mask_tile(tile);
+    if (kGrad && tile == kOnChip - 1 && tile > 0) {
 #pragma unroll
-        for (int j = 0; j < kUnits; ++j) kept[j * kTokThreads] = raw[j];
-      }
-      uint32_t w = Empty8<T>::word;
-      if (n_top) {
-        uint32_t most[kUnits];
+      for (int j = 0; j < kUnits; ++j) kept[j * kTokThreads] = raw[j];
+    }
+    uint32_t w = Empty8<T>::word;
 #pragma unroll
-        for (int j = 0; j < kUnits; ++j) {
-          const uint32_t v = max_unit<T>(Empty8<T>::word, raw[j]);
-          w = max2(w, v, T());
-          most[j] = unit_most<T>(v);
-        }
-        top.most[tile * kTokThreads + tid] = make_uint4(most[0] | most[1] << 16, most[2] | most[3] << 16, most[4] | most[5] << 16, most[6] | most[7] << 16);
-      } else {
-#pragma unroll
-        for (int j = 0; j < kUnits; ++j) w = max_unit<T>(w, raw[j]);
-      }
-      const float tm = max_of<T>(w);
-      refer(m, fmaxf(m, tm), c, s0, s1);
-      m = fmaxf(m, tm);
-      bool asked = false;
-      if (fabsf(m) > kHuge && fabsf(m) < INFINITY) {
-        sum_huge(at, bits, m, c, tile, s0, s1);
-      } else {
-        // y = l c - r in one rounding; what r = m c rounded is off by is taken back from the sums
-        const float ref = finite_ref(m), r = ref * c, off = fmaf(ref, c, -r);
-        // as a unit is done with, the next tile's is asked for
-        const bool ask = tile > 0 && whole_tile(at, tile - 1);
-        const uint64_t policy = kGrad && tile > kOnChip ? read_again : last_read;
-        float t0, t1;
-        if (ask) sum_tile<T, kEnt, true>(raw, c, r, t0, t1, tile_at(at, tile - 1), policy);
-        else sum_tile<T, kEnt, false>(raw, c, r, t0, t1, nullptr, 0);
-        asked = ask;
-        const float f = ex2(-off);
-        s0 += f * t0;
-        if (kEnt) s1 += f * fmaf(-off, t0, t1);
-      }
-      if (!kGrad && tile == p.tiles - 1) meet();
-      if (tile > 0 && !asked) load_tile(at, tile - 1, kGrad && tile > kOnChip ? read_again : last_read, raw);
-    }
-    if (at.edges > 0) {
-      const float x = kRest && tid < at.edges && s.edges >> tid & 1 ? -INFINITY : edge_x;
-      const float to = fmaxf(m, x), y = (x - finite_ref(to)) * c, e = ex2(y);
-      refer(m, to, c, s0, s1);
-      m = to;
-      s0 += e;
-      s1 += e * fmaxf(y, kFloorY);
-      edge_left = x;
-    }
-    if (n_list > 0) __syncthreads();                                // the list's ids are there
-    my.x = to_float(given_x);
-    if (warp < lists) {
-      if (my.tid >= 0) my.tx = to_float(listed_x);
-      if (my.tid >= 0 && again_later(s, my.tid, n_list)) my.tid = -1;
-      const bool used = my.tid >= 0;
-      const float x = used ? my.tx : -INFINITY;
-      ListSums l;
-      l.m = warp_most(x);
-      const float y = (x - finite_ref(l.m)) * c, e = used ? ex2(y) : 0.f;
-      l.s0 = warp_total(e);
-      l.s1 = warp_total(e * fmaxf(y, kFloorY));
-      l.etl = warp_total(e != 0.f ? e * my.tl : 0.f);
-      l.tm = p.t.kind == PG_DISTILL_FORWARD ? warp_most(used ? my.tl : -INFINITY) : 0.f;
-      const float t = used ? expf(my.tl - finite_ref(l.tm)) : 0.f;
-      l.ts = warp_total(t);
-      l.ttl = warp_total(t != 0.f ? t * (my.tl - finite_ref(l.tm)) : 0.f);
-      l.ty = warp_total(t != 0.f ? t * (x - finite_ref(l.m)) * inv : 0.f);
-      l.mass = kRest ? warp_total(used ? exp((double)my.tl) : 0.) : 0.;
-      if (lane == 0) s.list[warp] = l;
-    }
-    const float own = m;
-    m = warp_most(m);
-    refer(own, m, c, s0, s1);
-    s0 = warp_total(s0);
-    if (kEnt) s1 = warp_total(s1);
-    if (n_top)
-      select_top(top, at, n_top, p.tiles, own, edge_left, kRest && my.tid >= 0 && at.owns(my.tid) ? my.tx : -INFINITY, my.tid,
-                 kRest ? bits : nullptr);
-    // the triples of the parts' warps, to all parts
-    float4* const triples = s.part;
-    if (many) {
-      cluster_wait();
-      if (lane < p.parts) peer_store(peer(&triples[at.part * kTokWarps + warp], lane), m, s0, s1);
-      for (int i = tid; i < n_top; i += kTokThreads) peer_store(peer(merge + at.part * PG_TOKEN_MAX_TOP + i, 0), top.best[i]);
-      __syncwarp();
-      cluster_arrive();
-      cluster_wait();
+    for (int j = 0; j < kUnits; ++j) w = max_unit<T>(w, raw[j]);
+    if (n_top) top.most[tile * kTokThreads + tid] = (uint16_t)most_bits<T>(w);
+    const float tm = max_of<T>(w);
+    refer(m, fmaxf(m, tm), c, s0, s1);
+    m = fmaxf(m, tm);
+    bool asked = false;
+    if (fabsf(m) > kHuge && fabsf(m) < INFINITY) {
+      sum_huge(at, bits, m, c, tile, s0, s1);
     } else {
-      if (lane == 0) triples[warp] = make_float4(m, s0, s1, 0.f);
-      __syncthreads();
+      // y = l c - r in one rounding; what r = m c rounded is off by is taken back from the sums
+      const float ref = finite_ref(m), r = ref * c, off = fmaf(ref, c, -r);
+      // as a unit is done with, the next tile's is asked for
+      const bool ask = tile > 0 && whole_tile(at, tile - 1);
+      const uint64_t policy = kGrad && tile > kOnChip ? read_again : last_read;
+      float t0, t1;
+      if (ask) sum_tile<T, kEnt, true>(raw, c, r, t0, t1, tile_at(at, tile - 1), policy);
+      else sum_tile<T, kEnt, false>(raw, c, r, t0, t1, nullptr, 0);
+      asked = ask;
+      const float f = ex2(-off);
+      s0 += f * t0;
+      if (kEnt) s1 += f * fmaf(-off, t0, t1);
     }
-    TokenRow r;
-    if (warp == 0) {
-      r = finish_row(s, triples, p.parts, lists, kRest, p.t.kind, inv);
-      float lp_part = 0.f;
-      TokenSlope k = {};
-      if (kGrad) {
-        float d = 0.f;
-        for (int i = 0; i < (n_ids + 31) / 32; ++i) d += s.dsum[i];
-        lp_part = -fmaf(dh, r.h, d);                                // of p_v (.. - dh ln p_v)
-        k = slope_of(r, kRest, p.t.kind, lp_part, dh, dd, inv);
-      }
-      if (lane == 0) {
-        s.row = r;
-        s.slope = k;
-        s.lp_part = lp_part;
-      }
-    }
+    if (!kGrad && tile == p.tiles - 1) meet();
+    if (tile > 0 && !asked) load_tile(at, tile - 1, kGrad && tile > kOnChip ? read_again : last_read, raw);
+  }
+  if (at.edges > 0) {
+    const float x = kRest && tid < at.edges && s.edges >> tid & 1 ? -INFINITY : edge_x;
+    const float to = fmaxf(m, x), y = (x - finite_ref(to)) * c, e = ex2(y);
+    refer(m, to, c, s0, s1);
+    m = to;
+    s0 += e;
+    s1 += e * fmaxf(y, kFloorY);
+    edge_left = x;
+  }
+  if (n_list > 0) __syncthreads();                                // the list's ids are there
+  my.x = to_float(given_x);
+  if (warp < lists) {
+    if (my.tid >= 0) my.tx = to_float(listed_x);
+    if (my.tid >= 0 && again_later(s, my.tid, n_list)) my.tid = -1;
+    const bool used = my.tid >= 0;
+    const float x = used ? my.tx : -INFINITY;
+    ListSums l;
+    l.m = warp_most(x);
+    const float y = (x - finite_ref(l.m)) * c, e = used ? ex2(y) : 0.f;
+    l.s0 = warp_total(e);
+    l.s1 = warp_total(e * fmaxf(y, kFloorY));
+    l.etl = warp_total(e != 0.f ? e * my.tl : 0.f);
+    l.tm = p.t.kind == PG_DISTILL_FORWARD ? warp_most(used ? my.tl : -INFINITY) : 0.f;
+    const float t = used ? expf(my.tl - finite_ref(l.tm)) : 0.f;
+    l.ts = warp_total(t);
+    l.ttl = warp_total(t != 0.f ? t * (my.tl - finite_ref(l.tm)) : 0.f);
+    l.ty = warp_total(t != 0.f ? t * (x - finite_ref(l.m)) * inv : 0.f);
+    l.mass = kRest ? warp_total(used ? exp((double)my.tl) : 0.) : 0.;
+    if (lane == 0) s.list[warp] = l;
+  }
+  const float own = m;
+  m = warp_most(m);
+  refer(own, m, c, s0, s1);
+  s0 = warp_total(s0);
+  if (kEnt) s1 = warp_total(s1);
+  if (n_top)
+    select_top(top, at, n_top, p.tiles, own, edge_left, kRest && my.tid >= 0 && at.owns(my.tid) ? my.tx : -INFINITY, my.tid,
+               kRest ? bits : nullptr);
+  // the triples of the parts' warps, to all parts
+  float4* const triples = s.part;
+  if (many) {
+    cluster_wait();
+    if (lane < p.parts) peer_store(peer(&triples[at.part * kTokWarps + warp], lane), m, s0, s1);
+    for (int i = tid; i < n_top; i += kTokThreads) peer_store(peer(merge + at.part * PG_TOKEN_MAX_TOP + i, 0), top.best[i]);
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+  } else {
+    if (lane == 0) triples[warp] = make_float4(m, s0, s1, 0.f);
     __syncthreads();
-    r = s.row;
-    if (at.part == 0) {
-      if (tid < n_ids && p.o.logp) {
-        const float lp = r.some != 0.f ? (my.x - r.m) * inv - kLn2 * r.l2 : -INFINITY;
-        p.o.logp[(int64_t)row * n_ids + tid] = my.id >= 0 ? lp : 0.f;
-      }
-      if (tid == 0) {
-        if (p.o.lse) p.o.lse[row] = r.some != 0.f ? r.m * inv + kLn2 * r.l2 : -INFINITY;
-        if (p.o.entropy) p.o.entropy[row] = r.h;
-        if (p.o.distill) p.o.distill[row] = r.loss;
-        if (p.o.saved) save_row((float4*)p.o.saved + (int64_t)row * (PG_TOKEN_SAVED / 4), r);
-      }
-      if (n_top) {
-        auto write = [&](int at, unsigned long long key) {
-          const float x = key_value(key);
-          p.o.top_ids[(int64_t)row * n_top + at] = key ? (int)(0xFFFFFFFFu - (uint32_t)key) : -1;
-          if (p.o.top_logp) p.o.top_logp[(int64_t)row * n_top + at] = key ? (x - r.m) * inv - kLn2 * r.l2 : -INFINITY;
-        };
-        if (!many) {
-          for (int i = tid; i < n_top; i += kTokThreads) write(i, top.best[i]);
-        } else {
-          // the parts' lists are sorted: a key's rank is its own place and how many of each other list are above it
-          const unsigned long long* from = merge;
-          auto above = [&](int o, unsigned long long key) {
-            int a = 0, b = n_top;
-            while (a < b) {
-              const int mid = (a + b) >> 1;
-              if (from[o * PG_TOKEN_MAX_TOP + mid] > key) a = mid + 1;
-              else b = mid;
-            }
-            return a;
-          };
-          for (int i = tid; i < n_top * p.parts; i += kTokThreads) {
-            const int q = i / n_top, at = i - q * n_top;
-            const unsigned long long key = from[q * PG_TOKEN_MAX_TOP + at];
-            if (!key) continue;
-            int rank = at;
-            for (int o = 0; o < p.parts; ++o)
-              if (o != q) rank += above(o, key);
-            if (rank < n_top) write(rank, key);
-          }
-          if (tid < n_top) {                                        // places that are left over
-            int some = 0;
-            for (int o = 0; o < p.parts; ++o) some += above(o, 0);
-            if (tid >= some) write(tid, 0);
-          }
-        }
-      }
+  }
+  TokenRow r;
+  if (warp == 0) {
+    r = finish_row(s, triples, p.parts, lists, kRest, p.t.kind, inv);
+    float lp_part = 0.f;
+    TokenSlope k = {};
+    if (kGrad) {
+      float d = 0.f;
+      for (int i = 0; i < (n_ids + 31) / 32; ++i) d += s.dsum[i];
+      lp_part = -fmaf(dh, r.h, d);                                // of p_v (.. - dh ln p_v)
+      k = slope_of(r, kRest, p.t.kind, lp_part, dh, dd, inv);
     }
-    if constexpr (kGrad) {
-      const TokenSlope slope = s.slope;
-      const Slope2 k(slope, c);
-      T* dl = (T*)p.dl + row * p.dl_stride;
-      const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0;
-      if (fabsf(slope.ref) > kHuge || !aligned) {                       // rows masked throughout, by the type's lowest value; or off 16 bytes
-        slope_huge(at, dl, slope, c);
+    if (lane == 0) {
+      s.row = r;
+      s.slope = k;
+      s.lp_part = lp_part;
+    }
+  }
+  __syncthreads();
+  r = s.row;
+  if (at.part == 0) {
+    if (tid < n_ids && p.o.logp) {
+      const float lp = r.some != 0.f ? (my.x - r.m) * inv - kLn2 * r.l2 : -INFINITY;
+      p.o.logp[(int64_t)row * n_ids + tid] = my.id >= 0 ? lp : 0.f;
+    }
+    if (tid == 0) {
+      if (p.o.lse) p.o.lse[row] = r.some != 0.f ? r.m * inv + kLn2 * r.l2 : -INFINITY;
+      if (p.o.entropy) p.o.entropy[row] = r.h;
+      if (p.o.distill) p.o.distill[row] = r.loss;
+      if (p.o.saved) save_row((float4*)p.o.saved + (int64_t)row * (PG_TOKEN_SAVED / 4), r);
+    }
+    if (n_top) {
+      auto write = [&](int at, unsigned long long key) {
+        const float x = key_value(key);
+        p.o.top_ids[(int64_t)row * n_top + at] = key ? (int)(0xFFFFFFFFu - (uint32_t)key) : -1;
+        if (p.o.top_logp) p.o.top_logp[(int64_t)row * n_top + at] = key ? (x - r.m) * inv - kLn2 * r.l2 : -INFINITY;
+      };
+      if (!many) {
+        for (int i = tid; i < n_top; i += kTokThreads) write(i, top.best[i]);
       } else {
-        for (int tile = 0; tile < p.tiles; ++tile) {
-          const int next = tile + 1;
-          const bool ask = next >= kOnChip && next < p.tiles && whole_tile(at, next);
-          if (ask) slope_tile<T, kEnt, true>(at, tile, raw, k, dl + at.head, tile_at(at, next), last_read);
-          else slope_tile<T, kEnt, false>(at, tile, raw, k, dl + at.head, nullptr, 0);
-          if (next < kOnChip && next < p.tiles) {
-#pragma unroll
-            for (int j = 0; j < kUnits; ++j) raw[j] = kept[j * kTokThreads];
-          } else if (next < p.tiles && !ask) {
-            load_tile(at, next, last_read, raw);
+        // the parts' lists are sorted: a key's rank is its own place and how many of each other list are above it
+        const unsigned long long* from = merge;
+        auto above = [&](int o, unsigned long long key) {
+          int a = 0, b = n_top;
+          while (a < b) {
+            const int mid = (a + b) >> 1;
+            if (from[o * PG_TOKEN_MAX_TOP + mid] > key) a = mid + 1;
+            else b = mid;
           }
+          return a;
+        };
+        for (int i = tid; i < n_top * p.parts; i += kTokThreads) {
+          const int q = i / n_top, at = i - q * n_top;
+          const unsigned long long key = from[q * PG_TOKEN_MAX_TOP + at];
+          if (!key) continue;
+          int rank = at;
+          for (int o = 0; o < p.parts; ++o)
+            if (o != q) rank += above(o, key);
+          if (rank < n_top) write(rank, key);
+        }
+        if (tid < n_top) {                                        // places that are left over
+          int some = 0;
+          for (int o = 0; o < p.parts; ++o) some += above(o, 0);
+          if (tid >= some) write(tid, 0);
         }
       }
-      if (tid < at.edges) put_edge(dl + at.edge(tid), edge_x, slope, c);
-      const bool fix_list = n_list > 0 && (kRest || p.g.ddistill);
-      if (n_ids > 0 || fix_list) {
-        __syncthreads();
-        fix_tokens(s, at, my, r, dl, n_ids, n_list, fix_list, kRest, p.g.ddistill != nullptr, p.t.kind, s.lp_part, dh, dd, inv);
+    }
+  }
+  if constexpr (kGrad) {
+    const TokenSlope slope = s.slope;
+    const Slope2 k(slope, c);
+    T* dl = (T*)p.dl + row * p.dl_stride;
+    const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0;
+    if (fabsf(slope.ref) > kHuge || !aligned) {                       // rows masked throughout, by the type's lowest value; or off 16 bytes
+      slope_huge(at, dl, slope, c);
+    } else {
+      for (int tile = 0; tile < p.tiles; ++tile) {
+        const int next = tile + 1;
+        const bool ask = next >= kOnChip && next < p.tiles && whole_tile(at, next);
+        if (ask) slope_tile<T, kEnt, true>(at, tile, raw, k, dl + at.head, tile_at(at, next), last_read);      // from the L2 cache
+        else slope_tile<T, kEnt, false>(at, tile, raw, k, dl + at.head, nullptr, 0);
+        if (next < kOnChip && next < p.tiles) {
+#pragma unroll
+          for (int j = 0; j < kUnits; ++j) raw[j] = kept[j * kTokThreads];
+        } else if (next < p.tiles && !ask) {
+          load_tile(at, next, last_read, raw);
+        }
       }
     }
+    if (tid < at.edges) put_edge(dl + at.edge(tid), edge_x, slope, c);
+    const bool fix_list = n_list > 0 && (kRest || p.g.ddistill);
+    if (n_ids > 0 || fix_list) {
+      __syncthreads();
+      fix_tokens(s, at, my, r, dl, n_ids, n_list, fix_list, kRest, p.g.ddistill != nullptr, p.t.kind, s.lp_part, dh, dd, inv);
+    }
+  }
 }
 
 // The gradient alone, from what a forward pass has saved.
@@ -1126,7 +1121,8 @@ int launch_forward(TokenParams p, cudaStream_t st) {
   p.units = (total + parts - 1) / parts;
   p.tiles = (p.units + kTile - 1) / kTile;
   if ((int64_t)p.n_rows * parts > 0x7FFFFFFFLL) return PG_EINVAL;
-  const int bytes = (kGrad && kOnChip > 1 && p.tiles > 1 ? kTileBytes : 0) + (p.t.n_top ? top_bytes(p.tiles) + (parts > 1 ? kMergeBytes : 0) : 0) + (kRest ? p.tiles * kTileUnits : 0);
+  const int bytes = (kGrad && p.tiles > 1 ? kTileBytes : 0) + (p.t.n_top ? top_bytes(p.tiles) + (parts > 1 ? kMergeBytes : 0) : 0) +
+                    (kRest ? p.tiles * kTileUnits : 0);
   auto kernel = token_kernel<T, kGrad, kEnt, kRest>;
   static std::atomic<uint64_t> done{0};
   constexpr int kMostBytes = kTileBytes + (int)sizeof(TopShared) + kMergeBytes + PG_TOKEN_MAX_VOCAB / 4 / kMostParts + kTileUnits;
@@ -1151,9 +1147,9 @@ int launch_forward(TokenParams p, cudaStream_t st) {
 template <typename T, bool kEnt>
 int launch_backward(TokenParams p, cudaStream_t st) {
   const int total = std::max(p.vocab / kPer<T>, 1);
-  // what a CTA learns of its row serves up to four tiles, where there are rows enough
+  // what a CTA learns of its row serves two tiles, where there are rows enough
   const int tiles = (total + kTileUnits - 1) / kTileUnits;
-  const int most = (int)std::min<int64_t>(std::max<int64_t>((int64_t)p.n_rows * tiles / (2 * 148 * kTokCtas), 1), MT);
+  const int most = (int)std::min<int64_t>(std::max<int64_t>((int64_t)p.n_rows * tiles / (2 * 148 * kTokCtas), 1), kBackwardTiles);
   p.parts = (tiles + most - 1) / most;
   p.units = (total + p.parts - 1) / p.parts;
   p.tiles = (p.units + kTileUnits - 1) / kTileUnits;
