@@ -600,14 +600,19 @@ __device__ __forceinline__ void put_edge(T* to, float x, const TokenSlope& k, fl
   *to = from_float<T>(ex2(y) * fmaf(fmaxf(y, kFloorY), k.b * kLn2, k.a));
 }
 
+// The divergence's derivative to the logits outside the list, over their shares of what is there (pr = p_r, whose logarithm may be far beyond 32 bits).
+__device__ __forceinline__ float rest_slope(const TokenRow& r, int kind, float pr) {
+  if (kind == PG_DISTILL_FORWARD_REST) return pr * r.w - expf(r.lt);
+  return pr == 0.f ? 0.f : pr * (r.lr - r.lt - r.loss);
+}
+
 // By one warp: the gradient's slope from what is known of the row.
 __device__ __forceinline__ TokenSlope slope_of(const TokenRow& r, bool rest, int kind, float lp_part, float dh, float dd, float inv) {
   TokenSlope k;
   if (rest) {
     const bool outside = r.lr > -INFINITY;
-    const float pr = outside ? expf(r.lr) : 0.f, lr = outside ? r.lr : 0.f;
-    const float dist = kind == PG_DISTILL_FORWARD_REST ? pr * r.w - expf(r.lt) : pr * (lr - r.lt - r.loss);
-    k.a = outside || r.lr != r.lr ? inv * (pr * (lp_part - dh * lr) + dd * dist) : 0.f;
+    const float pr = outside || r.lr != r.lr ? expf(r.lr) : 0.f;
+    k.a = outside || r.lr != r.lr ? inv * ((pr == 0.f ? 0.f : pr * (lp_part - dh * r.lr)) + dd * rest_slope(r, kind, pr)) : 0.f;
     k.b = -inv * dh * pr;
     k.ref = r.mr;
     k.l2 = r.l2r;
@@ -650,8 +655,7 @@ __device__ __forceinline__ void fix_tokens(const TokenShared& s, const RowPart<T
       float sum = base(pv, kLn2 * y);
       if (!rest) sum += dd * r.w * pv;
       else if (distill) {                                           // outside the list
-        const float rv = ex2((e.x - r.mr) * c - r.l2r), pr = expf(r.lr);
-        sum += dd * rv * (kind == PG_DISTILL_FORWARD_REST ? pr * r.w - expf(r.lt) : pr * (r.lr - r.lt - r.loss));
+        sum += dd * ex2((e.x - r.mr) * c - r.l2r) * rest_slope(r, kind, expf(r.lr));
       }
       for (int j = 0; j <= tid; ++j)
         if (s.gid[j] == e.id) sum += s.gdl[j];

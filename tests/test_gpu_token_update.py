@@ -418,8 +418,9 @@ def test_gradient_against_differences():
         assert (d - g[0]).abs().max() <= tol, (kind, float((d - g[0]).abs().max()), tol)
 
 
-def test_rows_without_derivatives_are_zero_and_not_read():
-    R, V = 6, 5001
+@pytest.mark.parametrize("V,off", [(5001, 0), (40003, 0), (40003, 1), (131072, 0)])
+def test_rows_without_derivatives_are_zero_and_not_read(V, off):
+    R = 6
     c = make(R, V, torch.bfloat16, 12, n_list=10, masks=False)
     t, o = terms_of(c, "forward_rest"), outputs(R, c, 0, True)
     B.token_forward(c["x"], t, **o)
@@ -429,9 +430,66 @@ def test_rows_without_derivatives_are_zero_and_not_read():
     rows = reference(c, "forward_rest")
     x = c["x"].clone()
     x[1] = math.nan                                                # no longer looked at
-    g = torch.full_like(x, 9)
+    g = torch.full((R, V + off), 9.0, device="cuda", dtype=torch.bfloat16)[:, off:]
     B.token_backward(x, t, o["saved"], g, **{k: c[k] for k in ("dlogp", "dentropy", "ddistill")})
     assert (g[1:3] == 0).all()
+    check_gradient(c, g, rows)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_logits_next_to_the_types_ends(dtype):
+    """Logits of +-3e38, whose products with log2(e) / T have no 32-bit value: alone, beside ordinary ones, on the list."""
+    R, V = 7, 20011
+    c = make(R, V, dtype, 31, n_ids=2, n_list=6, masks=False)
+    big = torch.finfo(dtype).max
+    c["x"][0, ::3] = big
+    c["x"][1] = -big
+    c["x"][2, 5000:] = -big
+    c["x"][3, int(c["list_ids"][3, 0])] = big
+    c["x"][4] = big
+    c["x"][5, 1:] = -big
+    for kind in B.DISTILL_KINDS:
+        rows = reference(c, kind)
+        o, g, h = outputs(R, c, 3, True), torch.empty_like(c["x"]), torch.empty_like(c["x"])
+        grads = {k: c[k] for k in ("dlogp", "dentropy", "ddistill")}
+        B.token_forward_backward(c["x"], terms_of(c, kind, n_top=3), g, **o, **grads)
+        check_gradient(c, g, rows)
+        B.token_backward(c["x"], terms_of(c, kind), o["saved"], h, **grads)
+        check_gradient(c, h, rows)
+        for r in (1, 4):                                           # all equal
+            assert abs(float(o["entropy"][r]) - math.log(V)) <= U * (SUM + 16 * tiles_of(V, dtype)) * (1 + 3 * math.log(V))
+        for r in range(R):
+            assert o["top_ids"][r].tolist() == ref.alternatives(c["x"][r], 3).tolist()
+
+
+def test_rows_more_than_2_to_the_31_elements_apart():
+    """Rows at both ends of a buffer of 8 GB."""
+    V, pitch = 5003, 2 ** 31 + 24
+    c = make(3, V, torch.bfloat16, 41, n_list=5, masks=False)
+    room = torch.empty(2 * pitch + V, device="cuda", dtype=torch.bfloat16)
+    x = room.as_strided((3, V), (pitch, 1))
+    x.copy_(c["x"])
+    rows = reference(c, "forward_rest")
+    o, g = outputs(3, c, 4, True), torch.empty((3, V), device="cuda", dtype=torch.bfloat16)
+    grads = {k: c[k] for k in ("dlogp", "dentropy", "ddistill")}
+    B.token_forward_backward(x, terms_of(c, "forward_rest", n_top=4), g, **o, **grads)
+    check_forward(c, o, rows, 4)
+    check_gradient(c, g, rows)
+    B.token_backward(x, terms_of(c, "forward_rest"), o["saved"], x, **grads)
+    check_gradient(c, x, rows)
+    del room, x
+    torch.cuda.empty_cache()
+
+
+def test_calls_on_a_stream_that_is_given():
+    c = make(5, 9001, torch.float16, 42, n_list=5)
+    rows = reference(c, "forward")
+    side = torch.cuda.Stream()
+    o, g = outputs(5, c, 4, True), torch.empty_like(c["x"])
+    side.wait_stream(torch.cuda.current_stream())
+    B.token_forward_backward(c["x"], terms_of(c, "forward", n_top=4), g, **o, **{k: c[k] for k in ("dlogp", "dentropy", "ddistill")}, stream=side)
+    side.synchronize()
+    check_forward(c, o, rows, 4)
     check_gradient(c, g, rows)
 
 

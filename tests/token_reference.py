@@ -81,7 +81,7 @@ def row_terms(l, tau=1.0, ids=(), list_ids=(), list_logp=(), kind="forward", dlo
         size[at] += abs(ddistill) / tau * (t if kind != "reverse_rest" else torch.where(have, p.detach()[inside] * (tl.abs() + ld[inside].abs() + 1), torch.zeros_like(t)))
         if kind != "forward" and some:
             tr = max(1 - float(t.sum()), LEAST_REST)
-            lr, share_of = rest_of(x, rest, tau, out["lse"])
+            lr, share_of = rest_of(x, rest, tau)
             if kind == "forward_rest":
                 loss = loss + tr * (math.log(tr) - lr)
                 size_d += tr * (abs(math.log(tr)) + abs(float(lr)))
@@ -102,15 +102,14 @@ def row_terms(l, tau=1.0, ids=(), list_ids=(), list_logp=(), kind="forward", dlo
     return out
 
 
-def rest_of(x, rest, tau, lse):
-    """Logarithm of the mass of the tokens `rest` and their shares of it, from their own largest logit: next to the type's lowest
-    value, a logarithm of their number would be lost."""
-    y = x[rest]
-    top = y.max()
-    lr = torch.logsumexp((y - top.detach()) / tau, -1) + (top.detach() / tau - lse)
-    # lse depends on x as well: its derivative is p
-    lr = lr - (torch.logsumexp(x / tau, -1) - torch.logsumexp(x.detach() / tau, -1))
-    return lr, torch.softmax((y.detach() - top.detach()) / tau, -1)
+def rest_of(x, rest, tau):
+    """Logarithm of the mass of the tokens `rest` and their shares of it.  Next to the types' ends 64 bits lose small differences as
+    well, so sums are taken from the largest logit of their own, and the derivative is put in as what it is: shares - p."""
+    y, z = x[rest].detach(), x.detach()
+    share, p = torch.softmax((y - y.max()) / tau, -1), torch.softmax((z - z.max()) / tau, -1)
+    value = torch.logsumexp((y - y.max()) / tau, -1) - torch.logsumexp((z - z.max()) / tau, -1) + (y.max() - z.max()) / tau
+    slope = ((share * x[rest]).sum() - (p * x).sum()) / tau
+    return value + (slope - slope.detach()), share
 
 
 def loss_without_infinity(t, have, lp, inside, kind, lr):
