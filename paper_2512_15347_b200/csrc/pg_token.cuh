@@ -89,6 +89,7 @@ struct TokenShared {
   alignas(16) int tid[PG_TOKEN_MAX_LIST];       // listed tokens, -1: unused
   uint32_t edges;                               // bits of the listed ones among the edge tokens
 };
+
 typedef unsigned long long f2;                  // two floats for the packed fp32 instructions
 __device__ __forceinline__ f2 make2(float a, float b) {
   f2 r;
@@ -584,15 +585,21 @@ __device__ __forceinline__ void slope_unit(const uint4& v, const Slope2& k, floa
 }
 // A part from memory, logit by logit, differences first: whose reference is that far down, or whose gradient lies off 16 bytes.
 template <typename T>
-__device__ __noinline__ void slope_huge(const RowPart<T>& at, T* dl, const TokenSlope& k, float c, bool quiet = false) {
+__device__ __noinline__ void slope_huge(const RowPart<T>& at, T* dl, const TokenSlope& k, float c) {
   for (int t = at.head + at.first * kPer<T> + threadIdx.x; t < at.head + at.last * kPer<T>; t += kTokThreads) {
-    float g = 0.f;
-    if (!quiet) {
-      const float y = (to_float(at.in[t]) - k.ref) * c - k.l2;
-      g = ex2(y) * fmaf(fmaxf(y, kFloorY), k.b * kLn2, k.a);
-    }
-    dl[t] = from_float<T>(g);
+    const float y = (to_float(at.in[t]) - k.ref) * c - k.l2;
+    dl[t] = from_float<T>(ex2(y) * fmaf(fmaxf(y, kFloorY), k.b * kLn2, k.a));
   }
+}
+// The part's gradient where a row has no derivatives.
+template <typename T>
+__device__ __noinline__ void zero_part(const RowPart<T>& at, T* dl) {
+  if (((uintptr_t)(dl + at.head) & 15) == 0) {
+    for (int u = at.first + (int)threadIdx.x; u < at.last; u += kTokThreads) __stcs((uint4*)(dl + at.head) + u, make_uint4(0u, 0u, 0u, 0u));
+  } else {
+    for (int t = at.head + at.first * kPer<T> + threadIdx.x; t < at.head + at.last * kPer<T>; t += kTokThreads) dl[t] = from_float<T>(0.f);
+  }
+  if ((int)threadIdx.x < at.edges) dl[at.edge(threadIdx.x)] = from_float<T>(0.f);
 }
 template <typename T>
 __device__ __forceinline__ void put_edge(T* to, float x, const TokenSlope& k, float c) {
@@ -612,7 +619,7 @@ __device__ __forceinline__ TokenSlope slope_of(const TokenRow& r, bool rest, int
   if (rest) {
     const bool outside = r.lr > -INFINITY;
     const float pr = outside || r.lr != r.lr ? expf(r.lr) : 0.f;
-    k.a = outside || r.lr != r.lr ? inv * ((pr == 0.f ? 0.f : pr * (lp_part - dh * r.lr)) + dd * rest_slope(r, kind, pr)) : 0.f;
+    k.a = outside || r.lr != r.lr ? inv * ((pr == 0.f ? 0.f : pr * (lp_part - dh * r.lr)) + (dd == 0.f ? 0.f : dd * rest_slope(r, kind, pr))) : 0.f;
     k.b = -inv * dh * pr;
     k.ref = r.mr;
     k.l2 = r.l2r;
@@ -629,7 +636,7 @@ __device__ __forceinline__ TokenSlope slope_of(const TokenRow& r, bool rest, int
 // Given and listed tokens, over what the stream has written.
 template <typename T>
 __device__ __forceinline__ void fix_tokens(const TokenShared& s, const RowPart<T>& at, const Entry& e, const TokenRow& r, T* dl, int n_ids,
-                                           int n_list, bool fix_list, bool rest, bool distill, int kind, float lp_part, float dh, float dd,
+                                           int n_list, bool fix_list, bool rest, int kind, float lp_part, float dh, float dd,
                                            float inv) {
   const int tid = threadIdx.x;
   const float c = inv * kLog2e;
@@ -640,7 +647,7 @@ __device__ __forceinline__ void fix_tokens(const TokenShared& s, const RowPart<T
     if (kind == PG_DISTILL_FORWARD) dist = r.w * pv - expf(e.tl - r.lt);
     else if (kind == PG_DISTILL_FORWARD_REST) dist = r.w * pv - expf(e.tl);
     else dist = pv == 0.f ? 0.f : pv * (lp - e.tl - r.loss);
-    float sum = base(pv, lp) + dd * dist;
+    float sum = base(pv, lp) + (dd == 0.f ? 0.f : dd * dist);
     for (int j = 0; j < n_ids; ++j)
       if (s.gid[j] == e.tid) sum += s.gdl[j];
     dl[e.tid] = from_float<T>(r.some != 0.f ? inv * sum : 0.f);
@@ -654,9 +661,7 @@ __device__ __forceinline__ void fix_tokens(const TokenShared& s, const RowPart<T
       const float y = (e.x - r.m) * c - r.l2, pv = ex2(y);
       float sum = base(pv, kLn2 * y);
       if (!rest) sum += dd * r.w * pv;
-      else if (distill) {                                           // outside the list
-        sum += dd * ex2((e.x - r.mr) * c - r.l2r) * rest_slope(r, kind, expf(r.lr));
-      }
+      else if (dd != 0.f) sum += dd * ex2((e.x - r.mr) * c - r.l2r) * rest_slope(r, kind, expf(r.lr));   // outside the list
       for (int j = 0; j <= tid; ++j)
         if (s.gid[j] == e.id) sum += s.gdl[j];
       dl[e.id] = from_float<T>(r.some != 0.f ? inv * sum : 0.f);
@@ -755,6 +760,7 @@ __device__ __forceinline__ void sum_tile(uint4 (&raw)[kTokUnits], float c, float
   split2(add2(a1, b1), u, v);
   t1 = u + v;
 }
+
 // Forward, with the gradient on top (kGrad).
 template <typename T, bool kGrad, bool kEnt, bool kRest>
 __global__ void __launch_bounds__(kTokThreads, kTokCtas)
@@ -955,7 +961,9 @@ token_kernel(const __grid_constant__ TokenParams p) {
       s.lp_part = lp_part;
     }
   }
-  __syncthreads();
+  bool quiet = false;
+  if (kGrad) quiet = !__syncthreads_or(my.dl != 0.f || dh != 0.f || dd != 0.f);
+  else __syncthreads();
   r = s.row;
   if (at.part == 0) {
     if (tid < n_ids && p.o.logp) {
@@ -1006,9 +1014,13 @@ token_kernel(const __grid_constant__ TokenParams p) {
     }
   }
   if constexpr (kGrad) {
+    T* dl = (T*)p.dl + row * p.dl_stride;
+    if (quiet) {                                                      // no derivatives: zeros, whatever the row holds
+      zero_part(at, dl);
+      return;
+    }
     const TokenSlope slope = s.slope;
     const Slope2 k(slope, c);
-    T* dl = (T*)p.dl + row * p.dl_stride;
     const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0;
     if (fabsf(slope.ref) > kHuge || !aligned) {                       // rows masked throughout, by the type's lowest value; or off 16 bytes
       slope_huge(at, dl, slope, c);
@@ -1030,7 +1042,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
     const bool fix_list = n_list > 0 && (kRest || p.g.ddistill);
     if (n_ids > 0 || fix_list) {
       __syncthreads();
-      fix_tokens(s, at, my, r, dl, n_ids, n_list, fix_list, kRest, p.g.ddistill != nullptr, p.t.kind, s.lp_part, dh, dd, inv);
+      fix_tokens(s, at, my, r, dl, n_ids, n_list, fix_list, kRest, p.t.kind, s.lp_part, dh, dd, inv);
     }
   }
 }
@@ -1062,14 +1074,14 @@ token_backward_kernel(const __grid_constant__ TokenParams p) {
   }
   const bool quiet = !__syncthreads_or(my.dl != 0.f || dh != 0.f || dd != 0.f);
   const uint64_t last_read = keep_policy(false);
-  uint4 raw[kUnits];
-  if (!quiet) {
-    load_tile(at, p.tiles - 1, last_read, raw);                     // the cut tile first
-  } else {
-#pragma unroll
-    for (int j = 0; j < kUnits; ++j) raw[j] = empty_unit<T>();
+  T* dl = (T*)p.dl + row * p.dl_stride;
+  if (quiet) {
+    zero_part(at, dl);
+    return;
   }
-  const float edge_x = tid < at.edges && !quiet ? to_float(at.in[at.edge(tid)]) : -INFINITY;
+  uint4 raw[kUnits];
+  load_tile(at, p.tiles - 1, last_read, raw);                       // the cut tile first
+  const float edge_x = tid < at.edges ? to_float(at.in[at.edge(tid)]) : -INFINITY;
   if (my.id >= 0 && at.owns(my.id)) my.x = to_float(at.in[my.id]);
   if (distill && tid < n_list) {
     const int id = p.t.teacher_ids[(int64_t)row * n_list + tid];
@@ -1087,25 +1099,23 @@ token_backward_kernel(const __grid_constant__ TokenParams p) {
   float d = 0.f;
   for (int i = 0; i < (n_ids + 31) / 32; ++i) d += s.dsum[i];
   const float lp_part = -fmaf(dh, r.h, d);
-  TokenSlope slope = slope_of(r, rest, p.t.kind, lp_part, dh, dd, inv);
-  if (quiet) slope.a = slope.b = 0.f;
+  const TokenSlope slope = slope_of(r, rest, p.t.kind, lp_part, dh, dd, inv);
   const Slope2 k(slope, c);
-  T* dl = (T*)p.dl + row * p.dl_stride;
-  const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0, huge = !aligned || (fabsf(slope.ref) > kHuge && !quiet);
-  if (huge) {
-    slope_huge(at, dl, slope, c, quiet);
+  const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0;
+  if (fabsf(slope.ref) > kHuge || !aligned) {
+    slope_huge(at, dl, slope, c);
   } else {
     for (int tile = p.tiles - 1; tile >= 0; --tile) {
-      const bool ask = tile > 0 && !quiet && whole_tile(at, tile - 1);
+      const bool ask = tile > 0 && whole_tile(at, tile - 1);
       if (ask) slope_tile<T, kEnt, true>(at, tile, raw, k, dl + at.head, tile_at(at, tile - 1), last_read);
       else slope_tile<T, kEnt, false>(at, tile, raw, k, dl + at.head, nullptr, 0);
-      if (tile > 0 && !ask && !quiet) load_tile(at, tile - 1, last_read, raw);
+      if (tile > 0 && !ask) load_tile(at, tile - 1, last_read, raw);
     }
   }
   if (tid < at.edges) put_edge(dl + at.edge(tid), edge_x, slope, c);
-  if (quiet || (n_ids == 0 && !distill)) return;
+  if (n_ids == 0 && !distill) return;
   __syncthreads();
-  fix_tokens(s, at, my, r, dl, n_ids, n_list, distill, rest, distill, p.t.kind, lp_part, dh, dd, inv);
+  fix_tokens(s, at, my, r, dl, n_ids, n_list, distill, rest, p.t.kind, lp_part, dh, dd, inv);
 }
 
 template <typename T, bool kGrad, bool kEnt, bool kRest>

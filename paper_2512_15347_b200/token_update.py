@@ -47,8 +47,8 @@ def score(logits, ids=None, *, n_top: int = 0, temperature=None) -> Scores:
 class TokenUpdate:
     """The settings of an objective (see pg_token_objective) and what its calls need besides: workspaces, a status word.
 
-    ``step`` may be captured in a CUDA graph.  Calls run on the current stream; the workspaces are the stream's own, so calls on several
-    streams may overlap."""
+    ``step`` may be captured in a CUDA graph.  Calls run on the current stream; workspaces are a stream's or a graph's own, so calls on
+    several streams and replays of several graphs may overlap."""
 
     def __init__(self, *, clip_low: float = 0.2, clip_high: float = 0.2, beta: float = 0.0, entropy_coef: float = 0.0, distill_coef: float = 0.0,
                  kind: str = "forward", norm: str = "rows"):
@@ -60,18 +60,17 @@ class TokenUpdate:
         self.kind, self.entropy_coef, self.distill_coef = kind, entropy_coef, distill_coef
         self._rule = dict(clip_low=clip_low, clip_high=clip_high, beta=beta, norm=norm)
         self.status = torch.zeros(1, device=self.dev, dtype=torch.int32)
-        self._spaces, self._in_graphs = {}, {}
+        self._spaces = {}
 
     def _space(self, nbytes: int) -> torch.Tensor:
-        """The current stream's workspace, as ``PagedCache`` keeps its own."""
-        stream, capturing = B._stream(None), torch.cuda.is_current_stream_capturing()
+        """The current stream's workspace.  A capture takes one of the graph's own memory, zeroed at each replay: graphs recorded on one
+        stream may be replayed on several at once."""
+        if torch.cuda.is_current_stream_capturing():
+            return torch.zeros(nbytes, device=self.dev, dtype=torch.uint8)
+        stream = B._stream(None)
         space = self._spaces.get(stream)
         if space is None or space.nbytes < nbytes:
-            space = torch.zeros(nbytes, device=self.dev, dtype=torch.uint8)
-            if not capturing:
-                self._spaces[stream] = space
-        elif capturing:
-            self._in_graphs[space.data_ptr()] = space
+            space = self._spaces[stream] = torch.zeros(nbytes, device=self.dev, dtype=torch.uint8)
         return space
 
     def step(self, logits, ids, start, adv, logp_old=None, *, logp_ref=None, teacher: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,

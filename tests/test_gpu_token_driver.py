@@ -72,6 +72,32 @@ def test_driver_scores_steps_and_checks(kind):
         plain.check()
 
 
+def test_two_graphs_of_one_driver_run_at_once():
+    from paper_2512_15347_b200.token_update import TokenUpdate
+    V, n_rows = 4001, 600
+    rule, g = TokenUpdate(entropy_coef=0.1), torch.Generator(device="cuda").manual_seed(5)
+    start = torch.arange(n_rows + 1, device="cuda", dtype=torch.int32) * 8      # more tokens than one CTA of the objective takes
+    sides, graphs, eager = [torch.cuda.Stream() for _ in range(2)], [], []
+    for i in range(2):
+        x = torch.randn(n_rows * 8, V, device="cuda", generator=g).to(torch.bfloat16)
+        ids = torch.randint(0, V, (n_rows * 8,), device="cuda", generator=g, dtype=torch.int32)
+        adv, old = torch.randn(n_rows, device="cuda", generator=g), torch.full((n_rows * 8,), -8.0, device="cuda")
+        eager.append(rule.step(x, ids, start, adv, old))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            u = rule.step(x, ids, start, adv, old)
+        graphs.append((graph, u, (x, ids, adv, old)))           # a graph reads its inputs where they were
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for side, (graph, _, _) in zip(sides, graphs):
+            with torch.cuda.stream(side):
+                graph.replay()
+    torch.cuda.synchronize()
+    for (_, u, _), e in zip(graphs, eager):
+        assert torch.equal(u.objective, e.objective) and torch.equal(u.stats, e.stats) and torch.equal(u.dlogits, e.dlogits)
+    rule.check()
+
+
 def test_example_update_gives_the_objectives_gradient():
     from paper_2512_15347_b200.examples import token_rollout as T
     g = torch.Generator(device="cuda").manual_seed(3)

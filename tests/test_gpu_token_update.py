@@ -436,6 +436,27 @@ def test_rows_without_derivatives_are_zero_and_not_read(V, off):
     check_gradient(c, g, rows)
 
 
+@pytest.mark.parametrize("kind", B.DISTILL_KINDS)
+@pytest.mark.parametrize("V,off", [(7, 0), (5001, 0), (40003, 1), (131072, 0)])
+def test_padding_rows_of_any_content_have_no_gradient(V, off, kind):
+    R = 6
+    c = make(R, V, torch.bfloat16, 13, n_list=4, masks=False)
+    c["x"][1], c["x"][2, -1], c["x"][3, 0] = math.nan, math.inf, math.nan
+    for r in (1, 2, 3):
+        c["ids"][r], c["dlogp"][r], c["dentropy"][r], c["ddistill"][r] = -1, 5.0, 0, 0       # what padding's dlogp holds plays no part
+    c["list_logp"][5, 1], c["ddistill"][5] = math.nan, 0                                     # a teacher's list without weight
+    t, o, grads = terms_of(c, kind), outputs(R, c, 0, True), {k: c[k] for k in ("dlogp", "dentropy", "ddistill")}
+    both, back = (torch.full((R, V + off), 9.0, device="cuda", dtype=torch.bfloat16)[:, off:] for _ in range(2))
+    B.token_forward_backward(c["x"], t, both, **o, **grads)
+    B.token_backward(c["x"], t, o["saved"], back, **grads)
+    c["list_logp"][5, 1] = -1.0
+    good = [0, 4, 5]
+    rows = reference({k: v[good] for k, v in c.items()}, kind)
+    for g in (both, back):
+        assert (g[1:4] == 0).all()
+        check_gradient({k: v[good] for k, v in c.items()}, g[good], rows)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_logits_next_to_the_types_ends(dtype):
     """Logits of +-3e38, whose products with log2(e) / T have no 32-bit value: alone, beside ordinary ones, on the list."""
