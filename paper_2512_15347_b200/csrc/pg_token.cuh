@@ -46,6 +46,7 @@ constexpr float kFloorY = -1e4f;                // 2^y = 0 long before; keeps 0 
 constexpr float kHuge = 1e30f;                  // logits from here on (the type's lowest value as a mask) have no l c in 32 bits
 
 enum TokenMode { kForward, kBackward, kBoth };
+enum TokenLists { kNoList, kNormalised, kBucket };   // a teacher's list: none, PG_DISTILL_FORWARD, the kinds with a bucket
 
 struct TokenParams {
   pg_token_terms t;
@@ -246,8 +247,9 @@ __device__ __forceinline__ void join_warp(float& m, float& s0, float& s1, float 
   s1 = warp_total(s1);
 }
 
-// By one warp: from the sums over the row outside the list (`rest`) or over all of it, and the list's.
-__device__ __forceinline__ TokenRow finish_row(const TokenShared& s, const float4* triples, int parts, int lists, bool rest, int kind, float inv) {
+// By one warp: from the sums over the row, or over the row outside the list (kBucket), and the list's.
+template <int kLists>
+__device__ __forceinline__ TokenRow finish_row(const TokenShared& s, const float4* triples, int parts, int lists, int kind, float inv) {
   const float c = inv * kLog2e;
   const int lane = threadIdx.x & 31;
   TokenRow r;
@@ -261,44 +263,42 @@ __device__ __forceinline__ TokenRow finish_row(const TokenShared& s, const float
     s0 += v.y;
     s1 += v.z;
   }
-  join_warp(m, s0, s1, c);
-  r.mr = m;
-  const bool outside = !(s0 == 0.f);
-  r.l2r = outside ? log2f(s0) : 0.f;
   ListSums l;
   l.m = l.tm = -INFINITY;
   l.s0 = l.s1 = l.etl = l.ts = l.ttl = l.ty = 0.f;
   l.mass = 0.;
-  if (lane < lists) l = s.list[lane];
-  if (rest && lists > 0) {
-    float a = l.s0, b = l.s1;
-    if (lane == 31) {                                                  // the lists end before: at most eight
-      l.m = m;
-      a = s0;
-      b = s1;
-    }
-    float to = l.m;
-    join_warp(to, a, b, c);
-    if (lane == 31) l.m = -INFINITY;
+  if (kLists != kNoList && lane < lists) l = s.list[lane];
+  bool outside = true;
+  r.mr = r.lr = r.l2r = 0.f;
+  if (kLists == kBucket) {                                             // outside the list and in all, side by side
+    const float to = warp_most(fmaxf(m, l.m));
+    r.mr = warp_most(m);
+    float r0 = s0, r1 = 0.f, a = l.s0, b = l.s1;
+    refer(m, r.mr, c, r0, r1);
+    refer(m, to, c, s0, s1);
+    refer(l.m, to, c, a, b);
+    r0 = warp_total(r0);
+    s0 = warp_total(s0 + a);
+    s1 = warp_total(s1 + b);
     m = to;
-    s0 = a;
-    s1 = b;
+    outside = !(r0 == 0.f);
+    r.l2r = outside ? log2f(r0) : 0.f;
+  } else {
+    join_warp(m, s0, s1, c);
   }
   r.some = s0 == 0.f ? 0.f : 1.f;
   r.m = finite_ref(m);
   r.l2 = r.some != 0.f ? log2f(s0) : 0.f;
   r.h = r.some != 0.f ? kLn2 * (r.l2 - s1 / s0) : 0.f;
   double lr = 0.;
-  if (rest) {                                                          // in 64 bits: where only tokens of the type's lowest value are left,
+  if (kLists == kBucket) {                                             // in 64 bits: where only tokens of the type's lowest value are left,
     lr = ((double)finite_ref(r.mr) - r.m) * inv + (double)(kLn2 * (r.l2r - r.l2));      // it is finite and its share of the loss may be
     r.lr = !outside ? -INFINITY : lr < -3e38 ? -3e38f : (float)lr;
-  } else {
-    r.lr = 0.f;
   }
   r.mr = finite_ref(r.mr);
   r.loss = r.lt = r.w = 0.f;
-  if (lists == 0 || r.some == 0.f) return r;
-  if (kind == PG_DISTILL_FORWARD) {
+  if (kLists == kNoList || r.some == 0.f) return r;
+  if (kLists == kNormalised) {
     const float tm = warp_most(l.tm);
     float z = l.ts, ttl = 0.f, tlp = 0.f;                              // ts without tm: NaN
     if (l.tm != -INFINITY) {
@@ -762,9 +762,10 @@ __device__ __forceinline__ void sum_tile(uint4 (&raw)[kTokUnits], float c, float
 }
 
 // Forward, with the gradient on top (kGrad).
-template <typename T, bool kGrad, bool kEnt, bool kRest>
+template <typename T, bool kGrad, bool kEnt, int kLists>
 __global__ void __launch_bounds__(kTokThreads, kTokCtas)
 token_kernel(const __grid_constant__ TokenParams p) {
+  constexpr bool kRest = kLists == kBucket;
   constexpr int kUnits = kTokUnits, kTile = kTileUnits;
   __shared__ TokenShared s;
   extern __shared__ __align__(16) unsigned char more[];             // a tile; TopShared and the parts' lists if there are alternatives; bits (kRest)
@@ -773,7 +774,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
   const RowPart<T> at(p, row, blockIdx.x - row * p.parts);
   const bool many = p.parts > 1;
   if (many) cluster_arrive();                                       // all CTAs run before one writes into another's memory
-  const int n_ids = p.t.n_ids, n_list = p.t.n_teacher, n_top = p.t.n_top;
+  const int n_ids = p.t.n_ids, n_list = kLists == kNoList ? 0 : p.t.n_teacher, n_top = p.t.n_top;
   const int lists = (n_list + 31) / 32;
   unsigned char* const behind = more + (kGrad && p.tiles > 1 ? kTileBytes : 0);
   TopShared& top = *reinterpret_cast<TopShared*>(behind);
@@ -859,6 +860,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
     }
   };
 
+  const int lists_at = max(p.tiles - (kGrad ? 1 : 2), 0);           // the listed tokens' logits were asked for a tile before
   float m = -INFINITY, s0 = 0.f, s1 = 0.f, edge_left = -INFINITY;
   for (int tile = p.tiles - 1; tile >= 0; --tile) {
     mask_tile(tile);
@@ -891,6 +893,29 @@ token_kernel(const __grid_constant__ TokenParams p) {
       if (kEnt) s1 += f * fmaf(-off, t0, t1);
     }
     if (!kGrad && tile == p.tiles - 1) meet();
+    if (kLists != kNoList && tile == lists_at) {                    // while the next tile is on its way
+      if (lists > 1) __syncthreads();                               // the list's ids are there
+      else __syncwarp();
+      if (warp < lists) {
+        if (my.tid >= 0) my.tx = to_float(listed_x);
+        if (my.tid >= 0 && again_later(s, my.tid, n_list)) my.tid = -1;
+        const bool used = my.tid >= 0;
+        const float x = used ? my.tx : -INFINITY;
+        ListSums l;
+        l.m = warp_most(x);
+        const float y = (x - finite_ref(l.m)) * c, e = used ? ex2(y) : 0.f;
+        l.s0 = warp_total(e);
+        l.s1 = warp_total(e * fmaxf(y, kFloorY));
+        l.etl = warp_total(e != 0.f ? e * my.tl : 0.f);
+        l.tm = !kRest ? warp_most(used ? my.tl : -INFINITY) : 0.f;
+        const float t = used ? expf(my.tl - finite_ref(l.tm)) : 0.f;
+        l.ts = warp_total(t);
+        l.ttl = warp_total(t != 0.f ? t * (my.tl - finite_ref(l.tm)) : 0.f);
+        l.ty = warp_total(t != 0.f ? t * (x - finite_ref(l.m)) * inv : 0.f);
+        l.mass = kRest ? warp_total(used ? exp((double)my.tl) : 0.) : 0.;
+        if (lane == 0) s.list[warp] = l;
+      }
+    }
     if (tile > 0 && !asked) load_tile(at, tile - 1, kGrad && tile > kOnChip ? read_again : last_read, raw);
   }
   if (at.edges > 0) {
@@ -902,27 +927,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
     s1 += e * fmaxf(y, kFloorY);
     edge_left = x;
   }
-  if (n_list > 0) __syncthreads();                                // the list's ids are there
   my.x = to_float(given_x);
-  if (warp < lists) {
-    if (my.tid >= 0) my.tx = to_float(listed_x);
-    if (my.tid >= 0 && again_later(s, my.tid, n_list)) my.tid = -1;
-    const bool used = my.tid >= 0;
-    const float x = used ? my.tx : -INFINITY;
-    ListSums l;
-    l.m = warp_most(x);
-    const float y = (x - finite_ref(l.m)) * c, e = used ? ex2(y) : 0.f;
-    l.s0 = warp_total(e);
-    l.s1 = warp_total(e * fmaxf(y, kFloorY));
-    l.etl = warp_total(e != 0.f ? e * my.tl : 0.f);
-    l.tm = p.t.kind == PG_DISTILL_FORWARD ? warp_most(used ? my.tl : -INFINITY) : 0.f;
-    const float t = used ? expf(my.tl - finite_ref(l.tm)) : 0.f;
-    l.ts = warp_total(t);
-    l.ttl = warp_total(t != 0.f ? t * (my.tl - finite_ref(l.tm)) : 0.f);
-    l.ty = warp_total(t != 0.f ? t * (x - finite_ref(l.m)) * inv : 0.f);
-    l.mass = kRest ? warp_total(used ? exp((double)my.tl) : 0.) : 0.;
-    if (lane == 0) s.list[warp] = l;
-  }
   const float own = m;
   m = warp_most(m);
   refer(own, m, c, s0, s1);
@@ -946,7 +951,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
   }
   TokenRow r;
   if (warp == 0) {
-    r = finish_row(s, triples, p.parts, lists, kRest, p.t.kind, inv);
+    r = finish_row<kLists>(s, triples, p.parts, lists, p.t.kind, inv);
     float lp_part = 0.f;
     TokenSlope k = {};
     if (kGrad) {
@@ -1118,9 +1123,10 @@ token_backward_kernel(const __grid_constant__ TokenParams p) {
   fix_tokens(s, at, my, r, dl, n_ids, n_list, distill, rest, p.t.kind, lp_part, dh, dd, inv);
 }
 
-template <typename T, bool kGrad, bool kEnt, bool kRest>
+template <typename T, bool kGrad, bool kEnt, int kLists>
 int launch_forward(TokenParams p, cudaStream_t st) {
   constexpr int kTile = kTileUnits;
+  constexpr bool kRest = kLists == kBucket;
   const int total = std::max(p.vocab / kPer<T>, 1);
   int parts = 1;
   // Rows that are read twice: parts of 128 KB, so that what all SMs work on stays in the L2 cache.  With a bucket: bits of 16 KB at most.
@@ -1137,7 +1143,7 @@ int launch_forward(TokenParams p, cudaStream_t st) {
   if ((int64_t)p.n_rows * parts > 0x7FFFFFFFLL) return PG_EINVAL;
   const int bytes = (kGrad && p.tiles > 1 ? kTileBytes : 0) + (p.t.n_top ? top_bytes(p.tiles) + (parts > 1 ? kMergeBytes : 0) : 0) +
                     (kRest ? p.tiles * kTileUnits : 0);
-  auto kernel = token_kernel<T, kGrad, kEnt, kRest>;
+  auto kernel = token_kernel<T, kGrad, kEnt, kLists>;
   static std::atomic<uint64_t> done{0};
   constexpr int kMostBytes = kTileBytes + (int)sizeof(TopShared) + kMergeBytes + PG_TOKEN_MAX_VOCAB / 4 / kMostParts + kTileUnits;
   if (bytes > 32 * 1024)
@@ -1180,9 +1186,10 @@ int token_launch(const TokenParams& p, cudaStream_t st) {
     return ent ? launch_backward<T, true>(p, st) : launch_backward<T, false>(p, st);
   } else {
     constexpr bool kGrad = kMode == kBoth;
-    const bool rest = p.t.n_teacher > 0 && p.t.kind != PG_DISTILL_FORWARD;
-    if (rest) return ent ? launch_forward<T, kGrad, true, true>(p, st) : launch_forward<T, kGrad, false, true>(p, st);
-    return ent ? launch_forward<T, kGrad, true, false>(p, st) : launch_forward<T, kGrad, false, false>(p, st);
+    if (p.t.n_teacher == 0) return ent ? launch_forward<T, kGrad, true, kNoList>(p, st) : launch_forward<T, kGrad, false, kNoList>(p, st);
+    if (p.t.kind == PG_DISTILL_FORWARD)
+      return ent ? launch_forward<T, kGrad, true, kNormalised>(p, st) : launch_forward<T, kGrad, false, kNormalised>(p, st);
+    return ent ? launch_forward<T, kGrad, true, kBucket>(p, st) : launch_forward<T, kGrad, false, kBucket>(p, st);
   }
 }
 
