@@ -693,13 +693,13 @@ int pg_token_forward(int32_t n_rows, int32_t vocab, int32_t dtype, const void *l
  *     dlogits_v = 1/T ( sum_{j: ids[j] = v} dlogp_j - p_v sum_j dlogp_j - dentropy p_v (ln p_v + entropy) + ddistill d distill / d x_v ),
  * of dtype, rounded once.  dlogits has the logits' shape, rows dlogits_stride elements apart; it may be logits when the
  * strides agree (no other overlap).  terms and saved are those of pg_token_forward on the same logits (n_top plays no part).
- * Rows whose derivatives are all zero get zeros and are not read.
+ * Rows whose derivatives are all zero get zeros, whatever they hold, and are not read.
  */
 int pg_token_backward(int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t logits_stride,
                       const pg_token_terms *terms, const float *saved, const pg_token_grads *grads, void *dlogits,
                       int64_t dlogits_stride, void *stream);
 
-/* pg_token_forward and pg_token_backward in one pass: a row stays on chip between the two. */
+/* pg_token_forward and pg_token_backward in one pass: DRAM sees each logit once.  Rows without derivatives get zeros here too. */
 int pg_token_forward_backward(int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t logits_stride,
                               const pg_token_terms *terms, const pg_token_out *out, const pg_token_grads *grads, void *dlogits,
                               int64_t dlogits_stride, void *stream);

@@ -1,25 +1,28 @@
 // Policy update on rows of logits: log-probs of given tokens, entropy, alternatives, divergence from a teacher's list, and their
 // gradient (pg_token_forward / _backward / _forward_backward).
 //
-// Bound: HBM, each logit read once and each gradient written once.  A CTA takes a row, or a part of one, in tiles of eight 16-byte units a
-// thread that lie in registers as they came from memory; as a unit is done with, the next tile's is asked for.  In the base-2 domain,
-// with c = log2(e) / T,
+// Bound: HBM, each logit read once and each gradient written once.  A CTA takes a row, or a part of one, in tiles of eight 16-byte
+// units a thread that lie in registers as they came from memory; as a unit is done with, the next tile's is asked for.  In the base-2
+// domain, with c = log2(e) / T,
 //     y_v = (l_v - m) c,   s0 = sum 2^y,   s1 = sum 2^y y,   m the largest logit that the thread has,
-// so one exponential a logit gives lse = m / T + ln s0 and the entropy ln s0 - ln 2 s1 / s0.  The triples (m, s0, s1) of threads and warps, and
-// of the CTAs of a cluster through each other's shared memory, are joined in a fixed order.
-// The gradient of all terms together is, away from given and listed tokens, e (a + b ln e) with two numbers a row and e a softmax:
-// a second pass over the row.  Of its part the CTA has kept a tile in registers and one in shared memory; the others come back from the L2 cache, which
-// holds them because all else is read and written with the wish to be evicted first.  Given and listed tokens are written over the pass
-// afterwards, one thread each.
+// so one exponential a logit gives lse = m / T + ln s0 and the entropy ln s0 - ln 2 s1 / s0.  The triples (m, s0, s1) of threads and
+// warps, and of the CTAs of a cluster through each other's shared memory, are joined in a fixed order.
+// The gradient of all terms together is, away from given and listed tokens, e (a + b ln e) with two numbers a row and e a softmax: a
+// second pass over the row.  Of its part the CTA has kept a tile in registers and one in shared memory; the others come back from the
+// L2 cache, which holds them because all else is read and written with the wish to be evicted first.  Given and listed tokens are
+// written over the pass afterwards, one thread each.
 // With a bucket for the mass outside a teacher's list that mass is summed by itself (the list's logits are taken out of the registers),
 // since the difference 1 - (list's mass) has no digits left where the list has nearly everything.
-// Alternatives: bounds from the threads' largest logits leave few tiles of few threads to look at again; what passes is ranked by counting.
+// Alternatives: bounds from the threads' largest logits leave few tiles of few threads to look at again; what passes is ranked by
+// counting.
 //
-// Measured (B200; share of the floor at the copy rate, calls back to back): 2368 x 131072 bf16 forward 102 us (93 %), with gradient 222 us (85 %);
-// 2368 x 50001 fp16 50 us (73 %) and 95 us (76 %); 1024 x 131072 backward alone 86 us (95 %).  What is left: the join of a row, about 0.7 us in which its CTA
-// asks for nothing, and rows that are little longer than whole tiles.  Tried and left out: rows kept in the registers or shared memory of clusters (the join
-// of eight CTAs costs more than the second read: 343 and 302 us for 2048 x 131072, not 209), CTAs that stay and ask for their next row ahead (220 us),
-// bulk prefetches into the L2 cache (233 us), five CTAs an SM with smaller tiles (225 to 234 us).
+// Measured (B200; share of the floor at the copy rate, calls back to back): 2368 x 131072 bf16 forward 101 us (94 %), with gradient
+// 219 us (87 %), with a list of 64 237 us, with a bucket besides 264 us; 2368 x 50001 fp16 48 us (75 %) and 92 us (79 %); 1024 x 131072
+// backward alone 86 us (95 %).  What is left: the join of a row, about 0.7 us in which its CTA asks for nothing, longer with a list (one
+// or two warps sum it, the others wait), and rows that are little longer than whole tiles.  Tried and left out: rows kept in the
+// registers or shared memory of clusters (the join of eight CTAs costs more than the second read: 343 and 302 us for 2048 x 131072,
+// not 209), CTAs that stay and ask for their next row ahead (220 us), bulk prefetches into the L2 cache (233 us), five CTAs an SM with
+// smaller tiles (225 to 234 us), listed tokens in a hash table instead of a byte for each unit (1251 x 65536 forward 45 us, not 41).
 #pragma once
 
 #include "pg_kv.cuh"
@@ -34,8 +37,8 @@ namespace pg {
 constexpr int kTokThreads = 256, kTokCtas = 4;  // of a CTA; CTAs of an SM, 64 registers a thread
 constexpr int kPartBytes = 128 * 1024;          // of a row that is read twice; 256 KB: 237 us, not 209 (2048 x 131072 bf16), 64 KB: 251 us
 constexpr int kOnChip = 2;                      // tiles of a part that stay on chip: one in registers, one in shared memory
-constexpr int kSavedBytes = 64 << 20;           // of the logits that pg_token_backward meets first, wanted in the L2 cache when `saved` is asked for:
-                                                // both passes 1251 x 65536 bf16 93.2 us without, 90.2 us at 32 MB, 88.7 us at 64, 88.9 us at 96
+constexpr int kSavedBytes = 64 << 20;           // of the logits, which pg_token_backward meets first, wanted in the L2 cache with `saved`: both
+                                                // passes 1251 x 65536 bf16 92.5 us without; 64 MB 87.6 us, 1 to 2 us more at 32 or 96
 constexpr int kBackwardTiles = 2;               // of a CTA that only writes gradients: its row's numbers serve both (1: 69 us, not 65; 4: 72 us)
 constexpr int kTokWarps = kTokThreads / 32;
 constexpr int kMostParts = 8;                   // CTAs of a cluster
@@ -400,7 +403,7 @@ struct TopShared {
   unsigned int hist[256];
   unsigned long long prefix;
   int count, groups, left, shift;
-  unsigned int group[kMostGroups];                                  // threads' tiles that may hold alternatives: largest logit, tile * kTokThreads + thread
+  unsigned int group[kMostGroups];                                  // tiles of threads: largest logit, tile * kTokThreads + thread
   uint16_t most[kMostTiles * kTokThreads];                          // the largest logit of each thread's tile; as many as there are tiles
 
   __device__ __forceinline__ void push(float x, int id) {
@@ -609,7 +612,8 @@ __device__ __forceinline__ void put_edge(T* to, float x, const TokenSlope& k, fl
   *to = from_float<T>(ex2(y) * fmaf(fmaxf(y, kFloorY), k.b * kLn2, k.a));
 }
 
-// The divergence's derivative to the logits outside the list, over their shares of what is there (pr = p_r, whose logarithm may be far beyond 32 bits).
+// The divergence's derivative to the logits outside the list, over their shares of what is there (pr = p_r, whose logarithm may be far
+// beyond 32 bits).
 __device__ __forceinline__ float rest_slope(const TokenRow& r, int kind, float pr) {
   if (kind == PG_DISTILL_FORWARD_REST) return pr * r.w - expf(r.lt);
   return pr == 0.f ? 0.f : pr * (r.lr - r.lt - r.loss);
@@ -789,7 +793,8 @@ token_kernel(const __grid_constant__ TokenParams p) {
   }
   uint4* const kept = reinterpret_cast<uint4*>(more) + tid;         // a thread's own places: its units of tile 1, those of tile 0 stay in registers
   uint4 raw[kUnits];
-  const uint64_t last_read = keep_policy(!kGrad && p.o.saved && (int64_t)(p.n_rows - row) * p.vocab * (int)sizeof(T) <= kSavedBytes), read_again = keep_policy(true);
+  const bool soon = !kGrad && p.o.saved && (int64_t)(p.n_rows - row) * p.vocab * (int)sizeof(T) <= kSavedBytes;
+  const uint64_t last_read = keep_policy(soon), read_again = keep_policy(true);
   // the part's cut tile first: the last two, that stay here, are whole
   load_tile(at, p.tiles - 1, kGrad && p.tiles > kOnChip ? read_again : last_read, raw);
   const float inv = p.t.temperature ? 1.f / p.t.temperature[row] : 1.f, c = inv * kLog2e;
@@ -1061,9 +1066,8 @@ token_backward_kernel(const __grid_constant__ TokenParams p) {
   constexpr int kUnits = kTokUnits;
   __shared__ TokenShared s;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const unsigned int block = gridDim.x - 1 - blockIdx.x;            // the rows that a forward pass read last are in the L2 cache
-  const int row = block / p.parts;
-  const RowPart<T> at(p, row, block - row * p.parts);
+  const int back = blockIdx.x / p.parts, row = p.n_rows - 1 - back;   // the rows that a forward pass read last are in the L2 cache
+  const RowPart<T> at(p, row, blockIdx.x - back * p.parts);
   const int n_ids = p.g.dlogp ? p.t.n_ids : 0, n_list = p.t.n_teacher;
   const bool distill = p.g.ddistill != nullptr && n_list > 0, rest = distill && p.t.kind != PG_DISTILL_FORWARD;
   const float inv = p.t.temperature ? 1.f / p.t.temperature[row] : 1.f, c = inv * kLog2e;

@@ -91,7 +91,10 @@ token_objective_kernel(const __grid_constant__ ObjectiveParams p) {
     if (start[i] < 0 || start[i] > p.n_tokens || (i < p.n_rows && start[i] > start[i + 1])) flag(p.status, kStatusIndex);
   const int in_rows = start[p.n_rows] - start[0];
   const double lo = 1. - (double)b.clip_low, hi = 1. + (double)b.clip_high;
-  const double scale = b.norm == PG_NORM_ROWS ? (double)b.scale / p.n_rows : b.norm == PG_NORM_SUM ? (double)b.scale : in_rows > 0 ? (double)b.scale / in_rows : 0.;
+  const double scale = b.norm == PG_NORM_ROWS  ? (double)b.scale / p.n_rows
+                       : b.norm == PG_NORM_SUM ? (double)b.scale
+                       : in_rows > 0           ? (double)b.scale / in_rows
+                                               : 0.;
   double sums[kSums] = {};
   for (int chunk = 0; chunk < p.chunks; ++chunk) {
     const int64_t first = ((int64_t)blockIdx.x * p.chunks + chunk) * threads + (threadIdx.x & ~31);   // the warp's first token
