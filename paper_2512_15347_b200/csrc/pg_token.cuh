@@ -38,7 +38,7 @@ constexpr int kTokThreads = 256, kTokCtas = 4;  // of a CTA; CTAs of an SM, 64 r
 constexpr int kPartBytes = 128 * 1024;          // of a row that is read twice; 256 KB: 237 us, not 209 (2048 x 131072 bf16), 64 KB: 251 us
 constexpr int kOnChip = 2;                      // tiles of a part that stay on chip: one in registers, one in shared memory
 constexpr int kSavedBytes = 64 << 20;           // of the logits, which pg_token_backward meets first, wanted in the L2 cache with `saved`: both
-                                                // passes 1251 x 65536 bf16 92.5 us without; 64 MB 87.6 us, 1 to 2 us more at 32 or 96
+                                                // passes 1251 x 65536 bf16 92.5 us without; 64 MB 87.6 us, up to 2 us more at 32 or 96
 constexpr int kBackwardTiles = 2;               // of a CTA that only writes gradients: its row's numbers serve both (1: 69 us, not 65; 4: 72 us)
 constexpr int kTokWarps = kTokThreads / 32;
 constexpr int kMostParts = 8;                   // CTAs of a cluster

@@ -72,6 +72,32 @@ def test_driver_scores_steps_and_checks(kind):
         plain.check()
 
 
+def test_padded_batch_and_no_tokens():
+    from paper_2512_15347_b200.token_update import TokenUpdate, score
+    V, n, used = 5003, 16, 12
+    c = make(n, V, torch.bfloat16, 8, masks=False)
+    c["x"][used:] = math.nan                                       # what lies behind the last row's tokens
+    c["ids"][used + 1:] = -1
+    lists = score(torch.nan_to_num(c["x"]), n_top=10, temperature=c["tau"])
+    c["list_ids"], c["list_logp"] = lists.top_ids, lists.top_logp
+    start = torch.tensor([0, 3, 3, 10, used], device="cuda", dtype=torch.int32)
+    adv = torch.tensor([1.0, 3.0, -0.5, 0.25], device="cuda")
+    old = score(c["x"], c["ids"], temperature=c["tau"]).logp[:, 0].contiguous()
+    rule = TokenUpdate(entropy_coef=0.125, distill_coef=0.5, kind="reverse_rest", norm="tokens")
+    u = rule.step(c["x"], c["ids"].view(-1), start, adv, old, teacher=(lists.top_ids, lists.top_logp), temperature=c["tau"])
+    rule.check()
+    assert (u.dlogits[used:] == 0).all() and (u.weight[used:] == 0).all()
+    f = lambda v: ctypes.c_float(v).value
+    few = {k: v[:used] for k, v in c.items()}
+    cut = u._replace(dlogits=u.dlogits[:used], logp=u.logp[:used], entropy=u.entropy[:used], distill=u.distill[:used], weight=u.weight[:used])
+    check_update(cut, few, adv, old[:used], start, "reverse_rest", dict(clip_low=f(0.2), clip_high=f(0.2), entropy_coef=0.125, distill_coef=0.5,
+                                                                       norm="tokens"))
+    u = rule.step(c["x"][:0], c["ids"].view(-1)[:0], torch.zeros(5, device="cuda", dtype=torch.int32), adv, old[:0],
+                  teacher=(lists.top_ids[:0], lists.top_logp[:0]), temperature=c["tau"][:0])
+    rule.check()
+    assert float(u.objective) == 0 and u.dlogits.shape == (0, V) and (u.stats == 0).all()
+
+
 def test_two_graphs_of_one_driver_run_at_once():
     from paper_2512_15347_b200.token_update import TokenUpdate
     V, n_rows = 4001, 600

@@ -35,7 +35,7 @@ def row_terms(l, tau=1.0, ids=(), list_ids=(), list_logp=(), kind="forward", dlo
             spread.append(0.0)
             continue
         at = int(place[i])
-        logp.append(float(lp[at]) if at >= 0 else -math.inf)
+        logp.append(float(lp[at].detach()) if at >= 0 else -math.inf)
         spread.append(abs(float(l[i]) / tau - top) if at >= 0 else 0.0)
         if at >= 0:
             total = total + w * lp[at]
