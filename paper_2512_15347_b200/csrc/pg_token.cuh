@@ -639,6 +639,22 @@ __device__ __forceinline__ TokenSlope slope_of(const TokenRow& r, bool rest, int
   return k;
 }
 
+// Whether the list has `id` from entry j on, a multiple of 4.
+__device__ __forceinline__ bool on_list(const TokenShared& s, int id, int j, int n_list) {
+  bool on = false;
+#pragma unroll 4
+  for (; j < n_list; j += 4) {
+    const int4 o = *reinterpret_cast<const int4*>(&s.tid[j]);
+    on |= o.x == id || o.y == id || o.z == id || o.w == id;
+  }
+  return on;
+}
+// By whole warps, an entry a lane: whether a later entry of the list has the same id.  Of those the last one counts.
+__device__ __forceinline__ bool again_later(const TokenShared& s, int id, int n_list) {
+  const unsigned int same = __match_any_sync(~0u, id);
+  return (same >> (threadIdx.x & 31) >> 1) != 0u || on_list(s, id, (threadIdx.x | 31) + 1, n_list);
+}
+
 // Given and listed tokens, over what the stream has written.
 template <typename T>
 __device__ __forceinline__ void fix_tokens(const TokenShared& s, const RowPart<T>& at, const Entry& e, const TokenRow& r, T* dl, int n_ids,
@@ -661,8 +677,7 @@ __device__ __forceinline__ void fix_tokens(const TokenShared& s, const RowPart<T
   if (e.id >= 0 && at.owns(e.id)) {
     bool mine = true;                                               // the last of its token, and not on the list
     for (int j = tid + 1; j < n_ids; ++j) mine &= s.gid[j] != e.id;
-    if (fix_list)
-      for (int j = 0; j < n_list; ++j) mine &= s.tid[j] != e.id;
+    if (fix_list) mine &= !on_list(s, e.id, 0, n_list);
     if (mine) {
       const float y = (e.x - r.m) * c - r.l2, pv = ex2(y);
       float sum = base(pv, kLn2 * y);
@@ -673,17 +688,6 @@ __device__ __forceinline__ void fix_tokens(const TokenShared& s, const RowPart<T
       dl[e.id] = from_float<T>(r.some != 0.f ? inv * sum : 0.f);
     }
   }
-}
-
-// Whether a later entry of the list has the same id: of those the last one counts.
-__device__ __forceinline__ bool again_later(const TokenShared& s, int id, int n_list) {
-  const int tid = threadIdx.x;
-  bool later = false;
-  for (int j = tid & ~3; j < n_list; j += 4) {
-    const int4 o = *reinterpret_cast<const int4*>(&s.tid[j]);
-    later |= (o.x == id && j > tid) || (o.y == id && j + 1 > tid) || (o.z == id && j + 2 > tid) || (o.w == id && j + 3 > tid);
-  }
-  return later;
 }
 
 // How the L2 cache is to keep what a load brings: evicted first if it is not read again, so that it does not drive out what is.
@@ -905,7 +909,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
       else __syncwarp();
       if (warp < lists) {
         if (my.tid >= 0) my.tx = to_float(listed_x);
-        if (my.tid >= 0 && again_later(s, my.tid, n_list)) my.tid = -1;
+        if (again_later(s, my.tid, n_list)) my.tid = -1;
         const bool used = my.tid >= 0;
         const float x = used ? my.tx : -INFINITY;
         ListSums l;
@@ -1107,7 +1111,7 @@ token_backward_kernel(const __grid_constant__ TokenParams p) {
     if (lane == 0) s.dsum[warp] = d;
   }
   if (n_ids > 0 || distill) __syncthreads();
-  if (my.tid >= 0 && again_later(s, my.tid, n_list)) my.tid = -1;
+  if (distill && (tid & ~31) < n_list && again_later(s, my.tid, n_list)) my.tid = -1;
   float d = 0.f;
   for (int i = 0; i < (n_ids + 31) / 32; ++i) d += s.dsum[i];
   const float lp_part = -fmaf(dh, r.h, d);
