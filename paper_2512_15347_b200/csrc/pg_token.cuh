@@ -17,7 +17,7 @@
 // counting.
 //
 // Measured (B200; share of the floor at the copy rate, calls back to back): 2368 x 131072 bf16 forward 101 us (94 %), with gradient
-// 219 us (87 %), with a list of 64 237 us, with a bucket besides 264 us; 2368 x 50001 fp16 48 us (75 %) and 92 us (79 %); 1024 x 131072
+// 219 us (87 %), with a list of 64 235 us, with a bucket besides 254 us; 2368 x 50001 fp16 48 us (75 %) and 91 us (79 %); 1024 x 131072
 // backward alone 86 us (95 %).  What is left: the join of a row, about 0.7 us in which its CTA asks for nothing, longer with a list (one
 // or two warps sum it, the others wait), and rows that are little longer than whole tiles.  Tried and left out: rows kept in the
 // registers or shared memory of clusters (the join of eight CTAs costs more than the second read: 343 and 302 us for 2048 x 131072,
