@@ -321,6 +321,29 @@ def test_given_tokens_twice_beside_and_on_the_list():
         check_gradient(c, h, rows)
 
 
+@pytest.mark.parametrize("kind", B.DISTILL_KINDS)
+@pytest.mark.parametrize("n_list,different", [(30, 9), (64, 40), (201, 70), (256, 3)])
+def test_lists_with_the_same_ids_again(kind, n_list, different):
+    R, V = 4, 5003
+    c = make(R, V, torch.float32, 14, n_list=n_list, masks=False)
+    g = torch.Generator(device="cuda").manual_seed(n_list)
+    some = torch.randint(0, V, (different,), generator=g, device="cuda", dtype=torch.int32)
+    c["list_ids"] = some[torch.randint(0, different, (R, n_list), generator=g, device="cuda")].contiguous()
+    c["list_ids"][1, ::3] = -1
+    c["list_logp"] = -math.log(n_list) - torch.rand((R, n_list), generator=g, device="cuda")
+    rows = reference(c, kind)
+    o, both, back = outputs(R, c, 0, True), torch.empty_like(c["x"]), torch.empty_like(c["x"])
+    t, grads = terms_of(c, kind), {k: c[k] for k in ("dlogp", "dentropy", "ddistill")}
+    B.token_forward_backward(c["x"], t, both, **o, **grads)
+    check_forward(c, o, rows)
+    check_gradient(c, both, rows)
+    o = outputs(R, c, 0, True)
+    B.token_forward(c["x"], t, **o)
+    check_forward(c, o, rows)
+    B.token_backward(c["x"], t, o["saved"], back, **grads)
+    check_gradient(c, back, rows)
+
+
 def test_256_given_tokens_and_256_listed():
     R, V = 5, 2000
     c = make(R, V, torch.float32, 6, n_ids=256, n_list=256)
