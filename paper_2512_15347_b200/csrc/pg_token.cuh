@@ -49,6 +49,8 @@ constexpr int kMergeBytes = kMostParts * PG_TOKEN_MAX_TOP * 8;
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr float kFloorY = -1e4f;                // 2^y = 0 long before; keeps 0 * y from being NaN
 constexpr float kHuge = 1e30f;                  // logits from here on (the type's lowest value as a mask) have no l c in 32 bits
+constexpr float kFar = 4194304.f;               // 2^22: below it m c is off by 1/8 at most; from there on (finite masks of any size, a
+                                                // small T) l - m is taken first, or 2^off would leave 32 bits
 
 enum TokenMode { kForward, kBackward, kBoth };
 enum TokenLists { kNoList, kNormalised, kBucket };   // a teacher's list: none, PG_DISTILL_FORWARD, the kinds with a bucket
@@ -742,17 +744,17 @@ __device__ __forceinline__ void slope_tile(const RowPart<T>& at, int tile, uint4
     if (j * kTokThreads < left) store_unit<T>(to + j * kTokThreads * kPer<T>, g);
   }
 }
-// The sums of a tile in registers, against y = l c - r.
-template <typename T, bool kEnt, bool kAsk>
-__device__ __forceinline__ void sum_tile(uint4 (&raw)[kTokUnits], float c, float r, float& t0, float& t1, const T* from, uint64_t policy) {
-  const f2 nr = make2(-r, -r), c2 = make2(c, c);
+// The sums of a tile in registers, against y = l c - by; kFirst: y = (l - by) c, differences first.
+template <typename T, bool kEnt, bool kAsk, bool kFirst>
+__device__ __forceinline__ void sum_tile(uint4 (&raw)[kTokUnits], float c, float by, float& t0, float& t1, const T* from, uint64_t policy) {
+  const f2 nr = make2(-by, -by), c2 = make2(c, c);
   f2 a0 = make2(0.f, 0.f), a1 = a0, b0 = a0, b1 = a0;
 #pragma unroll
   for (int j = 0; j < kTokUnits; ++j) {
 #pragma unroll
     for (int i = 0; i < kPer<T> / 2; ++i) {
       float y0, y1;
-      split2(fma2(pair_of<T>(raw[j], i), c2, nr), y0, y1);
+      split2(kFirst ? mul2(add2(pair_of<T>(raw[j], i), nr), c2) : fma2(pair_of<T>(raw[j], i), c2, nr), y0, y1);
       const f2 e = make2(ex2(y0), ex2(y1));
       if (i & 1) b0 = add2(b0, e);
       else a0 = add2(a0, e);
@@ -776,7 +778,7 @@ template <typename T, bool kGrad, bool kEnt, int kLists>
 __global__ void __launch_bounds__(kTokThreads, kTokCtas)
 token_kernel(const __grid_constant__ TokenParams p) {
   constexpr bool kRest = kLists == kBucket;
-  constexpr int kUnits = kTokUnits, kTile = kTileUnits;
+  constexpr int kUnits = kTokUnits;
   __shared__ TokenShared s;
   extern __shared__ __align__(16) unsigned char more[];             // a tile; TopShared and the parts' lists if there are alternatives; bits (kRest)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -859,18 +861,6 @@ token_kernel(const __grid_constant__ TokenParams p) {
       }
     }
   };
-  // The thread's units of a tile whose logits are all that far down, from memory: differences first.
-  auto sum_huge = [&](const RowPart<T>& at, const uint8_t* bits, float m, float c, int tile, float& s0, float& s1) {
-    for (int u = tile * kTile + tid; u < (tile + 1) * kTile && at.first + u < at.last; u += kTokThreads) {
-      for (int k = 0; k < kPer<T>; ++k) {
-        if (kRest && bits[bits_at(u)] >> k & 1) continue;
-        const float y = (to_float(at.in[at.head + (at.first + u) * kPer<T> + k]) - m) * c, e = ex2(y);
-        s0 += e;
-        s1 += e * fmaxf(y, kFloorY);
-      }
-    }
-  };
-
   const int lists_at = max(p.tiles - (kGrad ? 1 : 2), 0);           // the listed tokens' logits were asked for a tile before
   float m = -INFINITY, s0 = 0.f, s1 = 0.f, edge_left = -INFINITY;
   for (int tile = p.tiles - 1; tile >= 0; --tile) {
@@ -886,20 +876,23 @@ token_kernel(const __grid_constant__ TokenParams p) {
     const float tm = max_of<T>(w);
     refer(m, fmaxf(m, tm), c, s0, s1);
     m = fmaxf(m, tm);
-    bool asked = false;
-    if (fabsf(m) > kHuge && fabsf(m) < INFINITY) {
-      sum_huge(at, bits, m, c, tile, s0, s1);
+    const float ref = finite_ref(m), r = ref * c;
+    float t0, t1;
+    // as a unit is done with, the next tile's is asked for
+    const bool ask = tile > 0 && whole_tile(at, tile - 1);
+    const uint64_t policy = kGrad && tile > kOnChip ? read_again : last_read;
+    // By warps: a mask's few allowed tokens lie in few threads, and one path is cheaper than two.  Both cost the same where HBM is the
+    // bound (2368 x 131072 bf16, all but 64 tokens masked: 97 us as without a mask).
+    if (__any_sync(~0u, !(fabsf(r) < kFar))) {
+      if (ask) sum_tile<T, kEnt, true, true>(raw, c, ref, t0, t1, tile_at(at, tile - 1), policy);
+      else sum_tile<T, kEnt, false, true>(raw, c, ref, t0, t1, nullptr, 0);
+      s0 += t0;
+      if (kEnt) s1 += t1;
     } else {
       // y = l c - r in one rounding; what r = m c rounded is off by is taken back from the sums
-      const float ref = finite_ref(m), r = ref * c, off = fmaf(ref, c, -r);
-      // as a unit is done with, the next tile's is asked for
-      const bool ask = tile > 0 && whole_tile(at, tile - 1);
-      const uint64_t policy = kGrad && tile > kOnChip ? read_again : last_read;
-      float t0, t1;
-      if (ask) sum_tile<T, kEnt, true>(raw, c, r, t0, t1, tile_at(at, tile - 1), policy);
-      else sum_tile<T, kEnt, false>(raw, c, r, t0, t1, nullptr, 0);
-      asked = ask;
-      const float f = ex2(-off);
+      const float off = fmaf(ref, c, -r), f = ex2(-off);
+      if (ask) sum_tile<T, kEnt, true, false>(raw, c, r, t0, t1, tile_at(at, tile - 1), policy);
+      else sum_tile<T, kEnt, false, false>(raw, c, r, t0, t1, nullptr, 0);
       s0 += f * t0;
       if (kEnt) s1 += f * fmaf(-off, t0, t1);
     }
@@ -927,7 +920,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
         if (lane == 0) s.list[warp] = l;
       }
     }
-    if (tile > 0 && !asked) load_tile(at, tile - 1, kGrad && tile > kOnChip ? read_again : last_read, raw);
+    if (tile > 0 && !ask) load_tile(at, tile - 1, policy, raw);
   }
   if (at.edges > 0) {
     const float x = kRest && tid < at.edges && s.edges >> tid & 1 ? -INFINITY : edge_x;
