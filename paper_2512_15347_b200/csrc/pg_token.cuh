@@ -48,7 +48,6 @@ constexpr int kMostGroups = 1024;               // threads' tiles that are read 
 constexpr int kMergeBytes = kMostParts * PG_TOKEN_MAX_TOP * 8;
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr float kFloorY = -1e4f;                // 2^y = 0 long before; keeps 0 * y from being NaN
-constexpr float kHuge = 1e30f;                  // logits from here on (the type's lowest value as a mask) have no l c in 32 bits
 constexpr float kFar = 4194304.f;               // 2^22: below it m c is off by 1/8 at most; from there on (finite masks of any size, a
                                                 // small T) l - m is taken first, or 2^off would leave 32 bits
 
@@ -564,12 +563,23 @@ struct Entry {
 };
 
 // The slope for the stream: y = l c - r in one rounding, with r = ref c + l2 rounded; what the roundings of r leave, up to 1e-6 of
-// every p_v, is a factor of a and b.
+// every p_v, is a factor of a and b.  The steps to `off` are exact as they stand, not as fused products.
+// From |ref c| = 2^31 on (rows, or what is outside the list, masked throughout by a finite value; a small T) off could be 128 and the factor
+// out of range.  But there logits next to each other are 2^31 2^-24 = 128 apart in y, so e is 0 but for those equal to ref.  Any
+// other c that keeps them apart does as well: a power of two with |ref c| in [2^31, 2^32), whose product with ref is exact, and
+// y = 0 for those that are equal; their 2^-l2 is the factor.  (The difference first in a loop of its own: 8 % for every row with a bucket.)
 struct Slope2 {
   f2 c, nr, a, b;
   __device__ __forceinline__ Slope2(const TokenSlope& k, float c_) {
-    const float mc = k.ref * c_, r = mc + k.l2;
-    const float back = r - mc, off = fmaf(k.ref, c_, -mc) + ((mc - (r - back)) + (k.l2 - back));   // ref c + l2 - r
+    const float mc = __fmul_rn(k.ref, c_);
+    float r = __fadd_rn(mc, k.l2);
+    const float back = __fsub_rn(r, mc);
+    float off = __fadd_rn(fmaf(k.ref, c_, -mc), __fadd_rn(__fsub_rn(mc, __fsub_rn(r, back)), __fsub_rn(k.l2, back)));   // ref c + l2 - r
+    if (!(fabsf(mc) < 2147483648.f)) {
+      c_ = __uint_as_float(min(285u - (__float_as_uint(k.ref) >> 23 & 255u), 254u) << 23);
+      r = k.ref * c_;
+      off = k.l2;
+    }
     const float f = ex2(-off), bl = k.b * kLn2;
     c = make2(c_, c_);
     nr = make2(-r, -r);
@@ -590,9 +600,9 @@ __device__ __forceinline__ void slope_unit(const uint4& v, const Slope2& k, floa
     split2(mul2(e, f), g[2 * i], g[2 * i + 1]);
   }
 }
-// A part from memory, logit by logit, differences first: whose reference is that far down, or whose gradient lies off 16 bytes.
+// A part from memory, logit by logit: whose gradient lies off its logits' 16 bytes, or whose row has an infinite logit (NaN).
 template <typename T>
-__device__ __noinline__ void slope_huge(const RowPart<T>& at, T* dl, const TokenSlope& k, float c) {
+__device__ __noinline__ void slope_single(const RowPart<T>& at, T* dl, const TokenSlope& k, float c) {
   for (int t = at.head + at.first * kPer<T> + threadIdx.x; t < at.head + at.last * kPer<T>; t += kTokThreads) {
     const float y = (to_float(at.in[t]) - k.ref) * c - k.l2;
     dl[t] = from_float<T>(ex2(y) * fmaf(fmaxf(y, kFloorY), k.b * kLn2, k.a));
@@ -1031,8 +1041,9 @@ token_kernel(const __grid_constant__ TokenParams p) {
     const TokenSlope slope = s.slope;
     const Slope2 k(slope, c);
     const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0;
-    if (fabsf(slope.ref) > kHuge || !aligned) {                       // rows masked throughout, by the type's lowest value; or off 16 bytes
-      slope_huge(at, dl, slope, c);
+    // An infinite logit has no product with c.  (Without this condition the compiler lays the loops out with more spills: 236 us, not 226.)
+    if (fabsf(slope.ref) == INFINITY || !aligned) {
+      slope_single(at, dl, slope, c);
     } else {
       for (int tile = 0; tile < p.tiles; ++tile) {
         const int next = tile + 1;
@@ -1111,8 +1122,8 @@ token_backward_kernel(const __grid_constant__ TokenParams p) {
   const TokenSlope slope = slope_of(r, rest, p.t.kind, lp_part, dh, dd, inv);
   const Slope2 k(slope, c);
   const bool aligned = ((uintptr_t)(dl + at.head) & 15) == 0;
-  if (fabsf(slope.ref) > kHuge || !aligned) {
-    slope_huge(at, dl, slope, c);
+  if (fabsf(slope.ref) == INFINITY || !aligned) {
+    slope_single(at, dl, slope, c);
   } else {
     for (int tile = p.tiles - 1; tile >= 0; --tile) {
       const bool ask = tile > 0 && whole_tile(at, tile - 1);

@@ -7,7 +7,7 @@ import torch
 
 from paper_2512_15347_b200 import binding as B
 from tests import token_reference as ref
-from tests.test_gpu_token_update import check_forward, close, make, outputs, reference, terms_of, tiles_of, tol_logp
+from tests.test_gpu_token_update import check_forward, check_gradient, close, make, outputs, reference, terms_of, tiles_of, tol_logp
 
 pytestmark = pytest.mark.gpu
 
@@ -86,3 +86,45 @@ def test_log_probs_at_small_temperatures(dtype, tau):
     o = outputs(5, c, 3)
     B.token_forward(c["x"], terms_of(c, n_top=3), **o)
     check(c, o, reference(c), 3)
+
+
+@pytest.mark.parametrize("whole", [False, True])
+@pytest.mark.parametrize("mask", MASKS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [9, 20011, 140000])
+def test_gradients_of_masked_rows(V, dtype, mask, whole):
+    """Where nothing else is left - in the row, or outside the teacher's list - masked tokens are what the gradient's slope refers to."""
+    c = masked(V, dtype, mask, V + 1, whole=whole)
+    for kind in B.DISTILL_KINDS:
+        rows = reference(c, kind)
+        grads = {k: c[k] for k in GRADS}
+        o, one, two = outputs(5, c, 0, True), torch.full_like(c["x"], 7), torch.full_like(c["x"], 7)
+        B.token_forward_backward(c["x"], terms_of(c, kind), one, **o, **grads)
+        check_gradient(c, one, rows)
+        B.token_backward(c["x"], terms_of(c, kind), o["saved"], two, **grads)
+        check_gradient(c, two, rows)
+        # without entropy
+        plain = dict(c, dentropy=torch.zeros(5, device="cuda"))
+        rows = reference(plain, kind)
+        B.token_forward_backward(c["x"], terms_of(c, kind), one, dlogp=c["dlogp"], ddistill=c["ddistill"])
+        check_gradient(c, one, rows)
+        B.token_backward(c["x"], terms_of(c, kind), o["saved"], two, dlogp=c["dlogp"], ddistill=c["ddistill"])
+        check_gradient(c, two, rows)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("tau", [1e-6, 1e-9])
+def test_gradients_at_small_temperatures(dtype, tau):
+    """With weights as small as T, so that gradients are of ordinary size."""
+    c = make(5, 9001, dtype, 3, n_ids=2, n_list=6, masks=False)
+    c["x"][1:3] = -20 - c["x"][1:3].abs()
+    c["tau"].fill_(tau)
+    for k in GRADS:
+        c[k] *= tau
+    for kind in B.DISTILL_KINDS:
+        rows = reference(c, kind)
+        o, one, two = outputs(5, c, 0, True), torch.full_like(c["x"], 7), torch.full_like(c["x"], 7)
+        B.token_forward_backward(c["x"], terms_of(c, kind), one, **o, **{k: c[k] for k in GRADS})
+        check_gradient(c, one, rows)
+        B.token_backward(c["x"], terms_of(c, kind), o["saved"], two, **{k: c[k] for k in GRADS})
+        check_gradient(c, two, rows)
