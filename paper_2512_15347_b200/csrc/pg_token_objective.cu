@@ -41,15 +41,19 @@ __device__ __forceinline__ double second_part(double r) {
   q = fma(q, r, 1. / 6.);
   return fma(q, r, .5);
 }
-// exp(x), and exp(x) - x - 1 in *rest.  Outside +-87 both are 0 or infinite in 32 bits or near it, and so they are from +-700 on.
-__device__ __forceinline__ double exp_rest(double x, double* rest) {
+// exp(x); exp(x) - x - 1 in *rest and exp(x) - 1 in *less, each of its own: from the other by x they would lose all digits where x is far
+// from 0.  Outside +-87 exp(x) is 0 or infinite in 32 bits or near it, and so it is from +-700 on.
+__device__ __forceinline__ double exp_rest(double x, double* rest, double* less) {
   const float f = (float)x;
   const float n = rintf(fminf(fmaxf(f, -700.f), 700.f) * 1.44269504f);
   const double r = fma((double)n, -0.693147180559945309417, x);         // off by n 2.3e-17
   const double k = second_part(r) * r * r;
   double y = (1. + (r + k)) * __hiloint2double((1023 + (int)n) << 20, 0);
   if (fabsf(f) > 700.f) y = f > 0.f ? INFINITY : 0.;
-  if (rest) *rest = n == 0.f ? k : y - x - 1.;
+  if (rest) {
+    *rest = n == 0.f ? k : f > 700.f ? INFINITY : y - x - 1.;
+    *less = n == 0.f ? k + r : y - 1.;
+  }
   return y;
 }
 // 1 / n for a whole number n >= 1.
@@ -134,17 +138,17 @@ token_objective_kernel(const __grid_constant__ ObjectiveParams p) {
     const double a = b.adv[row];
     double w = scale;
     if (b.norm == PG_NORM_ROWS) w *= reciprocal(to - from);
-    const double r = b.logp_old ? exp_rest((double)fresh - (double)old, nullptr) : 1.;
+    const double r = b.logp_old ? exp_rest((double)fresh - (double)old, nullptr, nullptr) : 1.;
     const double free = r * a, held = (r < lo ? lo : r > hi ? hi : r) * a;
     const bool clipped = held < free;
     double g = clipped ? 0. : free;
     sums[0] += w * (clipped ? held : free);
     if (b.logp_ref) {
       const double d = (double)ref - (double)fresh;
-      double kl;
-      exp_rest(d, &kl);
+      double kl, slope;
+      exp_rest(d, &kl, &slope);
       sums[1] += w * kl;
-      g += (double)b.beta * (kl + d);
+      if (b.beta != 0.f) g += (double)b.beta * slope;         // a reference that is only watched may be infinitely far
     }
     sums[2] += w * (double)ent;
     sums[3] += w * (double)div;
