@@ -715,6 +715,7 @@ int pg_token_forward_backward(int32_t n_rows, int32_t vocab, int32_t dtype, cons
  * pg_token_backward.  Evaluated in fp64 from the fp32 inputs, sums in a fixed order.  Empty rows add nothing; tokens that
  * belong to no row get dlogp, weight 0 and ratio 1, and their inputs are not read.
  * stats: the weighted sums of surr, kl, entropy and distill, and the share of the rows' tokens that are clipped.
+ * A term whose coefficient (beta, entropy_coef, distill_coef) is 0 is watched in stats and enters nothing else, whatever it is.
  */
 #define PG_NORM_ROWS   0
 #define PG_NORM_TOKENS 1

@@ -178,7 +178,12 @@ token_objective_kernel(const __grid_constant__ ObjectiveParams p) {
     if (threadIdx.x == 0) *p.ticket = 0u;                     // ready for the next call
   }
   if (threadIdx.x == 0) {
-    p.objective[0] = (float)(sums[0] - (double)b.beta * sums[1] + (double)b.entropy_coef * sums[2] - (double)b.distill_coef * sums[3]);
+    // a term without weight is left out: what is only watched may be infinite
+    double j = sums[0];
+    if (b.beta != 0.f) j -= (double)b.beta * sums[1];
+    if (b.entropy_coef != 0.f) j += (double)b.entropy_coef * sums[2];
+    if (b.distill_coef != 0.f) j -= (double)b.distill_coef * sums[3];
+    p.objective[0] = (float)j;
     if (p.stats) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) p.stats[k] = (float)sums[k];

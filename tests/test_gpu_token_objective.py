@@ -119,3 +119,37 @@ def test_an_update_step_against_a_reference_that_masks_tokens():
         w = dict(c, dlogp=torch.tensor(dlogp, device="cuda", dtype=torch.float64)[:, None], dentropy=torch.zeros(n, device="cuda"))
         check_gradient(w, u.dlogits, reference(w, entropy=False))
         assert bool(torch.isfinite(u.dlogits).all())
+
+
+@pytest.mark.parametrize("term", ["distill", "entropy", "logp_ref"])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_a_term_without_weight_is_not_in_the_objective(term, bad):
+    """Watched beside the objective: the divergence from a teacher of whose tokens the policy masks one is infinite."""
+    new, old = [-1.0, -2.0, -0.5], [-1.1, -1.8, -0.5]
+    kw = dict(entropy=[1.0, 2.0, 3.0], distill=[0.5, 0.25, 2.0], logp_ref=[-1.2, -2.0, -0.25])
+    coef = dict(entropy="entropy_coef", distill="distill_coef", logp_ref="beta")
+    use = dict(entropy_coef=0.01, distill_coef=0.5, beta=0.1)
+    use[coef[term]] = 0.0
+    kw[term] = [kw[term][0], bad, kw[term][2]]
+    o = run(new, 1.5, logp_old=old, **kw, **use)
+    terms, dlogp, _ = objective(new, 1.5, old=[F32(v) for v in old], ref=[F32(v) for v in kw["logp_ref"]], entropy=kw["entropy"], distill=kw["distill"], **use)
+    near(o["objective"][0], sum(terms), term, 1e-10 + U * sum(map(abs, terms)))
+    for j in range(3):
+        near(o["dlogp"][j], dlogp[j], (term, j), 1e-10)
+    at = dict(distill=3, entropy=2, logp_ref=1)[term]
+    assert not math.isfinite(o["stats"][at])                 # what was watched is still told
+    # with weight it is in there
+    use[coef[term]] = 0.25
+    assert not math.isfinite(run(new, 1.5, logp_old=old, **kw, **use)["objective"][0])
+
+
+def test_an_update_step_watches_an_infinite_divergence():
+    from paper_2512_15347_b200.token_update import TokenUpdate
+    n, V = 5, 1000
+    c = make(n, V, torch.float32, 4, n_list=8, masks=False)
+    c["x"][2, int(c["list_ids"][2, 0])] = -math.inf
+    c["ids"][2] = int(c["list_ids"][2, 1])
+    start, adv = torch.tensor([0, n], device="cuda", dtype=torch.int32), torch.tensor([0.5], device="cuda")
+    u = TokenUpdate(norm="tokens").step(c["x"], c["ids"].view(-1), start, adv, teacher=(c["list_ids"], c["list_logp"]), temperature=c["tau"])
+    assert float(u.distill[2]) == math.inf and float(u.stats[3]) == math.inf
+    assert abs(float(u.objective) - 0.5) <= U * 0.5 + 1e-9 and bool(torch.isfinite(u.dlogits).all())
