@@ -139,7 +139,8 @@ token_objective_kernel(const __grid_constant__ ObjectiveParams p) {
     double w = scale;
     if (b.norm == PG_NORM_ROWS) w *= reciprocal(to - from);
     const double r = b.logp_old ? exp_rest((double)fresh - (double)old, nullptr, nullptr) : 1.;
-    const double free = r * a, held = (r < lo ? lo : r > hi ? hi : r) * a;
+    const double free = a == 0. && r == INFINITY ? 0. : r * a;      // e^x times 0 for any x, also where e^x has no number
+    const double held = (r < lo ? lo : r > hi ? hi : r) * a;
     const bool clipped = held < free;
     double g = clipped ? 0. : free;
     sums[0] += w * (clipped ? held : free);

@@ -153,3 +153,20 @@ def test_an_update_step_watches_an_infinite_divergence():
     u = TokenUpdate(norm="tokens").step(c["x"], c["ids"].view(-1), start, adv, teacher=(c["list_ids"], c["list_logp"]), temperature=c["tau"])
     assert float(u.distill[2]) == math.inf and float(u.stats[3]) == math.inf
     assert abs(float(u.objective) - 0.5) <= U * 0.5 + 1e-9 and bool(torch.isfinite(u.dlogits).all())
+
+
+@pytest.mark.parametrize("adv", [0.0, -0.0, 1.5, -2.0])
+def test_ratios_beyond_all_numbers(adv):
+    """A rollout's log-prob far below the policy's.  No advantage times a ratio of any size is 0, as it is for one of e^700."""
+    new = [-1.0] * len(DIFFERENCES)
+    for sign in (1, -1):
+        for d in DIFFERENCES:
+            old = F32(-1.0 - sign * d)
+            o = run([-1.0], adv, logp_old=[old])
+            terms, dlogp, ratio = objective([-1.0], adv, old=[old])
+            for name, want in (("objective", terms), ("dlogp", dlogp), ("ratio", ratio)):
+                near(o[name][0], want[0], (name, sign * d))
+    # what is no number stays none
+    for old, a in ((math.nan, adv), (-1.0, math.nan)):
+        o = run([-1.0], a, logp_old=[old])
+        assert math.isnan(o["objective"][0]) and math.isnan(o["dlogp"][0])
