@@ -47,6 +47,8 @@ constexpr int kMostTiles = 16;                  // of a part with alternatives
 constexpr int kMostGroups = 1024;               // threads' tiles that are read again for them
 constexpr int kMergeBytes = kMostParts * PG_TOKEN_MAX_TOP * 8;
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
+constexpr float kMean = 1.f / (2 * PG_TOKEN_MAX_LIST);   // of sums over a list whose mean is wanted: log-probs near the type's end, of masked tokens,
+                                                // do not pass it on the way
 constexpr float kFloorY = -1e4f;                // 2^y = 0 long before; keeps 0 * y from being NaN
 constexpr float kFar = 4194304.f;               // 2^22: below it m c is off by 1/8 at most; from there on (finite masks of any size, a
                                                 // small T) l - m is taken first, or 2^off would leave 32 bits
@@ -80,7 +82,7 @@ struct TokenSlope {
 // Sums over a warp's share of a teacher's list.  Reference of e: the largest logit m among them; of t: `tm` (FORWARD), else 0.
 struct ListSums {
   float m, s0, s1, etl;                         // sum e, e y, e tl
-  float tm, ts, ttl, ty;                        // sum t, t (tl - tm), t (l - m) / T
+  float tm, ts, ttl, ty;                        // sum t, t (tl - tm), kMean t (l - m) / T
   double mass;                                  // sum t (the kinds with a bucket)
 };
 
@@ -311,7 +313,7 @@ __device__ __forceinline__ TokenRow finish_row(const TokenShared& s, const float
       const float f = expf(l.tm - tm);
       z = f * l.ts;
       ttl = f * (l.ttl + l.ts * (l.tm - tm));
-      tlp = f * (l.ty + l.ts * ((finite_ref(l.m) - r.m) * inv - kLn2 * r.l2));
+      tlp = f * (l.ty + kMean * l.ts * (finite_ref(l.m) - r.m) * inv - kMean * l.ts * (kLn2 * r.l2));
     }
     z = warp_total(z);
     ttl = warp_total(ttl);
@@ -322,7 +324,7 @@ __device__ __forceinline__ TokenRow finish_row(const TokenShared& s, const float
     }
     r.lt = tm + logf(z);
     r.w = 1.f;
-    r.loss = ttl / z - logf(z) - tlp / z;
+    r.loss = ttl / z - logf(z) - tlp / z / kMean;
     return r;
   }
   const double mass = warp_total(l.mass);
@@ -331,7 +333,7 @@ __device__ __forceinline__ TokenRow finish_row(const TokenShared& s, const float
   r.w = (float)(outside ? mass + tr : mass);
   if (mass != mass) r.lt = r.w = NAN;
   if (kind == PG_DISTILL_FORWARD_REST) {
-    const float tlp = warp_total(l.ts != 0.f ? l.ty + l.ts * ((finite_ref(l.m) - r.m) * inv - kLn2 * r.l2) : 0.f);
+    const float tlp = warp_total(l.ts != 0.f ? l.ty + kMean * l.ts * (finite_ref(l.m) - r.m) * inv - kMean * l.ts * (kLn2 * r.l2) : 0.f) / kMean;
     r.loss = warp_total(l.ttl) - tlp + (outside ? r.lr > -1e30f ? (float)tr * (r.lt - r.lr) : (float)(tr * (r.lt - lr)) : 0.f);
   } else {
     float plp = 0.f, ptl = 0.f;
@@ -925,7 +927,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
         const float t = used ? expf(my.tl - finite_ref(l.tm)) : 0.f;
         l.ts = warp_total(t);
         l.ttl = warp_total(t != 0.f ? t * (my.tl - finite_ref(l.tm)) : 0.f);
-        l.ty = warp_total(t != 0.f ? t * (x - finite_ref(l.m)) * inv : 0.f);
+        l.ty = warp_total(t != 0.f ? kMean * t * (x - finite_ref(l.m)) * inv : 0.f);
         l.mass = kRest ? warp_total(used ? exp((double)my.tl) : 0.) : 0.;
         if (lane == 0) s.list[warp] = l;
       }
