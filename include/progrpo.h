@@ -694,6 +694,8 @@ int pg_token_forward(int32_t n_rows, int32_t vocab, int32_t dtype, const void *l
  * of dtype, rounded once.  dlogits has the logits' shape, rows dlogits_stride elements apart; it may be logits when the
  * strides agree (no other overlap).  terms and saved are those of pg_token_forward on the same logits (n_top plays no part).
  * Rows whose derivatives are all zero get zeros, whatever they hold, and are not read.
+ * A row whose gradient begins on another offset from 16 bytes than its logits is read and written element by element, which takes up to
+ * five times as long: give the gradient of a padded vocabulary's slice the logits' row stride, or one that differs by whole 16 bytes.
  */
 int pg_token_backward(int32_t n_rows, int32_t vocab, int32_t dtype, const void *logits, int64_t logits_stride,
                       const pg_token_terms *terms, const float *saved, const pg_token_grads *grads, void *dlogits,

@@ -44,6 +44,18 @@ def score(logits, ids=None, *, n_top: int = 0, temperature=None) -> Scores:
     return Scores(logp, entropy, *top)
 
 
+def _gradient_room(logits) -> torch.Tensor:
+    """Room for the gradient of logits [rows, vocab], contiguous where the logits' rows allow it.  Rows lie on the 16-byte offsets of the logits' rows, so
+    that the kernels write whole units: of a padded vocabulary's slice each row is up to 15 bytes longer, not as long as the padded one."""
+    rows, vocab = logits.shape
+    size = logits.element_size()
+    first = logits.data_ptr() % 16 // size
+    pitch = vocab + ((logits.stride(0) - vocab) % (16 // size) if rows > 1 else 0)
+    if first == 0 and pitch == vocab:
+        return torch.empty((rows, vocab), device=logits.device, dtype=logits.dtype)
+    return torch.empty(first + rows * pitch, device=logits.device, dtype=logits.dtype).as_strided((rows, vocab), (pitch, 1), first)
+
+
 class TokenUpdate:
     """The settings of an objective (see pg_token_objective) and what its calls need besides: workspaces, a status word.
 
@@ -77,7 +89,8 @@ class TokenUpdate:
              temperature=None, scale: float = 1.0, dlogits=None) -> Update:
         """One step on packed tokens: logits [tokens, vocab] of the positions that made ids [tokens], rows of tokens by start [rows + 1], their
         advantages adv [rows]; logp_old, logp_ref [tokens] log-probs of the rollout (None: this policy's own) and of a reference; teacher
-        (ids, log-probs) [tokens, n] as ``score`` gives them, for distill_coef; dlogits (may be logits) receives the gradient."""
+        (ids, log-probs) [tokens, n] as ``score`` gives them, for distill_coef; dlogits (may be logits) receives the gradient, soonest where its
+        rows lie on the 16-byte offsets of the logits' rows.  Without it the gradient lies so, contiguous where contiguous rows do."""
         n, dev = logits.shape[0], logits.device
         if self.distill_coef and teacher is None:
             raise ValueError("distill_coef without a teacher's lists")
@@ -90,8 +103,8 @@ class TokenUpdate:
         logp, entropy, dlogp, weight = (torch.empty(n, device=dev) for _ in range(4))
         distill = torch.empty(n, device=dev) if teacher is not None else None
         saved, objective, stats = torch.empty((n, B.TOKEN_SAVED), device=dev), torch.empty(1, device=dev), torch.empty(B.TOKEN_STATS, device=dev)
-        dlogits = torch.empty_like(logits) if dlogits is None else dlogits
         B.token_forward(logits, terms, logp=logp, entropy=entropy, distill=distill, saved=saved)
+        dlogits = _gradient_room(logits) if dlogits is None else dlogits
         B.token_objective(start, logp, adv, objective, dlogp, self._space(B.token_objective_workspace_bytes(n)), logp_old=logp_old,
                           logp_ref=logp_ref, entropy=entropy, distill=distill, entropy_coef=self.entropy_coef, distill_coef=self.distill_coef,
                           scale=scale, weight=weight, stats=stats, status=self.status, **self._rule)
