@@ -59,7 +59,16 @@ class PreviewCoef(ctypes.Structure):
     _fields_ = [("p_x", ctypes.c_double), ("p_v", ctypes.c_double)]
 
 
-class Kv(ctypes.Structure):
+class Described(ctypes.Structure):
+    """A descriptor that holds the tensors it points to.  Its reference is made anew each time: kept in the descriptor it would be a cycle,
+    and the tensors would stay until the garbage collector runs."""
+
+    @property
+    def _ref(self):
+        return ctypes.byref(self)
+
+
+class Kv(Described):
     """Descriptor of a paged key-value cache (``make_kv``)."""
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int32),
                 ("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
@@ -68,7 +77,7 @@ class Kv(ctypes.Structure):
                 ("n_rows", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("grown", ctypes.c_void_p)]
 
 
-class LogitsRules(ctypes.Structure):
+class LogitsRules(Described):
     """Sampling rules (``make_logits_rules``)."""
     _fields_ = [("tokens", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("max_tokens", ctypes.c_int32),
                 ("n_tokens", ctypes.c_void_p), ("n_prompt", ctypes.c_void_p), ("repetition", ctypes.c_void_p),
@@ -77,7 +86,7 @@ class LogitsRules(ctypes.Structure):
                 ("mask", ctypes.c_void_p), ("mask_stride", ctypes.c_int64)]
 
 
-class TokenTerms(ctypes.Structure):
+class TokenTerms(Described):
     """What rows of logits are asked about (``make_token_terms``)."""
     _fields_ = [("temperature", ctypes.c_void_p), ("ids", ctypes.c_void_p), ("n_ids", ctypes.c_int32), ("n_top", ctypes.c_int32),
                 ("teacher_ids", ctypes.c_void_p), ("teacher_logp", ctypes.c_void_p), ("n_teacher", ctypes.c_int32),
@@ -535,7 +544,6 @@ def make_kv(k, v, table, length, grown=None) -> Kv:
            _i32(table, "table", dev=dev), _i32(length, "length", dev=dev), table.shape[0], table.shape[1],
            _i32(grown, "grown", table.shape[0], dev))
     c._keepalive = (k, v, table, length, grown)
-    c._ref = ctypes.byref(c)
     c._plain = (k.dtype, table.shape[0], heads, dim, n_pages, table.shape[1], dev)   # plain values, cheaper to read than the fields
     return c
 
@@ -698,7 +706,6 @@ def make_logits_rules(*, tokens=None, n_tokens=None, n_prompt=None, repetition=N
         r.mask, r.mask_stride = mask.data_ptr(), mask.stride(0) if mask.shape[0] > 1 else 0
     r._rows, r._mask_words, r._dev = rows, None if mask is None else mask.shape[1], dev
     r._keepalive = (tokens, n_tokens, n_prompt, repetition, presence, frequency, temperature, bias_ids, bias_values, mask)
-    r._ref = ctypes.byref(r)
     return r
 
 
@@ -782,7 +789,6 @@ def make_token_terms(*, temperature=None, ids=None, n_top: int = 0, teacher_ids=
     r.n_top, r.kind = n_top, DISTILL_KINDS.index(kind)
     r._plain = (rows, dev, n_ids, n_top, n_teacher)
     r._keepalive = (temperature, ids, teacher_ids, teacher_logp)
-    r._ref = ctypes.byref(r)
     return r
 
 
