@@ -11,6 +11,10 @@ import torch
 from . import binding as B
 
 
+def _empty(dev, *shape) -> torch.Tensor:
+    return torch.empty(shape, device=dev, dtype=torch.float32)
+
+
 class Scores(NamedTuple):
     """Of rows of logits: logp [rows, given tokens] or None, entropy [rows], top_ids / top_logp [rows, n_top] or None."""
     logp: Optional[torch.Tensor]
@@ -37,9 +41,9 @@ def score(logits, ids=None, *, n_top: int = 0, temperature=None) -> Scores:
     rows, dev = logits.shape[0], logits.device
     terms = B.make_token_terms(temperature=temperature, ids=ids, n_top=n_top)
     n_ids = terms._plain[2]
-    logp = torch.empty((rows, n_ids), device=dev) if n_ids else None
-    entropy = torch.empty(rows, device=dev)
-    top = (torch.empty((rows, n_top), device=dev, dtype=torch.int32), torch.empty((rows, n_top), device=dev)) if n_top else (None, None)
+    logp = _empty(dev, rows, n_ids) if n_ids else None
+    entropy = _empty(dev, rows)
+    top = (torch.empty((rows, n_top), device=dev, dtype=torch.int32), _empty(dev, rows, n_top)) if n_top else (None, None)
     B.token_forward(logits, terms, logp=logp, entropy=entropy, top_ids=top[0], top_logp=top[1])
     return Scores(logp, entropy, *top)
 
@@ -100,9 +104,9 @@ class TokenUpdate:
             raise ValueError("ids: one token for each row of logits")
         listed = dict(teacher_ids=teacher[0], teacher_logp=teacher[1], kind=self.kind) if teacher is not None else {}
         terms = B.make_token_terms(temperature=temperature, ids=ids, **listed)
-        logp, entropy, dlogp, weight = (torch.empty(n, device=dev) for _ in range(4))
-        distill = torch.empty(n, device=dev) if teacher is not None else None
-        saved, objective, stats = torch.empty((n, B.TOKEN_SAVED), device=dev), torch.empty(1, device=dev), torch.empty(B.TOKEN_STATS, device=dev)
+        logp, entropy, dlogp, weight = (_empty(dev, n) for _ in range(4))
+        distill = _empty(dev, n) if teacher is not None else None
+        saved, objective, stats = _empty(dev, n, B.TOKEN_SAVED), _empty(dev, 1), _empty(dev, B.TOKEN_STATS)
         B.token_forward(logits, terms, logp=logp, entropy=entropy, distill=distill, saved=saved)
         dlogits = _gradient_room(logits) if dlogits is None else dlogits
         B.token_objective(start, logp, adv, objective, dlogp, self._space(B.token_objective_workspace_bytes(n)), logp_old=logp_old,

@@ -1,4 +1,4 @@
-"""Logits that are not one block of memory: slices of a padded vocabulary, rows that begin off 16 bytes, through the update driver."""
+"""Logits that are not one block of memory: slices of a padded vocabulary, rows that begin off 16 bytes, through the update driver; what it allocates."""
 import pytest
 import torch
 
@@ -35,3 +35,27 @@ def test_a_contiguous_batch_gets_a_contiguous_gradient():
     x = torch.randn((4, 1000), device="cuda").to(torch.bfloat16)
     u = TokenUpdate().step(x, torch.zeros(4, device="cuda", dtype=torch.int32), torch.tensor([0, 4], device="cuda", dtype=torch.int32), torch.ones(1, device="cuda"))
     assert u.dlogits.is_contiguous()
+
+
+@pytest.mark.parametrize("default", [torch.bfloat16, torch.float64])
+def test_the_driver_does_not_depend_on_torchs_default_type(default):
+    """Training programs set it to their weights' type; the calls' outputs are fp32 all the same."""
+    from paper_2512_15347_b200.token_update import TokenUpdate, score
+    x = torch.randn((5, 1000), device="cuda", dtype=torch.bfloat16)
+    start, adv = torch.tensor([0, 2, 5], device="cuda", dtype=torch.int32), torch.tensor([0.5, -1.0], device="cuda")
+
+    def steps():
+        lists = score(x, torch.arange(5, device="cuda", dtype=torch.int32), n_top=8)
+        u = TokenUpdate(entropy_coef=0.1, distill_coef=0.5, kind="reverse_rest").step(x, lists.top_ids[:, 1].contiguous(), start, adv, lists.logp[:, 0].contiguous(),
+                                                                                     teacher=(lists.top_ids, lists.top_logp))
+        return list(lists) + list(u)
+
+    want = steps()
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(default)
+    try:
+        got = steps()
+    finally:
+        torch.set_default_dtype(before)
+    for a, b in zip(got, want):
+        assert a.dtype == b.dtype and torch.equal(a, b)
