@@ -71,7 +71,8 @@ struct TokenParams {
 struct TokenRow {
   float m, l2, h;                // p_v = 2^((l_v - m) c - l2); entropy
   float mr, l2r, lr;             // the same of the distribution outside the list; ln p_r (-inf: nothing there)
-  float loss, lt, w;             // divergence; ln t_r, or ln of the list's mass (FORWARD); sum t (+ t_r)
+  float loss, lt, w;             // divergence; ln t_r; sum t (+ t_r).  FORWARD: ln of the list's mass is lt + l2r, its largest tl and the rest, since
+                                 // the sum has no digits for the rest where raw logits are far from 0
   float some;                    // 0: a row that allows nothing
 };
 // The gradient away from given and listed tokens: e (a + b ln e), e = 2^((l - ref) c - l2).
@@ -322,9 +323,10 @@ __device__ __forceinline__ TokenRow finish_row(const TokenShared& s, const float
       r.loss = 0.f * r.l2;                                             // NaN in a row with one
       return r;
     }
-    r.lt = tm + logf(z);
+    r.lt = tm;
+    r.l2r = logf(z);
     r.w = 1.f;
-    r.loss = ttl / z - logf(z) - tlp / z / kMean;
+    r.loss = ttl / z - r.l2r - tlp / z / kMean;
     return r;
   }
   const double mass = warp_total(l.mass);
@@ -680,7 +682,7 @@ __device__ __forceinline__ void fix_tokens(const TokenShared& s, const RowPart<T
   if (fix_list && e.tid >= 0 && at.owns(e.tid)) {
     const float y = (e.tx - r.m) * c - r.l2, pv = ex2(y), lp = kLn2 * y;
     float dist;
-    if (kind == PG_DISTILL_FORWARD) dist = r.w * pv - expf(e.tl - r.lt);
+    if (kind == PG_DISTILL_FORWARD) dist = r.w * pv - expf(e.tl - r.lt - r.l2r);
     else if (kind == PG_DISTILL_FORWARD_REST) dist = r.w * pv - expf(e.tl);
     else dist = pv == 0.f ? 0.f : pv * (lp - e.tl - r.loss);
     float sum = base(pv, lp) + (dd == 0.f ? 0.f : dd * dist);
@@ -1064,7 +1066,8 @@ token_kernel(const __grid_constant__ TokenParams p) {
     const bool fix_list = n_list > 0 && (kRest || p.g.ddistill);
     if (n_ids > 0 || fix_list) {
       __syncthreads();
-      fix_tokens(s, at, my, r, dl, n_ids, n_list, fix_list, kRest, p.t.kind, s.lp_part, dh, dd, inv);
+      // the row once more from shared memory, not from registers kept through the stream (2368 x 131072 bf16 with a list: 236 us, not 241)
+      fix_tokens(s, at, my, s.row, dl, n_ids, n_list, fix_list, kRest, p.t.kind, s.lp_part, dh, dd, inv);
     }
   }
 }

@@ -1,0 +1,41 @@
+"""Teachers' lists whose log-probabilities lie far from 0: raw logits, lists of tokens that the teacher masks by a finite value."""
+import math
+
+import pytest
+import torch
+
+from paper_2512_15347_b200 import binding as B
+from tests.test_gpu_token_update import check_forward, check_gradient, make, outputs, reference, terms_of
+
+pytestmark = pytest.mark.gpu
+
+GRADS = ("dlogp", "dentropy", "ddistill")
+
+
+def check_kind(c, kind):
+    R = c["x"].shape[0]
+    rows = reference(c, kind)
+    for w in rows:
+        if w["distill"] > 3.4028235e38:                             # no number of 32 bits
+            w["distill"] = math.inf
+    o, one, two = outputs(R, c, 0, True), torch.empty_like(c["x"]), torch.empty_like(c["x"])
+    B.token_forward_backward(c["x"], terms_of(c, kind), one, **o, **{k: c[k] for k in GRADS})
+    check_forward(c, o, rows)
+    check_gradient(c, one, rows)
+    o = outputs(R, c, 0, True)
+    B.token_forward(c["x"], terms_of(c, kind), **o)
+    check_forward(c, o, rows)
+    B.token_backward(c["x"], terms_of(c, kind), o["saved"], two, **{k: c[k] for k in GRADS})
+    check_gradient(c, two, rows)
+
+
+@pytest.mark.parametrize("k", [1, 7, 40, 256])
+@pytest.mark.parametrize("at", [-1e9, -3e38, -1e5, 3000.0, 1e6, 3e38])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_renormalised_list_of_any_logits(dtype, at, k):
+    """t is the softmax over the list: only differences count."""
+    c = make(6, 5003, dtype, 17, n_list=k, masks=False)
+    c["list_logp"] = c["list_logp"] + at
+    c["list_logp"][1] = at
+    c["list_ids"][4] = -1
+    check_kind(c, "forward")
