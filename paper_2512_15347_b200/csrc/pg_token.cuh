@@ -82,7 +82,7 @@ struct TokenSlope {
 
 // Sums over a warp's share of a teacher's list.  Reference of e: the largest logit m among them; of t: `tm` (FORWARD), else 0.
 struct ListSums {
-  float m, s0, s1, etl;                         // sum e, e y, e tl
+  float m, s0, s1, etl;                         // sum e, e y, kMean e tl
   float tm, ts, ttl, ty;                        // sum t, t (tl - tm), kMean t (l - m) / T
   double mass;                                  // sum t (the kinds with a bucket)
 };
@@ -349,7 +349,7 @@ __device__ __forceinline__ TokenRow finish_row(const TokenShared& s, const float
     plp = warp_total(plp);
     ptl = warp_total(ptl);
     const float pr = outside ? expf(r.lr) : 0.f;
-    r.loss = (kLn2 * plp - ptl) / s0 + (outside ? pr * (r.lr - r.lt) : 0.f);
+    r.loss = kLn2 * plp / s0 - ptl / s0 / kMean + (outside ? pr * (r.lr - r.lt) : 0.f);
   }
   return r;
 }
@@ -924,7 +924,7 @@ token_kernel(const __grid_constant__ TokenParams p) {
         const float y = (x - finite_ref(l.m)) * c, e = used ? ex2(y) : 0.f;
         l.s0 = warp_total(e);
         l.s1 = warp_total(e * fmaxf(y, kFloorY));
-        l.etl = warp_total(e != 0.f ? e * my.tl : 0.f);
+        l.etl = warp_total(e != 0.f ? kMean * e * my.tl : 0.f);
         l.tm = !kRest ? warp_most(used ? my.tl : -INFINITY) : 0.f;
         const float t = used ? expf(my.tl - finite_ref(l.tm)) : 0.f;
         l.ts = warp_total(t);

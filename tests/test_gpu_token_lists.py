@@ -39,3 +39,17 @@ def test_a_renormalised_list_of_any_logits(dtype, at, k):
     c["list_logp"][1] = at
     c["list_ids"][4] = -1
     check_kind(c, "forward")
+
+
+@pytest.mark.parametrize("k", [2, 40, 256])
+@pytest.mark.parametrize("kind", ["forward_rest", "reverse_rest"])
+@pytest.mark.parametrize("far", [-200.0, -1e9, -3e38])
+def test_lists_with_tokens_that_the_teacher_masks(far, kind, k):
+    """As a teacher's alternatives are where its mask leaves fewer tokens than the list has places.  In the reverse kind what the policy gives
+    such a token costs p_i |tl_i|: with a p_i of 1e-6 a number of 32 bits."""
+    c = make(6, 5003, torch.float32, 18, n_list=k, masks=False, peaks=0.0)
+    c["x"] *= 0.1
+    c["list_logp"][:, 1:] = far
+    c["list_logp"][0, : k // 2] = -3.0
+    c["ddistill"] = c["ddistill"].sign() * 0.25
+    check_kind(c, kind)
