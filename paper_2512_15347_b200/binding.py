@@ -737,6 +737,7 @@ def logits_process(logits, out, rules: LogitsRules, stream=None) -> None:
 # ---------------------------------------------------------------- policy update on token trajectories
 
 _FLOAT32 = torch.float32
+_MOST = 2 ** 31 - 1                   # ctypes cuts what passes 32 bits without a word
 
 
 def _f32(t, what: str, n: int, dev: int) -> int:
@@ -799,6 +800,8 @@ def _token_rows(t, terms: TokenTerms, what: str):
         raise ValueError(f"{what}: [rows, vocab], fp32, bf16 or fp16")
     rows, vocab = t.shape
     dev = t.get_device()
+    if rows > _MOST or vocab > _MOST:
+        raise ValueError(f"{what}: rows and vocabulary in 32 bits")
     at, on = terms._plain[:2]
     if dev < 0 or (on is not None and on != dev):
         raise ValueError(f"{what} and the terms: on one CUDA device")
@@ -895,6 +898,8 @@ def token_forward_backward(logits, terms: TokenTerms, dlogits, *, logp=None, lse
 
 
 def token_objective_workspace_bytes(n_tokens: int) -> int:
+    if n_tokens > _MOST:
+        raise ValueError("n_tokens: in 32 bits")
     return int(lib().pg_token_objective_workspace_bytes(n_tokens))
 
 
@@ -910,6 +915,8 @@ def token_objective(start, logp_new, adv, objective, dlogp, workspace, *, logp_o
     rows, n = start.numel() - 1, logp_new.numel()
     if rows < 0:
         raise ValueError("start: [rows + 1] int32")
+    if rows > _MOST or n > _MOST:
+        raise ValueError("rows and tokens: in 32 bits")
     if norm not in TOKEN_NORMS:
         raise ValueError(f"norm: one of {TOKEN_NORMS}")
     b = TokenBatch()

@@ -58,3 +58,23 @@ def test_a_cache_lets_go_of_its_pool(no_collector):
     cache.check()
     del cache
     assert torch.cuda.memory_allocated() == before
+
+
+def test_counts_beyond_32_bits_are_refused():
+    """They would be cut to 32 bits on the way to the library: a batch of 2^32 + 5 tokens to one of five."""
+    n = 2 ** 32 + 5
+    logits = torch.empty(n, device="cuda", dtype=torch.bfloat16)
+    one = torch.full((1,), 7.0, device="cuda")
+    for shape in ((1, n), (n, 1)):
+        with pytest.raises(ValueError):
+            B.token_forward(logits.view(shape), B.make_token_terms(), lse=one)
+    del logits
+    lp = torch.empty(n, device="cuda")
+    ws = torch.zeros(B.token_objective_workspace_bytes(5), device="cuda", dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        B.token_objective(torch.tensor([0, 5], device="cuda", dtype=torch.int32), lp, one, one.clone(), lp, ws)
+    with pytest.raises(ValueError):
+        B.token_objective_workspace_bytes(n)
+    assert float(one) == 7.0
+    del lp
+    torch.cuda.empty_cache()
