@@ -715,7 +715,7 @@ int pg_token_forward_backward(int32_t n_rows, int32_t vocab, int32_t dtype, cons
  *     w = scale / (n_rows * the row's tokens) | scale / all rows' tokens | scale     (PG_NORM_ROWS | _TOKENS | _SUM)
  * so that dentropy = weight, entropy_scale = entropy_coef, ddistill = weight, distill_scale = -distill_coef belong to it in
  * pg_token_backward.  Evaluated in fp64 from the fp32 inputs, sums in a fixed order.  Empty rows add nothing; tokens that
- * belong to no row get dlogp, weight 0 and ratio 1, and their inputs are not read.
+ * belong to no row get dlogp, weight 0 and ratio 1; their inputs, which may hold anything, are read but enter nothing.
  * stats: the weighted sums of surr, kl, entropy and distill, and the share of the rows' tokens that are clipped.
  * A term whose coefficient (beta, entropy_coef, distill_coef) is 0 is watched in stats and enters nothing else, whatever it is.
  */

@@ -56,7 +56,7 @@ __device__ __forceinline__ double exp_rest(double x, double* rest, double* less)
   }
   return y;
 }
-// 1 / n for a whole number n >= 1.
+// 1 / n for a whole number n >= 1: Newton's iteration r + r (1 - n r), from 2^-23 over 2^-46 to the last bits.
 __device__ __forceinline__ double reciprocal(int n) {
   double r = (double)__frcp_rn((float)n);
   r = fma(r, fma(-(double)n, r, 1.), r);

@@ -1,4 +1,5 @@
-// Units of eight logits: how they are read, converted and written by the kernels that stream rows of logits.
+// Units of eight logits: how the rules on logits read, convert and write them.  Of it the policy update on tokens uses pack2; its own units are
+// 16 bytes of any type.
 #pragma once
 
 #include "pg_kv.cuh"

@@ -170,3 +170,41 @@ def test_ratios_beyond_all_numbers(adv):
     for old, a in ((math.nan, adv), (-1.0, math.nan)):
         o = run([-1.0], a, logp_old=[old])
         assert math.isnan(o["objective"][0]) and math.isnan(o["dlogp"][0])
+
+
+def test_what_lies_between_the_rows_enters_nothing():
+    """Inputs of tokens of no row may hold anything."""
+    start = torch.tensor([2, 4, 4, 7], device="cuda", dtype=torch.int32)
+    adv = torch.tensor([1.0, -3.0, 0.5], device="cuda")
+    values = [-torch.rand(9, generator=torch.Generator(device="cuda").manual_seed(i), device="cuda") for i in range(5)]
+    outs = []
+    for bad in (0.0, math.nan, math.inf):
+        new, old, ref, ent, div = (v.clone() for v in values)
+        for v in (new, old, ref, ent, div):
+            v[:2], v[7:] = bad, bad
+        o = [torch.full((k,), 7.0, device="cuda") for k in (1, 9, 9, 9, B.TOKEN_STATS)]
+        ws = torch.zeros(B.token_objective_workspace_bytes(9), device="cuda", dtype=torch.uint8)
+        B.token_objective(start, new, adv, o[0], o[1], ws, logp_old=old, logp_ref=ref, entropy=ent, distill=div, beta=0.1, entropy_coef=0.1, distill_coef=0.1,
+                          weight=o[2], ratio=o[3], stats=o[4])
+        outs.append(o)
+        assert o[1][:2].tolist() == o[1][7:].tolist() == o[2][:2].tolist() == o[2][7:].tolist() == [0.0, 0.0]
+        assert o[3][:2].tolist() == o[3][7:].tolist() == [1.0, 1.0]
+    for o in outs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(o, outs[0]))
+
+
+@pytest.mark.parametrize("n", [3, 1021, 2 ** 24 - 1, 2 ** 24 + 1, 2 ** 25 - 1, 100000007, 2 ** 31 - 2 ** 20])
+def test_weights_of_long_rows(n):
+    """A row's tokens weigh 1 / n of it, up to the longest batch."""
+    lp = torch.zeros(n, device="cuda")
+    weight = torch.full((n,), 7.0, device="cuda")
+    J = torch.zeros(1, device="cuda")
+    ws = torch.zeros(B.token_objective_workspace_bytes(n), device="cuda", dtype=torch.uint8)
+    B.token_objective(torch.tensor([0, n], device="cuda", dtype=torch.int32), lp, torch.ones(1, device="cuda"), J, lp, ws, weight=weight)
+    near(float(weight[0]), 1 / n, n)
+    for part in (weight, lp):                               # the derivative over the log-probs themselves: A w = w
+        for a in range(0, n, 2 ** 28):
+            assert bool((part[a: a + 2 ** 28] == weight[0]).all())
+    near(float(J), 1.0, n, 1e-9)                            # n terms, added in 64 bits
+    del lp, weight
+    torch.cuda.empty_cache()
