@@ -16,13 +16,18 @@
 // Alternatives: bounds from the threads' largest logits leave few tiles of few threads to look at again; what passes is ranked by
 // counting.
 //
-// Measured (B200; share of the floor at the copy rate, calls back to back): 2368 x 131072 bf16 forward 101 us (94 %), with gradient
-// 219 us (87 %), with a list of 64 235 us, with a bucket besides 254 us; 2368 x 50001 fp16 48 us (75 %) and 91 us (79 %); 1024 x 131072
-// backward alone 86 us (95 %).  What is left: the join of a row, about 0.7 us in which its CTA asks for nothing, longer with a list (one
-// or two warps sum it, the others wait), and rows that are little longer than whole tiles.  Tried and left out: rows kept in the
-// registers or shared memory of clusters (the join of eight CTAs costs more than the second read: 343 and 302 us for 2048 x 131072,
-// not 209), CTAs that stay and ask for their next row ahead (220 us), bulk prefetches into the L2 cache (233 us), five CTAs an SM with
-// smaller tiles (225 to 234 us), listed tokens in a hash table instead of a byte for each unit (1251 x 65536 forward 45 us, not 41).
+// Masks: logits of -inf leave the sums by themselves.  Where the reference lies far from 0 (a finite mask, a small T) the product l c loses what the
+// difference l - m still has; sums take the difference first from kFar on, gradients see Slope2.
+//
+// Measured (B200; share of the floor at the copy rate, calls back to back, a token and the entropy of each row): 2368 x 131072 bf16 forward 96 us
+// (98 %), with gradient 224 us (85 %; without the entropy 217 us), distillation from a list of 64 232 us (82 %), with a bucket 246 us (77 %);
+// 2368 x 50001 fp16 50 us (73 %), 104 us (69 %; without 92 us), 101 us (72 %), 112 us (64 %); 2368 x 32000 fp32 52 us (90 %), 112 us (83 %), 121 us
+// (76 %), 126 us (74 %); 1024 x 131072 bf16 gradient alone 90 us (91 %).  What is left: the join of a row, about 0.7 us in which its CTA asks for
+// nothing, longer with a list (one or two warps sum it, the others wait), and rows that are little longer than whole tiles.
+// Tried and left out, against builds of their time in which a list's distillation over 2048 x 131072 took 209 to 237 us (203 us in this one): rows kept
+// in the registers or shared memory of clusters (the join of eight CTAs costs more than the second read: 343 and 302 us), CTAs that stay and
+// ask for their next row ahead (220 us), bulk prefetches into the L2 cache (233 us), five CTAs an SM with smaller tiles (225 to 234 us); listed
+// tokens in a hash table instead of a byte for each unit (1251 x 65536 forward 45 us, not 41).
 #pragma once
 
 #include "pg_kv.cuh"
@@ -35,11 +40,12 @@
 namespace pg {
 
 constexpr int kTokThreads = 256, kTokCtas = 4;  // of a CTA; CTAs of an SM, 64 registers a thread
-constexpr int kPartBytes = 128 * 1024;          // of a row that is read twice; 256 KB: 237 us, not 209 (2048 x 131072 bf16), 64 KB: 251 us
+constexpr int kPartBytes = 128 * 1024;          // of a row that is read twice; 2048 x 131072 bf16 with gradient 197 us, 256 KB: 225 us, 64 KB: 215 us
 constexpr int kOnChip = 2;                      // tiles of a part that stay on chip: one in registers, one in shared memory
-constexpr int kSavedBytes = 64 << 20;           // of the logits, which pg_token_backward meets first, wanted in the L2 cache with `saved`: both
-                                                // passes 1251 x 65536 bf16 92.5 us without; 64 MB 87.6 us, up to 2 us more at 32 or 96
-constexpr int kBackwardTiles = 2;               // of a CTA that only writes gradients: its row's numbers serve both (1: 69 us, not 65; 4: 72 us)
+constexpr int kSavedBytes = 64 << 20;           // of the logits, which pg_token_backward meets first, wanted in the L2 cache with `saved`: both passes
+                                                // over 1251 x 65536 bf16 86.0 us; none 89.3 us, 32 MB 87.7 us, 96 MB 87.3 us
+constexpr int kBackwardTiles = 2;               // of a CTA that only writes gradients, whose row's numbers serve both: 2368 x 50001 fp16 81 us (1: 90 us, 4: 87 us),
+                                                // both passes over 1251 x 65536 86 us (1: 90 us, 4: 88 us); 1024 x 131072 90 us (1: 86 us, 4: 94 us)
 constexpr int kTokWarps = kTokThreads / 32;
 constexpr int kMostParts = 8;                   // CTAs of a cluster
 constexpr int kCandidates = 1024;
@@ -571,7 +577,9 @@ struct Entry {
 // From |ref c| = 2^31 on (rows, or what is outside the list, masked throughout by a finite value; a small T) off could be 128 and the factor
 // out of range.  But there logits next to each other are 2^31 2^-24 = 128 apart in y, so e is 0 but for those equal to ref.  Any
 // other c that keeps them apart does as well: a power of two with |ref c| in [2^31, 2^32), whose product with ref is exact, and
-// y = 0 for those that are equal; their 2^-l2 is the factor.  (The difference first in a loop of its own: 8 % for every row with a bucket.)
+// y = 0 for those that are equal; their 2^-l2 is the factor.  Short of
+// 2^31 e carries 2^off, |off| <= 64, and shares below 2^-62 may come out as 0.  (The difference first, in a loop of its own, costs every row with
+// a bucket 8 %.)
 struct Slope2 {
   f2 c, nr, a, b;
   __device__ __forceinline__ Slope2(const TokenSlope& k, float c_) {
