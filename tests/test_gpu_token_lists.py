@@ -53,3 +53,20 @@ def test_lists_with_tokens_that_the_teacher_masks(far, kind, k):
     c["list_logp"][0, : k // 2] = -3.0
     c["ddistill"] = c["ddistill"].sign() * 0.25
     check_kind(c, kind)
+
+
+@pytest.mark.parametrize("k", [33, 64, 200])
+@pytest.mark.parametrize("low,high", [(-65504.0, 0.0), (-1e9, 0.0), (-3e38, 3e38)])
+def test_entries_of_no_weight_whose_tokens_the_policy_masks(low, high, k):
+    """Teacher and policy under one grammar: the tail of the teacher's list has t_i = 0, and its tokens are not allowed."""
+    c = make(6, 5003, torch.bfloat16, 19, n_list=k, masks=False)
+    c["list_logp"] += high
+    c["list_ids"][0, k // 2:] = c["list_ids"][1, k // 2: 2 * (k // 2) + k % 2]      # make leaves them out
+    for r in (0, 2, 5):
+        tail = c["list_ids"][r, 20:].long()
+        keep = ~torch.isin(tail, c["ids"][r].long()) & ~torch.isin(tail, c["list_ids"][r, :20].long())
+        c["list_logp"][r, 20:] = low
+        c["x"][r, tail[keep]] = -math.inf
+    rows = reference(c, "forward")
+    assert all(math.isfinite(w["distill"]) for w in rows)
+    check_kind(c, "forward")
