@@ -54,7 +54,7 @@ constexpr int kMostGroups = 1024;               // threads' tiles that are read 
 constexpr int kMergeBytes = kMostParts * PG_TOKEN_MAX_TOP * 8;
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr float kMean = 1.f / (2 * PG_TOKEN_MAX_LIST);   // of sums over a list whose mean is wanted: log-probs near the type's end, of masked tokens,
-                                                // do not pass it on the way
+                                                // do not pass it on the way.  A factor of these, not of weights, which may be next to 0
 constexpr float kFloorY = -1e4f;                // 2^y = 0 long before; keeps 0 * y from being NaN
 constexpr float kFar = 4194304.f;               // 2^22: below it m c is off by 1/8 at most; from there on (finite masks of any size, a
                                                 // small T) l - m is taken first, or 2^off would leave 32 bits
@@ -321,7 +321,7 @@ __device__ __forceinline__ TokenRow finish_row(const TokenShared& s, const float
       z = f * l.ts;
       if (f != 0.f) {                                                  // entries of no weight add nothing, whatever p_i is
         ttl = f * (l.ttl + l.ts * (l.tm - tm));
-        tlp = f * (l.ty + kMean * l.ts * (finite_ref(l.m) - r.m) * inv - kMean * l.ts * (kLn2 * r.l2));
+        tlp = f * (l.ty + l.ts * (kMean * (finite_ref(l.m) - r.m)) * inv - l.ts * (kMean * kLn2 * r.l2));
       }
     }
     z = warp_total(z);
@@ -343,7 +343,7 @@ __device__ __forceinline__ TokenRow finish_row(const TokenShared& s, const float
   r.w = (float)(outside ? mass + tr : mass);
   if (mass != mass) r.lt = r.w = NAN;
   if (kind == PG_DISTILL_FORWARD_REST) {
-    const float tlp = warp_total(l.ts != 0.f ? l.ty + kMean * l.ts * (finite_ref(l.m) - r.m) * inv - kMean * l.ts * (kLn2 * r.l2) : 0.f) / kMean;
+    const float tlp = warp_total(l.ts != 0.f ? l.ty + l.ts * (kMean * (finite_ref(l.m) - r.m)) * inv - l.ts * (kMean * kLn2 * r.l2) : 0.f) / kMean;
     r.loss = warp_total(l.ttl) - tlp + (outside ? r.lr > -1e30f ? (float)tr * (r.lt - r.lr) : (float)(tr * (r.lt - lr)) : 0.f);
   } else {
     float plp = 0.f, ptl = 0.f;
@@ -934,12 +934,12 @@ token_kernel(const __grid_constant__ TokenParams p) {
         const float y = (x - finite_ref(l.m)) * c, e = used ? ex2(y) : 0.f;
         l.s0 = warp_total(e);
         l.s1 = warp_total(e * fmaxf(y, kFloorY));
-        l.etl = warp_total(e != 0.f ? kMean * e * my.tl : 0.f);
+        l.etl = warp_total(e != 0.f ? e * (kMean * my.tl) : 0.f);
         l.tm = !kRest ? warp_most(used ? my.tl : -INFINITY) : 0.f;
         const float t = used ? expf(my.tl - finite_ref(l.tm)) : 0.f;
         l.ts = warp_total(t);
         l.ttl = warp_total(t != 0.f ? t * (my.tl - finite_ref(l.tm)) : 0.f);
-        l.ty = warp_total(t != 0.f ? kMean * t * (x - finite_ref(l.m)) * inv : 0.f);
+        l.ty = warp_total(t != 0.f ? t * (kMean * (x - finite_ref(l.m))) * inv : 0.f);
         l.mass = kRest ? warp_total(used ? exp((double)my.tl) : 0.) : 0.;
         if (lane == 0) s.list[warp] = l;
       }

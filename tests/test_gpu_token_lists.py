@@ -70,3 +70,18 @@ def test_entries_of_no_weight_whose_tokens_the_policy_masks(low, high, k):
     rows = reference(c, "forward")
     assert all(math.isfinite(w["distill"]) for w in rows)
     check_kind(c, "forward")
+
+
+@pytest.mark.parametrize("kind", ["forward", "forward_rest"])
+@pytest.mark.parametrize("low", [-86.0, -90.0, -99.0, -102.5])
+def test_entries_of_next_to_no_weight_whose_tokens_the_policy_masks(low, kind):
+    """t_i is next to 0, below the smallest normal number, but not 0: the divergence is infinite."""
+    c = make(3, 5003, torch.float32, 23, n_list=12, masks=False)
+    c["list_logp"][:, 0], c["list_logp"][:, 9:] = -0.01, low
+    tail = c["list_ids"][:, 10].long()
+    c["x"][torch.arange(3), tail] = -math.inf
+    rows = reference(c, kind)
+    o = outputs(3, c, 0, True)
+    B.token_forward(c["x"], terms_of(c, kind), **o)
+    assert [w["distill"] for w in rows] == [math.inf] * 3
+    assert o["distill"].tolist() == [math.inf] * 3
